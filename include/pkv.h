@@ -490,6 +490,111 @@ pkv_status pkv_get_rotation_schedule(int32_t page_size, uint8_t *members, int64_
 pkv_status pkv_get_row_block_ranges(int64_t n_row_blocks, int32_t longest_tokens, int32_t page_size, int32_t n_sms,
                                     int32_t *n_ranges);
 
+/*
+ * ---- A paged cache held directly in 4 bits --------------------------------------------------------------------
+ * The storage form the paper compares its factors with under quantization (Section 4.3: KV caches quantised directly),
+ * as a cache of its own: rows are quantised as they are written, read back on request, and attended over without being
+ * widened in memory.  Symmetric INT4 with one scale per group of g neighbouring channels of a row (one token, one KV
+ * head; K and V alike), the rule of this library's INT4 factors:
+ *     scale = bf16(max|x| / 7), at most 36.25 * 2^120;  code = round(x / scale), ties to even, in [-7, 7]  (0 if scale is 0)
+ * and the group stands for code * scale.  A group that holds an infinity or a NaN stands for NaN throughout.
+ *
+ * The caller keeps the bookkeeping, on the device, so that a captured CUDA graph stays valid while sequences grow, come
+ * and go:  page_table [device] int32 [n_seqs, max_pages], position t of sequence s lies in row t % page_size of physical
+ * page page_table[s, t / page_size];  lengths [device] int32 [n_seqs], T = tokens of each sequence.  Sequences may share
+ * pages for reading (a common prefix); a page that a call writes to belongs to one place of one sequence.  One cache can
+ * hold any number of layers: give each its own pages.
+ * Rows of a call: sequence s owns rows offsets[s] .. offsets[s + 1] - 1 of the caller's buffers (offsets [device] int32
+ * [n_seqs + 1], not decreasing, or NULL: n_rows / n_seqs rows each), n in all, and they are its LAST positions: row j of
+ * n has position T - n + j, with T counting these rows (so set lengths, then append, then attend, all with the same
+ * arrays).  n = 0 is fine.  Rows of the buffers before offsets[0] or from offsets[n_seqs] on belong to nobody: they are
+ * neither read nor written.
+ * Arrays are read when the kernels run.  Contents that make no sense never lead outside a buffer: a page number outside
+ * the pool (its tokens are skipped: not written, not read, not attended to), a length outside [0, max_pages *
+ * page_size] (held inside it) and rows beyond a sequence's start (skipped) are counted in pkv_q4_stats.
+ * Strides are in elements: row_stride from one row (token) to the next, head_stride from one head to the next, channels
+ * adjacent; multiples of 8, base addresses 16-byte aligned, rows and heads not overlapping (slices of a fused projection
+ * output can be passed as they are).
+ * Every call is asynchronous on `stream`, may be captured into a CUDA graph, and must be made with the cache's device
+ * current (PKV_ERR_INVALID_ARG otherwise).  The cache object keeps no scratch: calls on different streams may overlap as
+ * long as the caller orders writes of a page against its other uses and gives each attention call in flight a workspace
+ * of its own.  The object is not thread-safe.  Results are bit-identical from run to run.
+ * Dry-run mode as above: pool and meta NULL, calls only validate.
+ */
+typedef struct pkv_q4_cache pkv_q4_cache;
+
+#define PKV_DTYPE_BF16 0
+#define PKV_DTYPE_FP16 1
+
+typedef struct pkv_q4_config {
+    int32_t n_kv_heads;         /* 1 .. 1024 */
+    int32_t n_q_heads;          /* a multiple of n_kv_heads, at most 64 times it; query head h reads KV head h / (H_q/H_kv) */
+    int32_t head_dim;           /* d: 64 or 128 */
+    int32_t page_size;          /* P: 16, 32, 64, 128 or 256 */
+    int32_t group_size;         /* g: 32, 64 or 128 channels per scale, at most head_dim */
+    int32_t dtype;              /* of k, v, q and out: PKV_DTYPE_BF16 or PKV_DTYPE_FP16 */
+    int64_t n_pages;            /* pages in the pool */
+    float   softmax_scale;      /* 0 => 1/sqrt(head_dim) */
+    int32_t n_ctas;             /* most CTAs an attention over few query rows is spread over; 0 => two per SM */
+} pkv_q4_config;
+
+typedef struct pkv_q4_sizes {
+    int64_t page_bytes;         /* H_kv * P * (d + 4 d / g): 144 bytes per token and head at d = 128, g = 32 (bf16: 512) */
+    int64_t pool_bytes;         /* n_pages * page_bytes */
+    int64_t meta_bytes;
+} pkv_q4_sizes;
+
+typedef struct pkv_q4_stats {
+    int64_t device_timeouts;    /* bounded in-kernel waits that gave up (must be 0) */
+    int64_t bad_pages;          /* uses of page numbers outside the pool (skipped; must be 0) */
+    int64_t bad_lengths;        /* uses of lengths or offsets that make no sense (held inside their range; must be 0) */
+} pkv_q4_stats;
+
+pkv_status pkv_q4_query_sizes(const pkv_q4_config *cfg, pkv_q4_sizes *out);
+/* pool, meta [device]: 256-byte aligned; the pool's contents need not be initialised (meta is, synchronously). */
+pkv_status pkv_q4_init_cache(const pkv_q4_config *cfg, void *pool, void *meta, pkv_q4_cache **out);
+pkv_status pkv_q4_destroy_cache(pkv_q4_cache *c);
+const char *pkv_q4_last_error(const pkv_q4_cache *c);
+/* Counters; synchronises `stream`. */
+pkv_status pkv_q4_get_stats(pkv_q4_cache *c, pkv_q4_stats *out, void *stream);
+
+/* Quantises new rows into the cache: k, v [device] dtype [n_rows, H_kv, d]. */
+pkv_status pkv_q4_append_kv(pkv_q4_cache *c, int32_t n_seqs, const int32_t *page_table, int32_t max_pages,
+                            const int32_t *lengths, int64_t n_rows, const int32_t *offsets,
+                            const void *k, int64_t k_row_stride, int64_t k_head_stride,
+                            const void *v, int64_t v_row_stride, int64_t v_head_stride, void *stream);
+/* The reverse: the values code * scale of the sequences' last positions, rounded once to dtype, into k, v [device]
+ * [n_rows, H_kv, d].  n = T reads whole sequences.  Rows that a bad page or length concerns are left as they were. */
+pkv_status pkv_q4_read_kv(pkv_q4_cache *c, int32_t n_seqs, const int32_t *page_table, int32_t max_pages,
+                          const int32_t *lengths, int64_t n_rows, const int32_t *offsets,
+                          void *k, int64_t k_row_stride, int64_t k_head_stride,
+                          void *v, int64_t v_row_stride, int64_t v_head_stride, void *stream);
+
+/*
+ * Attention of the sequences' newest positions over the cache: the query of row j (of n) of a sequence with T tokens
+ * attends over positions 0 .. T - n + j, its own included (causal, as pkv_decode_attention_multi; n = 1 decodes).  A
+ * query that sees nothing (T = 0, or a position before the sequence's start) gets zeros.
+ *   q     [device] dtype [n_rows, H_q, d]
+ *   out   [device] dtype [n_rows, H_q, d], or NULL and instead
+ *   state [device] fp32 [n_rows, H_q, d + 2], contiguous: per query head o (d values, not divided by l), then m, then l,
+ *         as pkv_decode_attention_partial() writes them (with l = 0 for a query that sees nothing; m is a bound of the
+ *         scores in base-2 units, and o and l are relative to 2^m): pkv_merge_attention_states() merges such states with
+ *         those of other caches (recent tokens in a dense / factor cache, older ones here)
+ *   max_q_len   a host-side bound of n over the sequences (rows of a sequence beyond it are left as they were and counted
+ *               as bad lengths; 0: no sequence has rows); ignored without offsets
+ *   max_len     a host-side estimate of the longest T that only steers how the work is spread; 0 = max_pages * page_size
+ *   workspace   [device] pkv_q4_attention_workspace(n_seqs, max_q_len, max_len) bytes, 16-byte aligned; contents before
+ *               and after do not matter.  NULL where that is 0.
+ * Scores, softmax and sums are held in fp32; codes times scale enter the products exactly, the weights rounded to fp16.
+ */
+pkv_status pkv_q4_attention_workspace(const pkv_q4_cache *c, int32_t n_seqs, int32_t max_q_len, int32_t max_len,
+                                      int64_t *bytes);
+pkv_status pkv_q4_attention(pkv_q4_cache *c, int32_t n_seqs, const int32_t *page_table, int32_t max_pages,
+                            const int32_t *lengths, int64_t n_rows, const int32_t *offsets, int32_t max_q_len,
+                            int32_t max_len, const void *q, int64_t q_row_stride, int64_t q_head_stride,
+                            void *out, int64_t out_row_stride, int64_t out_head_stride, float *state,
+                            void *workspace, int64_t workspace_bytes, void *stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -1,0 +1,455 @@
+// Paged cache that holds keys and values in 4 bits: C ABI, and the kernels that quantise rows into the cache and read
+// them back.  The attention over it is in pkv_q4_attention.cu.
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+
+#include <cmath>
+#include <cstdarg>
+#include <cstdio>
+#include <new>
+
+#include "pkv_q4.h"
+
+using namespace pkv;
+
+namespace {
+
+// ---- kernels -------------------------------------------------------------------------------------------------------
+// Both copy kernels give a row of d channels (one token, one head, K or V) to d/8 lanes, eight channels each: a 16-byte
+// load or store per lane.  Bound by HBM (4 d bytes of 16-bit rows and d + 4 d/g bytes of cache per token and head).
+constexpr int kCopyThreads = 256;
+
+struct RowPlace { int ok, t; long long off; };      // token within its tile; byte offset of the head-0 tile in the pool
+
+// Where row i of a call lies: its sequence, its position, the page that holds it.
+__device__ __forceinline__ RowPlace place_of(const Q4Rows &r, const Q4Geometry &g, int i, int *status) {
+    int s, end;
+    if (!r.offsets) {
+        s = i / r.per_seq;
+        end = (s + 1) * r.per_seq;
+        if (s >= r.n_seqs) return RowPlace{0, 0, 0};
+    } else {
+        int lo = 0, hi = r.n_seqs;                  // the last s with offsets[s] <= i
+        while (hi - lo > 1) {
+            const int mid = (lo + hi) >> 1;
+            if (__ldg(r.offsets + mid) <= i) lo = mid;
+            else hi = mid;
+        }
+        s = lo;
+        end = min(__ldg(r.offsets + s + 1), (int)r.n_rows);
+        if (i < __ldg(r.offsets + s) || i >= end) return RowPlace{0, 0, 0};          // rows before or behind the sequences
+    }
+    const int pos = q4_length(r, g, s, status) - (end - i);
+    if (pos < 0) {                                  // more new rows than the sequence is long
+        if (status) atomicAdd(status + 2, 1);
+        return RowPlace{0, 0, 0};
+    }
+    const int page = __ldg(r.table + (long long)s * r.max_pages + (pos >> g.page_shift));
+    if (page < 0 || page >= g.n_pages) {
+        if (status) atomicAdd(status + 1, 1);
+        return RowPlace{0, 0, 0};
+    }
+    const int in_page = pos & (g.page - 1);
+    return RowPlace{1, in_page & (kQ4Tile - 1), page * g.page_bytes + (long long)(in_page / kQ4Tile) * g.tile_bytes};
+}
+
+template <bool H16>
+__device__ __forceinline__ void unpack8(const uint4 &w, float *x) {
+    const uint32_t u[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        if (H16) {
+            const float2 f = __half22float2(*reinterpret_cast<const __half2 *>(&u[i]));
+            x[2 * i] = f.x; x[2 * i + 1] = f.y;
+        } else {
+            x[2 * i] = __uint_as_float(u[i] << 16); x[2 * i + 1] = __uint_as_float(u[i] & 0xffff0000u);
+        }
+    }
+}
+
+// Codes (+ 8) of eight values of a group with scale s (a bf16 value >= 0), as integers 1..15.
+// The quotient decides between neighbouring codes, and x / s may lie exactly on a border (both have few bits): a plain
+// x * (1/s) would land beside it.  x has 11 significant bits at most and s eight, so a quotient up to 7.5 that is not on a
+// border is at least 2^-14 away from it; rounding x * (1/s) (off by less than 2^-18) to a multiple of 2^-16 first -
+// adding and taking away 192 - therefore gives the border itself where the true quotient is on it and keeps the side
+// everywhere else, and the rounding to an integer then takes ties to even like the division would.
+__device__ __forceinline__ void codes8(const float *x, float s, uint32_t *u) {
+    // scales below 2^-64 (some are subnormal bf16 numbers, whose reciprocal overflows): both sides times 2^64
+    const float f = s < 5.4210109e-20f ? 1.8446744e19f : 1.f;
+    const float inv = s > 0.f ? __frcp_rn(s * f) : 0.f;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        float q = __fmul_rn(__fmul_rn(x[i], f), inv);
+        q = __fadd_rn(__fadd_rn(q, 192.f), -192.f);
+        q = fminf(fmaxf(q, -7.f), 7.f);             // (7.03 after a scale rounded down; more only for subnormal scales)
+        u[i] = __float_as_uint(__fadd_rn(q, 12582912.f + 8.f)) & 15u;
+    }
+}
+
+// (the scale's clamp: 7 * scale has to be finite in bf16; bf16(max / 7) of the type's two largest values is not)
+constexpr float kScaleMost = 4.8183102e37f;          // 36.25 * 2^120
+
+template <int D, int NG, bool H16>
+__global__ void __launch_bounds__(kCopyThreads) q4_append_kernel(const __grid_constant__ Q4CopyArgs a) {
+    constexpr int LR = D / 8, GL = LR / NG;          // lanes per row, lanes per group
+    const Q4Geometry &geo = a.geo;
+    const int H = geo.n_kv_heads, jobs_per_row = 2 * H;
+    const long long n_jobs = a.rows.n_rows * jobs_per_row;
+    const int lane = threadIdx.x & 31, l = lane % LR, j = l >> 2, c = l & 3;
+    const long long first = ((long long)blockIdx.x * kCopyThreads + threadIdx.x) / LR, step = (long long)gridDim.x * kCopyThreads / LR;
+    const long long warp_first = ((long long)blockIdx.x * kCopyThreads + (threadIdx.x & ~31)) / LR;
+    for (long long base = 0; warp_first + base < n_jobs; base += step) {
+        const long long job = first + base;
+        const bool in = job < n_jobs;
+        const int i = in ? (int)(job / jobs_per_row) : 0, x = in ? (int)(job - (long long)i * jobs_per_row) : 0;
+        const int is_v = x >= H, h = is_v ? x - H : x;
+        const unsigned short *src = reinterpret_cast<const unsigned short *>(is_v ? a.v : a.k) +
+                                    (is_v ? i * a.v_row + h * a.v_head : i * a.k_row + h * a.k_head);
+        const uint4 raw = in ? __ldg(reinterpret_cast<const uint4 *>(src) + l) : make_uint4(0u, 0u, 0u, 0u);
+        const RowPlace at = in ? place_of(a.rows, geo, i, x == 0 && l == 0 ? a.status : nullptr) : RowPlace{0, 0, 0};
+        // largest magnitude of the group, as bits: non-negative 16-bit floats order like integers, infinities and NaN last
+        uint32_t mx = __vmaxu2(__vmaxu2(raw.x & 0x7fff7fffu, raw.y & 0x7fff7fffu), __vmaxu2(raw.z & 0x7fff7fffu, raw.w & 0x7fff7fffu));
+        mx = max(mx & 0xffffu, mx >> 16);
+#pragma unroll
+        for (int d = 1; d < GL; d <<= 1) mx = max(mx, __shfl_xor_sync(0xffffffffu, mx, d));
+        const bool finite = mx < (H16 ? 0x7c00u : 0x7f80u);
+        const float amax = H16 ? __half2float(__ushort_as_half((unsigned short)mx)) : __uint_as_float(mx << 16);
+        const __nv_bfloat16 sb = __float2bfloat16_rn(fminf(__fdiv_rn(amax, 7.f), kScaleMost));
+        float v[8];
+        uint32_t u[8];
+        unpack8<H16>(raw, v);
+        codes8(v, __bfloat162float(sb), u);
+        uint32_t w = 0;
+        if (is_v) {
+#pragma unroll
+            for (int n = 0; n < 8; ++n) w |= u[n] << (4 * n);
+        } else {
+#pragma unroll
+            for (int n = 0; n < 4; ++n) w |= u[2 * n] << (4 * n) | u[2 * n + 1] << (4 * n + 16);
+        }
+        if (!finite) w = 0x88888888u;                // the group reads as NaN: zero codes, and a NaN for a scale
+        const uint32_t other = __shfl_xor_sync(0xffffffffu, w, 4);
+        if (!at.ok) continue;
+        unsigned char *tile = a.pool + at.off + (long long)h * geo.head_bytes;
+        if (is_v) {
+            // lanes j and j ^ 1 hold chunks 2c and 2c + 1 of 32-channel words j and j ^ 1: each stores one chunk's two words
+            const uint32_t two = j & 1 ? __byte_perm(other, w, 0x7632) : __byte_perm(w, other, 0x5410);
+            *reinterpret_cast<uint32_t *>(tile + q4_v_base(D) + q4_v_chunk(D, at.t, 2 * c + (j & 1)) + (j >> 1) * 4) = two;
+        } else {
+            *reinterpret_cast<uint32_t *>(tile + q4_k_chunk(D, at.t, c) + j * 4) = w;
+        }
+        if (l % GL == 0)
+            *reinterpret_cast<unsigned short *>(tile + (is_v ? q4_vs_base(D, NG) : q4_ks_base(D)) + (at.t * NG + l / GL) * 2) =
+                finite ? __bfloat16_as_ushort(sb) : (unsigned short)0x7fc0u;
+    }
+}
+
+template <int D, int NG, bool H16>
+__global__ void __launch_bounds__(kCopyThreads) q4_read_kernel(const __grid_constant__ Q4CopyArgs a) {
+    constexpr int LR = D / 8, GL = LR / NG;
+    const Q4Geometry &geo = a.geo;
+    const int H = geo.n_kv_heads, jobs_per_row = 2 * H;
+    const long long n_jobs = a.rows.n_rows * jobs_per_row;
+    const int lane = threadIdx.x & 31, l = lane % LR, j = l >> 2, c = l & 3;
+    const long long first = ((long long)blockIdx.x * kCopyThreads + threadIdx.x) / LR, step = (long long)gridDim.x * kCopyThreads / LR;
+    const long long warp_first = ((long long)blockIdx.x * kCopyThreads + (threadIdx.x & ~31)) / LR;
+    for (long long base = 0; warp_first + base < n_jobs; base += step) {
+        const long long job = first + base;
+        const bool in = job < n_jobs;
+        const int i = in ? (int)(job / jobs_per_row) : 0, x = in ? (int)(job - (long long)i * jobs_per_row) : 0;
+        const int is_v = x >= H, h = is_v ? x - H : x;
+        const RowPlace at = in ? place_of(a.rows, geo, i, x == 0 && l == 0 ? a.status : nullptr) : RowPlace{0, 0, 0};
+        uint32_t w = 0;
+        float s = 0.f;
+        if (at.ok) {
+            const unsigned char *tile = a.pool + at.off + (long long)h * geo.head_bytes;
+            w = *reinterpret_cast<const uint32_t *>(tile + (is_v ? q4_v_base(D) + q4_v_chunk(D, at.t, 2 * c + (j & 1)) + (j >> 1) * 4
+                                                                 : q4_k_chunk(D, at.t, c) + j * 4));
+            s = __uint_as_float((uint32_t)*reinterpret_cast<const unsigned short *>(
+                                    tile + (is_v ? q4_vs_base(D, NG) : q4_ks_base(D)) + (at.t * NG + l / GL) * 2) << 16);
+        }
+        const uint32_t other = __shfl_xor_sync(0xffffffffu, w, 4);
+        if (!at.ok) continue;
+        if (is_v) w = j & 1 ? __byte_perm(other, w, 0x7632) : __byte_perm(w, other, 0x5410);
+        uint32_t o[4];
+#pragma unroll
+        for (int p = 0; p < 4; ++p) {
+            const int n0 = is_v ? 8 * p : 4 * p, n1 = is_v ? 8 * p + 4 : 4 * p + 16;
+            const float lo = (float)((int)((w >> n0) & 15u) - 8) * s, hi = (float)((int)((w >> n1) & 15u) - 8) * s;
+            if (H16) {
+                const __half2 t = __floats2half2_rn(lo, hi);
+                o[p] = *reinterpret_cast<const uint32_t *>(&t);
+            } else {
+                const __nv_bfloat162 t = __floats2bfloat162_rn(lo, hi);
+                o[p] = *reinterpret_cast<const uint32_t *>(&t);
+            }
+        }
+        unsigned short *dst = reinterpret_cast<unsigned short *>(is_v ? a.v : a.k) +
+                              (is_v ? i * a.v_row + h * a.v_head : i * a.k_row + h * a.k_head);
+        reinterpret_cast<uint4 *>(dst)[l] = make_uint4(o[0], o[1], o[2], o[3]);
+    }
+}
+
+template <bool kWrite>
+cudaError_t launch_copy(const Q4CopyArgs &a, cudaStream_t st) {
+    const Q4Geometry &g = a.geo;
+    const long long jobs = a.rows.n_rows * 2 * g.n_kv_heads;
+    if (jobs <= 0) return cudaSuccess;
+    const int per_cta = kCopyThreads / (g.head_dim / 8);
+    const long long want = (jobs + per_cta - 1) / per_cta, most = 8LL * g.n_sms;
+    const unsigned grid = (unsigned)(want < most ? want : most);
+#define PKV_Q4_COPY(D, NG)                                                                                           \
+    if (g.head_dim == D && g.groups == NG) {                                                                         \
+        if (g.fp16) { if (kWrite) q4_append_kernel<D, NG, true><<<grid, kCopyThreads, 0, st>>>(a);                   \
+                      else q4_read_kernel<D, NG, true><<<grid, kCopyThreads, 0, st>>>(a); }                          \
+        else { if (kWrite) q4_append_kernel<D, NG, false><<<grid, kCopyThreads, 0, st>>>(a);                         \
+               else q4_read_kernel<D, NG, false><<<grid, kCopyThreads, 0, st>>>(a); }                                \
+        return cudaGetLastError();                                                                                   \
+    }
+    PKV_Q4_COPY(128, 4) PKV_Q4_COPY(128, 2) PKV_Q4_COPY(128, 1) PKV_Q4_COPY(64, 2) PKV_Q4_COPY(64, 1)
+#undef PKV_Q4_COPY
+    return cudaErrorInvalidValue;
+}
+
+}  // namespace
+
+namespace pkv {
+cudaError_t launch_q4_append(const Q4CopyArgs &a, cudaStream_t st) { return launch_copy<true>(a, st); }
+cudaError_t launch_q4_read(const Q4CopyArgs &a, cudaStream_t st) { return launch_copy<false>(a, st); }
+}  // namespace pkv
+
+// ---- host side -----------------------------------------------------------------------------------------------------
+struct pkv_q4_cache {
+    pkv_q4_config cfg;
+    Q4Geometry geo;
+    bool dry;
+    int device;
+    unsigned char *pool;
+    int *status;
+    char err[256];
+};
+
+namespace {
+
+pkv_status q4_fail(pkv_q4_cache *c, pkv_status code, const char *fmt, ...) {
+    if (c) {
+        va_list ap;
+        va_start(ap, fmt);
+        vsnprintf(c->err, sizeof c->err, fmt, ap);
+        va_end(ap);
+    }
+    return code;
+}
+
+pkv_status q4_validate(const pkv_q4_config *cfg, Q4Geometry *g) {
+    if (!cfg) return PKV_ERR_INVALID_ARG;
+    if (cfg->n_kv_heads <= 0 || cfg->n_q_heads <= 0 || cfg->n_pages <= 0 || cfg->n_ctas < 0 || cfg->n_ctas > 65535 ||
+        cfg->n_q_heads % cfg->n_kv_heads != 0 || !std::isfinite(cfg->softmax_scale) || cfg->softmax_scale < 0)
+        return PKV_ERR_INVALID_ARG;
+    if ((cfg->head_dim != 64 && cfg->head_dim != 128) ||
+        (cfg->group_size != 32 && cfg->group_size != 64 && cfg->group_size != 128) || cfg->group_size > cfg->head_dim ||
+        cfg->page_size < kQ4Tile || cfg->page_size > 256 || (cfg->page_size & (cfg->page_size - 1)) ||
+        (cfg->dtype != PKV_DTYPE_BF16 && cfg->dtype != PKV_DTYPE_FP16) || cfg->n_kv_heads > 1024 ||
+        cfg->n_q_heads / cfg->n_kv_heads > 64 || cfg->n_pages > 0x7fffffffLL)
+        return PKV_ERR_UNSUPPORTED;
+    *g = Q4Geometry{};
+    g->n_kv_heads = cfg->n_kv_heads;
+    g->n_q_heads = cfg->n_q_heads;
+    g->group = cfg->n_q_heads / cfg->n_kv_heads;
+    g->head_dim = cfg->head_dim;
+    g->page = cfg->page_size;
+    for (g->page_shift = 0; (1 << g->page_shift) < g->page;) ++g->page_shift;
+    g->groups = cfg->head_dim / cfg->group_size;
+    g->tile_bytes = kQ4Tile * (cfg->head_dim + 4 * g->groups);
+    g->head_bytes = g->page / kQ4Tile * g->tile_bytes;
+    g->fp16 = cfg->dtype == PKV_DTYPE_FP16;
+    g->page_bytes = (long long)g->n_kv_heads * g->head_bytes;
+    g->n_pages = cfg->n_pages;
+    if (g->n_pages > (1LL << 60) / g->page_bytes) return PKV_ERR_INVALID_ARG;
+    const float scale = cfg->softmax_scale > 0 ? cfg->softmax_scale : 1.f / std::sqrt((float)cfg->head_dim);
+    g->scale_log2e = scale * 1.4426950408889634f;
+    return PKV_OK;
+}
+
+// What append, read and attention have in common: the sequences, and the rows that belong to them.
+pkv_status q4_rows(pkv_q4_cache *c, const char *what, int32_t n_seqs, const int32_t *table, int32_t max_pages,
+                   const int32_t *lengths, int64_t n_rows, const int32_t *offsets, Q4Rows *r) {
+    if (n_seqs < 1 || n_seqs > 65535) return q4_fail(c, PKV_ERR_INVALID_ARG, "%s: n_seqs %d out of range", what, n_seqs);
+    if (max_pages < 1 || max_pages > (0x7fffffff >> c->geo.page_shift))
+        return q4_fail(c, PKV_ERR_INVALID_ARG, "%s: max_pages %d out of range", what, max_pages);
+    if (n_rows < 0 || n_rows > 0x7fffffff / (2 * c->geo.n_q_heads))
+        return q4_fail(c, PKV_ERR_INVALID_ARG, "%s: n_rows %lld out of range", what, (long long)n_rows);
+    if (!offsets && n_rows % n_seqs != 0)
+        return q4_fail(c, PKV_ERR_INVALID_ARG, "%s: %lld rows do not divide among %d sequences (give offsets)", what, (long long)n_rows, n_seqs);
+    if (!c->dry && (!table || !lengths)) return q4_fail(c, PKV_ERR_INVALID_ARG, "%s: page_table or lengths is NULL", what);
+    if (((uintptr_t)table | (uintptr_t)lengths | (uintptr_t)offsets) & 3)
+        return q4_fail(c, PKV_ERR_INVALID_ARG, "%s: page_table, lengths and offsets must be 4-byte aligned", what);
+    *r = Q4Rows{table, lengths, offsets, n_seqs, max_pages, offsets ? 0 : (int)(n_rows / n_seqs), n_rows};
+    return PKV_OK;
+}
+
+pkv_status q4_device(pkv_q4_cache *c, const char *what) {
+    int dev = -1;
+    const cudaError_t e = cudaGetDevice(&dev);
+    if (e != cudaSuccess) return q4_fail(c, PKV_ERR_CUDA, "%s: %s", what, cudaGetErrorString(e));
+    if (dev != c->device) return q4_fail(c, PKV_ERR_INVALID_ARG, "%s: the cache is on device %d, the current device is %d", what, c->device, dev);
+    return PKV_OK;
+}
+
+// strides of a [rows, heads, d] buffer in elements: rows and heads on 16-byte boundaries, heads apart from one another
+bool q4_strides(const void *p, int64_t row, int64_t head, int d, int heads, int64_t n_rows) {
+    if (((uintptr_t)p & 15) || row % 8 || head % 8 || row < 0 || head < 0) return false;
+    if (row > (1LL << 31) || head > (1LL << 31)) return false;
+    return (heads == 1 || head >= d) && (n_rows <= 1 || row >= d);
+}
+
+pkv_status q4_copy(pkv_q4_cache *c, bool write, int32_t n_seqs, const int32_t *table, int32_t max_pages, const int32_t *lengths,
+                   int64_t n_rows, const int32_t *offsets, void *k, int64_t k_row, int64_t k_head, void *v, int64_t v_row,
+                   int64_t v_head, void *stream) {
+    if (!c) return PKV_ERR_INVALID_ARG;
+    const char *what = write ? "pkv_q4_append_kv" : "pkv_q4_read_kv";
+    Q4CopyArgs a{};
+    if (pkv_status st = q4_rows(c, what, n_seqs, table, max_pages, lengths, n_rows, offsets, &a.rows)) return st;
+    const Q4Geometry &g = c->geo;
+    if (!c->dry && n_rows > 0 && (!k || !v)) return q4_fail(c, PKV_ERR_INVALID_ARG, "%s: k or v is NULL", what);
+    if (!q4_strides(k, k_row, k_head, g.head_dim, g.n_kv_heads, n_rows) || !q4_strides(v, v_row, v_head, g.head_dim, g.n_kv_heads, n_rows))
+        return q4_fail(c, PKV_ERR_INVALID_ARG, "%s: k and v need 16-byte aligned rows: strides that are multiples of 8 elements, rows and "
+                                               "heads at least head_dim apart", what);
+    if (c->dry || n_rows == 0) return PKV_OK;
+    if (pkv_status st = q4_device(c, what)) return st;
+    a.geo = g;
+    a.pool = c->pool;
+    a.k = k; a.v = v;
+    a.k_row = k_row; a.k_head = k_head; a.v_row = v_row; a.v_head = v_head;
+    a.status = c->status;
+    const cudaError_t e = write ? launch_q4_append(a, (cudaStream_t)stream) : launch_q4_read(a, (cudaStream_t)stream);
+    if (e != cudaSuccess) return q4_fail(c, PKV_ERR_CUDA, "%s: %s", what, cudaGetErrorString(e));
+    return PKV_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+pkv_status pkv_q4_query_sizes(const pkv_q4_config *cfg, pkv_q4_sizes *out) {
+    if (!out) return PKV_ERR_INVALID_ARG;
+    Q4Geometry g;
+    if (pkv_status st = q4_validate(cfg, &g)) return st;
+    out->page_bytes = g.page_bytes;
+    out->pool_bytes = g.page_bytes * g.n_pages;
+    out->meta_bytes = 256;
+    return PKV_OK;
+}
+
+pkv_status pkv_q4_init_cache(const pkv_q4_config *cfg, void *pool, void *meta, pkv_q4_cache **out) {
+    if (!out) return PKV_ERR_INVALID_ARG;
+    *out = nullptr;
+    Q4Geometry g;
+    if (pkv_status st = q4_validate(cfg, &g)) return st;
+    const bool dry = !pool && !meta;
+    if (!dry && (!pool || !meta || (((uintptr_t)pool | (uintptr_t)meta) & 255))) return PKV_ERR_INVALID_ARG;
+    pkv_q4_cache *c = new (std::nothrow) pkv_q4_cache();
+    if (!c) return PKV_ERR_INVALID_ARG;
+    c->cfg = *cfg;
+    c->dry = dry;
+    c->pool = static_cast<unsigned char *>(pool);
+    c->status = static_cast<int *>(meta);
+    c->err[0] = 0;
+    g.n_sms = 148;
+    if (!dry) {
+        cudaError_t e = cudaGetDevice(&c->device);
+        if (e == cudaSuccess) e = cudaDeviceGetAttribute(&g.n_sms, cudaDevAttrMultiProcessorCount, c->device);
+        if (e == cudaSuccess) e = q4_attention_setup();
+        if (e == cudaSuccess) e = cudaMemset(meta, 0, 256);
+        if (e != cudaSuccess) { delete c; return PKV_ERR_CUDA; }
+    }
+    g.n_ctas = cfg->n_ctas > 0 ? cfg->n_ctas : 2 * g.n_sms;
+    c->geo = g;
+    *out = c;
+    return PKV_OK;
+}
+
+pkv_status pkv_q4_destroy_cache(pkv_q4_cache *c) {
+    if (!c) return PKV_ERR_INVALID_ARG;
+    delete c;
+    return PKV_OK;
+}
+
+const char *pkv_q4_last_error(const pkv_q4_cache *c) { return c ? c->err : "cache is NULL"; }
+
+pkv_status pkv_q4_append_kv(pkv_q4_cache *c, int32_t n_seqs, const int32_t *page_table, int32_t max_pages, const int32_t *lengths,
+                            int64_t n_rows, const int32_t *offsets, const void *k, int64_t k_row_stride, int64_t k_head_stride,
+                            const void *v, int64_t v_row_stride, int64_t v_head_stride, void *stream) {
+    return q4_copy(c, true, n_seqs, page_table, max_pages, lengths, n_rows, offsets, const_cast<void *>(k), k_row_stride, k_head_stride,
+                   const_cast<void *>(v), v_row_stride, v_head_stride, stream);
+}
+
+pkv_status pkv_q4_read_kv(pkv_q4_cache *c, int32_t n_seqs, const int32_t *page_table, int32_t max_pages, const int32_t *lengths,
+                          int64_t n_rows, const int32_t *offsets, void *k, int64_t k_row_stride, int64_t k_head_stride, void *v,
+                          int64_t v_row_stride, int64_t v_head_stride, void *stream) {
+    return q4_copy(c, false, n_seqs, page_table, max_pages, lengths, n_rows, offsets, k, k_row_stride, k_head_stride, v, v_row_stride,
+                   v_head_stride, stream);
+}
+
+pkv_status pkv_q4_attention_workspace(const pkv_q4_cache *c, int32_t n_seqs, int32_t max_q_len, int32_t max_len, int64_t *bytes) {
+    if (!c || !bytes || n_seqs < 1 || n_seqs > 65535 || max_q_len < 1 || max_len < 1) return PKV_ERR_INVALID_ARG;
+    *bytes = q4_attention_workspace(c->geo, n_seqs, max_q_len, max_len);
+    return PKV_OK;
+}
+
+pkv_status pkv_q4_attention(pkv_q4_cache *c, int32_t n_seqs, const int32_t *page_table, int32_t max_pages, const int32_t *lengths,
+                            int64_t n_rows, const int32_t *offsets, int32_t max_q_len, int32_t max_len, const void *q,
+                            int64_t q_row_stride, int64_t q_head_stride, void *out, int64_t out_row_stride, int64_t out_head_stride,
+                            float *state, void *workspace, int64_t workspace_bytes, void *stream) {
+    if (!c) return PKV_ERR_INVALID_ARG;
+    const char *what = "pkv_q4_attention";
+    Q4AttentionArgs a{};
+    if (pkv_status st = q4_rows(c, what, n_seqs, page_table, max_pages, lengths, n_rows, offsets, &a.rows)) return st;
+    const Q4Geometry &g = c->geo;
+    const int capacity = max_pages << g.page_shift;
+    if (!offsets) max_q_len = a.rows.per_seq;
+    if (n_rows > 0 && (max_q_len < 0 || max_q_len > n_rows)) return q4_fail(c, PKV_ERR_INVALID_ARG, "%s: max_q_len %d out of range", what, max_q_len);
+    if (max_len < 0) return q4_fail(c, PKV_ERR_INVALID_ARG, "%s: max_len %d out of range", what, max_len);
+    if (max_len == 0 || max_len > capacity) max_len = capacity;
+    if (!c->dry && n_rows > 0 && (!q || (!out == !state)))
+        return q4_fail(c, PKV_ERR_INVALID_ARG, "%s: q is NULL, or not exactly one of out and state is given", what);
+    if (!q4_strides(q, q_row_stride, q_head_stride, g.head_dim, g.n_q_heads, n_rows) ||
+        (out && !q4_strides(out, out_row_stride, out_head_stride, g.head_dim, g.n_q_heads, n_rows)))
+        return q4_fail(c, PKV_ERR_INVALID_ARG, "%s: q and out need 16-byte aligned rows: strides that are multiples of 8 elements, rows and "
+                                               "heads at least head_dim apart", what);
+    if ((uintptr_t)state & 7) return q4_fail(c, PKV_ERR_INVALID_ARG, "%s: state must be 8-byte aligned", what);
+    if (n_rows == 0 || max_q_len == 0) return PKV_OK;
+    const long long need = q4_attention_workspace(g, n_seqs, max_q_len, max_len);
+    if (!c->dry && need > 0 && (!workspace || workspace_bytes < need || ((uintptr_t)workspace & 15)))
+        return q4_fail(c, PKV_ERR_INVALID_ARG, "%s: the workspace needs %lld bytes, 16-byte aligned", what, need);
+    if (c->dry) return PKV_OK;
+    if (pkv_status st = q4_device(c, what)) return st;
+    a.geo = g;
+    a.pool = c->pool;
+    a.q = q; a.out = out; a.state = state;
+    a.q_row = q_row_stride; a.q_head = q_head_stride; a.out_row = out_row_stride; a.out_head = out_head_stride;
+    a.max_q_len = max_q_len;
+    a.max_len = max_len;
+    a.workspace = static_cast<unsigned char *>(workspace);
+    a.status = c->status;
+    const cudaError_t e = launch_q4_attention(a, (cudaStream_t)stream);
+    if (e != cudaSuccess) return q4_fail(c, PKV_ERR_CUDA, "%s: %s", what, cudaGetErrorString(e));
+    return PKV_OK;
+}
+
+pkv_status pkv_q4_get_stats(pkv_q4_cache *c, pkv_q4_stats *out, void *stream) {
+    if (!c || !out) return PKV_ERR_INVALID_ARG;
+    int words[kQ4StatusWords] = {};
+    if (!c->dry) {
+        if (pkv_status st = q4_device(c, "pkv_q4_get_stats")) return st;
+        cudaError_t e = cudaMemcpyAsync(words, c->status, sizeof words, cudaMemcpyDeviceToHost, (cudaStream_t)stream);
+        if (e == cudaSuccess) e = cudaStreamSynchronize((cudaStream_t)stream);
+        if (e != cudaSuccess) return q4_fail(c, PKV_ERR_CUDA, "pkv_q4_get_stats: %s", cudaGetErrorString(e));
+    }
+    out->device_timeouts = words[0];
+    out->bad_pages = words[1];
+    out->bad_lengths = words[2];
+    return PKV_OK;
+}
+
+}  // extern "C"

@@ -32,6 +32,8 @@ EXPORTS = [
     "pkv_decode_attention_multi", "pkv_compress_begin", "pkv_compress_commit",
     "pkv_decode_attention_partial", "pkv_merge_attention_states",
     "pkv_get_rotation_schedule", "pkv_read_basis", "pkv_get_row_block_ranges",
+    "pkv_q4_query_sizes", "pkv_q4_init_cache", "pkv_q4_destroy_cache", "pkv_q4_last_error", "pkv_q4_get_stats",
+    "pkv_q4_append_kv", "pkv_q4_read_kv", "pkv_q4_attention_workspace", "pkv_q4_attention",
 ]
 
 
@@ -58,6 +60,25 @@ class PkvStats(ctypes.Structure):
     _fields_ = [(n, ctypes.c_int64) for n in ("dense_slots_in_use", "factor_slots_in_use", "pages_compressed",
                                               "page_svds_not_converged", "device_timeouts", "bad_slot_indices",
                                               "last_decode_bytes", "last_decode_units", "page_svds", "jacobi_rounds")]
+
+
+PKV_DTYPE_BF16, PKV_DTYPE_FP16 = 0, 1
+
+
+class PkvQ4Config(ctypes.Structure):
+    _fields_ = [
+        ("n_kv_heads", ctypes.c_int32), ("n_q_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32),
+        ("page_size", ctypes.c_int32), ("group_size", ctypes.c_int32), ("dtype", ctypes.c_int32),
+        ("n_pages", ctypes.c_int64), ("softmax_scale", ctypes.c_float), ("n_ctas", ctypes.c_int32),
+    ]
+
+
+class PkvQ4Sizes(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int64) for n in ("page_bytes", "pool_bytes", "meta_bytes")]
+
+
+class PkvQ4Stats(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int64) for n in ("device_timeouts", "bad_pages", "bad_lengths")]
 
 
 class PkvError(RuntimeError):
@@ -105,8 +126,18 @@ def lib():
         L.pkv_get_decode_trace.argtypes = [vp, ctypes.POINTER(ctypes.c_int64), i32, vp]
         L.pkv_get_rotation_schedule.argtypes = [i32, ctypes.POINTER(ctypes.c_uint8), i64, ip, ip, ip]
         L.pkv_get_row_block_ranges.argtypes = [i64, i32, i32, i32, ip]
+        L.pkv_q4_query_sizes.argtypes = [ctypes.POINTER(PkvQ4Config), ctypes.POINTER(PkvQ4Sizes)]
+        L.pkv_q4_init_cache.argtypes = [ctypes.POINTER(PkvQ4Config), vp, vp, ctypes.POINTER(vp)]
+        L.pkv_q4_destroy_cache.argtypes = [vp]
+        L.pkv_q4_last_error.argtypes = [vp]
+        L.pkv_q4_last_error.restype = ctypes.c_char_p
+        L.pkv_q4_get_stats.argtypes = [vp, ctypes.POINTER(PkvQ4Stats), vp]
+        L.pkv_q4_append_kv.argtypes = [vp, i32, vp, i32, vp, i64, vp, vp, i64, i64, vp, i64, i64, vp]
+        L.pkv_q4_read_kv.argtypes = L.pkv_q4_append_kv.argtypes
+        L.pkv_q4_attention_workspace.argtypes = [vp, i32, i32, i32, ctypes.POINTER(i64)]
+        L.pkv_q4_attention.argtypes = [vp, i32, vp, i32, vp, i64, vp, i32, i32, vp, i64, i64, vp, i64, i64, vp, vp, i64, vp]
         for name in EXPORTS:
-            if name != "pkv_last_error":
+            if name not in ("pkv_last_error", "pkv_q4_last_error"):
                 getattr(L, name).restype = ctypes.c_int32
         _lib = L
     return _lib
@@ -330,6 +361,66 @@ def pkv_read_basis(handle, seq, layer, kv_head, B_k, B_v, stream=None):
     _check(handle, lib().pkv_read_basis(handle, seq, layer, kv_head, _ptr(B_k), _ptr(B_v), _stream(stream)))
 
 
+# ---- the paged cache held in 4 bits ------------------------------------------------
+def pkv_q4_query_sizes(cfg: PkvQ4Config) -> PkvQ4Sizes:
+    out = PkvQ4Sizes()
+    st = lib().pkv_q4_query_sizes(ctypes.byref(cfg), ctypes.byref(out))
+    if st != PKV_OK:
+        raise PkvError(st, "pkv_q4_query_sizes")
+    return out
+
+
+def pkv_q4_init_cache(cfg, pool, meta):
+    """Tensors (or None for both = dry run) -> opaque handle."""
+    h = ctypes.c_void_p()
+    st = lib().pkv_q4_init_cache(ctypes.byref(cfg), _ptr(pool), _ptr(meta), ctypes.byref(h))
+    if st != PKV_OK:
+        raise PkvError(st, "pkv_q4_init_cache")
+    return h
+
+
+def _q4_check(handle, st):
+    if st != PKV_OK:
+        raise PkvError(st, lib().pkv_q4_last_error(handle).decode())
+
+
+def pkv_q4_destroy_cache(handle):
+    lib().pkv_q4_destroy_cache(handle)
+
+
+def pkv_q4_get_stats(handle, stream=None) -> dict:
+    s = PkvQ4Stats()
+    _q4_check(handle, lib().pkv_q4_get_stats(handle, ctypes.byref(s), _stream(stream)))
+    return {n: int(getattr(s, n)) for n, _ in PkvQ4Stats._fields_}
+
+
+def pkv_q4_append_kv(handle, n_seqs, page_table, max_pages, lengths, n_rows, offsets, k, k_strides, v, v_strides, stream=None):
+    """k, v: [n_rows, H_kv, d]; k_strides, v_strides: (row, head) in elements."""
+    _q4_check(handle, lib().pkv_q4_append_kv(handle, n_seqs, _ptr(page_table), max_pages, _ptr(lengths), n_rows, _ptr(offsets),
+                                             _ptr(k), *k_strides, _ptr(v), *v_strides, _stream(stream)))
+
+
+def pkv_q4_read_kv(handle, n_seqs, page_table, max_pages, lengths, n_rows, offsets, k, k_strides, v, v_strides, stream=None):
+    _q4_check(handle, lib().pkv_q4_read_kv(handle, n_seqs, _ptr(page_table), max_pages, _ptr(lengths), n_rows, _ptr(offsets),
+                                           _ptr(k), *k_strides, _ptr(v), *v_strides, _stream(stream)))
+
+
+def pkv_q4_attention_workspace(handle, n_seqs, max_q_len, max_len) -> int:
+    n = ctypes.c_int64(0)
+    st = lib().pkv_q4_attention_workspace(handle, n_seqs, max_q_len, max_len, ctypes.byref(n))
+    if st != PKV_OK:
+        raise PkvError(st, "pkv_q4_attention_workspace(%r, %r, %r)" % (n_seqs, max_q_len, max_len))
+    return n.value
+
+
+def pkv_q4_attention(handle, n_seqs, page_table, max_pages, lengths, n_rows, offsets, max_q_len, max_len, q, q_strides, out,
+                     out_strides, state, workspace, workspace_bytes, stream=None):
+    """q, out: [n_rows, H_q, d]; state: fp32 [n_rows, H_q, d + 2] instead of out."""
+    _q4_check(handle, lib().pkv_q4_attention(handle, n_seqs, _ptr(page_table), max_pages, _ptr(lengths), n_rows, _ptr(offsets),
+                                             max_q_len, max_len, _ptr(q), *q_strides, _ptr(out), *out_strides, _ptr(state),
+                                             _ptr(workspace), workspace_bytes, _stream(stream)))
+
+
 # ---- convenience wrapper ----------------------------------------------------------
 def make_config(n_layers, n_kv_heads, n_q_heads, rank, sink_tokens, recent_tokens, max_seqs, max_pages_per_seq,
                 n_dense_slots, n_factor_slots, head_dim=128, page_size=64, rank_v=None, softmax_scale=0.0,
@@ -450,6 +541,174 @@ class Cache:
             if not self.dry_run:
                 torch.cuda.synchronize(self.device)
             pkv_destroy_cache(self.handle)
+            self.handle = None
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+
+_Q4_DTYPES = {torch.bfloat16: PKV_DTYPE_BF16, torch.float16: PKV_DTYPE_FP16}
+
+
+def make_q4_config(n_kv_heads, n_q_heads, n_pages, head_dim=128, page_size=64, group_size=32, dtype=torch.bfloat16,
+                   softmax_scale=0.0, n_ctas=0) -> PkvQ4Config:
+    if dtype not in _Q4_DTYPES:
+        raise PkvError(PKV_ERR_UNSUPPORTED, "dtype must be torch.bfloat16 or torch.float16, not %r" % (dtype,))
+    return PkvQ4Config(n_kv_heads, n_q_heads, head_dim, page_size, group_size, _Q4_DTYPES[dtype], n_pages, softmax_scale, n_ctas)
+
+
+class Q4Cache:
+    """A paged KV cache held in 4 bits (see include/pkv.h): owns the pool and the library handle.
+
+    page_table: int32 [n_seqs, max_pages], lengths: int32 [n_seqs] (tokens of each sequence, the rows of the call included),
+    both on the cache's device.  Row buffers are either [n_seqs, n, heads, d] (n rows of every sequence) or, with
+    offsets (int32 [n_seqs + 1]), [rows, heads, d] with rows offsets[s] .. offsets[s + 1] - 1 belonging to sequence s; the rows
+    are the sequence's last positions.  Rows and heads may be strided (slices of a fused projection).  Calls run on the
+    current stream of the cache's device.
+    """
+
+    def __init__(self, cfg: PkvQ4Config, device="cuda", dry_run=False):
+        self.cfg = cfg
+        self.handle = None
+        self.sizes = pkv_q4_query_sizes(cfg)
+        self.dry_run = dry_run
+        self.dtype = torch.float16 if cfg.dtype == PKV_DTYPE_FP16 else torch.bfloat16
+        self._workspaces = {}
+        if dry_run:
+            self.device, self._device_index, self.pool, self.meta = torch.device("cpu"), None, None, None
+            self.handle = pkv_q4_init_cache(cfg, None, None)
+        else:
+            self._device_index = Cache.dense_pool_device_index(torch.device(device))
+            self.device = torch.device("cuda", self._device_index)
+            self.pool = torch.empty(self.sizes.pool_bytes, dtype=torch.uint8, device=self.device)
+            self.meta = torch.empty(self.sizes.meta_bytes, dtype=torch.uint8, device=self.device)
+            with torch.cuda.device(self._device_index):
+                self.handle = pkv_q4_init_cache(cfg, self.pool, self.meta)
+
+    def _fail(self, message):
+        raise PkvError(PKV_ERR_INVALID_ARG, message)
+
+    def _stream(self):
+        if self.dry_run:
+            return None
+        if _raw_current_stream is not None:
+            return _raw_current_stream(self._device_index)
+        return torch.cuda.current_stream(self.device)
+
+    def _call(self, fn, *args):
+        """fn with the cache's device current."""
+        if self.dry_run or torch.cuda.current_device() == self._device_index:
+            return fn(self.handle, *args, self._stream())
+        with torch.cuda.device(self._device_index):
+            return fn(self.handle, *args, self._stream())
+
+    def _seqs(self, page_table, lengths, offsets):
+        for name, t in (("page_table", page_table), ("lengths", lengths), ("offsets", offsets)):
+            if t is not None and (t.dtype != torch.int32 or t.device != self.device or not t.is_contiguous()):
+                self._fail("%s must be a contiguous int32 tensor on %s" % (name, self.device))
+        if page_table.dim() != 2 or lengths.shape != page_table.shape[:1]:
+            self._fail("page_table must be [n_seqs, max_pages] and lengths [n_seqs]")
+        if offsets is not None and offsets.shape != (page_table.shape[0] + 1,):
+            self._fail("offsets must be [n_seqs + 1]")
+        return page_table.shape
+
+    def _rows(self, name, t, heads, n_seqs, ragged):
+        """-> (rows, (row stride, head stride)) of a row buffer."""
+        shape, d = t.shape, self.cfg.head_dim
+        if t.dtype != self.dtype or t.device != self.device:
+            self._fail("%s must be %s on %s" % (name, self.dtype, self.device))
+        if ragged:
+            if len(shape) != 3 or shape[1] != heads or shape[2] != d:
+                self._fail("%s must be [rows, %d, %d] with offsets" % (name, heads, d))
+            n, st = shape[0], t.stride()
+            row = st[0]
+        else:
+            if len(shape) != 4 or shape[0] != n_seqs or shape[2] != heads or shape[3] != d:
+                self._fail("%s must be [%d, n, %d, %d] without offsets" % (name, n_seqs, heads, d))
+            n, st = shape[0] * shape[1], t.stride()
+            row = st[1] if shape[1] > 1 else st[0]
+            if shape[0] > 1 and shape[1] > 1 and st[0] != shape[1] * row:
+                self._fail("%s: the rows of all sequences must be equally far apart (pass [rows, heads, d] and offsets)" % name)
+        if st[-1] != 1:
+            self._fail("%s: the channels of a head must be adjacent" % name)
+        if n <= 1:
+            row = heads * d                              # a size-1 axis may carry any stride
+        return n, (row, st[-2] if heads > 1 else d)
+
+    def append_kv(self, page_table, lengths, k, v, offsets=None):
+        """Quantises the new rows k, v into the cache."""
+        n_seqs, max_pages = self._seqs(page_table, lengths, offsets)
+        n, ks = self._rows("k", k, self.cfg.n_kv_heads, n_seqs, offsets is not None)
+        nv, vs = self._rows("v", v, self.cfg.n_kv_heads, n_seqs, offsets is not None)
+        if n != nv:
+            self._fail("k and v must have the same number of rows")
+        self._call(pkv_q4_append_kv, n_seqs, page_table, max_pages, lengths, n, offsets, k, ks, v, vs)
+
+    def read_kv(self, page_table, lengths, k, v, offsets=None):
+        """Reads the last positions of each sequence back into k, v."""
+        n_seqs, max_pages = self._seqs(page_table, lengths, offsets)
+        n, ks = self._rows("k", k, self.cfg.n_kv_heads, n_seqs, offsets is not None)
+        nv, vs = self._rows("v", v, self.cfg.n_kv_heads, n_seqs, offsets is not None)
+        if n != nv:
+            self._fail("k and v must have the same number of rows")
+        self._call(pkv_q4_read_kv, n_seqs, page_table, max_pages, lengths, n, offsets, k, ks, v, vs)
+        return k, v
+
+    def attention(self, page_table, lengths, q, out=None, offsets=None, max_q_len=None, max_len=0):
+        """Attention of the newest positions over the cache; out (default: a new tensor like q) is returned.  With offsets,
+        max_q_len bounds the rows of a sequence (default: all rows)."""
+        if out is None:
+            out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+        elif out.shape != q.shape:
+            self._fail("out must have the shape of q")
+        self._attention(page_table, lengths, q, out, None, offsets, max_q_len, max_len)
+        return out
+
+    def attention_partial(self, page_table, lengths, q, state=None, offsets=None, max_q_len=None, max_len=0):
+        """The same as softmax states [..., d + 2] fp32 (o, m, l) for pkv_merge_attention_states()."""
+        shape = (*q.shape[:-1], q.shape[-1] + 2)
+        if state is None:
+            state = torch.empty(shape, dtype=torch.float32, device=q.device)
+        elif state.shape != shape or state.dtype != torch.float32 or state.device != self.device or not state.is_contiguous():
+            self._fail("state must be a contiguous fp32 tensor of shape %r on %s" % (shape, self.device))
+        self._attention(page_table, lengths, q, None, state, offsets, max_q_len, max_len)
+        return state
+
+    def _attention(self, page_table, lengths, q, out, state, offsets, max_q_len, max_len):
+        n_seqs, max_pages = self._seqs(page_table, lengths, offsets)
+        n, qs = self._rows("q", q, self.cfg.n_q_heads, n_seqs, offsets is not None)
+        os_ = qs if out is None else self._rows("out", out, self.cfg.n_q_heads, n_seqs, offsets is not None)[1]
+        if n == 0:
+            return
+        if offsets is None:
+            max_q_len = q.shape[1]
+        elif max_q_len is None:
+            max_q_len = n
+        if max_q_len == 0:
+            return
+        max_len = min(max_len, max_pages * self.cfg.page_size) if max_len > 0 else max_pages * self.cfg.page_size
+        key = (n_seqs, max_q_len, max_len)
+        size = self._workspaces.get(key)
+        if size is None:
+            if len(self._workspaces) >= 256:
+                self._workspaces.clear()
+            size = self._workspaces[key] = pkv_q4_attention_workspace(self.handle, *key)
+        # (from the caching allocator at each call: ordered with this stream, and private to a graph that is being captured)
+        work = torch.empty(size, dtype=torch.uint8, device=self.device) if size and not self.dry_run else None
+        self._call(pkv_q4_attention, n_seqs, page_table, max_pages, lengths, n, offsets, max_q_len, max_len, q, qs, out, os_, state,
+                   work, size)
+
+    def stats(self):
+        return self._call(pkv_q4_get_stats)
+
+    def close(self):
+        if self.handle is not None:
+            if not self.dry_run:
+                torch.cuda.synchronize(self.device)
+            pkv_q4_destroy_cache(self.handle)
             self.handle = None
 
     def __del__(self):
