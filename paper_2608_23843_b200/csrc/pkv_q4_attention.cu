@@ -1,85 +1,774 @@
-// Attention over the paged 4-bit cache.
+// Attention over the paged 4-bit cache, few query rows per KV head: decoding, speculative steps.
+//
+// Bound by HBM: a token costs d + 4 d/g bytes per KV head and is read once, against 4 G d flop, so the contractions go to
+// the tensor cores and what has to be kept short is the path from codes to operands (one warp-instruction is about
+// 0.7 bytes of HBM time per lane at 148 SMs).  Tokens are the row dimension of s = K q^T and the contraction dimension of
+// o^T += V^T p, so that eight query rows (NT = 1) fill the column dimension of one m16n8k16 product:
+//   K codes become fp16 operands by masking alone: code + 8 in the low bits of a 16-bit word is an fp16 subnormal,
+//     (code + 8) 2^-24 exactly, and in bits 4-7 that times 16 (the queries of those channels are divided by 16).  The + 8
+//     is taken away by the accumulators' start value -8 * sum(q).  Each group's product is multiplied by its scale in fp32.
+//   V codes become fp16 integers (magic constants 1024 and 64, then one packed subtraction); the scales go to the weights,
+//     p * scale, rounded once to fp16.  To keep that inside fp16's range whatever the values' size, the running reference
+//     of the softmax is max(s) + E with E the exponent of the largest value scale of the step: p * scale <= 2 then.
+//   Queries are brought to fp16 with a power of two per row, which is exact for bf16 and fp16 alike.
+// Every warp of a CTA walks its own units of 64 tokens with its own ring of bulk copies, and keeps (m, l, o) in registers;
+// at the end of a (sequence, KV head, row tile) segment the warps' states are joined through shared memory.  The CTAs of
+// a launch share the whole batch's units evenly, whatever the lengths; a segment that spans CTAs leaves its states in the
+// workspace and a second kernel joins them in token order.
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 
 #include "pkv_q4.h"
+#include "pkv_device.cuh"
 
 namespace pkv {
 
 namespace {
 
-// code * scale of one element of a tile (exact in fp32)
-__device__ __forceinline__ float q4_value(const Q4Geometry &g, const unsigned char *tile, bool v, int t, int ch) {
-    const int d = g.head_dim, w = ch >> 5, in = ch & 31;
-    const int off = v ? q4_v_base(d) + q4_v_chunk(d, t, in >> 2) + w * 2 + ((in & 3) >> 1) : q4_k_chunk(d, t, in >> 3) + w * 4;
-    int nib;
-    if (v) nib = tile[off] >> (4 * (in & 1)) & 15;
-    else nib = *reinterpret_cast<const uint32_t *>(tile + off) >> (4 * ((in & 7) >> 1) + 16 * (in & 1)) & 15;
-    const unsigned short s = *reinterpret_cast<const unsigned short *>(tile + (v ? q4_vs_base(d, g.groups) : q4_ks_base(d)) +
-                                                                       (t * g.groups + ch / (d / g.groups)) * 2);
-    return (float)(nib - 8) * __uint_as_float((uint32_t)s << 16);
+constexpr int kQ4Warps = 6, kQ4Threads = kQ4Warps * 32;
+constexpr int kQ4Unit = 64;            // tokens per unit
+
+template <int D, int NG, int NT>
+struct Q4Shape {
+    static constexpr int kTile = kQ4Tile * (D + 4 * NG), kUnitBytes = 4 * kTile;
+    static constexpr int kRowFloats = D + 4;                                        // a row of o in shared memory, padded against bank conflicts
+    static constexpr int kFlush = 8 * NT * kRowFloats * 4;                          // a warp's o at a segment's end: over the stage it has just read
+    static constexpr int kStage = ((kUnitBytes > kFlush ? kUnitBytes : kFlush) + 127) / 128 * 128;
+    static constexpr int kStages = 111 * 1024 / (kQ4Warps * kStage) < 4 ? 111 * 1024 / (kQ4Warps * kStage) : 4;
+    static constexpr int kSmem = kQ4Warps * kStages * kStage;
+    static_assert(kStages >= 2 && 2 * (kSmem + 3072) <= 227 * 1024, "two CTAs per SM with two stages per warp");
+};
+
+// A segment that begins in a CTA and ends in another (seq < 0: none); slot: where its first part is (see below)
+struct Q4Part { int seq, tile, head, slot, last_cta; };
+
+// Partial states: two per CTA (its first segment, its last), each [8 NT rows][D] o, then m and l of the rows.
+__host__ __device__ inline long long q4_state_floats(int rows, int d) { return (long long)rows * (d + 2); }
+__host__ __device__ inline long long q4_parts_bytes(int n_ctas) { return ((long long)n_ctas * (int)sizeof(Q4Part) + 255) / 256 * 256; }
+
+// The rows of a sequence that the call works on; `all`: with those beyond the caller's bound, which the positions go by.
+__device__ __forceinline__ int q4_new_rows(const Q4AttentionArgs &a, int s, int &first, int &all, int *status) {
+    first = q4_first_row(a.rows, s);
+    all = q4_first_row(a.rows, s + 1) - first;
+    if (status && all > a.max_q_len) atomicAdd(status + 2, 1);
+    return max(0, min(all, a.max_q_len));
 }
 
-// The simplest form: a warp per query row and head, a token at a time.
-__global__ void __launch_bounds__(128) q4_simple_kernel(const __grid_constant__ Q4AttentionArgs a) {
-    const Q4Geometry &g = a.geo;
-    const int lane = threadIdx.x & 31, d = g.head_dim, per = d / 32, s = blockIdx.y, h = blockIdx.z;
-    const int j = blockIdx.x * 4 + (threadIdx.x >> 5);
-    const int first = q4_first_row(a.rows, s), n = q4_first_row(a.rows, s + 1) - first;
-    const bool first_warp = j == 0 && h == 0 && lane == 0;
-    const int T = q4_length(a.rows, g, s, first_warp ? a.status : nullptr);
-    if (first_warp && n > a.max_q_len) atomicAdd(a.status + 2, 1);
-    if (j >= n || j >= a.max_q_len) return;
-    const int kv = h / g.group, see = T - n + j + 1;
-    float q[4], o[4] = {0.f, 0.f, 0.f, 0.f}, m = -1e30f, l = 0.f;
-    for (int i = 0; i < per; ++i) {
-        const long long at = (first + j) * a.q_row + h * a.q_head + lane + 32 * i;
-        q[i] = g.fp16 ? __half2float(reinterpret_cast<const __half *>(a.q)[at]) : __bfloat162float(reinterpret_cast<const __nv_bfloat16 *>(a.q)[at]);
-    }
-    for (int t = 0; t < see; ++t) {
-        const int page = a.rows.table[(long long)s * a.rows.max_pages + (t >> g.page_shift)];
-        if (page < 0 || page >= g.n_pages) {
-            if (lane == 0 && (t & (g.page - 1)) == 0) atomicAdd(a.status + 1, 1);
-            continue;
+__device__ __forceinline__ void mma_f16(float *d, const uint32_t *a, uint32_t b0, uint32_t b1, const float *c) {
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%10, %11, %12, %13};"
+        : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3])
+        : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1), "f"(c[0]), "f"(c[1]), "f"(c[2]), "f"(c[3]));
+}
+__device__ __forceinline__ uint32_t movmatrix(uint32_t x) {
+    uint32_t y;
+    asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
+    return y;
+}
+__device__ __forceinline__ float ex2(float x) {
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+__device__ __forceinline__ uint32_t pack_f16(float lo, float hi) {
+    uint32_t r;
+    asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+    return r;
+}
+__device__ __forceinline__ uint32_t sub_f16(uint32_t x, uint32_t y) {
+    uint32_t r;
+    asm("sub.rn.f16x2 %0, %1, %2;" : "=r"(r) : "r"(x), "r"(y));
+    return r;
+}
+__device__ __forceinline__ uint32_t max_bf16(uint32_t x, uint32_t y) {      // (the other operand where one is NaN)
+    uint32_t r;
+    asm("max.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(x), "r"(y));
+    return r;
+}
+// (x & mask) | bits in one instruction
+__device__ __forceinline__ uint32_t and_or(uint32_t x, uint32_t mask, uint32_t bits) {
+    uint32_t r;
+    asm("lop3.b32 %0, %1, %2, %3, 0xEA;" : "=r"(r) : "r"(x), "r"(mask), "r"(bits));
+    return r;
+}
+
+// Where a warp's next unit is: positions in the batch's order of units (sequence, row tile, head, unit of 64 tokens).
+struct Q4Cursor {
+    int seq, tile, head, unit;         // seq == n_seqs: past the end
+    int T, tiles, units;               // of the sequence
+};
+
+__device__ __forceinline__ void q4_load_seq(const Q4AttentionArgs &a, int rows_per_tile, Q4Cursor &c) {
+    int first, all;
+    const int n = q4_new_rows(a, c.seq, first, all, nullptr);
+    c.T = q4_length(a.rows, a.geo, c.seq, nullptr);
+    c.tiles = (n * a.geo.group + rows_per_tile - 1) / rows_per_tile;
+    c.units = max(1, (c.T + kQ4Unit - 1) / kQ4Unit);
+}
+__device__ __forceinline__ void q4_advance(const Q4AttentionArgs &a, int rows_per_tile, Q4Cursor &c, int by) {
+    c.unit += by;
+    while (c.unit >= c.units) {
+        c.unit -= c.units;
+        if (++c.head == a.geo.n_kv_heads) {
+            c.head = 0;
+            if (++c.tile == c.tiles) {
+                c.tile = 0;
+                do {
+                    if (++c.seq >= a.rows.n_seqs) return;
+                    q4_load_seq(a, rows_per_tile, c);
+                } while (c.tiles == 0);
+            }
         }
-        const int in = t & (g.page - 1);
-        const unsigned char *tile = a.pool + page * g.page_bytes + (long long)kv * g.head_bytes + in / kQ4Tile * g.tile_bytes;
-        float x = 0.f;
-        for (int i = 0; i < per; ++i) x += q[i] * q4_value(g, tile, false, in & 15, lane + 32 * i);
-        for (int k = 16; k; k >>= 1) x += __shfl_xor_sync(0xffffffffu, x, k);
-        x *= g.scale_log2e;
-        const float mn = fmaxf(m, x), f = exp2f(m - mn), p = exp2f(x - mn);
-        m = mn;
-        l = l * f + p;
-        for (int i = 0; i < per; ++i) o[i] = o[i] * f + p * q4_value(g, tile, true, in & 15, lane + 32 * i);
-    }
-    const float inv = see > 0 && l != 0.f ? 1.f / l : 0.f;
-    const long long row = first + j;
-    for (int i = 0; i < per; ++i) {
-        const int ch = lane + 32 * i;
-        if (a.state) {
-            a.state[(row * g.n_q_heads + h) * (d + 2) + ch] = o[i];
-        } else {
-            const long long at = row * a.out_row + h * a.out_head + ch;
-            if (g.fp16) reinterpret_cast<__half *>(a.out)[at] = __float2half_rn(o[i] * inv);
-            else reinterpret_cast<__nv_bfloat16 *>(a.out)[at] = __float2bfloat16_rn(o[i] * inv);
-        }
-    }
-    if (a.state && lane == 0) {
-        a.state[(row * g.n_q_heads + h) * (d + 2) + d] = m;
-        a.state[(row * g.n_q_heads + h) * (d + 2) + d + 1] = l;
     }
 }
+
+template <int D, int NG, bool H16, int NT>
+__global__ void __launch_bounds__(kQ4Threads, 2) q4_decode_kernel(const __grid_constant__ Q4AttentionArgs a) {
+    using S = Q4Shape<D, NG, NT>;
+    constexpr int NW = D / 32, WPG = NW / NG, R = 8 * NT;      // 32-channel words per row, words per scale, query rows
+    constexpr int TS = NT == 1 ? 4 : 2;                        // tiles per softmax step
+    constexpr int kSt = S::kStages;
+    const Q4Geometry &geo = a.geo;
+    extern __shared__ __align__(128) unsigned char smem[];
+    __shared__ unsigned long long bars[kQ4Warps][kSt];
+    __shared__ float2 ml[kQ4Warps][R];
+    __shared__ long long sums[kQ4Warps], found_at;
+    __shared__ int found_seq, offs[kQ4Warps];
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, c = lane & 3;
+    if (lane == 0)
+        for (int s = 0; s < kSt; ++s) mbar_init(smem_u32(&bars[warp][s]), 1);
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+
+    // ---- this CTA's share of the batch's units ----
+    const int H = geo.n_kv_heads, n_seqs = a.rows.n_seqs;
+    int *status = blockIdx.x == 0 ? a.status : nullptr;
+    long long total = 0;
+    auto weight = [&](int s, int *st) -> long long {           // units of a sequence, over its row tiles and heads
+        if (s >= n_seqs) return 0;
+        int first, all;
+        const int n = q4_new_rows(a, s, first, all, st), T = q4_length(a.rows, geo, s, st);
+        return (long long)((n * geo.group + R - 1) / R) * H * max(1, (T + kQ4Unit - 1) / kQ4Unit);
+    };
+    {
+        long long mine = 0;
+        for (int s = tid; s < n_seqs; s += kQ4Threads) mine += weight(s, status);
+#pragma unroll
+        for (int d = 16; d; d >>= 1) mine += __shfl_xor_sync(0xffffffffu, mine, d);
+        if (lane == 0) sums[warp] = mine;
+        __syncthreads();
+#pragma unroll
+        for (int w = 0; w < kQ4Warps; ++w) total += sums[w];
+    }
+    // (no more CTAs than there are units for a warp of each; the launch could only estimate that)
+    const int n_ctas = (int)min((long long)gridDim.x, max(1LL, total / kQ4Warps));
+    const long long begin = total * blockIdx.x / n_ctas, end = total * (blockIdx.x + 1) / n_ctas;
+    Q4Part *parts = reinterpret_cast<Q4Part *>(a.workspace);
+    float *states = reinterpret_cast<float *>(a.workspace + q4_parts_bytes(gridDim.x));
+    if (blockIdx.x >= n_ctas || begin >= end) {
+        if (tid == 0 && gridDim.x > 1) parts[blockIdx.x].seq = -1;
+        return;
+    }
+    // the sequence that holds unit `begin`
+    {
+        long long base = 0;
+        for (int s0 = 0; s0 < n_seqs; s0 += kQ4Threads) {
+            const long long v = weight(s0 + tid, nullptr);
+            long long x = v;
+#pragma unroll
+            for (int d = 1; d < 32; d <<= 1) {
+                const long long y = __shfl_up_sync(0xffffffffu, x, d);
+                if (lane >= d) x += y;
+            }
+            __syncthreads();
+            if (lane == 31) sums[warp] = x;
+            __syncthreads();
+            long long before = base, all = 0;
+#pragma unroll
+            for (int w = 0; w < kQ4Warps; ++w) {
+                if (w < warp) before += sums[w];
+                all += sums[w];
+            }
+            const long long lo = before + x - v;
+            if (begin >= lo && begin < lo + v) { found_seq = s0 + tid; found_at = begin - lo; }
+            base += all;
+            if (base > begin) break;
+        }
+        __syncthreads();
+    }
+    Q4Cursor seg;                                              // of the CTA: the segment being worked on, and its first unit here
+    seg.seq = found_seq;
+    q4_load_seq(a, R, seg);
+    {
+        const long long at = found_at;
+        seg.unit = (int)(at % seg.units);
+        seg.head = (int)(at / seg.units % H);
+        seg.tile = (int)(at / seg.units / H);
+    }
+
+    // ---- this warp's copies ----
+    const uint32_t ring = smem_u32(smem) + warp * kSt * S::kStage;
+    const unsigned char *ring_p = smem + warp * kSt * S::kStage;
+    const int left_cta = (int)(end - begin);                   // units of the CTA
+    Q4Cursor nx = seg;                                         // the next unit to fetch
+    int nx_at = warp;                                          // its index within the CTA's units
+    if (warp < left_cta) q4_advance(a, R, nx, warp);
+    const int per_page = min(kQ4Unit, geo.page), n_parts = kQ4Unit / per_page;      // copies per unit: 1, 2 or 4
+    auto page_of = [&]() -> int {                              // lane i < n_parts: the page of part i of unit nx
+        const int t = nx.unit * kQ4Unit + lane * per_page;
+        if (lane >= n_parts || nx_at >= left_cta || t >= nx.T) return -1;
+        return __ldg(a.rows.table + (long long)nx.seq * a.rows.max_pages + (t >> geo.page_shift));
+    };
+    int pg = page_of();
+    bool timed_out = false;                                    // a wait ran out: nothing more is fetched, what is left counts as not there
+    int lost = 0;                                              // ... and which of the warp's units did not come
+    uint32_t vm = 0;                                           // per stage four bits: which tiles of 16 tokens are there
+    int st_in = 0;
+    auto fetch = [&]() {
+        if (nx_at >= left_cta || timed_out) return;
+        const int t0 = nx.unit * kQ4Unit + lane * per_page;
+        const int toks = lane < n_parts ? max(0, min(per_page, nx.T - t0)) : 0;
+        const int tiles = (toks + kQ4Tile - 1) / kQ4Tile;
+        const bool ok = tiles > 0 && pg >= 0 && pg < geo.n_pages;
+        if (tiles > 0 && !ok) atomicAdd(a.status + 1, 1);
+        const int per_tiles = per_page / kQ4Tile;
+        uint32_t bits = ok ? ((1u << tiles) - 1u) << (lane * per_tiles) : 0u;
+        bits |= __shfl_xor_sync(0xffffffffu, bits, 1);
+        bits |= __shfl_xor_sync(0xffffffffu, bits, 2);
+        bits = __shfl_sync(0xffffffffu, bits, 0);
+        const uint32_t bar = smem_u32(&bars[warp][st_in]);
+        if (lane == 0) {
+            if (bits) mbar_arrive_expect_tx(bar, __popc(bits) * S::kTile);
+            else mbar_arrive(bar);
+        }
+        __syncwarp();
+        if (ok)
+            bulk_g2s(ring + st_in * S::kStage + lane * per_tiles * S::kTile,
+                     a.pool + (long long)pg * geo.page_bytes + (long long)nx.head * geo.head_bytes + ((t0 & (geo.page - 1)) / kQ4Tile) * S::kTile,
+                     tiles * S::kTile, bar);
+        vm = (vm & ~(15u << (4 * st_in))) | bits << (4 * st_in);
+        if (++st_in == kSt) st_in = 0;
+        nx_at += kQ4Warps;
+        if (nx_at < left_cta) q4_advance(a, R, nx, kQ4Warps);
+        pg = page_of();
+    };
+#pragma unroll 1
+    for (int s = 0; s < kSt; ++s) fetch();
+
+    int at = warp;                                             // this warp's next unit, within the CTA's units
+    int seg_lo = 0;                                            // the segment's first unit, within the CTA's units
+    int st_out = 0, phase = 0;
+    const float scale = geo.scale_log2e;
+    while (seg_lo < left_cta) {
+        const int seg_hi = min(left_cta, seg_lo + seg.units - seg.unit);
+        // ---- the segment's queries ----
+        int first, all;
+        const int n = q4_new_rows(a, seg.seq, first, all, nullptr), G = geo.group;
+        uint32_t qf[NT][NW][4];
+        float start[NT][NG][2], fcol[NT][2], F[NT][2], l[NT][2], o[NT][2 * NW][4];
+        int vis[NT][2];
+        int vis_all = seg.T;                                   // tokens every row of the tile sees
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+            const int row = seg.tile * R + nt * 8 + g, j = row / G, h = row - j * G;
+            const bool in = j < n;
+            float x[NW][8];
+            float mx = 0.f;
+#pragma unroll
+            for (int w = 0; w < NW; ++w) {
+                const uint4 raw = in ? __ldg(reinterpret_cast<const uint4 *>(
+                                           reinterpret_cast<const unsigned short *>(a.q) + (long long)(first + j) * a.q_row +
+                                           (long long)(seg.head * G + h) * a.q_head + 32 * w + 8 * c))
+                                     : make_uint4(0u, 0u, 0u, 0u);
+                const uint32_t u[4] = {raw.x, raw.y, raw.z, raw.w};
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    if (H16) {
+                        const float2 f = __half22float2(*reinterpret_cast<const __half2 *>(&u[i]));
+                        x[w][2 * i] = f.x; x[w][2 * i + 1] = f.y;
+                    } else {
+                        x[w][2 * i] = bf16lo_f(u[i]); x[w][2 * i + 1] = bf16hi_f(u[i]);
+                    }
+                    mx = fmaxf(mx, fmaxf(fabsf(x[w][2 * i]), fabsf(x[w][2 * i + 1])));
+                }
+            }
+            mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 1));
+            mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 2));
+            // times 2^(10 - exponent of the largest): 2^10 .. 2^11, so that a sixteenth of it is far from subnormal too
+            const int e = min(max((int)(__float_as_uint(mx) >> 23) - 127, -90), 126);
+            const float up = __uint_as_float((uint32_t)(10 - e + 127) << 23);
+            float sum[NG];
+#pragma unroll
+            for (int k = 0; k < NG; ++k) sum[k] = 0.f;
+#pragma unroll
+            for (int w = 0; w < NW; ++w)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const float f = i & 1 ? up * 0.0625f : up;
+                    qf[nt][w][i] = pack_f16(x[w][2 * i] * f, x[w][2 * i + 1] * f);
+                    const float2 r = __half22float2(*reinterpret_cast<const __half2 *>(&qf[nt][w][i]));
+                    sum[w / WPG] += (r.x + r.y) * (i & 1 ? 16.f : 1.f);
+                }
+            // per column: the accumulators' start value and the factor of the scores, from the lanes that hold the row
+            const float fr = 16384.f * __uint_as_float((uint32_t)(e + 127) << 23) * scale;      // 2^24 / up
+#pragma unroll
+            for (int k = 0; k < NG; ++k) {
+                sum[k] += __shfl_xor_sync(0xffffffffu, sum[k], 1);
+                sum[k] += __shfl_xor_sync(0xffffffffu, sum[k], 2);
+                sum[k] *= -8.f / 16777216.f;
+            }
+#pragma unroll
+            for (int b = 0; b < 2; ++b) {
+                const int col = 2 * c + b, r2 = seg.tile * R + nt * 8 + col, j2 = r2 / G;
+#pragma unroll
+                for (int k = 0; k < NG; ++k) start[nt][k][b] = __shfl_sync(0xffffffffu, sum[k], 4 * col);
+                fcol[nt][b] = __shfl_sync(0xffffffffu, fr, 4 * col);
+                vis[nt][b] = j2 < n ? seg.T - all + j2 + 1 : seg.T;
+                vis_all = min(vis_all, vis[nt][b]);
+                F[nt][b] = kNegInf;
+                l[nt][b] = 0.f;
+            }
+#pragma unroll
+            for (int i = 0; i < 2 * NW; ++i)
+#pragma unroll
+                for (int k = 0; k < 4; ++k) o[nt][i][k] = 0.f;
+        }
+        vis_all = __reduce_min_sync(0xffffffffu, vis_all);
+
+        // ---- the segment's units ----
+        const bool any = at < seg_hi;
+        while (at < seg_hi) {
+            const int t_unit = (seg.unit + at - seg_lo) * kQ4Unit;
+            const uint32_t bar = smem_u32(&bars[warp][st_out]);
+            if (!timed_out && !__all_sync(0xffffffffu, mbar_wait(bar, phase & 1))) {
+                if (lane == 0) atomicAdd(a.status, 1);
+                timed_out = true;
+                lost = phase * kSt + st_out;
+            }
+            const uint32_t have = timed_out ? 0u : (vm >> (4 * st_out)) & 15u;
+            const bool whole = have == 15u && t_unit + kQ4Unit <= vis_all;
+            const unsigned char *sp = ring_p + st_out * S::kStage;
+#pragma unroll 1
+            for (int step = 0; step < 4 / TS; ++step) {
+                const unsigned char *tp0 = sp + step * TS * S::kTile;
+                const int t0 = t_unit + step * TS * kQ4Tile;
+                float sc[TS][NT][4];
+                // ---- scores ----
+#pragma unroll
+                for (int tl = 0; tl < TS; ++tl) {
+                    const unsigned char *tp = tp0 + tl * S::kTile;
+                    uint32_t k0[NW], k1[NW], s0[(NG + 1) / 2], s1[(NG + 1) / 2];
+                    if (NW == 4) {
+                        const uint4 x = *reinterpret_cast<const uint4 *>(tp + q4_k_chunk(D, g, c)), y = *reinterpret_cast<const uint4 *>(tp + q4_k_chunk(D, g + 8, c));
+                        k0[0] = x.x; k0[1] = x.y; k0[NW - 2] = x.z; k0[NW - 1] = x.w;
+                        k1[0] = y.x; k1[1] = y.y; k1[NW - 2] = y.z; k1[NW - 1] = y.w;
+                    } else {
+                        const uint2 x = *reinterpret_cast<const uint2 *>(tp + q4_k_chunk(D, g, c)), y = *reinterpret_cast<const uint2 *>(tp + q4_k_chunk(D, g + 8, c));
+                        k0[0] = x.x; k0[1] = x.y; k1[0] = y.x; k1[1] = y.y;
+                    }
+                    const unsigned char *ks = tp + q4_ks_base(D);
+                    if (NG == 4) {
+                        const uint2 x = *reinterpret_cast<const uint2 *>(ks + g * 8), y = *reinterpret_cast<const uint2 *>(ks + (g + 8) * 8);
+                        s0[0] = x.x; s0[(NG - 1) / 2] = x.y; s1[0] = y.x; s1[(NG - 1) / 2] = y.y;
+                    } else if (NG == 2) {
+                        s0[0] = *reinterpret_cast<const uint32_t *>(ks + g * 4); s1[0] = *reinterpret_cast<const uint32_t *>(ks + (g + 8) * 4);
+                    } else {
+                        s0[0] = *reinterpret_cast<const unsigned short *>(ks + g * 2); s1[0] = *reinterpret_cast<const unsigned short *>(ks + (g + 8) * 2);
+                    }
+#pragma unroll
+                    for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) sc[tl][nt][i] = 0.f;
+#pragma unroll
+                    for (int k = 0; k < NG; ++k) {
+                        float acc[NT][4];
+#pragma unroll
+                        for (int nt = 0; nt < NT; ++nt) {
+                            acc[nt][0] = acc[nt][2] = start[nt][k][0];
+                            acc[nt][1] = acc[nt][3] = start[nt][k][1];
+                        }
+#pragma unroll
+                        for (int w = k * WPG; w < (k + 1) * WPG; ++w) {
+                            const uint32_t x0 = k0[w] >> 8, x1 = k1[w] >> 8;
+                            const uint32_t fa[4] = {k0[w] & 0x000f000fu, k1[w] & 0x000f000fu, k0[w] & 0x00f000f0u, k1[w] & 0x00f000f0u};
+                            const uint32_t fb[4] = {x0 & 0x000f000fu, x1 & 0x000f000fu, x0 & 0x00f000f0u, x1 & 0x00f000f0u};
+#pragma unroll
+                            for (int nt = 0; nt < NT; ++nt) {
+                                mma_f16(acc[nt], fa, qf[nt][w][0], qf[nt][w][1], acc[nt]);
+                                mma_f16(acc[nt], fb, qf[nt][w][2], qf[nt][w][3], acc[nt]);
+                            }
+                        }
+                        const float f0 = k & 1 ? bf16hi_f(s0[k / 2]) : bf16lo_f(s0[k / 2]), f1 = k & 1 ? bf16hi_f(s1[k / 2]) : bf16lo_f(s1[k / 2]);
+#pragma unroll
+                        for (int nt = 0; nt < NT; ++nt) {
+                            sc[tl][nt][0] += f0 * acc[nt][0]; sc[tl][nt][1] += f0 * acc[nt][1];
+                            sc[tl][nt][2] += f1 * acc[nt][2]; sc[tl][nt][3] += f1 * acc[nt][3];
+                        }
+                    }
+                }
+                // ---- E: exponent of the step's largest value scale (lane: tokens 2 lane, 2 lane + 1 of the step) ----
+                uint32_t big = 0;
+                if (lane < 8 * TS) {
+                    const int tl = lane >> 3, t2 = 2 * (lane & 7), t = t0 + tl * kQ4Tile + t2;
+                    const unsigned char *vs = tp0 + tl * S::kTile + q4_vs_base(D, NG) + t2 * NG * 2;
+                    uint32_t z[NG];
+                    if (NG == 4) {
+                        const uint4 x = *reinterpret_cast<const uint4 *>(vs);
+                        z[0] = x.x; z[NG > 1] = x.y; z[NG - 2 >= 0 ? NG - 2 : 0] = x.z; z[NG - 1] = x.w;
+                    } else if (NG == 2) {
+                        const uint2 x = *reinterpret_cast<const uint2 *>(vs);
+                        z[0] = x.x; z[NG - 1] = x.y;
+                    } else {
+                        z[0] = *reinterpret_cast<const uint32_t *>(vs);
+                    }
+                    if (!whole) {                              // rows past the end or on a page that is not there
+                        const bool here = (have >> (step * TS + tl)) & 1;
+#pragma unroll
+                        for (int k = 0; k < NG; ++k) {
+                            const bool lo = here && t + (NG == 1 ? 0 : k / ((NG + 1) / 2)) < seg.T;
+                            if (NG == 1) z[k] = (here && t < seg.T ? z[k] & 0xffffu : 0u) | (here && t + 1 < seg.T ? z[k] & 0xffff0000u : 0u);
+                            else z[k] = lo ? z[k] : 0u;
+                        }
+                    }
+                    big = z[0];
+#pragma unroll
+                    for (int k = 1; k < NG; ++k) big = max_bf16(big, z[k]);
+                }
+#pragma unroll
+                for (int d = 1; d < 8 * TS; d <<= 1) big = max_bf16(big, __shfl_xor_sync(0xffffffffu, big, d));
+                big = max_bf16(big, big >> 16) & 0xffffu;
+                if (TS < 4) big = __shfl_sync(0xffffffffu, big, 0);
+                const float E = big > 0x7f80u ? -60.f : (float)min(max((int)(big >> 7) - 127, -60), 100);
+
+                // ---- softmax ----
+                if (!whole) {
+#pragma unroll
+                    for (int tl = 0; tl < TS; ++tl)
+#pragma unroll
+                        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                            for (int i = 0; i < 4; ++i) {
+                                const int t = t0 + tl * kQ4Tile + g + (i >> 1) * 8;
+                                const bool see = t < vis[nt][i & 1] && ((have >> (step * TS + tl)) & 1);
+                                sc[tl][nt][i] = see ? sc[tl][nt][i] * fcol[nt][i & 1] : kMasked;
+                            }
+                } else {
+#pragma unroll
+                    for (int tl = 0; tl < TS; ++tl)
+#pragma unroll
+                        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                            for (int i = 0; i < 4; ++i) sc[tl][nt][i] *= fcol[nt][i & 1];
+                }
+                bool moved = false;
+                float corr[NT][2];
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                    for (int b = 0; b < 2; ++b) {
+                        float mx = fmaxf(sc[0][nt][b], sc[0][nt][b + 2]);
+#pragma unroll
+                        for (int tl = 1; tl < TS; ++tl) mx = fmaxf(mx, fmaxf(sc[tl][nt][b], sc[tl][nt][b + 2]));
+                        mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 4));
+                        mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 8));
+                        mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 16));
+                        const float Fn = mx > kNegInf ? fmaxf(F[nt][b], mx + E) : F[nt][b];
+                        corr[nt][b] = ex2(F[nt][b] - Fn);
+                        moved |= Fn != F[nt][b];
+                        F[nt][b] = Fn;
+                    }
+                if (__any_sync(0xffffffffu, moved)) {
+#pragma unroll
+                    for (int nt = 0; nt < NT; ++nt) {
+                        l[nt][0] *= corr[nt][0];
+                        l[nt][1] *= corr[nt][1];
+#pragma unroll
+                        for (int i = 0; i < 2 * NW; ++i)
+#pragma unroll
+                            for (int k = 0; k < 4; ++k) o[nt][i][k] *= corr[nt][k & 1];
+                    }
+                }
+#pragma unroll
+                for (int tl = 0; tl < TS; ++tl)
+#pragma unroll
+                    for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            sc[tl][nt][i] = ex2(sc[tl][nt][i] - F[nt][i & 1]);
+                            l[nt][i & 1] += sc[tl][nt][i];
+                        }
+                // ---- o^T += V^T (p * scale) ----
+#pragma unroll
+                for (int tl = 0; tl < TS; ++tl) {
+                    const unsigned char *tp = tp0 + tl * S::kTile, *vp = tp + q4_v_base(D), *vs = tp + q4_vs_base(D, NG);
+                    uint32_t s0[(NG + 1) / 2], s1[(NG + 1) / 2];
+                    if (NG == 4) {
+                        const uint2 x = *reinterpret_cast<const uint2 *>(vs + g * 8), y = *reinterpret_cast<const uint2 *>(vs + (g + 8) * 8);
+                        s0[0] = x.x; s0[(NG - 1) / 2] = x.y; s1[0] = y.x; s1[(NG - 1) / 2] = y.y;
+                    } else if (NG == 2) {
+                        s0[0] = *reinterpret_cast<const uint32_t *>(vs + g * 4); s1[0] = *reinterpret_cast<const uint32_t *>(vs + (g + 8) * 4);
+                    } else {
+                        s0[0] = *reinterpret_cast<const unsigned short *>(vs + g * 2); s1[0] = *reinterpret_cast<const unsigned short *>(vs + (g + 8) * 2);
+                    }
+                    // words of tokens 2c, 2c + 1, 2c + 8, 2c + 9: chunk g
+                    uint32_t wd[4][(NW + 1) / 2];
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const unsigned char *p = vp + q4_v_chunk(D, 2 * c + (i & 1) + (i >> 1) * 8, g);
+                        if (NW == 4) {
+                            const uint2 x = *reinterpret_cast<const uint2 *>(p);
+                            wd[i][0] = x.x; wd[i][(NW - 1) / 2] = x.y;
+                        } else {
+                            wd[i][0] = *reinterpret_cast<const uint32_t *>(p);
+                        }
+                    }
+#pragma unroll
+                    for (int k = 0; k < NG; ++k) {
+                        const float f0 = k & 1 ? bf16hi_f(s0[k / 2]) : bf16lo_f(s0[k / 2]), f1 = k & 1 ? bf16hi_f(s1[k / 2]) : bf16lo_f(s1[k / 2]);
+                        uint32_t b0[NT], b1[NT];
+#pragma unroll
+                        for (int nt = 0; nt < NT; ++nt) {
+                            const float *p = sc[tl][nt];
+                            float w0 = p[0] * f0, w1 = p[1] * f0, w2 = p[2] * f1, w3 = p[3] * f1;
+                            if (!whole) {                      // a weight of zero stays zero whatever the scale holds
+                                const int t = t0 + tl * kQ4Tile + g;
+                                const bool here = (have >> (step * TS + tl)) & 1;
+                                if (!(here && t < vis[nt][0])) w0 = 0.f;
+                                if (!(here && t < vis[nt][1])) w1 = 0.f;
+                                if (!(here && t + 8 < vis[nt][0])) w2 = 0.f;
+                                if (!(here && t + 8 < vis[nt][1])) w3 = 0.f;
+                            }
+                            b0[nt] = movmatrix(pack_f16(w0, w1));
+                            b1[nt] = movmatrix(pack_f16(w2, w3));
+                        }
+#pragma unroll
+                        for (int w = k * WPG; w < (k + 1) * WPG; ++w) {
+                            const uint32_t sel = w & 1 ? 0x7632u : 0x5410u;
+                            const uint32_t x = __byte_perm(wd[0][w / 2], wd[1][w / 2], sel), y = __byte_perm(wd[2][w / 2], wd[3][w / 2], sel);
+                            const uint32_t x8 = x >> 8, y8 = y >> 8;
+                            const uint32_t fa[4] = {sub_f16(and_or(x, 0x000f000fu, 0x64006400u), 0x64086408u), sub_f16(and_or(x, 0x00f000f0u, 0x54005400u), 0x54805480u),
+                                                    sub_f16(and_or(y, 0x000f000fu, 0x64006400u), 0x64086408u), sub_f16(and_or(y, 0x00f000f0u, 0x54005400u), 0x54805480u)};
+                            const uint32_t fb[4] = {sub_f16(and_or(x8, 0x000f000fu, 0x64006400u), 0x64086408u), sub_f16(and_or(x8, 0x00f000f0u, 0x54005400u), 0x54805480u),
+                                                    sub_f16(and_or(y8, 0x000f000fu, 0x64006400u), 0x64086408u), sub_f16(and_or(y8, 0x00f000f0u, 0x54005400u), 0x54805480u)};
+#pragma unroll
+                            for (int nt = 0; nt < NT; ++nt) {
+                                mma_f16(o[nt][2 * w], fa, b0[nt], b1[nt], o[nt][2 * w]);
+                                mma_f16(o[nt][2 * w + 1], fb, b0[nt], b1[nt], o[nt][2 * w + 1]);
+                            }
+                        }
+                    }
+                }
+            }
+            __syncwarp();
+            if (++st_out == kSt) { st_out = 0; ++phase; }
+            at += kQ4Warps;
+            if (at < seg_hi) fetch();                          // into the stage just read (the segment's last one is kept for the states)
+        }
+
+        // ---- join the warps' states ----
+        const int st_free = st_out == 0 ? kSt - 1 : st_out - 1;
+        float *mine = reinterpret_cast<float *>(smem + (warp * kSt + st_free) * S::kStage);
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+            for (int b = 0; b < 2; ++b) {
+                float v = l[nt][b];
+                v += __shfl_xor_sync(0xffffffffu, v, 4);
+                v += __shfl_xor_sync(0xffffffffu, v, 8);
+                v += __shfl_xor_sync(0xffffffffu, v, 16);
+                if (g == 0) ml[warp][nt * 8 + 2 * c + b] = make_float2(F[nt][b], any ? v : 0.f);
+                if (any)
+#pragma unroll
+                    for (int w = 0; w < NW; ++w)
+                        *reinterpret_cast<float4 *>(mine + (nt * 8 + 2 * c + b) * S::kRowFloats + 32 * w + 4 * g) =
+                            make_float4(o[nt][2 * w][b], o[nt][2 * w][2 + b], o[nt][2 * w + 1][b], o[nt][2 * w + 1][2 + b]);
+            }
+        if (lane == 0) offs[warp] = any ? (warp * kSt + st_free) * S::kStage : -1;
+        __syncthreads();
+        {
+            const bool starts = seg.unit == 0, ends = seg_hi - seg_lo == seg.units - seg.unit;
+            const bool complete = starts && ends;
+            const int slot = seg_lo == 0 ? 0 : 1;
+            float *part = states + (2LL * blockIdx.x + slot) * q4_state_floats(R, D);
+            for (int i = tid; i < R * (D / 4); i += kQ4Threads) {
+                const int r = i / (D / 4), ch = i % (D / 4) * 4;
+                float M = kNegInf;
+#pragma unroll
+                for (int w = 0; w < kQ4Warps; ++w) M = fmaxf(M, ml[w][r].x);
+                float L = 0.f;
+                float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+                for (int w = 0; w < kQ4Warps; ++w) {
+                    const int off = offs[w];
+                    if (off < 0) continue;
+                    const float f = ex2(ml[w][r].x - M);
+                    const float4 x = *reinterpret_cast<const float4 *>(smem + off + (r * S::kRowFloats + ch) * 4);
+                    L += f * ml[w][r].y;
+                    acc.x += f * x.x; acc.y += f * x.y; acc.z += f * x.z; acc.w += f * x.w;
+                }
+                if (!complete) {
+                    *reinterpret_cast<float4 *>(part + r * D + ch) = acc;
+                    if (ch == 0) { part[R * D + r] = M; part[R * D + R + r] = L; }
+                    continue;
+                }
+                const int row = seg.tile * R + r, j = row / G;
+                if (j >= n) continue;
+                const int h = seg.head * G + row - j * G;
+                if (a.state) {
+                    float *dst = a.state + ((long long)(first + j) * geo.n_q_heads + h) * (D + 2);
+                    *reinterpret_cast<float2 *>(dst + ch) = make_float2(acc.x, acc.y);
+                    *reinterpret_cast<float2 *>(dst + ch + 2) = make_float2(acc.z, acc.w);
+                    if (ch == 0) *reinterpret_cast<float2 *>(dst + D) = make_float2(M, L);
+                } else {
+                    const float inv = L != 0.f ? 1.f / L : 0.f;
+                    const uint2 v = H16 ? make_uint2(pack_f16(acc.x * inv, acc.y * inv), pack_f16(acc.z * inv, acc.w * inv))
+                                        : make_uint2(pack_bf16(acc.x * inv, acc.y * inv), pack_bf16(acc.z * inv, acc.w * inv));
+                    *reinterpret_cast<uint2 *>(reinterpret_cast<unsigned short *>(a.out) + (long long)(first + j) * a.out_row +
+                                               (long long)h * a.out_head + ch) = v;
+                }
+            }
+            if (tid == 0 && gridDim.x > 1 && seg_hi == left_cta) {
+                // the CTA's last segment: does it begin here and go on elsewhere?
+                Q4Part p{-1, 0, 0, 0, 0};
+                if (starts && !ends) {
+                    const long long w1 = begin + seg_lo + seg.units;          // one past the segment's last unit
+                    p = Q4Part{seg.seq, seg.tile, seg.head, slot, (int)((w1 * n_ctas - 1) / total)};
+                }
+                parts[blockIdx.x] = p;
+            }
+        }
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");      // the stages go back to the copies
+        __syncthreads();
+        if (any) fetch();
+        seg_lo = seg_hi;
+        if (seg_lo < left_cta) {
+            const int by = seg.units - seg.unit;
+            q4_advance(a, R, seg, by);
+        }
+    }
+    if (timed_out)                                             // copies still in flight must land before the CTA retires
+        for (int i = 0; i < kSt; ++i) (void)mbar_wait(smem_u32(&bars[warp][(lost + i) % kSt]), ((lost + i) / kSt) & 1);
+}
+
+// Joins the states of the segments that span CTAs: block b takes the one that begins in CTA b, in token order.
+template <int D, bool H16>
+__global__ void __launch_bounds__(128) q4_join_kernel(const __grid_constant__ Q4AttentionArgs a, int R) {
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    const Q4Geometry &geo = a.geo;
+    const int b = blockIdx.x;
+    const Q4Part p = reinterpret_cast<const Q4Part *>(a.workspace)[b];
+    if (p.seq < 0) return;
+    const float *states = reinterpret_cast<const float *>(a.workspace + q4_parts_bytes(gridDim.x));
+    const long long per = q4_state_floats(R, D);
+    // CTA b left it in slot 1 unless it is the CTA's only segment; the CTAs behind it in slot 0
+    int first, all;
+    const int n = q4_new_rows(a, p.seq, first, all, nullptr), G = geo.group;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    for (int r = blockIdx.y * 4 + warp; r < R; r += 4 * gridDim.y) {
+        const int row = p.tile * R + r, j = row / G;
+        if (j >= n) break;
+        const int slot0 = p.slot, last = p.last_cta;
+        float M = kNegInf;
+        for (int k = b + lane; k <= last; k += 32) {
+            const float *s = states + (2LL * k + (k == b ? slot0 : 0)) * per;
+            M = fmaxf(M, s[R * D + r]);
+        }
+#pragma unroll
+        for (int d = 16; d; d >>= 1) M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, d));
+        float L = 0.f, acc[D / 32];
+#pragma unroll
+        for (int i = 0; i < D / 32; ++i) acc[i] = 0.f;
+#pragma unroll 4
+        for (int k = b; k <= last; ++k) {
+            const float *s = states + (2LL * k + (k == b ? slot0 : 0)) * per;
+            const float f = ex2(s[R * D + r] - M);
+            L += f * s[R * D + R + r];
+            if (D == 128) {
+                const float4 x = *reinterpret_cast<const float4 *>(s + r * D + 4 * lane);
+                acc[0] += f * x.x; acc[1] += f * x.y; acc[D / 32 - 2] += f * x.z; acc[D / 32 - 1] += f * x.w;
+            } else {
+                const float2 x = *reinterpret_cast<const float2 *>(s + r * D + 2 * lane);
+                acc[0] += f * x.x; acc[1] += f * x.y;
+            }
+        }
+        const int h = p.head * G + row - j * G;
+        if (a.state) {
+            float *dst = a.state + ((long long)(first + j) * geo.n_q_heads + h) * (D + 2);
+#pragma unroll
+            for (int i = 0; i < D / 64; ++i) *reinterpret_cast<float2 *>(dst + D / 32 * lane + 2 * i) = make_float2(acc[2 * i], acc[2 * i + 1]);
+            if (lane == 0) *reinterpret_cast<float2 *>(dst + D) = make_float2(M, L);
+        } else {
+            const float inv = L != 0.f ? 1.f / L : 0.f;
+            uint32_t *dst = reinterpret_cast<uint32_t *>(reinterpret_cast<unsigned short *>(a.out) + (long long)(first + j) * a.out_row +
+                                                         (long long)h * a.out_head + D / 32 * lane);
+#pragma unroll
+            for (int i = 0; i < D / 64; ++i)
+                dst[i] = H16 ? pack_f16(acc[2 * i] * inv, acc[2 * i + 1] * inv) : pack_bf16(acc[2 * i] * inv, acc[2 * i + 1] * inv);
+        }
+    }
+}
+
+int q4_rows_per_tile(const Q4Geometry &g, int max_q_len) { return (long long)max_q_len * g.group <= 8 ? 8 : 16; }
+
+// CTAs of a launch: enough units for every warp of each, as far as the host can tell.
+int q4_grid(const Q4Geometry &g, int n_seqs, int max_q_len, int max_len) {
+    const int R = q4_rows_per_tile(g, max_q_len);
+    const long long tiles = ((long long)max_q_len * g.group + R - 1) / R, units = (max_len + kQ4Unit - 1) / kQ4Unit;
+    const double all = (double)n_seqs * g.n_kv_heads * tiles * units / kQ4Warps;
+    return all >= g.n_ctas ? g.n_ctas : all < 1 ? 1 : (int)all;
+}
+
+#define PKV_Q4_SHAPES(X) X(128, 4) X(128, 2) X(128, 1) X(64, 2) X(64, 1)
 
 }  // namespace
 
-cudaError_t q4_attention_setup() { return cudaSuccess; }
+cudaError_t q4_attention_setup() {
+    cudaError_t e;
+#define PKV_Q4_SETUP1(D, NG, H16, NT) \
+    if ((e = cudaFuncSetAttribute(q4_decode_kernel<D, NG, H16, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, Q4Shape<D, NG, NT>::kSmem)) != cudaSuccess) return e;
+#define PKV_Q4_SETUP(D, NG) PKV_Q4_SETUP1(D, NG, false, 1) PKV_Q4_SETUP1(D, NG, false, 2) PKV_Q4_SETUP1(D, NG, true, 1) PKV_Q4_SETUP1(D, NG, true, 2)
+    PKV_Q4_SHAPES(PKV_Q4_SETUP)
+    return cudaSuccess;
+}
 
-long long q4_attention_workspace(const Q4Geometry &, int, int, int) { return 0; }
+long long q4_attention_workspace(const Q4Geometry &g, int n_seqs, int max_q_len, int max_len) {
+    const int n = q4_grid(g, n_seqs, max_q_len, max_len);
+    return n <= 1 ? 0 : q4_parts_bytes(n) + 2LL * n * q4_state_floats(q4_rows_per_tile(g, max_q_len), g.head_dim) * 4;
+}
 
 cudaError_t launch_q4_attention(const Q4AttentionArgs &a, cudaStream_t st) {
-    q4_simple_kernel<<<dim3((a.max_q_len + 3) / 4, a.rows.n_seqs, a.geo.n_q_heads), 128, 0, st>>>(a);
-    return cudaGetLastError();
+    const Q4Geometry &g = a.geo;
+    const int n = q4_grid(g, a.rows.n_seqs, a.max_q_len, a.max_len), R = q4_rows_per_tile(g, a.max_q_len);
+    cudaLaunchAttribute at[1];
+    at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    at[0].val.programmaticStreamSerializationAllowed = 1;
+    cudaLaunchConfig_t cfg = {};
+    cfg.stream = st;
+    cfg.attrs = at;
+    cfg.numAttrs = 1;
+    cudaError_t e = cudaErrorInvalidValue;
+#define PKV_Q4_LAUNCH1(D, NG, H, NT)                                        \
+    if ((g.fp16 != 0) == H && R == 8 * NT) {                                \
+        cfg.gridDim = dim3(n);                                              \
+        cfg.blockDim = dim3(kQ4Threads);                                    \
+        cfg.dynamicSmemBytes = Q4Shape<D, NG, NT>::kSmem;                   \
+        e = cudaLaunchKernelEx(&cfg, q4_decode_kernel<D, NG, H, NT>, a);    \
+    }
+#define PKV_Q4_LAUNCH(D, NG)                                                                     \
+    if (g.head_dim == D && g.groups == NG) {                                                     \
+        PKV_Q4_LAUNCH1(D, NG, false, 1) PKV_Q4_LAUNCH1(D, NG, false, 2)                          \
+        PKV_Q4_LAUNCH1(D, NG, true, 1) PKV_Q4_LAUNCH1(D, NG, true, 2)                            \
+    }
+    PKV_Q4_SHAPES(PKV_Q4_LAUNCH)
+    if (e != cudaSuccess || n <= 1) return e;
+    cfg.gridDim = dim3(n, R / 8);
+    cfg.blockDim = dim3(128);
+    cfg.dynamicSmemBytes = 0;
+    if (g.head_dim == 128)
+        e = g.fp16 ? cudaLaunchKernelEx(&cfg, q4_join_kernel<128, true>, a, R) : cudaLaunchKernelEx(&cfg, q4_join_kernel<128, false>, a, R);
+    else
+        e = g.fp16 ? cudaLaunchKernelEx(&cfg, q4_join_kernel<64, true>, a, R) : cudaLaunchKernelEx(&cfg, q4_join_kernel<64, false>, a, R);
+    return e;
 }
 
 }  // namespace pkv

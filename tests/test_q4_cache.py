@@ -341,6 +341,28 @@ def test_spread_over_few_and_many_ctas(n_ctas, n, G):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("n, G", [(1, 4), (3, 8), (64, 4)])
+@pytest.mark.parametrize("fill", [0xff, 0x00, 0x7b])
+@pytest.mark.parametrize("lens", [[90, 0, 200], [1, 1, 1], [700, 64, 100]])
+def test_what_the_workspace_held_does_not_matter(n, G, fill, lens):
+    """Sequences far shorter than the table allows, so that CTAs of the launch stay without work; the scratch is full of
+    NaN, zeros, large numbers."""
+    lens = [max(n, t) if t else 0 for t in lens]
+    f = Filled(lens, G=G, H=2, P=16, seed=17)
+    table = torch.nn.functional.pad(f.table, (0, 300 - f.table.shape[1])).contiguous()
+    qs = f.queries([n] * 3)
+    q = torch.stack(qs).cuda()
+    out = torch.empty_like(q)
+    size = pkv.pkv_q4_attention_workspace(f.cache.handle, 3, n, 4800)
+    work = torch.full((max(16, size),), fill, dtype=torch.uint8, device="cuda")
+    strides = (2 * G * 128, 128)
+    pkv.pkv_q4_attention(f.cache.handle, 3, table, 300, f.lengths, 3 * n, None, n, 4800, q, strides, out, strides, None, work, size,
+                         torch.cuda.current_stream())
+    for s in range(3):
+        check(out[s], *f.expected(qs[s], s)[::2])
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("shape", SHAPES[:4], ids=str)
 @pytest.mark.parametrize("ns", [[0, 1, 5, 0, 33], [3, 0, 0, 0, 0], [1, 1, 1, 1, 1], [100, 1, 2, 150, 300]])
 def test_ragged_rows(shape, ns):
