@@ -6,9 +6,10 @@
 // o^T += V^T p, so that eight query rows (NT = 1) fill the column dimension of one m16n8k16 product:
 //   K codes become fp16 operands by masking alone: code + 8 in the low bits of a 16-bit word is an fp16 subnormal,
 //     (code + 8) 2^-24 exactly, and in bits 4-7 that times 16 (the queries of those channels are divided by 16).  The + 8
-//     is taken away by the accumulators' start value -8 * sum(q).  Each group's product is multiplied by its scale in fp32.
-//   V codes become fp16 integers (magic constants 1024 and 64, then one packed subtraction); the scales go to the weights,
-//     p * scale, rounded once to fp16.  To keep that inside fp16's range whatever the values' size, the running reference
+//     is taken away for all groups at once by one product of the scales with -8 * sum(q).  Each group's product is
+//     multiplied by its scale in fp32.
+//   V codes become exact fp16 integers (a constant's exponent, then one packed subtraction; as subnormals they would lose the
+//     contributions of small weights next to a large one's + 8); the scales go to the weights, p * scale, rounded once to fp16.  To keep that inside fp16's range whatever the values' size, the running reference
 //     of the softmax is max(s) + E with E the exponent of the largest value scale of the step: p * scale <= 2 then.
 //   Queries are brought to fp16 with a power of two per row, which is exact for bf16 and fp16 alike.
 // Every warp of a CTA walks its own units of 64 tokens with its own ring of bulk copies, and keeps (m, l, o) in registers;
@@ -17,6 +18,8 @@
 // workspace and a second kernel joins them in token order.
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
+
+#include <type_traits>
 
 #include "pkv_q4.h"
 #include "pkv_device.cuh"
@@ -59,6 +62,14 @@ __device__ __forceinline__ void mma_f16(float *d, const uint32_t *a, uint32_t b0
         : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3])
         : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1), "f"(c[0]), "f"(c[1]), "f"(c[2]), "f"(c[3]));
 }
+__device__ __forceinline__ void mma_bf16_k16(float *d, const uint32_t *a, uint32_t b0, uint32_t b1) {      // d = a b
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%10, %10, %10, %10};"
+        : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1), "f"(0.f));
+}
+__device__ __forceinline__ void mma_bf16_k8(float *d, uint32_t a0, uint32_t a1, uint32_t b0) {
+    asm("mma.sync.aligned.m16n8k8.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5}, {%6}, {%7, %7, %7, %7};"
+        : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3]) : "r"(a0), "r"(a1), "r"(b0), "f"(0.f));
+}
 __device__ __forceinline__ uint32_t movmatrix(uint32_t x) {
     uint32_t y;
     asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
@@ -74,21 +85,52 @@ __device__ __forceinline__ uint32_t pack_f16(float lo, float hi) {
     asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
     return r;
 }
-__device__ __forceinline__ uint32_t sub_f16(uint32_t x, uint32_t y) {
-    uint32_t r;
-    asm("sub.rn.f16x2 %0, %1, %2;" : "=r"(r) : "r"(x), "r"(y));
-    return r;
-}
 __device__ __forceinline__ uint32_t max_bf16(uint32_t x, uint32_t y) {      // (the other operand where one is NaN)
     uint32_t r;
     asm("max.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(x), "r"(y));
     return r;
 }
-// (x & mask) | bits in one instruction
-__device__ __forceinline__ uint32_t and_or(uint32_t x, uint32_t mask, uint32_t bits) {
+// Two codes as fp16 integers -7 .. 7, from bits 0-3 or 4-7 of either half: under an exponent that puts their last bit at 1
+// they read 1024 + 8 + code or 64 + 8 + code, and the difference is exact.
+__device__ __forceinline__ uint32_t code_lo(uint32_t x) {
     uint32_t r;
-    asm("lop3.b32 %0, %1, %2, %3, 0xEA;" : "=r"(r) : "r"(x), "r"(mask), "r"(bits));
+    asm("{\n\t.reg .b32 t;\n\tlop3.b32 t, %1, 0x000f000f, 0x64006400, 0xEA;\n\tsub.rn.f16x2 %0, t, %2;\n\t}" : "=r"(r) : "r"(x), "r"(0x64086408u));
     return r;
+}
+__device__ __forceinline__ uint32_t code_hi(uint32_t x) {
+    uint32_t r;
+    asm("{\n\t.reg .b32 t;\n\tlop3.b32 t, %1, 0x00f000f0, 0x54005400, 0xEA;\n\tsub.rn.f16x2 %0, t, %2;\n\t}" : "=r"(r) : "r"(x), "r"(0x54805480u));
+    return r;
+}
+// two fp32 values at once
+__device__ __forceinline__ uint64_t f2(float lo, float hi) {
+    uint64_t v;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(v) : "f"(lo), "f"(hi));
+    return v;
+}
+__device__ __forceinline__ void f2_split(uint64_t v, float &lo, float &hi) { asm("mov.b64 {%0, %1}, %2;" : "=f"(lo), "=f"(hi) : "l"(v)); }
+__device__ __forceinline__ uint64_t f2_fma(uint64_t a, uint64_t b, uint64_t c) {
+    uint64_t d;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(a), "l"(b), "l"(c));
+    return d;
+}
+__device__ __forceinline__ uint64_t f2_sum(uint64_t a, uint64_t b) {
+    uint64_t d;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+    return d;
+}
+
+// a lane's scales of rows g and g + 8: bf16, two to a word (one group: one in the low half)
+template <int NG>
+__device__ __forceinline__ void q4_scales(const unsigned char *p, int g, uint32_t *s0, uint32_t *s1) {
+    if (NG == 4) {
+        const uint2 x = *reinterpret_cast<const uint2 *>(p + g * 8), y = *reinterpret_cast<const uint2 *>(p + (g + 8) * 8);
+        s0[0] = x.x; s0[(NG - 1) / 2] = x.y; s1[0] = y.x; s1[(NG - 1) / 2] = y.y;
+    } else if (NG == 2) {
+        s0[0] = *reinterpret_cast<const uint32_t *>(p + g * 4); s1[0] = *reinterpret_cast<const uint32_t *>(p + (g + 8) * 4);
+    } else {
+        s0[0] = *reinterpret_cast<const unsigned short *>(p + g * 2); s1[0] = *reinterpret_cast<const unsigned short *>(p + (g + 8) * 2);
+    }
 }
 
 // Where a warp's next unit is: positions in the batch's order of units (sequence, row tile, head, unit of 64 tokens).
@@ -226,16 +268,16 @@ __global__ void __launch_bounds__(kQ4Threads, 2) q4_decode_kernel(const __grid_c
     int st_in = 0;
     auto fetch = [&]() {
         if (nx_at >= left_cta || timed_out) return;
-        const int t0 = nx.unit * kQ4Unit + lane * per_page;
-        const int toks = lane < n_parts ? max(0, min(per_page, nx.T - t0)) : 0;
-        const int tiles = (toks + kQ4Tile - 1) / kQ4Tile;
-        const bool ok = tiles > 0 && pg >= 0 && pg < geo.n_pages;
-        if (tiles > 0 && !ok) atomicAdd(a.status + 1, 1);
-        const int per_tiles = per_page / kQ4Tile;
-        uint32_t bits = ok ? ((1u << tiles) - 1u) << (lane * per_tiles) : 0u;
-        bits |= __shfl_xor_sync(0xffffffffu, bits, 1);
-        bits |= __shfl_xor_sync(0xffffffffu, bits, 2);
-        bits = __shfl_sync(0xffffffffu, bits, 0);
+        const int t0 = nx.unit * kQ4Unit, all_tiles = (max(0, min(kQ4Unit, nx.T - t0)) + kQ4Tile - 1) / kQ4Tile;
+        const int per_tiles = per_page / kQ4Tile, tiles = min(max(all_tiles - lane * per_tiles, 0), per_tiles);       // (lanes past the unit: 0)
+        const bool ok = tiles > 0 && (unsigned)pg < (unsigned)geo.n_pages;
+        uint32_t bits = (1u << all_tiles) - 1u;
+        const uint32_t bad = __ballot_sync(0xffffffffu, tiles > 0 && !ok);
+        if (bad) {
+            if (lane == 0) atomicAdd(a.status + 1, __popc(bad));
+            for (int i = 0; i < n_parts; ++i)
+                if (bad >> i & 1) bits &= ~(((1u << per_tiles) - 1u) << (i * per_tiles));
+        }
         const uint32_t bar = smem_u32(&bars[warp][st_in]);
         if (lane == 0) {
             if (bits) mbar_arrive_expect_tx(bar, __popc(bits) * S::kTile);
@@ -255,6 +297,7 @@ __global__ void __launch_bounds__(kQ4Threads, 2) q4_decode_kernel(const __grid_c
 #pragma unroll 1
     for (int s = 0; s < kSt; ++s) fetch();
 
+    const int v_at[4] = {q4_v_chunk(D, 2 * c, g), q4_v_chunk(D, 2 * c + 1, g), q4_v_chunk(D, 2 * c + 8, g), q4_v_chunk(D, 2 * c + 9, g)};
     int at = warp;                                             // this warp's next unit, within the CTA's units
     int seg_lo = 0;                                            // the segment's first unit, within the CTA's units
     int st_out = 0, phase = 0;
@@ -265,7 +308,9 @@ __global__ void __launch_bounds__(kQ4Threads, 2) q4_decode_kernel(const __grid_c
         int first, all;
         const int n = q4_new_rows(a, seg.seq, first, all, nullptr), G = geo.group;
         uint32_t qf[NT][NW][4];
-        float start[NT][NG][2], fcol[NT][2], F[NT][2], l[NT][2], o[NT][2 * NW][4];
+        uint32_t bias[NT][2];
+        float F[NT][2], o[NT][2 * NW][4];
+        uint64_t fcol[NT], l[NT];                              // (columns 2c, 2c + 1)
         int vis[NT][2];
         int vis_all = seg.T;                                   // tokens every row of the tile sees
 #pragma unroll
@@ -309,25 +354,46 @@ __global__ void __launch_bounds__(kQ4Threads, 2) q4_decode_kernel(const __grid_c
                     const float2 r = __half22float2(*reinterpret_cast<const __half2 *>(&qf[nt][w][i]));
                     sum[w / WPG] += (r.x + r.y) * (i & 1 ? 16.f : 1.f);
                 }
-            // per column: the accumulators' start value and the factor of the scores, from the lanes that hold the row
-            const float fr = 16384.f * __uint_as_float((uint32_t)(e + 127) << 23) * scale;      // 2^24 / up
+            // -8 * sum(q) per group, to be multiplied by the tokens' scales in one product: as a column operand of three bf16
+            // terms, k = group + NG * term
+            const float fr = 16384.f * __uint_as_float((uint32_t)(e + 127) << 23) * scale;      // 2^24 / up: the factor of the scores
+            uint32_t term[3][NG];
 #pragma unroll
             for (int k = 0; k < NG; ++k) {
                 sum[k] += __shfl_xor_sync(0xffffffffu, sum[k], 1);
                 sum[k] += __shfl_xor_sync(0xffffffffu, sum[k], 2);
-                sum[k] *= -8.f / 16777216.f;
+                float left = sum[k] * (-8.f / 16777216.f);
+#pragma unroll
+                for (int t = 0; t < 3; ++t) {
+                    term[t][k] = pack_bf16(left, 0.f);
+                    left -= bf16lo_f(term[t][k]);
+                }
             }
+            if (NG == 4) {
+                // b0: term c / 2, groups 2 (c & 1) and + 1; b1: term 2 for c < 2
+                const uint32_t x0 = c & 1 ? term[0][NG / 2] | term[0][NG - 1] << 16 : term[0][0] | term[0][NG / 4] << 16;
+                const uint32_t x1 = c & 1 ? term[1][NG / 2] | term[1][NG - 1] << 16 : term[1][0] | term[1][NG / 4] << 16;
+                const uint32_t x2 = c & 1 ? term[2][NG / 2] | term[2][NG - 1] << 16 : term[2][0] | term[2][NG / 4] << 16;
+                bias[nt][0] = c & 2 ? x1 : x0;
+                bias[nt][1] = c & 2 ? 0u : x2;
+            } else {
+                // term c (none for c = 3), groups 0 and 1
+                const uint32_t lo = c == 0 ? term[0][0] : c == 1 ? term[1][0] : c == 2 ? term[2][0] : 0u;
+                const uint32_t hi = NG == 1 ? 0u : c == 0 ? term[0][NG - 1] : c == 1 ? term[1][NG - 1] : c == 2 ? term[2][NG - 1] : 0u;
+                bias[nt][0] = lo | hi << 16;
+                bias[nt][1] = 0u;
+            }
+            float fb[2];
 #pragma unroll
             for (int b = 0; b < 2; ++b) {
                 const int col = 2 * c + b, r2 = seg.tile * R + nt * 8 + col, j2 = r2 / G;
-#pragma unroll
-                for (int k = 0; k < NG; ++k) start[nt][k][b] = __shfl_sync(0xffffffffu, sum[k], 4 * col);
-                fcol[nt][b] = __shfl_sync(0xffffffffu, fr, 4 * col);
+                fb[b] = __shfl_sync(0xffffffffu, fr, 4 * col);
                 vis[nt][b] = j2 < n ? seg.T - all + j2 + 1 : seg.T;
                 vis_all = min(vis_all, vis[nt][b]);
                 F[nt][b] = kNegInf;
-                l[nt][b] = 0.f;
             }
+            fcol[nt] = f2(fb[0], fb[1]);
+            l[nt] = f2(0.f, 0.f);
 #pragma unroll
             for (int i = 0; i < 2 * NW; ++i)
 #pragma unroll
@@ -348,10 +414,12 @@ __global__ void __launch_bounds__(kQ4Threads, 2) q4_decode_kernel(const __grid_c
             const uint32_t have = timed_out ? 0u : (vm >> (4 * st_out)) & 15u;
             const bool whole = have == 15u && t_unit + kQ4Unit <= vis_all;
             const unsigned char *sp = ring_p + st_out * S::kStage;
-#pragma unroll 1
-            for (int step = 0; step < 4 / TS; ++step) {
+            // One softmax step over TS tiles; kMask: some of its tokens are hidden from some row, or not there.
+            auto work = [&](int step, auto masked) {
+                constexpr bool kMask = decltype(masked)::value;
                 const unsigned char *tp0 = sp + step * TS * S::kTile;
                 const int t0 = t_unit + step * TS * kQ4Tile;
+                const uint32_t here = have >> (step * TS);
                 float sc[TS][NT][4];
                 // ---- scores ----
 #pragma unroll
@@ -366,27 +434,25 @@ __global__ void __launch_bounds__(kQ4Threads, 2) q4_decode_kernel(const __grid_c
                         const uint2 x = *reinterpret_cast<const uint2 *>(tp + q4_k_chunk(D, g, c)), y = *reinterpret_cast<const uint2 *>(tp + q4_k_chunk(D, g + 8, c));
                         k0[0] = x.x; k0[1] = x.y; k1[0] = y.x; k1[1] = y.y;
                     }
-                    const unsigned char *ks = tp + q4_ks_base(D);
+                    q4_scales<NG>(tp + q4_ks_base(D), g, s0, s1);
+                    // sum over the groups of scale * (-8 sum(q)): the scales, as stored, are the row operand
                     if (NG == 4) {
-                        const uint2 x = *reinterpret_cast<const uint2 *>(ks + g * 8), y = *reinterpret_cast<const uint2 *>(ks + (g + 8) * 8);
-                        s0[0] = x.x; s0[(NG - 1) / 2] = x.y; s1[0] = y.x; s1[(NG - 1) / 2] = y.y;
-                    } else if (NG == 2) {
-                        s0[0] = *reinterpret_cast<const uint32_t *>(ks + g * 4); s1[0] = *reinterpret_cast<const uint32_t *>(ks + (g + 8) * 4);
+                        const unsigned char *ks = tp + q4_ks_base(D) + 4 * (c & 1);
+                        const uint32_t x = *reinterpret_cast<const uint32_t *>(ks + g * 8), y = *reinterpret_cast<const uint32_t *>(ks + (g + 8) * 8);
+                        const uint32_t sa[4] = {x, y, x, y};
+#pragma unroll
+                        for (int nt = 0; nt < NT; ++nt) mma_bf16_k16(sc[tl][nt], sa, bias[nt][0], bias[nt][1]);
                     } else {
-                        s0[0] = *reinterpret_cast<const unsigned short *>(ks + g * 2); s1[0] = *reinterpret_cast<const unsigned short *>(ks + (g + 8) * 2);
+#pragma unroll
+                        for (int nt = 0; nt < NT; ++nt) mma_bf16_k8(sc[tl][nt], s0[0], s1[0], bias[nt][0]);
                     }
-#pragma unroll
-                    for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) sc[tl][nt][i] = 0.f;
 #pragma unroll
                     for (int k = 0; k < NG; ++k) {
                         float acc[NT][4];
 #pragma unroll
-                        for (int nt = 0; nt < NT; ++nt) {
-                            acc[nt][0] = acc[nt][2] = start[nt][k][0];
-                            acc[nt][1] = acc[nt][3] = start[nt][k][1];
-                        }
+                        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                            for (int i = 0; i < 4; ++i) acc[nt][i] = 0.f;
 #pragma unroll
                         for (int w = k * WPG; w < (k + 1) * WPG; ++w) {
                             const uint32_t x0 = k0[w] >> 8, x1 = k1[w] >> 8;
@@ -405,29 +471,36 @@ __global__ void __launch_bounds__(kQ4Threads, 2) q4_decode_kernel(const __grid_c
                             sc[tl][nt][2] += f1 * acc[nt][2]; sc[tl][nt][3] += f1 * acc[nt][3];
                         }
                     }
+                    if (kMask)
+#pragma unroll
+                        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                            for (int i = 0; i < 4; ++i) {
+                                const int t = t0 + tl * kQ4Tile + g + (i >> 1) * 8;
+                                if (!(t < vis[nt][i & 1] && ((here >> tl) & 1))) sc[tl][nt][i] = -INFINITY;
+                            }
                 }
                 // ---- E: exponent of the step's largest value scale (lane: tokens 2 lane, 2 lane + 1 of the step) ----
                 uint32_t big = 0;
-                if (lane < 8 * TS) {
+                if (TS == 4 || lane < 8 * TS) {
                     const int tl = lane >> 3, t2 = 2 * (lane & 7), t = t0 + tl * kQ4Tile + t2;
                     const unsigned char *vs = tp0 + tl * S::kTile + q4_vs_base(D, NG) + t2 * NG * 2;
                     uint32_t z[NG];
                     if (NG == 4) {
                         const uint4 x = *reinterpret_cast<const uint4 *>(vs);
-                        z[0] = x.x; z[NG > 1] = x.y; z[NG - 2 >= 0 ? NG - 2 : 0] = x.z; z[NG - 1] = x.w;
+                        z[0] = x.x; z[NG / 4] = x.y; z[NG / 2] = x.z; z[NG - 1] = x.w;
                     } else if (NG == 2) {
                         const uint2 x = *reinterpret_cast<const uint2 *>(vs);
                         z[0] = x.x; z[NG - 1] = x.y;
                     } else {
                         z[0] = *reinterpret_cast<const uint32_t *>(vs);
                     }
-                    if (!whole) {                              // rows past the end or on a page that is not there
-                        const bool here = (have >> (step * TS + tl)) & 1;
+                    if (kMask) {                               // rows past the end or on a page that is not there
+                        const bool ok = (here >> tl) & 1;
 #pragma unroll
                         for (int k = 0; k < NG; ++k) {
-                            const bool lo = here && t + (NG == 1 ? 0 : k / ((NG + 1) / 2)) < seg.T;
-                            if (NG == 1) z[k] = (here && t < seg.T ? z[k] & 0xffffu : 0u) | (here && t + 1 < seg.T ? z[k] & 0xffff0000u : 0u);
-                            else z[k] = lo ? z[k] : 0u;
+                            if (NG == 1) z[k] = (ok && t < seg.T ? z[k] & 0xffffu : 0u) | (ok && t + 1 < seg.T ? z[k] & 0xffff0000u : 0u);
+                            else z[k] = ok && t + k / ((NG + 1) / 2) < seg.T ? z[k] : 0u;
                         }
                     }
                     big = z[0];
@@ -441,29 +514,12 @@ __global__ void __launch_bounds__(kQ4Threads, 2) q4_decode_kernel(const __grid_c
                 const float E = big > 0x7f80u ? -60.f : (float)min(max((int)(big >> 7) - 127, -60), 100);
 
                 // ---- softmax ----
-                if (!whole) {
-#pragma unroll
-                    for (int tl = 0; tl < TS; ++tl)
-#pragma unroll
-                        for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-                            for (int i = 0; i < 4; ++i) {
-                                const int t = t0 + tl * kQ4Tile + g + (i >> 1) * 8;
-                                const bool see = t < vis[nt][i & 1] && ((have >> (step * TS + tl)) & 1);
-                                sc[tl][nt][i] = see ? sc[tl][nt][i] * fcol[nt][i & 1] : kMasked;
-                            }
-                } else {
-#pragma unroll
-                    for (int tl = 0; tl < TS; ++tl)
-#pragma unroll
-                        for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-                            for (int i = 0; i < 4; ++i) sc[tl][nt][i] *= fcol[nt][i & 1];
-                }
                 bool moved = false;
                 float corr[NT][2];
 #pragma unroll
-                for (int nt = 0; nt < NT; ++nt)
+                for (int nt = 0; nt < NT; ++nt) {
+                    float fc[2];
+                    f2_split(fcol[nt], fc[0], fc[1]);
 #pragma unroll
                     for (int b = 0; b < 2; ++b) {
                         float mx = fmaxf(sc[0][nt][b], sc[0][nt][b + 2]);
@@ -472,16 +528,18 @@ __global__ void __launch_bounds__(kQ4Threads, 2) q4_decode_kernel(const __grid_c
                         mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 4));
                         mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 8));
                         mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 16));
-                        const float Fn = mx > kNegInf ? fmaxf(F[nt][b], mx + E) : F[nt][b];
+                        const float Fn = mx > kNegInf ? fmaxf(F[nt][b], fmaf(mx, fc[b], E)) : F[nt][b];
                         corr[nt][b] = ex2(F[nt][b] - Fn);
                         moved |= Fn != F[nt][b];
                         F[nt][b] = Fn;
                     }
+                }
                 if (__any_sync(0xffffffffu, moved)) {
 #pragma unroll
                     for (int nt = 0; nt < NT; ++nt) {
-                        l[nt][0] *= corr[nt][0];
-                        l[nt][1] *= corr[nt][1];
+                        float x, y;
+                        f2_split(l[nt], x, y);
+                        l[nt] = f2(x * corr[nt][0], y * corr[nt][1]);
 #pragma unroll
                         for (int i = 0; i < 2 * NW; ++i)
 #pragma unroll
@@ -489,32 +547,30 @@ __global__ void __launch_bounds__(kQ4Threads, 2) q4_decode_kernel(const __grid_c
                     }
                 }
 #pragma unroll
-                for (int tl = 0; tl < TS; ++tl)
+                for (int nt = 0; nt < NT; ++nt) {
+                    const uint64_t F2 = f2(-F[nt][0], -F[nt][1]);
 #pragma unroll
-                    for (int nt = 0; nt < NT; ++nt)
+                    for (int tl = 0; tl < TS; ++tl)
 #pragma unroll
-                        for (int i = 0; i < 4; ++i) {
-                            sc[tl][nt][i] = ex2(sc[tl][nt][i] - F[nt][i & 1]);
-                            l[nt][i & 1] += sc[tl][nt][i];
+                        for (int i = 0; i < 4; i += 2) {
+                            float x, y;
+                            f2_split(f2_fma(f2(sc[tl][nt][i], sc[tl][nt][i + 1]), fcol[nt], F2), x, y);
+                            sc[tl][nt][i] = ex2(x);
+                            sc[tl][nt][i + 1] = ex2(y);
+                            l[nt] = f2_sum(l[nt], f2(sc[tl][nt][i], sc[tl][nt][i + 1]));
                         }
+                }
                 // ---- o^T += V^T (p * scale) ----
 #pragma unroll
                 for (int tl = 0; tl < TS; ++tl) {
-                    const unsigned char *tp = tp0 + tl * S::kTile, *vp = tp + q4_v_base(D), *vs = tp + q4_vs_base(D, NG);
+                    const unsigned char *tp = tp0 + tl * S::kTile, *vp = tp + q4_v_base(D);
                     uint32_t s0[(NG + 1) / 2], s1[(NG + 1) / 2];
-                    if (NG == 4) {
-                        const uint2 x = *reinterpret_cast<const uint2 *>(vs + g * 8), y = *reinterpret_cast<const uint2 *>(vs + (g + 8) * 8);
-                        s0[0] = x.x; s0[(NG - 1) / 2] = x.y; s1[0] = y.x; s1[(NG - 1) / 2] = y.y;
-                    } else if (NG == 2) {
-                        s0[0] = *reinterpret_cast<const uint32_t *>(vs + g * 4); s1[0] = *reinterpret_cast<const uint32_t *>(vs + (g + 8) * 4);
-                    } else {
-                        s0[0] = *reinterpret_cast<const unsigned short *>(vs + g * 2); s1[0] = *reinterpret_cast<const unsigned short *>(vs + (g + 8) * 2);
-                    }
+                    q4_scales<NG>(tp + q4_vs_base(D, NG), g, s0, s1);
                     // words of tokens 2c, 2c + 1, 2c + 8, 2c + 9: chunk g
                     uint32_t wd[4][(NW + 1) / 2];
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
-                        const unsigned char *p = vp + q4_v_chunk(D, 2 * c + (i & 1) + (i >> 1) * 8, g);
+                        const unsigned char *p = vp + v_at[i];
                         if (NW == 4) {
                             const uint2 x = *reinterpret_cast<const uint2 *>(p);
                             wd[i][0] = x.x; wd[i][(NW - 1) / 2] = x.y;
@@ -530,13 +586,13 @@ __global__ void __launch_bounds__(kQ4Threads, 2) q4_decode_kernel(const __grid_c
                         for (int nt = 0; nt < NT; ++nt) {
                             const float *p = sc[tl][nt];
                             float w0 = p[0] * f0, w1 = p[1] * f0, w2 = p[2] * f1, w3 = p[3] * f1;
-                            if (!whole) {                      // a weight of zero stays zero whatever the scale holds
+                            if (kMask) {                       // a hidden token's weight is zero whatever its scale holds
                                 const int t = t0 + tl * kQ4Tile + g;
-                                const bool here = (have >> (step * TS + tl)) & 1;
-                                if (!(here && t < vis[nt][0])) w0 = 0.f;
-                                if (!(here && t < vis[nt][1])) w1 = 0.f;
-                                if (!(here && t + 8 < vis[nt][0])) w2 = 0.f;
-                                if (!(here && t + 8 < vis[nt][1])) w3 = 0.f;
+                                const bool ok = (here >> tl) & 1;
+                                if (!(ok && t < vis[nt][0])) w0 = 0.f;
+                                if (!(ok && t < vis[nt][1])) w1 = 0.f;
+                                if (!(ok && t + 8 < vis[nt][0])) w2 = 0.f;
+                                if (!(ok && t + 8 < vis[nt][1])) w3 = 0.f;
                             }
                             b0[nt] = movmatrix(pack_f16(w0, w1));
                             b1[nt] = movmatrix(pack_f16(w2, w3));
@@ -546,10 +602,8 @@ __global__ void __launch_bounds__(kQ4Threads, 2) q4_decode_kernel(const __grid_c
                             const uint32_t sel = w & 1 ? 0x7632u : 0x5410u;
                             const uint32_t x = __byte_perm(wd[0][w / 2], wd[1][w / 2], sel), y = __byte_perm(wd[2][w / 2], wd[3][w / 2], sel);
                             const uint32_t x8 = x >> 8, y8 = y >> 8;
-                            const uint32_t fa[4] = {sub_f16(and_or(x, 0x000f000fu, 0x64006400u), 0x64086408u), sub_f16(and_or(x, 0x00f000f0u, 0x54005400u), 0x54805480u),
-                                                    sub_f16(and_or(y, 0x000f000fu, 0x64006400u), 0x64086408u), sub_f16(and_or(y, 0x00f000f0u, 0x54005400u), 0x54805480u)};
-                            const uint32_t fb[4] = {sub_f16(and_or(x8, 0x000f000fu, 0x64006400u), 0x64086408u), sub_f16(and_or(x8, 0x00f000f0u, 0x54005400u), 0x54805480u),
-                                                    sub_f16(and_or(y8, 0x000f000fu, 0x64006400u), 0x64086408u), sub_f16(and_or(y8, 0x00f000f0u, 0x54005400u), 0x54805480u)};
+                            const uint32_t fa[4] = {code_lo(x), code_hi(x), code_lo(y), code_hi(y)};
+                            const uint32_t fb[4] = {code_lo(x8), code_hi(x8), code_lo(y8), code_hi(y8)};
 #pragma unroll
                             for (int nt = 0; nt < NT; ++nt) {
                                 mma_f16(o[nt][2 * w], fa, b0[nt], b1[nt], o[nt][2 * w]);
@@ -558,6 +612,13 @@ __global__ void __launch_bounds__(kQ4Threads, 2) q4_decode_kernel(const __grid_c
                         }
                     }
                 }
+            };
+            if (whole) {
+#pragma unroll 1
+                for (int step = 0; step < 4 / TS; ++step) work(step, std::false_type());
+            } else {
+#pragma unroll 1
+                for (int step = 0; step < 4 / TS; ++step) work(step, std::true_type());
             }
             __syncwarp();
             if (++st_out == kSt) { st_out = 0; ++phase; }
@@ -572,7 +633,9 @@ __global__ void __launch_bounds__(kQ4Threads, 2) q4_decode_kernel(const __grid_c
         for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
             for (int b = 0; b < 2; ++b) {
-                float v = l[nt][b];
+                float lx, ly;
+                f2_split(l[nt], lx, ly);
+                float v = b ? ly : lx;
                 v += __shfl_xor_sync(0xffffffffu, v, 4);
                 v += __shfl_xor_sync(0xffffffffu, v, 8);
                 v += __shfl_xor_sync(0xffffffffu, v, 16);
@@ -650,61 +713,63 @@ __global__ void __launch_bounds__(kQ4Threads, 2) q4_decode_kernel(const __grid_c
         for (int i = 0; i < kSt; ++i) (void)mbar_wait(smem_u32(&bars[warp][(lost + i) % kSt]), ((lost + i) / kSt) & 1);
 }
 
-// Joins the states of the segments that span CTAs: block b takes the one that begins in CTA b, in token order.
+// Joins the states of the segments that span CTAs, in token order: block (b, r) takes row r of the segment that begins in
+// CTA b.  A chain of loads over the parts would cost a trip to L2 each (37 parts of a 128K sequence: 41 us); the parts are
+// shared by four warps and their loads do not wait for one another.
+constexpr int kQ4JoinWarps = 4;
 template <int D, bool H16>
-__global__ void __launch_bounds__(128) q4_join_kernel(const __grid_constant__ Q4AttentionArgs a, int R) {
+__global__ void __launch_bounds__(32 * kQ4JoinWarps) q4_join_kernel(const __grid_constant__ Q4AttentionArgs a) {
     asm volatile("griddepcontrol.wait;" ::: "memory");
     const Q4Geometry &geo = a.geo;
-    const int b = blockIdx.x;
+    const int b = blockIdx.x, r = blockIdx.y, R = gridDim.y;
     const Q4Part p = reinterpret_cast<const Q4Part *>(a.workspace)[b];
     if (p.seq < 0) return;
-    const float *states = reinterpret_cast<const float *>(a.workspace + q4_parts_bytes(gridDim.x));
-    const long long per = q4_state_floats(R, D);
-    // CTA b left it in slot 1 unless it is the CTA's only segment; the CTAs behind it in slot 0
     int first, all;
     const int n = q4_new_rows(a, p.seq, first, all, nullptr), G = geo.group;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    for (int r = blockIdx.y * 4 + warp; r < R; r += 4 * gridDim.y) {
-        const int row = p.tile * R + r, j = row / G;
-        if (j >= n) break;
-        const int slot0 = p.slot, last = p.last_cta;
-        float M = kNegInf;
-        for (int k = b + lane; k <= last; k += 32) {
-            const float *s = states + (2LL * k + (k == b ? slot0 : 0)) * per;
-            M = fmaxf(M, s[R * D + r]);
-        }
+    const int row = p.tile * R + r, j = row / G;
+    if (j >= n) return;
+    const float *states = reinterpret_cast<const float *>(a.workspace + q4_parts_bytes(gridDim.x));
+    const long long per = q4_state_floats(R, D);
+    // the first part is in slot p.slot of CTA b, the others in slot 0 of the CTAs behind it
+    auto state = [&](int k) { return states + (2LL * k + (k == b ? p.slot : 0)) * per; };
+    float M = kNegInf;
+    for (int k = b + lane; k <= p.last_cta; k += 32) M = fmaxf(M, state(k)[R * D + r]);
 #pragma unroll
-        for (int d = 16; d; d >>= 1) M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, d));
-        float L = 0.f, acc[D / 32];
+    for (int d = 16; d; d >>= 1) M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, d));
+    constexpr int C = D / 32;
+    float L = 0.f, acc[C];
 #pragma unroll
-        for (int i = 0; i < D / 32; ++i) acc[i] = 0.f;
+    for (int i = 0; i < C; ++i) acc[i] = 0.f;
 #pragma unroll 4
-        for (int k = b; k <= last; ++k) {
-            const float *s = states + (2LL * k + (k == b ? slot0 : 0)) * per;
-            const float f = ex2(s[R * D + r] - M);
-            L += f * s[R * D + R + r];
-            if (D == 128) {
-                const float4 x = *reinterpret_cast<const float4 *>(s + r * D + 4 * lane);
-                acc[0] += f * x.x; acc[1] += f * x.y; acc[D / 32 - 2] += f * x.z; acc[D / 32 - 1] += f * x.w;
-            } else {
-                const float2 x = *reinterpret_cast<const float2 *>(s + r * D + 2 * lane);
-                acc[0] += f * x.x; acc[1] += f * x.y;
-            }
-        }
-        const int h = p.head * G + row - j * G;
-        if (a.state) {
-            float *dst = a.state + ((long long)(first + j) * geo.n_q_heads + h) * (D + 2);
+    for (int k = b + warp; k <= p.last_cta; k += kQ4JoinWarps) {
+        const float *s = state(k);
+        const float f = ex2(s[R * D + r] - M);
+        L += f * s[R * D + R + r];
+        const float2 *x = reinterpret_cast<const float2 *>(s + r * D + C * lane);
 #pragma unroll
-            for (int i = 0; i < D / 64; ++i) *reinterpret_cast<float2 *>(dst + D / 32 * lane + 2 * i) = make_float2(acc[2 * i], acc[2 * i + 1]);
-            if (lane == 0) *reinterpret_cast<float2 *>(dst + D) = make_float2(M, L);
-        } else {
-            const float inv = L != 0.f ? 1.f / L : 0.f;
-            uint32_t *dst = reinterpret_cast<uint32_t *>(reinterpret_cast<unsigned short *>(a.out) + (long long)(first + j) * a.out_row +
-                                                         (long long)h * a.out_head + D / 32 * lane);
+        for (int i = 0; i < C / 2; ++i) { const float2 v = x[i]; acc[2 * i] += f * v.x; acc[2 * i + 1] += f * v.y; }
+    }
+    __shared__ float part[kQ4JoinWarps][D + 1];
 #pragma unroll
-            for (int i = 0; i < D / 64; ++i)
-                dst[i] = H16 ? pack_f16(acc[2 * i] * inv, acc[2 * i + 1] * inv) : pack_bf16(acc[2 * i] * inv, acc[2 * i + 1] * inv);
-        }
+    for (int i = 0; i < C; ++i) part[warp][C * lane + i] = acc[i];
+    if (lane == 0) part[warp][D] = L;
+    __syncthreads();
+    const int ch = threadIdx.x * 2;
+    if (ch >= D) return;
+    float x = 0.f, y = 0.f;
+    L = 0.f;
+#pragma unroll
+    for (int w = 0; w < kQ4JoinWarps; ++w) { x += part[w][ch]; y += part[w][ch + 1]; L += part[w][D]; }
+    const int h = p.head * G + row - j * G;
+    if (a.state) {
+        float *dst = a.state + ((long long)(first + j) * geo.n_q_heads + h) * (D + 2);
+        *reinterpret_cast<float2 *>(dst + ch) = make_float2(x, y);
+        if (ch == 0) *reinterpret_cast<float2 *>(dst + D) = make_float2(M, L);
+    } else {
+        const float inv = L != 0.f ? 1.f / L : 0.f;
+        *reinterpret_cast<uint32_t *>(reinterpret_cast<unsigned short *>(a.out) + (long long)(first + j) * a.out_row +
+                                      (long long)h * a.out_head + ch) = H16 ? pack_f16(x * inv, y * inv) : pack_bf16(x * inv, y * inv);
     }
 }
 
@@ -761,13 +826,13 @@ cudaError_t launch_q4_attention(const Q4AttentionArgs &a, cudaStream_t st) {
     }
     PKV_Q4_SHAPES(PKV_Q4_LAUNCH)
     if (e != cudaSuccess || n <= 1) return e;
-    cfg.gridDim = dim3(n, R / 8);
-    cfg.blockDim = dim3(128);
+    cfg.gridDim = dim3(n, R);
+    cfg.blockDim = dim3(32 * kQ4JoinWarps);
     cfg.dynamicSmemBytes = 0;
     if (g.head_dim == 128)
-        e = g.fp16 ? cudaLaunchKernelEx(&cfg, q4_join_kernel<128, true>, a, R) : cudaLaunchKernelEx(&cfg, q4_join_kernel<128, false>, a, R);
+        e = g.fp16 ? cudaLaunchKernelEx(&cfg, q4_join_kernel<128, true>, a) : cudaLaunchKernelEx(&cfg, q4_join_kernel<128, false>, a);
     else
-        e = g.fp16 ? cudaLaunchKernelEx(&cfg, q4_join_kernel<64, true>, a, R) : cudaLaunchKernelEx(&cfg, q4_join_kernel<64, false>, a, R);
+        e = g.fp16 ? cudaLaunchKernelEx(&cfg, q4_join_kernel<64, true>, a) : cudaLaunchKernelEx(&cfg, q4_join_kernel<64, false>, a);
     return e;
 }
 
