@@ -577,8 +577,8 @@ pkv_status pkv_q4_read_kv(pkv_q4_cache *c, int32_t n_seqs, const int32_t *page_t
  *   q     [device] dtype [n_rows, H_q, d]
  *   out   [device] dtype [n_rows, H_q, d], or NULL and instead
  *   state [device] fp32 [n_rows, H_q, d + 2], contiguous: per query head o (d values, not divided by l), then m, then l,
- *         as pkv_decode_attention_partial() writes them (with l = 0 for a query that sees nothing; m is a bound of the
- *         scores in base-2 units, and o and l are relative to 2^m): pkv_merge_attention_states() merges such states with
+ *         as pkv_decode_attention_partial() writes them (with l = 0 for a query that sees nothing; m is a reference near
+ *         the largest score, in base-2 units, and o and l are relative to 2^m): pkv_merge_attention_states() merges such states with
  *         those of other caches (recent tokens in a dense / factor cache, older ones here)
  *   max_q_len   a host-side bound of n over the sequences (rows of a sequence beyond it are left as they were and counted
  *               as bad lengths; 0: no sequence has rows); ignored without offsets

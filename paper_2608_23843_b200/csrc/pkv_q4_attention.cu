@@ -8,12 +8,13 @@
 //     (code + 8) 2^-24 exactly, and in bits 4-7 that times 16 (the queries of those channels are divided by 16).  The + 8
 //     is taken away for all groups at once by one product of the scales with -8 * sum(q).  Each group's product is
 //     multiplied by its scale in fp32.
-//   V codes become exact fp16 integers (a constant's exponent, then one packed subtraction; as subnormals they would lose the
+//   V codes become exact fp16 integers, two products' rows from each byte (see there; as subnormals they would lose the
 //     contributions of small weights next to a large one's + 8); the scales go to the weights, p * scale, rounded once to fp16.  To keep that inside fp16's range whatever the values' size, the running reference
-//     of the softmax is max(s) + E with E the exponent of the largest value scale of the step: p * scale <= 2 then.
+//     of the softmax is max(s) + E with E the exponent of the largest value scale so far; it follows when some score has passed
+//     it by 2^8 only, so p * scale <= 2^9, and a unit that moves nothing costs one vote.
 //   Queries are brought to fp16 with a power of two per row, which is exact for bf16 and fp16 alike.
-// Every warp of a CTA walks its own units of 64 tokens with its own ring of bulk copies, and keeps (m, l, o) in registers;
-// at the end of a (sequence, KV head, row tile) segment the warps' states are joined through shared memory.  The CTAs of
+// One warp of a CTA looks up pages and issues the bulk copies; the others take the units of 64 tokens in turn and keep (m, l, o)
+// in registers; at the end of a (sequence, KV head, row tile) segment the warps' states are joined through shared memory.  The CTAs of
 // a launch share the whole batch's units evenly, whatever the lengths; a segment that spans CTAs leaves its states in the
 // workspace and a second kernel joins them in token order.
 #include <cuda_bf16.h>
@@ -28,18 +29,24 @@ namespace pkv {
 
 namespace {
 
-constexpr int kQ4Warps = 6, kQ4Threads = kQ4Warps * 32;
-constexpr int kQ4Unit = 64;            // tokens per unit
+constexpr int kQ4Unit = 64;            // tokens per unit: four tiles
+constexpr int kQ4UnitTiles = kQ4Unit / kQ4Tile;
+constexpr int kQ4Step = 2;             // tiles per softmax step
+constexpr float kQ4Lag = 8.f;          // how far (base 2) scores may pass the softmax's reference before it follows
+// Warps of a CTA (two CTAs per SM), the last one for the copies: the kernel is bound by instruction issue, so as many warps as
+// their registers allow - one column of query rows in 128 registers a thread, two in 168.
+__host__ __device__ constexpr int q4_warps(int nt) { return nt == 1 ? 8 : 6; }
 
 template <int D, int NG, int NT>
 struct Q4Shape {
-    static constexpr int kTile = kQ4Tile * (D + 4 * NG), kUnitBytes = 4 * kTile;
+    static constexpr int kWarps = q4_warps(NT), kCons = kWarps - 1, kThreads = 32 * kWarps;
+    static constexpr int kTile = kQ4Tile * (D + 4 * NG), kUnitBytes = kQ4UnitTiles * kTile;
     static constexpr int kRowFloats = D + 4;                                        // a row of o in shared memory, padded against bank conflicts
-    static constexpr int kFlush = 8 * NT * kRowFloats * 4;                          // a warp's o at a segment's end: over the stage it has just read
+    static constexpr int kFlush = 8 * kRowFloats * 4;                               // a warp's o (eight rows at a time) at a segment's end: over the stage it has just read
     static constexpr int kStage = ((kUnitBytes > kFlush ? kUnitBytes : kFlush) + 127) / 128 * 128;
-    static constexpr int kStages = 111 * 1024 / (kQ4Warps * kStage) < 4 ? 111 * 1024 / (kQ4Warps * kStage) : 4;
-    static constexpr int kSmem = kQ4Warps * kStages * kStage;
-    static_assert(kStages >= 2 && 2 * (kSmem + 3072) <= 227 * 1024, "two CTAs per SM with two stages per warp");
+    static constexpr int kFit = 110 * 1024 / kStage, kStages = kFit < 16 ? kFit : 16;
+    static constexpr int kSmem = kStages * kStage;
+    static_assert(kStages > kCons && 2 * (kSmem + 3072) <= 227 * 1024, "two CTAs per SM, a stage per warp and some in flight");
 };
 
 // A segment that begins in a CTA and ends in another (seq < 0: none); slot: where its first part is (see below)
@@ -90,18 +97,6 @@ __device__ __forceinline__ uint32_t max_bf16(uint32_t x, uint32_t y) {      // (
     asm("max.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(x), "r"(y));
     return r;
 }
-// Two codes as fp16 integers -7 .. 7, from bits 0-3 or 4-7 of either half: under an exponent that puts their last bit at 1
-// they read 1024 + 8 + code or 64 + 8 + code, and the difference is exact.
-__device__ __forceinline__ uint32_t code_lo(uint32_t x) {
-    uint32_t r;
-    asm("{\n\t.reg .b32 t;\n\tlop3.b32 t, %1, 0x000f000f, 0x64006400, 0xEA;\n\tsub.rn.f16x2 %0, t, %2;\n\t}" : "=r"(r) : "r"(x), "r"(0x64086408u));
-    return r;
-}
-__device__ __forceinline__ uint32_t code_hi(uint32_t x) {
-    uint32_t r;
-    asm("{\n\t.reg .b32 t;\n\tlop3.b32 t, %1, 0x00f000f0, 0x54005400, 0xEA;\n\tsub.rn.f16x2 %0, t, %2;\n\t}" : "=r"(r) : "r"(x), "r"(0x54805480u));
-    return r;
-}
 // two fp32 values at once
 __device__ __forceinline__ uint64_t f2(float lo, float hi) {
     uint64_t v;
@@ -113,6 +108,16 @@ __device__ __forceinline__ uint64_t f2_fma(uint64_t a, uint64_t b, uint64_t c) {
     uint64_t d;
     asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(a), "l"(b), "l"(c));
     return d;
+}
+__device__ __forceinline__ uint32_t sub_h2(uint32_t x, uint32_t y) {
+    uint32_t r;
+    asm("sub.rn.f16x2 %0, %1, %2;" : "=r"(r) : "r"(x), "r"(y));
+    return r;
+}
+__device__ __forceinline__ uint32_t fma_h2(uint32_t x, uint32_t y, uint32_t z) {
+    uint32_t r;
+    asm("fma.rn.f16x2 %0, %1, %2, %3;" : "=r"(r) : "r"(x), "r"(y), "r"(z));
+    return r;
 }
 __device__ __forceinline__ uint64_t f2_sum(uint64_t a, uint64_t b) {
     uint64_t d;
@@ -133,7 +138,16 @@ __device__ __forceinline__ void q4_scales(const unsigned char *p, int g, uint32_
     }
 }
 
-// Where a warp's next unit is: positions in the batch's order of units (sequence, row tile, head, unit of 64 tokens).
+// Bounded wait that also ends when another warp has given up.
+__device__ __forceinline__ bool mbar_wait_or(uint32_t bar, uint32_t parity, volatile int *abort_flag) {
+    if (mbar_try_wait(bar, parity)) return true;
+    const long long t0 = clock64();
+    while (!mbar_try_wait(bar, parity))
+        if (clock64() - t0 > kWaitClocks || *abort_flag) return false;
+    return true;
+}
+
+// Where a unit is: positions in the batch's order of units (sequence, row tile, head, unit of 64 tokens).
 struct Q4Cursor {
     int seq, tile, head, unit;         // seq == n_seqs: past the end
     int T, tiles, units;               // of the sequence
@@ -164,20 +178,22 @@ __device__ __forceinline__ void q4_advance(const Q4AttentionArgs &a, int rows_pe
 }
 
 template <int D, int NG, bool H16, int NT>
-__global__ void __launch_bounds__(kQ4Threads, 2) q4_decode_kernel(const __grid_constant__ Q4AttentionArgs a) {
+__global__ void __launch_bounds__(Q4Shape<D, NG, NT>::kThreads, 2) q4_decode_kernel(const __grid_constant__ Q4AttentionArgs a) {
     using S = Q4Shape<D, NG, NT>;
     constexpr int NW = D / 32, WPG = NW / NG, R = 8 * NT;      // 32-channel words per row, words per scale, query rows
-    constexpr int TS = NT == 1 ? 4 : 2;                        // tiles per softmax step
-    constexpr int kSt = S::kStages;
+    constexpr int TS = kQ4Step, kSt = S::kStages, kQ4Warps = S::kWarps, kCons = S::kCons, kQ4Threads = S::kThreads;
     const Q4Geometry &geo = a.geo;
     extern __shared__ __align__(128) unsigned char smem[];
-    __shared__ unsigned long long bars[kQ4Warps][kSt];
-    __shared__ float2 ml[kQ4Warps][R];
+    __shared__ unsigned long long full[kSt], empty[kSt];
+    __shared__ uint32_t tiles_here[kSt];                       // which tiles of a stage's unit are there
+    __shared__ float2 ml[kCons][8];
     __shared__ long long sums[kQ4Warps], found_at;
-    __shared__ int found_seq, offs[kQ4Warps];
+    __shared__ int found_seq, offs[kCons], gave_up;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, c = lane & 3;
-    if (lane == 0)
-        for (int s = 0; s < kSt; ++s) mbar_init(smem_u32(&bars[warp][s]), 1);
+    if (tid == 0) {
+        for (int s = 0; s < kSt; ++s) { mbar_init(smem_u32(&full[s]), 1); mbar_init(smem_u32(&empty[s]), 1); }
+        gave_up = 0;
+    }
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     asm volatile("griddepcontrol.wait;" ::: "memory");
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
@@ -203,7 +219,7 @@ __global__ void __launch_bounds__(kQ4Threads, 2) q4_decode_kernel(const __grid_c
         for (int w = 0; w < kQ4Warps; ++w) total += sums[w];
     }
     // (no more CTAs than there are units for a warp of each; the launch could only estimate that)
-    const int n_ctas = (int)min((long long)gridDim.x, max(1LL, total / kQ4Warps));
+    const int n_ctas = (int)min((long long)gridDim.x, max(1LL, total / kCons));
     const long long begin = total * blockIdx.x / n_ctas, end = total * (blockIdx.x + 1) / n_ctas;
     Q4Part *parts = reinterpret_cast<Q4Part *>(a.workspace);
     float *states = reinterpret_cast<float *>(a.workspace + q4_parts_bytes(gridDim.x));
@@ -248,59 +264,68 @@ __global__ void __launch_bounds__(kQ4Threads, 2) q4_decode_kernel(const __grid_c
         seg.tile = (int)(at / seg.units / H);
     }
 
-    // ---- this warp's copies ----
-    const uint32_t ring = smem_u32(smem) + warp * kSt * S::kStage;
-    const unsigned char *ring_p = smem + warp * kSt * S::kStage;
     const int left_cta = (int)(end - begin);                   // units of the CTA
-    Q4Cursor nx = seg;                                         // the next unit to fetch
-    int nx_at = warp;                                          // its index within the CTA's units
-    if (warp < left_cta) q4_advance(a, R, nx, warp);
-    const int per_page = min(kQ4Unit, geo.page), n_parts = kQ4Unit / per_page;      // copies per unit: 1, 2 or 4
-    auto page_of = [&]() -> int {                              // lane i < n_parts: the page of part i of unit nx
-        const int t = nx.unit * kQ4Unit + lane * per_page;
-        if (lane >= n_parts || nx_at >= left_cta || t >= nx.T) return -1;
-        return __ldg(a.rows.table + (long long)nx.seq * a.rows.max_pages + (t >> geo.page_shift));
-    };
-    int pg = page_of();
-    bool timed_out = false;                                    // a wait ran out: nothing more is fetched, what is left counts as not there
-    int lost = 0;                                              // ... and which of the warp's units did not come
-    uint32_t vm = 0;                                           // per stage four bits: which tiles of 16 tokens are there
-    int st_in = 0;
-    auto fetch = [&]() {
-        if (nx_at >= left_cta || timed_out) return;
-        const int t0 = nx.unit * kQ4Unit, all_tiles = (max(0, min(kQ4Unit, nx.T - t0)) + kQ4Tile - 1) / kQ4Tile;
-        const int per_tiles = per_page / kQ4Tile, tiles = min(max(all_tiles - lane * per_tiles, 0), per_tiles);       // (lanes past the unit: 0)
-        const bool ok = tiles > 0 && (unsigned)pg < (unsigned)geo.n_pages;
-        uint32_t bits = (1u << all_tiles) - 1u;
-        const uint32_t bad = __ballot_sync(0xffffffffu, tiles > 0 && !ok);
-        if (bad) {
-            if (lane == 0) atomicAdd(a.status + 1, __popc(bad));
-            for (int i = 0; i < n_parts; ++i)
-                if (bad >> i & 1) bits &= ~(((1u << per_tiles) - 1u) << (i * per_tiles));
+    volatile int *abort_flag = &gave_up;
+
+    if (warp == kCons) {
+        // ---- copies: 32 units are looked up at a time, a lane each, and issued in turn ----
+        const int per_page = min(kQ4Unit, geo.page), n_parts = kQ4Unit / per_page, per_tiles = per_page / kQ4Tile;      // copies per unit: 1, 2 or 4
+        Q4Cursor nx = seg;
+        if (lane < left_cta) q4_advance(a, R, nx, lane);
+        bool ok = true;
+        int st = 0, use = 0, u = 0;                            // stage, times it has been used before; units issued
+        for (int at = lane; u < left_cta && ok; at += 32) {
+            uint32_t bits = 0;
+            int pg[4] = {-1, -1, -1, -1};
+            const int t0 = nx.unit * kQ4Unit, head = nx.head;
+            if (at < left_cta) {
+                const int tiles = (max(0, min(kQ4Unit, nx.T - t0)) + kQ4Tile - 1) / kQ4Tile;
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    if (i * per_tiles < tiles)
+                        pg[i] = __ldg(a.rows.table + (long long)nx.seq * a.rows.max_pages + ((t0 + i * per_page) >> geo.page_shift));
+                bits = (1u << tiles) - 1u;
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    if (i * per_tiles < tiles && (unsigned)pg[i] >= (unsigned)geo.n_pages) {
+                        atomicAdd(a.status + 1, 1);
+                        bits &= ~(((1u << per_tiles) - 1u) << (i * per_tiles));
+                    }
+                if (at + 32 < left_cta) q4_advance(a, R, nx, 32);
+            }
+            for (int i = 0; i < 32 && u < left_cta; ++i, ++u) {
+                const uint32_t bar = smem_u32(&full[st]);
+                if (use > 0 && !__all_sync(0xffffffffu, mbar_wait_or(smem_u32(&empty[st]), (use - 1) & 1, abort_flag))) { ok = false; break; }
+                if (lane == i) {
+                    tiles_here[st] = bits;
+                    if (bits) mbar_arrive_expect_tx(bar, __popc(bits) * S::kTile);
+                    else mbar_arrive(bar);
+                    const uint32_t dst = smem_u32(smem) + st * S::kStage;
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) {
+                        if (k >= n_parts) break;
+                        const int n = __popc(bits >> (k * per_tiles) & ((1u << per_tiles) - 1u));      // tiles of this part
+                        if (n > 0)
+                            bulk_g2s(dst + k * per_tiles * S::kTile,
+                                     a.pool + (long long)pg[k] * geo.page_bytes + (long long)head * geo.head_bytes +
+                                         (((t0 + k * per_page) & (geo.page - 1)) / kQ4Tile) * S::kTile, n * S::kTile, bar);
+                    }
+                }
+                __syncwarp();
+                if (++st == kSt) { st = 0; ++use; }
+            }
         }
-        const uint32_t bar = smem_u32(&bars[warp][st_in]);
-        if (lane == 0) {
-            if (bits) mbar_arrive_expect_tx(bar, __popc(bits) * S::kTile);
-            else mbar_arrive(bar);
-        }
-        __syncwarp();
-        if (ok)
-            bulk_g2s(ring + st_in * S::kStage + lane * per_tiles * S::kTile,
-                     a.pool + (long long)pg * geo.page_bytes + (long long)nx.head * geo.head_bytes + ((t0 & (geo.page - 1)) / kQ4Tile) * S::kTile,
-                     tiles * S::kTile, bar);
-        vm = (vm & ~(15u << (4 * st_in))) | bits << (4 * st_in);
-        if (++st_in == kSt) st_in = 0;
-        nx_at += kQ4Warps;
-        if (nx_at < left_cta) q4_advance(a, R, nx, kQ4Warps);
-        pg = page_of();
-    };
-#pragma unroll 1
-    for (int s = 0; s < kSt; ++s) fetch();
+        if (!ok && lane == 0 && !*abort_flag) { *abort_flag = 1; atomicAdd(a.status, 1); }
+        // copies in flight must land before the CTA retires: wait (bounded) for the stages armed last
+        for (int back = 1; back <= min(u, kSt); ++back) (void)mbar_wait(smem_u32(&full[(u - back) % kSt]), ((u - back) / kSt) & 1);
+        return;
+    }
 
     const int v_at[4] = {q4_v_chunk(D, 2 * c, g), q4_v_chunk(D, 2 * c + 1, g), q4_v_chunk(D, 2 * c + 8, g), q4_v_chunk(D, 2 * c + 9, g)};
+    auto consumers_sync = [] { asm volatile("bar.sync 1, %0;" ::"n"(32 * kCons) : "memory"); };
     int at = warp;                                             // this warp's next unit, within the CTA's units
     int seg_lo = 0;                                            // the segment's first unit, within the CTA's units
-    int st_out = 0, phase = 0;
+    int st = warp, phase = 0;                                  // its stage and the parity of that use
     const float scale = geo.scale_log2e;
     while (seg_lo < left_cta) {
         const int seg_hi = min(left_cta, seg_lo + seg.units - seg.unit);
@@ -308,7 +333,8 @@ __global__ void __launch_bounds__(kQ4Threads, 2) q4_decode_kernel(const __grid_c
         int first, all;
         const int n = q4_new_rows(a, seg.seq, first, all, nullptr), G = geo.group;
         uint32_t qf[NT][NW][4];
-        uint32_t bias[NT][2];
+        uint32_t bias[NT][2], big_run = 0;                     // (big_run: largest value scale so far, in both halves)
+        float E = -60.f;                                       // ... and its exponent
         float F[NT][2], o[NT][2 * NW][4];
         uint64_t fcol[NT], l[NT];                              // (columns 2c, 2c + 1)
         int vis[NT][2];
@@ -403,23 +429,45 @@ __global__ void __launch_bounds__(kQ4Threads, 2) q4_decode_kernel(const __grid_c
 
         // ---- the segment's units ----
         const bool any = at < seg_hi;
+        int st_last = 0;
         while (at < seg_hi) {
             const int t_unit = (seg.unit + at - seg_lo) * kQ4Unit;
-            const uint32_t bar = smem_u32(&bars[warp][st_out]);
-            if (!timed_out && !__all_sync(0xffffffffu, mbar_wait(bar, phase & 1))) {
-                if (lane == 0) atomicAdd(a.status, 1);
-                timed_out = true;
-                lost = phase * kSt + st_out;
+            uint32_t tiles = 0;
+            if (__all_sync(0xffffffffu, mbar_wait_or(smem_u32(&full[st]), phase, abort_flag))) tiles = tiles_here[st];
+            else if (lane == 0 && !*abort_flag) { *abort_flag = 1; atomicAdd(a.status, 1); }      // (the unit counts as not there)
+            const bool whole = tiles == (1u << kQ4UnitTiles) - 1u && t_unit + kQ4Unit <= vis_all;
+            const unsigned char *sp = smem + st * S::kStage;
+            // E: exponent of the largest value scale so far (lane: tokens 2 lane, 2 lane + 1)
+            {
+                const unsigned char *vs = sp + (lane >> 3) * S::kTile + q4_vs_base(D, NG) + (lane & 7) * 4 * NG;
+                const bool tile_ok = (tiles >> (lane >> 3)) & 1;
+                const bool ok0 = whole || (tile_ok && t_unit + 2 * lane < seg.T), ok1 = whole || (tile_ok && t_unit + 2 * lane + 1 < seg.T);
+                uint32_t z;
+                if (NG == 4) {
+                    const uint4 x = *reinterpret_cast<const uint4 *>(vs);
+                    z = max_bf16(ok0 ? max_bf16(x.x, x.y) : 0u, ok1 ? max_bf16(x.z, x.w) : 0u);
+                } else if (NG == 2) {
+                    const uint2 x = *reinterpret_cast<const uint2 *>(vs);
+                    z = max_bf16(ok0 ? x.x : 0u, ok1 ? x.y : 0u);
+                } else {
+                    z = *reinterpret_cast<const uint32_t *>(vs);
+                    z = (ok0 ? z & 0xffffu : 0u) | (ok1 ? z & 0xffff0000u : 0u);
+                }
+                z = max_bf16(z, big_run);
+                if (__any_sync(0xffffffffu, z != big_run)) {
+                    z = max_bf16(z, z << 16 | z >> 16);
+#pragma unroll
+                    for (int d = 1; d < 32; d <<= 1) z = max_bf16(z, __shfl_xor_sync(0xffffffffu, z, d));
+                    big_run = z;
+                    E = (float)min(max((int)(z >> 23) - 127, -60), 100);
+                }
             }
-            const uint32_t have = timed_out ? 0u : (vm >> (4 * st_out)) & 15u;
-            const bool whole = have == 15u && t_unit + kQ4Unit <= vis_all;
-            const unsigned char *sp = ring_p + st_out * S::kStage;
-            // One softmax step over TS tiles; kMask: some of its tokens are hidden from some row, or not there.
+            // kMask: some of the unit's tokens are hidden from some row, or not there.
             auto work = [&](int step, auto masked) {
                 constexpr bool kMask = decltype(masked)::value;
                 const unsigned char *tp0 = sp + step * TS * S::kTile;
                 const int t0 = t_unit + step * TS * kQ4Tile;
-                const uint32_t here = have >> (step * TS);
+                const uint32_t here = tiles >> (step * TS);
                 float sc[TS][NT][4];
                 // ---- scores ----
 #pragma unroll
@@ -480,70 +528,43 @@ __global__ void __launch_bounds__(kQ4Threads, 2) q4_decode_kernel(const __grid_c
                                 if (!(t < vis[nt][i & 1] && ((here >> tl) & 1))) sc[tl][nt][i] = -INFINITY;
                             }
                 }
-                // ---- E: exponent of the step's largest value scale (lane: tokens 2 lane, 2 lane + 1 of the step) ----
-                uint32_t big = 0;
-                if (TS == 4 || lane < 8 * TS) {
-                    const int tl = lane >> 3, t2 = 2 * (lane & 7), t = t0 + tl * kQ4Tile + t2;
-                    const unsigned char *vs = tp0 + tl * S::kTile + q4_vs_base(D, NG) + t2 * NG * 2;
-                    uint32_t z[NG];
-                    if (NG == 4) {
-                        const uint4 x = *reinterpret_cast<const uint4 *>(vs);
-                        z[0] = x.x; z[NG / 4] = x.y; z[NG / 2] = x.z; z[NG - 1] = x.w;
-                    } else if (NG == 2) {
-                        const uint2 x = *reinterpret_cast<const uint2 *>(vs);
-                        z[0] = x.x; z[NG - 1] = x.y;
-                    } else {
-                        z[0] = *reinterpret_cast<const uint32_t *>(vs);
-                    }
-                    if (kMask) {                               // rows past the end or on a page that is not there
-                        const bool ok = (here >> tl) & 1;
-#pragma unroll
-                        for (int k = 0; k < NG; ++k) {
-                            if (NG == 1) z[k] = (ok && t < seg.T ? z[k] & 0xffffu : 0u) | (ok && t + 1 < seg.T ? z[k] & 0xffff0000u : 0u);
-                            else z[k] = ok && t + k / ((NG + 1) / 2) < seg.T ? z[k] : 0u;
-                        }
-                    }
-                    big = z[0];
-#pragma unroll
-                    for (int k = 1; k < NG; ++k) big = max_bf16(big, z[k]);
-                }
-#pragma unroll
-                for (int d = 1; d < 8 * TS; d <<= 1) big = max_bf16(big, __shfl_xor_sync(0xffffffffu, big, d));
-                big = max_bf16(big, big >> 16) & 0xffffu;
-                if (TS < 4) big = __shfl_sync(0xffffffffu, big, 0);
-                const float E = big > 0x7f80u ? -60.f : (float)min(max((int)(big >> 7) - 127, -60), 100);
-
                 // ---- softmax ----
-                bool moved = false;
-                float corr[NT][2];
+                bool passed = false;
+                float mx[NT][2];
 #pragma unroll
                 for (int nt = 0; nt < NT; ++nt) {
                     float fc[2];
                     f2_split(fcol[nt], fc[0], fc[1]);
 #pragma unroll
                     for (int b = 0; b < 2; ++b) {
-                        float mx = fmaxf(sc[0][nt][b], sc[0][nt][b + 2]);
+                        float x = fmaxf(sc[0][nt][b], sc[0][nt][b + 2]);
 #pragma unroll
-                        for (int tl = 1; tl < TS; ++tl) mx = fmaxf(mx, fmaxf(sc[tl][nt][b], sc[tl][nt][b + 2]));
-                        mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 4));
-                        mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 8));
-                        mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 16));
-                        const float Fn = mx > kNegInf ? fmaxf(F[nt][b], fmaf(mx, fc[b], E)) : F[nt][b];
-                        corr[nt][b] = ex2(F[nt][b] - Fn);
-                        moved |= Fn != F[nt][b];
-                        F[nt][b] = Fn;
+                        for (int tl = 1; tl < TS; ++tl) x = fmaxf(x, fmaxf(sc[tl][nt][b], sc[tl][nt][b + 2]));
+                        mx[nt][b] = fmaf(x, fc[b], E);
+                        passed |= mx[nt][b] > F[nt][b] + kQ4Lag;
                     }
                 }
-                if (__any_sync(0xffffffffu, moved)) {
+                if (__any_sync(0xffffffffu, passed)) {         // the reference follows
 #pragma unroll
                     for (int nt = 0; nt < NT; ++nt) {
+                        float corr[2];
+#pragma unroll
+                        for (int b = 0; b < 2; ++b) {
+                            float x = mx[nt][b];
+                            x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 4));
+                            x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 8));
+                            x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 16));
+                            const float Fn = x > kNegInf ? fmaxf(F[nt][b], x) : F[nt][b];
+                            corr[b] = ex2(F[nt][b] - Fn);
+                            F[nt][b] = Fn;
+                        }
                         float x, y;
                         f2_split(l[nt], x, y);
-                        l[nt] = f2(x * corr[nt][0], y * corr[nt][1]);
+                        l[nt] = f2(x * corr[0], y * corr[1]);
 #pragma unroll
                         for (int i = 0; i < 2 * NW; ++i)
 #pragma unroll
-                            for (int k = 0; k < 4; ++k) o[nt][i][k] *= corr[nt][k & 1];
+                            for (int k = 0; k < 4; ++k) o[nt][i][k] *= corr[k & 1];
                     }
                 }
 #pragma unroll
@@ -601,9 +622,19 @@ __global__ void __launch_bounds__(kQ4Threads, 2) q4_decode_kernel(const __grid_c
                         for (int w = k * WPG; w < (k + 1) * WPG; ++w) {
                             const uint32_t sel = w & 1 ? 0x7632u : 0x5410u;
                             const uint32_t x = __byte_perm(wd[0][w / 2], wd[1][w / 2], sel), y = __byte_perm(wd[2][w / 2], wd[3][w / 2], sel);
-                            const uint32_t x8 = x >> 8, y8 = y >> 8;
-                            const uint32_t fa[4] = {code_lo(x), code_hi(x), code_lo(y), code_hi(y)};
-                            const uint32_t fb[4] = {code_lo(x8), code_hi(x8), code_lo(y8), code_hi(y8)};
+                            // a byte is u0 + 16 u1 (u = code + 8, never 0); as fp16 under an exponent that makes its last bit 1:
+                            // m = 1024 + u0 + 16 u1.  m - 1160 = c0 + 16 c1, and m / 16 + 1023.5 rounds to 1088 + u1 since u0 / 16 lies
+                            // strictly inside (0, 1): c1 without a mask, on the pipe that has room.  Row g of the product gets
+                            // c0 + 16 c1 and row g + 8 gets c1; the segment's end takes them apart.
+                            uint32_t fa[4], fb[4];
+#pragma unroll
+                            for (int i = 0; i < 2; ++i) {
+                                const uint32_t v = i ? y : x, m0 = __byte_perm(v, 0x64646464u, 0x4240u), m1 = __byte_perm(v, 0x64646464u, 0x4341u);
+                                fa[2 * i] = sub_h2(m0, 0x64886488u);
+                                fb[2 * i] = sub_h2(m1, 0x64886488u);
+                                fa[2 * i + 1] = sub_h2(fma_h2(m0, 0x2c002c00u, 0x63ff63ffu), 0x64486448u);
+                                fb[2 * i + 1] = sub_h2(fma_h2(m1, 0x2c002c00u, 0x63ff63ffu), 0x64486448u);
+                            }
 #pragma unroll
                             for (int nt = 0; nt < NT; ++nt) {
                                 mma_f16(o[nt][2 * w], fa, b0[nt], b1[nt], o[nt][2 * w]);
@@ -615,22 +646,27 @@ __global__ void __launch_bounds__(kQ4Threads, 2) q4_decode_kernel(const __grid_c
             };
             if (whole) {
 #pragma unroll 1
-                for (int step = 0; step < 4 / TS; ++step) work(step, std::false_type());
+                for (int step = 0; step < kQ4UnitTiles / TS; ++step) work(step, std::false_type());
             } else {
 #pragma unroll 1
-                for (int step = 0; step < 4 / TS; ++step) work(step, std::true_type());
+                for (int step = 0; step < kQ4UnitTiles / TS; ++step) work(step, std::true_type());
             }
+            at += kCons;
+            st_last = st;
+            st += kCons;
+            if (st >= kSt) { st -= kSt; phase ^= 1; }
             __syncwarp();
-            if (++st_out == kSt) { st_out = 0; ++phase; }
-            at += kQ4Warps;
-            if (at < seg_hi) fetch();                          // into the stage just read (the segment's last one is kept for the states)
+            if (at < seg_hi && lane == 0) mbar_arrive(smem_u32(&empty[st_last]));      // (the segment's last stage is kept for the states)
         }
 
         // ---- join the warps' states ----
-        const int st_free = st_out == 0 ? kSt - 1 : st_out - 1;
-        float *mine = reinterpret_cast<float *>(smem + (warp * kSt + st_free) * S::kStage);
+        float *mine = reinterpret_cast<float *>(smem + st_last * S::kStage);
+        const bool starts = seg.unit == 0, ends = seg_hi - seg_lo == seg.units - seg.unit;
+        const bool complete = starts && ends;
+        const int slot = seg_lo == 0 ? 0 : 1;
+        if (lane == 0) offs[warp] = any ? st_last * S::kStage : -1;
 #pragma unroll
-        for (int nt = 0; nt < NT; ++nt)
+        for (int nt = 0; nt < NT; ++nt) {
 #pragma unroll
             for (int b = 0; b < 2; ++b) {
                 float lx, ly;
@@ -639,34 +675,31 @@ __global__ void __launch_bounds__(kQ4Threads, 2) q4_decode_kernel(const __grid_c
                 v += __shfl_xor_sync(0xffffffffu, v, 4);
                 v += __shfl_xor_sync(0xffffffffu, v, 8);
                 v += __shfl_xor_sync(0xffffffffu, v, 16);
-                if (g == 0) ml[warp][nt * 8 + 2 * c + b] = make_float2(F[nt][b], any ? v : 0.f);
+                if (g == 0) ml[warp][2 * c + b] = make_float2(F[nt][b], any ? v : 0.f);
                 if (any)
 #pragma unroll
-                    for (int w = 0; w < NW; ++w)
-                        *reinterpret_cast<float4 *>(mine + (nt * 8 + 2 * c + b) * S::kRowFloats + 32 * w + 4 * g) =
-                            make_float4(o[nt][2 * w][b], o[nt][2 * w][2 + b], o[nt][2 * w + 1][b], o[nt][2 * w + 1][2 + b]);
+                    for (int w = 0; w < NW; ++w) {
+                        const float *x = o[nt][2 * w], *y = o[nt][2 * w + 1];
+                        *reinterpret_cast<float4 *>(mine + (2 * c + b) * S::kRowFloats + 32 * w + 4 * g) =
+                            make_float4(fmaf(-16.f, x[2 + b], x[b]), x[2 + b], fmaf(-16.f, y[2 + b], y[b]), y[2 + b]);
+                    }
             }
-        if (lane == 0) offs[warp] = any ? (warp * kSt + st_free) * S::kStage : -1;
-        __syncthreads();
-        {
-            const bool starts = seg.unit == 0, ends = seg_hi - seg_lo == seg.units - seg.unit;
-            const bool complete = starts && ends;
-            const int slot = seg_lo == 0 ? 0 : 1;
+            consumers_sync();
             float *part = states + (2LL * blockIdx.x + slot) * q4_state_floats(R, D);
-            for (int i = tid; i < R * (D / 4); i += kQ4Threads) {
-                const int r = i / (D / 4), ch = i % (D / 4) * 4;
+            for (int i = tid; i < 8 * (D / 4); i += 32 * kCons) {
+                const int r8 = i / (D / 4), r = nt * 8 + r8, ch = i % (D / 4) * 4;
                 float M = kNegInf;
 #pragma unroll
-                for (int w = 0; w < kQ4Warps; ++w) M = fmaxf(M, ml[w][r].x);
+                for (int w = 0; w < kCons; ++w) M = fmaxf(M, ml[w][r8].x);
                 float L = 0.f;
                 float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
-                for (int w = 0; w < kQ4Warps; ++w) {
+                for (int w = 0; w < kCons; ++w) {
                     const int off = offs[w];
                     if (off < 0) continue;
-                    const float f = ex2(ml[w][r].x - M);
-                    const float4 x = *reinterpret_cast<const float4 *>(smem + off + (r * S::kRowFloats + ch) * 4);
-                    L += f * ml[w][r].y;
+                    const float f = ex2(ml[w][r8].x - M);
+                    const float4 x = *reinterpret_cast<const float4 *>(smem + off + (r8 * S::kRowFloats + ch) * 4);
+                    L += f * ml[w][r8].y;
                     acc.x += f * x.x; acc.y += f * x.y; acc.z += f * x.z; acc.w += f * x.w;
                 }
                 if (!complete) {
@@ -690,27 +723,25 @@ __global__ void __launch_bounds__(kQ4Threads, 2) q4_decode_kernel(const __grid_c
                                                (long long)h * a.out_head + ch) = v;
                 }
             }
-            if (tid == 0 && gridDim.x > 1 && seg_hi == left_cta) {
-                // the CTA's last segment: does it begin here and go on elsewhere?
-                Q4Part p{-1, 0, 0, 0, 0};
-                if (starts && !ends) {
-                    const long long w1 = begin + seg_lo + seg.units;          // one past the segment's last unit
-                    p = Q4Part{seg.seq, seg.tile, seg.head, slot, (int)((w1 * n_ctas - 1) / total)};
-                }
-                parts[blockIdx.x] = p;
-            }
+            if (nt == NT - 1) asm volatile("fence.proxy.async.shared::cta;" ::: "memory");      // the stages go back to the copies
+            consumers_sync();
         }
-        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");      // the stages go back to the copies
-        __syncthreads();
-        if (any) fetch();
+        if (tid == 0 && gridDim.x > 1 && seg_hi == left_cta) {
+            // the CTA's last segment: does it begin here and go on elsewhere?
+            Q4Part p{-1, 0, 0, 0, 0};
+            if (starts && !ends) {
+                const long long w1 = begin + seg_lo + seg.units;          // one past the segment's last unit
+                p = Q4Part{seg.seq, seg.tile, seg.head, slot, (int)((w1 * n_ctas - 1) / total)};
+            }
+            parts[blockIdx.x] = p;
+        }
+        if (any && lane == 0) mbar_arrive(smem_u32(&empty[st_last]));
         seg_lo = seg_hi;
         if (seg_lo < left_cta) {
             const int by = seg.units - seg.unit;
             q4_advance(a, R, seg, by);
         }
     }
-    if (timed_out)                                             // copies still in flight must land before the CTA retires
-        for (int i = 0; i < kSt; ++i) (void)mbar_wait(smem_u32(&bars[warp][(lost + i) % kSt]), ((lost + i) / kSt) & 1);
 }
 
 // Joins the states of the segments that span CTAs, in token order: block (b, r) takes row r of the segment that begins in
@@ -779,7 +810,7 @@ int q4_rows_per_tile(const Q4Geometry &g, int max_q_len) { return (long long)max
 int q4_grid(const Q4Geometry &g, int n_seqs, int max_q_len, int max_len) {
     const int R = q4_rows_per_tile(g, max_q_len);
     const long long tiles = ((long long)max_q_len * g.group + R - 1) / R, units = (max_len + kQ4Unit - 1) / kQ4Unit;
-    const double all = (double)n_seqs * g.n_kv_heads * tiles * units / kQ4Warps;
+    const double all = (double)n_seqs * g.n_kv_heads * tiles * units / (q4_warps(R / 8) - 1);
     return all >= g.n_ctas ? g.n_ctas : all < 1 ? 1 : (int)all;
 }
 
@@ -815,7 +846,7 @@ cudaError_t launch_q4_attention(const Q4AttentionArgs &a, cudaStream_t st) {
 #define PKV_Q4_LAUNCH1(D, NG, H, NT)                                        \
     if ((g.fp16 != 0) == H && R == 8 * NT) {                                \
         cfg.gridDim = dim3(n);                                              \
-        cfg.blockDim = dim3(kQ4Threads);                                    \
+        cfg.blockDim = dim3(Q4Shape<D, NG, NT>::kThreads);                  \
         cfg.dynamicSmemBytes = Q4Shape<D, NG, NT>::kSmem;                   \
         e = cudaLaunchKernelEx(&cfg, q4_decode_kernel<D, NG, H, NT>, a);    \
     }

@@ -49,6 +49,9 @@ def attention(q, K, V, first_position, scale, out_type):
       each product weight * scale to fp16                     2^-11 * A   (relative half step of fp16)
                                                               + 2^-25 * tokens * vmax / l: half its smallest step, for
                                                               weights relative to the largest (l: their sum)
+                                                              + 17 * 2^-23 * tokens / 16 * vmax: fp32 sums over 16 tokens each of
+                                                              weight * scale * (c0 + 16 c1), |c0 + 16 c1| <= 119 = 17 * 7, two codes
+                                                              to a product, and c0 as their difference
       scores: fp32 sums of d products of |q| with codes up to 15 and their offset 8 (the codes are stored + 8), every
       partial sum off by 2^-23 of the largest one: ds = 2^-23 * (d + 8) * 4 * sum|q| |k|max in base-2 units; it moves a
       weight by a factor 1 +- ds, numerator and denominator alike
@@ -76,5 +79,5 @@ def attention(q, K, V, first_position, scale, out_type):
             out[j, h] = (w @ v[:see]) / l
             A = (w @ v[:see].abs()) / l
             ds = 2.0 ** -23 * (d + 8) * 4 * q[j, h].abs().sum() * k[:see].abs().max() * scale * math.log2(math.e)
-            tol[j, h] = info.eps / 2 * out[j, h].abs().clamp(min=info.smallest_normal) + (2.0 ** -11 + 2.0 ** -19 + 2 * ds) * A + 2.0 ** -25 * see * v[:see].abs().max() / l
+            tol[j, h] = info.eps / 2 * out[j, h].abs().clamp(min=info.smallest_normal) + (2.0 ** -11 + 2.0 ** -19 + 2 * ds) * A + (2.0 ** -25 * see / l + 17 * 2.0 ** -23 * -(-see // 16)) * v[:see].abs().max()
     return out, lse, tol
