@@ -15,11 +15,13 @@ using namespace pkv;
 namespace {
 
 // ---- kernels -------------------------------------------------------------------------------------------------------
-// Both copy kernels give a row of d channels (one token, one head, K or V) to d/8 lanes, eight channels each: a 16-byte
-// load or store per lane.  Bound by HBM (4 d bytes of 16-bit rows and d + 4 d/g bytes of cache per token and head).
-constexpr int kCopyThreads = 256;
+// Both copy kernels are bound by HBM: 4 d bytes of 16-bit rows and d + 4 d/g bytes of cache per token and KV head.  A CTA
+// takes a few rows of the call: it looks up where they lie once, a thread each, while the first 16-byte loads are in flight
+// (of d/8 lanes per row and head, K and V together), so that nothing but the loads, the arithmetic and the stores is paid per
+// head.
+constexpr int kCopyThreads = 256, kCopyUnroll = 4, kCopyRows = 128;
 
-struct RowPlace { int ok, t; long long off; };      // token within its tile; byte offset of the head-0 tile in the pool
+struct RowPlace { long long off; int t, ok; };      // byte offset of the head-0 tile in the pool; token within its tile
 
 // Where row i of a call lies: its sequence, its position, the page that holds it.
 __device__ __forceinline__ RowPlace place_of(const Q4Rows &r, const Q4Geometry &g, int i, int *status) {
@@ -50,7 +52,7 @@ __device__ __forceinline__ RowPlace place_of(const Q4Rows &r, const Q4Geometry &
         return RowPlace{0, 0, 0};
     }
     const int in_page = pos & (g.page - 1);
-    return RowPlace{1, in_page & (kQ4Tile - 1), page * g.page_bytes + (long long)(in_page / kQ4Tile) * g.tile_bytes};
+    return RowPlace{page * g.page_bytes + (long long)(in_page / kQ4Tile) * g.tile_bytes, in_page & (kQ4Tile - 1), 1};
 }
 
 template <bool H16>
@@ -67,137 +69,208 @@ __device__ __forceinline__ void unpack8(const uint4 &w, float *x) {
     }
 }
 
-// Codes (+ 8) of eight values of a group with scale s (a bf16 value >= 0), as integers 1..15.
+// Codes of eight values x of a group with scale s (a bf16 value >= 0), packed: value n's code + 8 (1..15) in the nibble of word
+// kV ? n : n / 2 + 4 (n % 2).
 // The quotient decides between neighbouring codes, and x / s may lie exactly on a border (both have few bits): a plain
 // x * (1/s) would land beside it.  x has 11 significant bits at most and s eight, so a quotient up to 7.5 that is not on a
-// border is at least 2^-14 away from it; rounding x * (1/s) (off by less than 2^-18) to a multiple of 2^-16 first -
-// adding and taking away 192 - therefore gives the border itself where the true quotient is on it and keeps the side
-// everywhere else, and the rounding to an integer then takes ties to even like the division would.
-__device__ __forceinline__ void codes8(const float *x, float s, uint32_t *u) {
-    // scales below 2^-64 (some are subnormal bf16 numbers, whose reciprocal overflows): both sides times 2^64
-    const float f = s < 5.4210109e-20f ? 1.8446744e19f : 1.f;
-    const float inv = s > 0.f ? __frcp_rn(s * f) : 0.f;
+// border is at least 2^-14 away from it; rounding x * (1/s) (off by less than 2^-18, with a reciprocal good to 2^-22) to a multiple of 2^-16 first -
+// adding 192 - therefore gives the border itself where the true quotient is on it and keeps the side everywhere else, and
+// the rounding to an integer that follows - adding 2^23 * 1.5 - takes ties to even like the division would.
+template <bool kV>
+__device__ __forceinline__ uint32_t codes8(const float *x, float s) {
+    uint32_t w = 0;
+    if (s < 5.4210109e-20f) {                       // below 2^-64 (some are subnormal bf16 numbers, whose reciprocal overflows): both sides times 2^64
+        const float inv = s > 0.f ? 1.f / (s * 1.8446744e19f) : 0.f;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        float q = __fmul_rn(__fmul_rn(x[i], f), inv);
-        q = __fadd_rn(__fadd_rn(q, 192.f), -192.f);
-        q = fminf(fmaxf(q, -7.f), 7.f);             // (7.03 after a scale rounded down; more only for subnormal scales)
-        u[i] = __float_as_uint(__fadd_rn(q, 12582912.f + 8.f)) & 15u;
+        for (int n = 0; n < 8; ++n) {
+            const float q = fminf(fmaxf(__fmul_rn(__fmul_rn(x[n], 1.8446744e19f), inv), -7.f), 7.f);      // (a subnormal scale may be rounded far down)
+            const float r = __fadd_rn(__fadd_rn(q, 192.f), 12582912.f + 8.f - 192.f);
+            w += __float_as_uint(r) << (kV ? 4 * n : 4 * (n >> 1) + 16 * (n & 1));
+        }
+    } else {                                        // |q| < 7.04: no clamp
+        float inv;
+        asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(inv) : "f"(s));
+#pragma unroll
+        for (int n = 0; n < 8; n += 2) {
+            float lo, hi;
+            asm("{\n\t.reg .b64 a, b;\n\tmov.b64 a, {%2, %3};\n\tmov.b64 b, {%4, %4};\n\tmul.rn.f32x2 a, a, b;\n\tmov.b64 b, {%5, %5};\n\tadd.rn.f32x2 a, a, b;\n\t"
+                "mov.b64 b, {%6, %6};\n\tadd.rn.f32x2 a, a, b;\n\tmov.b64 {%0, %1}, a;\n\t}"
+                : "=f"(lo), "=f"(hi) : "f"(x[n]), "f"(x[n + 1]), "f"(inv), "f"(192.f), "f"(12582912.f + 8.f - 192.f));
+            w += __float_as_uint(lo) << (kV ? 4 * n : 2 * n);
+            w += __float_as_uint(hi) << (kV ? 4 * n + 4 : 2 * n + 16);
+        }
     }
+    return w - 0x4b400000u * 0x11111111u;           // (the eight exponents of the last sums: 0x4b400000 in every shift, modulo 2^32)
 }
 
-// (the scale's clamp: 7 * scale has to be finite in bf16; bf16(max / 7) of the type's two largest values is not)
+// The scale bf16(max / 7) from max * (1/7), off by less than 2^-22: a seventh of a number of at most 11 bits is at least 2^-13
+// of itself away from the middle between two bf16 numbers.
+// (its clamp: 7 * scale has to be finite in bf16; bf16(max / 7) of the type's two largest values is not)
 constexpr float kScaleMost = 4.8183102e37f;          // 36.25 * 2^120
+
+// A lane's eight channels of one row: the codes' word and the group's scale.
+template <int GL, bool H16, bool kV>
+__device__ __forceinline__ void quantise8(const uint4 &raw, uint32_t &w, unsigned short &scale) {
+    // largest magnitude of the group, as bits: non-negative 16-bit floats order like integers, infinities and NaN last
+    uint32_t mx = __vmaxu2(__vmaxu2(raw.x & 0x7fff7fffu, raw.y & 0x7fff7fffu), __vmaxu2(raw.z & 0x7fff7fffu, raw.w & 0x7fff7fffu));
+    mx = max(mx & 0xffffu, mx >> 16);
+#pragma unroll
+    for (int d = 1; d < GL; d <<= 1) mx = max(mx, __shfl_xor_sync(0xffffffffu, mx, d));
+    const float amax = H16 ? __half2float(__ushort_as_half((unsigned short)mx)) : __uint_as_float(mx << 16);
+    const __nv_bfloat16 sb = __float2bfloat16_rn(fminf(amax * (1.f / 7.f), kScaleMost));
+    float v[8];
+    unpack8<H16>(raw, v);
+    w = codes8<kV>(v, __bfloat162float(sb));
+    scale = __bfloat16_as_ushort(sb);
+    if (mx >= (H16 ? 0x7c00u : 0x7f80u)) { w = 0x88888888u; scale = 0x7fc0u; }      // not finite: zero codes, and a NaN for a scale
+}
+
+// Rows of a CTA and where they lie.
+struct CopyRows {
+    int row0, n_jobs;                               // jobs: (row, KV head)
+};
+template <int D>
+__device__ __forceinline__ CopyRows copy_rows(const Q4CopyArgs &a) {
+    const int row0 = (int)blockIdx.x * a.rows_per_cta;
+    return CopyRows{row0, min(a.rows_per_cta, (int)a.rows.n_rows - row0) * a.geo.n_kv_heads};
+}
 
 template <int D, int NG, bool H16>
 __global__ void __launch_bounds__(kCopyThreads) q4_append_kernel(const __grid_constant__ Q4CopyArgs a) {
-    constexpr int LR = D / 8, GL = LR / NG;          // lanes per row, lanes per group
+    constexpr int LR = D / 8, GL = LR / NG, kSlots = kCopyThreads / LR;          // lanes per row and head, lanes per group
+    __shared__ RowPlace places[kCopyRows];
     const Q4Geometry &geo = a.geo;
-    const int H = geo.n_kv_heads, jobs_per_row = 2 * H;
-    const long long n_jobs = a.rows.n_rows * jobs_per_row;
-    const int lane = threadIdx.x & 31, l = lane % LR, j = l >> 2, c = l & 3;
-    const long long first = ((long long)blockIdx.x * kCopyThreads + threadIdx.x) / LR, step = (long long)gridDim.x * kCopyThreads / LR;
-    const long long warp_first = ((long long)blockIdx.x * kCopyThreads + (threadIdx.x & ~31)) / LR;
-    for (long long base = 0; warp_first + base < n_jobs; base += step) {
-        const long long job = first + base;
-        const bool in = job < n_jobs;
-        const int i = in ? (int)(job / jobs_per_row) : 0, x = in ? (int)(job - (long long)i * jobs_per_row) : 0;
-        const int is_v = x >= H, h = is_v ? x - H : x;
-        const unsigned short *src = reinterpret_cast<const unsigned short *>(is_v ? a.v : a.k) +
-                                    (is_v ? i * a.v_row + h * a.v_head : i * a.k_row + h * a.k_head);
-        const uint4 raw = in ? __ldg(reinterpret_cast<const uint4 *>(src) + l) : make_uint4(0u, 0u, 0u, 0u);
-        const RowPlace at = in ? place_of(a.rows, geo, i, x == 0 && l == 0 ? a.status : nullptr) : RowPlace{0, 0, 0};
-        // largest magnitude of the group, as bits: non-negative 16-bit floats order like integers, infinities and NaN last
-        uint32_t mx = __vmaxu2(__vmaxu2(raw.x & 0x7fff7fffu, raw.y & 0x7fff7fffu), __vmaxu2(raw.z & 0x7fff7fffu, raw.w & 0x7fff7fffu));
-        mx = max(mx & 0xffffu, mx >> 16);
+    const CopyRows cr = copy_rows<D>(a);
+    const int l = threadIdx.x % LR, slot = threadIdx.x / LR, j = l >> 2, c = l & 3;
+    bool looked_up = false;
+    for (int base = 0; base < cr.n_jobs; base += kSlots * kCopyUnroll) {
+        uint4 k[kCopyUnroll], v[kCopyUnroll];
+        int row[kCopyUnroll], head[kCopyUnroll];
 #pragma unroll
-        for (int d = 1; d < GL; d <<= 1) mx = max(mx, __shfl_xor_sync(0xffffffffu, mx, d));
-        const bool finite = mx < (H16 ? 0x7c00u : 0x7f80u);
-        const float amax = H16 ? __half2float(__ushort_as_half((unsigned short)mx)) : __uint_as_float(mx << 16);
-        const __nv_bfloat16 sb = __float2bfloat16_rn(fminf(__fdiv_rn(amax, 7.f), kScaleMost));
-        float v[8];
-        uint32_t u[8];
-        unpack8<H16>(raw, v);
-        codes8(v, __bfloat162float(sb), u);
-        uint32_t w = 0;
-        if (is_v) {
-#pragma unroll
-            for (int n = 0; n < 8; ++n) w |= u[n] << (4 * n);
-        } else {
-#pragma unroll
-            for (int n = 0; n < 4; ++n) w |= u[2 * n] << (4 * n) | u[2 * n + 1] << (4 * n + 16);
+        for (int u = 0; u < kCopyUnroll; ++u) {
+            const int job = base + u * kSlots + slot;
+            row[u] = __float2int_rz((job + 0.5f) * a.inv_heads);
+            head[u] = job - row[u] * geo.n_kv_heads;
+            k[u] = v[u] = make_uint4(0u, 0u, 0u, 0u);
+            if (job < cr.n_jobs) {
+                const long long i = cr.row0 + row[u];
+                k[u] = __ldg(reinterpret_cast<const uint4 *>(reinterpret_cast<const unsigned short *>(a.k) + i * a.k_row + head[u] * a.k_head) + l);
+                v[u] = __ldg(reinterpret_cast<const uint4 *>(reinterpret_cast<const unsigned short *>(a.v) + i * a.v_row + head[u] * a.v_head) + l);
+            }
         }
-        if (!finite) w = 0x88888888u;                // the group reads as NaN: zero codes, and a NaN for a scale
-        const uint32_t other = __shfl_xor_sync(0xffffffffu, w, 4);
-        if (!at.ok) continue;
-        unsigned char *tile = a.pool + at.off + (long long)h * geo.head_bytes;
-        if (is_v) {
-            // lanes j and j ^ 1 hold chunks 2c and 2c + 1 of 32-channel words j and j ^ 1: each stores one chunk's two words
-            const uint32_t two = j & 1 ? __byte_perm(other, w, 0x7632) : __byte_perm(w, other, 0x5410);
+        if (!looked_up) {
+            looked_up = true;
+            if (threadIdx.x < a.rows_per_cta && cr.row0 + threadIdx.x < a.rows.n_rows) places[threadIdx.x] = place_of(a.rows, geo, cr.row0 + threadIdx.x, a.status);
+            __syncthreads();
+        }
+#pragma unroll
+        for (int u = 0; u < kCopyUnroll; ++u) {
+            if (base + u * kSlots >= cr.n_jobs) break;          // (the same for all threads)
+            uint32_t wk, wv;
+            unsigned short sk, sv;
+            quantise8<GL, H16, false>(k[u], wk, sk);
+            quantise8<GL, H16, true>(v[u], wv, sv);
+            const uint32_t other = __shfl_xor_sync(0xffffffffu, wv, 4);
+            if (base + u * kSlots + slot >= cr.n_jobs) continue;
+            const RowPlace at = places[row[u]];
+            if (!at.ok) continue;
+            unsigned char *tile = a.pool + at.off + (long long)head[u] * geo.head_bytes;
+            // V: lanes j and j ^ 1 hold chunks 2c and 2c + 1 of 32-channel words j and j ^ 1: each stores one chunk's two words
+            const uint32_t two = j & 1 ? __byte_perm(other, wv, 0x7632) : __byte_perm(wv, other, 0x5410);
+            *reinterpret_cast<uint32_t *>(tile + q4_k_chunk(D, at.t, c) + j * 4) = wk;
             *reinterpret_cast<uint32_t *>(tile + q4_v_base(D) + q4_v_chunk(D, at.t, 2 * c + (j & 1)) + (j >> 1) * 4) = two;
-        } else {
-            *reinterpret_cast<uint32_t *>(tile + q4_k_chunk(D, at.t, c) + j * 4) = w;
+            if (l % GL == 0) {
+                *reinterpret_cast<unsigned short *>(tile + q4_ks_base(D) + (at.t * NG + l / GL) * 2) = sk;
+                *reinterpret_cast<unsigned short *>(tile + q4_vs_base(D, NG) + (at.t * NG + l / GL) * 2) = sv;
+            }
         }
-        if (l % GL == 0)
-            *reinterpret_cast<unsigned short *>(tile + (is_v ? q4_vs_base(D, NG) : q4_ks_base(D)) + (at.t * NG + l / GL) * 2) =
-                finite ? __bfloat16_as_ushort(sb) : (unsigned short)0x7fc0u;
     }
+}
+
+// Eight values code * scale, rounded once: w holds value n's code + 8 in nibble n / 2 + 4 (n % 2).
+template <bool H16>
+__device__ __forceinline__ uint4 values8(uint32_t w, unsigned short scale) {
+    uint32_t o[4];
+#pragma unroll
+    for (int p = 0; p < 4; ++p) {
+        const uint32_t u = (w >> (4 * p)) & 0x000f000fu;
+        if (H16) {                                  // (the scale need not be an fp16 number: products in fp32)
+            const uint32_t m = u | 0x64006400u;     // 1024 + code + 8
+            const __half2 code = __hsub2(*reinterpret_cast<const __half2 *>(&m), __floats2half2_rn(1032.f, 1032.f));
+            const float2 f = __half22float2(code);
+            const float s = __uint_as_float((uint32_t)scale << 16);
+            const __half2 t = __floats2half2_rn(f.x * s, f.y * s);
+            o[p] = *reinterpret_cast<const uint32_t *>(&t);
+        } else {
+            const uint32_t m = u | 0x43004300u, s = scale | (uint32_t)scale << 16;      // 128 + code + 8
+            const __nv_bfloat162 code = __hsub2(*reinterpret_cast<const __nv_bfloat162 *>(&m), __floats2bfloat162_rn(136.f, 136.f));
+            const __nv_bfloat162 t = __hmul2(code, *reinterpret_cast<const __nv_bfloat162 *>(&s));
+            o[p] = *reinterpret_cast<const uint32_t *>(&t);
+        }
+    }
+    return make_uint4(o[0], o[1], o[2], o[3]);
 }
 
 template <int D, int NG, bool H16>
 __global__ void __launch_bounds__(kCopyThreads) q4_read_kernel(const __grid_constant__ Q4CopyArgs a) {
-    constexpr int LR = D / 8, GL = LR / NG;
+    constexpr int LR = D / 8, GL = LR / NG, kSlots = kCopyThreads / LR;
+    __shared__ RowPlace places[kCopyRows];
     const Q4Geometry &geo = a.geo;
-    const int H = geo.n_kv_heads, jobs_per_row = 2 * H;
-    const long long n_jobs = a.rows.n_rows * jobs_per_row;
-    const int lane = threadIdx.x & 31, l = lane % LR, j = l >> 2, c = l & 3;
-    const long long first = ((long long)blockIdx.x * kCopyThreads + threadIdx.x) / LR, step = (long long)gridDim.x * kCopyThreads / LR;
-    const long long warp_first = ((long long)blockIdx.x * kCopyThreads + (threadIdx.x & ~31)) / LR;
-    for (long long base = 0; warp_first + base < n_jobs; base += step) {
-        const long long job = first + base;
-        const bool in = job < n_jobs;
-        const int i = in ? (int)(job / jobs_per_row) : 0, x = in ? (int)(job - (long long)i * jobs_per_row) : 0;
-        const int is_v = x >= H, h = is_v ? x - H : x;
-        const RowPlace at = in ? place_of(a.rows, geo, i, x == 0 && l == 0 ? a.status : nullptr) : RowPlace{0, 0, 0};
-        uint32_t w = 0;
-        float s = 0.f;
-        if (at.ok) {
-            const unsigned char *tile = a.pool + at.off + (long long)h * geo.head_bytes;
-            w = *reinterpret_cast<const uint32_t *>(tile + (is_v ? q4_v_base(D) + q4_v_chunk(D, at.t, 2 * c + (j & 1)) + (j >> 1) * 4
-                                                                 : q4_k_chunk(D, at.t, c) + j * 4));
-            s = __uint_as_float((uint32_t)*reinterpret_cast<const unsigned short *>(
-                                    tile + (is_v ? q4_vs_base(D, NG) : q4_ks_base(D)) + (at.t * NG + l / GL) * 2) << 16);
-        }
-        const uint32_t other = __shfl_xor_sync(0xffffffffu, w, 4);
-        if (!at.ok) continue;
-        if (is_v) w = j & 1 ? __byte_perm(other, w, 0x7632) : __byte_perm(w, other, 0x5410);
-        uint32_t o[4];
+    const CopyRows cr = copy_rows<D>(a);
+    const int l = threadIdx.x % LR, slot = threadIdx.x / LR, j = l >> 2, c = l & 3;
+    if (threadIdx.x < a.rows_per_cta && cr.row0 + threadIdx.x < a.rows.n_rows) places[threadIdx.x] = place_of(a.rows, geo, cr.row0 + threadIdx.x, a.status);
+    __syncthreads();
+    for (int base = 0; base < cr.n_jobs; base += kSlots * kCopyUnroll) {
+        uint32_t wk[kCopyUnroll], wv[kCopyUnroll];
+        unsigned short sk[kCopyUnroll], sv[kCopyUnroll];
+        int row[kCopyUnroll], head[kCopyUnroll];
 #pragma unroll
-        for (int p = 0; p < 4; ++p) {
-            const int n0 = is_v ? 8 * p : 4 * p, n1 = is_v ? 8 * p + 4 : 4 * p + 16;
-            const float lo = (float)((int)((w >> n0) & 15u) - 8) * s, hi = (float)((int)((w >> n1) & 15u) - 8) * s;
-            if (H16) {
-                const __half2 t = __floats2half2_rn(lo, hi);
-                o[p] = *reinterpret_cast<const uint32_t *>(&t);
-            } else {
-                const __nv_bfloat162 t = __floats2bfloat162_rn(lo, hi);
-                o[p] = *reinterpret_cast<const uint32_t *>(&t);
-            }
+        for (int u = 0; u < kCopyUnroll; ++u) {
+            const int job = base + u * kSlots + slot;
+            row[u] = __float2int_rz((job + 0.5f) * a.inv_heads);
+            head[u] = job - row[u] * geo.n_kv_heads;
+            wk[u] = wv[u] = 0;
+            sk[u] = sv[u] = 0;
+            if (job >= cr.n_jobs) { row[u] = -1; continue; }
+            const RowPlace at = places[row[u]];
+            if (!at.ok) { row[u] = -1; continue; }
+            const unsigned char *tile = a.pool + at.off + (long long)head[u] * geo.head_bytes;
+            wk[u] = __ldg(reinterpret_cast<const uint32_t *>(tile + q4_k_chunk(D, at.t, c) + j * 4));
+            wv[u] = __ldg(reinterpret_cast<const uint32_t *>(tile + q4_v_base(D) + q4_v_chunk(D, at.t, 2 * c + (j & 1)) + (j >> 1) * 4));
+            sk[u] = __ldg(reinterpret_cast<const unsigned short *>(tile + q4_ks_base(D) + (at.t * NG + l / GL) * 2));
+            sv[u] = __ldg(reinterpret_cast<const unsigned short *>(tile + q4_vs_base(D, NG) + (at.t * NG + l / GL) * 2));
         }
-        unsigned short *dst = reinterpret_cast<unsigned short *>(is_v ? a.v : a.k) +
-                              (is_v ? i * a.v_row + h * a.v_head : i * a.k_row + h * a.k_head);
-        reinterpret_cast<uint4 *>(dst)[l] = make_uint4(o[0], o[1], o[2], o[3]);
+#pragma unroll
+        for (int u = 0; u < kCopyUnroll; ++u) {
+            if (base + u * kSlots >= cr.n_jobs) break;          // (the same for all threads)
+            const uint32_t other = __shfl_xor_sync(0xffffffffu, wv[u], 4);
+            if (row[u] < 0) continue;
+            // V: nibble n is channel n; put it into the order of values8()
+            uint32_t w = j & 1 ? __byte_perm(other, wv[u], 0x7632) : __byte_perm(wv[u], other, 0x5410);
+            const uint32_t ev = w & 0x0f0f0f0fu, od = (w >> 4) & 0x0f0f0f0fu;      // channels 0 2 4 6 / 1 3 5 7, a byte each
+            const uint32_t e2 = (ev | ev >> 4) & 0x00ff00ffu, o2 = (od | od >> 4) & 0x00ff00ffu;
+            w = __byte_perm(e2, o2, 0x6420);
+            const long long i = cr.row0 + row[u];
+            reinterpret_cast<uint4 *>(reinterpret_cast<unsigned short *>(a.k) + i * a.k_row + head[u] * a.k_head)[l] = values8<H16>(wk[u], sk[u]);
+            reinterpret_cast<uint4 *>(reinterpret_cast<unsigned short *>(a.v) + i * a.v_row + head[u] * a.v_head)[l] = values8<H16>(w, sv[u]);
+        }
     }
 }
 
 template <bool kWrite>
-cudaError_t launch_copy(const Q4CopyArgs &a, cudaStream_t st) {
+cudaError_t launch_copy(Q4CopyArgs a, cudaStream_t st) {
     const Q4Geometry &g = a.geo;
-    const long long jobs = a.rows.n_rows * 2 * g.n_kv_heads;
-    if (jobs <= 0) return cudaSuccess;
-    const int per_cta = kCopyThreads / (g.head_dim / 8);
-    const long long want = (jobs + per_cta - 1) / per_cta, most = 8LL * g.n_sms;
-    const unsigned grid = (unsigned)(want < most ? want : most);
+    const long long n = a.rows.n_rows;
+    if (n <= 0) return cudaSuccess;
+    // rows per CTA: four jobs (row, head) for each of its groups of lanes, fewer where that would leave SMs idle
+    const int slots = kCopyThreads / (g.head_dim / 8);
+    long long rows = slots * kCopyUnroll / g.n_kv_heads;
+    if (rows > n / g.n_sms) rows = n / g.n_sms;
+    if (rows < 1) rows = 1;
+    if (rows > kCopyRows) rows = kCopyRows;
+    a.rows_per_cta = (int)rows;
+    a.inv_heads = 1.f / (float)g.n_kv_heads;
+    const unsigned grid = (unsigned)((n + rows - 1) / rows);
 #define PKV_Q4_COPY(D, NG)                                                                                           \
     if (g.head_dim == D && g.groups == NG) {                                                                         \
         if (g.fp16) { if (kWrite) q4_append_kernel<D, NG, true><<<grid, kCopyThreads, 0, st>>>(a);                   \

@@ -49,6 +49,8 @@ struct Q4CopyArgs {
     void *k, *v;                       // read by append, written by read
     long long k_row, k_head, v_row, v_head;      // strides in elements
     int *status;
+    int rows_per_cta;                  // set by the launcher, with 1 / n_kv_heads
+    float inv_heads;
 };
 
 struct Q4AttentionArgs {
