@@ -71,6 +71,12 @@ cudaError_t launch_q4_append(const Q4CopyArgs &a, cudaStream_t st);
 cudaError_t launch_q4_read(const Q4CopyArgs &a, cudaStream_t st);
 cudaError_t launch_q4_attention(const Q4AttentionArgs &a, cudaStream_t st);
 cudaError_t q4_attention_setup();      // raises dynamic shared-memory limits, once per cache
+// the row-block kernel (pkv_q4_block.cu); n: CTAs, from q4_block_grid
+constexpr int kQ4BlockRows = 256;
+cudaError_t q4_block_setup();
+int q4_block_grid(const Q4Geometry &g, int n_seqs, int max_q_len, int max_len);
+long long q4_block_workspace(const Q4Geometry &g, int n_seqs, int max_q_len, int max_len);
+cudaError_t launch_q4_block(const Q4AttentionArgs &a, int n, cudaStream_t st);
 long long q4_attention_workspace(const Q4Geometry &g, int n_seqs, int max_q_len, int max_len);
 
 // byte offsets inside a tile

@@ -22,17 +22,13 @@
 
 #include <type_traits>
 
-#include "pkv_q4.h"
-#include "pkv_device.cuh"
+#include "pkv_q4_device.cuh"
 
 namespace pkv {
 
 namespace {
 
-constexpr int kQ4Unit = 64;            // tokens per unit: four tiles
-constexpr int kQ4UnitTiles = kQ4Unit / kQ4Tile;
 constexpr int kQ4Step = 2;             // tiles per softmax step
-constexpr float kQ4Lag = 8.f;          // how far (base 2) scores may pass the softmax's reference before it follows
 // Warps of a CTA (two CTAs per SM), the last one for the copies: the kernel is bound by instruction issue, so as many warps as
 // their registers allow - one column of query rows in 128 registers a thread, two in 168.
 __host__ __device__ constexpr int q4_warps(int nt) { return nt == 1 ? 8 : 6; }
@@ -48,21 +44,6 @@ struct Q4Shape {
     static constexpr int kSmem = kStages * kStage;
     static_assert(kStages > kCons && 2 * (kSmem + 3072) <= 227 * 1024, "two CTAs per SM, a stage per warp and some in flight");
 };
-
-// A segment that begins in a CTA and ends in another (seq < 0: none); slot: where its first part is (see below)
-struct Q4Part { int seq, tile, head, slot, last_cta; };
-
-// Partial states: two per CTA (its first segment, its last), each [8 NT rows][D] o, then m and l of the rows.
-__host__ __device__ inline long long q4_state_floats(int rows, int d) { return (long long)rows * (d + 2); }
-__host__ __device__ inline long long q4_parts_bytes(int n_ctas) { return ((long long)n_ctas * (int)sizeof(Q4Part) + 255) / 256 * 256; }
-
-// The rows of a sequence that the call works on; `all`: with those beyond the caller's bound, which the positions go by.
-__device__ __forceinline__ int q4_new_rows(const Q4AttentionArgs &a, int s, int &first, int &all, int *status) {
-    first = q4_first_row(a.rows, s);
-    all = q4_first_row(a.rows, s + 1) - first;
-    if (status && all > a.max_q_len) atomicAdd(status + 2, 1);
-    return max(0, min(all, a.max_q_len));
-}
 
 __device__ __forceinline__ void mma_f16(float *d, const uint32_t *a, uint32_t b0, uint32_t b1, const float *c) {
     asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%10, %11, %12, %13};"
@@ -82,21 +63,6 @@ __device__ __forceinline__ uint32_t movmatrix(uint32_t x) {
     asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
     return y;
 }
-__device__ __forceinline__ float ex2(float x) {
-    float y;
-    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-    return y;
-}
-__device__ __forceinline__ uint32_t pack_f16(float lo, float hi) {
-    uint32_t r;
-    asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
-    return r;
-}
-__device__ __forceinline__ uint32_t max_bf16(uint32_t x, uint32_t y) {      // (the other operand where one is NaN)
-    uint32_t r;
-    asm("max.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(x), "r"(y));
-    return r;
-}
 // two fp32 values at once
 __device__ __forceinline__ uint64_t f2(float lo, float hi) {
     uint64_t v;
@@ -108,11 +74,6 @@ __device__ __forceinline__ uint64_t f2_fma(uint64_t a, uint64_t b, uint64_t c) {
     uint64_t d;
     asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(a), "l"(b), "l"(c));
     return d;
-}
-__device__ __forceinline__ uint32_t sub_h2(uint32_t x, uint32_t y) {
-    uint32_t r;
-    asm("sub.rn.f16x2 %0, %1, %2;" : "=r"(r) : "r"(x), "r"(y));
-    return r;
 }
 __device__ __forceinline__ uint32_t fma_h2(uint32_t x, uint32_t y, uint32_t z) {
     uint32_t r;
@@ -136,15 +97,6 @@ __device__ __forceinline__ void q4_scales(const unsigned char *p, int g, uint32_
     } else {
         s0[0] = *reinterpret_cast<const unsigned short *>(p + g * 2); s1[0] = *reinterpret_cast<const unsigned short *>(p + (g + 8) * 2);
     }
-}
-
-// Bounded wait that also ends when another warp has given up.
-__device__ __forceinline__ bool mbar_wait_or(uint32_t bar, uint32_t parity, volatile int *abort_flag) {
-    if (mbar_try_wait(bar, parity)) return true;
-    const long long t0 = clock64();
-    while (!mbar_try_wait(bar, parity))
-        if (clock64() - t0 > kWaitClocks || *abort_flag) return false;
-    return true;
 }
 
 // Where a unit is: positions in the batch's order of units (sequence, row tile, head, unit of 64 tokens).
@@ -413,7 +365,7 @@ __global__ void __launch_bounds__(Q4Shape<D, NG, NT>::kThreads, 2) q4_decode_ker
 #pragma unroll
             for (int b = 0; b < 2; ++b) {
                 const int col = 2 * c + b, r2 = seg.tile * R + nt * 8 + col, j2 = r2 / G;
-                fb[b] = __shfl_sync(0xffffffffu, fr, 4 * col);
+                fb[b] = fmaxf(__shfl_sync(0xffffffffu, fr, 4 * col), 1.2e-38f);      // (never 0: a hidden score is -inf)
                 vis[nt][b] = j2 < n ? seg.T - all + j2 + 1 : seg.T;
                 vis_all = min(vis_all, vis[nt][b]);
                 F[nt][b] = kNegInf;
@@ -744,65 +696,72 @@ __global__ void __launch_bounds__(Q4Shape<D, NG, NT>::kThreads, 2) q4_decode_ker
     }
 }
 
-// Joins the states of the segments that span CTAs, in token order: block (b, r) takes row r of the segment that begins in
-// CTA b.  A chain of loads over the parts would cost a trip to L2 each (37 parts of a 128K sequence: 41 us); the parts are
+// Joins the states of the segments (tiles of R rows) that span CTAs, in token order: blocks (b, y) take the rows of the
+// segment that begins in CTA b.  A chain of loads over the parts would cost a trip to L2 each (37 parts of a 128K sequence: 41 us); the parts are
 // shared by four warps and their loads do not wait for one another.
 constexpr int kQ4JoinWarps = 4;
 template <int D, bool H16>
-__global__ void __launch_bounds__(32 * kQ4JoinWarps) q4_join_kernel(const __grid_constant__ Q4AttentionArgs a) {
+__global__ void __launch_bounds__(32 * kQ4JoinWarps) q4_join_kernel(const __grid_constant__ Q4AttentionArgs a, int R) {
     asm volatile("griddepcontrol.wait;" ::: "memory");
     const Q4Geometry &geo = a.geo;
-    const int b = blockIdx.x, r = blockIdx.y, R = gridDim.y;
+    const int b = blockIdx.x;
     const Q4Part p = reinterpret_cast<const Q4Part *>(a.workspace)[b];
     if (p.seq < 0) return;
     int first, all;
     const int n = q4_new_rows(a, p.seq, first, all, nullptr), G = geo.group;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const int row = p.tile * R + r, j = row / G;
-    if (j >= n) return;
     const float *states = reinterpret_cast<const float *>(a.workspace + q4_parts_bytes(gridDim.x));
     const long long per = q4_state_floats(R, D);
     // the first part is in slot p.slot of CTA b, the others in slot 0 of the CTAs behind it
     auto state = [&](int k) { return states + (2LL * k + (k == b ? p.slot : 0)) * per; };
-    float M = kNegInf;
-    for (int k = b + lane; k <= p.last_cta; k += 32) M = fmaxf(M, state(k)[R * D + r]);
-#pragma unroll
-    for (int d = 16; d; d >>= 1) M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, d));
-    constexpr int C = D / 32;
-    float L = 0.f, acc[C];
-#pragma unroll
-    for (int i = 0; i < C; ++i) acc[i] = 0.f;
-#pragma unroll 4
-    for (int k = b + warp; k <= p.last_cta; k += kQ4JoinWarps) {
-        const float *s = state(k);
-        const float f = ex2(s[R * D + r] - M);
-        L += f * s[R * D + R + r];
-        const float2 *x = reinterpret_cast<const float2 *>(s + r * D + C * lane);
-#pragma unroll
-        for (int i = 0; i < C / 2; ++i) { const float2 v = x[i]; acc[2 * i] += f * v.x; acc[2 * i + 1] += f * v.y; }
-    }
     __shared__ float part[kQ4JoinWarps][D + 1];
+    constexpr int C = D / 32;
+    for (int r = blockIdx.y; r < R; r += gridDim.y) {
+        const long long row = (long long)p.tile * R + r;
+        const int j = (int)(row / G);
+        if (j >= n) return;
+        float M = kNegInf;
+        for (int k = b + lane; k <= p.last_cta; k += 32) M = fmaxf(M, state(k)[R * D + r]);
 #pragma unroll
-    for (int i = 0; i < C; ++i) part[warp][C * lane + i] = acc[i];
-    if (lane == 0) part[warp][D] = L;
-    __syncthreads();
-    const int ch = threadIdx.x * 2;
-    if (ch >= D) return;
-    float x = 0.f, y = 0.f;
-    L = 0.f;
+        for (int d = 16; d; d >>= 1) M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, d));
+        float L = 0.f, acc[C];
 #pragma unroll
-    for (int w = 0; w < kQ4JoinWarps; ++w) { x += part[w][ch]; y += part[w][ch + 1]; L += part[w][D]; }
-    const int h = p.head * G + row - j * G;
-    if (a.state) {
-        float *dst = a.state + ((long long)(first + j) * geo.n_q_heads + h) * (D + 2);
-        *reinterpret_cast<float2 *>(dst + ch) = make_float2(x, y);
-        if (ch == 0) *reinterpret_cast<float2 *>(dst + D) = make_float2(M, L);
-    } else {
-        const float inv = L != 0.f ? 1.f / L : 0.f;
-        *reinterpret_cast<uint32_t *>(reinterpret_cast<unsigned short *>(a.out) + (long long)(first + j) * a.out_row +
-                                      (long long)h * a.out_head + ch) = H16 ? pack_f16(x * inv, y * inv) : pack_bf16(x * inv, y * inv);
+        for (int i = 0; i < C; ++i) acc[i] = 0.f;
+#pragma unroll 4
+        for (int k = b + warp; k <= p.last_cta; k += kQ4JoinWarps) {
+            const float *s = state(k);
+            const float f = ex2(s[R * D + r] - M);
+            L += f * s[R * D + R + r];
+            const float2 *x = reinterpret_cast<const float2 *>(s + r * D + C * lane);
+#pragma unroll
+            for (int i = 0; i < C / 2; ++i) { const float2 v = x[i]; acc[2 * i] += f * v.x; acc[2 * i + 1] += f * v.y; }
+        }
+        if (r != (int)blockIdx.y) __syncthreads();             // (the row before has been read)
+#pragma unroll
+        for (int i = 0; i < C; ++i) part[warp][C * lane + i] = acc[i];
+        if (lane == 0) part[warp][D] = L;
+        __syncthreads();
+        const int ch = threadIdx.x * 2;
+        if (ch >= D) continue;
+        float x = 0.f, y = 0.f;
+        L = 0.f;
+#pragma unroll
+        for (int w = 0; w < kQ4JoinWarps; ++w) { x += part[w][ch]; y += part[w][ch + 1]; L += part[w][D]; }
+        const int h = p.head * G + (int)(row - (long long)j * G);
+        if (a.state) {
+            float *dst = a.state + ((long long)(first + j) * geo.n_q_heads + h) * (D + 2);
+            *reinterpret_cast<float2 *>(dst + ch) = make_float2(x, y);
+            if (ch == 0) *reinterpret_cast<float2 *>(dst + D) = make_float2(M, L);
+        } else {
+            const float inv = L != 0.f ? 1.f / L : 0.f;
+            *reinterpret_cast<uint32_t *>(reinterpret_cast<unsigned short *>(a.out) + (long long)(first + j) * a.out_row +
+                                          (long long)h * a.out_head + ch) = H16 ? pack_f16(x * inv, y * inv) : pack_bf16(x * inv, y * inv);
+        }
     }
 }
+
+// Many query rows per KV head go to the row-block kernel (pkv_q4_block.cu).
+bool q4_by_blocks(const Q4Geometry &g, int max_q_len) { return (long long)max_q_len * g.group > 16; }
 
 int q4_rows_per_tile(const Q4Geometry &g, int max_q_len) { return (long long)max_q_len * g.group <= 8 ? 8 : 16; }
 
@@ -819,7 +778,8 @@ int q4_grid(const Q4Geometry &g, int n_seqs, int max_q_len, int max_len) {
 }  // namespace
 
 cudaError_t q4_attention_setup() {
-    cudaError_t e;
+    cudaError_t e = q4_block_setup();
+    if (e != cudaSuccess) return e;
 #define PKV_Q4_SETUP1(D, NG, H16, NT) \
     if ((e = cudaFuncSetAttribute(q4_decode_kernel<D, NG, H16, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, Q4Shape<D, NG, NT>::kSmem)) != cudaSuccess) return e;
 #define PKV_Q4_SETUP(D, NG) PKV_Q4_SETUP1(D, NG, false, 1) PKV_Q4_SETUP1(D, NG, false, 2) PKV_Q4_SETUP1(D, NG, true, 1) PKV_Q4_SETUP1(D, NG, true, 2)
@@ -828,13 +788,16 @@ cudaError_t q4_attention_setup() {
 }
 
 long long q4_attention_workspace(const Q4Geometry &g, int n_seqs, int max_q_len, int max_len) {
+    if (q4_by_blocks(g, max_q_len)) return q4_block_workspace(g, n_seqs, max_q_len, max_len);
     const int n = q4_grid(g, n_seqs, max_q_len, max_len);
     return n <= 1 ? 0 : q4_parts_bytes(n) + 2LL * n * q4_state_floats(q4_rows_per_tile(g, max_q_len), g.head_dim) * 4;
 }
 
 cudaError_t launch_q4_attention(const Q4AttentionArgs &a, cudaStream_t st) {
     const Q4Geometry &g = a.geo;
-    const int n = q4_grid(g, a.rows.n_seqs, a.max_q_len, a.max_len), R = q4_rows_per_tile(g, a.max_q_len);
+    const bool blocks = q4_by_blocks(g, a.max_q_len);
+    const int n = blocks ? q4_block_grid(g, a.rows.n_seqs, a.max_q_len, a.max_len) : q4_grid(g, a.rows.n_seqs, a.max_q_len, a.max_len);
+    const int R = blocks ? kQ4BlockRows : q4_rows_per_tile(g, a.max_q_len);
     cudaLaunchAttribute at[1];
     at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     at[0].val.programmaticStreamSerializationAllowed = 1;
@@ -855,15 +818,19 @@ cudaError_t launch_q4_attention(const Q4AttentionArgs &a, cudaStream_t st) {
         PKV_Q4_LAUNCH1(D, NG, false, 1) PKV_Q4_LAUNCH1(D, NG, false, 2)                          \
         PKV_Q4_LAUNCH1(D, NG, true, 1) PKV_Q4_LAUNCH1(D, NG, true, 2)                            \
     }
-    PKV_Q4_SHAPES(PKV_Q4_LAUNCH)
+    if (blocks) {
+        e = launch_q4_block(a, n, st);
+    } else {
+        PKV_Q4_SHAPES(PKV_Q4_LAUNCH)
+    }
     if (e != cudaSuccess || n <= 1) return e;
-    cfg.gridDim = dim3(n, R);
+    cfg.gridDim = dim3(n, R < 32 ? R : 32);
     cfg.blockDim = dim3(32 * kQ4JoinWarps);
     cfg.dynamicSmemBytes = 0;
     if (g.head_dim == 128)
-        e = g.fp16 ? cudaLaunchKernelEx(&cfg, q4_join_kernel<128, true>, a) : cudaLaunchKernelEx(&cfg, q4_join_kernel<128, false>, a);
+        e = g.fp16 ? cudaLaunchKernelEx(&cfg, q4_join_kernel<128, true>, a, R) : cudaLaunchKernelEx(&cfg, q4_join_kernel<128, false>, a, R);
     else
-        e = g.fp16 ? cudaLaunchKernelEx(&cfg, q4_join_kernel<64, true>, a) : cudaLaunchKernelEx(&cfg, q4_join_kernel<64, false>, a);
+        e = g.fp16 ? cudaLaunchKernelEx(&cfg, q4_join_kernel<64, true>, a, R) : cudaLaunchKernelEx(&cfg, q4_join_kernel<64, false>, a, R);
     return e;
 }
 

@@ -1,0 +1,721 @@
+// Attention over the paged 4-bit cache, many query rows per KV head (a chunk of a prefill, a few dozen new positions), on
+// the fifth-generation tensor cores.
+//
+// A CTA works on blocks of up to 256 query rows of one (sequence, KV head), as two halves of 128 (the M dimension of every
+// product; one thread owns one row).  Tokens come in units of 64:
+//     warp 13        looks up pages and copies a unit's tiles of codes and scales into a ring,
+//     warps 8-11     a tile each: codes times scales as fp16 into shared memory, K and V in the layouts the products read
+//                    (128-byte swizzle, panels of 64 channels).  A code (3 bits and a sign) times a bf16 scale (8 bits) has
+//                    11 bits, so fp16 holds it exactly; a power of two per tile (the exponent of its largest scale, handed on
+//                    to the rows) keeps it inside fp16's range whatever the values' size,
+//     warp 12        one lane issues the products: s = Q K^T with Q and, later, p as row operands in tensor memory,
+//                    o += p V; while one half's rows are in their softmax the other half's products run,
+//     warps 0-7      softmax: s from tensor memory, p as fp16 back over it, o rescaled only when the running reference has
+//                    been passed by 2^8 (then p * value may still not leave fp16: 2^8 * 14).
+// What bounds it: per unit and 256 rows the products take 1024 cycles and the exponentials as many (16 per cycle and SM),
+// which overlap; the widening of the codes (some 370 instructions per warp and unit) hides behind both and is paid once for
+// 256 rows.  CTAs share the batch's units evenly, one CTA per SM; blocks that span CTAs leave states that a second kernel
+// joins.  Units after a block's last visible position are not visited.
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+
+#include "pkv_q4_device.cuh"
+#include "pkv_umma.cuh"
+
+namespace pkv {
+
+namespace {
+
+constexpr int kBRows = kQ4BlockRows, kBHalf = 128, kBThreads = 448;
+constexpr int kBRowWarps = 8, kBWidenWarps = 4, kBIssueWarp = 12, kBCopyWarp = 13;
+constexpr uint32_t kBTmemCols = 512;
+
+template <int D, int NG>
+struct BlockShape {
+    static constexpr int kPanels = D / 64, kSide = kPanels * kQ4Unit * 128, kWide = 2 * kSide;      // K panels, then V panels of a unit
+    static constexpr int kTile = kQ4Tile * (D + 4 * NG), kUnitBytes = kQ4UnitTiles * kTile, kCodes = (kUnitBytes + 127) / 128 * 128;
+    static constexpr int kWideStages = 4, kFit = (222 * 1024 - kWideStages * kWide) / kCodes, kCodeStages = kFit < 8 ? kFit : 8;
+    static constexpr int kSmem = kWideStages * kWide + kCodeStages * kCodes + 1024;                 // (+ alignment)
+    static_assert(kCodeStages >= 4 && kSmem <= 226 * 1024, "fits one CTA per SM");
+    // columns of tensor memory: o of both halves, Q of both halves (fp16 pairs), s of both halves
+    static constexpr uint32_t kColO = 0, kColQ = 2 * D, kColS = 2 * D + D;
+    static_assert(kColS + 2 * kQ4Unit <= kBTmemCols, "fits tensor memory");
+};
+
+// sum over i < n of floor((a i + b) / m), for a, b >= 0 and m > 0 (by the Euclid-like recursion on (a, m))
+__device__ long long floor_sum(long long n, long long m, long long a, long long b) {
+    long long sum = 0;
+    while (n > 0) {
+        sum += n * (n - 1) / 2 * (a / m) + n * (b / m);
+        a %= m;
+        b %= m;
+        const long long y = a * n + b;
+        if (y < m) break;
+        n = y / m;
+        b = y % m;
+        const long long t = m;
+        m = a;
+        a = t;
+    }
+    return sum;
+}
+
+// A sequence's blocks of query rows.  Block r's last row sees the first `see` tokens; it visits the units that hold them.
+struct BlockSeq { int first, all, n, T, blocks, G; };
+
+__device__ __forceinline__ BlockSeq block_seq(const Q4AttentionArgs &a, int s, int *status) {
+    BlockSeq q;
+    q.n = q4_new_rows(a, s, q.first, q.all, status);
+    q.T = q4_length(a.rows, a.geo, s, status);
+    q.G = a.geo.group;
+    q.blocks = (int)(((long long)q.n * q.G + kBRows - 1) / kBRows);
+    return q;
+}
+__device__ __forceinline__ int block_units(const BlockSeq &q, int r) {
+    const int last = min(q.n - 1, (int)(((long long)(r + 1) * kBRows - 1) / q.G));
+    const int see = q.all > q.T ? q.T : q.T - q.all + last + 1;          // (more rows than tokens: not worth a rule of its own)
+    return max(1, (see + kQ4Unit - 1) / kQ4Unit);
+}
+// units of the blocks before r (the last block may end before its rows do, so r is at most the number of blocks minus one
+// in the closed form: block i's last row is (i + 1) * 256 - 1, its units floor((T - all + 1 + floor((256 i + 255) / G) + 63) / 64))
+__device__ long long block_units_before(const BlockSeq &q, int r) {
+    if (r == 0) return 0;
+    if (q.all > q.T) return (long long)r * block_units(q, 0);
+    const int full = min(r, q.blocks - 1);
+    const long long A = (long long)q.T - q.all + 1 + kQ4Unit - 1;
+    long long sum = floor_sum(full, (long long)kQ4Unit * q.G, kBRows, kBRows - 1 + A * q.G);
+    if (r > full) sum += block_units(q, q.blocks - 1);
+    return sum;
+}
+
+// A place in the batch's order of units: sequence, block, head, unit.
+struct BlockCursor {
+    int seq, block, head, unit, units;
+    BlockSeq q;
+};
+__device__ __forceinline__ void block_advance(const Q4AttentionArgs &a, BlockCursor &c, int by) {
+    c.unit += by;
+    while (c.unit >= c.units) {
+        c.unit -= c.units;
+        if (++c.head < a.geo.n_kv_heads) continue;
+        c.head = 0;
+        if (++c.block == c.q.blocks) {
+            c.block = 0;
+            do {
+                if (++c.seq >= a.rows.n_seqs) return;
+                c.q = block_seq(a, c.seq, nullptr);
+            } while (c.q.blocks == 0);
+        }
+        c.units = block_units(c.q, c.block);
+    }
+}
+
+// What the widening warps tell the rows about a unit.
+struct UnitInfo {
+    float ek[kQ4UnitTiles], ev[kQ4UnitTiles];       // exponents taken out of the tiles' keys and values
+    uint32_t v_nan[kQ4UnitTiles];                   // tokens with a value group that is not finite (stored as zeros here)
+    uint32_t tiles, tokens;                         // which tiles are there; tokens of the sequence in the unit
+};
+
+__device__ __forceinline__ uint32_t h2_mul(uint32_t x, uint32_t y) {
+    uint32_t r;
+    asm("mul.rn.f16x2 %0, %1, %2;" : "=r"(r) : "r"(x), "r"(y));
+    return r;
+}
+// two codes as fp16 integers, from bits 0-3 (4-7) of either half: 1024 + 8 + code and 64 + 8 + code under a constant's exponent
+__device__ __forceinline__ uint32_t codes_lo(uint32_t x) { return sub_h2((x & 0x000f000fu) | 0x64006400u, 0x64086408u); }
+__device__ __forceinline__ uint32_t codes_hi(uint32_t x) { return sub_h2((x & 0x00f000f0u) | 0x54005400u, 0x54805480u); }
+
+__device__ __forceinline__ uint64_t f2_fma3(uint64_t a, uint64_t b, uint64_t c) {
+    uint64_t d;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(a), "l"(b), "l"(c));
+    return d;
+}
+__device__ __forceinline__ float pow2(int e) { return __uint_as_float((uint32_t)(e + 127) << 23); }      // -126 <= e <= 127
+
+template <int D, int NG, bool H16>
+__global__ void __launch_bounds__(kBThreads, 1) q4_block_kernel(const __grid_constant__ Q4AttentionArgs a) {
+    using S = BlockShape<D, NG>;
+    constexpr int NW = D / 32, WPG = NW / NG, kWS = S::kWideStages, kCS = S::kCodeStages;
+    const Q4Geometry &geo = a.geo;
+    extern __shared__ unsigned char smem_raw[];
+    unsigned char *wide = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u), *codes = wide + kWS * S::kWide;
+    __shared__ unsigned long long code_full[kCS], code_empty[kCS], wide_full[kWS], wide_empty[kWS];
+    __shared__ unsigned long long s_full[2], p_ready[2], q_ready[2], o_done, drain;
+    __shared__ uint32_t code_tiles[kCS], code_tokens[kCS];
+    __shared__ UnitInfo info[kWS];
+    __shared__ long long sums[kBThreads / 32], found_at;
+    __shared__ int found_seq, gave_up;
+    __shared__ uint32_t tmem_slot;
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    volatile int *abort_flag = &gave_up;
+    if (tid == 0) {
+        for (int s = 0; s < kCS; ++s) { mbar_init(smem_u32(&code_full[s]), 1); mbar_init(smem_u32(&code_empty[s]), kBWidenWarps); }
+        for (int s = 0; s < kWS; ++s) { mbar_init(smem_u32(&wide_full[s]), kBWidenWarps); mbar_init(smem_u32(&wide_empty[s]), 1); }
+        for (int x = 0; x < 2; ++x) { mbar_init(smem_u32(&s_full[x]), 1); mbar_init(smem_u32(&p_ready[x]), kBHalf); mbar_init(smem_u32(&q_ready[x]), kBHalf); }
+        mbar_init(smem_u32(&o_done), 1);
+        mbar_init(smem_u32(&drain), 1);
+        gave_up = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+
+    // ---- this CTA's share of the batch's units ----
+    const int H = geo.n_kv_heads, n_seqs = a.rows.n_seqs;
+    int *status = blockIdx.x == 0 ? a.status : nullptr;
+    auto weight = [&](int s, int *st) -> long long {
+        if (s >= n_seqs) return 0;
+        const BlockSeq q = block_seq(a, s, st);
+        return block_units_before(q, q.blocks) * H;
+    };
+    long long total = 0;
+    {
+        long long mine = 0;
+        for (int s = tid; s < n_seqs; s += kBThreads) mine += weight(s, status);
+#pragma unroll
+        for (int d = 16; d; d >>= 1) mine += __shfl_xor_sync(0xffffffffu, mine, d);
+        if (lane == 0) sums[warp] = mine;
+        __syncthreads();
+#pragma unroll
+        for (int w = 0; w < kBThreads / 32; ++w) total += sums[w];
+    }
+    const int n_ctas = (int)min((long long)gridDim.x, max(1LL, total / 4));
+    const long long begin = total * blockIdx.x / n_ctas, end = total * (blockIdx.x + 1) / n_ctas;
+    Q4Part *parts = reinterpret_cast<Q4Part *>(a.workspace);
+    float *states = reinterpret_cast<float *>(a.workspace + q4_parts_bytes(gridDim.x));
+    if (blockIdx.x >= n_ctas || begin >= end) {
+        if (tid == 0 && gridDim.x > 1) parts[blockIdx.x].seq = -1;
+        return;
+    }
+    {
+        long long base = 0;
+        for (int s0 = 0; s0 < n_seqs; s0 += kBThreads) {
+            const long long v = weight(s0 + tid, nullptr);
+            long long x = v;
+#pragma unroll
+            for (int d = 1; d < 32; d <<= 1) {
+                const long long y = __shfl_up_sync(0xffffffffu, x, d);
+                if (lane >= d) x += y;
+            }
+            __syncthreads();
+            if (lane == 31) sums[warp] = x;
+            __syncthreads();
+            long long before = base, all = 0;
+#pragma unroll
+            for (int w = 0; w < kBThreads / 32; ++w) {
+                if (w < warp) before += sums[w];
+                all += sums[w];
+            }
+            const long long lo = before + x - v;
+            if (begin >= lo && begin < lo + v) { found_seq = s0 + tid; found_at = begin - lo; }
+            base += all;
+            if (base > begin) break;
+        }
+    }
+    if (warp == 0) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&tmem_slot)), "r"(kBTmemCols) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+    }
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tm = tmem_slot;
+    BlockCursor seg;
+    seg.seq = found_seq;
+    seg.q = block_seq(a, seg.seq, nullptr);
+    {
+        // the block that holds unit `found_at`: the last one with no more units (of all heads) before it
+        int lo = 0, hi = seg.q.blocks;
+        while (hi - lo > 1) {
+            const int mid = (lo + hi) >> 1;
+            if (block_units_before(seg.q, mid) * H <= found_at) lo = mid;
+            else hi = mid;
+        }
+        seg.block = lo;
+        seg.units = block_units(seg.q, lo);
+        const long long in = found_at - block_units_before(seg.q, lo) * H;
+        seg.head = (int)(in / seg.units);
+        seg.unit = (int)(in - (long long)seg.head * seg.units);
+    }
+    const int left = (int)(end - begin);                       // units of the CTA
+    const long long limit = kWaitClocks;
+
+    if (warp == kBCopyWarp) {
+        // ---------------- copies: 32 units are looked up at a time, a lane each, and issued in turn ----------------
+        const int per_page = min(kQ4Unit, geo.page), n_parts = kQ4Unit / per_page, per_tiles = per_page / kQ4Tile;
+        BlockCursor nx = seg;
+        if (lane < left) block_advance(a, nx, lane);
+        bool ok = true;
+        int st = 0, use = 0, u = 0;
+        for (int at = lane; u < left && ok; at += 32) {
+            uint32_t bits = 0;
+            int pg[4] = {-1, -1, -1, -1};
+            const int t0 = nx.unit * kQ4Unit, head = nx.head, tokens = at < left ? max(0, min(kQ4Unit, nx.q.T - t0)) : 0;
+            if (at < left) {
+                const int tiles = (tokens + kQ4Tile - 1) / kQ4Tile;
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    if (i * per_tiles < tiles)
+                        pg[i] = __ldg(a.rows.table + (long long)nx.seq * a.rows.max_pages + ((t0 + i * per_page) >> geo.page_shift));
+                bits = (1u << tiles) - 1u;
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    if (i * per_tiles < tiles && (unsigned)pg[i] >= (unsigned)geo.n_pages) {
+                        atomicAdd(a.status + 1, 1);
+                        bits &= ~(((1u << per_tiles) - 1u) << (i * per_tiles));
+                    }
+                if (at + 32 < left) block_advance(a, nx, 32);
+            }
+            for (int i = 0; i < 32 && u < left; ++i, ++u) {
+                const uint32_t bar = smem_u32(&code_full[st]);
+                if (use > 0 && !wait_warp(smem_u32(&code_empty[st]), (use - 1) & 1, abort_flag, limit)) { ok = false; break; }
+                if (lane == i) {
+                    code_tiles[st] = bits;
+                    code_tokens[st] = tokens;
+                    if (bits) mbar_arrive_expect_tx(bar, __popc(bits) * S::kTile);
+                    else mbar_arrive(bar);
+                    const uint32_t dst = smem_u32(codes) + st * S::kCodes;
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) {
+                        if (k >= n_parts) break;
+                        const int n = __popc(bits >> (k * per_tiles) & ((1u << per_tiles) - 1u));
+                        if (n > 0)
+                            bulk_g2s_keep(dst + k * per_tiles * S::kTile,
+                                          a.pool + (long long)pg[k] * geo.page_bytes + (long long)head * geo.head_bytes +
+                                              (((t0 + k * per_page) & (geo.page - 1)) / kQ4Tile) * S::kTile, n * S::kTile, bar);
+                    }
+                }
+                __syncwarp();
+                if (++st == kCS) { st = 0; ++use; }
+            }
+        }
+        if (!ok && lane == 0 && !*abort_flag) { *abort_flag = 1; atomicAdd(a.status, 1); }
+        // copies in flight must land before the CTA retires: wait (bounded) for the stages armed last
+        for (int back = 1; back <= min(u, kCS); ++back) (void)mbar_wait(smem_u32(&code_full[(u - back) % kCS]), ((u - back) / kCS) & 1, limit);
+    } else if (warp >= kBRowWarps && warp < kBRowWarps + kBWidenWarps) {
+        // ---------------- codes times scales as fp16, a tile of 16 tokens per warp ----------------
+        const int dw = warp - kBRowWarps, c = lane & 3, i8 = lane >> 2;
+        const int t_lane = (i8 >> 1) ^ (i8 & 1 ? 5 : 0);       // tokens t and t ^ 5 side by side: different halves of a line of codes, different banks of a line of fp16
+        bool ok = true;
+        int cs = 0, cu = 0, ws = 0, wu = 0;                    // stages and times they have been used before
+        for (int u = 0; u < left; ++u) {
+            if (!wait_warp(smem_u32(&code_full[cs]), cu & 1, abort_flag, limit) ||
+                (wu > 0 && !wait_warp(smem_u32(&wide_empty[ws]), (wu - 1) & 1, abort_flag, limit))) { ok = false; break; }
+            const uint32_t bits = code_tiles[cs], tokens = code_tokens[cs];
+            const int valid = (bits >> dw) & 1 ? min(max((int)tokens - dw * kQ4Tile, 0), kQ4Tile) : 0;      // tokens of this tile
+            const unsigned char *tp = codes + cs * S::kCodes + dw * S::kTile;
+            unsigned char *wp = wide + ws * S::kWide;
+            // exponents of the largest scales (lanes 0-15: keys of token `lane`, 16-31: values)
+            {
+                const unsigned char *sp = tp + (lane < 16 ? q4_ks_base(D) : q4_vs_base(D, NG)) + (lane & 15) * 2 * NG;
+                uint32_t z, any_nan = 0;
+                if (NG == 4) {
+                    const uint2 x = *reinterpret_cast<const uint2 *>(sp);
+                    z = max_bf16(x.x, x.y);
+                    any_nan = (x.x & 0x7fffu) > 0x7f80u || (x.x >> 16 & 0x7fffu) > 0x7f80u || (x.y & 0x7fffu) > 0x7f80u || (x.y >> 16 & 0x7fffu) > 0x7f80u;
+                } else if (NG == 2) {
+                    z = *reinterpret_cast<const uint32_t *>(sp);
+                    any_nan = (z & 0x7fffu) > 0x7f80u || (z >> 16 & 0x7fffu) > 0x7f80u;
+                } else {
+                    z = *reinterpret_cast<const unsigned short *>(sp);
+                    any_nan = (z & 0x7fffu) > 0x7f80u;
+                }
+                if ((lane & 15) >= valid) { z = 0u; any_nan = 0; }
+                z = max_bf16(z, z >> 16);
+#pragma unroll
+                for (int d = 1; d < 16; d <<= 1) z = max_bf16(z, __shfl_xor_sync(0xffffffffu, z, d));
+                z &= 0xffffu;
+                const int e = z > 0x7f80u ? -60 : min(max((int)(z >> 7) - 127, -60), 60);
+                const uint32_t nan_mask = __ballot_sync(0xffffffffu, any_nan) >> 16;
+                const int ek = __shfl_sync(0xffffffffu, e, 0), ev = __shfl_sync(0xffffffffu, e, 16);
+                if (lane == 0) {
+                    info[ws].ek[dw] = pow2(ek);
+                    info[ws].ev[dw] = (float)ev;
+                    info[ws].v_nan[dw] = nan_mask;
+                    if (dw == 0) { info[ws].tiles = bits; info[ws].tokens = tokens; }
+                }
+                const float fk = pow2(-ek), fv = pow2(-ev);
+#pragma unroll
+                for (int half = 0; half < 2; ++half) {
+                    const int t = t_lane + 8 * half, row = dw * kQ4Tile + t;
+                    const bool there = t < valid;
+                    // K: chunk c of the row, a 16-byte block of eight channels per word
+                    uint32_t kw[NW], sk[NG], sv[NG];
+                    if (NW == 4) {
+                        const uint4 x = *reinterpret_cast<const uint4 *>(tp + q4_k_chunk(D, t, c));
+                        kw[0] = x.x; kw[1] = x.y; kw[NW - 2] = x.z; kw[NW - 1] = x.w;
+                    } else {
+                        const uint2 x = *reinterpret_cast<const uint2 *>(tp + q4_k_chunk(D, t, c));
+                        kw[0] = x.x; kw[1] = x.y;
+                    }
+                    const unsigned short *ks = reinterpret_cast<const unsigned short *>(tp + q4_ks_base(D)) + t * NG;
+                    const unsigned short *vs = reinterpret_cast<const unsigned short *>(tp + q4_vs_base(D, NG)) + t * NG;
+#pragma unroll
+                    for (int k = 0; k < NG; ++k) {
+                        const float x = there ? __uint_as_float((uint32_t)ks[k] << 16) * fk : 0.f;
+                        float y = there ? __uint_as_float((uint32_t)vs[k] << 16) * fv : 0.f;
+                        if (y != y) y = 0.f;                   // (told to the rows by v_nan)
+                        sk[k] = pack_f16(x, x);
+                        sv[k] = pack_f16(y, y);
+                    }
+#pragma unroll
+                    for (int w = 0; w < NW; ++w) {
+                        const uint32_t x = kw[w], x8 = x >> 8, s = sk[w / WPG];
+                        const uint4 o = make_uint4(h2_mul(codes_lo(x), s), h2_mul(codes_hi(x), s), h2_mul(codes_lo(x8), s), h2_mul(codes_hi(x8), s));
+                        *reinterpret_cast<uint4 *>(wp + (w >> 1) * (kQ4Unit * 128) + row * 128 + ((((w & 1) * 4 + c) ^ (row & 7)) << 4)) = o;
+                    }
+                    // V: chunks 2c and 2c + 1, four channels of each per 16-bit word
+                    uint32_t va[(NW + 1) / 2], vb[(NW + 1) / 2];
+                    if (NW == 4) {
+                        const uint2 x = *reinterpret_cast<const uint2 *>(tp + q4_v_base(D) + q4_v_chunk(D, t, 2 * c));
+                        const uint2 y = *reinterpret_cast<const uint2 *>(tp + q4_v_base(D) + q4_v_chunk(D, t, 2 * c + 1));
+                        va[0] = x.x; va[(NW - 1) / 2] = x.y; vb[0] = y.x; vb[(NW - 1) / 2] = y.y;
+                    } else {
+                        va[0] = *reinterpret_cast<const uint32_t *>(tp + q4_v_base(D) + q4_v_chunk(D, t, 2 * c));
+                        vb[0] = *reinterpret_cast<const uint32_t *>(tp + q4_v_base(D) + q4_v_chunk(D, t, 2 * c + 1));
+                    }
+#pragma unroll
+                    for (int w = 0; w < NW; ++w) {
+                        // nibbles n0 .. n3 of 16 bits, and again 12 bits up: n0 and n1 are in bits 0-3 of the halves, n2 and n3 in bits 8-11
+                        uint32_t A = w & 1 ? va[w / 2] >> 16 : va[w / 2] & 0xffffu, B = w & 1 ? vb[w / 2] >> 16 : vb[w / 2] & 0xffffu;
+                        A |= A << 12;
+                        B |= B << 12;
+                        const uint32_t s = sv[w / WPG];
+                        const uint4 o = make_uint4(h2_mul(codes_lo(A), s), h2_mul(codes_lo(A >> 8), s), h2_mul(codes_lo(B), s), h2_mul(codes_lo(B >> 8), s));
+                        *reinterpret_cast<uint4 *>(wp + S::kSide + (w >> 1) * (kQ4Unit * 128) + row * 128 + ((((w & 1) * 4 + c) ^ (row & 7)) << 4)) = o;
+                    }
+                }
+            }
+            fence_async_smem();                                // the products read through the async proxy
+            __syncwarp();
+            if (lane == 0) {
+                mbar_arrive(smem_u32(&wide_full[ws]));
+                mbar_arrive(smem_u32(&code_empty[cs]));
+            }
+            if (++cs == kCS) { cs = 0; ++cu; }
+            if (++ws == kWS) { ws = 0; ++wu; }
+        }
+        if (!ok && lane == 0 && !*abort_flag) { *abort_flag = 1; atomicAdd(a.status, 1); }
+    } else if (warp == kBIssueWarp) {
+        // ---------------- products (one lane) ----------------
+        if (elect_one()) {
+            const uint32_t wide_a = smem_u32(wide);
+            bool ok = true;
+            uint32_t ph_p[2] = {0, 0}, ph_q[2] = {0, 0};
+            int u = 0, ws = 0, wu = 0, ws_old = 0;
+            // s of half x [128 x 64] = Q . K^T: steps of 16 channels, four to a panel
+            auto qk = [&](int x, int stage) {
+                const uint64_t dk = umma_desc(wide_a + stage * S::kWide, 16, 1024, 2);
+#pragma unroll
+                for (int ks = 0; ks < D / 16; ++ks)
+                    umma_ts(tm + S::kColS + x * kQ4Unit, tm + S::kColQ + x * (D / 2) + ks * 8, umma_desc_step(dk, (ks >> 2) * (kQ4Unit * 128) + (ks & 3) * 32),
+                            umma_idesc<true>(128, kQ4Unit, 0), ks > 0);
+            };
+            // o of half x [128 x D] (+)= p . V: steps of 16 tokens
+            auto pv = [&](int x, int stage, bool add) {
+                const uint64_t dv = umma_desc(wide_a + stage * S::kWide + S::kSide, kQ4Unit * 128, 1024, 2);
+#pragma unroll
+                for (int ks = 0; ks < kQ4Unit / 16; ++ks)
+                    umma_ts(tm + S::kColO + x * D, tm + S::kColS + x * kQ4Unit + ks * 8, umma_desc_step(dv, ks * 2048), umma_idesc<true>(128, D, 1), add || ks > 0);
+            };
+            BlockCursor c = seg;
+            while (u < left && ok) {
+                const int n_units = min(left - u, c.units - c.unit);
+                const bool two = (long long)c.block * kBRows + kBHalf < (long long)c.q.n * c.q.G;      // rows in the second half
+                for (int x = 0; x < (two ? 2 : 1); ++x) {
+                    if (!wait_lane(smem_u32(&q_ready[x]), ph_q[x], abort_flag, limit)) { ok = false; break; }
+                    ph_q[x] ^= 1;
+                }
+                if (!ok) break;
+                tc_fence_after();
+                for (int i = 0; i < n_units; ++i) {
+                    if (!wait_lane(smem_u32(&wide_full[ws]), wu & 1, abort_flag, limit)) { ok = false; break; }
+                    tc_fence_after();
+                    qk(0, ws);
+                    umma_commit(smem_u32(&s_full[0]));
+                    if (two) {
+                        if (i > 0) {
+                            if (!wait_lane(smem_u32(&p_ready[1]), ph_p[1], abort_flag, limit)) { ok = false; break; }
+                            ph_p[1] ^= 1;
+                            tc_fence_after();
+                            pv(1, ws_old, i > 1);
+                            umma_commit(smem_u32(&wide_empty[ws_old]));
+                        }
+                        qk(1, ws);
+                        umma_commit(smem_u32(&s_full[1]));
+                    }
+                    if (!wait_lane(smem_u32(&p_ready[0]), ph_p[0], abort_flag, limit)) { ok = false; break; }
+                    ph_p[0] ^= 1;
+                    tc_fence_after();
+                    pv(0, ws, i > 0);
+                    if (!two) umma_commit(smem_u32(&wide_empty[ws]));
+                    ws_old = ws;
+                    if (++ws == kWS) { ws = 0; ++wu; }
+                }
+                if (!ok) break;
+                if (two) {
+                    if (!wait_lane(smem_u32(&p_ready[1]), ph_p[1], abort_flag, limit)) { ok = false; break; }
+                    ph_p[1] ^= 1;
+                    tc_fence_after();
+                    pv(1, ws_old, n_units > 1);
+                    umma_commit(smem_u32(&wide_empty[ws_old]));
+                }
+                umma_commit(smem_u32(&o_done));
+                u += n_units;
+                if (u < left) block_advance(a, c, n_units);
+            }
+            if (!ok && !*abort_flag) { *abort_flag = 1; atomicAdd(a.status, 1); }
+            // nothing of this CTA's may still be running on the tensor cores when tensor memory is given back
+            umma_commit(smem_u32(&drain));
+            (void)mbar_wait(smem_u32(&drain), 0, limit);
+        }
+    } else if (warp < kBRowWarps) {
+        // ---------------- rows: one query row per thread ----------------
+        const int x = warp >> 2, r_half = (warp & 3) * 32 + lane;
+        const uint32_t t_lane = tm + ((uint32_t)((warp & 3) * 32) << 16);
+        const uint32_t t_o = t_lane + S::kColO + x * D, t_q = t_lane + S::kColQ + x * (D / 2), t_s = t_lane + S::kColS + x * kQ4Unit;
+        bool ok = true;
+        uint32_t ph_s = 0, ph_o = 0;
+        int u = 0, ws = 0, wu = 0;
+        BlockCursor c = seg;
+        while (u < left && ok) {
+            const int n_units = min(left - u, c.units - c.unit), G = geo.group;
+            const long long row = (long long)c.block * kBRows + x * kBHalf + r_half;
+            const int j = (int)(row / G), h = c.head * G + (int)(row - (long long)j * G);
+            const bool row_ok = j < c.q.n;
+            if ((long long)c.block * kBRows + x * kBHalf < (long long)c.q.n * G) {      // this half has rows
+                // ---- Q: times a power of two that brings the row's largest magnitude to 1 .. 2, exact in fp16 ----
+                float f;
+                {
+                    const uint4 *qg = reinterpret_cast<const uint4 *>(reinterpret_cast<const unsigned short *>(a.q) + (long long)(c.q.first + j) * a.q_row + (long long)h * a.q_head);
+                    uint4 raw[D / 8];
+                    uint32_t mx = 0;
+#pragma unroll
+                    for (int i = 0; i < D / 8; ++i) {
+                        raw[i] = row_ok ? __ldg(qg + i) : make_uint4(0u, 0u, 0u, 0u);
+                        mx = __vmaxu2(mx, __vmaxu2(__vmaxu2(raw[i].x & 0x7fff7fffu, raw[i].y & 0x7fff7fffu), __vmaxu2(raw[i].z & 0x7fff7fffu, raw[i].w & 0x7fff7fffu)));
+                    }
+                    mx = max(mx & 0xffffu, mx >> 16);
+                    const float big = H16 ? __half2float(__ushort_as_half((unsigned short)mx)) : __uint_as_float(mx << 16);
+                    const int e = min(max((int)(__float_as_uint(big) >> 23) - 127, -60), 60);
+                    const float up = pow2(-e);
+                    f = pow2(e) * geo.scale_log2e;
+#pragma unroll
+                    for (int i = 0; i < D / 32; ++i) {
+                        uint32_t pk[16];
+#pragma unroll
+                        for (int k = 0; k < 4; ++k) {
+                            const uint32_t w[4] = {raw[4 * i + k].x, raw[4 * i + k].y, raw[4 * i + k].z, raw[4 * i + k].w};
+#pragma unroll
+                            for (int b = 0; b < 4; ++b) {
+                                float lo, hi;
+                                if (H16) {
+                                    const float2 v = __half22float2(*reinterpret_cast<const __half2 *>(&w[b]));
+                                    lo = v.x; hi = v.y;
+                                } else {
+                                    lo = bf16lo_f(w[b]); hi = bf16hi_f(w[b]);
+                                }
+                                pk[4 * k + b] = pack_f16(lo * up, hi * up);
+                            }
+                        }
+                        tmem_st16(t_q + 16 * i, pk);
+                    }
+                    tmem_st_wait();
+                    tc_fence_before();
+                    mbar_arrive(smem_u32(&q_ready[x]));
+                }
+                float F = kNegInf, l = 0.f;
+                const int vis = row_ok ? c.q.T - c.q.all + j + 1 : c.q.T;
+                for (int i = 0; i < n_units; ++i, ++u) {
+                    if (!wait_warp(smem_u32(&s_full[x]), ph_s, abort_flag, limit) || !wait_warp(smem_u32(&wide_full[ws]), wu & 1, abort_flag, limit)) { ok = false; break; }
+                    ph_s ^= 1;
+                    tc_fence_after();
+                    float sv[kQ4Unit];
+                    tmem_ld<kQ4Unit>(t_s, reinterpret_cast<uint32_t *>(sv));
+                    const UnitInfo &inf = info[ws];
+                    const int t0 = (c.unit + i) * kQ4Unit, lim = min(vis - t0, (int)inf.tokens);
+                    const uint32_t tiles = inf.tiles;
+                    if (__any_sync(0xffffffffu, lim < kQ4Unit) || tiles != (1u << kQ4UnitTiles) - 1u) {
+                        uint32_t nan = 0;
+#pragma unroll
+                        for (int k = 0; k < kQ4Unit; ++k)
+                            if (!(k < lim && (tiles >> (k / kQ4Tile) & 1))) sv[k] = -INFINITY;
+#pragma unroll
+                        for (int k = 0; k < kQ4UnitTiles; ++k) {
+                            const int m = min(max(lim - k * kQ4Tile, 0), kQ4Tile);
+                            nan |= inf.v_nan[k] & ((1u << m) - 1u);
+                        }
+                        if (nan) l = __int_as_float(0x7fc00000);
+                    } else if (inf.v_nan[0] | inf.v_nan[1] | inf.v_nan[2] | inf.v_nan[3]) {
+                        l = __int_as_float(0x7fc00000);        // a value that is not finite: the row is not either
+                    }
+                    // x = s * f 2^Ek + Ev, against a reference that the largest has not passed by more than 2^8
+                    float fk[kQ4UnitTiles], ev[kQ4UnitTiles], top = -INFINITY;
+#pragma unroll
+                    for (int k = 0; k < kQ4UnitTiles; ++k) {
+                        fk[k] = fmaxf(f * inf.ek[k], 1.2e-38f);      // (never 0: a hidden score is -inf)
+                        ev[k] = inf.ev[k];
+                        const float *p = sv + k * kQ4Tile;
+                        float m0 = max3(p[0], p[1], p[2]), m1 = max3(p[3], p[4], p[5]);
+                        m0 = max3(m0, p[6], p[7]); m1 = max3(m1, p[8], p[9]);
+                        m0 = max3(m0, p[10], p[11]); m1 = max3(m1, p[12], p[13]);
+                        m0 = max3(m0, p[14], p[15]);
+                        top = fmaxf(top, fmaf(fmaxf(m0, m1), fk[k], ev[k]));
+                    }
+                    if (__any_sync(0xffffffffu, top > F + kQ4Lag)) {
+                        const float Fn = top > kNegInf ? fmaxf(F, top) : F, corr = ex2(F - Fn);
+                        F = Fn;
+                        l *= corr;
+                        if (i > 0) {                           // (every earlier product of this half is complete: s was committed behind it)
+                            uint32_t r[32];
+#pragma unroll 1
+                            for (int b = 0; b < D / 32; ++b) {
+                                tmem_ld32(t_o + 32 * b, r);
+                                tmem_ld_wait();
+#pragma unroll
+                                for (int k = 0; k < 32; ++k) r[k] = __float_as_uint(__uint_as_float(r[k]) * corr);
+                                tmem_st32(t_o + 32 * b, r);
+                            }
+                        }
+                    }
+                    uint32_t pk[kQ4Unit / 2];
+#pragma unroll
+                    for (int k = 0; k < kQ4UnitTiles; ++k) {
+                        const uint64_t m2 = f2_pack(fk[k], fk[k]), b2 = f2_pack(ev[k] - F, ev[k] - F);
+                        uint64_t sum[2] = {0ull, 0ull};
+#pragma unroll
+                        for (int b = 0; b < kQ4Tile / 2; ++b) {
+                            const int q = k * kQ4Tile + 2 * b;
+                            float y0, y1;
+                            f2_unpack(f2_fma3(f2_pack(sv[q], sv[q + 1]), m2, b2), y0, y1);
+                            y0 = exp2_fast(y0);
+                            y1 = exp2_fast(y1);
+                            sum[b & 1] = f2_add(sum[b & 1], f2_pack(y0, y1));
+                            pk[q / 2] = pack_f16(y0, y1);
+                        }
+                        float s0, s1;
+                        f2_unpack(f2_add(sum[0], sum[1]), s0, s1);
+                        l = fmaf(s0 + s1, pow2(-(int)ev[k]), l);
+                    }
+                    tmem_st32(t_s, pk);
+                    tmem_st_wait();
+                    tc_fence_before();
+                    mbar_arrive(smem_u32(&p_ready[x]));
+                    if (++ws == kWS) { ws = 0; ++wu; }
+                }
+                if (!ok) break;
+                if (!wait_warp(smem_u32(&o_done), ph_o, abort_flag, limit)) { ok = false; break; }
+                tc_fence_after();
+                // ---- the block's result, or its state where the block goes on in another CTA ----
+                const bool complete = c.unit == 0 && n_units == c.units;
+                const int slot = u == n_units ? 0 : 1;
+                const float inv = complete && !a.state ? (l != 0.f ? 1.f / l : 0.f) : 1.f;
+                float *dst = nullptr;
+                if (!complete) dst = states + (2LL * blockIdx.x + slot) * q4_state_floats(kBRows, D) + (long long)(x * kBHalf + r_half) * D;
+                else if (a.state && row_ok) dst = a.state + ((long long)(c.q.first + j) * geo.n_q_heads + h) * (D + 2);
+                unsigned short *out = reinterpret_cast<unsigned short *>(a.out) + (long long)(c.q.first + j) * a.out_row + (long long)h * a.out_head;
+#pragma unroll 1
+                for (int b = 0; b < D / 32; ++b) {
+                    uint32_t r[32];
+                    tmem_ld32(t_o + 32 * b, r);
+                    tmem_ld_wait();
+#pragma unroll
+                    for (int k = 0; k < 32; ++k) r[k] = __float_as_uint(__uint_as_float(r[k]) * inv);
+                    if (dst) {
+#pragma unroll
+                        for (int k = 0; k < 16; ++k) *reinterpret_cast<uint2 *>(dst + 32 * b + 2 * k) = make_uint2(r[2 * k], r[2 * k + 1]);
+                    } else if (complete && row_ok) {
+#pragma unroll
+                        for (int k = 0; k < 4; ++k) {
+                            uint32_t w[4];
+#pragma unroll
+                            for (int m = 0; m < 4; ++m) {
+                                const float y0 = __uint_as_float(r[8 * k + 2 * m]), y1 = __uint_as_float(r[8 * k + 2 * m + 1]);
+                                w[m] = H16 ? pack_f16(y0, y1) : pack_bf16(y0, y1);
+                            }
+                            *reinterpret_cast<uint4 *>(out + 32 * b + 8 * k) = make_uint4(w[0], w[1], w[2], w[3]);
+                        }
+                    }
+                }
+                if (!complete) {
+                    float *ml = states + (2LL * blockIdx.x + slot) * q4_state_floats(kBRows, D) + (long long)kBRows * D;
+                    ml[x * kBHalf + r_half] = F;
+                    ml[kBRows + x * kBHalf + r_half] = l;
+                } else if (dst) {
+                    *reinterpret_cast<float2 *>(dst + D) = make_float2(F, l);
+                }
+                tc_fence_before();                             // (o is read before the next block's products, which wait for Q, overwrite it)
+            } else {
+                u += n_units;
+                const int steps = ws + n_units;
+                wu += steps / kWS;
+                ws = steps % kWS;
+            }
+            ph_o ^= 1;
+            if (tid == 0 && gridDim.x > 1 && u == left) {
+                Q4Part p{-1, 0, 0, 0, 0};
+                if (c.unit == 0 && n_units < c.units) {
+                    const long long w1 = begin + u - n_units + c.units;      // one past the block's last unit
+                    p = Q4Part{c.seq, c.block, c.head, u == n_units ? 0 : 1, (int)((w1 * n_ctas - 1) / total)};
+                }
+                parts[blockIdx.x] = p;
+            }
+            if (u < left) block_advance(a, c, n_units);
+        }
+        if (!ok && lane == 0 && !*abort_flag) { *abort_flag = 1; atomicAdd(a.status, 1); }
+        if (!ok && tid == 0 && gridDim.x > 1) parts[blockIdx.x].seq = -1;
+    }
+    // ---------------- every thread: give tensor memory back ----------------
+    tc_fence_before();
+    __syncthreads();
+    if (warp == 0) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tm), "r"(kBTmemCols) : "memory");
+}
+
+#define PKV_Q4_SHAPES(X) X(128, 4) X(128, 2) X(128, 1) X(64, 2) X(64, 1)
+
+}  // namespace
+
+cudaError_t q4_block_setup() {
+    cudaError_t e;
+#define PKV_Q4_SETUP1(D, NG, H16) \
+    if ((e = cudaFuncSetAttribute(q4_block_kernel<D, NG, H16>, cudaFuncAttributeMaxDynamicSharedMemorySize, BlockShape<D, NG>::kSmem)) != cudaSuccess) return e;
+#define PKV_Q4_SETUP(D, NG) PKV_Q4_SETUP1(D, NG, false) PKV_Q4_SETUP1(D, NG, true)
+    PKV_Q4_SHAPES(PKV_Q4_SETUP)
+    return cudaSuccess;
+}
+
+// CTAs: one per SM, four units each at least, as far as the host can tell.
+int q4_block_grid(const Q4Geometry &g, int n_seqs, int max_q_len, int max_len) {
+    const double blocks = (double)(((long long)max_q_len * g.group + kBRows - 1) / kBRows), units = (max_len + kQ4Unit - 1) / kQ4Unit;
+    const double all = (double)n_seqs * g.n_kv_heads * blocks * units / 4;
+    return all >= g.n_sms ? g.n_sms : all < 1 ? 1 : (int)all;
+}
+
+long long q4_block_workspace(const Q4Geometry &g, int n_seqs, int max_q_len, int max_len) {
+    const int n = q4_block_grid(g, n_seqs, max_q_len, max_len);
+    return n <= 1 ? 0 : q4_parts_bytes(n) + 2LL * n * q4_state_floats(kBRows, g.head_dim) * 4;
+}
+
+cudaError_t launch_q4_block(const Q4AttentionArgs &a, int n, cudaStream_t st) {
+    const Q4Geometry &g = a.geo;
+    cudaLaunchAttribute at[1];
+    at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    at[0].val.programmaticStreamSerializationAllowed = 1;
+    cudaLaunchConfig_t cfg = {};
+    cfg.stream = st;
+    cfg.attrs = at;
+    cfg.numAttrs = 1;
+    cfg.gridDim = dim3(n);
+    cfg.blockDim = dim3(kBThreads);
+#define PKV_Q4_LAUNCH1(D, NG, H16)                                                                       \
+    if (g.head_dim == D && g.groups == NG && (g.fp16 != 0) == H16) {                                     \
+        cfg.dynamicSmemBytes = BlockShape<D, NG>::kSmem;                                                 \
+        return cudaLaunchKernelEx(&cfg, q4_block_kernel<D, NG, H16>, a);                                 \
+    }
+#define PKV_Q4_LAUNCH(D, NG) PKV_Q4_LAUNCH1(D, NG, false) PKV_Q4_LAUNCH1(D, NG, true)
+    PKV_Q4_SHAPES(PKV_Q4_LAUNCH)
+    return cudaErrorInvalidValue;
+}
+
+}  // namespace pkv

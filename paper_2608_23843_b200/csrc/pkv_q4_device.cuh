@@ -1,0 +1,63 @@
+// Device-side helpers shared by the kernels that attend over the 4-bit cache.  Internal linkage, as in pkv_device.cuh.
+#pragma once
+
+#include <cuda_fp16.h>
+
+#include "pkv_device.cuh"
+#include "pkv_q4.h"
+
+namespace pkv {
+
+namespace {
+
+constexpr int kQ4Unit = 64;            // tokens per unit: four tiles
+constexpr int kQ4UnitTiles = kQ4Unit / kQ4Tile;
+constexpr float kQ4Lag = 8.f;          // how far (base 2) scores may pass the softmax's reference before it follows
+
+// A segment that begins in a CTA and ends in another (seq < 0: none); slot: where its first part is (see below)
+struct Q4Part { int seq, tile, head, slot, last_cta; };
+
+// Partial states: two per CTA (its first segment, its last), each [8 NT rows][D] o, then m and l of the rows.
+__host__ __device__ inline long long q4_state_floats(int rows, int d) { return (long long)rows * (d + 2); }
+__host__ __device__ inline long long q4_parts_bytes(int n_ctas) { return ((long long)n_ctas * (int)sizeof(Q4Part) + 255) / 256 * 256; }
+
+// The rows of a sequence that the call works on; `all`: with those beyond the caller's bound, which the positions go by.
+__device__ __forceinline__ int q4_new_rows(const Q4AttentionArgs &a, int s, int &first, int &all, int *status) {
+    first = q4_first_row(a.rows, s);
+    all = q4_first_row(a.rows, s + 1) - first;
+    if (status && all > a.max_q_len) atomicAdd(status + 2, 1);
+    return max(0, min(all, a.max_q_len));
+}
+
+__device__ __forceinline__ float ex2(float x) {
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+__device__ __forceinline__ uint32_t pack_f16(float lo, float hi) {
+    uint32_t r;
+    asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+    return r;
+}
+__device__ __forceinline__ uint32_t max_bf16(uint32_t x, uint32_t y) {      // (the other operand where one is NaN)
+    uint32_t r;
+    asm("max.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(x), "r"(y));
+    return r;
+}
+__device__ __forceinline__ uint32_t sub_h2(uint32_t x, uint32_t y) {
+    uint32_t r;
+    asm("sub.rn.f16x2 %0, %1, %2;" : "=r"(r) : "r"(x), "r"(y));
+    return r;
+}
+// Bounded wait that also ends when another warp has given up.
+__device__ __forceinline__ bool mbar_wait_or(uint32_t bar, uint32_t parity, volatile int *abort_flag) {
+    if (mbar_try_wait(bar, parity)) return true;
+    const long long t0 = clock64();
+    while (!mbar_try_wait(bar, parity))
+        if (clock64() - t0 > kWaitClocks || *abort_flag) return false;
+    return true;
+}
+
+}  // namespace
+
+}  // namespace pkv

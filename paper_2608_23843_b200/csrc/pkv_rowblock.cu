@@ -31,6 +31,7 @@
 // the row threads ahead of commit "Q".  Two CTAs per SM overlap one another's remaining waits; the blocks of a
 // launch are taken longest first.  Every wait is bounded; tensor memory is released on every path out.
 #include "pkv_device.cuh"
+#include "pkv_umma.cuh"
 
 namespace pkv {
 
@@ -69,130 +70,6 @@ __host__ __device__ inline int umma_stages(const Geometry &g) {
     return max(3, min(6, room / umma_stage_bytes(g)));
 }
 
-// ---- tcgen05 wrappers --------------------------------------------------------------------------------------
-// Shared-memory matrix descriptor: start address, leading / stride byte offsets (all in 16-byte units), descriptor
-// version 1, layout 0 = no swizzle, 2 = 128-byte swizzle.
-__device__ __forceinline__ uint64_t umma_desc(uint32_t saddr, uint32_t lbo, uint32_t sbo, uint32_t layout) {
-    return (uint64_t)((saddr >> 4) & 0x3FFF) | (uint64_t)((lbo >> 4) & 0x3FFF) << 16 | (uint64_t)((sbo >> 4) & 0x3FFF) << 32 |
-           (uint64_t)1 << 46 | (uint64_t)layout << 61;
-}
-// The same descriptor `bytes` further on (a multiple of 16; the start-address field, in 16-byte units, is the lowest
-// field and the sum stays inside the 256 KB the field covers): one 32-bit add on the low word.
-__device__ __forceinline__ uint64_t umma_desc_step(uint64_t desc, uint32_t bytes) {
-    uint32_t lo, hi;
-    asm("mov.b64 {%0, %1}, %2;" : "=r"(lo), "=r"(hi) : "l"(desc));
-    lo += bytes >> 4;
-    uint64_t d;
-    asm("mov.b64 %0, {%1, %2};" : "=l"(d) : "r"(lo), "r"(hi));
-    return d;
-}
-// Instruction descriptor: bf16 x bf16 -> fp32, M x N, B operand K-major (0) or MN-major (1); A always K-major.
-__host__ __device__ constexpr uint32_t umma_idesc(int M, int N, int b_mn_major) {
-    return (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)b_mn_major << 16) | ((uint32_t)(N >> 3) << 17) | ((uint32_t)(M >> 4) << 24);
-}
-// d (+)= a . b with a in shared memory / in tensor memory (row = lane, two bf16 per 32-bit column, 8 columns per
-// step of 16 along the contraction)
-__device__ __forceinline__ void umma_ss(uint32_t d_tmem, uint64_t adesc, uint64_t bdesc, uint32_t idesc, uint32_t accumulate) {
-    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\ttcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}"
-                 ::"r"(d_tmem), "l"(adesc), "l"(bdesc), "r"(idesc), "r"(accumulate) : "memory");
-}
-__device__ __forceinline__ void umma_ts(uint32_t d_tmem, uint32_t a_tmem, uint64_t bdesc, uint32_t idesc, uint32_t accumulate) {
-    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\ttcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}"
-                 ::"r"(d_tmem), "r"(a_tmem), "l"(bdesc), "r"(idesc), "r"(accumulate) : "memory");
-}
-__device__ __forceinline__ void umma_commit(uint32_t bar) {
-    asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
-}
-__device__ __forceinline__ void tc_fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
-__device__ __forceinline__ void tc_fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
-__device__ __forceinline__ void fence_async_smem() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
-// Tiled copy of one box (64 channels x the map's rows) starting at channel x of pool row y; completes on `bar`.
-__device__ __forceinline__ void tma_box(uint32_t dst, const CUtensorMap *map, int x, int y, uint32_t bar) {
-    asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];"
-                 ::"r"(dst), "l"(map), "r"(x), "r"(y), "r"(bar) : "memory");
-}
-
-#define PKV_R8(r, o) "=r"(r[o]), "=r"(r[o + 1]), "=r"(r[o + 2]), "=r"(r[o + 3]), "=r"(r[o + 4]), "=r"(r[o + 5]), "=r"(r[o + 6]), "=r"(r[o + 7])
-#define PKV_W8(r, o) "r"(r[o]), "r"(r[o + 1]), "r"(r[o + 2]), "r"(r[o + 3]), "r"(r[o + 4]), "r"(r[o + 5]), "r"(r[o + 6]), "r"(r[o + 7])
-// consecutive 32-bit columns of this thread's lane
-__device__ __forceinline__ void tmem_ld32(uint32_t taddr, uint32_t *r) {
-    asm volatile("tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,"
-                 "%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%32];"
-                 : PKV_R8(r, 0), PKV_R8(r, 8), PKV_R8(r, 16), PKV_R8(r, 24) : "r"(taddr));
-}
-__device__ __forceinline__ void tmem_ld16(uint32_t taddr, uint32_t *r) {
-    asm volatile("tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];"
-                 : PKV_R8(r, 0), PKV_R8(r, 8) : "r"(taddr));
-}
-__device__ __forceinline__ void tmem_ld_wait() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
-__device__ __forceinline__ void tmem_st32(uint32_t taddr, const uint32_t *r) {
-    asm volatile("tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,"
-                 "%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31,%32};"
-                 ::"r"(taddr), PKV_W8(r, 0), PKV_W8(r, 8), PKV_W8(r, 16), PKV_W8(r, 24) : "memory");
-}
-__device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t *r) {
-    asm volatile("tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16};"
-                 ::"r"(taddr), PKV_W8(r, 0), PKV_W8(r, 8) : "memory");
-}
-__device__ __forceinline__ void tmem_st8(uint32_t taddr, const uint32_t *r) {
-    asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"r"(taddr), PKV_W8(r, 0) : "memory");
-}
-__device__ __forceinline__ void tmem_st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
-template <int N>
-__device__ __forceinline__ void tmem_ld_nowait(uint32_t taddr, uint32_t *r) {
-    static_assert(N == 16 || N == 32, "16 or 32 columns");
-    if (N == 16) tmem_ld16(taddr, r);
-    else tmem_ld32(taddr, r);
-}
-template <int N>
-__device__ __forceinline__ void tmem_ld(uint32_t taddr, uint32_t *r) {
-    static_assert(N == 16 || N == 32 || N == 64, "16, 32 or 64 columns");
-    if (N == 16) tmem_ld16(taddr, r);
-    else { tmem_ld32(taddr, r); if (N == 64) tmem_ld32(taddr + 32, r + 32); }
-    tmem_ld_wait();
-}
-template <int N>
-__device__ __forceinline__ void tmem_st(uint32_t taddr, const uint32_t *r) {
-    static_assert(N == 8 || N == 16 || N == 32, "8, 16 or 32 columns");
-    if (N == 8) tmem_st8(taddr, r);
-    else if (N == 16) tmem_st16(taddr, r);
-    else tmem_st32(taddr, r);
-}
-// True in exactly one lane of a converged warp.  The single-lane roles are entered through this rather than through
-// `lane == 0`: the compiler then knows that one lane runs the code, and issues tcgen05.mma (whose operands are
-// warp-uniform registers) directly; behind a plain lane test each issue measured 230 clocks instead of 40.
-__device__ __forceinline__ bool elect_one() {
-    uint32_t leader;
-    asm volatile("{\n\t.reg .pred P;\n\telect.sync _|P, 0xffffffff;\n\tselp.u32 %0, 1, 0, P;\n\t}" : "=r"(leader));
-    return leader != 0;
-}
-// 2^x for x <= 0 (and the large negative stand-ins for -inf, which give 0)
-__device__ __forceinline__ float exp2_fast(float x) {
-    float y;
-    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-    return y;
-}
-
-// Bounded waits.  One lane (producer, issuer): gives up when the clock limit passes or another role has given up.
-__device__ __forceinline__ bool wait_lane(uint32_t bar, uint32_t parity, volatile int *abort_flag, long long limit) {
-    if (mbar_try_wait(bar, parity)) return true;
-    const long long t0 = clock64();
-    while (!mbar_try_wait(bar, parity)) {
-        if (clock64() - t0 > limit || *abort_flag) return false;
-    }
-    return true;
-}
-// A whole warp (the row threads run warp-collective tensor-memory loads right after): the outcome is the same for
-// all 32 lanes.
-__device__ __forceinline__ bool wait_warp(uint32_t bar, uint32_t parity, volatile int *abort_flag, long long limit) {
-    if (__all_sync(0xffffffffu, mbar_try_wait(bar, parity))) return true;
-    const long long t0 = clock64();
-    for (;;) {
-        if (__all_sync(0xffffffffu, mbar_try_wait(bar, parity))) return true;
-        if (__any_sync(0xffffffffu, clock64() - t0 > limit || *abort_flag)) return false;
-    }
-}
-
 // Softmax state of this thread's row.  p and l are always taken against the true running maximum m, so the largest
 // weight is exactly 1 and its bf16 rounding costs nothing.  o, which lives in tensor memory, is kept against an
 // older maximum m_ref <= m instead of being rescaled every time m grows: a factor page's contribution enters o
@@ -225,36 +102,6 @@ __host__ __device__ inline StageLayout umma_layout(const Geometry &g) {
     }
     L.d_panel = umma_part_rows(g) * 128; L.dk = 0; L.dv = 2 * L.d_panel;
     return L;
-}
-
-// Two fp32 values in one 64-bit register, and the sm_100 instructions that work on both halves at once: the row
-// threads' arithmetic is issue-bound (two row warps per scheduler), so halving the instruction count of the
-// subtractions, sums and scalings shows.  Likewise the three-input maximum.
-__device__ __forceinline__ uint64_t f2_pack(float lo, float hi) {
-    uint64_t v;
-    asm("mov.b64 %0, {%1, %2};" : "=l"(v) : "f"(lo), "f"(hi));
-    return v;
-}
-__device__ __forceinline__ void f2_unpack(uint64_t v, float &lo, float &hi) { asm("mov.b64 {%0, %1}, %2;" : "=f"(lo), "=f"(hi) : "l"(v)); }
-__device__ __forceinline__ uint64_t f2_add(uint64_t a, uint64_t b) {
-    uint64_t d;
-    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
-    return d;
-}
-__device__ __forceinline__ uint64_t f2_sub(uint64_t a, uint64_t b) {
-    uint64_t d;
-    asm("sub.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
-    return d;
-}
-__device__ __forceinline__ uint64_t f2_mul(uint64_t a, uint64_t b) {
-    uint64_t d;
-    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
-    return d;
-}
-__device__ __forceinline__ float max3(float a, float b, float c) {
-    float d;
-    asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
-    return d;
 }
 
 // RP fp32 values x (a row of q~ or w) times `scale`, as bf16 pairs; columns from `rank` on become exact zeros.  The
@@ -530,7 +377,7 @@ __global__ void __launch_bounds__(kUThreads, 2) block_umma_kernel(const __grid_c
             // other CTA's products for half as long at a time)
             // (n: rows of the K side - RP for G1, the rows of a block for a dense unit)
             auto qk = [&](uint32_t t_dst, uint32_t kside, int panel, int ks0, int ks1, int n) {
-                const uint32_t idesc = umma_idesc(128, n, 0);
+                const uint32_t idesc = umma_idesc<>(128, n, 0);
                 const uint64_t db0 = umma_desc(kside, 16, 1024, 2), db1 = umma_desc(kside + panel, 16, 1024, 2);
 #pragma unroll
                 for (int ks = 0; ks < 8; ++ks)
@@ -543,7 +390,7 @@ __global__ void __launch_bounds__(kUThreads, 2) block_umma_kernel(const __grid_c
                 const uint64_t dv = umma_desc(vside, panel, 1024, 2);
 #pragma unroll
                 for (int ks = 0; ks < 2; ++ks)
-                    if (ks * 16 < k) umma_ts(t_o, t_src + ks * 8, umma_desc_step(dv, ks * 2048), umma_idesc(128, 128, 1), o_valid || ks > 0);
+                    if (ks * 16 < k) umma_ts(t_o, t_src + ks * 8, umma_desc_step(dv, ks * 2048), umma_idesc<>(128, 128, 1), o_valid || ks > 0);
                 o_valid = true;
             };
             // kind of a unit as the products see it: units without tokens run as dense units with every score masked
@@ -570,7 +417,7 @@ __global__ void __launch_bounds__(kUThreads, 2) block_umma_kernel(const __grid_c
                             const uint64_t da = umma_desc(sb + L.av + j * umma_a_bytes(geo, geo.rank_v), 16, kAGroup, kASwizzle);
 #pragma unroll
                             for (int ks = 0; ks < P / 16; ++ks)      // w = p . A_v, A_v^T in place (K-major)
-                                umma_ts(t_w + j * RP1, t_s + (j * (P / 16) + ks) * 8, umma_desc_step(da, ks * 32), umma_idesc(128, RP1, 0), ks > 0);
+                                umma_ts(t_w + j * RP1, t_s + (j * (P / 16) + ks) * 8, umma_desc_step(da, ks * 32), umma_idesc<>(128, RP1, 0), ks > 0);
                         }
                     } else {
                         pv(t_s, sb + L.dv, L.d_panel, kDB);
@@ -591,7 +438,7 @@ __global__ void __launch_bounds__(kUThreads, 2) block_umma_kernel(const __grid_c
                                 const uint64_t dak = umma_desc(sb + L.ak + j * umma_a_bytes(geo, geo.rank_k), 16, kAGroup, kASwizzle);
 #pragma unroll
                                 for (int t = 0; t < 2; ++t)
-                                    umma_ts(t_s + j * P, t_qt + t * (RP / 2) + j * 8, dak, umma_idesc(128, P, 1), t > 0);
+                                    umma_ts(t_s + j * P, t_qt + t * (RP / 2) + j * 8, dak, umma_idesc<>(128, P, 1), t > 0);
                             }
                         } else {
                             const uint64_t dak = umma_desc(sb + L.ak, 16, kAGroup, kASwizzle);
@@ -600,7 +447,7 @@ __global__ void __launch_bounds__(kUThreads, 2) block_umma_kernel(const __grid_c
 #pragma unroll
                                 for (int ks = 0; ks < RP / 16; ++ks)
                                     umma_ts(t_s, t_qt + t * (RP / 2) + ks * 8, umma_desc_step(dak, ks * 2 * kAGroup),
-                                            umma_idesc(128, P, 1), (t | ks) > 0);
+                                            umma_idesc<>(128, P, 1), (t | ks) > 0);
                         }
                     } else {
                         qk(t_s, sb + L.dk, L.d_panel, 0, 8, kDB);
