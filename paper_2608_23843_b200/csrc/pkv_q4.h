@@ -80,14 +80,14 @@ cudaError_t launch_q4_block(const Q4AttentionArgs &a, int n, cudaStream_t st);
 long long q4_attention_workspace(const Q4Geometry &g, int n_seqs, int max_q_len, int max_len);
 
 // byte offsets inside a tile
-__host__ __device__ inline int q4_v_base(int d) { return kQ4Tile * d / 2; }
-__host__ __device__ inline int q4_ks_base(int d) { return kQ4Tile * d; }
-__host__ __device__ inline int q4_vs_base(int d, int groups) { return kQ4Tile * d + kQ4Tile * groups * 2; }
+__host__ __device__ constexpr int q4_v_base(int d) { return kQ4Tile * d / 2; }
+__host__ __device__ constexpr int q4_ks_base(int d) { return kQ4Tile * d; }
+__host__ __device__ constexpr int q4_vs_base(int d, int groups) { return kQ4Tile * d + kQ4Tile * groups * 2; }
 // K: a row is d/2 bytes, chunk c = d/8 bytes of it
-__host__ __device__ inline int q4_k_chunk(int d, int t, int c) { return t * (d / 2) + c * (d / 8); }
+__host__ __device__ constexpr int q4_k_chunk(int d, int t, int c) { return t * (d / 2) + c * (d / 8); }
 // V: chunk g = d/16 bytes (8 or 4).  A warp reads chunk g of tokens 2c (then 2c + 1, ...) in one load: within each 128-byte
 // line the chunks are XORed so that the lanes that are served together hit different banks.
-__host__ __device__ inline int q4_v_chunk(int d, int t, int g) {
+__host__ __device__ constexpr int q4_v_chunk(int d, int t, int g) {
     if (d == 128) {                    // a line is two tokens of eight 8-byte chunks
         const int line = t >> 1, slot = ((t & 1) << 3 | g) ^ ((line & 1) << 2 | ((line >> 1) & 1) << 3);
         return line * 128 + slot * 8;

@@ -247,7 +247,7 @@ __global__ void __launch_bounds__(Q4Shape<D, NG, NT>::kThreads, 2) q4_decode_ker
             }
             for (int i = 0; i < 32 && u < left_cta; ++i, ++u) {
                 const uint32_t bar = smem_u32(&full[st]);
-                if (use > 0 && !__all_sync(0xffffffffu, mbar_wait_or(smem_u32(&empty[st]), (use - 1) & 1, abort_flag))) { ok = false; break; }
+                if (use > 0 && !(mbar_wait_warp(smem_u32(&empty[st]), (use - 1) & 1, abort_flag))) { ok = false; break; }
                 if (lane == i) {
                     tiles_here[st] = bits;
                     if (bits) mbar_arrive_expect_tx(bar, __popc(bits) * S::kTile);
@@ -385,7 +385,7 @@ __global__ void __launch_bounds__(Q4Shape<D, NG, NT>::kThreads, 2) q4_decode_ker
         while (at < seg_hi) {
             const int t_unit = (seg.unit + at - seg_lo) * kQ4Unit;
             uint32_t tiles = 0;
-            if (__all_sync(0xffffffffu, mbar_wait_or(smem_u32(&full[st]), phase, abort_flag))) tiles = tiles_here[st];
+            if ((mbar_wait_warp(smem_u32(&full[st]), phase, abort_flag))) tiles = tiles_here[st];
             else if (lane == 0 && !*abort_flag) { *abort_flag = 1; atomicAdd(a.status, 1); }      // (the unit counts as not there)
             const bool whole = tiles == (1u << kQ4UnitTiles) - 1u && t_unit + kQ4Unit <= vis_all;
             const unsigned char *sp = smem + st * S::kStage;

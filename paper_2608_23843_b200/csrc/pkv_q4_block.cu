@@ -2,20 +2,22 @@
 // the fifth-generation tensor cores.
 //
 // A CTA works on blocks of up to 256 query rows of one (sequence, KV head), as two halves of 128 (the M dimension of every
-// product; one thread owns one row).  Tokens come in units of 64:
-//     warp 13        looks up pages and copies a unit's tiles of codes and scales into a ring,
-//     warps 8-11     a tile each: codes times scales as fp16 into shared memory, K and V in the layouts the products read
-//                    (128-byte swizzle, panels of 64 channels).  A code (3 bits and a sign) times a bf16 scale (8 bits) has
-//                    11 bits, so fp16 holds it exactly; a power of two per tile (the exponent of its largest scale, handed on
-//                    to the rows) keeps it inside fp16's range whatever the values' size,
-//     warp 12        one lane issues the products: s = Q K^T with Q and, later, p as row operands in tensor memory,
-//                    o += p V; while one half's rows are in their softmax the other half's products run,
-//     warps 0-7      softmax: s from tensor memory, p as fp16 back over it, o rescaled only when the running reference has
-//                    been passed by 2^8 (then p * value may still not leave fp16: 2^8 * 14).
-// What bounds it: per unit and 256 rows the products take 1024 cycles and the exponentials as many (16 per cycle and SM),
-// which overlap; the widening of the codes (some 370 instructions per warp and unit) hides behind both and is paid once for
-// 256 rows.  CTAs share the batch's units evenly, one CTA per SM; blocks that span CTAs leave states that a second kernel
-// joins.  Units after a block's last visible position are not visited.
+// product; one thread owns one row).  A block of at most 128 rows gives both halves the same rows and every other unit, and
+// their states are joined at its end.  Tokens come in units of 64:
+//     one warp       looks up pages and copies a unit's tiles of codes and scales into a ring,
+//     five warps     widen: a tile at a time in turn, codes times scales as fp16 into shared memory, in the layouts the
+//                    products read (128-byte swizzle, panels of 64 channels).  A code (3 bits and a sign) times a bf16 scale
+//                    (8 bits) has 11 bits, so fp16 holds it exactly; a power of two per tile (the exponent of its largest
+//                    scale, handed on to the rows) keeps it inside fp16's range whatever the values' size,
+//     two warps      issue the products, one lane per half: s = Q K^T, o += p V with s, o and p in tensor memory (p as the row
+//                    operand; Q too for the first half - tensor memory is full - and in shared memory for the second),
+//     eight warps    softmax: s from tensor memory, p as fp16 beside it, o rescaled only when the running reference has been
+//                    passed by 2^8 (then p * value may still not leave fp16: 2^8 * 14).
+// s of the next unit is computed as soon as the rows have s of this one in registers, and o += p V runs behind their next
+// softmax, so the rows wait for neither.  What bounds it: per unit and 256 rows the products take 1150 cycles and the
+// exponentials 1024 (16 per cycle and SM), beside some 1000 instructions per scheduler; the widening is paid once for 256
+// rows.  CTAs share the batch's units evenly, one CTA per SM; blocks that span CTAs leave states that a second kernel joins.
+// Units after a block's last visible position are not visited.
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 
@@ -26,20 +28,22 @@ namespace pkv {
 
 namespace {
 
-constexpr int kBRows = kQ4BlockRows, kBHalf = 128, kBThreads = 448;
-constexpr int kBRowWarps = 8, kBWidenWarps = 4, kBIssueWarp = 12, kBCopyWarp = 13;
+constexpr int kBRows = kQ4BlockRows, kBHalf = 128;
+// warps: 0-7 rows, 8-12 widening, 13 and 14 issue the products, 15 copies (sixteen warps of 128 registers fill the register file)
+constexpr int kBThreads = 512, kBRowWarps = 8, kBWidenWarps = 5, kBIssueWarp = 13, kBCopyWarp = 15;
 constexpr uint32_t kBTmemCols = 512;
 
 template <int D, int NG>
 struct BlockShape {
     static constexpr int kPanels = D / 64, kSide = kPanels * kQ4Unit * 128, kWide = 2 * kSide;      // K panels, then V panels of a unit
     static constexpr int kTile = kQ4Tile * (D + 4 * NG), kUnitBytes = kQ4UnitTiles * kTile, kCodes = (kUnitBytes + 127) / 128 * 128;
-    static constexpr int kWideStages = 4, kFit = (222 * 1024 - kWideStages * kWide) / kCodes, kCodeStages = kFit < 8 ? kFit : 8;
-    static constexpr int kSmem = kWideStages * kWide + kCodeStages * kCodes + 1024;                 // (+ alignment)
-    static_assert(kCodeStages >= 4 && kSmem <= 226 * 1024, "fits one CTA per SM");
-    // columns of tensor memory: o of both halves, Q of both halves (fp16 pairs), s of both halves
-    static constexpr uint32_t kColO = 0, kColQ = 2 * D, kColS = 2 * D + D;
-    static_assert(kColS + 2 * kQ4Unit <= kBTmemCols, "fits tensor memory");
+    static constexpr int kQPanel = kBHalf * 128, kQBytes = kPanels * kQPanel;                       // Q of the second half
+    static constexpr int kWideStages = 4, kFit = (220 * 1024 - kWideStages * kWide - kQBytes) / kCodes, kCodeStages = kFit < 8 ? kFit : 8;
+    static constexpr int kSmem = kWideStages * kWide + kQBytes + kCodeStages * kCodes + 1024;       // (+ alignment)
+    static_assert(kCodeStages >= 4 && kSmem <= 224 * 1024, "fits one CTA per SM");
+    // columns of tensor memory: o of both halves, Q of the first (fp16 pairs), s of both, p of both (fp16 pairs)
+    static constexpr uint32_t kColO = 0, kColQ = 2 * D, kColS = kColQ + D / 2, kColP = kColS + 2 * kQ4Unit;
+    static_assert(kColP + kQ4Unit <= kBTmemCols, "fits tensor memory");
 };
 
 // sum over i < n of floor((a i + b) / m), for a, b >= 0 and m > 0 (by the Euclid-like recursion on (a, m))
@@ -126,6 +130,22 @@ __device__ __forceinline__ uint32_t h2_mul(uint32_t x, uint32_t y) {
 __device__ __forceinline__ uint32_t codes_lo(uint32_t x) { return sub_h2((x & 0x000f000fu) | 0x64006400u, 0x64086408u); }
 __device__ __forceinline__ uint32_t codes_hi(uint32_t x) { return sub_h2((x & 0x00f000f0u) | 0x54005400u, 0x54805480u); }
 
+// shared-memory accesses in the order they are written down
+__device__ __forceinline__ void lds32(uint32_t *r, uint32_t at) { asm volatile("ld.shared.u32 %0, [%1];" : "=r"(r[0]) : "r"(at)); }
+__device__ __forceinline__ void lds64(uint32_t *r, uint32_t at) { asm volatile("ld.shared.v2.u32 {%0, %1}, [%2];" : "=r"(r[0]), "=r"(r[1]) : "r"(at)); }
+__device__ __forceinline__ void lds128(uint32_t *r, uint32_t at) {
+    asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(at));
+}
+__device__ __forceinline__ void sts128(uint32_t at, uint32_t x, uint32_t y, uint32_t z, uint32_t w) {
+    asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(x), "r"(y), "r"(z), "r"(w) : "memory");
+}
+template <int NG>
+__device__ __forceinline__ void lds_scales(uint32_t *r, uint32_t at) {      // a token's scales, two to a word
+    if (NG == 4) lds64(r, at);
+    else if (NG == 2) lds32(r, at);
+    else { uint16_t x; asm volatile("ld.shared.u16 %0, [%1];" : "=h"(x) : "r"(at)); r[0] = x; }
+}
+
 __device__ __forceinline__ uint64_t f2_fma3(uint64_t a, uint64_t b, uint64_t c) {
     uint64_t d;
     asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(a), "l"(b), "l"(c));
@@ -139,22 +159,27 @@ __global__ void __launch_bounds__(kBThreads, 1) q4_block_kernel(const __grid_con
     constexpr int NW = D / 32, WPG = NW / NG, kWS = S::kWideStages, kCS = S::kCodeStages;
     const Q4Geometry &geo = a.geo;
     extern __shared__ unsigned char smem_raw[];
-    unsigned char *wide = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u), *codes = wide + kWS * S::kWide;
+    unsigned char *wide = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u), *q_mem = wide + kWS * S::kWide, *codes = q_mem + S::kQBytes;
     __shared__ unsigned long long code_full[kCS], code_empty[kCS], wide_full[kWS], wide_empty[kWS];
-    __shared__ unsigned long long s_full[2], p_ready[2], q_ready[2], o_done, drain;
+    __shared__ unsigned long long s_full[2], s_read[2], p_ready[2], p_free[2], q_ready[2], o_done[2], drain[2], state_ready, state_read;
     __shared__ uint32_t code_tiles[kCS], code_tokens[kCS];
     __shared__ UnitInfo info[kWS];
+    __shared__ float2 ml_other[kBHalf];
     __shared__ long long sums[kBThreads / 32], found_at;
     __shared__ int found_seq, gave_up;
     __shared__ uint32_t tmem_slot;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     volatile int *abort_flag = &gave_up;
     if (tid == 0) {
-        for (int s = 0; s < kCS; ++s) { mbar_init(smem_u32(&code_full[s]), 1); mbar_init(smem_u32(&code_empty[s]), kBWidenWarps); }
-        for (int s = 0; s < kWS; ++s) { mbar_init(smem_u32(&wide_full[s]), kBWidenWarps); mbar_init(smem_u32(&wide_empty[s]), 1); }
-        for (int x = 0; x < 2; ++x) { mbar_init(smem_u32(&s_full[x]), 1); mbar_init(smem_u32(&p_ready[x]), kBHalf); mbar_init(smem_u32(&q_ready[x]), kBHalf); }
-        mbar_init(smem_u32(&o_done), 1);
-        mbar_init(smem_u32(&drain), 1);
+        for (int s = 0; s < kCS; ++s) { mbar_init(smem_u32(&code_full[s]), 1); mbar_init(smem_u32(&code_empty[s]), kQ4UnitTiles); }
+        for (int s = 0; s < kWS; ++s) { mbar_init(smem_u32(&wide_full[s]), kQ4UnitTiles); mbar_init(smem_u32(&wide_empty[s]), 2); }
+        for (int x = 0; x < 2; ++x) {
+            mbar_init(smem_u32(&s_full[x]), 1); mbar_init(smem_u32(&s_read[x]), kBHalf); mbar_init(smem_u32(&p_ready[x]), kBHalf);
+            mbar_init(smem_u32(&p_free[x]), 1); mbar_init(smem_u32(&q_ready[x]), kBHalf); mbar_init(smem_u32(&o_done[x]), 1);
+            mbar_init(smem_u32(&drain[x]), 1);
+        }
+        mbar_init(smem_u32(&state_ready), kBHalf);
+        mbar_init(smem_u32(&state_read), kBHalf);
         gave_up = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
@@ -269,7 +294,7 @@ __global__ void __launch_bounds__(kBThreads, 1) q4_block_kernel(const __grid_con
             }
             for (int i = 0; i < 32 && u < left; ++i, ++u) {
                 const uint32_t bar = smem_u32(&code_full[st]);
-                if (use > 0 && !wait_warp(smem_u32(&code_empty[st]), (use - 1) & 1, abort_flag, limit)) { ok = false; break; }
+                if (use > 0 && !mbar_wait_warp(smem_u32(&code_empty[st]), (use - 1) & 1, abort_flag)) { ok = false; break; }
                 if (lane == i) {
                     code_tiles[st] = bits;
                     code_tokens[st] = tokens;
@@ -294,97 +319,103 @@ __global__ void __launch_bounds__(kBThreads, 1) q4_block_kernel(const __grid_con
         // copies in flight must land before the CTA retires: wait (bounded) for the stages armed last
         for (int back = 1; back <= min(u, kCS); ++back) (void)mbar_wait(smem_u32(&code_full[(u - back) % kCS]), ((u - back) / kCS) & 1, limit);
     } else if (warp >= kBRowWarps && warp < kBRowWarps + kBWidenWarps) {
-        // ---------------- codes times scales as fp16, a tile of 16 tokens per warp ----------------
-        const int dw = warp - kBRowWarps, c = lane & 3, i8 = lane >> 2;
+        // ---------------- codes times scales as fp16: a tile of 16 tokens per warp, keys or values ----------------
+        const int c = lane & 3, i8 = lane >> 2;
         const int t_lane = (i8 >> 1) ^ (i8 & 1 ? 5 : 0);       // tokens t and t ^ 5 side by side: different halves of a line of codes, different banks of a line of fp16
         bool ok = true;
-        int cs = 0, cu = 0, ws = 0, wu = 0;                    // stages and times they have been used before
-        for (int u = 0; u < left; ++u) {
-            if (!wait_warp(smem_u32(&code_full[cs]), cu & 1, abort_flag, limit) ||
-                (wu > 0 && !wait_warp(smem_u32(&wide_empty[ws]), (wu - 1) & 1, abort_flag, limit))) { ok = false; break; }
+        int dw = warp - kBRowWarps;                            // tile of the unit
+        int cs = 0, cu = 0;                                    // stage of the codes and times it has been used before
+        const uint32_t k_at = q4_k_chunk(D, t_lane, c), va_at = q4_v_base(D) + q4_v_chunk(D, t_lane, 2 * c), vb_at = q4_v_base(D) + q4_v_chunk(D, t_lane, 2 * c + 1);
+        const uint32_t s_at = (lane < 16 ? q4_ks_base(D) : q4_vs_base(D, NG)) + (lane & 15) * 2 * NG;
+        constexpr uint32_t kNext = q4_k_chunk(D, 8, 0);        // tokens t + 8: the same place eight rows on, for V too
+        static_assert(q4_v_chunk(D, 8, 0) == (int)kNext && q4_v_chunk(D, 13, 5) == q4_v_chunk(D, 5, 5) + (int)kNext, "the pattern repeats");
+        for (int u = 0; u < left; dw += kBWidenWarps) {
+            while (dw >= kQ4UnitTiles && u < left) {
+                dw -= kQ4UnitTiles;
+                if (++cs == kCS) { cs = 0; ++cu; }
+                ++u;
+            }
+            if (u >= left) break;
+            const int ws = u % kWS, wu = u / kWS;
+            if (!mbar_wait_warp(smem_u32(&code_full[cs]), cu & 1, abort_flag)) { ok = false; break; }
             const uint32_t bits = code_tiles[cs], tokens = code_tokens[cs];
             const int valid = (bits >> dw) & 1 ? min(max((int)tokens - dw * kQ4Tile, 0), kQ4Tile) : 0;      // tokens of this tile
-            const unsigned char *tp = codes + cs * S::kCodes + dw * S::kTile;
-            unsigned char *wp = wide + ws * S::kWide;
-            // exponents of the largest scales (lanes 0-15: keys of token `lane`, 16-31: values)
-            {
-                const unsigned char *sp = tp + (lane < 16 ? q4_ks_base(D) : q4_vs_base(D, NG)) + (lane & 15) * 2 * NG;
-                uint32_t z, any_nan = 0;
-                if (NG == 4) {
-                    const uint2 x = *reinterpret_cast<const uint2 *>(sp);
-                    z = max_bf16(x.x, x.y);
-                    any_nan = (x.x & 0x7fffu) > 0x7f80u || (x.x >> 16 & 0x7fffu) > 0x7f80u || (x.y & 0x7fffu) > 0x7f80u || (x.y >> 16 & 0x7fffu) > 0x7f80u;
-                } else if (NG == 2) {
-                    z = *reinterpret_cast<const uint32_t *>(sp);
-                    any_nan = (z & 0x7fffu) > 0x7f80u || (z >> 16 & 0x7fffu) > 0x7f80u;
+            const uint32_t tp = smem_u32(codes) + cs * S::kCodes + dw * S::kTile;
+            // everything is read before anything is written: nothing here waits for a store
+            uint32_t z2[(NG + 1) / 2], ksc[2][(NG + 1) / 2], vsc[2][(NG + 1) / 2], kw[2][NW], va[2][(NW + 1) / 2], vb[2][(NW + 1) / 2];
+            lds_scales<NG>(z2, tp + s_at);
+#pragma unroll
+            for (int half = 0; half < 2; ++half) {
+                lds_scales<NG>(ksc[half], tp + q4_ks_base(D) + (t_lane + 8 * half) * 2 * NG);
+                lds_scales<NG>(vsc[half], tp + q4_vs_base(D, NG) + (t_lane + 8 * half) * 2 * NG);
+                if (NW == 4) {
+                    lds128(kw[half], tp + k_at + half * kNext);
+                    lds64(va[half], tp + va_at + half * kNext);
+                    lds64(vb[half], tp + vb_at + half * kNext);
                 } else {
-                    z = *reinterpret_cast<const unsigned short *>(sp);
-                    any_nan = (z & 0x7fffu) > 0x7f80u;
+                    lds64(kw[half], tp + k_at + half * kNext);
+                    lds32(va[half], tp + va_at + half * kNext);
+                    lds32(vb[half], tp + vb_at + half * kNext);
                 }
-                if ((lane & 15) >= valid) { z = 0u; any_nan = 0; }
-                z = max_bf16(z, z >> 16);
-#pragma unroll
-                for (int d = 1; d < 16; d <<= 1) z = max_bf16(z, __shfl_xor_sync(0xffffffffu, z, d));
-                z &= 0xffffu;
-                const int e = z > 0x7f80u ? -60 : min(max((int)(z >> 7) - 127, -60), 60);
-                const uint32_t nan_mask = __ballot_sync(0xffffffffu, any_nan) >> 16;
-                const int ek = __shfl_sync(0xffffffffu, e, 0), ev = __shfl_sync(0xffffffffu, e, 16);
-                if (lane == 0) {
-                    info[ws].ek[dw] = pow2(ek);
-                    info[ws].ev[dw] = (float)ev;
-                    info[ws].v_nan[dw] = nan_mask;
-                    if (dw == 0) { info[ws].tiles = bits; info[ws].tokens = tokens; }
-                }
-                const float fk = pow2(-ek), fv = pow2(-ev);
-#pragma unroll
-                for (int half = 0; half < 2; ++half) {
-                    const int t = t_lane + 8 * half, row = dw * kQ4Tile + t;
-                    const bool there = t < valid;
-                    // K: chunk c of the row, a 16-byte block of eight channels per word
-                    uint32_t kw[NW], sk[NG], sv[NG];
-                    if (NW == 4) {
-                        const uint4 x = *reinterpret_cast<const uint4 *>(tp + q4_k_chunk(D, t, c));
-                        kw[0] = x.x; kw[1] = x.y; kw[NW - 2] = x.z; kw[NW - 1] = x.w;
-                    } else {
-                        const uint2 x = *reinterpret_cast<const uint2 *>(tp + q4_k_chunk(D, t, c));
-                        kw[0] = x.x; kw[1] = x.y;
-                    }
-                    const unsigned short *ks = reinterpret_cast<const unsigned short *>(tp + q4_ks_base(D)) + t * NG;
-                    const unsigned short *vs = reinterpret_cast<const unsigned short *>(tp + q4_vs_base(D, NG)) + t * NG;
+            }
+            // exponents of the largest scales (lanes 0-15: keys of token `lane`, 16-31: values): as bits, which order like the values
+            uint32_t z = z2[0], nans = 0;
+            if (NG == 4) z = __vmaxu2(z, z2[(NG - 1) / 2]);
+            z = max(z & 0xffffu, z >> 16);
+            if ((lane & 15) >= valid) z = 0u;
+            if (__any_sync(0xffffffffu, z > 0x7f80u)) {        // a group that is not finite: look at the others of its token
+                const bool nan = z > 0x7f80u;
+                nans = __ballot_sync(0xffffffffu, nan) >> 16;
+                if (nan) {
+                    z = 0u;
 #pragma unroll
                     for (int k = 0; k < NG; ++k) {
-                        const float x = there ? __uint_as_float((uint32_t)ks[k] << 16) * fk : 0.f;
-                        float y = there ? __uint_as_float((uint32_t)vs[k] << 16) * fv : 0.f;
-                        if (y != y) y = 0.f;                   // (told to the rows by v_nan)
-                        sk[k] = pack_f16(x, x);
-                        sv[k] = pack_f16(y, y);
+                        const uint32_t x = (z2[k / 2] >> (16 * (k & 1))) & 0xffffu;
+                        if (x <= 0x7f80u) z = max(z, x);
                     }
+                }
+            }
+            const int ek = min(max((int)(__reduce_max_sync(0xffffffffu, lane < 16 ? z : 0u) >> 7) - 127, -60), 60);
+            const int ev = min(max((int)(__reduce_max_sync(0xffffffffu, lane < 16 ? 0u : z) >> 7) - 127, -60), 60);
+            const float fk = pow2(-ek), fv = pow2(-ev);
+            uint32_t sk[2][NG], sv[2][NG];
 #pragma unroll
-                    for (int w = 0; w < NW; ++w) {
-                        const uint32_t x = kw[w], x8 = x >> 8, s = sk[w / WPG];
-                        const uint4 o = make_uint4(h2_mul(codes_lo(x), s), h2_mul(codes_hi(x), s), h2_mul(codes_lo(x8), s), h2_mul(codes_hi(x8), s));
-                        *reinterpret_cast<uint4 *>(wp + (w >> 1) * (kQ4Unit * 128) + row * 128 + ((((w & 1) * 4 + c) ^ (row & 7)) << 4)) = o;
-                    }
-                    // V: chunks 2c and 2c + 1, four channels of each per 16-bit word
-                    uint32_t va[(NW + 1) / 2], vb[(NW + 1) / 2];
-                    if (NW == 4) {
-                        const uint2 x = *reinterpret_cast<const uint2 *>(tp + q4_v_base(D) + q4_v_chunk(D, t, 2 * c));
-                        const uint2 y = *reinterpret_cast<const uint2 *>(tp + q4_v_base(D) + q4_v_chunk(D, t, 2 * c + 1));
-                        va[0] = x.x; va[(NW - 1) / 2] = x.y; vb[0] = y.x; vb[(NW - 1) / 2] = y.y;
-                    } else {
-                        va[0] = *reinterpret_cast<const uint32_t *>(tp + q4_v_base(D) + q4_v_chunk(D, t, 2 * c));
-                        vb[0] = *reinterpret_cast<const uint32_t *>(tp + q4_v_base(D) + q4_v_chunk(D, t, 2 * c + 1));
-                    }
+            for (int half = 0; half < 2; ++half)
 #pragma unroll
-                    for (int w = 0; w < NW; ++w) {
-                        // nibbles n0 .. n3 of 16 bits, and again 12 bits up: n0 and n1 are in bits 0-3 of the halves, n2 and n3 in bits 8-11
-                        uint32_t A = w & 1 ? va[w / 2] >> 16 : va[w / 2] & 0xffffu, B = w & 1 ? vb[w / 2] >> 16 : vb[w / 2] & 0xffffu;
-                        A |= A << 12;
-                        B |= B << 12;
-                        const uint32_t s = sv[w / WPG];
-                        const uint4 o = make_uint4(h2_mul(codes_lo(A), s), h2_mul(codes_lo(A >> 8), s), h2_mul(codes_lo(B), s), h2_mul(codes_lo(B >> 8), s));
-                        *reinterpret_cast<uint4 *>(wp + S::kSide + (w >> 1) * (kQ4Unit * 128) + row * 128 + ((((w & 1) * 4 + c) ^ (row & 7)) << 4)) = o;
-                    }
+                for (int k = 0; k < NG; ++k) {
+                    float x = (k & 1 ? bf16hi_f(ksc[half][k / 2]) : bf16lo_f(ksc[half][k / 2])) * fk;
+                    float y = (k & 1 ? bf16hi_f(vsc[half][k / 2]) : bf16lo_f(vsc[half][k / 2])) * fv;
+                    if (t_lane + 8 * half >= valid) x = y = 0.f;
+                    if (y != y) y = 0.f;                       // (a value that is not finite: told to the rows by v_nan)
+                    sk[half][k] = pack_f16(x, x);
+                    sv[half][k] = pack_f16(y, y);
+                }
+            if (wu > 0 && !mbar_wait_warp(smem_u32(&wide_empty[ws]), (wu - 1) & 1, abort_flag)) { ok = false; break; }
+            if (lane == 0) {
+                info[ws].ek[dw] = pow2(ek);
+                info[ws].ev[dw] = (float)ev;
+                info[ws].v_nan[dw] = nans;
+                if (dw == 0) { info[ws].tiles = bits; info[ws].tokens = tokens; }
+            }
+#pragma unroll
+            for (int half = 0; half < 2; ++half) {
+                const int row = dw * kQ4Tile + t_lane + 8 * half;
+                const uint32_t dst = smem_u32(wide) + ws * S::kWide + row * 128;
+#pragma unroll
+                for (int w = 0; w < NW; ++w) {                 // K: a 16-byte block of eight channels per word
+                    const uint32_t x = kw[half][w], x8 = x >> 8, s = sk[half][w / WPG];
+                    sts128(dst + (w >> 1) * (kQ4Unit * 128) + ((((w & 1) * 4 + c) ^ (row & 7)) << 4), h2_mul(codes_lo(x), s), h2_mul(codes_hi(x), s),
+                           h2_mul(codes_lo(x8), s), h2_mul(codes_hi(x8), s));
+                }
+#pragma unroll
+                for (int w = 0; w < NW; ++w) {
+                    // V: nibbles n0 .. n3 of 16 bits, and again 12 bits up: n0 and n1 are in bits 0-3 of the halves, n2 and n3 in bits 8-11
+                    uint32_t A = w & 1 ? va[half][w / 2] >> 16 : va[half][w / 2] & 0xffffu, B = w & 1 ? vb[half][w / 2] >> 16 : vb[half][w / 2] & 0xffffu;
+                    A |= A << 12;
+                    B |= B << 12;
+                    const uint32_t s = sv[half][w / WPG];
+                    sts128(dst + S::kSide + (w >> 1) * (kQ4Unit * 128) + ((((w & 1) * 4 + c) ^ (row & 7)) << 4), h2_mul(codes_lo(A), s), h2_mul(codes_lo(A >> 8), s),
+                           h2_mul(codes_lo(B), s), h2_mul(codes_lo(B >> 8), s));
                 }
             }
             fence_async_smem();                                // the products read through the async proxy
@@ -393,98 +424,98 @@ __global__ void __launch_bounds__(kBThreads, 1) q4_block_kernel(const __grid_con
                 mbar_arrive(smem_u32(&wide_full[ws]));
                 mbar_arrive(smem_u32(&code_empty[cs]));
             }
-            if (++cs == kCS) { cs = 0; ++cu; }
-            if (++ws == kWS) { ws = 0; ++wu; }
         }
         if (!ok && lane == 0 && !*abort_flag) { *abort_flag = 1; atomicAdd(a.status, 1); }
-    } else if (warp == kBIssueWarp) {
-        // ---------------- products (one lane) ----------------
+    } else if (warp == kBIssueWarp || warp == kBIssueWarp + 1) {
+        // ---------------- products of one half (one lane) ----------------
         if (elect_one()) {
-            const uint32_t wide_a = smem_u32(wide);
+            const int x = warp - kBIssueWarp;
+            const uint32_t wide_a = smem_u32(wide), t_s = tm + S::kColS + x * kQ4Unit, t_p = tm + S::kColP + x * (kQ4Unit / 2), t_o = tm + S::kColO + x * D;
+            const uint64_t dq = umma_desc(smem_u32(q_mem), 16, 1024, 2);
             bool ok = true;
-            uint32_t ph_p[2] = {0, 0}, ph_q[2] = {0, 0};
-            int u = 0, ws = 0, wu = 0, ws_old = 0;
-            // s of half x [128 x 64] = Q . K^T: steps of 16 channels, four to a panel
-            auto qk = [&](int x, int stage) {
+            uint32_t ph_s = 0, ph_p = 0, ph_q = 0;
+            int u = 0;
+            // s [128 x 64] = Q . K^T: steps of 16 channels, four to a panel
+            auto qk = [&](int stage) {
                 const uint64_t dk = umma_desc(wide_a + stage * S::kWide, 16, 1024, 2);
 #pragma unroll
-                for (int ks = 0; ks < D / 16; ++ks)
-                    umma_ts(tm + S::kColS + x * kQ4Unit, tm + S::kColQ + x * (D / 2) + ks * 8, umma_desc_step(dk, (ks >> 2) * (kQ4Unit * 128) + (ks & 3) * 32),
-                            umma_idesc<true>(128, kQ4Unit, 0), ks > 0);
+                for (int ks = 0; ks < D / 16; ++ks) {
+                    const uint64_t b = umma_desc_step(dk, (ks >> 2) * (kQ4Unit * 128) + (ks & 3) * 32);
+                    if (x == 0) umma_ts(t_s, tm + S::kColQ + ks * 8, b, umma_idesc<true>(128, kQ4Unit, 0), ks > 0);
+                    else umma_ss(t_s, umma_desc_step(dq, (ks >> 2) * S::kQPanel + (ks & 3) * 32), b, umma_idesc<true>(128, kQ4Unit, 0), ks > 0);
+                }
+                umma_commit(smem_u32(&s_full[x]));
             };
-            // o of half x [128 x D] (+)= p . V: steps of 16 tokens
-            auto pv = [&](int x, int stage, bool add) {
+            // o [128 x D] (+)= p . V: steps of 16 tokens
+            auto pv = [&](int stage, bool add) {
                 const uint64_t dv = umma_desc(wide_a + stage * S::kWide + S::kSide, kQ4Unit * 128, 1024, 2);
 #pragma unroll
                 for (int ks = 0; ks < kQ4Unit / 16; ++ks)
-                    umma_ts(tm + S::kColO + x * D, tm + S::kColS + x * kQ4Unit + ks * 8, umma_desc_step(dv, ks * 2048), umma_idesc<true>(128, D, 1), add || ks > 0);
+                    umma_ts(t_o, t_p + ks * 8, umma_desc_step(dv, ks * 2048), umma_idesc<true>(128, D, 1), add || ks > 0);
+                umma_commit(smem_u32(&wide_empty[stage]));
             };
             BlockCursor c = seg;
             while (u < left && ok) {
                 const int n_units = min(left - u, c.units - c.unit);
-                const bool two = (long long)c.block * kBRows + kBHalf < (long long)c.q.n * c.q.G;      // rows in the second half
-                for (int x = 0; x < (two ? 2 : 1); ++x) {
-                    if (!wait_lane(smem_u32(&q_ready[x]), ph_q[x], abort_flag, limit)) { ok = false; break; }
-                    ph_q[x] ^= 1;
-                }
-                if (!ok) break;
-                tc_fence_after();
-                for (int i = 0; i < n_units; ++i) {
-                    if (!wait_lane(smem_u32(&wide_full[ws]), wu & 1, abort_flag, limit)) { ok = false; break; }
-                    tc_fence_after();
-                    qk(0, ws);
-                    umma_commit(smem_u32(&s_full[0]));
-                    if (two) {
-                        if (i > 0) {
-                            if (!wait_lane(smem_u32(&p_ready[1]), ph_p[1], abort_flag, limit)) { ok = false; break; }
-                            ph_p[1] ^= 1;
-                            tc_fence_after();
-                            pv(1, ws_old, i > 1);
-                            umma_commit(smem_u32(&wide_empty[ws_old]));
-                        }
-                        qk(1, ws);
-                        umma_commit(smem_u32(&s_full[1]));
+                const bool two = (long long)c.block * kBRows + kBHalf < (long long)c.q.n * c.q.G;      // the halves have rows of their own
+                int done = 0, stage = 0;                       // units of this half issued, and the stage of the last
+                for (int i = 0; i < n_units && ok; ++i, ++u) {
+                    const int ws = u % kWS;
+                    if (!mbar_wait_or(smem_u32(&wide_full[ws]), (u / kWS) & 1, abort_flag)) { ok = false; break; }
+                    if (!two && (i & 1) != x) {                // the other half's
+                        mbar_arrive(smem_u32(&wide_empty[ws]));
+                        continue;
                     }
-                    if (!wait_lane(smem_u32(&p_ready[0]), ph_p[0], abort_flag, limit)) { ok = false; break; }
-                    ph_p[0] ^= 1;
+                    const uint32_t bar = done == 0 ? smem_u32(&q_ready[x]) : smem_u32(&s_read[x]);      // Q is there, or s is in registers
+                    if (!mbar_wait_or(bar, done == 0 ? ph_q : ph_s, abort_flag)) { ok = false; break; }
+                    if (done == 0) ph_q ^= 1;
+                    else ph_s ^= 1;
                     tc_fence_after();
-                    pv(0, ws, i > 0);
-                    if (!two) umma_commit(smem_u32(&wide_empty[ws]));
-                    ws_old = ws;
-                    if (++ws == kWS) { ws = 0; ++wu; }
+                    qk(ws);
+                    if (done > 0) {
+                        if (!mbar_wait_or(smem_u32(&p_ready[x]), ph_p, abort_flag)) { ok = false; break; }
+                        ph_p ^= 1;
+                        tc_fence_after();
+                        pv(stage, done > 1);
+                        umma_commit(smem_u32(&p_free[x]));
+                    }
+                    stage = ws;
+                    ++done;
                 }
                 if (!ok) break;
-                if (two) {
-                    if (!wait_lane(smem_u32(&p_ready[1]), ph_p[1], abort_flag, limit)) { ok = false; break; }
-                    ph_p[1] ^= 1;
+                if (done > 0) {
+                    if (!mbar_wait_or(smem_u32(&s_read[x]), ph_s, abort_flag) || !mbar_wait_or(smem_u32(&p_ready[x]), ph_p, abort_flag)) { ok = false; break; }
+                    ph_s ^= 1;
+                    ph_p ^= 1;
                     tc_fence_after();
-                    pv(1, ws_old, n_units > 1);
-                    umma_commit(smem_u32(&wide_empty[ws_old]));
+                    pv(stage, done > 1);
+                    umma_commit(smem_u32(&o_done[x]));
                 }
-                umma_commit(smem_u32(&o_done));
-                u += n_units;
                 if (u < left) block_advance(a, c, n_units);
             }
             if (!ok && !*abort_flag) { *abort_flag = 1; atomicAdd(a.status, 1); }
             // nothing of this CTA's may still be running on the tensor cores when tensor memory is given back
-            umma_commit(smem_u32(&drain));
-            (void)mbar_wait(smem_u32(&drain), 0, limit);
+            umma_commit(smem_u32(&drain[x]));
+            (void)mbar_wait(smem_u32(&drain[x]), 0, limit);
         }
     } else if (warp < kBRowWarps) {
         // ---------------- rows: one query row per thread ----------------
         const int x = warp >> 2, r_half = (warp & 3) * 32 + lane;
         const uint32_t t_lane = tm + ((uint32_t)((warp & 3) * 32) << 16);
-        const uint32_t t_o = t_lane + S::kColO + x * D, t_q = t_lane + S::kColQ + x * (D / 2), t_s = t_lane + S::kColS + x * kQ4Unit;
+        const uint32_t t_o = t_lane + S::kColO + x * D, t_s = t_lane + S::kColS + x * kQ4Unit, t_p = t_lane + S::kColP + x * (kQ4Unit / 2);
         bool ok = true;
-        uint32_t ph_s = 0, ph_o = 0;
-        int u = 0, ws = 0, wu = 0;
+        uint32_t ph_s = 0, ph_o = 0, ph_f = 0, ph_st = 0;
+        int u = 0;
         BlockCursor c = seg;
         while (u < left && ok) {
             const int n_units = min(left - u, c.units - c.unit), G = geo.group;
-            const long long row = (long long)c.block * kBRows + x * kBHalf + r_half;
+            const bool two = (long long)c.block * kBRows + kBHalf < (long long)c.q.n * G;
+            const long long row = (long long)c.block * kBRows + (two ? x * kBHalf : 0) + r_half;
             const int j = (int)(row / G), h = c.head * G + (int)(row - (long long)j * G);
             const bool row_ok = j < c.q.n;
-            if ((long long)c.block * kBRows + x * kBHalf < (long long)c.q.n * G) {      // this half has rows
+            const int i0 = two ? 0 : x, step = two ? 1 : 2;    // this half's units
+            float F = kNegInf, l = 0.f;
+            if (i0 < n_units) {
                 // ---- Q: times a power of two that brings the row's largest magnitude to 1 .. 2, exact in fp16 ----
                 float f;
                 {
@@ -519,23 +550,34 @@ __global__ void __launch_bounds__(kBThreads, 1) q4_block_kernel(const __grid_con
                                 pk[4 * k + b] = pack_f16(lo * up, hi * up);
                             }
                         }
-                        tmem_st16(t_q + 16 * i, pk);
+                        if (x == 0) {
+                            tmem_st16(t_lane + S::kColQ + 16 * i, pk);
+                        } else {                               // 32 channels: half a 128-byte row of a panel
+#pragma unroll
+                            for (int k = 0; k < 4; ++k)
+                                *reinterpret_cast<uint4 *>(q_mem + (i >> 1) * S::kQPanel + r_half * 128 + ((((i & 1) * 4 + k) ^ (r_half & 7)) << 4)) =
+                                    make_uint4(pk[4 * k], pk[4 * k + 1], pk[4 * k + 2], pk[4 * k + 3]);
+                        }
                     }
-                    tmem_st_wait();
+                    if (x == 0) tmem_st_wait();
+                    else fence_async_smem();
                     tc_fence_before();
                     mbar_arrive(smem_u32(&q_ready[x]));
                 }
-                float F = kNegInf, l = 0.f;
                 const int vis = row_ok ? c.q.T - c.q.all + j + 1 : c.q.T;
-                for (int i = 0; i < n_units; ++i, ++u) {
-                    if (!wait_warp(smem_u32(&s_full[x]), ph_s, abort_flag, limit) || !wait_warp(smem_u32(&wide_full[ws]), wu & 1, abort_flag, limit)) { ok = false; break; }
+                for (int i = i0; i < n_units; i += step) {
+                    const int ws = (u + i) % kWS;
+                    if (!mbar_wait_warp(smem_u32(&s_full[x]), ph_s, abort_flag) || !mbar_wait_warp(smem_u32(&wide_full[ws]), ((u + i) / kWS) & 1, abort_flag)) { ok = false; break; }
                     ph_s ^= 1;
                     tc_fence_after();
                     float sv[kQ4Unit];
                     tmem_ld<kQ4Unit>(t_s, reinterpret_cast<uint32_t *>(sv));
+                    tc_fence_before();
+                    mbar_arrive(smem_u32(&s_read[x]));
                     const UnitInfo &inf = info[ws];
                     const int t0 = (c.unit + i) * kQ4Unit, lim = min(vis - t0, (int)inf.tokens);
                     const uint32_t tiles = inf.tiles;
+                    bool free = i == i0;                       // p and o of the unit before are no longer in use
                     if (__any_sync(0xffffffffu, lim < kQ4Unit) || tiles != (1u << kQ4UnitTiles) - 1u) {
                         uint32_t nan = 0;
 #pragma unroll
@@ -567,7 +609,11 @@ __global__ void __launch_bounds__(kBThreads, 1) q4_block_kernel(const __grid_con
                         const float Fn = top > kNegInf ? fmaxf(F, top) : F, corr = ex2(F - Fn);
                         F = Fn;
                         l *= corr;
-                        if (i > 0) {                           // (every earlier product of this half is complete: s was committed behind it)
+                        if (i > i0) {
+                            if (!mbar_wait_warp(smem_u32(&p_free[x]), ph_f, abort_flag)) { ok = false; break; }
+                            ph_f ^= 1;
+                            free = true;
+                            tc_fence_after();
                             uint32_t r[32];
 #pragma unroll 1
                             for (int b = 0; b < D / 32; ++b) {
@@ -598,21 +644,53 @@ __global__ void __launch_bounds__(kBThreads, 1) q4_block_kernel(const __grid_con
                         f2_unpack(f2_add(sum[0], sum[1]), s0, s1);
                         l = fmaf(s0 + s1, pow2(-(int)ev[k]), l);
                     }
-                    tmem_st32(t_s, pk);
+                    if (!free) {
+                        if (!mbar_wait_warp(smem_u32(&p_free[x]), ph_f, abort_flag)) { ok = false; break; }
+                        ph_f ^= 1;
+                        tc_fence_after();
+                    }
+                    tmem_st32(t_p, pk);
                     tmem_st_wait();
                     tc_fence_before();
                     mbar_arrive(smem_u32(&p_ready[x]));
-                    if (++ws == kWS) { ws = 0; ++wu; }
                 }
                 if (!ok) break;
-                if (!wait_warp(smem_u32(&o_done), ph_o, abort_flag, limit)) { ok = false; break; }
+                if (!mbar_wait_warp(smem_u32(&o_done[x]), ph_o, abort_flag)) { ok = false; break; }
+                ph_o ^= 1;
                 tc_fence_after();
-                // ---- the block's result, or its state where the block goes on in another CTA ----
+            }
+            // ---- the halves' states become one where they had the same rows: the first half writes it ----
+            float f0 = 1.f, f1 = 0.f;
+            if (!two) {
+                if (x == 1) {
+                    ml_other[r_half] = make_float2(F, l);
+                    tc_fence_before();
+                    mbar_arrive(smem_u32(&state_ready));
+                    if (!mbar_wait_warp(smem_u32(&state_read), ph_st, abort_flag)) { ok = false; break; }
+                } else {
+                    if (!mbar_wait_warp(smem_u32(&state_ready), ph_st, abort_flag)) { ok = false; break; }
+                    tc_fence_after();
+                    if (n_units > 1) {
+                        const float2 other = ml_other[r_half];
+                        const float M = fmaxf(F, other.x);
+                        f0 = ex2(F - M);
+                        f1 = ex2(other.x - M);
+                        F = M;
+                        l = f0 * l + f1 * other.y;
+                    }
+                }
+                ph_st ^= 1;
+            }
+            // ---- the block's result, or its state where the block goes on in another CTA ----
+            if (two || x == 0) {
                 const bool complete = c.unit == 0 && n_units == c.units;
-                const int slot = u == n_units ? 0 : 1;
+                const int slot = u == 0 ? 0 : 1, r_block = (two ? x * kBHalf : 0) + r_half;
                 const float inv = complete && !a.state ? (l != 0.f ? 1.f / l : 0.f) : 1.f;
+                const bool merge = !two && n_units > 1;
+                f0 *= inv;
+                f1 *= inv;
                 float *dst = nullptr;
-                if (!complete) dst = states + (2LL * blockIdx.x + slot) * q4_state_floats(kBRows, D) + (long long)(x * kBHalf + r_half) * D;
+                if (!complete) dst = states + (2LL * blockIdx.x + slot) * q4_state_floats(kBRows, D) + (long long)r_block * D;
                 else if (a.state && row_ok) dst = a.state + ((long long)(c.q.first + j) * geo.n_q_heads + h) * (D + 2);
                 unsigned short *out = reinterpret_cast<unsigned short *>(a.out) + (long long)(c.q.first + j) * a.out_row + (long long)h * a.out_head;
 #pragma unroll 1
@@ -621,7 +699,14 @@ __global__ void __launch_bounds__(kBThreads, 1) q4_block_kernel(const __grid_con
                     tmem_ld32(t_o + 32 * b, r);
                     tmem_ld_wait();
 #pragma unroll
-                    for (int k = 0; k < 32; ++k) r[k] = __float_as_uint(__uint_as_float(r[k]) * inv);
+                    for (int k = 0; k < 32; ++k) r[k] = __float_as_uint(__uint_as_float(r[k]) * f0);
+                    if (merge) {
+                        uint32_t r1[32];
+                        tmem_ld32(t_o + D + 32 * b, r1);       // the second half's o, the same lanes
+                        tmem_ld_wait();
+#pragma unroll
+                        for (int k = 0; k < 32; ++k) r[k] = __float_as_uint(fmaf(__uint_as_float(r1[k]), f1, __uint_as_float(r[k])));
+                    }
                     if (dst) {
 #pragma unroll
                         for (int k = 0; k < 16; ++k) *reinterpret_cast<uint2 *>(dst + 32 * b + 2 * k) = make_uint2(r[2 * k], r[2 * k + 1]);
@@ -640,19 +725,15 @@ __global__ void __launch_bounds__(kBThreads, 1) q4_block_kernel(const __grid_con
                 }
                 if (!complete) {
                     float *ml = states + (2LL * blockIdx.x + slot) * q4_state_floats(kBRows, D) + (long long)kBRows * D;
-                    ml[x * kBHalf + r_half] = F;
-                    ml[kBRows + x * kBHalf + r_half] = l;
+                    ml[r_block] = F;
+                    ml[kBRows + r_block] = l;
                 } else if (dst) {
                     *reinterpret_cast<float2 *>(dst + D) = make_float2(F, l);
                 }
-                tc_fence_before();                             // (o is read before the next block's products, which wait for Q, overwrite it)
-            } else {
-                u += n_units;
-                const int steps = ws + n_units;
-                wu += steps / kWS;
-                ws = steps % kWS;
+                tc_fence_before();                             // (o has been read when the next block's Q, which its products wait for, is handed over)
+                if (!two) mbar_arrive(smem_u32(&state_read));
             }
-            ph_o ^= 1;
+            u += n_units;
             if (tid == 0 && gridDim.x > 1 && u == left) {
                 Q4Part p{-1, 0, 0, 0, 0};
                 if (c.unit == 0 && n_units < c.units) {

@@ -49,13 +49,27 @@ __device__ __forceinline__ uint32_t sub_h2(uint32_t x, uint32_t y) {
     asm("sub.rn.f16x2 %0, %1, %2;" : "=r"(r) : "r"(x), "r"(y));
     return r;
 }
-// Bounded wait that also ends when another warp has given up.
+// Bounded wait that also ends when another warp has given up.  The thread sleeps until the phase completes (or for some
+// microseconds at a time): a warp that polls instead takes issue slots from the ones that work.
+__device__ __forceinline__ bool mbar_sleep(uint32_t bar, uint32_t parity) {
+    uint32_t ok;
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, %3;\n\t"
+        "selp.u32 %0, 1, 0, p;\n\t}"
+        : "=r"(ok) : "r"(bar), "r"(parity), "r"(20000u) : "memory");
+    return ok != 0;
+}
 __device__ __forceinline__ bool mbar_wait_or(uint32_t bar, uint32_t parity, volatile int *abort_flag) {
-    if (mbar_try_wait(bar, parity)) return true;
+    if (mbar_sleep(bar, parity)) return true;
     const long long t0 = clock64();
-    while (!mbar_try_wait(bar, parity))
+    while (!mbar_sleep(bar, parity))
         if (clock64() - t0 > kWaitClocks || *abort_flag) return false;
     return true;
+}
+// the same for a whole warp: the outcome is the same for all lanes
+__device__ __forceinline__ bool mbar_wait_warp(uint32_t bar, uint32_t parity, volatile int *abort_flag) {
+    return __all_sync(0xffffffffu, mbar_wait_or(bar, parity, abort_flag));
 }
 
 }  // namespace
