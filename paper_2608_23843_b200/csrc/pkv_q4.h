@@ -63,13 +63,14 @@ struct Q4AttentionArgs {
     long long q_row, q_head, out_row, out_head;
     int max_q_len;                     // no sequence has more rows than this
     int max_len;                       // hint: lengths are expected up to this
+    int whole;                         // set by the launcher: no segment is cut
     unsigned char *workspace;
     int *status;
 };
 
 cudaError_t launch_q4_append(const Q4CopyArgs &a, cudaStream_t st);
 cudaError_t launch_q4_read(const Q4CopyArgs &a, cudaStream_t st);
-cudaError_t launch_q4_attention(const Q4AttentionArgs &a, cudaStream_t st);
+cudaError_t launch_q4_attention(Q4AttentionArgs a, cudaStream_t st);
 cudaError_t q4_attention_setup();      // raises dynamic shared-memory limits, once per cache
 // the row-block kernel (pkv_q4_block.cu); n: CTAs, from q4_block_grid
 constexpr int kQ4BlockRows = 256;

@@ -150,17 +150,19 @@ __global__ void __launch_bounds__(Q4Shape<D, NG, NT>::kThreads, 2) q4_decode_ker
     asm volatile("griddepcontrol.wait;" ::: "memory");
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
 
-    // ---- this CTA's share of the batch's units ----
+    // ---- this CTA's share of the batch's units (a.whole: of its segments) ----
     const int H = geo.n_kv_heads, n_seqs = a.rows.n_seqs;
     int *status = blockIdx.x == 0 ? a.status : nullptr;
-    long long total = 0;
     auto weight = [&](int s, int *st) -> long long {           // units of a sequence, over its row tiles and heads
         if (s >= n_seqs) return 0;
         int first, all;
         const int n = q4_new_rows(a, s, first, all, st), T = q4_length(a.rows, geo, s, st);
-        return (long long)((n * geo.group + R - 1) / R) * H * max(1, (T + kQ4Unit - 1) / kQ4Unit);
+        return (long long)((n * geo.group + R - 1) / R) * H * (a.whole ? 1 : max(1, (T + kQ4Unit - 1) / kQ4Unit));
     };
-    {
+    long long total = 0;
+    if (n_seqs == 1) {
+        total = weight(0, tid == 0 ? status : nullptr);
+    } else {
         long long mine = 0;
         for (int s = tid; s < n_seqs; s += kQ4Threads) mine += weight(s, status);
 #pragma unroll
@@ -171,16 +173,21 @@ __global__ void __launch_bounds__(Q4Shape<D, NG, NT>::kThreads, 2) q4_decode_ker
         for (int w = 0; w < kQ4Warps; ++w) total += sums[w];
     }
     // (no more CTAs than there are units for a warp of each; the launch could only estimate that)
-    const int n_ctas = (int)min((long long)gridDim.x, max(1LL, total / kCons));
+    const int n_ctas = (int)min((long long)gridDim.x, max(1LL, a.whole ? total : total / kCons));
     const long long begin = total * blockIdx.x / n_ctas, end = total * (blockIdx.x + 1) / n_ctas;
     Q4Part *parts = reinterpret_cast<Q4Part *>(a.workspace);
     float *states = reinterpret_cast<float *>(a.workspace + q4_parts_bytes(gridDim.x));
+    const bool joined = !a.whole && gridDim.x > 1;             // segments may span CTAs
     if (blockIdx.x >= n_ctas || begin >= end) {
-        if (tid == 0 && gridDim.x > 1) parts[blockIdx.x].seq = -1;
+        if (tid == 0 && joined) parts[blockIdx.x].seq = -1;
         return;
     }
-    // the sequence that holds unit `begin`
-    {
+    Q4Cursor seg;                                              // of the CTA: the segment being worked on, and its first unit here
+    long long at0 = begin;                                     // `begin` within its sequence
+    if (n_seqs == 1) {
+        seg.seq = 0;
+        __syncthreads();                                       // (the barriers are initialised)
+    } else {                                                   // the sequence that holds `begin`
         long long base = 0;
         for (int s0 = 0; s0 < n_seqs; s0 += kQ4Threads) {
             const long long v = weight(s0 + tid, nullptr);
@@ -205,18 +212,27 @@ __global__ void __launch_bounds__(Q4Shape<D, NG, NT>::kThreads, 2) q4_decode_ker
             if (base > begin) break;
         }
         __syncthreads();
+        seg.seq = found_seq;
+        at0 = found_at;
     }
-    Q4Cursor seg;                                              // of the CTA: the segment being worked on, and its first unit here
-    seg.seq = found_seq;
     q4_load_seq(a, R, seg);
-    {
-        const long long at = found_at;
-        seg.unit = (int)(at % seg.units);
-        seg.head = (int)(at / seg.units % H);
-        seg.tile = (int)(at / seg.units / H);
+    int left_cta = (int)(end - begin);                         // units of the CTA
+    if (a.whole) {
+        seg.unit = 0;
+        seg.head = (int)(at0 % H);
+        seg.tile = (int)(at0 / H);
+        Q4Cursor w = seg;
+        const int segs = left_cta;
+        left_cta = w.units;
+        for (int k = 1; k < segs; ++k) {
+            q4_advance(a, R, w, w.units);
+            left_cta += w.units;
+        }
+    } else {
+        seg.unit = (int)(at0 % seg.units);
+        seg.head = (int)(at0 / seg.units % H);
+        seg.tile = (int)(at0 / seg.units / H);
     }
-
-    const int left_cta = (int)(end - begin);                   // units of the CTA
     volatile int *abort_flag = &gave_up;
 
     if (warp == kCons) {
@@ -678,7 +694,7 @@ __global__ void __launch_bounds__(Q4Shape<D, NG, NT>::kThreads, 2) q4_decode_ker
             if (nt == NT - 1) asm volatile("fence.proxy.async.shared::cta;" ::: "memory");      // the stages go back to the copies
             consumers_sync();
         }
-        if (tid == 0 && gridDim.x > 1 && seg_hi == left_cta) {
+        if (tid == 0 && joined && seg_hi == left_cta) {
             // the CTA's last segment: does it begin here and go on elsewhere?
             Q4Part p{-1, 0, 0, 0, 0};
             if (starts && !ends) {
@@ -697,66 +713,74 @@ __global__ void __launch_bounds__(Q4Shape<D, NG, NT>::kThreads, 2) q4_decode_ker
 }
 
 // Joins the states of the segments (tiles of R rows) that span CTAs, in token order: blocks (b, y) take the rows of the
-// segment that begins in CTA b.  A chain of loads over the parts would cost a trip to L2 each (37 parts of a 128K sequence: 41 us); the parts are
-// shared by four warps and their loads do not wait for one another.
+// segment that begins in CTA b.  A chain of loads over the parts would cost a trip to L2 each (37 parts of a 128K sequence:
+// 41 us), so the parts of a row are shared by four warps; a row block's rows, many of few parts, get a warp each.
 constexpr int kQ4JoinWarps = 4;
-template <int D, bool H16>
+template <int D, bool H16, int W>
 __global__ void __launch_bounds__(32 * kQ4JoinWarps) q4_join_kernel(const __grid_constant__ Q4AttentionArgs a, int R) {
     asm volatile("griddepcontrol.wait;" ::: "memory");
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     const Q4Geometry &geo = a.geo;
     const int b = blockIdx.x;
     const Q4Part p = reinterpret_cast<const Q4Part *>(a.workspace)[b];
     if (p.seq < 0) return;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int r = W == 1 ? (int)blockIdx.y * kQ4JoinWarps + warp : (int)blockIdx.y;      // W warps per row
     int first, all;
     const int n = q4_new_rows(a, p.seq, first, all, nullptr), G = geo.group;
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const long long row = (long long)p.tile * R + r;
+    const int j = (int)(row / G);
+    if (j >= n) return;
     const float *states = reinterpret_cast<const float *>(a.workspace + q4_parts_bytes(gridDim.x));
     const long long per = q4_state_floats(R, D);
     // the first part is in slot p.slot of CTA b, the others in slot 0 of the CTAs behind it
     auto state = [&](int k) { return states + (2LL * k + (k == b ? p.slot : 0)) * per; };
-    __shared__ float part[kQ4JoinWarps][D + 1];
+    float M = kNegInf;
+    for (int k = b + lane; k <= p.last_cta; k += 32) M = fmaxf(M, state(k)[R * D + r]);
+#pragma unroll
+    for (int d = 16; d; d >>= 1) M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, d));
     constexpr int C = D / 32;
-    for (int r = blockIdx.y; r < R; r += gridDim.y) {
-        const long long row = (long long)p.tile * R + r;
-        const int j = (int)(row / G);
-        if (j >= n) return;
-        float M = kNegInf;
-        for (int k = b + lane; k <= p.last_cta; k += 32) M = fmaxf(M, state(k)[R * D + r]);
+    float L = 0.f, acc[C];
 #pragma unroll
-        for (int d = 16; d; d >>= 1) M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, d));
-        float L = 0.f, acc[C];
-#pragma unroll
-        for (int i = 0; i < C; ++i) acc[i] = 0.f;
+    for (int i = 0; i < C; ++i) acc[i] = 0.f;
 #pragma unroll 4
-        for (int k = b + warp; k <= p.last_cta; k += kQ4JoinWarps) {
-            const float *s = state(k);
-            const float f = ex2(s[R * D + r] - M);
-            L += f * s[R * D + R + r];
-            const float2 *x = reinterpret_cast<const float2 *>(s + r * D + C * lane);
+    for (int k = b + (W == 1 ? 0 : warp); k <= p.last_cta; k += W) {
+        const float *s = state(k);
+        const float f = ex2(s[R * D + r] - M);
+        L += f * s[R * D + R + r];
+        const float2 *x = reinterpret_cast<const float2 *>(s + r * D + C * lane);
 #pragma unroll
-            for (int i = 0; i < C / 2; ++i) { const float2 v = x[i]; acc[2 * i] += f * v.x; acc[2 * i + 1] += f * v.y; }
-        }
-        if (r != (int)blockIdx.y) __syncthreads();             // (the row before has been read)
+        for (int i = 0; i < C / 2; ++i) { const float2 v = x[i]; acc[2 * i] += f * v.x; acc[2 * i + 1] += f * v.y; }
+    }
+    if (W > 1) {
+        __shared__ float part[kQ4JoinWarps][D + 1];
 #pragma unroll
         for (int i = 0; i < C; ++i) part[warp][C * lane + i] = acc[i];
         if (lane == 0) part[warp][D] = L;
         __syncthreads();
-        const int ch = threadIdx.x * 2;
-        if (ch >= D) continue;
-        float x = 0.f, y = 0.f;
+        if (warp > 0) return;
         L = 0.f;
 #pragma unroll
-        for (int w = 0; w < kQ4JoinWarps; ++w) { x += part[w][ch]; y += part[w][ch + 1]; L += part[w][D]; }
-        const int h = p.head * G + (int)(row - (long long)j * G);
-        if (a.state) {
-            float *dst = a.state + ((long long)(first + j) * geo.n_q_heads + h) * (D + 2);
-            *reinterpret_cast<float2 *>(dst + ch) = make_float2(x, y);
-            if (ch == 0) *reinterpret_cast<float2 *>(dst + D) = make_float2(M, L);
-        } else {
-            const float inv = L != 0.f ? 1.f / L : 0.f;
-            *reinterpret_cast<uint32_t *>(reinterpret_cast<unsigned short *>(a.out) + (long long)(first + j) * a.out_row +
-                                          (long long)h * a.out_head + ch) = H16 ? pack_f16(x * inv, y * inv) : pack_bf16(x * inv, y * inv);
+        for (int i = 0; i < C; ++i) acc[i] = 0.f;
+#pragma unroll
+        for (int w = 0; w < W; ++w) {
+#pragma unroll
+            for (int i = 0; i < C; ++i) acc[i] += part[w][C * lane + i];
+            L += part[w][D];
         }
+    }
+    const int h = p.head * G + (int)(row - (long long)j * G);
+    if (a.state) {
+        float *dst = a.state + ((long long)(first + j) * geo.n_q_heads + h) * (D + 2);
+#pragma unroll
+        for (int i = 0; i < C; i += 2) *reinterpret_cast<float2 *>(dst + C * lane + i) = make_float2(acc[i], acc[i + 1]);
+        if (lane == 0) *reinterpret_cast<float2 *>(dst + D) = make_float2(M, L);
+    } else {
+        const float inv = L != 0.f ? 1.f / L : 0.f;
+        uint32_t *dst = reinterpret_cast<uint32_t *>(reinterpret_cast<unsigned short *>(a.out) + (long long)(first + j) * a.out_row +
+                                                     (long long)h * a.out_head + C * lane);
+#pragma unroll
+        for (int i = 0; i < C; i += 2) dst[i / 2] = H16 ? pack_f16(acc[i] * inv, acc[i + 1] * inv) : pack_bf16(acc[i] * inv, acc[i + 1] * inv);
     }
 }
 
@@ -765,11 +789,15 @@ bool q4_by_blocks(const Q4Geometry &g, int max_q_len) { return (long long)max_q_
 
 int q4_rows_per_tile(const Q4Geometry &g, int max_q_len) { return (long long)max_q_len * g.group <= 8 ? 8 : 16; }
 
+// Sequences of up to 24 units (1536 tokens), as far as the host can tell: a segment stays in one CTA (at most four rounds of
+// its warps, 1.7 us each), which saves the second kernel (4 us).
+bool q4_whole(int max_len) { return (max_len + kQ4Unit - 1) / kQ4Unit <= 24; }
+
 // CTAs of a launch: enough units for every warp of each, as far as the host can tell.
 int q4_grid(const Q4Geometry &g, int n_seqs, int max_q_len, int max_len) {
     const int R = q4_rows_per_tile(g, max_q_len);
     const long long tiles = ((long long)max_q_len * g.group + R - 1) / R, units = (max_len + kQ4Unit - 1) / kQ4Unit;
-    const double all = (double)n_seqs * g.n_kv_heads * tiles * units / (q4_warps(R / 8) - 1);
+    const double segs = (double)n_seqs * g.n_kv_heads * tiles, all = q4_whole(max_len) ? segs : segs * units / (q4_warps(R / 8) - 1);
     return all >= g.n_ctas ? g.n_ctas : all < 1 ? 1 : (int)all;
 }
 
@@ -790,14 +818,15 @@ cudaError_t q4_attention_setup() {
 long long q4_attention_workspace(const Q4Geometry &g, int n_seqs, int max_q_len, int max_len) {
     if (q4_by_blocks(g, max_q_len)) return q4_block_workspace(g, n_seqs, max_q_len, max_len);
     const int n = q4_grid(g, n_seqs, max_q_len, max_len);
-    return n <= 1 ? 0 : q4_parts_bytes(n) + 2LL * n * q4_state_floats(q4_rows_per_tile(g, max_q_len), g.head_dim) * 4;
+    return n <= 1 || q4_whole(max_len) ? 0 : q4_parts_bytes(n) + 2LL * n * q4_state_floats(q4_rows_per_tile(g, max_q_len), g.head_dim) * 4;
 }
 
-cudaError_t launch_q4_attention(const Q4AttentionArgs &a, cudaStream_t st) {
+cudaError_t launch_q4_attention(Q4AttentionArgs a, cudaStream_t st) {
     const Q4Geometry &g = a.geo;
     const bool blocks = q4_by_blocks(g, a.max_q_len);
     const int n = blocks ? q4_block_grid(g, a.rows.n_seqs, a.max_q_len, a.max_len) : q4_grid(g, a.rows.n_seqs, a.max_q_len, a.max_len);
     const int R = blocks ? kQ4BlockRows : q4_rows_per_tile(g, a.max_q_len);
+    a.whole = !blocks && q4_whole(a.max_len);
     cudaLaunchAttribute at[1];
     at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     at[0].val.programmaticStreamSerializationAllowed = 1;
@@ -823,15 +852,15 @@ cudaError_t launch_q4_attention(const Q4AttentionArgs &a, cudaStream_t st) {
     } else {
         PKV_Q4_SHAPES(PKV_Q4_LAUNCH)
     }
-    if (e != cudaSuccess || n <= 1) return e;
-    cfg.gridDim = dim3(n, R < 32 ? R : 32);
+    if (e != cudaSuccess || n <= 1 || a.whole) return e;
+    cfg.gridDim = dim3(n, blocks ? R / kQ4JoinWarps : R);
     cfg.blockDim = dim3(32 * kQ4JoinWarps);
     cfg.dynamicSmemBytes = 0;
-    if (g.head_dim == 128)
-        e = g.fp16 ? cudaLaunchKernelEx(&cfg, q4_join_kernel<128, true>, a, R) : cudaLaunchKernelEx(&cfg, q4_join_kernel<128, false>, a, R);
-    else
-        e = g.fp16 ? cudaLaunchKernelEx(&cfg, q4_join_kernel<64, true>, a, R) : cudaLaunchKernelEx(&cfg, q4_join_kernel<64, false>, a, R);
-    return e;
+#define PKV_Q4_JOIN(D, H)                                                                                         \
+    if (g.head_dim == D && (g.fp16 != 0) == H)                                                                    \
+        return blocks ? cudaLaunchKernelEx(&cfg, q4_join_kernel<D, H, 1>, a, R) : cudaLaunchKernelEx(&cfg, q4_join_kernel<D, H, kQ4JoinWarps>, a, R);
+    PKV_Q4_JOIN(128, false) PKV_Q4_JOIN(128, true) PKV_Q4_JOIN(64, false) PKV_Q4_JOIN(64, true)
+    return cudaErrorInvalidValue;
 }
 
 }  // namespace pkv

@@ -550,6 +550,7 @@ class Cache:
             pass
 
 
+_INT32 = torch.int32
 _Q4_DTYPES = {torch.bfloat16: PKV_DTYPE_BF16, torch.float16: PKV_DTYPE_FP16}
 
 
@@ -576,9 +577,10 @@ class Q4Cache:
         self.sizes = pkv_q4_query_sizes(cfg)
         self.dry_run = dry_run
         self.dtype = torch.float16 if cfg.dtype == PKV_DTYPE_FP16 else torch.bfloat16
+        self._d, self._hq, self._hk = cfg.head_dim, cfg.n_q_heads, cfg.n_kv_heads
         self._workspaces = {}
         if dry_run:
-            self.device, self._device_index, self.pool, self.meta = torch.device("cpu"), None, None, None
+            self.device, self._device_index, self.pool, self.meta = torch.device("cpu"), -1, None, None
             self.handle = pkv_q4_init_cache(cfg, None, None)
         else:
             self._device_index = Cache.dense_pool_device_index(torch.device(device))
@@ -596,72 +598,81 @@ class Q4Cache:
             return None
         if _raw_current_stream is not None:
             return _raw_current_stream(self._device_index)
-        return torch.cuda.current_stream(self.device)
+        return torch.cuda.current_stream(self.device).cuda_stream
 
     def _call(self, fn, *args):
-        """fn with the cache's device current."""
-        if self.dry_run or torch.cuda.current_device() == self._device_index:
-            return fn(self.handle, *args, self._stream())
-        with torch.cuda.device(self._device_index):
-            return fn(self.handle, *args, self._stream())
+        """A C call with the cache's device current (the library refuses another one)."""
+        st = fn(self.handle, *args)
+        if st != PKV_OK:
+            if not self.dry_run and torch.cuda.current_device() != self._device_index:
+                with torch.cuda.device(self._device_index):
+                    st = fn(self.handle, *args)
+            _q4_check(self.handle, st)
 
+    # A decode step makes a few of these calls per layer and each is some microseconds of host time: the checks below are
+    # written for the calls that pass them.
     def _seqs(self, page_table, lengths, offsets):
-        for name, t in (("page_table", page_table), ("lengths", lengths), ("offsets", offsets)):
-            if t is not None and (t.dtype != torch.int32 or t.device != self.device or not t.is_contiguous()):
-                self._fail("%s must be a contiguous int32 tensor on %s" % (name, self.device))
-        if page_table.dim() != 2 or lengths.shape != page_table.shape[:1]:
-            self._fail("page_table must be [n_seqs, max_pages] and lengths [n_seqs]")
-        if offsets is not None and offsets.shape != (page_table.shape[0] + 1,):
-            self._fail("offsets must be [n_seqs + 1]")
-        return page_table.shape
+        dev, shape = self._device_index, page_table.shape
+        if not (len(shape) == 2 and page_table.dtype is _INT32 and page_table.get_device() == dev and page_table.is_contiguous()):
+            self._fail("page_table must be a contiguous int32 tensor [n_seqs, max_pages] on %s" % self.device)
+        if not (lengths.dim() == 1 and lengths.numel() == shape[0] and lengths.dtype is _INT32 and lengths.get_device() == dev and lengths.is_contiguous()):
+            self._fail("lengths must be a contiguous int32 tensor [n_seqs] on %s" % self.device)
+        if offsets is not None and not (offsets.dim() == 1 and offsets.numel() == shape[0] + 1 and offsets.dtype is _INT32 and
+                                        offsets.get_device() == dev and offsets.is_contiguous()):
+            self._fail("offsets must be a contiguous int32 tensor [n_seqs + 1] on %s" % self.device)
+        return shape
 
     def _rows(self, name, t, heads, n_seqs, ragged):
-        """-> (rows, (row stride, head stride)) of a row buffer."""
-        shape, d = t.shape, self.cfg.head_dim
-        if t.dtype != self.dtype or t.device != self.device:
+        """-> rows, row stride, head stride of a row buffer."""
+        shape, d = t.shape, self._d
+        if t.dtype is not self.dtype or t.get_device() != self._device_index:
             self._fail("%s must be %s on %s" % (name, self.dtype, self.device))
         if ragged:
             if len(shape) != 3 or shape[1] != heads or shape[2] != d:
                 self._fail("%s must be [rows, %d, %d] with offsets" % (name, heads, d))
-            n, st = shape[0], t.stride()
-            row = st[0]
+            row, head, ch = t.stride()
+            n = shape[0]
         else:
             if len(shape) != 4 or shape[0] != n_seqs or shape[2] != heads or shape[3] != d:
                 self._fail("%s must be [%d, n, %d, %d] without offsets" % (name, n_seqs, heads, d))
-            n, st = shape[0] * shape[1], t.stride()
-            row = st[1] if shape[1] > 1 else st[0]
-            if shape[0] > 1 and shape[1] > 1 and st[0] != shape[1] * row:
+            seq, row, head, ch = t.stride()
+            n = n_seqs * shape[1]
+            if shape[1] <= 1:
+                row = seq
+            elif n_seqs > 1 and seq != shape[1] * row:
                 self._fail("%s: the rows of all sequences must be equally far apart (pass [rows, heads, d] and offsets)" % name)
-        if st[-1] != 1:
+        if ch != 1:
             self._fail("%s: the channels of a head must be adjacent" % name)
+        if heads == 1:
+            head = d                                     # a size-1 axis may carry any stride
         if n <= 1:
-            row = heads * d                              # a size-1 axis may carry any stride
-        return n, (row, st[-2] if heads > 1 else d)
+            row = heads * d
+        return n, row, head
 
     def append_kv(self, page_table, lengths, k, v, offsets=None):
         """Quantises the new rows k, v into the cache."""
-        n_seqs, max_pages = self._seqs(page_table, lengths, offsets)
-        n, ks = self._rows("k", k, self.cfg.n_kv_heads, n_seqs, offsets is not None)
-        nv, vs = self._rows("v", v, self.cfg.n_kv_heads, n_seqs, offsets is not None)
-        if n != nv:
-            self._fail("k and v must have the same number of rows")
-        self._call(pkv_q4_append_kv, n_seqs, page_table, max_pages, lengths, n, offsets, k, ks, v, vs)
+        self._copy(lib().pkv_q4_append_kv, page_table, lengths, k, v, offsets)
 
     def read_kv(self, page_table, lengths, k, v, offsets=None):
         """Reads the last positions of each sequence back into k, v."""
-        n_seqs, max_pages = self._seqs(page_table, lengths, offsets)
-        n, ks = self._rows("k", k, self.cfg.n_kv_heads, n_seqs, offsets is not None)
-        nv, vs = self._rows("v", v, self.cfg.n_kv_heads, n_seqs, offsets is not None)
-        if n != nv:
-            self._fail("k and v must have the same number of rows")
-        self._call(pkv_q4_read_kv, n_seqs, page_table, max_pages, lengths, n, offsets, k, ks, v, vs)
+        self._copy(lib().pkv_q4_read_kv, page_table, lengths, k, v, offsets)
         return k, v
 
+    def _copy(self, fn, page_table, lengths, k, v, offsets):
+        n_seqs, max_pages = self._seqs(page_table, lengths, offsets)
+        ragged = offsets is not None
+        n, k_row, k_head = self._rows("k", k, self._hk, n_seqs, ragged)
+        nv, v_row, v_head = self._rows("v", v, self._hk, n_seqs, ragged)
+        if n != nv:
+            self._fail("k and v must have the same number of rows")
+        self._call(fn, n_seqs, page_table.data_ptr(), max_pages, lengths.data_ptr(), n, offsets.data_ptr() if ragged else None,
+                   k.data_ptr(), k_row, k_head, v.data_ptr(), v_row, v_head, self._stream())
+
     def attention(self, page_table, lengths, q, out=None, offsets=None, max_q_len=None, max_len=0):
-        """Attention of the newest positions over the cache; out (default: a new tensor like q) is returned.  With offsets,
-        max_q_len bounds the rows of a sequence (default: all rows)."""
+        """Attention of the newest positions over the cache; out (default: a new tensor of q's shape) is returned.  With
+        offsets, max_q_len bounds the rows of a sequence (default: all rows)."""
         if out is None:
-            out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+            out = torch.empty_like(q, memory_format=torch.contiguous_format)
         elif out.shape != q.shape:
             self._fail("out must have the shape of q")
         self._attention(page_table, lengths, q, out, None, offsets, max_q_len, max_len)
@@ -679,30 +690,39 @@ class Q4Cache:
 
     def _attention(self, page_table, lengths, q, out, state, offsets, max_q_len, max_len):
         n_seqs, max_pages = self._seqs(page_table, lengths, offsets)
-        n, qs = self._rows("q", q, self.cfg.n_q_heads, n_seqs, offsets is not None)
-        os_ = qs if out is None else self._rows("out", out, self.cfg.n_q_heads, n_seqs, offsets is not None)[1]
+        ragged = offsets is not None
+        n, q_row, q_head = self._rows("q", q, self._hq, n_seqs, ragged)
+        o_row, o_head = q_row, q_head
+        if out is not None:
+            _, o_row, o_head = self._rows("out", out, self._hq, n_seqs, ragged)
         if n == 0:
             return
-        if offsets is None:
+        if not ragged:
             max_q_len = q.shape[1]
         elif max_q_len is None:
             max_q_len = n
         if max_q_len == 0:
             return
-        max_len = min(max_len, max_pages * self.cfg.page_size) if max_len > 0 else max_pages * self.cfg.page_size
-        key = (n_seqs, max_q_len, max_len)
-        size = self._workspaces.get(key)
+        most = max_pages * self.cfg.page_size
+        if not 0 < max_len < most:
+            max_len = most
+        size = self._workspaces.get((n_seqs, max_q_len, max_len))
         if size is None:
             if len(self._workspaces) >= 256:
                 self._workspaces.clear()
-            size = self._workspaces[key] = pkv_q4_attention_workspace(self.handle, *key)
+            size = self._workspaces[n_seqs, max_q_len, max_len] = pkv_q4_attention_workspace(self.handle, n_seqs, max_q_len, max_len)
         # (from the caching allocator at each call: ordered with this stream, and private to a graph that is being captured)
         work = torch.empty(size, dtype=torch.uint8, device=self.device) if size and not self.dry_run else None
-        self._call(pkv_q4_attention, n_seqs, page_table, max_pages, lengths, n, offsets, max_q_len, max_len, q, qs, out, os_, state,
-                   work, size)
+        self._call(lib().pkv_q4_attention, n_seqs, page_table.data_ptr(), max_pages, lengths.data_ptr(), n,
+                   offsets.data_ptr() if ragged else None, max_q_len, max_len, q.data_ptr(), q_row, q_head,
+                   None if out is None else out.data_ptr(), o_row, o_head, None if state is None else state.data_ptr(),
+                   None if work is None else work.data_ptr(), size, self._stream())
 
     def stats(self):
-        return self._call(pkv_q4_get_stats)
+        if not self.dry_run:
+            with torch.cuda.device(self._device_index):
+                return pkv_q4_get_stats(self.handle, self._stream())
+        return pkv_q4_get_stats(self.handle)
 
     def close(self):
         if self.handle is not None:
