@@ -5,19 +5,21 @@
 // product; one thread owns one row).  A block of at most 128 rows gives both halves the same rows and every other unit, and
 // their states are joined at its end.  Tokens come in units of 64:
 //     one warp       looks up pages and copies a unit's tiles of codes and scales into a ring,
-//     five warps     widen: a tile at a time in turn, codes times scales as fp16 into shared memory, in the layouts the
-//                    products read (128-byte swizzle, panels of 64 channels).  A code (3 bits and a sign) times a bf16 scale
-//                    (8 bits) has 11 bits, so fp16 holds it exactly; a power of two per tile (the exponent of its largest
-//                    scale, handed on to the rows) keeps it inside fp16's range whatever the values' size,
-//     two warps      issue the products, one lane per half: s = Q K^T, o += p V with s, o and p in tensor memory (p as the row
-//                    operand; Q too for the first half - tensor memory is full - and in shared memory for the second),
-//     eight warps    softmax: s from tensor memory, p as fp16 beside it, o rescaled only when the running reference has been
+//     four warps     widen, a tile each: codes times scales as fp16 into shared memory, in the layouts the products read
+//                    (128-byte swizzle, panels of 64 channels).  A code (3 bits and a sign) times a bf16 scale (8 bits) has
+//                    11 bits, so fp16 holds it exactly; a power of two per tile (the exponent of its largest scale, handed on
+//                    to the rows) keeps it inside fp16's range whatever the values' size,
+//     one warp       issues the products, one lane: s = Q K^T with Q and, later, p as row operands in tensor memory,
+//                    o += p V; while one half's rows are in their softmax the other half's products run,
+//     eight warps    softmax: s from tensor memory, p as fp16 back over it, o rescaled only when the running reference has been
 //                    passed by 2^8 (then p * value may still not leave fp16: 2^8 * 14).
-// s of the next unit is computed as soon as the rows have s of this one in registers, and o += p V runs behind their next
-// softmax, so the rows wait for neither.  What bounds it: per unit and 256 rows the products take 1150 cycles and the
-// exponentials 1024 (16 per cycle and SM), beside some 1000 instructions per scheduler; the widening is paid once for 256
-// rows.  CTAs share the batch's units evenly, one CTA per SM; blocks that span CTAs leave states that a second kernel joins.
-// Units after a block's last visible position are not visited.
+// What bounds it: products and exponentials each take 1024 cycles per unit of 256 rows, but a half's chain - s, softmax, o,
+// the hand-overs between them - is some 1800 cycles long even with both for free, and the widening competes with the softmax
+// for issue slots.  Measured on 2048 positions against 32K (32 / 8 heads, g = 32) and not kept: Q of one half in shared memory
+// so that s of the next unit can be computed behind the softmax (the products then wait for shared memory), five or six
+// widening warps, a quarter of the exponentials by polynomial, the halves' exponentials in turn.
+// CTAs share the batch's units evenly, one CTA per SM; blocks that span CTAs leave states that a second kernel joins.  Units
+// after a block's last visible position are not visited.
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 
@@ -29,21 +31,19 @@ namespace pkv {
 namespace {
 
 constexpr int kBRows = kQ4BlockRows, kBHalf = 128;
-// warps: 0-7 rows, 8-12 widening, 13 and 14 issue the products, 15 copies (sixteen warps of 128 registers fill the register file)
-constexpr int kBThreads = 512, kBRowWarps = 8, kBWidenWarps = 5, kBIssueWarp = 13, kBCopyWarp = 15;
+constexpr int kBThreads = 448, kBRowWarps = 8, kBWidenWarps = kQ4UnitTiles, kBIssueWarp = 12, kBCopyWarp = 13;
 constexpr uint32_t kBTmemCols = 512;
 
 template <int D, int NG>
 struct BlockShape {
     static constexpr int kPanels = D / 64, kSide = kPanels * kQ4Unit * 128, kWide = 2 * kSide;      // K panels, then V panels of a unit
     static constexpr int kTile = kQ4Tile * (D + 4 * NG), kUnitBytes = kQ4UnitTiles * kTile, kCodes = (kUnitBytes + 127) / 128 * 128;
-    static constexpr int kQPanel = kBHalf * 128, kQBytes = kPanels * kQPanel;                       // Q of the second half
-    static constexpr int kWideStages = 4, kFit = (220 * 1024 - kWideStages * kWide - kQBytes) / kCodes, kCodeStages = kFit < 8 ? kFit : 8;
-    static constexpr int kSmem = kWideStages * kWide + kQBytes + kCodeStages * kCodes + 1024;       // (+ alignment)
+    static constexpr int kWideStages = 4, kFit = (222 * 1024 - kWideStages * kWide) / kCodes, kCodeStages = kFit < 8 ? kFit : 8;
+    static constexpr int kSmem = kWideStages * kWide + kCodeStages * kCodes + 1024;                 // (+ alignment)
     static_assert(kCodeStages >= 4 && kSmem <= 224 * 1024, "fits one CTA per SM");
-    // columns of tensor memory: o of both halves, Q of the first (fp16 pairs), s of both, p of both (fp16 pairs)
-    static constexpr uint32_t kColO = 0, kColQ = 2 * D, kColS = kColQ + D / 2, kColP = kColS + 2 * kQ4Unit;
-    static_assert(kColP + kQ4Unit <= kBTmemCols, "fits tensor memory");
+    // columns of tensor memory: o of both halves, Q of both (fp16 pairs), s of both
+    static constexpr uint32_t kColO = 0, kColQ = 2 * D, kColS = kColQ + D;
+    static_assert(kColS + 2 * kQ4Unit <= kBTmemCols, "fits tensor memory");
 };
 
 // sum over i < n of floor((a i + b) / m), for a, b >= 0 and m > 0 (by the Euclid-like recursion on (a, m))
@@ -76,7 +76,7 @@ __device__ __forceinline__ BlockSeq block_seq(const Q4AttentionArgs &a, int s, i
     return q;
 }
 __device__ __forceinline__ int block_units(const BlockSeq &q, int r) {
-    const int last = min(q.n - 1, (int)(((long long)(r + 1) * kBRows - 1) / q.G));
+    const int last = min(q.n - 1, ((r + 1) * kBRows - 1) / q.G);
     const int see = q.all > q.T ? q.T : q.T - q.all + last + 1;          // (more rows than tokens: not worth a rule of its own)
     return max(1, (see + kQ4Unit - 1) / kQ4Unit);
 }
@@ -85,6 +85,11 @@ __device__ __forceinline__ int block_units(const BlockSeq &q, int r) {
 __device__ long long block_units_before(const BlockSeq &q, int r) {
     if (r == 0) return 0;
     if (q.all > q.T) return (long long)r * block_units(q, 0);
+    if (r <= 8) {                                   // (few: adding them up beats the recursion's divisions)
+        long long few = 0;
+        for (int i = 0; i < r; ++i) few += block_units(q, i);
+        return few;
+    }
     const int full = min(r, q.blocks - 1);
     const long long A = (long long)q.T - q.all + 1 + kQ4Unit - 1;
     long long sum = floor_sum(full, (long long)kQ4Unit * q.G, kBRows, kBRows - 1 + A * q.G);
@@ -159,9 +164,9 @@ __global__ void __launch_bounds__(kBThreads, 1) q4_block_kernel(const __grid_con
     constexpr int NW = D / 32, WPG = NW / NG, kWS = S::kWideStages, kCS = S::kCodeStages;
     const Q4Geometry &geo = a.geo;
     extern __shared__ unsigned char smem_raw[];
-    unsigned char *wide = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u), *q_mem = wide + kWS * S::kWide, *codes = q_mem + S::kQBytes;
+    unsigned char *wide = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u), *codes = wide + kWS * S::kWide;
     __shared__ unsigned long long code_full[kCS], code_empty[kCS], wide_full[kWS], wide_empty[kWS];
-    __shared__ unsigned long long s_full[2], s_read[2], p_ready[2], p_free[2], q_ready[2], o_done[2], drain[2], state_ready, state_read;
+    __shared__ unsigned long long s_full[2], p_ready[2], q_ready[2], o_done[2], drain, state_ready, state_read;
     __shared__ uint32_t code_tiles[kCS], code_tokens[kCS];
     __shared__ UnitInfo info[kWS];
     __shared__ float2 ml_other[kBHalf];
@@ -172,12 +177,12 @@ __global__ void __launch_bounds__(kBThreads, 1) q4_block_kernel(const __grid_con
     volatile int *abort_flag = &gave_up;
     if (tid == 0) {
         for (int s = 0; s < kCS; ++s) { mbar_init(smem_u32(&code_full[s]), 1); mbar_init(smem_u32(&code_empty[s]), kQ4UnitTiles); }
-        for (int s = 0; s < kWS; ++s) { mbar_init(smem_u32(&wide_full[s]), kQ4UnitTiles); mbar_init(smem_u32(&wide_empty[s]), 2); }
+        for (int s = 0; s < kWS; ++s) { mbar_init(smem_u32(&wide_full[s]), kQ4UnitTiles); mbar_init(smem_u32(&wide_empty[s]), 1); }
         for (int x = 0; x < 2; ++x) {
-            mbar_init(smem_u32(&s_full[x]), 1); mbar_init(smem_u32(&s_read[x]), kBHalf); mbar_init(smem_u32(&p_ready[x]), kBHalf);
-            mbar_init(smem_u32(&p_free[x]), 1); mbar_init(smem_u32(&q_ready[x]), kBHalf); mbar_init(smem_u32(&o_done[x]), 1);
-            mbar_init(smem_u32(&drain[x]), 1);
+            mbar_init(smem_u32(&s_full[x]), 1); mbar_init(smem_u32(&p_ready[x]), kBHalf);
+            mbar_init(smem_u32(&q_ready[x]), kBHalf); mbar_init(smem_u32(&o_done[x]), 1);
         }
+        mbar_init(smem_u32(&drain), 1);
         mbar_init(smem_u32(&state_ready), kBHalf);
         mbar_init(smem_u32(&state_read), kBHalf);
         gave_up = 0;
@@ -323,19 +328,15 @@ __global__ void __launch_bounds__(kBThreads, 1) q4_block_kernel(const __grid_con
         const int c = lane & 3, i8 = lane >> 2;
         const int t_lane = (i8 >> 1) ^ (i8 & 1 ? 5 : 0);       // tokens t and t ^ 5 side by side: different halves of a line of codes, different banks of a line of fp16
         bool ok = true;
-        int dw = warp - kBRowWarps;                            // tile of the unit
-        int cs = 0, cu = 0;                                    // stage of the codes and times it has been used before
+        const int dw = warp - kBRowWarps;                      // tile of the unit
         const uint32_t k_at = q4_k_chunk(D, t_lane, c), va_at = q4_v_base(D) + q4_v_chunk(D, t_lane, 2 * c), vb_at = q4_v_base(D) + q4_v_chunk(D, t_lane, 2 * c + 1);
         const uint32_t s_at = (lane < 16 ? q4_ks_base(D) : q4_vs_base(D, NG)) + (lane & 15) * 2 * NG;
         constexpr uint32_t kNext = q4_k_chunk(D, 8, 0);        // tokens t + 8: the same place eight rows on, for V too
         static_assert(q4_v_chunk(D, 8, 0) == (int)kNext && q4_v_chunk(D, 13, 5) == q4_v_chunk(D, 5, 5) + (int)kNext, "the pattern repeats");
-        for (int u = 0; u < left; dw += kBWidenWarps) {
-            while (dw >= kQ4UnitTiles && u < left) {
-                dw -= kQ4UnitTiles;
-                if (++cs == kCS) { cs = 0; ++cu; }
-                ++u;
-            }
-            if (u >= left) break;
+        // where this lane's 16-byte blocks of a row go: words 0, 2 and words 1, 3
+        const uint32_t d_row = smem_u32(wide) + (dw * kQ4Tile + t_lane) * 128, d_at[2] = {d_row + ((c ^ (t_lane & 7)) << 4), d_row + (((4 + c) ^ (t_lane & 7)) << 4)};
+        int cs = 0, cu = 0;                                    // stage of the codes and times it has been used before
+        for (int u = 0; u < left; ++u) {
             const int ws = u % kWS, wu = u / kWS;
             if (!mbar_wait_warp(smem_u32(&code_full[cs]), cu & 1, abort_flag)) { ok = false; break; }
             const uint32_t bits = code_tiles[cs], tokens = code_tokens[cs];
@@ -363,8 +364,10 @@ __global__ void __launch_bounds__(kBThreads, 1) q4_block_kernel(const __grid_con
             if (NG == 4) z = __vmaxu2(z, z2[(NG - 1) / 2]);
             z = max(z & 0xffffu, z >> 16);
             if ((lane & 15) >= valid) z = 0u;
+            bool plain = valid == kQ4Tile;                     // all tokens there, all groups finite
             if (__any_sync(0xffffffffu, z > 0x7f80u)) {        // a group that is not finite: look at the others of its token
                 const bool nan = z > 0x7f80u;
+                plain = false;
                 nans = __ballot_sync(0xffffffffu, nan) >> 16;
                 if (nan) {
                     z = 0u;
@@ -378,18 +381,6 @@ __global__ void __launch_bounds__(kBThreads, 1) q4_block_kernel(const __grid_con
             const int ek = min(max((int)(__reduce_max_sync(0xffffffffu, lane < 16 ? z : 0u) >> 7) - 127, -60), 60);
             const int ev = min(max((int)(__reduce_max_sync(0xffffffffu, lane < 16 ? 0u : z) >> 7) - 127, -60), 60);
             const float fk = pow2(-ek), fv = pow2(-ev);
-            uint32_t sk[2][NG], sv[2][NG];
-#pragma unroll
-            for (int half = 0; half < 2; ++half)
-#pragma unroll
-                for (int k = 0; k < NG; ++k) {
-                    float x = (k & 1 ? bf16hi_f(ksc[half][k / 2]) : bf16lo_f(ksc[half][k / 2])) * fk;
-                    float y = (k & 1 ? bf16hi_f(vsc[half][k / 2]) : bf16lo_f(vsc[half][k / 2])) * fv;
-                    if (t_lane + 8 * half >= valid) x = y = 0.f;
-                    if (y != y) y = 0.f;                       // (a value that is not finite: told to the rows by v_nan)
-                    sk[half][k] = pack_f16(x, x);
-                    sv[half][k] = pack_f16(y, y);
-                }
             if (wu > 0 && !mbar_wait_warp(smem_u32(&wide_empty[ws]), (wu - 1) & 1, abort_flag)) { ok = false; break; }
             if (lane == 0) {
                 info[ws].ek[dw] = pow2(ek);
@@ -397,25 +388,34 @@ __global__ void __launch_bounds__(kBThreads, 1) q4_block_kernel(const __grid_con
                 info[ws].v_nan[dw] = nans;
                 if (dw == 0) { info[ws].tiles = bits; info[ws].tokens = tokens; }
             }
+            const uint32_t d0 = d_at[0] + ws * S::kWide, d1 = d_at[1] + ws * S::kWide;
 #pragma unroll
             for (int half = 0; half < 2; ++half) {
-                const int row = dw * kQ4Tile + t_lane + 8 * half;
-                const uint32_t dst = smem_u32(wide) + ws * S::kWide + row * 128;
+                uint32_t sk[NG], sv[NG];
+#pragma unroll
+                for (int k = 0; k < NG; ++k) {
+                    float x = (k & 1 ? bf16hi_f(ksc[half][k / 2]) : bf16lo_f(ksc[half][k / 2])) * fk;
+                    float y = (k & 1 ? bf16hi_f(vsc[half][k / 2]) : bf16lo_f(vsc[half][k / 2])) * fv;
+                    if (!plain) {
+                        if (t_lane + 8 * half >= valid) x = y = 0.f;
+                        if (y != y) y = 0.f;                   // (a value that is not finite: told to the rows by v_nan)
+                    }
+                    sk[k] = pack_f16(x, x);
+                    sv[k] = pack_f16(y, y);
+                }
 #pragma unroll
                 for (int w = 0; w < NW; ++w) {                 // K: a 16-byte block of eight channels per word
-                    const uint32_t x = kw[half][w], x8 = x >> 8, s = sk[half][w / WPG];
-                    sts128(dst + (w >> 1) * (kQ4Unit * 128) + ((((w & 1) * 4 + c) ^ (row & 7)) << 4), h2_mul(codes_lo(x), s), h2_mul(codes_hi(x), s),
-                           h2_mul(codes_lo(x8), s), h2_mul(codes_hi(x8), s));
+                    const uint32_t x = kw[half][w], x8 = x >> 8, k = sk[w / WPG];
+                    sts128((w & 1 ? d1 : d0) + (w >> 1) * (kQ4Unit * 128) + half * 1024, h2_mul(codes_lo(x), k), h2_mul(codes_hi(x), k),
+                           h2_mul(codes_lo(x8), k), h2_mul(codes_hi(x8), k));
                 }
 #pragma unroll
                 for (int w = 0; w < NW; ++w) {
-                    // V: nibbles n0 .. n3 of 16 bits, and again 12 bits up: n0 and n1 are in bits 0-3 of the halves, n2 and n3 in bits 8-11
-                    uint32_t A = w & 1 ? va[half][w / 2] >> 16 : va[half][w / 2] & 0xffffu, B = w & 1 ? vb[half][w / 2] >> 16 : vb[half][w / 2] & 0xffffu;
-                    A |= A << 12;
-                    B |= B << 12;
-                    const uint32_t s = sv[half][w / WPG];
-                    sts128(dst + S::kSide + (w >> 1) * (kQ4Unit * 128) + ((((w & 1) * 4 + c) ^ (row & 7)) << 4), h2_mul(codes_lo(A), s), h2_mul(codes_lo(A >> 8), s),
-                           h2_mul(codes_lo(B), s), h2_mul(codes_lo(B >> 8), s));
+                    // V: four channels of chunk 2c below four of chunk 2c + 1; a register then holds channels i and i + 4 of the
+                    // eight, an order that the rows undo when they write o (kVOrder)
+                    const uint32_t x = __byte_perm(va[half][w / 2], vb[half][w / 2], w & 1 ? 0x7632u : 0x5410u), x8 = x >> 8, v = sv[w / WPG];
+                    sts128((w & 1 ? d1 : d0) + S::kSide + (w >> 1) * (kQ4Unit * 128) + half * 1024, h2_mul(codes_lo(x), v), h2_mul(codes_hi(x), v),
+                           h2_mul(codes_lo(x8), v), h2_mul(codes_hi(x8), v));
                 }
             }
             fence_async_smem();                                // the products read through the async proxy
@@ -424,87 +424,77 @@ __global__ void __launch_bounds__(kBThreads, 1) q4_block_kernel(const __grid_con
                 mbar_arrive(smem_u32(&wide_full[ws]));
                 mbar_arrive(smem_u32(&code_empty[cs]));
             }
+            if (++cs == kCS) { cs = 0; ++cu; }
         }
         if (!ok && lane == 0 && !*abort_flag) { *abort_flag = 1; atomicAdd(a.status, 1); }
-    } else if (warp == kBIssueWarp || warp == kBIssueWarp + 1) {
-        // ---------------- products of one half (one lane) ----------------
+    } else if (warp == kBIssueWarp) {
+        // ---------------- products (one lane) ----------------
         if (elect_one()) {
-            const int x = warp - kBIssueWarp;
-            const uint32_t wide_a = smem_u32(wide), t_s = tm + S::kColS + x * kQ4Unit, t_p = tm + S::kColP + x * (kQ4Unit / 2), t_o = tm + S::kColO + x * D;
-            const uint64_t dq = umma_desc(smem_u32(q_mem), 16, 1024, 2);
+            const uint32_t wide_a = smem_u32(wide);
             bool ok = true;
-            uint32_t ph_s = 0, ph_p = 0, ph_q = 0;
+            uint32_t ph_p[2] = {0, 0}, ph_q[2] = {0, 0};
             int u = 0;
-            // s [128 x 64] = Q . K^T: steps of 16 channels, four to a panel
-            auto qk = [&](int stage) {
+            // s of half x [128 x 64] = Q . K^T: steps of 16 channels, four to a panel
+            auto qk = [&](int x, int stage) {
                 const uint64_t dk = umma_desc(wide_a + stage * S::kWide, 16, 1024, 2);
 #pragma unroll
-                for (int ks = 0; ks < D / 16; ++ks) {
-                    const uint64_t b = umma_desc_step(dk, (ks >> 2) * (kQ4Unit * 128) + (ks & 3) * 32);
-                    if (x == 0) umma_ts(t_s, tm + S::kColQ + ks * 8, b, umma_idesc<true>(128, kQ4Unit, 0), ks > 0);
-                    else umma_ss(t_s, umma_desc_step(dq, (ks >> 2) * S::kQPanel + (ks & 3) * 32), b, umma_idesc<true>(128, kQ4Unit, 0), ks > 0);
-                }
+                for (int ks = 0; ks < D / 16; ++ks)
+                    umma_ts(tm + S::kColS + x * kQ4Unit, tm + S::kColQ + x * (D / 2) + ks * 8, umma_desc_step(dk, (ks >> 2) * (kQ4Unit * 128) + (ks & 3) * 32),
+                            umma_idesc<true>(128, kQ4Unit, 0), ks > 0);
                 umma_commit(smem_u32(&s_full[x]));
             };
-            // o [128 x D] (+)= p . V: steps of 16 tokens
-            auto pv = [&](int stage, bool add) {
+            // o of half x [128 x D] (+)= p . V: steps of 16 tokens
+            auto pv = [&](int x, int stage, bool add) {
                 const uint64_t dv = umma_desc(wide_a + stage * S::kWide + S::kSide, kQ4Unit * 128, 1024, 2);
 #pragma unroll
                 for (int ks = 0; ks < kQ4Unit / 16; ++ks)
-                    umma_ts(t_o, t_p + ks * 8, umma_desc_step(dv, ks * 2048), umma_idesc<true>(128, D, 1), add || ks > 0);
-                umma_commit(smem_u32(&wide_empty[stage]));
+                    umma_ts(tm + S::kColO + x * D, tm + S::kColS + x * kQ4Unit + ks * 8, umma_desc_step(dv, ks * 2048), umma_idesc<true>(128, D, 1), add || ks > 0);
             };
             BlockCursor c = seg;
             while (u < left && ok) {
                 const int n_units = min(left - u, c.units - c.unit);
                 const bool two = (long long)c.block * kBRows + kBHalf < (long long)c.q.n * c.q.G;      // the halves have rows of their own
-                int done = 0, stage = 0;                       // units of this half issued, and the stage of the last
-                for (int i = 0; i < n_units && ok; ++i, ++u) {
-                    const int ws = u % kWS;
-                    if (!mbar_wait_or(smem_u32(&wide_full[ws]), (u / kWS) & 1, abort_flag)) { ok = false; break; }
-                    if (!two && (i & 1) != x) {                // the other half's
-                        mbar_arrive(smem_u32(&wide_empty[ws]));
-                        continue;
-                    }
-                    const uint32_t bar = done == 0 ? smem_u32(&q_ready[x]) : smem_u32(&s_read[x]);      // Q is there, or s is in registers
-                    if (!mbar_wait_or(bar, done == 0 ? ph_q : ph_s, abort_flag)) { ok = false; break; }
-                    if (done == 0) ph_q ^= 1;
-                    else ph_s ^= 1;
-                    tc_fence_after();
-                    qk(ws);
-                    if (done > 0) {
-                        if (!mbar_wait_or(smem_u32(&p_ready[x]), ph_p, abort_flag)) { ok = false; break; }
-                        ph_p ^= 1;
+                // the halves in turn: job k is a unit of half k & 1 (its own copy of unit k / 2, or unit k).  A half's s may
+                // be overwritten once its p, which lies there, has been used.
+                const int jobs = two ? 2 * n_units : n_units;
+                for (int k = 0; k < jobs + 2; ++k) {
+                    const int x = k & 1;
+                    if (k >= 2) {
+                        if (k - 2 >= jobs) break;
+                        const int i = two ? (k - 2) >> 1 : k - 2, stage = (u + i) % kWS;
+                        if (!mbar_wait_or(smem_u32(&p_ready[x]), ph_p[x], abort_flag)) { ok = false; break; }
+                        ph_p[x] ^= 1;
                         tc_fence_after();
-                        pv(stage, done > 1);
-                        umma_commit(smem_u32(&p_free[x]));
+                        pv(x, stage, k >= 4);
+                        if (!two || x == 1) umma_commit(smem_u32(&wide_empty[stage]));
+                        if (k >= jobs) umma_commit(smem_u32(&o_done[x]));      // the half's last
                     }
-                    stage = ws;
-                    ++done;
+                    if (k < jobs) {
+                        const int i = two ? k >> 1 : k, stage = (u + i) % kWS;
+                        if (k < 2) {
+                            if (!mbar_wait_or(smem_u32(&q_ready[x]), ph_q[x], abort_flag)) { ok = false; break; }
+                            ph_q[x] ^= 1;
+                        }
+                        if (!mbar_wait_or(smem_u32(&wide_full[stage]), ((u + i) / kWS) & 1, abort_flag)) { ok = false; break; }
+                        tc_fence_after();
+                        qk(x, stage);
+                    }
                 }
-                if (!ok) break;
-                if (done > 0) {
-                    if (!mbar_wait_or(smem_u32(&s_read[x]), ph_s, abort_flag) || !mbar_wait_or(smem_u32(&p_ready[x]), ph_p, abort_flag)) { ok = false; break; }
-                    ph_s ^= 1;
-                    ph_p ^= 1;
-                    tc_fence_after();
-                    pv(stage, done > 1);
-                    umma_commit(smem_u32(&o_done[x]));
-                }
-                if (u < left) block_advance(a, c, n_units);
+                u += n_units;
+                if (u < left && ok) block_advance(a, c, n_units);
             }
             if (!ok && !*abort_flag) { *abort_flag = 1; atomicAdd(a.status, 1); }
             // nothing of this CTA's may still be running on the tensor cores when tensor memory is given back
-            umma_commit(smem_u32(&drain[x]));
-            (void)mbar_wait(smem_u32(&drain[x]), 0, limit);
+            umma_commit(smem_u32(&drain));
+            (void)mbar_wait(smem_u32(&drain), 0, limit);
         }
     } else if (warp < kBRowWarps) {
         // ---------------- rows: one query row per thread ----------------
         const int x = warp >> 2, r_half = (warp & 3) * 32 + lane;
         const uint32_t t_lane = tm + ((uint32_t)((warp & 3) * 32) << 16);
-        const uint32_t t_o = t_lane + S::kColO + x * D, t_s = t_lane + S::kColS + x * kQ4Unit, t_p = t_lane + S::kColP + x * (kQ4Unit / 2);
+        const uint32_t t_o = t_lane + S::kColO + x * D, t_s = t_lane + S::kColS + x * kQ4Unit;
         bool ok = true;
-        uint32_t ph_s = 0, ph_o = 0, ph_f = 0, ph_st = 0;
+        uint32_t ph_s = 0, ph_o = 0, ph_st = 0;
         int u = 0;
         BlockCursor c = seg;
         while (u < left && ok) {
@@ -550,35 +540,34 @@ __global__ void __launch_bounds__(kBThreads, 1) q4_block_kernel(const __grid_con
                                 pk[4 * k + b] = pack_f16(lo * up, hi * up);
                             }
                         }
-                        if (x == 0) {
-                            tmem_st16(t_lane + S::kColQ + 16 * i, pk);
-                        } else {                               // 32 channels: half a 128-byte row of a panel
-#pragma unroll
-                            for (int k = 0; k < 4; ++k)
-                                *reinterpret_cast<uint4 *>(q_mem + (i >> 1) * S::kQPanel + r_half * 128 + ((((i & 1) * 4 + k) ^ (r_half & 7)) << 4)) =
-                                    make_uint4(pk[4 * k], pk[4 * k + 1], pk[4 * k + 2], pk[4 * k + 3]);
-                        }
+                        tmem_st16(t_lane + S::kColQ + x * (D / 2) + 16 * i, pk);
                     }
-                    if (x == 0) tmem_st_wait();
-                    else fence_async_smem();
+                    tmem_st_wait();
                     tc_fence_before();
                     mbar_arrive(smem_u32(&q_ready[x]));
                 }
                 const int vis = row_ok ? c.q.T - c.q.all + j + 1 : c.q.T;
                 for (int i = i0; i < n_units; i += step) {
                     const int ws = (u + i) % kWS;
-                    if (!mbar_wait_warp(smem_u32(&s_full[x]), ph_s, abort_flag) || !mbar_wait_warp(smem_u32(&wide_full[ws]), ((u + i) / kWS) & 1, abort_flag)) { ok = false; break; }
+                    // what the unit is like, while its scores are being computed
+                    if (!mbar_wait_warp(smem_u32(&wide_full[ws]), ((u + i) / kWS) & 1, abort_flag)) { ok = false; break; }
+                    const UnitInfo &inf = info[ws];
+                    const int t0 = (c.unit + i) * kQ4Unit, lim = min(vis - t0, (int)inf.tokens);
+                    const uint32_t tiles = inf.tiles;
+                    const bool masked = __any_sync(0xffffffffu, lim < kQ4Unit) || tiles != (1u << kQ4UnitTiles) - 1u;
+                    const bool nans = (inf.v_nan[0] | inf.v_nan[1] | inf.v_nan[2] | inf.v_nan[3]) != 0;
+                    float fk[kQ4UnitTiles], ev[kQ4UnitTiles];
+#pragma unroll
+                    for (int k = 0; k < kQ4UnitTiles; ++k) {
+                        fk[k] = fmaxf(f * inf.ek[k], 1.2e-38f);      // (never 0: a hidden score is -inf)
+                        ev[k] = inf.ev[k];
+                    }
+                    if (!mbar_wait_warp(smem_u32(&s_full[x]), ph_s, abort_flag)) { ok = false; break; }
                     ph_s ^= 1;
                     tc_fence_after();
                     float sv[kQ4Unit];
                     tmem_ld<kQ4Unit>(t_s, reinterpret_cast<uint32_t *>(sv));
-                    tc_fence_before();
-                    mbar_arrive(smem_u32(&s_read[x]));
-                    const UnitInfo &inf = info[ws];
-                    const int t0 = (c.unit + i) * kQ4Unit, lim = min(vis - t0, (int)inf.tokens);
-                    const uint32_t tiles = inf.tiles;
-                    bool free = i == i0;                       // p and o of the unit before are no longer in use
-                    if (__any_sync(0xffffffffu, lim < kQ4Unit) || tiles != (1u << kQ4UnitTiles) - 1u) {
+                    if (masked) {
                         uint32_t nan = 0;
 #pragma unroll
                         for (int k = 0; k < kQ4Unit; ++k)
@@ -589,15 +578,13 @@ __global__ void __launch_bounds__(kBThreads, 1) q4_block_kernel(const __grid_con
                             nan |= inf.v_nan[k] & ((1u << m) - 1u);
                         }
                         if (nan) l = __int_as_float(0x7fc00000);
-                    } else if (inf.v_nan[0] | inf.v_nan[1] | inf.v_nan[2] | inf.v_nan[3]) {
+                    } else if (nans) {
                         l = __int_as_float(0x7fc00000);        // a value that is not finite: the row is not either
                     }
                     // x = s * f 2^Ek + Ev, against a reference that the largest has not passed by more than 2^8
-                    float fk[kQ4UnitTiles], ev[kQ4UnitTiles], top = -INFINITY;
+                    float top = -INFINITY;
 #pragma unroll
                     for (int k = 0; k < kQ4UnitTiles; ++k) {
-                        fk[k] = fmaxf(f * inf.ek[k], 1.2e-38f);      // (never 0: a hidden score is -inf)
-                        ev[k] = inf.ev[k];
                         const float *p = sv + k * kQ4Tile;
                         float m0 = max3(p[0], p[1], p[2]), m1 = max3(p[3], p[4], p[5]);
                         m0 = max3(m0, p[6], p[7]); m1 = max3(m1, p[8], p[9]);
@@ -609,11 +596,7 @@ __global__ void __launch_bounds__(kBThreads, 1) q4_block_kernel(const __grid_con
                         const float Fn = top > kNegInf ? fmaxf(F, top) : F, corr = ex2(F - Fn);
                         F = Fn;
                         l *= corr;
-                        if (i > i0) {
-                            if (!mbar_wait_warp(smem_u32(&p_free[x]), ph_f, abort_flag)) { ok = false; break; }
-                            ph_f ^= 1;
-                            free = true;
-                            tc_fence_after();
+                        if (i > i0) {                          // (every earlier product of this half is complete: s was committed behind it)
                             uint32_t r[32];
 #pragma unroll 1
                             for (int b = 0; b < D / 32; ++b) {
@@ -644,12 +627,7 @@ __global__ void __launch_bounds__(kBThreads, 1) q4_block_kernel(const __grid_con
                         f2_unpack(f2_add(sum[0], sum[1]), s0, s1);
                         l = fmaf(s0 + s1, pow2(-(int)ev[k]), l);
                     }
-                    if (!free) {
-                        if (!mbar_wait_warp(smem_u32(&p_free[x]), ph_f, abort_flag)) { ok = false; break; }
-                        ph_f ^= 1;
-                        tc_fence_after();
-                    }
-                    tmem_st32(t_p, pk);
+                    tmem_st32(t_s, pk);
                     tmem_st_wait();
                     tc_fence_before();
                     mbar_arrive(smem_u32(&p_ready[x]));
@@ -700,6 +678,8 @@ __global__ void __launch_bounds__(kBThreads, 1) q4_block_kernel(const __grid_con
                     tmem_ld_wait();
 #pragma unroll
                     for (int k = 0; k < 32; ++k) r[k] = __float_as_uint(__uint_as_float(r[k]) * f0);
+                    // (channel i of eight is column kVOrder[i]: the order in which V was widened)
+                    constexpr int kVOrder[8] = {0, 2, 4, 6, 1, 3, 5, 7};
                     if (merge) {
                         uint32_t r1[32];
                         tmem_ld32(t_o + D + 32 * b, r1);       // the second half's o, the same lanes
@@ -709,14 +689,14 @@ __global__ void __launch_bounds__(kBThreads, 1) q4_block_kernel(const __grid_con
                     }
                     if (dst) {
 #pragma unroll
-                        for (int k = 0; k < 16; ++k) *reinterpret_cast<uint2 *>(dst + 32 * b + 2 * k) = make_uint2(r[2 * k], r[2 * k + 1]);
+                        for (int k = 0; k < 16; ++k) *reinterpret_cast<uint2 *>(dst + 32 * b + 2 * k) = make_uint2(r[(2 * k & ~7) + kVOrder[2 * k & 7]], r[(2 * k & ~7) + kVOrder[(2 * k + 1) & 7]]);
                     } else if (complete && row_ok) {
 #pragma unroll
                         for (int k = 0; k < 4; ++k) {
                             uint32_t w[4];
 #pragma unroll
                             for (int m = 0; m < 4; ++m) {
-                                const float y0 = __uint_as_float(r[8 * k + 2 * m]), y1 = __uint_as_float(r[8 * k + 2 * m + 1]);
+                                const float y0 = __uint_as_float(r[8 * k + kVOrder[2 * m]]), y1 = __uint_as_float(r[8 * k + kVOrder[2 * m + 1]]);
                                 w[m] = H16 ? pack_f16(y0, y1) : pack_bf16(y0, y1);
                             }
                             *reinterpret_cast<uint4 *>(out + 32 * b + 8 * k) = make_uint4(w[0], w[1], w[2], w[3]);
