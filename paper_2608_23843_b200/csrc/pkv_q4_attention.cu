@@ -29,6 +29,9 @@ namespace pkv {
 namespace {
 
 constexpr int kQ4Step = 2;             // tiles per softmax step
+// What a segment costs a CTA beside its units - queries, joining the warps' states - in units: a CTA of many short segments
+// takes no longer than one of few long ones (32 sequences of 512 to 16384 tokens: 47 -> see the table of measurements).
+constexpr int kQ4SegCost = 6;
 // Warps of a CTA (two CTAs per SM), the last one for the copies: the kernel is bound by instruction issue, so as many warps as
 // their registers allow - one column of query rows in 128 registers a thread, two in 168.
 __host__ __device__ constexpr int q4_warps(int nt) { return nt == 1 ? 8 : 6; }
@@ -157,7 +160,7 @@ __global__ void __launch_bounds__(Q4Shape<D, NG, NT>::kThreads, 2) q4_decode_ker
         if (s >= n_seqs) return 0;
         int first, all;
         const int n = q4_new_rows(a, s, first, all, st), T = q4_length(a.rows, geo, s, st);
-        return (long long)((n * geo.group + R - 1) / R) * H * (a.whole ? 1 : max(1, (T + kQ4Unit - 1) / kQ4Unit));
+        return (long long)((n * geo.group + R - 1) / R) * H * (a.whole ? 1 : max(1, (T + kQ4Unit - 1) / kQ4Unit) + kQ4SegCost);
     };
     long long total = 0;
     if (n_seqs == 1) {
@@ -173,8 +176,14 @@ __global__ void __launch_bounds__(Q4Shape<D, NG, NT>::kThreads, 2) q4_decode_ker
         for (int w = 0; w < kQ4Warps; ++w) total += sums[w];
     }
     // (no more CTAs than there are units for a warp of each; the launch could only estimate that)
-    const int n_ctas = (int)min((long long)gridDim.x, max(1LL, a.whole ? total : total / kCons));
-    const long long begin = total * blockIdx.x / n_ctas, end = total * (blockIdx.x + 1) / n_ctas;
+    const int n_ctas = (int)min((long long)gridDim.x, max(1LL, a.whole ? total : total / (kCons + kQ4SegCost)));
+    // (b * total / n without a 64-bit division where the total has 31 bits)
+    auto share = [&](long long b) -> long long {
+        if (total >> 31) return total * b / n_ctas;
+        const unsigned q = (unsigned)total / (unsigned)n_ctas, r = (unsigned)total % (unsigned)n_ctas;
+        return (long long)q * b + r * (unsigned)b / (unsigned)n_ctas;
+    };
+    const long long begin = share(blockIdx.x), end = share(blockIdx.x + 1LL);
     Q4Part *parts = reinterpret_cast<Q4Part *>(a.workspace);
     float *states = reinterpret_cast<float *>(a.workspace + q4_parts_bytes(gridDim.x));
     const bool joined = !a.whole && gridDim.x > 1;             // segments may span CTAs
@@ -216,22 +225,43 @@ __global__ void __launch_bounds__(Q4Shape<D, NG, NT>::kThreads, 2) q4_decode_ker
         at0 = found_at;
     }
     q4_load_seq(a, R, seg);
-    int left_cta = (int)(end - begin);                         // units of the CTA
+    int left_cta;                                              // units of the CTA
+    long long seg_pos = 0;                                     // where the current segment begins, on the scale of the weights
     if (a.whole) {
         seg.unit = 0;
         seg.head = (int)(at0 % H);
         seg.tile = (int)(at0 / H);
         Q4Cursor w = seg;
-        const int segs = left_cta;
         left_cta = w.units;
-        for (int k = 1; k < segs; ++k) {
+        for (int k = 1; k < (int)(end - begin); ++k) {
             q4_advance(a, R, w, w.units);
             left_cta += w.units;
         }
     } else {
-        seg.unit = (int)(at0 % seg.units);
-        seg.head = (int)(at0 / seg.units % H);
-        seg.tile = (int)(at0 / seg.units / H);
+        const int len = seg.units + kQ4SegCost;
+        const int idx = (int)(at0 / len), off = (int)(at0 - (long long)idx * len);      // (a sequence's segments number fewer than 2^31)
+        seg.head = idx % H;
+        seg.tile = idx / H;
+        seg.unit = min(off, seg.units);
+        seg_pos = begin - off;
+        if (seg.unit == seg.units) {                           // the share begins behind a segment's units
+            seg_pos += len;
+            q4_advance(a, R, seg, 0);
+        }
+        left_cta = 0;
+        Q4Cursor w = seg;
+        long long pos = seg_pos;
+        while (w.seq < n_seqs && pos + w.unit < end) {
+            const int here = (int)min((long long)(w.units - w.unit), end - pos - w.unit);
+            left_cta += here;
+            if (here < w.units - w.unit) break;
+            pos += w.units + kQ4SegCost;
+            q4_advance(a, R, w, w.units - w.unit);
+        }
+        if (left_cta == 0) {
+            if (tid == 0 && joined) parts[blockIdx.x].seq = -1;
+            return;
+        }
     }
     volatile int *abort_flag = &gave_up;
 
@@ -698,16 +728,16 @@ __global__ void __launch_bounds__(Q4Shape<D, NG, NT>::kThreads, 2) q4_decode_ker
             // the CTA's last segment: does it begin here and go on elsewhere?
             Q4Part p{-1, 0, 0, 0, 0};
             if (starts && !ends) {
-                const long long w1 = begin + seg_lo + seg.units;          // one past the segment's last unit
-                p = Q4Part{seg.seq, seg.tile, seg.head, slot, (int)((w1 * n_ctas - 1) / total)};
+                // the CTA whose share holds the last unit
+                p = Q4Part{seg.seq, seg.tile, seg.head, slot, (int)(((seg_pos + seg.units) * n_ctas - 1) / total)};
             }
             parts[blockIdx.x] = p;
         }
         if (any && lane == 0) mbar_arrive(smem_u32(&empty[st_last]));
         seg_lo = seg_hi;
         if (seg_lo < left_cta) {
-            const int by = seg.units - seg.unit;
-            q4_advance(a, R, seg, by);
+            seg_pos += seg.units + kQ4SegCost;
+            q4_advance(a, R, seg, seg.units - seg.unit);
         }
     }
 }
