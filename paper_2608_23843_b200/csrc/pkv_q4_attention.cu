@@ -765,38 +765,61 @@ __global__ void __launch_bounds__(32 * kQ4JoinWarps) q4_join_kernel(const __grid
     const long long per = q4_state_floats(R, D);
     // the first part is in slot p.slot of CTA b, the others in slot 0 of the CTAs behind it
     auto state = [&](int k) { return states + (2LL * k + (k == b ? p.slot : 0)) * per; };
-    float M = kNegInf;
-    for (int k = b + lane; k <= p.last_cta; k += 32) M = fmaxf(M, state(k)[R * D + r]);
-#pragma unroll
-    for (int d = 16; d; d >>= 1) M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, d));
-    constexpr int C = D / 32;
-    float L = 0.f, acc[C];
+    // a warp's parts in one pass, four at a time: the weights are not waited for before o is asked for
+    constexpr int C = D / 32, kAhead = 4;
+    float M = kNegInf, L = 0.f, acc[C];
 #pragma unroll
     for (int i = 0; i < C; ++i) acc[i] = 0.f;
-#pragma unroll 4
-    for (int k = b + (W == 1 ? 0 : warp); k <= p.last_cta; k += W) {
-        const float *s = state(k);
-        const float f = ex2(s[R * D + r] - M);
-        L += f * s[R * D + R + r];
-        const float2 *x = reinterpret_cast<const float2 *>(s + r * D + C * lane);
+    for (int k0 = b + (W == 1 ? 0 : warp); k0 <= p.last_cta; k0 += W * kAhead) {
+        float m[kAhead], l[kAhead], x[kAhead][C], top = M;
 #pragma unroll
-        for (int i = 0; i < C / 2; ++i) { const float2 v = x[i]; acc[2 * i] += f * v.x; acc[2 * i + 1] += f * v.y; }
+        for (int i = 0; i < kAhead; ++i) {
+            const int k = k0 + i * W;
+            m[i] = kNegInf;
+            l[i] = 0.f;
+#pragma unroll
+            for (int c = 0; c < C; ++c) x[i][c] = 0.f;
+            if (k <= p.last_cta) {
+                const float *s = state(k);
+                m[i] = s[R * D + r];
+                l[i] = s[R * D + R + r];
+#pragma unroll
+                for (int c = 0; c < C; c += 2) { const float2 v = *reinterpret_cast<const float2 *>(s + r * D + C * lane + c); x[i][c] = v.x; x[i][c + 1] = v.y; }
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i) top = fmaxf(top, m[i]);
+        const float f = ex2(M - top);
+        M = top;
+        L *= f;
+#pragma unroll
+        for (int c = 0; c < C; ++c) acc[c] *= f;
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i) {
+            const float w = ex2(m[i] - M);
+            L += w * l[i];
+#pragma unroll
+            for (int c = 0; c < C; ++c) acc[c] += w * x[i][c];
+        }
     }
     if (W > 1) {
-        __shared__ float part[kQ4JoinWarps][D + 1];
+        __shared__ float part[kQ4JoinWarps][D + 2];
 #pragma unroll
         for (int i = 0; i < C; ++i) part[warp][C * lane + i] = acc[i];
-        if (lane == 0) part[warp][D] = L;
+        if (lane == 0) { part[warp][D] = L; part[warp][D + 1] = M; }
         __syncthreads();
         if (warp > 0) return;
+#pragma unroll
+        for (int w = 0; w < W; ++w) M = fmaxf(M, part[w][D + 1]);
         L = 0.f;
 #pragma unroll
         for (int i = 0; i < C; ++i) acc[i] = 0.f;
 #pragma unroll
         for (int w = 0; w < W; ++w) {
+            const float f = ex2(part[w][D + 1] - M);
 #pragma unroll
-            for (int i = 0; i < C; ++i) acc[i] += part[w][C * lane + i];
-            L += part[w][D];
+            for (int i = 0; i < C; ++i) acc[i] += f * part[w][C * lane + i];
+            L += f * part[w][D];
         }
     }
     const int h = p.head * G + (int)(row - (long long)j * G);
