@@ -17,7 +17,7 @@ namespace {
 // ---- kernels -------------------------------------------------------------------------------------------------------
 // Both copy kernels are bound by HBM: 4 d bytes of 16-bit rows and d + 4 d/g bytes of cache per token and KV head.  A CTA
 // takes a few rows of the call: it looks up where they lie once, a thread each, while the first 16-byte loads are in flight
-// (of d/8 lanes per row and head, K and V together), so that nothing but the loads, the arithmetic and the stores is paid per
+// (K and V of a row and head together), so that nothing but the loads, the arithmetic and the stores is paid per
 // head.
 constexpr int kCopyThreads = 256, kCopyUnroll = 4, kCopyRows = 128;
 
@@ -108,21 +108,29 @@ __device__ __forceinline__ uint32_t codes8(const float *x, float s) {
 // (its clamp: 7 * scale has to be finite in bf16; bf16(max / 7) of the type's two largest values is not)
 constexpr float kScaleMost = 4.8183102e37f;          // 36.25 * 2^120
 
-// A lane's eight channels of one row: the codes' word and the group's scale.
+// A lane's sixteen channels of one row: the codes' two words and the group's scale (of which the lane holds a half, a quarter
+// or an eighth: sixteen channels to a lane rather than eight, so that what is done once per lane - the group's maximum over the
+// lanes, scale, reciprocal, addresses - is done half as often; the kernel was bound by instructions).
 template <int GL, bool H16, bool kV>
-__device__ __forceinline__ void quantise8(const uint4 &raw, uint32_t &w, unsigned short &scale) {
+__device__ __forceinline__ void quantise16(const uint4 *raw, uint32_t *w, unsigned short &scale) {
     // largest magnitude of the group, as bits: non-negative 16-bit floats order like integers, infinities and NaN last
-    uint32_t mx = __vmaxu2(__vmaxu2(raw.x & 0x7fff7fffu, raw.y & 0x7fff7fffu), __vmaxu2(raw.z & 0x7fff7fffu, raw.w & 0x7fff7fffu));
+    uint32_t mx = 0;
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+        mx = __vmaxu2(mx, __vmaxu2(__vmaxu2(raw[i].x & 0x7fff7fffu, raw[i].y & 0x7fff7fffu), __vmaxu2(raw[i].z & 0x7fff7fffu, raw[i].w & 0x7fff7fffu)));
     mx = max(mx & 0xffffu, mx >> 16);
 #pragma unroll
     for (int d = 1; d < GL; d <<= 1) mx = max(mx, __shfl_xor_sync(0xffffffffu, mx, d));
     const float amax = H16 ? __half2float(__ushort_as_half((unsigned short)mx)) : __uint_as_float(mx << 16);
     const __nv_bfloat16 sb = __float2bfloat16_rn(fminf(amax * (1.f / 7.f), kScaleMost));
-    float v[8];
-    unpack8<H16>(raw, v);
-    w = codes8<kV>(v, __bfloat162float(sb));
     scale = __bfloat16_as_ushort(sb);
-    if (mx >= (H16 ? 0x7c00u : 0x7f80u)) { w = 0x88888888u; scale = 0x7fc0u; }      // not finite: zero codes, and a NaN for a scale
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        float v[8];
+        unpack8<H16>(raw[i], v);
+        w[i] = codes8<kV>(v, __bfloat162float(sb));
+    }
+    if (mx >= (H16 ? 0x7c00u : 0x7f80u)) { w[0] = w[1] = 0x88888888u; scale = 0x7fc0u; }      // not finite: zero codes, and a NaN for a scale
 }
 
 // Rows of a CTA and where they lie.
@@ -137,25 +145,27 @@ __device__ __forceinline__ CopyRows copy_rows(const Q4CopyArgs &a) {
 
 template <int D, int NG, bool H16>
 __global__ void __launch_bounds__(kCopyThreads) q4_append_kernel(const __grid_constant__ Q4CopyArgs a) {
-    constexpr int LR = D / 8, GL = LR / NG, kSlots = kCopyThreads / LR;          // lanes per row and head, lanes per group
+    constexpr int LR = D / 16, GL = LR / NG, kSlots = kCopyThreads / LR, kUnroll = 2;      // lanes per row and head, lanes per group
     __shared__ RowPlace places[kCopyRows];
     const Q4Geometry &geo = a.geo;
     const CopyRows cr = copy_rows<D>(a);
-    const int l = threadIdx.x % LR, slot = threadIdx.x / LR, j = l >> 2, c = l & 3;
+    const int l = threadIdx.x % LR, slot = threadIdx.x / LR, j = l >> 1, b = l & 1;      // 32-channel word j, its half b
     bool looked_up = false;
-    for (int base = 0; base < cr.n_jobs; base += kSlots * kCopyUnroll) {
-        uint4 k[kCopyUnroll], v[kCopyUnroll];
-        int row[kCopyUnroll], head[kCopyUnroll];
+    for (int base = 0; base < cr.n_jobs; base += kSlots * kUnroll) {
+        uint4 k[kUnroll][2], v[kUnroll][2];
+        int row[kUnroll], head[kUnroll];
 #pragma unroll
-        for (int u = 0; u < kCopyUnroll; ++u) {
+        for (int u = 0; u < kUnroll; ++u) {
             const int job = base + u * kSlots + slot;
             row[u] = __float2int_rz((job + 0.5f) * a.inv_heads);
             head[u] = job - row[u] * geo.n_kv_heads;
-            k[u] = v[u] = make_uint4(0u, 0u, 0u, 0u);
+            k[u][0] = k[u][1] = v[u][0] = v[u][1] = make_uint4(0u, 0u, 0u, 0u);
             if (job < cr.n_jobs) {
                 const long long i = cr.row0 + row[u];
-                k[u] = __ldg(reinterpret_cast<const uint4 *>(reinterpret_cast<const unsigned short *>(a.k) + i * a.k_row + head[u] * a.k_head) + l);
-                v[u] = __ldg(reinterpret_cast<const uint4 *>(reinterpret_cast<const unsigned short *>(a.v) + i * a.v_row + head[u] * a.v_head) + l);
+                const uint4 *kp = reinterpret_cast<const uint4 *>(reinterpret_cast<const unsigned short *>(a.k) + i * a.k_row + head[u] * a.k_head) + 2 * l;
+                const uint4 *vp = reinterpret_cast<const uint4 *>(reinterpret_cast<const unsigned short *>(a.v) + i * a.v_row + head[u] * a.v_head) + 2 * l;
+                k[u][0] = __ldg(kp); k[u][1] = __ldg(kp + 1);
+                v[u][0] = __ldg(vp); v[u][1] = __ldg(vp + 1);
             }
         }
         if (!looked_up) {
@@ -164,21 +174,26 @@ __global__ void __launch_bounds__(kCopyThreads) q4_append_kernel(const __grid_co
             __syncthreads();
         }
 #pragma unroll
-        for (int u = 0; u < kCopyUnroll; ++u) {
+        for (int u = 0; u < kUnroll; ++u) {
             if (base + u * kSlots >= cr.n_jobs) break;          // (the same for all threads)
-            uint32_t wk, wv;
+            uint32_t wk[2], wv[2];
             unsigned short sk, sv;
-            quantise8<GL, H16, false>(k[u], wk, sk);
-            quantise8<GL, H16, true>(v[u], wv, sv);
-            const uint32_t other = __shfl_xor_sync(0xffffffffu, wv, 4);
+            quantise16<GL, H16, false>(k[u], wk, sk);
+            quantise16<GL, H16, true>(v[u], wv, sv);
+            // V: this lane has chunks 4b .. 4b + 3 of word j, lane l ^ 2 those of word j ^ 1; even words keep the first two
+            // chunks of both lanes and odd words the other two
+            const uint32_t other = __shfl_xor_sync(0xffffffffu, j & 1 ? wv[0] : wv[1], 2);
             if (base + u * kSlots + slot >= cr.n_jobs) continue;
             const RowPlace at = places[row[u]];
             if (!at.ok) continue;
             unsigned char *tile = a.pool + at.off + (long long)head[u] * geo.head_bytes;
-            // V: lanes j and j ^ 1 hold chunks 2c and 2c + 1 of 32-channel words j and j ^ 1: each stores one chunk's two words
-            const uint32_t two = j & 1 ? __byte_perm(other, wv, 0x7632) : __byte_perm(wv, other, 0x5410);
-            *reinterpret_cast<uint32_t *>(tile + q4_k_chunk(D, at.t, c) + j * 4) = wk;
-            *reinterpret_cast<uint32_t *>(tile + q4_v_base(D) + q4_v_chunk(D, at.t, 2 * c + (j & 1)) + (j >> 1) * 4) = two;
+            const uint32_t lo = j & 1 ? other : wv[0], hi = j & 1 ? wv[1] : other;      // words j & ~1 and j | 1 of two chunks
+            *reinterpret_cast<uint32_t *>(tile + q4_k_chunk(D, at.t, 2 * b) + j * 4) = wk[0];
+            *reinterpret_cast<uint32_t *>(tile + q4_k_chunk(D, at.t, 2 * b + 1) + j * 4) = wk[1];
+            unsigned char *vt = tile + q4_v_base(D) + (j >> 1) * 4;
+            const int g0 = 4 * b + 2 * (j & 1);
+            *reinterpret_cast<uint32_t *>(vt + q4_v_chunk(D, at.t, g0)) = __byte_perm(lo, hi, 0x5410);
+            *reinterpret_cast<uint32_t *>(vt + q4_v_chunk(D, at.t, g0 + 1)) = __byte_perm(lo, hi, 0x7632);
             if (l % GL == 0) {
                 *reinterpret_cast<unsigned short *>(tile + q4_ks_base(D) + (at.t * NG + l / GL) * 2) = sk;
                 *reinterpret_cast<unsigned short *>(tile + q4_vs_base(D, NG) + (at.t * NG + l / GL) * 2) = sv;
