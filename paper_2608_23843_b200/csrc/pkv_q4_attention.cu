@@ -11,7 +11,7 @@
 //   V codes become exact fp16 integers, two products' rows from each byte (see there; as subnormals they would lose the
 //     contributions of small weights next to a large one's + 8); the scales go to the weights, p * scale, rounded once to fp16.  To keep that inside fp16's range whatever the values' size, the running reference
 //     of the softmax is max(s) + E with E the exponent of the largest value scale so far; it follows when some score has passed
-//     it by 2^8 only, so p * scale <= 2^9, and a unit that moves nothing costs one vote.
+//     it by 2^14 only, so p * scale <= 2^15, and a unit that moves nothing costs one vote.
 //   Queries are brought to fp16 with a power of two per row, which is exact for bf16 and fp16 alike.
 // One warp of a CTA looks up pages and issues the bulk copies; the others take the units of 64 tokens in turn and keep (m, l, o)
 // in registers; at the end of a (sequence, KV head, row tile) segment the warps' states are joined through shared memory.  The CTAs of

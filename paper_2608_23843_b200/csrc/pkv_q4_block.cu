@@ -12,12 +12,13 @@
 //     one warp       issues the products, one lane: s = Q K^T with Q and, later, p as row operands in tensor memory,
 //                    o += p V; while one half's rows are in their softmax the other half's products run,
 //     eight warps    softmax: s from tensor memory, p as fp16 back over it, o rescaled only when the running reference has been
-//                    passed by 2^8 (then p * value may still not leave fp16: 2^8 * 14).
+//                    passed by 2^14 (p stays inside fp16).
 // What bounds it: products and exponentials each take 1024 cycles per unit of 256 rows, but a half's chain - s, softmax, o,
 // the hand-overs between them - is some 1800 cycles long even with both for free, and the widening competes with the softmax
 // for issue slots.  Measured on 2048 positions against 32K (32 / 8 heads, g = 32) and not kept: Q of one half in shared memory
 // so that s of the next unit can be computed behind the softmax (the products then wait for shared memory), five or six
-// widening warps, a quarter of the exponentials by polynomial, the halves' exponentials in turn.
+// widening warps, a quarter of the exponentials by polynomial, the halves' exponentials in turn, weights with the old
+// reference before the maximum is known.
 // CTAs share the batch's units evenly, one CTA per SM; blocks that span CTAs leave states that a second kernel joins.  Units
 // after a block's last visible position are not visited.
 #include <cuda_bf16.h>
@@ -121,7 +122,8 @@ __device__ __forceinline__ void block_advance(const Q4AttentionArgs &a, BlockCur
 
 // What the widening warps tell the rows about a unit.
 struct UnitInfo {
-    float ek[kQ4UnitTiles], ev[kQ4UnitTiles];       // exponents taken out of the tiles' keys and values
+    float ek[kQ4UnitTiles];                         // powers of two taken out of the tiles' keys
+    float ev[kQ4UnitTiles], ev_inv[kQ4UnitTiles];   // ... and values: exponents, and 2^-exponent
     uint32_t v_nan[kQ4UnitTiles];                   // tokens with a value group that is not finite (stored as zeros here)
     uint32_t tiles, tokens;                         // which tiles are there; tokens of the sequence in the unit
 };
@@ -385,6 +387,7 @@ __global__ void __launch_bounds__(kBThreads, 1) q4_block_kernel(const __grid_con
             if (lane == 0) {
                 info[ws].ek[dw] = pow2(ek);
                 info[ws].ev[dw] = (float)ev;
+                info[ws].ev_inv[dw] = fv;
                 info[ws].v_nan[dw] = nans;
                 if (dw == 0) { info[ws].tiles = bits; info[ws].tokens = tokens; }
             }
@@ -581,7 +584,7 @@ __global__ void __launch_bounds__(kBThreads, 1) q4_block_kernel(const __grid_con
                     } else if (nans) {
                         l = __int_as_float(0x7fc00000);        // a value that is not finite: the row is not either
                     }
-                    // x = s * f 2^Ek + Ev, against a reference that the largest has not passed by more than 2^8
+                    // x = s * f 2^Ek + Ev, against a reference that the largest has not passed by more than 2^14
                     float top = -INFINITY;
 #pragma unroll
                     for (int k = 0; k < kQ4UnitTiles; ++k) {
@@ -625,7 +628,7 @@ __global__ void __launch_bounds__(kBThreads, 1) q4_block_kernel(const __grid_con
                         }
                         float s0, s1;
                         f2_unpack(f2_add(sum[0], sum[1]), s0, s1);
-                        l = fmaf(s0 + s1, pow2(-(int)ev[k]), l);
+                        l = fmaf(s0 + s1, inf.ev_inv[k], l);
                     }
                     tmem_st32(t_s, pk);
                     tmem_st_wait();

@@ -12,7 +12,7 @@ namespace {
 
 constexpr int kQ4Unit = 64;            // tokens per unit: four tiles
 constexpr int kQ4UnitTiles = kQ4Unit / kQ4Tile;
-constexpr float kQ4Lag = 8.f;          // how far (base 2) scores may pass the softmax's reference before it follows
+constexpr float kQ4Lag = 14.f;         // how far (base 2) scores may pass the softmax's reference before it follows: weights stay inside fp16
 
 // A segment that begins in a CTA and ends in another (seq < 0: none); slot: where its first part is (see below)
 struct Q4Part { int seq, tile, head, slot, last_cta; };
