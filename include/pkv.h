@@ -501,7 +501,7 @@ pkv_status pkv_get_row_block_ranges(int64_t n_row_blocks, int32_t longest_tokens
  *
  * The caller keeps the bookkeeping, on the device, so that a captured CUDA graph stays valid while sequences grow, come
  * and go:  page_table [device] int32 [n_seqs, max_pages], position t of sequence s lies in row t % page_size of physical
- * page page_table[s, t / page_size];  lengths [device] int32 [n_seqs], T = tokens of each sequence.  Sequences may share
+ * page page_table[s, t / page_size] (max_pages * page_size at most 2^30);  lengths [device] int32 [n_seqs], T = tokens of each sequence.  Sequences may share
  * pages for reading (a common prefix); a page that a call writes to belongs to one place of one sequence.  One cache can
  * hold any number of layers: give each its own pages.
  * Rows of a call: sequence s owns rows offsets[s] .. offsets[s + 1] - 1 of the caller's buffers (offsets [device] int32

@@ -363,7 +363,7 @@ pkv_status q4_validate(const pkv_q4_config *cfg, Q4Geometry *g) {
 pkv_status q4_rows(pkv_q4_cache *c, const char *what, int32_t n_seqs, const int32_t *table, int32_t max_pages,
                    const int32_t *lengths, int64_t n_rows, const int32_t *offsets, Q4Rows *r) {
     if (n_seqs < 1 || n_seqs > 65535) return q4_fail(c, PKV_ERR_INVALID_ARG, "%s: n_seqs %d out of range", what, n_seqs);
-    if (max_pages < 1 || max_pages > (0x7fffffff >> c->geo.page_shift))
+    if (max_pages < 1 || max_pages > ((1 << 30) >> c->geo.page_shift))
         return q4_fail(c, PKV_ERR_INVALID_ARG, "%s: max_pages %d out of range", what, max_pages);
     if (n_rows < 0 || n_rows > 0x7fffffff / (2 * c->geo.n_q_heads))
         return q4_fail(c, PKV_ERR_INVALID_ARG, "%s: n_rows %lld out of range", what, (long long)n_rows);

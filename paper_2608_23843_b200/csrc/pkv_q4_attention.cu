@@ -744,9 +744,10 @@ __global__ void __launch_bounds__(Q4Shape<D, NG, NT>::kThreads, 2) q4_decode_ker
 
 // Joins the states of the segments (tiles of R rows) that span CTAs, in token order: blocks (b, y) take the rows of the
 // segment that begins in CTA b.  A chain of loads over the parts would cost a trip to L2 each (37 parts of a 128K sequence:
-// 41 us), so the parts of a row are shared by four warps; a row block's rows, many of few parts, get a warp each.
+// 41 us), so the parts of a row are shared by four warps (kRows = 1); of a row block's rows, many of few parts, a warp takes
+// four at once, eight lanes each (a warp per row: 13 us instead of 7 for 148 parts of 256 rows).
 constexpr int kQ4JoinWarps = 4;
-template <int D, bool H16, int W>
+template <int D, bool H16, int kRows>
 __global__ void __launch_bounds__(32 * kQ4JoinWarps) q4_join_kernel(const __grid_constant__ Q4AttentionArgs a, int R) {
     asm volatile("griddepcontrol.wait;" ::: "memory");
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
@@ -754,37 +755,45 @@ __global__ void __launch_bounds__(32 * kQ4JoinWarps) q4_join_kernel(const __grid
     const int b = blockIdx.x;
     const Q4Part p = reinterpret_cast<const Q4Part *>(a.workspace)[b];
     if (p.seq < 0) return;
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const int r = W == 1 ? (int)blockIdx.y * kQ4JoinWarps + warp : (int)blockIdx.y;      // W warps per row
+    constexpr int W = kRows == 1 ? kQ4JoinWarps : 1;           // warps that share a row
+    constexpr int LR = 32 / kRows, C = D / LR;                 // lanes and channels per lane of a row, the latter in groups of four (two)
+    constexpr int V = C < 4 ? C : 4, NV = C / V;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, l = lane % LR;
+    const int r = kRows == 1 ? (int)blockIdx.y : ((int)blockIdx.y * kQ4JoinWarps + warp) * kRows + lane / LR;
     int first, all;
     const int n = q4_new_rows(a, p.seq, first, all, nullptr), G = geo.group;
     const long long row = (long long)p.tile * R + r;
     const int j = (int)(row / G);
-    if (j >= n) return;
+    if (W > 1 && j >= n) return;                               // (the same for the whole CTA)
+    const bool in = j < n;
     const float *states = reinterpret_cast<const float *>(a.workspace + q4_parts_bytes(gridDim.x));
     const long long per = q4_state_floats(R, D);
     // the first part is in slot p.slot of CTA b, the others in slot 0 of the CTAs behind it
     auto state = [&](int k) { return states + (2LL * k + (k == b ? p.slot : 0)) * per; };
-    // a warp's parts in one pass, four at a time: the weights are not waited for before o is asked for
-    constexpr int C = D / 32, kAhead = 4;
+    // the parts in one pass, some at a time: the weights are not waited for before o is asked for
+    constexpr int kAhead = kRows == 1 ? 4 : 2;
     float M = kNegInf, L = 0.f, acc[C];
 #pragma unroll
     for (int i = 0; i < C; ++i) acc[i] = 0.f;
     for (int k0 = b + (W == 1 ? 0 : warp); k0 <= p.last_cta; k0 += W * kAhead) {
-        float m[kAhead], l[kAhead], x[kAhead][C], top = M;
+        float m[kAhead], s1[kAhead], x[kAhead][C], top = M;
 #pragma unroll
         for (int i = 0; i < kAhead; ++i) {
             const int k = k0 + i * W;
             m[i] = kNegInf;
-            l[i] = 0.f;
+            s1[i] = 0.f;
 #pragma unroll
             for (int c = 0; c < C; ++c) x[i][c] = 0.f;
-            if (k <= p.last_cta) {
+            if (in && k <= p.last_cta) {
                 const float *s = state(k);
                 m[i] = s[R * D + r];
-                l[i] = s[R * D + R + r];
+                s1[i] = s[R * D + R + r];
 #pragma unroll
-                for (int c = 0; c < C; c += 2) { const float2 v = *reinterpret_cast<const float2 *>(s + r * D + C * lane + c); x[i][c] = v.x; x[i][c + 1] = v.y; }
+                for (int c = 0; c < NV; ++c) {
+                    const float *src = s + r * D + (c * LR + l) * V;
+                    if (V == 4) { const float4 v = *reinterpret_cast<const float4 *>(src); x[i][4 * c] = v.x; x[i][4 * c + 1] = v.y; x[i][4 * c + V - 2] = v.z; x[i][4 * c + V - 1] = v.w; }
+                    else { const float2 v = *reinterpret_cast<const float2 *>(src); x[i][2 * c] = v.x; x[i][2 * c + 1] = v.y; }
+                }
             }
         }
 #pragma unroll
@@ -797,7 +806,7 @@ __global__ void __launch_bounds__(32 * kQ4JoinWarps) q4_join_kernel(const __grid
 #pragma unroll
         for (int i = 0; i < kAhead; ++i) {
             const float w = ex2(m[i] - M);
-            L += w * l[i];
+            L += w * s1[i];
 #pragma unroll
             for (int c = 0; c < C; ++c) acc[c] += w * x[i][c];
         }
@@ -822,18 +831,24 @@ __global__ void __launch_bounds__(32 * kQ4JoinWarps) q4_join_kernel(const __grid
             L += f * part[w][D];
         }
     }
+    if (!in) return;
     const int h = p.head * G + (int)(row - (long long)j * G);
     if (a.state) {
         float *dst = a.state + ((long long)(first + j) * geo.n_q_heads + h) * (D + 2);
 #pragma unroll
-        for (int i = 0; i < C; i += 2) *reinterpret_cast<float2 *>(dst + C * lane + i) = make_float2(acc[i], acc[i + 1]);
-        if (lane == 0) *reinterpret_cast<float2 *>(dst + D) = make_float2(M, L);
+        for (int c = 0; c < NV; ++c)
+#pragma unroll
+            for (int i = 0; i < V; i += 2) *reinterpret_cast<float2 *>(dst + (c * LR + l) * V + i) = make_float2(acc[V * c + i], acc[V * c + i + 1]);
+        if (l == 0) *reinterpret_cast<float2 *>(dst + D) = make_float2(M, L);
     } else {
         const float inv = L != 0.f ? 1.f / L : 0.f;
-        uint32_t *dst = reinterpret_cast<uint32_t *>(reinterpret_cast<unsigned short *>(a.out) + (long long)(first + j) * a.out_row +
-                                                     (long long)h * a.out_head + C * lane);
+        unsigned short *dst = reinterpret_cast<unsigned short *>(a.out) + (long long)(first + j) * a.out_row + (long long)h * a.out_head;
 #pragma unroll
-        for (int i = 0; i < C; i += 2) dst[i / 2] = H16 ? pack_f16(acc[i] * inv, acc[i + 1] * inv) : pack_bf16(acc[i] * inv, acc[i + 1] * inv);
+        for (int c = 0; c < NV; ++c)
+#pragma unroll
+            for (int i = 0; i < V; i += 2)
+                *reinterpret_cast<uint32_t *>(dst + (c * LR + l) * V + i) =
+                    H16 ? pack_f16(acc[V * c + i] * inv, acc[V * c + i + 1] * inv) : pack_bf16(acc[V * c + i] * inv, acc[V * c + i + 1] * inv);
     }
 }
 
@@ -906,12 +921,12 @@ cudaError_t launch_q4_attention(Q4AttentionArgs a, cudaStream_t st) {
         PKV_Q4_SHAPES(PKV_Q4_LAUNCH)
     }
     if (e != cudaSuccess || n <= 1 || a.whole) return e;
-    cfg.gridDim = dim3(n, blocks ? R / kQ4JoinWarps : R);
+    cfg.gridDim = dim3(n, blocks ? R / (4 * kQ4JoinWarps) : R);
     cfg.blockDim = dim3(32 * kQ4JoinWarps);
     cfg.dynamicSmemBytes = 0;
 #define PKV_Q4_JOIN(D, H)                                                                                         \
     if (g.head_dim == D && (g.fp16 != 0) == H)                                                                    \
-        return blocks ? cudaLaunchKernelEx(&cfg, q4_join_kernel<D, H, 1>, a, R) : cudaLaunchKernelEx(&cfg, q4_join_kernel<D, H, kQ4JoinWarps>, a, R);
+        return blocks ? cudaLaunchKernelEx(&cfg, q4_join_kernel<D, H, 4>, a, R) : cudaLaunchKernelEx(&cfg, q4_join_kernel<D, H, 1>, a, R);
     PKV_Q4_JOIN(128, false) PKV_Q4_JOIN(128, true) PKV_Q4_JOIN(64, false) PKV_Q4_JOIN(64, true)
     return cudaErrorInvalidValue;
 }

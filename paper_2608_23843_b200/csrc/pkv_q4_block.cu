@@ -81,21 +81,46 @@ __device__ __forceinline__ int block_units(const BlockSeq &q, int r) {
     const int see = q.all > q.T ? q.T : q.T - q.all + last + 1;          // (more rows than tokens: not worth a rule of its own)
     return max(1, (see + kQ4Unit - 1) / kQ4Unit);
 }
-// units of the blocks before r (the last block may end before its rows do, so r is at most the number of blocks minus one
-// in the closed form: block i's last row is (i + 1) * 256 - 1, its units floor((T - all + 1 + floor((256 i + 255) / G) + 63) / 64))
-__device__ long long block_units_before(const BlockSeq &q, int r) {
-    if (r == 0) return 0;
-    if (q.all > q.T) return (long long)r * block_units(q, 0);
-    if (r <= 8) {                                   // (few: adding them up beats the recursion's divisions)
-        long long few = 0;
-        for (int i = 0; i < r; ++i) few += block_units(q, i);
-        return few;
+// What a block costs a CTA beside its units - queries, results, the first unit's latency - in units.
+constexpr int kBSegCost = 5;
+// Units and fixed costs of all blocks of a sequence, for one head.  (The last block may end before its 256 rows do; the others
+// have a closed form: block i's last row is 256 i + 255, its units floor((T - all + 1 + floor((256 i + 255) / G) + 63) / 64).)
+__device__ long long block_weight(const BlockSeq &q) {
+    if (q.blocks == 0) return 0;
+    const long long fixed = (long long)q.blocks * kBSegCost;
+    if (q.all > q.T) return fixed + (long long)q.blocks * block_units(q, 0);
+    long long sum = fixed + block_units(q, q.blocks - 1);
+    if (q.blocks <= 8) {                            // (few: adding them up beats the recursion's divisions)
+        for (int i = 0; i < q.blocks - 1; ++i) sum += block_units(q, i);
+        return sum;
     }
-    const int full = min(r, q.blocks - 1);
     const long long A = (long long)q.T - q.all + 1 + kQ4Unit - 1;
-    long long sum = floor_sum(full, (long long)kQ4Unit * q.G, kBRows, kBRows - 1 + A * q.G);
-    if (r > full) sum += block_units(q, q.blocks - 1);
-    return sum;
+    return sum + floor_sum(q.blocks - 1, (long long)kQ4Unit * q.G, kBRows, kBRows - 1 + A * q.G);
+}
+// The block that holds position `at` of a sequence's weights (blocks in turn, all heads of one before the next), and the
+// position where it begins; a whole warp, 32 blocks at a time.
+__device__ int block_locate(const BlockSeq &q, int H, long long at, long long &begins) {
+    const int lane = threadIdx.x & 31;
+    long long base = 0;
+    for (int r0 = 0;; r0 += 32) {
+        const int r = r0 + lane;
+        const int v = r < q.blocks ? block_units(q, r) + kBSegCost : 0;
+        int x = v;                                  // (at most 32 * 2^25)
+#pragma unroll
+        for (int d = 1; d < 32; d <<= 1) {
+            const int y = __shfl_up_sync(0xffffffffu, x, d);
+            if (lane >= d) x += y;
+        }
+        const uint32_t before = __ballot_sync(0xffffffffu, base + (long long)x * H <= at);      // blocks that end before `at`
+        const int k = __popc(before);
+        const long long all = base + (long long)__shfl_sync(0xffffffffu, x, 31) * H;
+        if (k < 32 || r0 + 32 >= q.blocks) {
+            const int kk = min(k, min(31, q.blocks - 1 - r0));
+            begins = base + (long long)(__shfl_sync(0xffffffffu, x, kk) - __shfl_sync(0xffffffffu, v, kk)) * H;
+            return r0 + kk;
+        }
+        base = all;
+    }
 }
 
 // A place in the batch's order of units: sequence, block, head, unit.
@@ -198,11 +223,12 @@ __global__ void __launch_bounds__(kBThreads, 1) q4_block_kernel(const __grid_con
     int *status = blockIdx.x == 0 ? a.status : nullptr;
     auto weight = [&](int s, int *st) -> long long {
         if (s >= n_seqs) return 0;
-        const BlockSeq q = block_seq(a, s, st);
-        return block_units_before(q, q.blocks) * H;
+        return block_weight(block_seq(a, s, st)) * H;
     };
     long long total = 0;
-    {
+    if (n_seqs == 1) {
+        total = weight(0, tid == 0 ? status : nullptr);
+    } else {
         long long mine = 0;
         for (int s = tid; s < n_seqs; s += kBThreads) mine += weight(s, status);
 #pragma unroll
@@ -212,7 +238,7 @@ __global__ void __launch_bounds__(kBThreads, 1) q4_block_kernel(const __grid_con
 #pragma unroll
         for (int w = 0; w < kBThreads / 32; ++w) total += sums[w];
     }
-    const int n_ctas = (int)min((long long)gridDim.x, max(1LL, total / 4));
+    const int n_ctas = (int)min((long long)gridDim.x, max(1LL, total / (4 + kBSegCost)));
     const long long begin = total * blockIdx.x / n_ctas, end = total * (blockIdx.x + 1) / n_ctas;
     Q4Part *parts = reinterpret_cast<Q4Part *>(a.workspace);
     float *states = reinterpret_cast<float *>(a.workspace + q4_parts_bytes(gridDim.x));
@@ -220,7 +246,11 @@ __global__ void __launch_bounds__(kBThreads, 1) q4_block_kernel(const __grid_con
         if (tid == 0 && gridDim.x > 1) parts[blockIdx.x].seq = -1;
         return;
     }
-    {
+    BlockCursor seg;
+    long long at0 = begin;                                     // `begin` within its sequence
+    if (n_seqs == 1) {
+        seg.seq = 0;
+    } else {
         long long base = 0;
         for (int s0 = 0; s0 < n_seqs; s0 += kBThreads) {
             const long long v = weight(s0 + tid, nullptr);
@@ -244,6 +274,41 @@ __global__ void __launch_bounds__(kBThreads, 1) q4_block_kernel(const __grid_con
             base += all;
             if (base > begin) break;
         }
+        __syncthreads();
+        seg.seq = found_seq;
+        at0 = found_at;
+    }
+    seg.q = block_seq(a, seg.seq, nullptr);
+    long long seg_pos;                                         // where the current block begins, on the scale of the weights
+    {
+        long long b0;
+        seg.block = block_locate(seg.q, H, at0, b0);
+        seg.units = block_units(seg.q, seg.block);
+        const int len = seg.units + kBSegCost;
+        seg.head = (int)((at0 - b0) / len);
+        const int off = (int)(at0 - b0 - (long long)seg.head * len);
+        seg.unit = min(off, seg.units);
+        seg_pos = begin - off;
+        if (seg.unit == seg.units) {                           // the share begins behind a block's units
+            seg_pos += len;
+            block_advance(a, seg, 0);
+        }
+    }
+    int left = 0;                                              // units of the CTA
+    {
+        BlockCursor w = seg;
+        long long pos = seg_pos;
+        while (w.seq < n_seqs && pos + w.unit < end) {
+            const int here = (int)min((long long)(w.units - w.unit), end - pos - w.unit);
+            left += here;
+            if (here < w.units - w.unit) break;
+            pos += w.units + kBSegCost;
+            block_advance(a, w, w.units - w.unit);
+        }
+    }
+    if (left == 0) {
+        if (tid == 0 && gridDim.x > 1) parts[blockIdx.x].seq = -1;
+        return;
     }
     if (warp == 0) {
         asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&tmem_slot)), "r"(kBTmemCols) : "memory");
@@ -253,24 +318,6 @@ __global__ void __launch_bounds__(kBThreads, 1) q4_block_kernel(const __grid_con
     __syncthreads();
     tc_fence_after();
     const uint32_t tm = tmem_slot;
-    BlockCursor seg;
-    seg.seq = found_seq;
-    seg.q = block_seq(a, seg.seq, nullptr);
-    {
-        // the block that holds unit `found_at`: the last one with no more units (of all heads) before it
-        int lo = 0, hi = seg.q.blocks;
-        while (hi - lo > 1) {
-            const int mid = (lo + hi) >> 1;
-            if (block_units_before(seg.q, mid) * H <= found_at) lo = mid;
-            else hi = mid;
-        }
-        seg.block = lo;
-        seg.units = block_units(seg.q, lo);
-        const long long in = found_at - block_units_before(seg.q, lo) * H;
-        seg.head = (int)(in / seg.units);
-        seg.unit = (int)(in - (long long)seg.head * seg.units);
-    }
-    const int left = (int)(end - begin);                       // units of the CTA
     const long long limit = kWaitClocks;
 
     if (warp == kBCopyWarp) {
@@ -690,10 +737,16 @@ __global__ void __launch_bounds__(kBThreads, 1) q4_block_kernel(const __grid_con
 #pragma unroll
                         for (int k = 0; k < 32; ++k) r[k] = __float_as_uint(fmaf(__uint_as_float(r1[k]), f1, __uint_as_float(r[k])));
                     }
-                    if (dst) {
+                    if (!complete) {                           // (16-byte aligned, unlike a row of the caller's states)
+#pragma unroll
+                        for (int k = 0; k < 8; ++k)
+                            *reinterpret_cast<uint4 *>(dst + 32 * b + 4 * k) =
+                                make_uint4(r[(4 * k & ~7) + kVOrder[4 * k & 7]], r[(4 * k & ~7) + kVOrder[(4 * k + 1) & 7]],
+                                           r[(4 * k & ~7) + kVOrder[(4 * k + 2) & 7]], r[(4 * k & ~7) + kVOrder[(4 * k + 3) & 7]]);
+                    } else if (dst) {
 #pragma unroll
                         for (int k = 0; k < 16; ++k) *reinterpret_cast<uint2 *>(dst + 32 * b + 2 * k) = make_uint2(r[(2 * k & ~7) + kVOrder[2 * k & 7]], r[(2 * k & ~7) + kVOrder[(2 * k + 1) & 7]]);
-                    } else if (complete && row_ok) {
+                    } else if (row_ok) {
 #pragma unroll
                         for (int k = 0; k < 4; ++k) {
                             uint32_t w[4];
@@ -720,11 +773,12 @@ __global__ void __launch_bounds__(kBThreads, 1) q4_block_kernel(const __grid_con
             if (tid == 0 && gridDim.x > 1 && u == left) {
                 Q4Part p{-1, 0, 0, 0, 0};
                 if (c.unit == 0 && n_units < c.units) {
-                    const long long w1 = begin + u - n_units + c.units;      // one past the block's last unit
-                    p = Q4Part{c.seq, c.block, c.head, u == n_units ? 0 : 1, (int)((w1 * n_ctas - 1) / total)};
+                    // the CTA whose share holds the block's last unit
+                    p = Q4Part{c.seq, c.block, c.head, u == n_units ? 0 : 1, (int)(((seg_pos + c.units) * n_ctas - 1) / total)};
                 }
                 parts[blockIdx.x] = p;
             }
+            seg_pos += c.units + kBSegCost;
             if (u < left) block_advance(a, c, n_units);
         }
         if (!ok && lane == 0 && !*abort_flag) { *abort_flag = 1; atomicAdd(a.status, 1); }
@@ -752,7 +806,7 @@ cudaError_t q4_block_setup() {
 // CTAs: one per SM, four units each at least, as far as the host can tell.
 int q4_block_grid(const Q4Geometry &g, int n_seqs, int max_q_len, int max_len) {
     const double blocks = (double)(((long long)max_q_len * g.group + kBRows - 1) / kBRows), units = (max_len + kQ4Unit - 1) / kQ4Unit;
-    const double all = (double)n_seqs * g.n_kv_heads * blocks * units / 4;
+    const double all = (double)n_seqs * g.n_kv_heads * blocks * (units + kBSegCost) / (4 + kBSegCost);
     return all >= g.n_sms ? g.n_sms : all < 1 ? 1 : (int)all;
 }
 
