@@ -384,11 +384,14 @@ pkv_status q4_device(pkv_q4_cache *c, const char *what) {
     return PKV_OK;
 }
 
-// strides of a [rows, heads, d] buffer in elements: rows and heads on 16-byte boundaries, heads apart from one another
+// strides of a [rows, heads, d] buffer in elements: rows and heads on 16-byte boundaries, none on top of another
 bool q4_strides(const void *p, int64_t row, int64_t head, int d, int heads, int64_t n_rows) {
     if (((uintptr_t)p & 15) || row % 8 || head % 8 || row < 0 || head < 0) return false;
     if (row > (1LL << 31) || head > (1LL << 31)) return false;
-    return (heads == 1 || head >= d) && (n_rows <= 1 || row >= d);
+    if (heads == 1) return n_rows <= 1 || row >= d;
+    if (n_rows <= 1) return head >= d;
+    // rows of all heads one after the other, or the other way round
+    return (head >= d && row >= (heads - 1) * head + d) || (row >= d && head >= (n_rows - 1) * row + d);
 }
 
 pkv_status q4_copy(pkv_q4_cache *c, bool write, int32_t n_seqs, const int32_t *table, int32_t max_pages, const int32_t *lengths,
@@ -401,8 +404,8 @@ pkv_status q4_copy(pkv_q4_cache *c, bool write, int32_t n_seqs, const int32_t *t
     const Q4Geometry &g = c->geo;
     if (!c->dry && n_rows > 0 && (!k || !v)) return q4_fail(c, PKV_ERR_INVALID_ARG, "%s: k or v is NULL", what);
     if (!q4_strides(k, k_row, k_head, g.head_dim, g.n_kv_heads, n_rows) || !q4_strides(v, v_row, v_head, g.head_dim, g.n_kv_heads, n_rows))
-        return q4_fail(c, PKV_ERR_INVALID_ARG, "%s: k and v need 16-byte aligned rows: strides that are multiples of 8 elements, rows and "
-                                               "heads at least head_dim apart", what);
+        return q4_fail(c, PKV_ERR_INVALID_ARG, "%s: k and v need 16-byte aligned rows: strides that are multiples of 8 elements, no row or "
+                                               "head on top of another", what);
     if (c->dry || n_rows == 0) return PKV_OK;
     if (pkv_status st = q4_device(c, what)) return st;
     a.geo = g;
@@ -503,8 +506,8 @@ pkv_status pkv_q4_attention(pkv_q4_cache *c, int32_t n_seqs, const int32_t *page
         return q4_fail(c, PKV_ERR_INVALID_ARG, "%s: q is NULL, or not exactly one of out and state is given", what);
     if (!q4_strides(q, q_row_stride, q_head_stride, g.head_dim, g.n_q_heads, n_rows) ||
         (out && !q4_strides(out, out_row_stride, out_head_stride, g.head_dim, g.n_q_heads, n_rows)))
-        return q4_fail(c, PKV_ERR_INVALID_ARG, "%s: q and out need 16-byte aligned rows: strides that are multiples of 8 elements, rows and "
-                                               "heads at least head_dim apart", what);
+        return q4_fail(c, PKV_ERR_INVALID_ARG, "%s: q and out need 16-byte aligned rows: strides that are multiples of 8 elements, no row or "
+                                               "head on top of another", what);
     if ((uintptr_t)state & 7) return q4_fail(c, PKV_ERR_INVALID_ARG, "%s: state must be 8-byte aligned", what);
     if (n_rows == 0 || max_q_len == 0) return PKV_OK;
     const long long need = q4_attention_workspace(g, n_seqs, max_q_len, max_len);

@@ -41,8 +41,8 @@ def offsets_of(ns, start=0):
 
 
 def attention(q, K, V, first_position, scale, out_type):
-    """One sequence: q [n, H_q, d] (any type), K and V [T, H, d] fp64 as the cache stands for them.  Query j sees positions
-    up to first_position + j.  -> (out fp64 [n, H_q, d], lse in base 2 [n, H_q], tolerance per element).
+    """One sequence: q [n, H_q, d] (any type), K and V [T, H, d] fp64 as the cache stands for them (finite where a query that is
+    compared sees them).  Query j sees positions up to first_position + j.  -> (out fp64 [n, H_q, d], lse in base 2 [n, H_q], tolerance per element).
 
     The tolerance bounds what a kernel does that is exact but for these roundings (A = sum of weight * |v| per channel):
       the result to its type                                  eps / 2 * |out|, at least half its smallest step
@@ -65,19 +65,27 @@ def attention(q, K, V, first_position, scale, out_type):
     out = torch.zeros(n, hq, d, dtype=torch.float64)
     tol = torch.zeros_like(out)
     lse = torch.full((n, hq), -math.inf, dtype=torch.float64)
+    see = first_position + torch.arange(1, n + 1)                  # tokens that query j sees
+    any_seen = see > 0
+    hidden = torch.arange(T)[None] >= see[:, None]
+    seen = torch.where(hidden, 0.0, 1.0)
     for h in range(hq):
         k, v = K[:, h // (hq // hk)], V[:, h // (hq // hk)]
-        for j in range(n):
-            see = first_position + j + 1
-            if see <= 0:
-                continue
-            s = (k[:see] @ q[j, h]) * scale * math.log2(math.e)
-            m = s.max()
-            w = torch.exp2(s - m)
-            l = w.sum()
-            lse[j, h] = m + torch.log2(l)
-            out[j, h] = (w @ v[:see]) / l
-            A = (w @ v[:see].abs()) / l
-            ds = 2.0 ** -23 * (d + 8) * 4 * q[j, h].abs().sum() * k[:see].abs().max() * scale * math.log2(math.e)
-            tol[j, h] = info.eps / 2 * out[j, h].abs().clamp(min=info.smallest_normal) + (2.0 ** -11 + 2.0 ** -19 + 2 * ds) * A + (2.0 ** -25 * see / l + 17 * 2.0 ** -23 * -(-see // 16)) * v[:see].abs().max()
+        s = ((q[:, h] @ k.T) * scale * math.log2(math.e)).masked_fill(hidden, -math.inf)
+        m = torch.where(any_seen, s.amax(-1) if T else torch.zeros(n, dtype=torch.float64), 0.0)
+        w = torch.exp2(s - m[:, None])
+        l = w.sum(-1)
+        some = l > 0
+        l1 = torch.where(some, l, 1.0)
+        lse[:, h] = torch.where(some, m + torch.log2(l1), -math.inf)
+        out[:, h] = (w @ v.nan_to_num()) / l1[:, None]
+        A = (w @ v.nan_to_num().abs()) / l1[:, None]
+        # the largest key and value that each query sees
+        kmax = (seen * k.nan_to_num().abs().amax(-1)).amax(-1) if T else torch.zeros(n, dtype=torch.float64)
+        vmax = (seen * v.nan_to_num().abs().amax(-1)).amax(-1) if T else torch.zeros(n, dtype=torch.float64)
+        ds = 2.0 ** -23 * (d + 8) * 4 * q[:, h].abs().sum(-1) * kmax * scale * math.log2(math.e)
+        steps = (see.clamp(min=0) + 15) // 16
+        tol[:, h] = (info.eps / 2 * out[:, h].abs().clamp(min=info.smallest_normal) + (2.0 ** -11 + 2.0 ** -19 + 2 * ds[:, None]) * A
+                     + ((2.0 ** -25 * see / l1 + 17 * 2.0 ** -23 * steps) * vmax)[:, None])
+        tol[~any_seen, h] = 0.0
     return out, lse, tol

@@ -65,6 +65,7 @@ def test_calls_that_are_accepted_in_a_dry_run():
     assert cache.attention_partial(table, lengths, q).shape == (3, 2, 8, 130)
     cache.append_kv(table, lengths, k[:, :0], k[:, :0])                       # no rows
     cache.attention(table, lengths, q[:, :0])
+    cache.append_kv(table, lengths, torch.zeros(2, 3, 2, 128, dtype=BF16).permute(1, 2, 0, 3), k)      # heads first
     cache.append_kv(table, lengths, k[..., :1, :].expand(3, 2, 2, 128).contiguous(), k)
     assert cache.stats() == {"device_timeouts": 0, "bad_pages": 0, "bad_lengths": 0}
 
@@ -90,6 +91,7 @@ def test_calls_that_are_accepted_in_a_dry_run():
     lambda c, t, n, k, q: c.append_kv(t, n, torch.zeros(3 * 2 * 2 * 128 + 8, dtype=BF16)[1:-7].view(3, 2, 2, 128), k),
     lambda c, t, n, k, q: c.append_kv(t, n, k[:, :, :1].expand(3, 2, 2, 128), k),       # heads on top of one another
     lambda c, t, n, k, q: c.append_kv(t, n, k[:1, :1].expand(3, 2, 2, 128), k),         # rows on top of one another
+    lambda c, t, n, k, q: c.append_kv(t, n, torch.zeros(2000, dtype=BF16).as_strided((3, 2, 2, 128), (256, 128, 128, 1)), k),      # head 1 on row 1
     lambda c, t, n, k, q: c.read_kv(t, n, k, k.half()),
     lambda c, t, n, k, q: c.attention(t, n, k),
     lambda c, t, n, k, q: c.attention(t, n, q.half()),
@@ -474,6 +476,55 @@ def test_pages_and_lengths_that_make_no_sense(n, G):
     bad = f.cache.stats()["bad_lengths"]
     f.cache.attention(f.table, torch.tensor([1 << 30, 90], **INTS).cuda(), q)      # as if 160 (5 pages of 32)
     assert f.cache.stats()["bad_lengths"] > bad
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("G", [33, 64])
+def test_many_query_heads_per_kv_head(G):
+    f = Filled([1, 70, 333], G=G, H=2, seed=24)
+    run_uniform(f, 1)
+    run_uniform(Filled([9, 200], G=G, H=1, seed=25), 9)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("n, most", [(1, 40), (1, 3000), (9, 40)])
+def test_more_sequences_than_a_cta_has_threads(n, most):
+    """900 sequences, empty ones among them; `most` is the length the call is told to expect."""
+    gen = torch.Generator().manual_seed(n)
+    lens = [0 if i % 7 == 0 else max(n, int(t)) for i, t in enumerate(torch.randint(1, 41, (900,), generator=gen))]
+    f = Filled(lens, G=2, H=1, P=16, seed=26)
+    qs = f.queries([n] * 900)
+    out = f.cache.attention(f.table, f.lengths, torch.stack(qs).cuda(), max_len=most).cpu()
+    for s, q in enumerate(qs):
+        check(out[s], *f.expected(q, s)[::2])
+    f.clean()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype, d, g, G, lens", [(BF16, 128, 32, 4, [1200]), (FP16, 64, 64, 7, [700, 10, 390]), (BF16, 128, 128, 1, [2600, 300])])
+def test_whole_prompts(dtype, d, g, G, lens):
+    """Every position of the prompts is a query: blocks of very different lengths, more than a warp looks up at once."""
+    f = Filled(lens, dtype=dtype, d=d, g=g, G=G, H=1, P=32, seed=27)
+    qs = f.queries(lens)
+    out = f.cache.attention(f.table, f.lengths, torch.cat(qs).cuda(), offsets=f.off, max_q_len=max(lens)).cpu()
+    at = 0
+    for s, q in enumerate(qs):
+        check(out[at:at + lens[s]], *f.expected(q, s)[::2])
+        at += lens[s]
+    f.clean()
+
+
+@pytest.mark.gpu
+def test_a_long_prompt_in_more_blocks_than_a_warp_looks_up_at_once():
+    n, G = 2200, 8                                         # 69 blocks of 256 rows
+    f = Filled([n], G=G, H=1, P=64, seed=28)
+    q = f.queries([n])[0]
+    out = f.cache.attention(f.table, f.lengths, q[None].cuda())[0].cpu()
+    rows = torch.tensor([0, 1, 31, 32, 33, 63, 64, 1000, 1023, 1024, 1025, 2111, 2112, 2198, 2199])
+    for j in rows.tolist():
+        ref, _, tol = attention(q[j:j + 1], f.K[0][:j + 1], f.V[0][:j + 1], j, 1 / math.sqrt(128), BF16)
+        check(out[j:j + 1], ref, tol)
+    f.clean()
 
 
 @pytest.mark.gpu
