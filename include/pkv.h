@@ -535,7 +535,7 @@ typedef struct pkv_q4_config {
     int32_t dtype;              /* of k, v, q and out: PKV_DTYPE_BF16 or PKV_DTYPE_FP16 */
     int64_t n_pages;            /* pages in the pool */
     float   softmax_scale;      /* 0 => 1/sqrt(head_dim) */
-    int32_t n_ctas;             /* most CTAs an attention over few query rows is spread over; 0 => two per SM */
+    int32_t n_ctas;             /* most CTAs an attention over up to 8 query rows per KV head is spread over (up to 16 rows: half as many); 0 => two per SM */
 } pkv_q4_config;
 
 typedef struct pkv_q4_sizes {

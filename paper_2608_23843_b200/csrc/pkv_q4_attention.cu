@@ -28,24 +28,28 @@ namespace pkv {
 
 namespace {
 
-constexpr int kQ4Step = 2;             // tiles per softmax step
 // What a segment costs a CTA beside its units - queries, joining the warps' states - in units: a CTA of many short segments
-// takes no longer than one of few long ones (32 sequences of 512 to 16384 tokens: 47 -> see the table of measurements).
-constexpr int kQ4SegCost = 6;
-// Warps of a CTA (two CTAs per SM), the last one for the copies: the kernel is bound by instruction issue, so as many warps as
-// their registers allow - one column of query rows in 128 registers a thread, two in 168.
-__host__ __device__ constexpr int q4_warps(int nt) { return nt == 1 ? 8 : 6; }
+// takes no longer than one of few long ones (32 sequences of 512 to 16384 tokens: 47.7 -> 42.6 us; 16 rows against 8 x 32K:
+// 103.5 -> 101.8 us).
+__host__ __device__ constexpr int q4_seg_cost(int nt) { return nt == 1 ? 6 : 12; }
+// Warps of a CTA, the last one for the copies: the kernel is bound by instruction issue and latency, so as many warps as their
+// registers allow - of one column of query rows, in 128 registers a thread, two CTAs of eight per SM (one CTA of sixteen, which
+// idles while it joins its warps' states: 87 us instead of 69 for 8 x 32K); of two columns, in 168 registers, one CTA of
+// twelve (two of six, with one consumer fewer and twice the segments: 115 us instead of 103).
+__host__ __device__ constexpr int q4_warps(int nt) { return nt == 1 ? 8 : 12; }
+__host__ __device__ constexpr int q4_ctas_per_sm(int nt) { return nt == 1 ? 2 : 1; }
 
 template <int D, int NG, int NT>
 struct Q4Shape {
-    static constexpr int kWarps = q4_warps(NT), kCons = kWarps - 1, kThreads = 32 * kWarps;
+    static constexpr int kWarps = q4_warps(NT), kCons = kWarps - 1, kThreads = 32 * kWarps, kPerSM = q4_ctas_per_sm(NT);
+    static constexpr int kStep = NT == 1 ? 2 : 1;                                   // tiles per softmax step (two of two columns would spill: 128 us instead of 115)
     static constexpr int kTile = kQ4Tile * (D + 4 * NG), kUnitBytes = kQ4UnitTiles * kTile;
     static constexpr int kRowFloats = D + 4;                                        // a row of o in shared memory, padded against bank conflicts
     static constexpr int kFlush = 8 * kRowFloats * 4;                               // a warp's o (eight rows at a time) at a segment's end: over the stage it has just read
     static constexpr int kStage = ((kUnitBytes > kFlush ? kUnitBytes : kFlush) + 127) / 128 * 128;
-    static constexpr int kFit = 110 * 1024 / kStage, kStages = kFit < 16 ? kFit : 16;
+    static constexpr int kFit = (227 * 1024 / kPerSM - 3584) / kStage, kStages = kFit < 32 / kPerSM ? kFit : 32 / kPerSM;
     static constexpr int kSmem = kStages * kStage;
-    static_assert(kStages > kCons && 2 * (kSmem + 3072) <= 227 * 1024, "two CTAs per SM, a stage per warp and some in flight");
+    static_assert(kStages > kCons && kPerSM * (kSmem + 3072) <= 227 * 1024, "a stage per warp and some in flight");
 };
 
 __device__ __forceinline__ void mma_f16(float *d, const uint32_t *a, uint32_t b0, uint32_t b1, const float *c) {
@@ -133,10 +137,10 @@ __device__ __forceinline__ void q4_advance(const Q4AttentionArgs &a, int rows_pe
 }
 
 template <int D, int NG, bool H16, int NT>
-__global__ void __launch_bounds__(Q4Shape<D, NG, NT>::kThreads, 2) q4_decode_kernel(const __grid_constant__ Q4AttentionArgs a) {
+__global__ void __launch_bounds__(Q4Shape<D, NG, NT>::kThreads, q4_ctas_per_sm(NT)) q4_decode_kernel(const __grid_constant__ Q4AttentionArgs a) {
     using S = Q4Shape<D, NG, NT>;
     constexpr int NW = D / 32, WPG = NW / NG, R = 8 * NT;      // 32-channel words per row, words per scale, query rows
-    constexpr int TS = kQ4Step, kSt = S::kStages, kQ4Warps = S::kWarps, kCons = S::kCons, kQ4Threads = S::kThreads;
+    constexpr int TS = S::kStep, kSt = S::kStages, kQ4Warps = S::kWarps, kCons = S::kCons, kQ4Threads = S::kThreads, kSegCost = q4_seg_cost(NT);
     const Q4Geometry &geo = a.geo;
     extern __shared__ __align__(128) unsigned char smem[];
     __shared__ unsigned long long full[kSt], empty[kSt];
@@ -160,7 +164,7 @@ __global__ void __launch_bounds__(Q4Shape<D, NG, NT>::kThreads, 2) q4_decode_ker
         if (s >= n_seqs) return 0;
         int first, all;
         const int n = q4_new_rows(a, s, first, all, st), T = q4_length(a.rows, geo, s, st);
-        return (long long)((n * geo.group + R - 1) / R) * H * (a.whole ? 1 : max(1, (T + kQ4Unit - 1) / kQ4Unit) + kQ4SegCost);
+        return (long long)((n * geo.group + R - 1) / R) * H * (a.whole ? 1 : max(1, (T + kQ4Unit - 1) / kQ4Unit) + kSegCost);
     };
     long long total = 0;
     if (n_seqs == 1) {
@@ -176,7 +180,7 @@ __global__ void __launch_bounds__(Q4Shape<D, NG, NT>::kThreads, 2) q4_decode_ker
         for (int w = 0; w < kQ4Warps; ++w) total += sums[w];
     }
     // (no more CTAs than there are units for a warp of each; the launch could only estimate that)
-    const int n_ctas = (int)min((long long)gridDim.x, max(1LL, a.whole ? total : total / (kCons + kQ4SegCost)));
+    const int n_ctas = (int)min((long long)gridDim.x, max(1LL, a.whole ? total : total / (kCons + kSegCost)));
     // (b * total / n without a 64-bit division where the total has 31 bits)
     auto share = [&](long long b) -> long long {
         if (total >> 31) return total * b / n_ctas;
@@ -238,7 +242,7 @@ __global__ void __launch_bounds__(Q4Shape<D, NG, NT>::kThreads, 2) q4_decode_ker
             left_cta += w.units;
         }
     } else {
-        const int len = seg.units + kQ4SegCost;
+        const int len = seg.units + kSegCost;
         const int idx = (int)(at0 / len), off = (int)(at0 - (long long)idx * len);      // (a sequence's segments number fewer than 2^31)
         seg.head = idx % H;
         seg.tile = idx / H;
@@ -255,7 +259,7 @@ __global__ void __launch_bounds__(Q4Shape<D, NG, NT>::kThreads, 2) q4_decode_ker
             const int here = (int)min((long long)(w.units - w.unit), end - pos - w.unit);
             left_cta += here;
             if (here < w.units - w.unit) break;
-            pos += w.units + kQ4SegCost;
+            pos += w.units + kSegCost;
             q4_advance(a, R, w, w.units - w.unit);
         }
         if (left_cta == 0) {
@@ -736,7 +740,7 @@ __global__ void __launch_bounds__(Q4Shape<D, NG, NT>::kThreads, 2) q4_decode_ker
         if (any && lane == 0) mbar_arrive(smem_u32(&empty[st_last]));
         seg_lo = seg_hi;
         if (seg_lo < left_cta) {
-            seg_pos += seg.units + kQ4SegCost;
+            seg_pos += seg.units + kSegCost;
             q4_advance(a, R, seg, seg.units - seg.unit);
         }
     }
@@ -866,7 +870,8 @@ int q4_grid(const Q4Geometry &g, int n_seqs, int max_q_len, int max_len) {
     const int R = q4_rows_per_tile(g, max_q_len);
     const long long tiles = ((long long)max_q_len * g.group + R - 1) / R, units = (max_len + kQ4Unit - 1) / kQ4Unit;
     const double segs = (double)n_seqs * g.n_kv_heads * tiles, all = q4_whole(max_len) ? segs : segs * units / (q4_warps(R / 8) - 1);
-    return all >= g.n_ctas ? g.n_ctas : all < 1 ? 1 : (int)all;
+    const int most = max(1, g.n_ctas * q4_ctas_per_sm(R / 8) / 2);
+    return all >= most ? most : all < 1 ? 1 : (int)all;
 }
 
 #define PKV_Q4_SHAPES(X) X(128, 4) X(128, 2) X(128, 1) X(64, 2) X(64, 1)
