@@ -856,21 +856,32 @@ __global__ void __launch_bounds__(32 * kQ4JoinWarps) q4_join_kernel(const __grid
     }
 }
 
-// Many query rows per KV head go to the row-block kernel (pkv_q4_block.cu).
-bool q4_by_blocks(const Q4Geometry &g, int max_q_len) { return (long long)max_q_len * g.group > 16; }
-
 int q4_rows_per_tile(const Q4Geometry &g, int max_q_len) { return (long long)max_q_len * g.group <= 8 ? 8 : 16; }
 
 // Sequences of up to 24 units (1536 tokens), as far as the host can tell: a segment stays in one CTA (at most four rounds of
 // its warps, 1.7 us each), which saves the second kernel (4 us).
 bool q4_whole(int max_len) { return (max_len + kQ4Unit - 1) / kQ4Unit <= 24; }
 
+// Segments of the column kernel, as far as the host can tell.
+double q4_segments(const Q4Geometry &g, int n_seqs, int max_q_len) {
+    const int R = q4_rows_per_tile(g, max_q_len);
+    return (double)n_seqs * g.n_kv_heads * (((long long)max_q_len * g.group + R - 1) / R);
+}
+
+// Many query rows per KV head go to the row-block kernel (pkv_q4_block.cu).  The column kernel reads a sequence once per sixteen
+// rows, the row-block kernel once per 256 but with a long chain of steps per unit: 8 sequences of 32K, 8 KV heads, column
+// against block, 16 rows 102 and 238 us, 24 and 32 rows 189 and 239, 48 rows 278 and 240; one of 128K, 32 rows 99 and 131.  Where
+// short sequences leave an SM no more than one segment, a segment's length is all that counts (four of 1000, 64 rows: 18
+// and 28 us; one of 1500, 256 rows: 20 and 35); with more, the blocks again (four of 1000, 148 rows: 45 and 36 us).
+bool q4_by_blocks(const Q4Geometry &g, int n_seqs, int max_q_len, int max_len) {
+    return (long long)max_q_len * g.group > 32 && !(q4_whole(max_len) && q4_segments(g, n_seqs, max_q_len) <= g.n_ctas / 2);
+}
+
 // CTAs of a launch: enough units for every warp of each, as far as the host can tell.
 int q4_grid(const Q4Geometry &g, int n_seqs, int max_q_len, int max_len) {
-    const int R = q4_rows_per_tile(g, max_q_len);
-    const long long tiles = ((long long)max_q_len * g.group + R - 1) / R, units = (max_len + kQ4Unit - 1) / kQ4Unit;
-    const double segs = (double)n_seqs * g.n_kv_heads * tiles, all = q4_whole(max_len) ? segs : segs * units / (q4_warps(R / 8) - 1);
-    const int most = max(1, g.n_ctas * q4_ctas_per_sm(R / 8) / 2);
+    const int nt = q4_rows_per_tile(g, max_q_len) / 8, most = max(1, g.n_ctas * q4_ctas_per_sm(nt) / 2);
+    const double segs = q4_segments(g, n_seqs, max_q_len), units = (max_len + kQ4Unit - 1) / kQ4Unit;
+    const double all = q4_whole(max_len) ? segs : segs * units / (q4_warps(nt) - 1);
     return all >= most ? most : all < 1 ? 1 : (int)all;
 }
 
@@ -889,14 +900,14 @@ cudaError_t q4_attention_setup() {
 }
 
 long long q4_attention_workspace(const Q4Geometry &g, int n_seqs, int max_q_len, int max_len) {
-    if (q4_by_blocks(g, max_q_len)) return q4_block_workspace(g, n_seqs, max_q_len, max_len);
+    if (q4_by_blocks(g, n_seqs, max_q_len, max_len)) return q4_block_workspace(g, n_seqs, max_q_len, max_len);
     const int n = q4_grid(g, n_seqs, max_q_len, max_len);
     return n <= 1 || q4_whole(max_len) ? 0 : q4_parts_bytes(n) + 2LL * n * q4_state_floats(q4_rows_per_tile(g, max_q_len), g.head_dim) * 4;
 }
 
 cudaError_t launch_q4_attention(Q4AttentionArgs a, cudaStream_t st) {
     const Q4Geometry &g = a.geo;
-    const bool blocks = q4_by_blocks(g, a.max_q_len);
+    const bool blocks = q4_by_blocks(g, a.rows.n_seqs, a.max_q_len, a.max_len);
     const int n = blocks ? q4_block_grid(g, a.rows.n_seqs, a.max_q_len, a.max_len) : q4_grid(g, a.rows.n_seqs, a.max_q_len, a.max_len);
     const int R = blocks ? kQ4BlockRows : q4_rows_per_tile(g, a.max_q_len);
     a.whole = !blocks && q4_whole(a.max_len);

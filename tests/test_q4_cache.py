@@ -146,11 +146,12 @@ def rows_of(gen, n, heads, d, dtype, spread=True):
 
 class Filled:
     """A cache on the GPU holding sequences of random rows, and what it stands for in 64 bits."""
+    room = 0                                               # tokens that the tables have place for, at least
 
     def __init__(self, lengths, dtype=BF16, d=128, g=32, P=64, H=2, G=4, seed=0, **kw):
         gen = torch.Generator().manual_seed(seed)
         self.gen, self.dtype, self.d, self.g, self.H, self.G, self.lens = gen, dtype, d, g, H, G, list(lengths)
-        self.rows = Rows(lengths, P, seed)
+        self.rows = Rows(lengths, P, seed, max_pages=max(-(-t // P) for t in [1, self.room, *lengths]))
         self.cache = pkv.Q4Cache(config(n_kv_heads=H, n_q_heads=H * G, head_dim=d, group_size=g, page_size=P, dtype=dtype,
                                         n_pages=self.rows.n_pages, **kw))
         self.cache.pool.fill_(0xff)                        # what no row was written to reads as NaN
@@ -307,12 +308,19 @@ def test_pages_beyond_four_gigabytes():
 
 
 # ---- GPU: attention ---------------------------------------------------------------------------------------------------
+@pytest.fixture(params=["no more pages than used", "room for more"])
+def room(request, monkeypatch):
+    """How long the sequences could be steers which kernel runs, how it is spread and whether states are joined."""
+    monkeypatch.setattr(Filled, "room", 3000 * (request.param == "room for more"))
+
+
 def run_uniform(f, n, **kw):
     qs = f.queries([n] * len(f.lens))
     out = f.cache.attention(f.table, f.lengths, torch.stack(qs).cuda(), **kw)
     return [check(out[s], *f.expected(q, s)[::2]) for s, q in enumerate(qs)]
 
 
+@pytest.mark.usefixtures("room")
 @pytest.mark.gpu
 @pytest.mark.parametrize("shape", SHAPES, ids=str)
 @pytest.mark.parametrize("G", [1, 4, 8, 7, 12])
@@ -322,6 +330,7 @@ def test_decode(shape, G):
     f.clean()
 
 
+@pytest.mark.usefixtures("room")
 @pytest.mark.gpu
 @pytest.mark.parametrize("shape", SHAPES, ids=str)
 @pytest.mark.parametrize("n, G", [(2, 4), (3, 1), (4, 4), (5, 7), (16, 2), (17, 8), (40, 4), (130, 3)])
@@ -331,6 +340,7 @@ def test_several_positions(shape, n, G):
     f.clean()
 
 
+@pytest.mark.usefixtures("room")
 @pytest.mark.gpu
 @pytest.mark.parametrize("n_ctas", [1, 3, 40])
 @pytest.mark.parametrize("n, G", [(1, 4), (3, 8), (64, 4)])
@@ -364,6 +374,7 @@ def test_what_the_workspace_held_does_not_matter(n, G, fill, lens):
         check(out[s], *f.expected(qs[s], s)[::2])
 
 
+@pytest.mark.usefixtures("room")
 @pytest.mark.gpu
 @pytest.mark.parametrize("shape", SHAPES[:4], ids=str)
 @pytest.mark.parametrize("ns", [[0, 1, 5, 0, 33], [3, 0, 0, 0, 0], [1, 1, 1, 1, 1], [100, 1, 2, 150, 300]])
@@ -387,6 +398,7 @@ def test_ragged_rows(shape, ns):
     f.clean()
 
 
+@pytest.mark.usefixtures("room")
 @pytest.mark.gpu
 @pytest.mark.parametrize("n, G", [(1, 4), (4, 8), (70, 4)])
 def test_empty_sequences_and_queries_before_the_start_give_zeros(n, G):
@@ -402,6 +414,7 @@ def test_empty_sequences_and_queries_before_the_start_give_zeros(n, G):
     assert (state[0, :, :, 128 + 1] == 0).all() and (state[0, :, :, :128] == 0).all()
 
 
+@pytest.mark.usefixtures("room")
 @pytest.mark.gpu
 @pytest.mark.parametrize("n, G", [(1, 4), (2, 4), (1, 16), (70, 4)])
 @pytest.mark.parametrize("dtype", [BF16, FP16])
@@ -421,6 +434,7 @@ def test_values_of_very_different_sizes(n, G, dtype):
         check(out[s], *f.expected(q, s)[::2])
 
 
+@pytest.mark.usefixtures("room")
 @pytest.mark.gpu
 @pytest.mark.parametrize("n, G", [(1, 4), (4, 4), (70, 4)])
 def test_infinite_and_nan_rows_reach_only_the_queries_that_see_them(n, G):
@@ -443,6 +457,7 @@ def test_infinite_and_nan_rows_reach_only_the_queries_that_see_them(n, G):
         assert torch.isnan(out[0, -1, :, 32:64]).all()
 
 
+@pytest.mark.usefixtures("room")
 @pytest.mark.gpu
 @pytest.mark.parametrize("n, G", [(1, 4), (8, 4), (70, 2)])
 def test_pages_and_lengths_that_make_no_sense(n, G):
@@ -474,10 +489,11 @@ def test_pages_and_lengths_that_make_no_sense(n, G):
     assert (out[0] == 0).all()
     check(out[1], *f.expected(qs[1], 1)[::2])
     bad = f.cache.stats()["bad_lengths"]
-    f.cache.attention(f.table, torch.tensor([1 << 30, 90], **INTS).cuda(), q)      # as if 160 (5 pages of 32)
+    f.cache.attention(f.table, torch.tensor([1 << 30, 90], **INTS).cuda(), q)      # as if it filled its table
     assert f.cache.stats()["bad_lengths"] > bad
 
 
+@pytest.mark.usefixtures("room")
 @pytest.mark.gpu
 @pytest.mark.parametrize("G", [33, 64])
 def test_many_query_heads_per_kv_head(G):
@@ -500,6 +516,7 @@ def test_more_sequences_than_a_cta_has_threads(n, most):
     f.clean()
 
 
+@pytest.mark.usefixtures("room")
 @pytest.mark.gpu
 @pytest.mark.parametrize("dtype, d, g, G, lens", [(BF16, 128, 32, 4, [1200]), (FP16, 64, 64, 7, [700, 10, 390]), (BF16, 128, 128, 1, [2600, 300])])
 def test_whole_prompts(dtype, d, g, G, lens):
@@ -527,6 +544,7 @@ def test_a_long_prompt_in_more_blocks_than_a_warp_looks_up_at_once():
     f.clean()
 
 
+@pytest.mark.usefixtures("room")
 @pytest.mark.gpu
 def test_more_rows_than_the_bound_says():
     f = Filled([100, 50], G=4, seed=9)
@@ -539,6 +557,7 @@ def test_more_rows_than_the_bound_says():
     check(out[5:], *f.expected(qs[1], 1)[::2])
 
 
+@pytest.mark.usefixtures("room")
 @pytest.mark.gpu
 @pytest.mark.parametrize("n, G, H", [(1, 4, 2), (6, 8, 1), (80, 4, 2)])
 @pytest.mark.parametrize("dtype, d", [(BF16, 128), (FP16, 64)])
@@ -554,6 +573,7 @@ def test_states(n, G, H, dtype, d):
         assert (st[s, ..., d] + torch.log2(st[s, ..., d + 1]) - lse).abs().max() < 2.0 ** -12
 
 
+@pytest.mark.usefixtures("room")
 @pytest.mark.gpu
 @pytest.mark.parametrize("scale", [0.02, 1.0])
 def test_softmax_scale(scale):
@@ -564,6 +584,7 @@ def test_softmax_scale(scale):
         check(out[s], *f.expected(q, s, scale)[::2])
 
 
+@pytest.mark.usefixtures("room")
 @pytest.mark.gpu
 @pytest.mark.parametrize("n, G", [(1, 4), (3, 8), (90, 4)])
 def test_strided_queries_and_results(n, G):
@@ -581,6 +602,7 @@ def test_strided_queries_and_results(n, G):
 
 
 # ---- GPU: how a user's program runs them ------------------------------------------------------------------------------
+@pytest.mark.usefixtures("room")
 @pytest.mark.gpu
 @pytest.mark.parametrize("n, G", [(1, 4), (2, 4), (64, 4)])
 def test_same_bits_every_run_on_any_stream_and_in_a_graph(n, G):
@@ -707,6 +729,7 @@ def test_shared_pages():
     check(out[1], ref, tol)
 
 
+@pytest.mark.usefixtures("room")
 @pytest.mark.gpu
 @pytest.mark.parametrize("seed", range(6))
 def test_random_configurations(seed):
