@@ -586,6 +586,9 @@ pkv_status pkv_q4_read_kv(pkv_q4_cache *c, int32_t n_seqs, const int32_t *page_t
  *   workspace   [device] pkv_q4_attention_workspace(n_seqs, max_q_len, max_len) bytes, 16-byte aligned; contents before
  *               and after do not matter.  NULL where that is 0.
  * Scores, softmax and sums are held in fp32; codes times scale enter the products exactly, the weights rounded to fp16.
+ * That holds for magnitudes of q, k and v from 2^-60 to 2^60 (every fp16 value lies inside); of larger ones products may
+ * become infinite or NaN, smaller ones may count as zero.  A query, key or value that is not finite makes the results that
+ * depend on it NaN or meaningless, and no others.
  */
 pkv_status pkv_q4_attention_workspace(const pkv_q4_cache *c, int32_t n_seqs, int32_t max_q_len, int32_t max_len,
                                       int64_t *bytes);

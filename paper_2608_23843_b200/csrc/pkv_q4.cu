@@ -356,6 +356,7 @@ pkv_status q4_validate(const pkv_q4_config *cfg, Q4Geometry *g) {
     if (g->n_pages > (1LL << 60) / g->page_bytes) return PKV_ERR_INVALID_ARG;
     const float scale = cfg->softmax_scale > 0 ? cfg->softmax_scale : 1.f / std::sqrt((float)cfg->head_dim);
     g->scale_log2e = scale * 1.4426950408889634f;
+    if (!std::isfinite(g->scale_log2e)) return PKV_ERR_INVALID_ARG;
     return PKV_OK;
 }
 

@@ -35,7 +35,7 @@ def test_sizes(d, g, P, H, token_bytes):
     (dict(n_q_heads=7), pkv.PKV_ERR_INVALID_ARG), (dict(n_kv_heads=0), pkv.PKV_ERR_INVALID_ARG),
     (dict(n_pages=0), pkv.PKV_ERR_INVALID_ARG), (dict(n_pages=1 << 31), pkv.PKV_ERR_UNSUPPORTED),
     (dict(softmax_scale=math.inf), pkv.PKV_ERR_INVALID_ARG), (dict(softmax_scale=math.nan), pkv.PKV_ERR_INVALID_ARG),
-    (dict(softmax_scale=-1.0), pkv.PKV_ERR_INVALID_ARG), (dict(n_ctas=-1), pkv.PKV_ERR_INVALID_ARG)])
+    (dict(softmax_scale=-1.0), pkv.PKV_ERR_INVALID_ARG), (dict(softmax_scale=3e38), pkv.PKV_ERR_INVALID_ARG), (dict(n_ctas=-1), pkv.PKV_ERR_INVALID_ARG)])
 def test_configurations_that_are_refused(change, status):
     with pytest.raises(pkv.PkvError) as e:
         pkv.Q4Cache(config(**change), dry_run=True)
@@ -437,6 +437,41 @@ def test_values_of_very_different_sizes(n, G, dtype):
 @pytest.mark.usefixtures("room")
 @pytest.mark.gpu
 @pytest.mark.parametrize("n, G", [(1, 4), (4, 4), (70, 4)])
+@pytest.mark.parametrize("k, v", [(50, 0), (-50, 0), (0, 55), (0, -55), (50, -55)])
+def test_magnitudes_near_the_ends_of_the_documented_range(n, G, k, v):
+    f = Filled([150, 90], G=G, H=1, seed=30)
+    ks, vs = [x * 2.0 ** k for x in f.k], [x * 2.0 ** v for x in f.v]
+    f.cache.append_kv(f.table, f.lengths, torch.cat(ks).cuda(), torch.cat(vs).cuda(), f.off)
+    f.K, f.V = [quantised(x, 32) for x in ks], [quantised(x, 32) for x in vs]
+    qs = [q * 2.0 ** -k for q in f.queries([n, n])]
+    out = f.cache.attention(f.table, f.lengths, torch.stack(qs).cuda())
+    for s, q in enumerate(qs):
+        check(out[s], *f.expected(q, s)[::2])
+
+
+@pytest.mark.usefixtures("room")
+@pytest.mark.gpu
+@pytest.mark.parametrize("n, G", [(1, 4), (4, 4), (70, 4)])
+@pytest.mark.parametrize("value", [math.nan, math.inf])
+def test_queries_that_are_not_finite_leave_the_others_alone(n, G, value):
+    f = Filled([200, 90], G=G, H=2, seed=31)
+    qs = torch.stack(f.queries([n, n]))
+    bad = qs.clone()
+    bad[0, n // 2, 1, 5] = value
+    out = f.cache.attention(f.table, f.lengths, bad.cuda()).cpu()
+    if value != value:
+        assert torch.isnan(out[0, n // 2, 1]).all()
+    for s in range(2):
+        ref, _, tol = f.expected(qs[s], s)
+        if s == 0:
+            out[0, n // 2, 1] = 0.0
+            ref[n // 2, 1] = 0.0
+        check(out[s], ref, tol)
+
+
+@pytest.mark.usefixtures("room")
+@pytest.mark.gpu
+@pytest.mark.parametrize("n, G", [(1, 4), (4, 4), (70, 4)])
 def test_infinite_and_nan_rows_reach_only_the_queries_that_see_them(n, G):
     """A key or value that is not finite makes the queries that see it NaN (a value: at least its group's channels) and
     leaves the others alone, whether they come before it or belong to other sequences."""
@@ -528,6 +563,29 @@ def test_whole_prompts(dtype, d, g, G, lens):
     for s, q in enumerate(qs):
         check(out[at:at + lens[s]], *f.expected(q, s)[::2])
         at += lens[s]
+    f.clean()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("n", [1, 9, 40])
+def test_many_kv_heads(n):
+    f = Filled([21, 70], G=1, H=200, P=16, d=64, seed=32)
+    k, v = (torch.empty(91, 200, 64, dtype=BF16, device="cuda") for _ in "kv")
+    f.cache.read_kv(f.table, f.lengths, k, v, f.off)
+    assert torch.equal(k.cpu(), torch.cat(f.K).to(BF16)) and torch.equal(v.cpu(), torch.cat(f.V).to(BF16))
+    qs = f.queries([min(n, 21), n])
+    out = f.cache.attention(f.table, f.lengths, torch.cat(qs).cuda(), offsets=offsets_of([min(n, 21), n]).cuda(), max_q_len=n).cpu()
+    check(out[:min(n, 21)], *f.expected(qs[0], 0)[::2])
+    check(out[min(n, 21):], *f.expected(qs[1], 1)[::2])
+    f.clean()
+
+
+@pytest.mark.gpu
+def test_one_very_long_sequence():
+    f = Filled([300_003], G=2, H=1, P=256, d=64, seed=33)
+    for n in (1, 7, 40):
+        q = f.queries([n])[0]
+        check(f.cache.attention(f.table, f.lengths, q[None].cuda())[0], *f.expected(q, 0)[::2])
     f.clean()
 
 
@@ -715,6 +773,18 @@ def test_old_tokens_in_4_bits_recent_ones_in_a_dense_and_factor_cache():
     # the dense rows' weights are rounded to bf16 there: one unit of 2^-9 of the largest value, instead of fp16's 2^-11
     check(out, ref, tol + 2.0 ** -9 * V.abs().max())
     c.close()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("n, G", [(1, 4), (5, 8)])
+def test_states_of_an_empty_cache_merge_as_nothing(n, G):
+    f = Filled([0, 100], H=2, G=G, seed=34)
+    q = f.queries([n])[0]
+    both = torch.stack([q, q]).cuda()
+    states = f.cache.attention_partial(f.table, f.lengths, both)      # shard 0 has no tokens
+    out = torch.empty(n, 2 * G, 128, dtype=BF16, device="cuda")
+    pkv.pkv_merge_attention_states(states, 2, n * 2 * G, out=out, stream=torch.cuda.current_stream())
+    check(out, *f.expected(q, 1)[::2])
 
 
 @pytest.mark.gpu
