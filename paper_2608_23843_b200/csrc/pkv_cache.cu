@@ -2,6 +2,7 @@
 // decode planning (split of the page list over CTAs) and the C ABI.  All device
 // work is delegated to the launchers declared in pkv_internal.h.
 #include <algorithm>
+#include <atomic>
 #include <cmath>
 #include <cstdarg>
 #include <cstdio>
@@ -12,8 +13,11 @@
 #include <vector>
 
 #include "pkv_internal.h"
+#include "pkv_q4.h"
 
 using namespace pkv;
+
+std::atomic<bool> pkv::unordered_decodes{false};
 
 namespace {
 
@@ -558,6 +562,7 @@ pkv_status pkv_init_cache(const pkv_config *cfg, void *dense_pool, void *factor_
     if (!c) return PKV_ERR_INVALID_ARG;
     c->cfg = *cfg;
     c->dry = dry;
+    if (!dry && cfg->decode_overlap == 2) unordered_decodes = true;
     { const char *t = getenv("PKV_DECODE_TRACE"); c->trace = t && t[0] == '1'; }
     { const char *t = getenv("PKV_TEST_WAIT_CLOCKS"); if (t && atoll(t) > 0) c->wait_clocks = atoll(t); }
     { const char *t = getenv("PKV_TEST_DROP_UNIT"); if (t && t[0]) c->drop_unit = atoi(t); }

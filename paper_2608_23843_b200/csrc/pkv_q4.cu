@@ -150,6 +150,8 @@ __global__ void __launch_bounds__(kCopyThreads) q4_append_kernel(const __grid_co
     const Q4Geometry &geo = a.geo;
     const CopyRows cr = copy_rows<D>(a);
     const int l = threadIdx.x % LR, slot = threadIdx.x / LR, j = l >> 1, b = l & 1;      // 32-channel word j, its half b
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    if (a.chained) asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     bool looked_up = false;
     for (int base = 0; base < cr.n_jobs; base += kSlots * kUnroll) {
         uint4 k[kUnroll][2], v[kUnroll][2];
@@ -233,6 +235,8 @@ __global__ void __launch_bounds__(kCopyThreads) q4_read_kernel(const __grid_cons
     const Q4Geometry &geo = a.geo;
     const CopyRows cr = copy_rows<D>(a);
     const int l = threadIdx.x % LR, slot = threadIdx.x / LR, j = l >> 2, c = l & 3;
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    if (a.chained) asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     if (threadIdx.x < a.rows_per_cta && cr.row0 + threadIdx.x < a.rows.n_rows) places[threadIdx.x] = place_of(a.rows, geo, cr.row0 + threadIdx.x, a.status);
     __syncthreads();
     for (int base = 0; base < cr.n_jobs; base += kSlots * kCopyUnroll) {
@@ -285,17 +289,26 @@ cudaError_t launch_copy(Q4CopyArgs a, cudaStream_t st) {
     if (rows > kCopyRows) rows = kCopyRows;
     a.rows_per_cta = (int)rows;
     a.inv_heads = 1.f / (float)g.n_kv_heads;
-    const unsigned grid = (unsigned)((n + rows - 1) / rows);
-#define PKV_Q4_COPY(D, NG)                                                                                           \
-    if (g.head_dim == D && g.groups == NG) {                                                                         \
-        if (g.fp16) { if (kWrite) q4_append_kernel<D, NG, true><<<grid, kCopyThreads, 0, st>>>(a);                   \
-                      else q4_read_kernel<D, NG, true><<<grid, kCopyThreads, 0, st>>>(a); }                          \
-        else { if (kWrite) q4_append_kernel<D, NG, false><<<grid, kCopyThreads, 0, st>>>(a);                         \
-               else q4_read_kernel<D, NG, false><<<grid, kCopyThreads, 0, st>>>(a); }                                \
-        return cudaGetLastError();                                                                                   \
+    a.chained = q4_chained();
+    cudaLaunchAttribute at[1];
+    at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    at[0].val.programmaticStreamSerializationAllowed = 1;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)((n + rows - 1) / rows));
+    cfg.blockDim = dim3(kCopyThreads);
+    cfg.stream = st;
+    cfg.attrs = at;
+    cfg.numAttrs = a.chained;
+#define PKV_Q4_COPY1(D, NG, H16) \
+    return kWrite ? cudaLaunchKernelEx(&cfg, q4_append_kernel<D, NG, H16>, a) : cudaLaunchKernelEx(&cfg, q4_read_kernel<D, NG, H16>, a);
+#define PKV_Q4_COPY(D, NG)                          \
+    if (g.head_dim == D && g.groups == NG) {        \
+        if (g.fp16) PKV_Q4_COPY1(D, NG, true)       \
+        PKV_Q4_COPY1(D, NG, false)                  \
     }
     PKV_Q4_COPY(128, 4) PKV_Q4_COPY(128, 2) PKV_Q4_COPY(128, 1) PKV_Q4_COPY(64, 2) PKV_Q4_COPY(64, 1)
 #undef PKV_Q4_COPY
+#undef PKV_Q4_COPY1
     return cudaErrorInvalidValue;
 }
 

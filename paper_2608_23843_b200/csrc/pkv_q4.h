@@ -16,6 +16,8 @@
 #include <cuda_runtime.h>
 #include <stdint.h>
 
+#include <atomic>
+
 #include "pkv.h"
 
 namespace pkv {
@@ -49,7 +51,8 @@ struct Q4CopyArgs {
     void *k, *v;                       // read by append, written by read
     long long k_row, k_head, v_row, v_head;      // strides in elements
     int *status;
-    int rows_per_cta;                  // set by the launcher, with 1 / n_kv_heads
+    int chained;                       // set by the launcher: the next kernel may be set up early (see q4_chained)
+    int rows_per_cta;                  // ... rows of a CTA, with 1 / n_kv_heads
     float inv_heads;
 };
 
@@ -64,9 +67,19 @@ struct Q4AttentionArgs {
     int max_q_len;                     // no sequence has more rows than this
     int max_len;                       // hint: lengths are expected up to this
     int whole;                         // set by the launcher: no segment is cut
+    int chained;                       // ... the kernel that follows the call's last may be set up early (see q4_chained)
+    int join;                          // ... the call's second kernel follows
     unsigned char *workspace;
     int *status;
 };
+
+// Calls of this cache are launched so that one may be set up while the kernel before it on the stream finishes
+// (programmatic stream serialization): each waits for that kernel before it touches memory, and only then lets the next one
+// start.  That orders a chain of kernels as long as all of them wait.  Decode launches with decode_overlap = 2 do not: one of
+// them between two kernels of this cache would hide the first from the second.  Once a process has such a cache, kernels
+// here are launched the ordinary way (1 to 2 us per call), but for the one that joins the states of its own call.
+extern std::atomic<bool> unordered_decodes;
+inline bool q4_chained() { return !unordered_decodes; }
 
 cudaError_t launch_q4_append(const Q4CopyArgs &a, cudaStream_t st);
 cudaError_t launch_q4_read(const Q4CopyArgs &a, cudaStream_t st);

@@ -155,7 +155,7 @@ __global__ void __launch_bounds__(Q4Shape<D, NG, NT>::kThreads, q4_ctas_per_sm(N
     }
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     asm volatile("griddepcontrol.wait;" ::: "memory");
-    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    if (a.chained || a.join) asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
 
     // ---- this CTA's share of the batch's units (a.whole: of its segments) ----
     const int H = geo.n_kv_heads, n_seqs = a.rows.n_seqs;
@@ -754,7 +754,7 @@ constexpr int kQ4JoinWarps = 4;
 template <int D, bool H16, int kRows>
 __global__ void __launch_bounds__(32 * kQ4JoinWarps) q4_join_kernel(const __grid_constant__ Q4AttentionArgs a, int R) {
     asm volatile("griddepcontrol.wait;" ::: "memory");
-    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    if (a.chained) asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     const Q4Geometry &geo = a.geo;
     const int b = blockIdx.x;
     const Q4Part p = reinterpret_cast<const Q4Part *>(a.workspace)[b];
@@ -911,13 +911,15 @@ cudaError_t launch_q4_attention(Q4AttentionArgs a, cudaStream_t st) {
     const int n = blocks ? q4_block_grid(g, a.rows.n_seqs, a.max_q_len, a.max_len) : q4_grid(g, a.rows.n_seqs, a.max_q_len, a.max_len);
     const int R = blocks ? kQ4BlockRows : q4_rows_per_tile(g, a.max_q_len);
     a.whole = !blocks && q4_whole(a.max_len);
+    a.chained = q4_chained();
+    a.join = n > 1 && !a.whole;
     cudaLaunchAttribute at[1];
     at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     at[0].val.programmaticStreamSerializationAllowed = 1;
     cudaLaunchConfig_t cfg = {};
     cfg.stream = st;
     cfg.attrs = at;
-    cfg.numAttrs = 1;
+    cfg.numAttrs = a.chained;
     cudaError_t e = cudaErrorInvalidValue;
 #define PKV_Q4_LAUNCH1(D, NG, H, NT)                                        \
     if ((g.fp16 != 0) == H && R == 8 * NT) {                                \
@@ -936,7 +938,8 @@ cudaError_t launch_q4_attention(Q4AttentionArgs a, cudaStream_t st) {
     } else {
         PKV_Q4_SHAPES(PKV_Q4_LAUNCH)
     }
-    if (e != cudaSuccess || n <= 1 || a.whole) return e;
+    if (e != cudaSuccess || !a.join) return e;
+    cfg.numAttrs = 1;
     cfg.gridDim = dim3(n, blocks ? R / (4 * kQ4JoinWarps) : R);
     cfg.blockDim = dim3(32 * kQ4JoinWarps);
     cfg.dynamicSmemBytes = 0;

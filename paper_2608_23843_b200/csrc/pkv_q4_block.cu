@@ -216,7 +216,7 @@ __global__ void __launch_bounds__(kBThreads, 1) q4_block_kernel(const __grid_con
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     asm volatile("griddepcontrol.wait;" ::: "memory");
-    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    if (a.chained || a.join) asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
 
     // ---- this CTA's share of the batch's units ----
     const int H = geo.n_kv_heads, n_seqs = a.rows.n_seqs;
@@ -823,7 +823,7 @@ cudaError_t launch_q4_block(const Q4AttentionArgs &a, int n, cudaStream_t st) {
     cudaLaunchConfig_t cfg = {};
     cfg.stream = st;
     cfg.attrs = at;
-    cfg.numAttrs = 1;
+    cfg.numAttrs = a.chained;
     cfg.gridDim = dim3(n);
     cfg.blockDim = dim3(kBThreads);
 #define PKV_Q4_LAUNCH1(D, NG, H16)                                                                       \

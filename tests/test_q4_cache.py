@@ -148,10 +148,10 @@ class Filled:
     """A cache on the GPU holding sequences of random rows, and what it stands for in 64 bits."""
     room = 0                                               # tokens that the tables have place for, at least
 
-    def __init__(self, lengths, dtype=BF16, d=128, g=32, P=64, H=2, G=4, seed=0, **kw):
+    def __init__(self, lengths, dtype=BF16, d=128, g=32, P=64, H=2, G=4, seed=0, room=None, **kw):
         gen = torch.Generator().manual_seed(seed)
         self.gen, self.dtype, self.d, self.g, self.H, self.G, self.lens = gen, dtype, d, g, H, G, list(lengths)
-        self.rows = Rows(lengths, P, seed, max_pages=max(-(-t // P) for t in [1, self.room, *lengths]))
+        self.rows = Rows(lengths, P, seed, max_pages=max(-(-t // P) for t in [1, room or self.room, *lengths]))
         self.cache = pkv.Q4Cache(config(n_kv_heads=H, n_q_heads=H * G, head_dim=d, group_size=g, page_size=P, dtype=dtype,
                                         n_pages=self.rows.n_pages, **kw))
         self.cache.pool.fill_(0xff)                        # what no row was written to reads as NaN
@@ -821,3 +821,50 @@ def test_random_configurations(seed):
             check(out[at:at + n], *f.expected(qs[s], s)[::2])
             at += n
         f.clean()
+
+
+@pytest.mark.gpu
+def test_between_decodes_of_the_page_cache_that_do_not_wait_for_one_another():
+    """A page cache whose decode launches overlap freely (decode_overlap = 2) shares the stream: rows appended before one of
+    its launches are there for the attention behind it, whatever memory the buffers in between get."""
+    H, G, T = 2, 4, 2000
+    f = Filled([T, 300], H=H, G=G, seed=35, room=3000)
+    c = pkv.Cache(pkv.make_config(n_layers=1, n_kv_heads=H, n_q_heads=H * G, rank=16, sink_tokens=64, recent_tokens=64, max_seqs=1,
+                                  max_pages_per_seq=8, n_dense_slots=8, n_factor_slots=1, decode_overlap=2))
+    k, v = rows_of(f.gen, 130, H, 128, BF16), rows_of(f.gen, 130, H, 128, BF16, False)
+    c.append_kv(0, [0], [130], k.cuda(), v.cuda())
+    q = f.queries([1])[0]
+    qs = [torch.stack(f.queries([n, n])).cuda() for n in (1, 4, 40)]
+    qd = q.cuda()
+    want = [f.cache.attention(f.table, f.lengths, x) for x in qs]
+    dense, _, tol = attention(q, k.double(), v.double(), 129, 1 / math.sqrt(128), BF16)
+    torch.cuda.synchronize()
+    rows = [torch.cat(x).cuda() for x in (f.k, f.v)]
+    kept = []
+    for i in range(12):
+        f.cache.append_kv(f.table, f.lengths, *rows, f.off)
+        a = torch.empty(1, H * G, 128, dtype=BF16, device="cuda")
+        c.decode_attention(0, [0], qd, out=a)
+        b = f.cache.attention(f.table, f.lengths, qs[i % 3])
+        back = [torch.empty_like(x) for x in rows]
+        c.decode_attention(0, [0], qd, out=torch.empty_like(a))
+        f.cache.read_kv(f.table, f.lengths, *back, f.off)
+        kept.append((a, b, back))
+    torch.cuda.synchronize()
+    for i, (a, b, back) in enumerate(kept):
+        assert torch.equal(b, want[i % 3])
+        check(a, dense, tol + 2.0 ** -9 * v.abs().max())      # (bf16 weights there, see above)
+        assert torch.equal(back[0].cpu(), torch.cat(f.K).to(BF16)) and torch.equal(back[1].cpu(), torch.cat(f.V).to(BF16))
+    f.clean()
+    c.close()
+
+
+@pytest.mark.gpu
+def test_in_a_process_without_such_a_cache():
+    """Kernels are launched differently there: the tests of calls that follow one another, by themselves."""
+    import subprocess
+    import sys
+    names = "same_bits or decode_loop or prefill_in_chunks or written_in_several_calls or random_configurations or whole_prompts"
+    r = subprocess.run([sys.executable, "-m", "pytest", "-q", "-x", "-m", "gpu", "-k", names, "-p", "no:cacheprovider", __file__],
+                       capture_output=True, text=True, timeout=600)
+    assert r.returncode == 0, r.stdout[-3000:]
