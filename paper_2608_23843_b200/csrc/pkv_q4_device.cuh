@@ -17,7 +17,7 @@ constexpr float kQ4Lag = 14.f;         // how far (base 2) scores may pass the s
 // A segment that begins in a CTA and ends in another (seq < 0: none); slot: where its first part is (see below)
 struct Q4Part { int seq, tile, head, slot, last_cta; };
 
-// Partial states: two per CTA (its first segment, its last), each [8 NT rows][D] o, then m and l of the rows.
+// Partial states: two per CTA (its first segment, its last), each [rows of a tile or block][D] o, then m and l of the rows.
 __host__ __device__ inline long long q4_state_floats(int rows, int d) { return (long long)rows * (d + 2); }
 __host__ __device__ inline long long q4_parts_bytes(int n_ctas) { return ((long long)n_ctas * (int)sizeof(Q4Part) + 255) / 256 * 256; }
 
