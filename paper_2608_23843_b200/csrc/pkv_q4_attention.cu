@@ -14,8 +14,8 @@
 //     with E the exponent of the largest value scale so far; it follows when some score has passed it by 2^14 only, so
 //     p * scale <= 2^15, and a unit that moves nothing costs one vote.
 //   Queries are brought to fp16 with a power of two per row, which is exact for bf16 and fp16 alike.
-// Measured, 8 KV heads, d = 128, g = 32: 8 sequences of 32K (302 MB) 69 us with 4 or 8 rows per KV head (4.4 TB/s; issue slots
-// 58 % busy, tensor pipe 26 %), 102 us with 16; one of 128K 40.6 us; the kernel's rate on further tokens is 5.5 to 5.8 TB/s,
+// Measured, 8 KV heads, d = 128, g = 32: 8 sequences of 32K (302 MB) 67 us with 4 or 8 rows per KV head (4.5 TB/s; issue slots
+// 58 % busy, tensor pipe 26 %), 102 us with 16; one of 128K 39.5 us; the kernel's rate on further tokens is 5.5 to 5.8 TB/s,
 // and some 15 us of a call that joins states are launches, the first copies, the last units and the join.
 // One warp of a CTA looks up pages and issues the bulk copies; the others take the units of 64 tokens in turn and keep (m, l, o)
 // in registers; at the end of a (sequence, KV head, row tile) segment the warps' states are joined through shared memory.  The CTAs of
@@ -38,7 +38,7 @@ namespace {
 __host__ __device__ constexpr int q4_seg_cost(int nt) { return nt == 1 ? 6 : 12; }
 // Warps of a CTA, the last one for the copies: the kernel is bound by instruction issue and latency, so as many warps as their
 // registers allow - of one column of query rows, in 128 registers a thread, two CTAs of eight per SM (one CTA of sixteen, which
-// idles while it joins its warps' states: 87 us instead of 69 for 8 x 32K); of two columns, in 168 registers, one CTA of
+// idles while it joins its warps' states: 87 us instead of 69 for 8 x 32K when this was measured); of two columns, in 168 registers, one CTA of
 // twelve (two of six, with one consumer fewer and twice the segments: 115 us instead of 103).
 __host__ __device__ constexpr int q4_warps(int nt) { return nt == 1 ? 8 : 12; }
 __host__ __device__ constexpr int q4_ctas_per_sm(int nt) { return nt == 1 ? 2 : 1; }
@@ -46,14 +46,17 @@ __host__ __device__ constexpr int q4_ctas_per_sm(int nt) { return nt == 1 ? 2 : 
 template <int D, int NG, int NT>
 struct Q4Shape {
     static constexpr int kWarps = q4_warps(NT), kCons = kWarps - 1, kThreads = 32 * kWarps, kPerSM = q4_ctas_per_sm(NT);
-    static constexpr int kStep = NT == 1 ? 2 : 1;                                   // tiles per softmax step (two of two columns would spill: 128 us instead of 115)
+    // tiles per softmax step: with one column a whole unit, which leaves the scheduler most to choose from (8 x 32K: one tile 72 us,
+    // two 69, four 66.7); with two columns more than one would spill (16 rows, two tiles: 105 us instead of 103)
+    static constexpr int kStep = NT == 1 ? 4 : 1;
+    static constexpr int kQueries = NT * (D / 32) * 512;                            // query operands, in shared memory: registers are what is short
     static constexpr int kTile = kQ4Tile * (D + 4 * NG), kUnitBytes = kQ4UnitTiles * kTile;
     static constexpr int kRowFloats = D + 4;                                        // a row of o in shared memory, padded against bank conflicts
     static constexpr int kFlush = 8 * kRowFloats * 4;                               // a warp's o (eight rows at a time) at a segment's end: over the stage it has just read
     static constexpr int kStage = ((kUnitBytes > kFlush ? kUnitBytes : kFlush) + 127) / 128 * 128;
-    static constexpr int kFit = (227 * 1024 / kPerSM - 3584) / kStage, kStages = kFit < 32 / kPerSM ? kFit : 32 / kPerSM;
+    static constexpr int kFit = (227 * 1024 / kPerSM - 3584 - kQueries) / kStage, kStages = kFit < 32 / kPerSM ? kFit : 32 / kPerSM;
     static constexpr int kSmem = kStages * kStage;
-    static_assert(kStages > kCons && kPerSM * (kSmem + 3072) <= 227 * 1024, "a stage per warp and some in flight");
+    static_assert(kStages > kCons && kPerSM * (kSmem + kQueries + 3072) <= 227 * 1024, "a stage per warp and some in flight");
 };
 
 __device__ __forceinline__ void mma_f16(float *d, const uint32_t *a, uint32_t b0, uint32_t b1, const float *c) {
@@ -150,6 +153,7 @@ __global__ void __launch_bounds__(Q4Shape<D, NG, NT>::kThreads, q4_ctas_per_sm(N
     __shared__ unsigned long long full[kSt], empty[kSt];
     __shared__ uint32_t tiles_here[kSt];                       // which tiles of a stage's unit are there
     __shared__ float2 ml[kCons][8];
+    __shared__ uint4 queries[NT][NW][32];                      // of the segment, as the lanes of a warp take them
     __shared__ long long sums[kQ4Warps], found_at;
     __shared__ int found_seq, offs[kCons], gave_up;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, c = lane & 3;
@@ -338,7 +342,6 @@ __global__ void __launch_bounds__(Q4Shape<D, NG, NT>::kThreads, q4_ctas_per_sm(N
         // ---- the segment's queries ----
         int first, all;
         const int n = q4_new_rows(a, seg.seq, first, all, nullptr), G = geo.group;
-        uint32_t qf[NT][NW][4];
         uint32_t bias[NT][2], big_run = 0;                     // (big_run: largest value scale so far, in both halves)
         float E = -60.f;                                       // ... and its exponent
         float F[NT][2], o[NT][2 * NW][4];
@@ -374,6 +377,7 @@ __global__ void __launch_bounds__(Q4Shape<D, NG, NT>::kThreads, q4_ctas_per_sm(N
             // times 2^(10 - exponent of the largest): 2^10 .. 2^11, so that a sixteenth of it is far from subnormal too
             const int e = min(max((int)(__float_as_uint(mx) >> 23) - 127, -90), 126);
             const float up = __uint_as_float((uint32_t)(10 - e + 127) << 23);
+            uint32_t qf[NW][4];
             float sum[NG];
 #pragma unroll
             for (int k = 0; k < NG; ++k) sum[k] = 0.f;
@@ -382,10 +386,13 @@ __global__ void __launch_bounds__(Q4Shape<D, NG, NT>::kThreads, q4_ctas_per_sm(N
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
                     const float f = i & 1 ? up * 0.0625f : up;
-                    qf[nt][w][i] = pack_f16(x[w][2 * i] * f, x[w][2 * i + 1] * f);
-                    const float2 r = __half22float2(*reinterpret_cast<const __half2 *>(&qf[nt][w][i]));
+                    qf[w][i] = pack_f16(x[w][2 * i] * f, x[w][2 * i + 1] * f);
+                    const float2 r = __half22float2(*reinterpret_cast<const __half2 *>(&qf[w][i]));
                     sum[w / WPG] += (r.x + r.y) * (i & 1 ? 16.f : 1.f);
                 }
+            if (warp == 0)                                     // (every warp has the same: it needs its sums anyway)
+#pragma unroll
+                for (int w = 0; w < NW; ++w) queries[nt][w][lane] = make_uint4(qf[w][0], qf[w][1], qf[w][2], qf[w][3]);
             // -8 * sum(q) per group, to be multiplied by the tokens' scales in one product: as a column operand of three bf16
             // terms, k = group + NG * term
             const float fr = 16384.f * __uint_as_float((uint32_t)(e + 127) << 23) * scale;      // 2^24 / up: the factor of the scores
@@ -432,6 +439,8 @@ __global__ void __launch_bounds__(Q4Shape<D, NG, NT>::kThreads, q4_ctas_per_sm(N
                 for (int k = 0; k < 4; ++k) o[nt][i][k] = 0.f;
         }
         vis_all = __reduce_min_sync(0xffffffffu, vis_all);
+        consumers_sync();                                      // (the queries are there; those before were done with at the segment's end)
+        const uint32_t q_at = smem_u32(&queries[0][0][lane]);
 
         // ---- the segment's units ----
         const bool any = at < seg_hi;
@@ -514,8 +523,10 @@ __global__ void __launch_bounds__(Q4Shape<D, NG, NT>::kThreads, q4_ctas_per_sm(N
                             const uint32_t fb[4] = {x0 & 0x000f000fu, x1 & 0x000f000fu, x0 & 0x00f000f0u, x1 & 0x00f000f0u};
 #pragma unroll
                             for (int nt = 0; nt < NT; ++nt) {
-                                mma_f16(acc[nt], fa, qf[nt][w][0], qf[nt][w][1], acc[nt]);
-                                mma_f16(acc[nt], fb, qf[nt][w][2], qf[nt][w][3], acc[nt]);
+                                uint32_t q[4];
+                                lds128(q, q_at + (nt * NW + w) * 512);
+                                mma_f16(acc[nt], fa, q[0], q[1], acc[nt]);
+                                mma_f16(acc[nt], fb, q[2], q[3], acc[nt]);
                             }
                         }
                         const float f0 = k & 1 ? bf16hi_f(s0[k / 2]) : bf16lo_f(s0[k / 2]), f1 = k & 1 ? bf16hi_f(s1[k / 2]) : bf16lo_f(s1[k / 2]);

@@ -168,9 +168,6 @@ __device__ __forceinline__ uint32_t codes_hi(uint32_t x) { return sub_h2((x & 0x
 // shared-memory accesses in the order they are written down
 __device__ __forceinline__ void lds32(uint32_t *r, uint32_t at) { asm volatile("ld.shared.u32 %0, [%1];" : "=r"(r[0]) : "r"(at)); }
 __device__ __forceinline__ void lds64(uint32_t *r, uint32_t at) { asm volatile("ld.shared.v2.u32 {%0, %1}, [%2];" : "=r"(r[0]), "=r"(r[1]) : "r"(at)); }
-__device__ __forceinline__ void lds128(uint32_t *r, uint32_t at) {
-    asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(at));
-}
 __device__ __forceinline__ void sts128(uint32_t at, uint32_t x, uint32_t y, uint32_t z, uint32_t w) {
     asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(x), "r"(y), "r"(z), "r"(w) : "memory");
 }

@@ -49,6 +49,10 @@ __device__ __forceinline__ uint32_t sub_h2(uint32_t x, uint32_t y) {
     asm("sub.rn.f16x2 %0, %1, %2;" : "=r"(r) : "r"(x), "r"(y));
     return r;
 }
+// (volatile: where it is written down, and not kept in registers for later)
+__device__ __forceinline__ void lds128(uint32_t *r, uint32_t at) {
+    asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(at));
+}
 // Bounded wait that also ends when another warp has given up.  The thread sleeps until the phase completes (or for some
 // microseconds at a time): a warp that polls instead takes issue slots from the ones that work.
 __device__ __forceinline__ bool mbar_sleep(uint32_t bar, uint32_t parity) {
