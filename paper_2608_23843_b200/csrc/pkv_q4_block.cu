@@ -19,7 +19,9 @@
 // What bounds it: products and exponentials each take 1024 cycles per unit of 256 rows, but a half's chain - s, softmax, o,
 // the hand-overs between them - is some 1800 cycles long even with both for free, and the widening competes with the softmax
 // for issue slots (tensor pipe 42 %, exponentials 42 %, issue slots 56 % busy).  Tried on the same call and not kept: Q of one half in shared memory
-// so that s of the next unit can be computed behind the softmax (the products then wait for shared memory), five or six
+// so that s of the next unit can be computed behind the softmax (the products then wait for shared memory), s in two
+// buffers of 32 tokens for the same end (1509 us: twice the hand-overs, 40 products to issue per unit instead of 24; 1364 with an
+// issuing warp per half, which by itself costs more than it gives, 1501), five or six
 // widening warps, a quarter of the exponentials by polynomial, the halves' exponentials in turn, weights with the old
 // reference before the maximum is known.
 // CTAs share the batch's units evenly, one CTA per SM; blocks that span CTAs leave states that a second kernel joins.  Units
