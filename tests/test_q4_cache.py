@@ -581,6 +581,35 @@ def test_many_kv_heads(n):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("max_len", [16, 0])
+def test_as_many_sequences_as_a_call_takes(max_len):
+    """65535 sequences of one token, every ninth empty: attention gives the token's value, as it was quantised."""
+    S, H, d, P = 65535, 2, 64, 16
+    cache = pkv.Q4Cache(config(n_kv_heads=H, n_q_heads=2 * H, head_dim=d, page_size=P, n_pages=S))
+    table = torch.full((S, 1 if max_len else 200), -1, dtype=torch.int32)
+    table[:, 0] = torch.randperm(S, generator=torch.Generator().manual_seed(1)).int()
+    lengths = torch.ones(S, dtype=torch.int32)
+    lengths[::9] = 0
+    off = offsets_of(lengths.tolist()).cuda()
+    table, there = table.cuda(), lengths.bool()
+    n = int(there.sum())
+    k, v = (torch.randn(n, H, d, generator=torch.Generator().manual_seed(i)).to(BF16) for i in (2, 3))
+    cache.append_kv(table, lengths.cuda(), k.cuda(), v.cuda(), off)
+    q = torch.randn(n, 2 * H, d, generator=torch.Generator().manual_seed(4)).to(BF16).cuda()
+    out = cache.attention(table, lengths.cuda(), q, offsets=off, max_q_len=1, max_len=max_len)
+    # One token: o = w * code * scale and l = w for one weight w = 2^-E (1 + e), |e| <= 2^-20 (the exponent is score - (score +
+    # E), of numbers below 2^4 here: half an fp32 step is 2^-20, times ln 2; exp2 is good to 2^-22).  w * scale is rounded to fp16:
+    # scale has 8 bits and fp16 holds 11, so that is 2^-E scale itself.  o / l is then code * scale (1 - e), and a code * scale
+    # that lies halfway between two bf16 numbers may go to either: half a step, 2^-8 of the value, and e.
+    exact = quantised(v, 32).repeat_interleave(2, 1)
+    assert ((out.cpu().double() - exact).abs() <= exact.abs() * (2.0 ** -8 + 2.0 ** -20)).all()
+    uniform = cache.attention(table, lengths.cuda(), torch.ones(S, 1, 2 * H, d, dtype=BF16, device="cuda"), max_len=max_len)[:, 0]
+    assert ((uniform[there.cuda()].cpu().double() - exact).abs() <= exact.abs() * (2.0 ** -8 + 2.0 ** -20)).all()
+    assert (uniform[~there.cuda()] == 0).all()
+    assert cache.stats() == {"device_timeouts": 0, "bad_pages": 0, "bad_lengths": 0}
+
+
+@pytest.mark.gpu
 def test_one_very_long_sequence():
     f = Filled([300_003], G=2, H=1, P=256, d=64, seed=33)
     for n in (1, 7, 40):
