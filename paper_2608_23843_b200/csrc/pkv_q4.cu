@@ -18,8 +18,8 @@ namespace {
 // Both copy kernels are bound by HBM: 4 d bytes of 16-bit rows and d + 4 d/g bytes of cache per token and KV head.  A CTA
 // takes a few rows of the call: it looks up where they lie once, a thread each, while the first 16-byte loads are in flight
 // (K and V of a row and head together), so that nothing but the loads, the arithmetic and the stores is paid per
-// head.  Measured, 8 heads, d = 128, g = 32, bf16: append of 65536 rows 65 us (5.3 TB/s), read of 131072 rows 122 us
-// (5.6 TB/s); both have issue slots 65 % and the integer pipe 58 % busy, next to a copy's 6.45 TB/s.
+// head.  Measured, 8 heads, d = 128, g = 32, bf16: append of 65536 rows 65 us (5.3 TB/s), read of 131072 rows 117 us
+// (5.9 TB/s); both have issue slots 65 % and the integer pipe 58 % busy, next to a copy's 6.45 TB/s.
 constexpr int kCopyThreads = 256, kCopyUnroll = 4, kCopyRows = 128;
 
 struct RowPlace { long long off; int t, ok; };      // byte offset of the head-0 tile in the pool; token within its tile
@@ -282,9 +282,13 @@ cudaError_t launch_copy(Q4CopyArgs a, cudaStream_t st) {
     const Q4Geometry &g = a.geo;
     const long long n = a.rows.n_rows;
     if (n <= 0) return cudaSuccess;
-    // rows per CTA: four jobs (row, head) for each of its groups of lanes, fewer where that would leave SMs idle
+    // rows per CTA: 64 (128 at d = 64) jobs (row, head), twice that where it leaves three CTAs per SM, so that a CTA's start, the
+    // look-up, is paid half as often (8 heads: 4096 rows, append 13.3 and 14.4 us with the double, 8192 rows 18.4 and 17.4; read of
+    // 131072 rows 123 and 117; 40 heads, 4096 rows: append 38.9 and 30.8); fewer where SMs would be idle
     const int slots = kCopyThreads / (g.head_dim / 8);
     long long rows = slots * kCopyUnroll / g.n_kv_heads;
+    const long long more = 2LL * slots * kCopyUnroll / g.n_kv_heads;
+    if (more > 0 && n / more > 3LL * g.n_sms) rows = more;
     if (rows > n / g.n_sms) rows = n / g.n_sms;
     if (rows < 1) rows = 1;
     if (rows > kCopyRows) rows = kCopyRows;
