@@ -56,7 +56,7 @@ struct Q4Shape {
     static constexpr int kStage = ((kUnitBytes > kFlush ? kUnitBytes : kFlush) + 127) / 128 * 128;
     static constexpr int kFit = (227 * 1024 / kPerSM - 3584 - kQueries) / kStage, kStages = kFit < 32 / kPerSM ? kFit : 32 / kPerSM;
     static constexpr int kSmem = kStages * kStage;
-    static_assert(kStages > kCons && kPerSM * (kSmem + kQueries + 3072) <= 227 * 1024, "a stage per warp and some in flight");
+    static_assert(kStages > kCons && kPerSM * (kSmem + kQueries + 3 * 1024) <= 227 * 1024, "a stage per warp and some in flight");
 };
 
 __device__ __forceinline__ void mma_f16(float *d, const uint32_t *a, uint32_t b0, uint32_t b1, const float *c) {
