@@ -374,9 +374,10 @@ __global__ void __launch_bounds__(Q4Shape<D, NG, NT>::kThreads, q4_ctas_per_sm(N
             }
             mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 1));
             mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 2));
-            // times 2^(10 - exponent of the largest): 2^10 .. 2^11, so that a sixteenth of it is far from subnormal too
+            // times 2^(14 - exponent of the largest): 2^14 .. 2^15, so that a sixteenth of a channel 2^-24 (bf16: 2^-27) of the
+            // largest is exact too
             const int e = min(max((int)(__float_as_uint(mx) >> 23) - 127, -90), 126);
-            const float up = __uint_as_float((uint32_t)(10 - e + 127) << 23);
+            const float up = __uint_as_float((uint32_t)(14 - e + 127) << 23);
             uint32_t qf[NW][4];
             float sum[NG];
 #pragma unroll
@@ -395,7 +396,7 @@ __global__ void __launch_bounds__(Q4Shape<D, NG, NT>::kThreads, q4_ctas_per_sm(N
                 for (int w = 0; w < NW; ++w) queries[nt][w][lane] = make_uint4(qf[w][0], qf[w][1], qf[w][2], qf[w][3]);
             // -8 * sum(q) per group, to be multiplied by the tokens' scales in one product: as a column operand of three bf16
             // terms, k = group + NG * term
-            const float fr = 16384.f * __uint_as_float((uint32_t)(e + 127) << 23) * scale;      // 2^24 / up: the factor of the scores
+            const float fr = 1024.f * __uint_as_float((uint32_t)(e + 127) << 23) * scale;      // 2^24 / up: the factor of the scores
             uint32_t term[3][NG];
 #pragma unroll
             for (int k = 0; k < NG; ++k) {

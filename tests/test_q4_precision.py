@@ -1,0 +1,75 @@
+"""The 4-bit cache's attention where numbers of very different sizes meet: every channel is judged by its own group's values, and rows
+that a query does not see must not matter to it."""
+import math
+
+import pytest
+import torch
+
+from paper_2608_23843_b200 import pkv
+from q4_precision_reference import attention
+from q4_reference import Rows, offsets_of, quantised
+
+BF16, FP16 = torch.bfloat16, torch.float16
+# new positions and query heads per KV head: eight query rows at a time, sixteen
+ROWS = [(1, 4), (2, 4), (4, 4)]
+
+
+class Held:
+    """A cache on the GPU and the rows that were written to it."""
+
+    def __init__(self, k, v, G=4, g=32, P=64, room=3000, **kw):
+        """k, v: a list of [T, H, d] per sequence."""
+        _, H, d = k[0].shape
+        self.k, self.v, self.g, self.G, self.d, self.H, self.dtype = k, v, g, G, d, H, k[0].dtype
+        lens = [x.shape[0] for x in k]
+        self.rows = Rows(lens, P, 1, max_pages=max(-(-t // P) for t in [room, *lens]))
+        self.cache = pkv.Q4Cache(pkv.make_q4_config(n_kv_heads=H, n_q_heads=H * G, head_dim=d, page_size=P, group_size=g,
+                                                    dtype=self.dtype, n_pages=self.rows.n_pages, **kw))
+        self.cache.pool.fill_(0xff)
+        self.table, self.lengths = self.rows.device()
+        self.cache.append_kv(self.table, self.lengths, torch.cat(k).cuda(), torch.cat(v).cuda(), offsets_of(lens).cuda())
+
+    def attend(self, qs, **kw):
+        return self.cache.attention(self.table, self.lengths, torch.stack(qs).cuda(), **kw).cpu()
+
+    def expected(self, q, s, steps=None):
+        return attention(q, self.k[s], self.v[s], self.g, self.k[s].shape[0] - q.shape[0], 1 / math.sqrt(self.d), self.dtype, steps)
+
+
+def randn(seed, *shape):
+    return torch.randn(*shape, generator=torch.Generator().manual_seed(seed))
+
+
+def check(out, ref, tol):
+    out = out.to(torch.float64)
+    assert torch.isfinite(out).all()
+    worst = ((out - ref).abs() / tol).max().item()
+    assert worst <= 1, worst
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("n, G", ROWS)
+@pytest.mark.parametrize("dtype", [BF16, FP16])
+def test_scores_beside_a_large_query_channel(n, G, dtype):
+    """A query's large channel meets keys whose codes are zero there: it must not cost the other channels' products."""
+    T = 500
+    k, q = randn(1, T, 1, 128), randn(2, n, G, 128)
+    k[..., 3] *= 0.0
+    q[..., 3] = 30000.0
+    h = Held([k.to(dtype)], [randn(3, T, 1, 128).to(dtype)], G=G)
+    q = q.to(dtype)
+    check(h.attend([q])[0], *h.expected(q, 0))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("n, G", ROWS)
+@pytest.mark.parametrize("dtype, power", [(BF16, 16), (BF16, 20), (BF16, 26), (FP16, 14)])
+def test_keys_and_queries_of_opposite_sizes(n, G, dtype, power):
+    """The first group's keys are 2^power times the others', and the queries' channels there as much smaller."""
+    T = 400
+    k, q = randn(1, T, 1, 128) * 2.0 ** (-power // 2), randn(2, n, G, 128) * 2.0 ** (power // 2)
+    k[..., :32] *= 2.0 ** power
+    q[..., :32] *= 2.0 ** -power
+    h = Held([k.to(dtype)], [randn(3, T, 1, 128).to(dtype)], G=G)
+    q = q.to(dtype)
+    check(h.attend([q])[0], *h.expected(q, 0))
