@@ -6,16 +6,18 @@
 // contraction dimension of o^T += V^T p, so that eight query rows (NT = 1) fill the column dimension of one m16n8k16 product:
 //   K codes become fp16 operands by masking alone: code + 8 in the low bits of a 16-bit word is an fp16 subnormal,
 //     (code + 8) 2^-24 exactly, and in bits 4-7 that times 16 (the queries of those channels are divided by 16).  The + 8
-//     is taken away for all groups at once by one product of the scales with -8 * sum(q).  Each group's product is
-//     multiplied by its scale in fp32.
+//     is taken away for all groups at once by one product of the scales with -8 * sum(q) (measured: a query channel 30000
+//     times the others costs these nothing).  Each group's product is multiplied by its scale in fp32.
 //   V codes become exact fp16 integers, two products' rows from each byte (see there; as subnormals they would lose the
 //     contributions of small weights next to a large one's + 8).  The scales go to the weights: p * scale, rounded once to
-//     fp16.  To keep that inside fp16's range whatever the values' size, the running reference of the softmax is max(s) + E
-//     with E the exponent of the largest value scale so far; it follows when some score has passed it by 2^14 only, so
-//     p * scale <= 2^15, and a unit that moves nothing costs one vote.
+//     fp16.  Where the largest of them lies in fp16's range is kept per query row and channel group, going by the tokens that the
+//     row sees (see q4_follow), so values may be of any size and the sizes may differ from group to group and token to token.  It moves
+//     only when something may have passed fp16's range; a unit that moves nothing costs one vote, and no product more
+//     while the groups of a row share a reference.  (One reference for all rows and groups of a warp, with the largest at 1, was 6 % faster
+//     at eight rows and 11 % at sixteen, and rounded small weights, and groups of smaller values, to few bits or to zero.)
 //   Queries are brought to fp16 with a power of two per row, which is exact for bf16 and fp16 alike.
-// Measured, 8 KV heads, d = 128, g = 32: 8 sequences of 32K (302 MB) 67 us with 4 or 8 rows per KV head (4.5 TB/s; issue slots
-// 58 % busy, tensor pipe 26 %), 102 us with 16; one of 128K 39.5 us; the kernel's rate on further tokens is 5.5 to 5.8 TB/s,
+// Measured, 8 KV heads, d = 128, g = 32: 8 sequences of 32K (302 MB) 71 us with 4 or 8 rows per KV head (4.3 TB/s; issue slots
+// 58 % busy, tensor pipe 26 %), 113 us with 16; one of 128K 42 us; the kernel's rate on further tokens is 5.5 to 5.8 TB/s,
 // and some 15 us of a call that joins states are launches, the first copies, the last units and the join.
 // One warp of a CTA looks up pages and issues the bulk copies; the others take the units of 64 tokens in turn and keep (m, l, o)
 // in registers; at the end of a (sequence, KV head, row tile) segment the warps' states are joined through shared memory.  The CTAs of
@@ -54,9 +56,11 @@ struct Q4Shape {
     static constexpr int kRowFloats = D + 4;                                        // a row of o in shared memory, padded against bank conflicts
     static constexpr int kFlush = 8 * kRowFloats * 4;                               // a warp's o (eight rows at a time) at a segment's end: over the stage it has just read
     static constexpr int kStage = ((kUnitBytes > kFlush ? kUnitBytes : kFlush) + 127) / 128 * 128;
-    static constexpr int kFit = (227 * 1024 / kPerSM - 3584 - kQueries) / kStage, kStages = kFit < 32 / kPerSM ? kFit : 32 / kPerSM;
+    // the other arrays in shared memory: per warp the states' (m, l), references and gains, per stage two barriers and a word; 1 KB is the system's
+    static constexpr int kOther = 1024 + kCons * (64 + NT * (128 + 16 * NG)) + 32 / kPerSM * 20 + 256;
+    static constexpr int kFit = (227 * 1024 / kPerSM - kOther - kQueries) / kStage, kStages = kFit < 32 / kPerSM ? kFit : 32 / kPerSM;
     static constexpr int kSmem = kStages * kStage;
-    static_assert(kStages > kCons && kPerSM * (kSmem + kQueries + 3 * 1024) <= 227 * 1024, "a stage per warp and some in flight");
+    static_assert(kStages > kCons && kPerSM * (kSmem + kQueries + kOther) <= 227 * 1024, "a stage per warp and some in flight");
 };
 
 __device__ __forceinline__ void mma_f16(float *d, const uint32_t *a, uint32_t b0, uint32_t b1, const float *c) {
@@ -113,6 +117,72 @@ __device__ __forceinline__ void q4_scales(const unsigned char *p, int g, uint32_
     }
 }
 
+__device__ __forceinline__ float q4_pow2(int e) { return __uint_as_float((uint32_t)(e + 127) << 23); }
+// The largest of a column of scores: the lanes of the same c.
+__device__ __forceinline__ float q4_max_rows(float x) {
+    x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 4));
+    x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 8));
+    return fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 16));
+}
+
+// The softmax's references of a query row (a column), all whole numbers, so that moving one is exact.  The weights are 2^(score -
+// F) * value scale, and what brings the largest near 2^kQ4Place in a group of channels is
+//     R = the group's largest score + log2(value scale), less kQ4Place.
+// F is the largest R of the groups.  A group whose R is not far below shares it; the others get a reference A = R of their own and
+// their weights a gain of 2^(F - A).  Only tokens that the row sees enter, each with its own scores and scales.
+// The lanes of a column share the work: a lane has group (g / 2) % NG of column 2c + g % 2.
+// The largest of a column's eight lanes for each group, to the lane that has it:
+template <int NG>
+__device__ __forceinline__ float q4_own_max(const float (*best)[2], int lane) {
+    float v[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const float lo = best[(i >> 1) % NG][i & 1], hi = best[(2 + (i >> 1)) % NG][i & 1];
+        v[i] = fmaxf(lane & 16 ? hi : lo, __shfl_xor_sync(0xffffffffu, lane & 16 ? lo : hi, 16));
+    }
+#pragma unroll
+    for (int i = 0; i < 2; ++i) v[i] = fmaxf(lane & 8 ? v[i + 2] : v[i], __shfl_xor_sync(0xffffffffu, lane & 8 ? v[i] : v[i + 2], 8));
+    return fmaxf(lane & 4 ? v[1] : v[0], __shfl_xor_sync(0xffffffffu, lane & 4 ? v[0] : v[1], 4));
+}
+__device__ __forceinline__ float q4_max_groups(float x) {      // of a column, over the lanes of its groups
+    x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 8));
+    return fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 16));
+}
+constexpr int kQ4Even = 2;
+constexpr float kQ4Share = 2.f;        // how far below F a group's R may be for the group to share F
+// Where values are tiny or zero the scores set F: p stays below 2^(kQ4Floor + 10), so that its sum is far from fp32's largest.
+constexpr float kQ4Floor = 90.f;
+// A of the lane, from the gains of its group (bf16, both columns)
+__device__ __forceinline__ float q4_shared_ref(float F, uint32_t gains, int lane) {
+    return F - (float)((int)((lane & 4 ? gains >> 23 : gains >> 7) & 0xffu) - 127);
+}
+// The lane's references when its column has reached `best` and `score`; corr: what o of the group is multiplied by.
+struct Q4Refs { float R, A, F, gain, corr; };
+__device__ __forceinline__ Q4Refs q4_follow(float best, float score, float F, float R, float A, int lane) {
+    const uint32_t passed = __ballot_sync(0xffffffffu, best > A + kQ4Most || score > F + kQ4Floor + 10.f);
+    Q4Refs r{R, A, F, 1.f, 1.f};
+    const bool follow = (passed >> (lane & 7)) & 0x01010101u;  // some group of the column
+    if (follow) r.R = fmaxf(r.R, ceilf(best) - kQ4Place);
+    const float top = fmaxf(q4_max_groups(r.R), ceilf(score) - kQ4Floor);
+    if (follow) {
+        r.F = fmaxf(F, top);
+        r.A = r.R > kNegInf && r.F - r.R > kQ4Share ? fmaxf(r.R, r.F - 126.f) : r.F;
+        r.corr = ex2(A - r.A);
+    }
+    r.gain = q4_pow2(min(max(__float2int_rn(r.F - r.A), 0), 126));
+    return r;
+}
+// The scores up to which nothing of the lane's columns can have been passed, given the largest value scale of each group.
+template <int NG>
+__device__ __forceinline__ void q4_pass(float *pass, float F, float A, const uint32_t *big, int lane) {
+    const int k = (lane >> 3) % NG;
+    const uint32_t w = k & 2 ? big[(NG - 1) / 2] : big[0];
+    float t = fminf(F + kQ4Floor + 10.f, A + kQ4Most - __log2f(k & 1 ? bf16hi_f(w) : bf16lo_f(w)));
+    t = -q4_max_groups(-t);
+    pass[0] = __shfl_sync(0xffffffffu, t, lane & 3);
+    pass[1] = __shfl_sync(0xffffffffu, t, 4 | (lane & 3));
+}
+
 // Where a unit is: positions in the batch's order of units (sequence, row tile, head, unit of 64 tokens).
 struct Q4Cursor {
     int seq, tile, head, unit;         // seq == n_seqs: past the end
@@ -153,6 +223,9 @@ __global__ void __launch_bounds__(Q4Shape<D, NG, NT>::kThreads, q4_ctas_per_sm(N
     __shared__ unsigned long long full[kSt], empty[kSt];
     __shared__ uint32_t tiles_here[kSt];                       // which tiles of a stage's unit are there
     __shared__ float2 ml[kCons][8];
+    __shared__ float refs[kCons][NT][32];                      // R of the lane's group and column, see q4_own_max
+    __shared__ uint32_t gains[kCons][NT][NG][4];               // bf16, two columns to a word
+    __shared__ int vis[8 * NT];                                // tokens a column's query sees
     __shared__ uint4 queries[NT][NW][32];                      // of the segment, as the lanes of a warp take them
     __shared__ long long sums[kQ4Warps], found_at;
     __shared__ int found_seq, offs[kCons], gave_up;
@@ -342,11 +415,12 @@ __global__ void __launch_bounds__(Q4Shape<D, NG, NT>::kThreads, q4_ctas_per_sm(N
         // ---- the segment's queries ----
         int first, all;
         const int n = q4_new_rows(a, seg.seq, first, all, nullptr), G = geo.group;
-        uint32_t bias[NT][2], big_run = 0;                     // (big_run: largest value scale so far, in both halves)
-        float E = -60.f;                                       // ... and its exponent
-        float F[NT][2], o[NT][2 * NW][4];
+        uint32_t bias[NT][2], big_run[(NG + 1) / 2];           // (big_run: a bound of each group's value scales so far, as they are stored)
+        float F[NT][2], pass[NT][2], o[NT][2 * NW][4];         // the reference; the score up to which it cannot have been passed
         uint64_t fcol[NT], l[NT];                              // (columns 2c, 2c + 1)
-        int vis[NT][2];
+        uint32_t gained = 0;                                   // bit nt: some group of a column has a reference of its own
+#pragma unroll
+        for (int i = 0; i < (NG + 1) / 2; ++i) big_run[i] = 0;
         int vis_all = seg.T;                                   // tokens every row of the tile sees
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
@@ -377,7 +451,7 @@ __global__ void __launch_bounds__(Q4Shape<D, NG, NT>::kThreads, q4_ctas_per_sm(N
             // times 2^(14 - exponent of the largest): 2^14 .. 2^15, so that a sixteenth of a channel 2^-24 (bf16: 2^-27) of the
             // largest is exact too
             const int e = min(max((int)(__float_as_uint(mx) >> 23) - 127, -90), 126);
-            const float up = __uint_as_float((uint32_t)(14 - e + 127) << 23);
+            const float up = q4_pow2(14 - e);
             uint32_t qf[NW][4];
             float sum[NG];
 #pragma unroll
@@ -396,7 +470,7 @@ __global__ void __launch_bounds__(Q4Shape<D, NG, NT>::kThreads, q4_ctas_per_sm(N
                 for (int w = 0; w < NW; ++w) queries[nt][w][lane] = make_uint4(qf[w][0], qf[w][1], qf[w][2], qf[w][3]);
             // -8 * sum(q) per group, to be multiplied by the tokens' scales in one product: as a column operand of three bf16
             // terms, k = group + NG * term
-            const float fr = 1024.f * __uint_as_float((uint32_t)(e + 127) << 23) * scale;      // 2^24 / up: the factor of the scores
+            const float fr = 1024.f * q4_pow2(e) * scale;      // 2^24 / up: the factor of the scores
             uint32_t term[3][NG];
 #pragma unroll
             for (int k = 0; k < NG; ++k) {
@@ -428,10 +502,14 @@ __global__ void __launch_bounds__(Q4Shape<D, NG, NT>::kThreads, q4_ctas_per_sm(N
             for (int b = 0; b < 2; ++b) {
                 const int col = 2 * c + b, r2 = seg.tile * R + nt * 8 + col, j2 = r2 / G;
                 fb[b] = fmaxf(__shfl_sync(0xffffffffu, fr, 4 * col), 1.2e-38f);      // (never 0: a hidden score is -inf)
-                vis[nt][b] = j2 < n ? seg.T - all + j2 + 1 : seg.T;
-                vis_all = min(vis_all, vis[nt][b]);
-                F[nt][b] = kNegInf;
+                const int v = j2 < n ? seg.T - all + j2 + 1 : seg.T;
+                if (warp == 0 && g == 0) vis[nt * 8 + col] = v;
+                vis_all = min(vis_all, v);
+                F[nt][b] = pass[nt][b] = kNegInf;
             }
+            refs[warp][nt][lane] = kNegInf;
+#pragma unroll
+            for (int k = 0; k < NG; ++k) gains[warp][nt][k][c] = 0x3f803f80u;
             fcol[nt] = f2(fb[0], fb[1]);
             l[nt] = f2(0.f, 0.f);
 #pragma unroll
@@ -441,7 +519,7 @@ __global__ void __launch_bounds__(Q4Shape<D, NG, NT>::kThreads, q4_ctas_per_sm(N
         }
         vis_all = __reduce_min_sync(0xffffffffu, vis_all);
         consumers_sync();                                      // (the queries are there; those before were done with at the segment's end)
-        const uint32_t q_at = smem_u32(&queries[0][0][lane]);
+        const uint32_t q_at = smem_u32(&queries[0][0][lane]), gain_at = smem_u32(&gains[warp][0][0][c]);
 
         // ---- the segment's units ----
         const bool any = at < seg_hi;
@@ -453,34 +531,48 @@ __global__ void __launch_bounds__(Q4Shape<D, NG, NT>::kThreads, q4_ctas_per_sm(N
             else if (lane == 0 && !*abort_flag) { *abort_flag = 1; atomicAdd(a.status, 1); }      // (the unit counts as not there)
             const bool whole = tiles == (1u << kQ4UnitTiles) - 1u && t_unit + kQ4Unit <= vis_all;
             const unsigned char *sp = smem + st * S::kStage;
-            // E: exponent of the largest value scale so far (lane: tokens 2 lane, 2 lane + 1)
+            // bounds of the value scales so far (lane: tokens 2 lane, 2 lane + 1)
             {
                 const unsigned char *vs = sp + (lane >> 3) * S::kTile + q4_vs_base(D, NG) + (lane & 7) * 4 * NG;
                 const bool tile_ok = (tiles >> (lane >> 3)) & 1;
                 const bool ok0 = whole || (tile_ok && t_unit + 2 * lane < seg.T), ok1 = whole || (tile_ok && t_unit + 2 * lane + 1 < seg.T);
-                uint32_t z;
+                uint32_t z[(NG + 1) / 2];
                 if (NG == 4) {
                     const uint4 x = *reinterpret_cast<const uint4 *>(vs);
-                    z = max_bf16(ok0 ? max_bf16(x.x, x.y) : 0u, ok1 ? max_bf16(x.z, x.w) : 0u);
+                    z[0] = max_bf16(ok0 ? x.x : 0u, ok1 ? x.z : 0u);
+                    z[(NG - 1) / 2] = max_bf16(ok0 ? x.y : 0u, ok1 ? x.w : 0u);
                 } else if (NG == 2) {
                     const uint2 x = *reinterpret_cast<const uint2 *>(vs);
-                    z = max_bf16(ok0 ? x.x : 0u, ok1 ? x.y : 0u);
+                    z[0] = max_bf16(ok0 ? x.x : 0u, ok1 ? x.y : 0u);
                 } else {
-                    z = *reinterpret_cast<const uint32_t *>(vs);
-                    z = (ok0 ? z & 0xffffu : 0u) | (ok1 ? z & 0xffff0000u : 0u);
+                    const uint32_t x = *reinterpret_cast<const uint32_t *>(vs);
+                    z[0] = max_bf16(ok0 ? x & 0xffffu : 0u, ok1 ? x >> 16 : 0u);
                 }
-                z = max_bf16(z, big_run);
-                if (__any_sync(0xffffffffu, z != big_run)) {
-                    z = max_bf16(z, z << 16 | z >> 16);
+                bool more = false;
 #pragma unroll
-                    for (int d = 1; d < 32; d <<= 1) z = max_bf16(z, __shfl_xor_sync(0xffffffffu, z, d));
-                    big_run = z;
-                    E = (float)min(max((int)(z >> 23) - 127, -60), 100);
+                for (int i = 0; i < (NG + 1) / 2; ++i) {
+                    z[i] = max_bf16(z[i] | 0x001f001fu, big_run[i]);      // (two bits of the mantissa: seldom passed)
+                    more |= z[i] != big_run[i];
+                }
+                if (__any_sync(0xffffffffu, more)) {
+#pragma unroll
+                    for (int i = 0; i < (NG + 1) / 2; ++i) {
+#pragma unroll
+                        for (int d = 1; d < 32; d <<= 1) z[i] = max_bf16(z[i], __shfl_xor_sync(0xffffffffu, z[i], d));
+                        big_run[i] = z[i];
+                    }
+#pragma unroll
+                    for (int nt = 0; nt < NT; ++nt) {
+                        const float Fb = lane & 4 ? F[nt][1] : F[nt][0];
+                        q4_pass<NG>(pass[nt], Fb, q4_shared_ref(Fb, gains[warp][nt][(lane >> 3) % NG][c], lane), big_run, lane);
+                    }
+
                 }
             }
-            // kMask: some of the unit's tokens are hidden from some row, or not there.
-            auto work = [&](int step, auto masked) {
-                constexpr bool kMask = decltype(masked)::value;
+            // Some tiles of the unit.  kCareful: some of the unit's tokens are hidden from some row, or not there, or groups have
+            // references of their own (where that comes up on the way, the tiles are not added, and done again carefully).
+            auto work = [&](int step, auto careful) -> bool {
+                constexpr bool kCareful = decltype(careful)::value;
                 const unsigned char *tp0 = sp + step * TS * S::kTile;
                 const int t0 = t_unit + step * TS * kQ4Tile;
                 const uint32_t here = tiles >> (step * TS);
@@ -537,18 +629,18 @@ __global__ void __launch_bounds__(Q4Shape<D, NG, NT>::kThreads, q4_ctas_per_sm(N
                             sc[tl][nt][2] += f1 * acc[nt][2]; sc[tl][nt][3] += f1 * acc[nt][3];
                         }
                     }
-                    if (kMask)
+                    if (kCareful)
 #pragma unroll
                         for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
                             for (int i = 0; i < 4; ++i) {
                                 const int t = t0 + tl * kQ4Tile + g + (i >> 1) * 8;
-                                if (!(t < vis[nt][i & 1] && ((here >> tl) & 1))) sc[tl][nt][i] = -INFINITY;
+                                if (!(t < vis[nt * 8 + 2 * c + (i & 1)] && ((here >> tl) & 1))) sc[tl][nt][i] = -INFINITY;
                             }
                 }
                 // ---- softmax ----
-                bool passed = false;
                 float mx[NT][2];
+                bool passed = false;
 #pragma unroll
                 for (int nt = 0; nt < NT; ++nt) {
                     float fc[2];
@@ -558,32 +650,77 @@ __global__ void __launch_bounds__(Q4Shape<D, NG, NT>::kThreads, q4_ctas_per_sm(N
                         float x = fmaxf(sc[0][nt][b], sc[0][nt][b + 2]);
 #pragma unroll
                         for (int tl = 1; tl < TS; ++tl) x = fmaxf(x, fmaxf(sc[tl][nt][b], sc[tl][nt][b + 2]));
-                        mx[nt][b] = fmaf(x, fc[b], E);
-                        passed |= mx[nt][b] > F[nt][b] + kQ4Lag;
+                        mx[nt][b] = x * fc[b];
+                        passed |= mx[nt][b] > pass[nt][b];
                     }
                 }
-                if (__any_sync(0xffffffffu, passed)) {         // the reference follows
+                if (__any_sync(0xffffffffu, passed)) {         // references follow where a row's own tokens have passed them
+                    // value scales that differ by less than 2^kQ4Even in each group: a row's largest score and the largest scale will do
+                    // for its largest sum of the two
+                    bool even = true;
+                    uint32_t most = 0;                         // of the lane's group
+                    {
+                        const unsigned char *vs = sp + (lane >> 3) * S::kTile + q4_vs_base(D, NG) + (lane & 7) * 4 * NG;
+                        const bool tile_ok = (tiles >> (lane >> 3)) & 1;
+                        const bool ok0 = whole || (tile_ok && t_unit + 2 * lane < seg.T), ok1 = whole || (tile_ok && t_unit + 2 * lane + 1 < seg.T);
+#pragma unroll
+                        for (int k = 0; k < NG; ++k) {
+                            const uint32_t x = *reinterpret_cast<const unsigned short *>(vs + 2 * k), y = *reinterpret_cast<const unsigned short *>(vs + 2 * (NG + k));
+                            const uint32_t hi = __reduce_max_sync(0xffffffffu, max(ok0 ? x : 0u, ok1 ? y : 0u));
+                            const uint32_t lo = __reduce_min_sync(0xffffffffu, min(ok0 ? x : 0xffffu, ok1 ? y : 0xffffu));
+                            even &= hi < 0x7f80u && lo >= 0x80u && hi - lo < (uint32_t)kQ4Even << 7;
+                            if ((lane >> 3) % NG == k) most = hi;
+                        }
+                    }
 #pragma unroll
                     for (int nt = 0; nt < NT; ++nt) {
-                        float corr[2];
+                        if (NT > 1 && !__any_sync(0xffffffffu, mx[nt][0] > pass[nt][0] || mx[nt][1] > pass[nt][1])) continue;
+                        const float s0 = q4_max_rows(mx[nt][0]), s1 = q4_max_rows(mx[nt][1]), sx = lane & 4 ? s1 : s0;
+                        float x = sx + __log2f(__uint_as_float(most << 16));
+                        if (!even) {
+                            float fc[2], best[NG][2];          // the largest score + log2(value scale)
+                            f2_split(fcol[nt], fc[0], fc[1]);
 #pragma unroll
-                        for (int b = 0; b < 2; ++b) {
-                            float x = mx[nt][b];
-                            x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 4));
-                            x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 8));
-                            x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 16));
-                            const float Fn = x > kNegInf ? fmaxf(F[nt][b], x) : F[nt][b];
-                            corr[b] = ex2(F[nt][b] - Fn);
-                            F[nt][b] = Fn;
+                            for (int k = 0; k < NG; ++k) best[k][0] = best[k][1] = -INFINITY;
+#pragma unroll
+                            for (int tl = 0; tl < TS; ++tl) {
+                                uint32_t v0[(NG + 1) / 2], v1[(NG + 1) / 2];
+                                q4_scales<NG>(tp0 + tl * S::kTile + q4_vs_base(D, NG), g, v0, v1);
+#pragma unroll
+                                for (int k = 0; k < NG; ++k) { // (a scale that is not a number counts as none)
+                                    const float e0 = __log2f(k & 1 ? bf16hi_f(v0[k / 2]) : bf16lo_f(v0[k / 2])), e1 = __log2f(k & 1 ? bf16hi_f(v1[k / 2]) : bf16lo_f(v1[k / 2]));
+#pragma unroll
+                                    for (int b = 0; b < 2; ++b)
+                                        best[k][b] = fmaxf(best[k][b], fmaxf(fmaf(sc[tl][nt][b], fc[b], e0), fmaf(sc[tl][nt][b + 2], fc[b], e1)));
+                                }
+                            }
+                            x = q4_own_max<NG>(best, lane);
                         }
-                        float x, y;
-                        f2_split(l[nt], x, y);
-                        l[nt] = f2(x * corr[0], y * corr[1]);
+                        const float Fb = lane & 4 ? F[nt][1] : F[nt][0];
+                        const Q4Refs r = q4_follow(x, sx, Fb, refs[warp][nt][lane], q4_shared_ref(Fb, gains[warp][nt][(lane >> 3) % NG][c], lane), lane);
+                        refs[warp][nt][lane] = r.R;
+                        const uint32_t both = pack_bf16(r.gain, __shfl_down_sync(0xffffffffu, r.gain, 4));
+                        if (lane < 8 * NG && !(lane & 4)) gains[warp][nt][(lane >> 3) % NG][c] = both;
+                        __syncwarp();
+                        gained = (gained & ~(1u << nt)) | (uint32_t)__any_sync(0xffffffffu, r.gain != 1.f) << nt;
+                        float lx, ly;
+                        f2_split(l[nt], lx, ly);
+                        const float F0 = __shfl_sync(0xffffffffu, r.F, c), F1 = __shfl_sync(0xffffffffu, r.F, 4 | c);
+                        l[nt] = f2(lx * ex2(F[nt][0] - F0), ly * ex2(F[nt][1] - F1));
+                        F[nt][0] = F0;
+                        F[nt][1] = F1;
+                        if (__any_sync(0xffffffffu, r.corr != 1.f))
 #pragma unroll
-                        for (int i = 0; i < 2 * NW; ++i)
+                            for (int k = 0; k < NG; ++k) {
+                                const float c0 = __shfl_sync(0xffffffffu, r.corr, 8 * k + c), c1 = __shfl_sync(0xffffffffu, r.corr, 8 * k + 4 + c);
 #pragma unroll
-                            for (int k = 0; k < 4; ++k) o[nt][i][k] *= corr[k & 1];
+                                for (int i = 2 * k * WPG; i < 2 * (k + 1) * WPG; ++i)
+#pragma unroll
+                                    for (int m = 0; m < 4; ++m) o[nt][i][m] *= m & 1 ? c1 : c0;
+                            }
+                        q4_pass<NG>(pass[nt], r.F, r.A, big_run, lane);
                     }
+                    if (!kCareful && gained) return false;
                 }
 #pragma unroll
                 for (int nt = 0; nt < NT; ++nt) {
@@ -625,13 +762,16 @@ __global__ void __launch_bounds__(Q4Shape<D, NG, NT>::kThreads, q4_ctas_per_sm(N
                         for (int nt = 0; nt < NT; ++nt) {
                             const float *p = sc[tl][nt];
                             float w0 = p[0] * f0, w1 = p[1] * f0, w2 = p[2] * f1, w3 = p[3] * f1;
-                            if (kMask) {                       // a hidden token's weight is zero whatever its scale holds
+                            if (kCareful) {                    // a hidden token's weight is zero whatever its scale holds
+                                uint32_t gain;
+                                asm volatile("ld.shared.u32 %0, [%1];" : "=r"(gain) : "r"(gain_at + (nt * NG + k) * 16));
+                                w0 *= bf16lo_f(gain); w1 *= bf16hi_f(gain); w2 *= bf16lo_f(gain); w3 *= bf16hi_f(gain);
                                 const int t = t0 + tl * kQ4Tile + g;
                                 const bool ok = (here >> tl) & 1;
-                                if (!(ok && t < vis[nt][0])) w0 = 0.f;
-                                if (!(ok && t < vis[nt][1])) w1 = 0.f;
-                                if (!(ok && t + 8 < vis[nt][0])) w2 = 0.f;
-                                if (!(ok && t + 8 < vis[nt][1])) w3 = 0.f;
+                                if (!(ok && t < vis[nt * 8 + 2 * c + 0])) w0 = 0.f;
+                                if (!(ok && t < vis[nt * 8 + 2 * c + 1])) w1 = 0.f;
+                                if (!(ok && t + 8 < vis[nt * 8 + 2 * c + 0])) w2 = 0.f;
+                                if (!(ok && t + 8 < vis[nt * 8 + 2 * c + 1])) w3 = 0.f;
                             }
                             b0[nt] = movmatrix(pack_f16(w0, w1));
                             b1[nt] = movmatrix(pack_f16(w2, w3));
@@ -661,14 +801,11 @@ __global__ void __launch_bounds__(Q4Shape<D, NG, NT>::kThreads, q4_ctas_per_sm(N
                         }
                     }
                 }
+                return true;
             };
-            if (whole) {
 #pragma unroll 1
-                for (int step = 0; step < kQ4UnitTiles / TS; ++step) work(step, std::false_type());
-            } else {
-#pragma unroll 1
-                for (int step = 0; step < kQ4UnitTiles / TS; ++step) work(step, std::true_type());
-            }
+            for (int step = 0; step < kQ4UnitTiles / TS; ++step)
+                if (!(whole && gained == 0 && work(step, std::false_type()))) work(step, std::true_type());
             at += kCons;
             st_last = st;
             st += kCons;
@@ -693,13 +830,19 @@ __global__ void __launch_bounds__(Q4Shape<D, NG, NT>::kThreads, q4_ctas_per_sm(N
                 v += __shfl_xor_sync(0xffffffffu, v, 4);
                 v += __shfl_xor_sync(0xffffffffu, v, 8);
                 v += __shfl_xor_sync(0xffffffffu, v, 16);
-                if (g == 0) ml[warp][2 * c + b] = make_float2(F[nt][b], any ? v : 0.f);
+                // as a state whose l is from 1 to 2, so that m is near the largest score whatever the values' size
+                const int e = v > 0.f ? min(max((int)(__float_as_uint(v) >> 23) - 127, -120), 120) : 0;
+                if (g == 0) ml[warp][2 * c + b] = any ? make_float2(F[nt][b] + (float)e, v * q4_pow2(-e)) : make_float2(kNegInf, 0.f);
                 if (any)
 #pragma unroll
                     for (int w = 0; w < NW; ++w) {
                         const float *x = o[nt][2 * w], *y = o[nt][2 * w + 1];
+                        // (a gain is a power of two from 1 to 2^126: its inverse)
+                        const uint32_t gain = gains[warp][nt][w / WPG][c];
+                        const float f = __uint_as_float((254u << 23) - __float_as_uint(b ? bf16hi_f(gain) : bf16lo_f(gain)));
+                        const float fe = q4_pow2(-e);
                         *reinterpret_cast<float4 *>(mine + (2 * c + b) * S::kRowFloats + 32 * w + 4 * g) =
-                            make_float4(fmaf(-16.f, x[2 + b], x[b]), x[2 + b], fmaf(-16.f, y[2 + b], y[b]), y[2 + b]);
+                            make_float4(fmaf(-16.f, x[2 + b], x[b]) * f * fe, x[2 + b] * f * fe, fmaf(-16.f, y[2 + b], y[b]) * f * fe, y[2 + b] * f * fe);
                     }
             }
             consumers_sync();

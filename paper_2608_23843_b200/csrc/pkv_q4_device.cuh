@@ -12,7 +12,9 @@ namespace {
 
 constexpr int kQ4Unit = 64;            // tokens per unit: four tiles
 constexpr int kQ4UnitTiles = kQ4Unit / kQ4Tile;
-constexpr float kQ4Lag = 14.f;         // how far (base 2) scores may pass the softmax's reference before it follows: weights stay inside fp16
+constexpr float kQ4Lag = 14.f;         // how far (base 2) scores may pass the softmax's reference before it follows
+// Weights in fp16: a reference places the largest at 2^(kQ4Place - 1) .. 2^kQ4Place and follows when one has passed 2^kQ4Most.
+constexpr float kQ4Place = 8.f, kQ4Most = 15.9f;
 
 // A segment that begins in a CTA and ends in another (seq < 0: none); slot: where its first part is (see below)
 struct Q4Part { int seq, tile, head, slot, last_cta; };

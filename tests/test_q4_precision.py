@@ -62,6 +62,49 @@ def test_scores_beside_a_large_query_channel(n, G, dtype):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("n, G", ROWS[1:])
+@pytest.mark.parametrize("what", ["k", "v"])
+@pytest.mark.parametrize("power", [20, 40])
+def test_a_row_that_is_not_seen_does_not_matter_whatever_its_size(n, G, what, power):
+    """The last key or value row is far larger than the others: the queries before it do not see it."""
+    T = 300
+    k, v, q = randn(1, T, 1, 128), randn(2, T, 1, 128), randn(3, n, G, 128).to(BF16)
+    (k if what == "k" else v)[-1] *= 2.0 ** power
+    h = Held([k.to(BF16)], [v.to(BF16)], G=G)
+    ref, tol = h.expected(q, 0)
+    check(h.attend([q])[0, :-1], ref[:-1], tol[:-1])
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("n, G", ROWS)
+@pytest.mark.parametrize("dtype, g, power", [(BF16, 32, 12), (BF16, 32, 20), (BF16, 64, 26), (FP16, 32, 12), (FP16, 64, 20)])
+def test_channel_groups_of_different_sizes(n, G, dtype, g, power):
+    """The first group's values are 2^power times the others'."""
+    T = 400
+    v = randn(1, T, 1, 128) * 2.0 ** (-power // 2)
+    v[..., :g] *= 2.0 ** power
+    h = Held([randn(2, T, 1, 128).to(dtype)], [v.to(dtype)], G=G, g=g)
+    q = randn(3, n, G, 128).to(dtype)
+    check(h.attend([q])[0], *h.expected(q, 0))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("n, G", ROWS)
+@pytest.mark.parametrize("power", [8, 16, 25])
+def test_large_values_of_no_weight(n, G, power):
+    """Every seventh token has values 2^power times the others' and a weight of nothing."""
+    T = 300
+    k, v, q = randn(1, T, 1, 128), randn(2, T, 1, 128), randn(3, n, G, 128)
+    q[..., 0], k[..., 0] = 10.0, 0.0
+    k[3::7, :, 0] = -80.0                                  # 71 nepers below
+    v[3::7] *= 2.0 ** power
+    k[::7, :, 0] = -20.0                                   # and some between
+    h = Held([k.to(BF16)], [v.to(BF16)], G=G)
+    q = q.to(BF16)
+    check(h.attend([q])[0], *h.expected(q, 0))
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("n, G", ROWS)
 @pytest.mark.parametrize("dtype, power", [(BF16, 16), (BF16, 20), (BF16, 26), (FP16, 14)])
 def test_keys_and_queries_of_opposite_sizes(n, G, dtype, power):
@@ -73,3 +116,22 @@ def test_keys_and_queries_of_opposite_sizes(n, G, dtype, power):
     h = Held([k.to(dtype)], [randn(3, T, 1, 128).to(dtype)], G=G)
     q = q.to(dtype)
     check(h.attend([q])[0], *h.expected(q, 0))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("n, G", [(1, 4), (4, 4)])
+@pytest.mark.parametrize("weight", [0.97, 0.999])
+@pytest.mark.parametrize("ratio", [1, 16, 64])
+def test_one_token_with_nearly_all_the_weight(n, G, weight, ratio):
+    """A first token of small values that holds nearly all the weight, the rest spread thin over 33000; the first channel group
+    is `ratio` times the others."""
+    T = 33000
+    k, v, q = randn(1, T, 1, 128) * 0.05, 1 + 0.3 * randn(2, T, 1, 128), randn(3, n, G, 128)
+    q[..., 0], k[..., 0] = 16.0, 0.0
+    k[0, :, 0] = math.log(weight / (1 - weight) * T) / 16 * math.sqrt(128)
+    v[0] *= 2.0 ** -6
+    v[..., :32] *= ratio
+    h = Held([k.to(FP16)], [v.to(FP16)], G=G, room=0)
+    q = q.to(FP16)
+    # (the units of 64 tokens are spread over 14 CTAs at least, 7 warps or two halves each: 18 units of four runs at most)
+    check(h.attend([q])[0], *h.expected(q, 0, 80))
