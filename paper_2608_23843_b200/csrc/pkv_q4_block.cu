@@ -154,7 +154,8 @@ __device__ __forceinline__ void block_advance(const Q4AttentionArgs &a, BlockCur
 struct UnitInfo {
     float ek[kQ4UnitTiles];                         // powers of two taken out of the tiles' keys
     float ev[kQ4UnitTiles], ev_inv[kQ4UnitTiles];   // ... and values: exponents, and 2^-exponent
-    uint32_t v_nan[kQ4UnitTiles];                   // tokens with a value group that is not finite (stored as zeros here)
+    uint16_t v_nan[kQ4UnitTiles][4];                // per channel group: tokens whose values are not finite there (zeros here)
+    uint32_t any_nan[kQ4UnitTiles];                 // ... whether there are any
     uint32_t tiles, tokens;                         // which tiles are there; tokens of the sequence in the unit
 };
 
@@ -199,6 +200,7 @@ __global__ void __launch_bounds__(kBThreads, 1) q4_block_kernel(const __grid_con
     __shared__ uint32_t code_tiles[kCS], code_tokens[kCS];
     __shared__ UnitInfo info[kWS];
     __shared__ float2 ml_other[kBHalf];
+    __shared__ uint32_t bad_other[kBHalf];
     __shared__ long long sums[kBThreads / 32], found_at;
     __shared__ int found_seq, gave_up;
     __shared__ uint32_t tmem_slot;
@@ -411,22 +413,20 @@ __global__ void __launch_bounds__(kBThreads, 1) q4_block_kernel(const __grid_con
                 }
             }
             // exponents of the largest scales (lanes 0-15: keys of token `lane`, 16-31: values): as bits, which order like the values
-            uint32_t z = z2[0], nans = 0;
+            uint32_t z = z2[0], nans[NG] = {};
             if (NG == 4) z = __vmaxu2(z, z2[(NG - 1) / 2]);
             z = max(z & 0xffffu, z >> 16);
             if ((lane & 15) >= valid) z = 0u;
             bool plain = valid == kQ4Tile;                     // all tokens there, all groups finite
             if (__any_sync(0xffffffffu, z > 0x7f80u)) {        // a group that is not finite: look at the others of its token
-                const bool nan = z > 0x7f80u;
+                const bool there = z != 0u;
                 plain = false;
-                nans = __ballot_sync(0xffffffffu, nan) >> 16;
-                if (nan) {
-                    z = 0u;
+                z = 0u;
 #pragma unroll
-                    for (int k = 0; k < NG; ++k) {
-                        const uint32_t x = (z2[k / 2] >> (16 * (k & 1))) & 0xffffu;
-                        if (x <= 0x7f80u) z = max(z, x);
-                    }
+                for (int k = 0; k < NG; ++k) {
+                    const uint32_t x = there ? (z2[k / 2] >> (16 * (k & 1))) & 0xffffu : 0u;
+                    nans[k] = __ballot_sync(0xffffffffu, x > 0x7f80u) >> 16;
+                    if (x <= 0x7f80u) z = max(z, x);
                 }
             }
             const int ek = min(max((int)(__reduce_max_sync(0xffffffffu, lane < 16 ? z : 0u) >> 7) - 127, -60), 60);
@@ -437,7 +437,13 @@ __global__ void __launch_bounds__(kBThreads, 1) q4_block_kernel(const __grid_con
                 info[ws].ek[dw] = pow2(ek);
                 info[ws].ev[dw] = (float)ev;
                 info[ws].ev_inv[dw] = fv;
-                info[ws].v_nan[dw] = nans;
+                uint32_t any = 0;
+#pragma unroll
+                for (int k = 0; k < NG; ++k) {
+                    any |= nans[k];
+                    info[ws].v_nan[dw][k] = (uint16_t)nans[k];
+                }
+                info[ws].any_nan[dw] = any;
                 if (dw == 0) { info[ws].tiles = bits; info[ws].tokens = tokens; }
             }
             const uint32_t d0 = d_at[0] + ws * S::kWide, d1 = d_at[1] + ws * S::kWide;
@@ -557,6 +563,7 @@ __global__ void __launch_bounds__(kBThreads, 1) q4_block_kernel(const __grid_con
             const bool row_ok = j < c.q.n;
             const int i0 = two ? 0 : x, step = two ? 1 : 2;    // this half's units
             float F = kNegInf, l = 0.f;
+            uint32_t bad = 0;                                  // channel groups in which the row sees a value that is not finite
             if (i0 < n_units) {
                 // ---- Q: times a power of two that brings the row's largest magnitude to 1 .. 2, exact in fp16 ----
                 float f;
@@ -607,7 +614,12 @@ __global__ void __launch_bounds__(kBThreads, 1) q4_block_kernel(const __grid_con
                     const int t0 = (c.unit + i) * kQ4Unit, lim = min(vis - t0, (int)inf.tokens);
                     const uint32_t tiles = inf.tiles;
                     const bool masked = __any_sync(0xffffffffu, lim < kQ4Unit) || tiles != (1u << kQ4UnitTiles) - 1u;
-                    const bool nans = (inf.v_nan[0] | inf.v_nan[1] | inf.v_nan[2] | inf.v_nan[3]) != 0;
+                    if (inf.any_nan[0] | inf.any_nan[1] | inf.any_nan[2] | inf.any_nan[3])
+                        for (int k = 0; k < kQ4UnitTiles; ++k) {
+                            const uint32_t seen = (1u << min(max(lim - k * kQ4Tile, 0), kQ4Tile)) - 1u;
+#pragma unroll
+                            for (int b = 0; b < NG; ++b) bad |= (inf.v_nan[k][b] & seen) ? 1u << b : 0u;
+                        }
                     float fk[kQ4UnitTiles], ev[kQ4UnitTiles];
 #pragma unroll
                     for (int k = 0; k < kQ4UnitTiles; ++k) {
@@ -619,20 +631,10 @@ __global__ void __launch_bounds__(kBThreads, 1) q4_block_kernel(const __grid_con
                     tc_fence_after();
                     float sv[kQ4Unit];
                     tmem_ld<kQ4Unit>(t_s, reinterpret_cast<uint32_t *>(sv));
-                    if (masked) {
-                        uint32_t nan = 0;
+                    if (masked)
 #pragma unroll
                         for (int k = 0; k < kQ4Unit; ++k)
                             if (!(k < lim && (tiles >> (k / kQ4Tile) & 1))) sv[k] = -INFINITY;
-#pragma unroll
-                        for (int k = 0; k < kQ4UnitTiles; ++k) {
-                            const int m = min(max(lim - k * kQ4Tile, 0), kQ4Tile);
-                            nan |= inf.v_nan[k] & ((1u << m) - 1u);
-                        }
-                        if (nan) l = __int_as_float(0x7fc00000);
-                    } else if (nans) {
-                        l = __int_as_float(0x7fc00000);        // a value that is not finite: the row is not either
-                    }
                     // x = s * f 2^Ek + Ev, against a reference that the largest has not passed by more than 2^14
                     float top = -INFINITY;
 #pragma unroll
@@ -694,6 +696,7 @@ __global__ void __launch_bounds__(kBThreads, 1) q4_block_kernel(const __grid_con
             if (!two) {
                 if (x == 1) {
                     ml_other[r_half] = make_float2(F, l);
+                    bad_other[r_half] = bad;
                     tc_fence_before();
                     mbar_arrive(smem_u32(&state_ready));
                     if (!mbar_wait_warp(smem_u32(&state_read), ph_st, abort_flag)) { ok = false; break; }
@@ -707,6 +710,7 @@ __global__ void __launch_bounds__(kBThreads, 1) q4_block_kernel(const __grid_con
                         f1 = ex2(other.x - M);
                         F = M;
                         l = f0 * l + f1 * other.y;
+                        bad |= bad_other[r_half];
                     }
                 }
                 ph_st ^= 1;
@@ -739,6 +743,9 @@ __global__ void __launch_bounds__(kBThreads, 1) q4_block_kernel(const __grid_con
 #pragma unroll
                         for (int k = 0; k < 32; ++k) r[k] = __float_as_uint(fmaf(__uint_as_float(r1[k]), f1, __uint_as_float(r[k])));
                     }
+                    if (bad >> (b / WPG) & 1)                  // (a group is 32 channels or more)
+#pragma unroll
+                        for (int k = 0; k < 32; ++k) r[k] = 0x7fc00000u;
                     if (!complete) {                           // (16-byte aligned, unlike a row of the caller's states)
 #pragma unroll
                         for (int k = 0; k < 8; ++k)

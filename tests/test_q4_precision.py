@@ -135,3 +135,26 @@ def test_one_token_with_nearly_all_the_weight(n, G, weight, ratio):
     q = q.to(FP16)
     # (the units of 64 tokens are spread over 14 CTAs at least, 7 warps or two halves each: 18 units of four runs at most)
     check(h.attend([q])[0], *h.expected(q, 0, 80))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("n, G", ROWS + [(70, 4), (20, 4)])
+@pytest.mark.parametrize("room", [0, 3000])
+@pytest.mark.parametrize("value", [math.nan, math.inf])
+def test_a_value_that_is_not_finite_reaches_its_channel_group_only(n, G, room, value):
+    T, hit = 700, 650
+    k, v, q = (randn(i, *s).to(BF16) for i, s in enumerate(((T, 1, 128), (T, 1, 128), (n, G, 128))))
+    h = Held([k], [v], G=G, room=room)
+    bad = v.clone()
+    bad[hit, 0, 40] = value
+    h.cache.append_kv(h.table, h.lengths, k[None].cuda(), bad[None].cuda())
+    ref, tol = h.expected(q, 0)
+    sees = max(0, hit - (T - n))                           # the first query that sees it
+    outs = [h.attend([q])[0]]
+    st = h.cache.attention_partial(h.table, h.lengths, q[None].cuda())[0].cpu()
+    outs.append(st[..., :128] / st[..., 129:])
+    for out in outs:
+        check(out[:sees], ref[:sees], tol[:sees]) if sees else None
+        assert torch.isnan(out[sees:, :, 32:64]).all()
+        rest = [c for c in range(128) if not 32 <= c < 64]
+        check(out[..., rest], ref[..., rest], tol[..., rest])
