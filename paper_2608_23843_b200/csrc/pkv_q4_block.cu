@@ -46,7 +46,7 @@ struct BlockShape {
     static constexpr int kTile = kQ4Tile * (D + 4 * NG), kUnitBytes = kQ4UnitTiles * kTile, kCodes = (kUnitBytes + 127) / 128 * 128;
     static constexpr int kWideStages = 4, kFit = (222 * 1024 - kWideStages * kWide) / kCodes, kCodeStages = kFit < 8 ? kFit : 8;
     static constexpr int kSmem = kWideStages * kWide + kCodeStages * kCodes + 1024;                 // (+ alignment)
-    static_assert(kCodeStages >= 4 && kSmem <= 224 * 1024, "fits one CTA per SM");
+    static_assert(kCodeStages >= 4 && kSmem <= 220 * 1024, "fits one CTA per SM");
     // columns of tensor memory: o of both halves, Q of both (fp16 pairs), s of both
     static constexpr uint32_t kColO = 0, kColQ = 2 * D, kColS = kColQ + D;
     static_assert(kColS + 2 * kQ4Unit <= kBTmemCols, "fits tensor memory");
@@ -150,12 +150,20 @@ __device__ __forceinline__ void block_advance(const Q4AttentionArgs &a, BlockCur
     }
 }
 
+// A tile's scales lose one power of two, kBAbove above that of the first token's largest, which comes to 2^kBTop .. 2^(kBTop + 1): seven
+// times that fits fp16, and a scale 2^-29 of it times a code is still exact.  Where another token's largest is more than kBAbove
+// above or kBKeys below, the tile is uneven: each token has a power of two of its own.  (The tile's largest instead of the
+// first token's, by redux: 2048 positions 38 us slower.)
+constexpr uint32_t kBAbove = 2, kBKeys = 8;
+constexpr int kBTop = 12;
+
 // What the widening warps tell the rows about a unit.
-struct UnitInfo {
-    float ek[kQ4UnitTiles];                         // powers of two taken out of the tiles' keys
+struct __align__(16) UnitInfo {
+    float tk[kQ4Unit];                              // powers of two taken out of each token's keys, in uneven tiles
+    float ek[kQ4UnitTiles];                         // ... of the other tiles' keys (uneven: 1)
     float ev[kQ4UnitTiles], ev_inv[kQ4UnitTiles];   // ... and values: exponents, and 2^-exponent
+    uint8_t odd[kQ4UnitTiles];                      // 1: uneven keys, 4: values that are not finite
     uint16_t v_nan[kQ4UnitTiles][4];                // per channel group: tokens whose values are not finite there (zeros here)
-    uint32_t any_nan[kQ4UnitTiles];                 // ... whether there are any
     uint32_t tiles, tokens;                         // which tiles are there; tokens of the sequence in the unit
 };
 
@@ -429,21 +437,32 @@ __global__ void __launch_bounds__(kBThreads, 1) q4_block_kernel(const __grid_con
                     if (x <= 0x7f80u) z = max(z, x);
                 }
             }
-            const int ek = min(max((int)(__reduce_max_sync(0xffffffffu, lane < 16 ? z : 0u) >> 7) - 127, -60), 60);
+            // one for the tile's keys, or for each token
+            const uint32_t own = z >> 7, side = lane & 16, k_first = __shfl_sync(0xffffffffu, own, 0);
+            const uint32_t uneven = __ballot_sync(0xffffffffu, (lane & 15) < valid && (!side && z != 0u && own + kBKeys - k_first > kBKeys + kBAbove));
+            const bool each = uneven >> side & 0xffffu;
+            const int e = each ? min(max((int)own - 127 - kBTop, -80), 100) : 0;
+            const int ek = min(max((int)(k_first + kBAbove) - 127 - kBTop, -80), 100);
             const int ev = min(max((int)(__reduce_max_sync(0xffffffffu, lane < 16 ? 0u : z) >> 7) - 127, -60), 60);
-            const float fk = pow2(-ek), fv = pow2(-ev);
+            const float fv = pow2(-ev);
+            float fk[2];                                       // of tokens t_lane, t_lane + 8
+            fk[0] = fk[1] = pow2(-ek);
+            if (uneven)
+#pragma unroll
+                for (int half = 0; half < 2; ++half) fk[half] = pow2(-__shfl_sync(0xffffffffu, e, t_lane + 8 * half));
             if (wu > 0 && !mbar_wait_warp(smem_u32(&wide_empty[ws]), (wu - 1) & 1, abort_flag)) { ok = false; break; }
+            if (each && !side) info[ws].tk[dw * kQ4Tile + lane] = pow2(e);
             if (lane == 0) {
-                info[ws].ek[dw] = pow2(ek);
-                info[ws].ev[dw] = (float)ev;
-                info[ws].ev_inv[dw] = fv;
                 uint32_t any = 0;
 #pragma unroll
                 for (int k = 0; k < NG; ++k) {
                     any |= nans[k];
                     info[ws].v_nan[dw][k] = (uint16_t)nans[k];
                 }
-                info[ws].any_nan[dw] = any;
+                info[ws].ek[dw] = uneven ? 1.f : pow2(ek);
+                info[ws].odd[dw] = (uint8_t)((uneven ? 1 : 0) | (any ? 4 : 0));
+                info[ws].ev[dw] = (float)ev;
+                info[ws].ev_inv[dw] = fv;
                 if (dw == 0) { info[ws].tiles = bits; info[ws].tokens = tokens; }
             }
             const uint32_t d0 = d_at[0] + ws * S::kWide, d1 = d_at[1] + ws * S::kWide;
@@ -452,7 +471,7 @@ __global__ void __launch_bounds__(kBThreads, 1) q4_block_kernel(const __grid_con
                 uint32_t sk[NG], sv[NG];
 #pragma unroll
                 for (int k = 0; k < NG; ++k) {
-                    float x = (k & 1 ? bf16hi_f(ksc[half][k / 2]) : bf16lo_f(ksc[half][k / 2])) * fk;
+                    float x = (k & 1 ? bf16hi_f(ksc[half][k / 2]) : bf16lo_f(ksc[half][k / 2])) * fk[half];
                     float y = (k & 1 ? bf16hi_f(vsc[half][k / 2]) : bf16lo_f(vsc[half][k / 2])) * fv;
                     if (!plain) {
                         if (t_lane + 8 * half >= valid) x = y = 0.f;
@@ -565,7 +584,8 @@ __global__ void __launch_bounds__(kBThreads, 1) q4_block_kernel(const __grid_con
             float F = kNegInf, l = 0.f;
             uint32_t bad = 0;                                  // channel groups in which the row sees a value that is not finite
             if (i0 < n_units) {
-                // ---- Q: times a power of two that brings the row's largest magnitude to 1 .. 2, exact in fp16 ----
+                // ---- Q: times a power of two that brings the row's largest magnitude to 2^14 .. 2^15; channels 2^-28 (bf16: 2^-31) of it
+                // are exact in fp16 ----
                 float f;
                 {
                     const uint4 *qg = reinterpret_cast<const uint4 *>(reinterpret_cast<const unsigned short *>(a.q) + (long long)(c.q.first + j) * a.q_row + (long long)h * a.q_head);
@@ -578,7 +598,7 @@ __global__ void __launch_bounds__(kBThreads, 1) q4_block_kernel(const __grid_con
                     }
                     mx = max(mx & 0xffffu, mx >> 16);
                     const float big = H16 ? __half2float(__ushort_as_half((unsigned short)mx)) : __uint_as_float(mx << 16);
-                    const int e = min(max((int)(__float_as_uint(big) >> 23) - 127, -60), 60);
+                    const int e = min(max((int)(__float_as_uint(big) >> 23) - 127, -60), 60) - 14;
                     const float up = pow2(-e);
                     f = pow2(e) * geo.scale_log2e;
 #pragma unroll
@@ -612,14 +632,8 @@ __global__ void __launch_bounds__(kBThreads, 1) q4_block_kernel(const __grid_con
                     if (!mbar_wait_warp(smem_u32(&wide_full[ws]), ((u + i) / kWS) & 1, abort_flag)) { ok = false; break; }
                     const UnitInfo &inf = info[ws];
                     const int t0 = (c.unit + i) * kQ4Unit, lim = min(vis - t0, (int)inf.tokens);
-                    const uint32_t tiles = inf.tiles;
-                    const bool masked = __any_sync(0xffffffffu, lim < kQ4Unit) || tiles != (1u << kQ4UnitTiles) - 1u;
-                    if (inf.any_nan[0] | inf.any_nan[1] | inf.any_nan[2] | inf.any_nan[3])
-                        for (int k = 0; k < kQ4UnitTiles; ++k) {
-                            const uint32_t seen = (1u << min(max(lim - k * kQ4Tile, 0), kQ4Tile)) - 1u;
-#pragma unroll
-                            for (int b = 0; b < NG; ++b) bad |= (inf.v_nan[k][b] & seen) ? 1u << b : 0u;
-                        }
+                    const uint32_t tiles = inf.tiles, odd = *reinterpret_cast<const uint32_t *>(inf.odd);
+                    const bool special = __any_sync(0xffffffffu, lim < kQ4Unit || odd != 0u) || tiles != (1u << kQ4UnitTiles) - 1u;
                     float fk[kQ4UnitTiles], ev[kQ4UnitTiles];
 #pragma unroll
                     for (int k = 0; k < kQ4UnitTiles; ++k) {
@@ -631,10 +645,39 @@ __global__ void __launch_bounds__(kBThreads, 1) q4_block_kernel(const __grid_con
                     tc_fence_after();
                     float sv[kQ4Unit];
                     tmem_ld<kQ4Unit>(t_s, reinterpret_cast<uint32_t *>(sv));
-                    if (masked)
+                    if (special) {
+                        if (odd) {
+                            // each token's power of two, in tensor memory, four at a time: little code, out of the way of
+                            // the registers
+#pragma unroll 1
+                            for (int k = 0; k < kQ4UnitTiles; ++k) {
+                                const uint32_t un = odd >> (8 * k);
+                                const int see = tiles >> k & 1 ? lim : 0;
+                                if (un & 4u) {
+                                    const uint32_t seen = (1u << min(max(see - k * kQ4Tile, 0), kQ4Tile)) - 1u;
+#pragma unroll 1
+                                    for (int b = 0; b < NG; ++b) bad |= (inf.v_nan[k][b] & seen) ? 1u << b : 0u;
+                                }
+                                if (!(un & 1u)) continue;
+#pragma unroll 1
+                                for (int b = k * kQ4Tile; b < (k + 1) * kQ4Tile; b += 4) {
+                                    uint32_t r[4];
+                                    tmem_ld4(t_s + b, r);
+                                    tmem_ld_wait();
+#pragma unroll
+                                    for (int i = 0; i < 4; ++i) {
+                                        r[i] = __float_as_uint(__uint_as_float(r[i]) * inf.tk[b + i]);
+                                    }
+                                    tmem_st4(t_s + b, r);
+                                }
+                            }
+                            tmem_st_wait();
+                            tmem_ld<kQ4Unit>(t_s, reinterpret_cast<uint32_t *>(sv));
+                        }
 #pragma unroll
                         for (int k = 0; k < kQ4Unit; ++k)
                             if (!(k < lim && (tiles >> (k / kQ4Tile) & 1))) sv[k] = -INFINITY;
+                    }
                     // x = s * f 2^Ek + Ev, against a reference that the largest has not passed by more than 2^14
                     float top = -INFINITY;
 #pragma unroll

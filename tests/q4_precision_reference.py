@@ -22,11 +22,12 @@ def attention(q, k, v, group, first_position, scale, out_type, steps=None):
       the result's rounding to its type            eps / 2 of it
       weights (times S) rounded to fp16            2^-11 A
       ... those that are too small for that        fp16's smallest step is 2^-24, half of it 2^-25.  A kernel that places the largest w S of
-                                                   a query and channel group at 2^3 or above: 2^-28 max(w S) on each of w S, 7 times that in
-                                                   a sum with codes.  One that has weights for all groups alike, and takes S* of a
-                                                   token from a run of tokens whose S* differ by less than 2^4 (so that the
-                                                   largest is at 2^3 or above again): 2^-28 max(w S*) on each of w S*, so on the product
-                                                   with a value 2^-27 max(w S*) |value| / S* (a scale is less than twice its power of two)
+                                                   a query and channel group at 2 or above: 2^-26 max(w S) on each of w S, 7 times that in
+                                                   a sum with codes.  One that has weights for all groups alike and brings values to fp16
+                                                   with a power of two 2^E for a run of tokens, 2^(E - 4) <= S* < 2^(E + 1), its largest
+                                                   weight times 2^E at 2^5 or above: the largest w S* is 2^(5 - 4) of those units or more, a weight
+                                                   is off by 2^-25 2^-E of them, so w S* by 2^-25 max(w S*) and the product with a
+                                                   value by 2^-25 max(w S*) |value| / S*
       fp32 sums                                    a run of 16 products and the sum so far are aligned to the largest of the 17 and lose
                                                    less than 2^-25 of it each: 17 * 2^-25 < 2^-20 of sum(w S |c0 + 16 c1|) / l per run, with
                                                    |c0 + 16 c1| <= 119: two neighbouring codes share a product; c0 is a difference of sums.
@@ -56,9 +57,9 @@ def attention(q, k, v, group, first_position, scale, out_type, steps=None):
         A = w @ vv.abs() / l
         star = ss.amax(-1)
         per_group = torch.stack([(w * ss[:, i]).amax(-1) for i in range(ss.shape[1])], -1) / l               # max(w S) / l
-        own = (7 * 2.0 ** -28 * see[:, None] * per_group).repeat_interleave(group, -1)
+        own = (7 * 2.0 ** -26 * see[:, None] * per_group).repeat_interleave(group, -1)
         ratio = vv.abs() / star.clamp(min=1e-300)[:, None]
-        alike = 2.0 ** -27 * ((w * star).amax(-1, keepdim=True) / l) * ((~hidden).to(torch.float64) @ ratio)
+        alike = 2.0 ** -25 * ((w * star).amax(-1, keepdim=True) / l) * ((~hidden).to(torch.float64) @ ratio)
         sums = (119 * 2.0 ** -20 * runs * (w @ ss) / l).repeat_interleave(group, -1)
         size = ((q[:, h].abs() @ kk.abs().T) * to2).masked_fill(hidden, 0.0).amax(-1, keepdim=True)
         ds = (2.0 ** -20 * d / 16 + 2.0 ** -23 * d / group) * size + 2.0 ** -22 * (size + 64)

@@ -10,8 +10,9 @@ from q4_precision_reference import attention
 from q4_reference import Rows, offsets_of, quantised
 
 BF16, FP16 = torch.bfloat16, torch.float16
-# new positions and query heads per KV head: eight query rows at a time, sixteen
+# new positions and query heads per KV head: eight query rows at a time, sixteen; row blocks of both halves, of one
 ROWS = [(1, 4), (2, 4), (4, 4)]
+BLOCKS = [(70, 4), (20, 4)]
 
 
 class Held:
@@ -48,7 +49,7 @@ def check(out, ref, tol):
 
 
 @pytest.mark.gpu
-@pytest.mark.parametrize("n, G", ROWS)
+@pytest.mark.parametrize("n, G", ROWS + BLOCKS)
 @pytest.mark.parametrize("dtype", [BF16, FP16])
 def test_scores_beside_a_large_query_channel(n, G, dtype):
     """A query's large channel meets keys whose codes are zero there: it must not cost the other channels' products."""
@@ -62,8 +63,7 @@ def test_scores_beside_a_large_query_channel(n, G, dtype):
 
 
 @pytest.mark.gpu
-@pytest.mark.parametrize("n, G", ROWS[1:])
-@pytest.mark.parametrize("what", ["k", "v"])
+@pytest.mark.parametrize("n, G, what", [(*x, w) for w in "kv" for x in ROWS[1:]] + [(*x, "k") for x in BLOCKS])
 @pytest.mark.parametrize("power", [20, 40])
 def test_a_row_that_is_not_seen_does_not_matter_whatever_its_size(n, G, what, power):
     """The last key or value row is far larger than the others: the queries before it do not see it."""
@@ -105,7 +105,7 @@ def test_large_values_of_no_weight(n, G, power):
 
 
 @pytest.mark.gpu
-@pytest.mark.parametrize("n, G", ROWS)
+@pytest.mark.parametrize("n, G", ROWS + BLOCKS)
 @pytest.mark.parametrize("dtype, power", [(BF16, 16), (BF16, 20), (BF16, 26), (FP16, 14)])
 def test_keys_and_queries_of_opposite_sizes(n, G, dtype, power):
     """The first group's keys are 2^power times the others', and the queries' channels there as much smaller."""
@@ -138,7 +138,7 @@ def test_one_token_with_nearly_all_the_weight(n, G, weight, ratio):
 
 
 @pytest.mark.gpu
-@pytest.mark.parametrize("n, G", ROWS + [(70, 4), (20, 4)])
+@pytest.mark.parametrize("n, G", ROWS + BLOCKS)
 @pytest.mark.parametrize("room", [0, 3000])
 @pytest.mark.parametrize("value", [math.nan, math.inf])
 def test_a_value_that_is_not_finite_reaches_its_channel_group_only(n, G, room, value):
