@@ -7,14 +7,15 @@
 //     one warp       looks up pages and copies a unit's tiles of codes and scales into a ring,
 //     four warps     widen, a tile each: codes times scales as fp16 into shared memory, in the layouts the products read
 //                    (128-byte swizzle, panels of 64 channels).  A code (3 bits and a sign) times a bf16 scale (8 bits) has
-//                    11 bits, so fp16 holds it exactly; a power of two per tile (the exponent of its largest scale, handed on
-//                    to the rows) keeps it inside fp16's range whatever the values' size,
+//                    11 bits, so fp16 holds it exactly where the scale is in its range: a power of two per tile, or per token in tiles of
+//                    uneven sizes, is handed on to the rows, and what is left lies at the upper end of the range, so that a channel group
+//                    2^-18 (in most tiles 2^-26) of the tile's largest is exact too,
 //     one warp       issues the products, one lane: s = Q K^T with Q and, later, p as row operands in tensor memory,
 //                    o += p V; while one half's rows are in their softmax the other half's products run,
-//     eight warps    softmax (fp32): s from tensor memory, p as fp16 back over it, o rescaled only when the running reference has been
-//                    passed by 2^14 (p stays inside fp16).
-// Measured: 2048 positions against 32K (32 / 8 heads, d = 128, g = 32; 1.07 TFLOP, one call) 1190 us, 895 TFLOP/s; 5 x 37
-// positions of sequences up to 4001 (28 / 4 heads, d = 64) 27 us, of which the launch, the partition, the first units, the last
+//     eight warps    softmax (fp32): s from tensor memory, p as fp16 back over it, o rescaled only when a row's weights may have passed
+//                    fp16's range (see kQ4Place).
+// Measured: 2048 positions against 32K (32 / 8 heads, d = 128, g = 32; 1.07 TFLOP, one call) 1254 us, 850 TFLOP/s; 5 x 37
+// positions of sequences up to 4001 (28 / 4 heads, d = 64) 28 us, of which the launch, the partition, the first units, the last
 // states and the join are most.
 // What bounds it: products and exponentials each take 1024 cycles per unit of 256 rows, but a half's chain - s, softmax, o,
 // the hand-overs between them - is some 1800 cycles long even with both for free, and the widening competes with the softmax
@@ -152,17 +153,20 @@ __device__ __forceinline__ void block_advance(const Q4AttentionArgs &a, BlockCur
 
 // A tile's scales lose one power of two, kBAbove above that of the first token's largest, which comes to 2^kBTop .. 2^(kBTop + 1): seven
 // times that fits fp16, and a scale 2^-29 of it times a code is still exact.  Where another token's largest is more than kBAbove
-// above or kBKeys below, the tile is uneven: each token has a power of two of its own.  (The tile's largest instead of the
+// above or kBKeys (kBValues) below, the tile is uneven: each token has a power of two of its own.  (The tile's largest instead of the
 // first token's, by redux: 2048 positions 38 us slower.)
-constexpr uint32_t kBAbove = 2, kBKeys = 8;
+constexpr uint32_t kBAbove = 2, kBKeys = 8, kBValues = 2;
 constexpr int kBTop = 12;
+// (values that are zero count as the least there are: their tokens' weights must not set the reference that all share)
+constexpr int kBLeast = -80;                        // least exponent: below those of all values of the documented range, far above fp32's least
 
 // What the widening warps tell the rows about a unit.
 struct __align__(16) UnitInfo {
     float tk[kQ4Unit];                              // powers of two taken out of each token's keys, in uneven tiles
+    float tv[kQ4Unit];                              // ... of its values: exponents
     float ek[kQ4UnitTiles];                         // ... of the other tiles' keys (uneven: 1)
-    float ev[kQ4UnitTiles], ev_inv[kQ4UnitTiles];   // ... and values: exponents, and 2^-exponent
-    uint8_t odd[kQ4UnitTiles];                      // 1: uneven keys, 4: values that are not finite
+    float ev[kQ4UnitTiles], ev_inv[kQ4UnitTiles];   // ... and values: exponents, and 2^-exponent (uneven: 0, 0)
+    uint8_t odd[kQ4UnitTiles];                      // 1: uneven keys, 2: uneven values, 4: values that are not finite
     uint16_t v_nan[kQ4UnitTiles][4];                // per channel group: tokens whose values are not finite there (zeros here)
     uint32_t tiles, tokens;                         // which tiles are there; tokens of the sequence in the unit
 };
@@ -437,21 +441,24 @@ __global__ void __launch_bounds__(kBThreads, 1) q4_block_kernel(const __grid_con
                     if (x <= 0x7f80u) z = max(z, x);
                 }
             }
-            // one for the tile's keys, or for each token
-            const uint32_t own = z >> 7, side = lane & 16, k_first = __shfl_sync(0xffffffffu, own, 0);
-            const uint32_t uneven = __ballot_sync(0xffffffffu, (lane & 15) < valid && (!side && z != 0u && own + kBKeys - k_first > kBKeys + kBAbove));
+            // one for the tile's keys and one for its values, or for each token
+            const uint32_t own = z >> 7, side = lane & 16, k_first = __shfl_sync(0xffffffffu, own, 0), v_first = __shfl_sync(0xffffffffu, own, 16);
+            const uint32_t uneven = __ballot_sync(0xffffffffu, (lane & 15) < valid && (side ? own + kBValues - v_first > kBValues + kBAbove || v_first == 0u : z != 0u && own + kBKeys - k_first > kBKeys + kBAbove));
             const bool each = uneven >> side & 0xffffu;
-            const int e = each ? min(max((int)own - 127 - kBTop, -80), 100) : 0;
-            const int ek = min(max((int)(k_first + kBAbove) - 127 - kBTop, -80), 100);
-            const int ev = min(max((int)(__reduce_max_sync(0xffffffffu, lane < 16 ? 0u : z) >> 7) - 127, -60), 60);
-            const float fv = pow2(-ev);
-            float fk[2];                                       // of tokens t_lane, t_lane + 8
+            const int top = 127 + kBTop, e = each ? min(max((int)own - top, kBLeast), 100) : 0;
+            const int ek = min(max((int)(k_first + kBAbove) - top, kBLeast), 100), ev = min(max((int)(v_first + kBAbove) - top, kBLeast), 100);
+            float fk[2], fv[2];                                // of tokens t_lane, t_lane + 8
             fk[0] = fk[1] = pow2(-ek);
+            fv[0] = fv[1] = pow2(-ev);
             if (uneven)
 #pragma unroll
-                for (int half = 0; half < 2; ++half) fk[half] = pow2(-__shfl_sync(0xffffffffu, e, t_lane + 8 * half));
+                for (int half = 0; half < 2; ++half) {
+                    const int x = __shfl_sync(0xffffffffu, e, t_lane + 8 * half), y = __shfl_sync(0xffffffffu, e, 16 + t_lane + 8 * half);
+                    if (uneven & 0xffffu) fk[half] = pow2(-x);
+                    if (uneven >> 16) fv[half] = pow2(-y);
+                }
             if (wu > 0 && !mbar_wait_warp(smem_u32(&wide_empty[ws]), (wu - 1) & 1, abort_flag)) { ok = false; break; }
-            if (each && !side) info[ws].tk[dw * kQ4Tile + lane] = pow2(e);
+            if (each) (side ? info[ws].tv : info[ws].tk)[dw * kQ4Tile + (lane & 15)] = side ? (float)e : pow2(e);
             if (lane == 0) {
                 uint32_t any = 0;
 #pragma unroll
@@ -459,10 +466,10 @@ __global__ void __launch_bounds__(kBThreads, 1) q4_block_kernel(const __grid_con
                     any |= nans[k];
                     info[ws].v_nan[dw][k] = (uint16_t)nans[k];
                 }
-                info[ws].ek[dw] = uneven ? 1.f : pow2(ek);
-                info[ws].odd[dw] = (uint8_t)((uneven ? 1 : 0) | (any ? 4 : 0));
-                info[ws].ev[dw] = (float)ev;
-                info[ws].ev_inv[dw] = fv;
+                info[ws].ek[dw] = uneven & 0xffffu ? 1.f : pow2(ek);
+                info[ws].ev[dw] = uneven >> 16 ? 0.f : (float)ev;
+                info[ws].ev_inv[dw] = uneven >> 16 ? 0.f : pow2(-ev);
+                info[ws].odd[dw] = (uint8_t)((uneven & 0xffffu ? 1 : 0) | (uneven >> 16 ? 2 : 0) | (any ? 4 : 0));
                 if (dw == 0) { info[ws].tiles = bits; info[ws].tokens = tokens; }
             }
             const uint32_t d0 = d_at[0] + ws * S::kWide, d1 = d_at[1] + ws * S::kWide;
@@ -472,7 +479,7 @@ __global__ void __launch_bounds__(kBThreads, 1) q4_block_kernel(const __grid_con
 #pragma unroll
                 for (int k = 0; k < NG; ++k) {
                     float x = (k & 1 ? bf16hi_f(ksc[half][k / 2]) : bf16lo_f(ksc[half][k / 2])) * fk[half];
-                    float y = (k & 1 ? bf16hi_f(vsc[half][k / 2]) : bf16lo_f(vsc[half][k / 2])) * fv;
+                    float y = (k & 1 ? bf16hi_f(vsc[half][k / 2]) : bf16lo_f(vsc[half][k / 2])) * fv[half];
                     if (!plain) {
                         if (t_lane + 8 * half >= valid) x = y = 0.f;
                         if (y != y) y = 0.f;                   // (a value that is not finite: told to the rows by v_nan)
@@ -645,9 +652,10 @@ __global__ void __launch_bounds__(kBThreads, 1) q4_block_kernel(const __grid_con
                     tc_fence_after();
                     float sv[kQ4Unit];
                     tmem_ld<kQ4Unit>(t_s, reinterpret_cast<uint32_t *>(sv));
+                    float apart = 0.f, apart_m = kNegInf;      // sum of the weights of tiles with uneven values, relative to 2^apart_m
                     if (special) {
                         if (odd) {
-                            // each token's power of two, in tensor memory, four at a time: little code, out of the way of
+                            // each token's powers of two, in tensor memory, four at a time: little code, out of the way of
                             // the registers
 #pragma unroll 1
                             for (int k = 0; k < kQ4UnitTiles; ++k) {
@@ -658,7 +666,8 @@ __global__ void __launch_bounds__(kBThreads, 1) q4_block_kernel(const __grid_con
 #pragma unroll 1
                                     for (int b = 0; b < NG; ++b) bad |= (inf.v_nan[k][b] & seen) ? 1u << b : 0u;
                                 }
-                                if (!(un & 1u)) continue;
+                                if (!(un & 3u)) continue;
+                                const float fx = fmaxf(f * inf.ek[k], 1.2e-38f);
 #pragma unroll 1
                                 for (int b = k * kQ4Tile; b < (k + 1) * kQ4Tile; b += 4) {
                                     uint32_t r[4];
@@ -666,19 +675,33 @@ __global__ void __launch_bounds__(kBThreads, 1) q4_block_kernel(const __grid_con
                                     tmem_ld_wait();
 #pragma unroll
                                     for (int i = 0; i < 4; ++i) {
-                                        r[i] = __float_as_uint(__uint_as_float(r[i]) * inf.tk[b + i]);
+                                        float x = __uint_as_float(r[i]);
+                                        if (un & 1u) x *= inf.tk[b + i];
+                                        if (un & 2u) {
+                                            x *= fx;
+                                            if (b + i < see) {
+                                                const float m = fmaxf(apart_m, x);
+                                                apart = apart * ex2(apart_m - m) + ex2(x - m);
+                                                apart_m = m;
+                                            }
+                                            x += inf.tv[b + i];
+                                        }
+                                        r[i] = __float_as_uint(x);
                                     }
                                     tmem_st4(t_s + b, r);
                                 }
                             }
                             tmem_st_wait();
                             tmem_ld<kQ4Unit>(t_s, reinterpret_cast<uint32_t *>(sv));
+#pragma unroll
+                            for (int k = 0; k < kQ4UnitTiles; ++k)
+                                if (odd >> (8 * k) & 2u) fk[k] = 1.f;      // (its columns are x itself)
                         }
 #pragma unroll
                         for (int k = 0; k < kQ4Unit; ++k)
                             if (!(k < lim && (tiles >> (k / kQ4Tile) & 1))) sv[k] = -INFINITY;
                     }
-                    // x = s * f 2^Ek + Ev, against a reference that the largest has not passed by more than 2^14
+                    // x = s * f 2^Ek + Ev, against a reference of the row's own
                     float top = -INFINITY;
 #pragma unroll
                     for (int k = 0; k < kQ4UnitTiles; ++k) {
@@ -689,8 +712,8 @@ __global__ void __launch_bounds__(kBThreads, 1) q4_block_kernel(const __grid_con
                         m0 = max3(m0, p[14], p[15]);
                         top = fmaxf(top, fmaf(fmaxf(m0, m1), fk[k], ev[k]));
                     }
-                    if (__any_sync(0xffffffffu, top > F + kQ4Lag)) {
-                        const float Fn = top > kNegInf ? fmaxf(F, top) : F, corr = ex2(F - Fn);
+                    if (__any_sync(0xffffffffu, top > F + kQ4Most)) {
+                        const float Fn = top > F + kQ4Most ? ceilf(top) - kQ4Place : F, corr = ex2(F - Fn);
                         F = Fn;
                         l *= corr;
                         if (i > i0) {                          // (every earlier product of this half is complete: s was committed behind it)
@@ -724,6 +747,7 @@ __global__ void __launch_bounds__(kBThreads, 1) q4_block_kernel(const __grid_con
                         f2_unpack(f2_add(sum[0], sum[1]), s0, s1);
                         l = fmaf(s0 + s1, inf.ev_inv[k], l);
                     }
+                    l = fmaf(apart, ex2(apart_m - F), l);
                     tmem_st32(t_s, pk);
                     tmem_st_wait();
                     tc_fence_before();
@@ -762,7 +786,16 @@ __global__ void __launch_bounds__(kBThreads, 1) q4_block_kernel(const __grid_con
             if (two || x == 0) {
                 const bool complete = c.unit == 0 && n_units == c.units;
                 const int slot = u == 0 ? 0 : 1, r_block = (two ? x * kBHalf : 0) + r_half;
-                const float inv = complete && !a.state ? (l != 0.f ? 1.f / l : 0.f) : 1.f;
+                // (a state with l from 1 to 2, so that m is near the largest score whatever the values' size)
+                float inv = 1.f;
+                if (complete && !a.state) {
+                    inv = l != 0.f ? 1.f / l : 0.f;
+                } else if (l > 0.f) {
+                    const int e = min(max((int)(__float_as_uint(l) >> 23) - 127, -120), 120);
+                    inv = pow2(-e);
+                    l *= inv;
+                    F += (float)e;
+                }
                 const bool merge = !two && n_units > 1;
                 f0 *= inv;
                 f1 *= inv;
