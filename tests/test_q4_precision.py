@@ -159,3 +159,31 @@ def test_a_value_that_is_not_finite_reaches_its_channel_group_only(n, G, room, v
         assert torch.isnan(out[sees:, :, 32:64]).all()
         rest = [c for c in range(128) if not 32 <= c < 64]
         check(out[..., rest], ref[..., rest], tol[..., rest])
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("n, G", ROWS + BLOCKS)
+@pytest.mark.parametrize("d, g, P", [(128, 32, 64), (128, 64, 16), (128, 128, 32), (64, 32, 32), (64, 64, 128)])
+@pytest.mark.parametrize("seed", range(2))
+def test_sizes_drawn_at_random(n, G, d, g, P, seed):
+    """Every token and channel group has a size of its own; some tokens are zero; sequences of several lengths, in several shares."""
+    gen = torch.Generator().manual_seed(100 * seed + n)
+    power = lambda lo, hi, *s: torch.exp2(torch.randint(lo, hi + 1, s, generator=gen).float())      # noqa: E731
+    H = 2
+    k, v, qs = [], [], []
+    groups = power(-8, 8, H, d // g, 1)                    # of the keys; the queries the other way round
+    for T in (n, 37 + n, 300, 901):
+        some = (torch.rand(T, 1, 1, 1, generator=gen) < 0.3).float()
+        kt, vt = (torch.randn(T, H, d // g, g, generator=gen) for _ in "kv")
+        kt = kt * groups * torch.where(some > 0, power(-16, 1, T, 1, 1, 1), torch.ones(1))
+        vt = vt * power(-12, 12, T, H, d // g, 1) * torch.where(some > 0, power(-20, 20, T, 1, 1, 1), torch.ones(1))
+        zero = torch.rand(T, 1, 1, 1, generator=gen) < 0.05
+        k.append(kt.masked_fill(zero, 0.0).flatten(2).to(BF16))
+        v.append(vt.masked_fill(zero.roll(1, 0) & (torch.arange(T) > 0).view(T, 1, 1, 1), 0.0).flatten(2).to(BF16))
+        q = torch.randn(n, H, G, d // g, g, generator=gen) / groups[:, None]
+        qs.append(q.view(n, H * G, d).to(BF16))
+    h = Held(k, v, G=G, g=g, P=P, room=3000 * seed)
+    out = h.attend(qs)
+    for s, q in enumerate(qs):
+        check(out[s], *h.expected(q, s))
+    assert h.cache.stats() == {"device_timeouts": 0, "bad_pages": 0, "bad_lengths": 0}
