@@ -507,8 +507,9 @@ pkv_status pkv_get_row_block_ranges(int64_t n_row_blocks, int32_t longest_tokens
  * Rows of a call: sequence s owns rows offsets[s] .. offsets[s + 1] - 1 of the caller's buffers (offsets [device] int32
  * [n_seqs + 1], not decreasing, or NULL: n_rows / n_seqs rows each), n in all, and they are its LAST positions: row j of
  * n has position T - n + j, with T counting these rows (so set lengths, then append, then attend, all with the same
- * arrays).  n = 0 is fine.  Rows of the buffers before offsets[0] or from offsets[n_seqs] on belong to nobody: they are
- * neither read nor written.
+ * arrays).  n = 0 is fine (a call needs one sequence at least).  Rows of the buffers before offsets[0] or from
+ * offsets[n_seqs] on belong to nobody: they are not written and what they hold does not matter (append may read them, so all
+ * n_rows rows have to exist).
  * Arrays are read when the kernels run.  Contents that make no sense never lead outside a buffer: a page number outside
  * the pool (its tokens are skipped: not written, not read, not attended to), a length outside [0, max_pages *
  * page_size] (held inside it) and rows beyond a sequence's start (skipped) are counted in pkv_q4_stats.
@@ -516,7 +517,12 @@ pkv_status pkv_get_row_block_ranges(int64_t n_row_blocks, int32_t longest_tokens
  * adjacent; multiples of 8, base addresses 16-byte aligned, rows and heads not overlapping (slices of a fused projection
  * output can be passed as they are).
  * Every call is asynchronous on `stream`, may be captured into a CUDA graph, and must be made with the cache's device
- * current (PKV_ERR_INVALID_ARG otherwise).  The cache object keeps no scratch: calls on different streams may overlap as
+ * current (PKV_ERR_INVALID_ARG otherwise).  Work that follows on the stream sees what a call wrote, as always; but the kernels
+ * let a kernel launched with programmatic stream serialization (cudaLaunchAttributeProgrammaticStreamSerialization, never set unless
+ * asked for) start early, so such a kernel of the caller's own has to execute griddepcontrol.wait (cudaGridDependencySynchronize)
+ * in every launch, even one that reads nothing of this library: a later call waits for the kernel just before it, and through it
+ * for the ones before that.  (Caches of this library with decode_overlap = 2, which do not wait, are allowed for: once a process has
+ * made one, the kernels here are launched the ordinary way and let nothing start early.)  The cache object keeps no scratch: calls on different streams may overlap as
  * long as the caller orders writes of a page against its other uses and gives each attention call in flight a workspace
  * of its own.  The object is not thread-safe.  Results are bit-identical from run to run.
  * Dry-run mode as above: pool and meta NULL, calls only validate.
@@ -580,15 +586,24 @@ pkv_status pkv_q4_read_kv(pkv_q4_cache *c, int32_t n_seqs, const int32_t *page_t
  *         as pkv_decode_attention_partial() writes them (with l = 0 for a query that sees nothing; m is a reference near
  *         the largest score, in base-2 units, and o and l are relative to 2^m): pkv_merge_attention_states() merges such states with
  *         those of other caches (recent tokens in a dense / factor cache, older ones here)
- *   max_q_len   a host-side bound of n over the sequences (rows of a sequence beyond it are left as they were and counted
- *               as bad lengths; 0: no sequence has rows); ignored without offsets
- *   max_len     a host-side estimate of the longest T that only steers how the work is spread; 0 = max_pages * page_size
- *   workspace   [device] pkv_q4_attention_workspace(n_seqs, max_q_len, max_len) bytes, 16-byte aligned; contents before
- *               and after do not matter.  NULL where that is 0.
- * Scores, softmax and sums are held in fp32; codes times scale enter the products exactly, the weights rounded to fp16.
- * That holds for magnitudes of q, k and v from 2^-60 to 2^60 (every fp16 value lies inside); of larger ones products may
- * become infinite or NaN, smaller ones may count as zero.  A query, key or value that is not finite makes the results that
- * depend on it NaN or meaningless, and no others.
+ *   max_q_len   a host-side bound of n over the sequences, at most n_rows (rows of a sequence beyond it are left as they were and
+ *               counted as bad lengths; 0: no sequence has rows); ignored without offsets, where it is n_rows / n_seqs
+ *   max_len     a host-side estimate of the longest T that only steers how the work is spread; 0, or more than that, stands for
+ *               max_pages * page_size
+ *   workspace   [device] pkv_q4_attention_workspace() bytes, 16-byte aligned; contents before and after do not matter.  NULL where
+ *               that is 0.  The size goes by the max_q_len and max_len that the call uses, 1 or more each: pass
+ *               n_rows / n_seqs and max_pages * page_size where the call takes these
+ * Accuracy.  Codes, scales and queries enter the products exactly, scores, softmax statistics and sums are held in fp32, and the
+ * weights are rounded to fp16.  With up to 32 query rows (n * H_q / H_kv) per KV head a weight is rounded together with the value's scale, by
+ * 2^-11 of itself or 2^-26 of the largest such product of its query and channel group, whichever is more; with more rows by
+ * 2^-11 of itself or, together with the row's largest scale, by 2^-25 of the largest such product of its query.  Only rows that a query
+ * sees count for it, and sizes may differ from token to token and from channel group to channel group: query channels down to 2^-24 of a
+ * query's largest (bf16: 2^-27) are exact; with more than 32 rows, so are channel groups down to 2^-18 (values: 2^-25) of their row's largest,
+ * smaller ones are rounded by 2^-27 (2^-33) of that.
+ * That holds for magnitudes of q, k and v from 2^-60 to 2^60 (every fp16 value lies inside) and for values of a sequence that differ by
+ * less than 2^100; of larger ones products may become infinite or NaN, smaller ones may count as zero.  A query or key that is not
+ * finite makes the results that depend on it NaN or meaningless, and no others; a value that is not finite makes its channel
+ * group of the results of the queries that see it NaN.
  */
 pkv_status pkv_q4_attention_workspace(const pkv_q4_cache *c, int32_t n_seqs, int32_t max_q_len, int32_t max_len,
                                       int64_t *bytes);

@@ -8,8 +8,8 @@
 //     four warps     widen, a tile each: codes times scales as fp16 into shared memory, in the layouts the products read
 //                    (128-byte swizzle, panels of 64 channels).  A code (3 bits and a sign) times a bf16 scale (8 bits) has
 //                    11 bits, so fp16 holds it exactly where the scale is in its range: a power of two per tile, or per token in tiles of
-//                    uneven sizes, is handed on to the rows, and what is left lies at the upper end of the range, so that a channel group
-//                    2^-18 (in most tiles 2^-26) of the tile's largest is exact too,
+//                    uneven sizes, is handed on to the rows, and what is left lies at the upper end of the range, so that channel groups
+//                    down to 2^-18 (values: 2^-25) of their row's largest are exact too,
 //     one warp       issues the products, one lane: s = Q K^T with Q and, later, p as row operands in tensor memory,
 //                    o += p V; while one half's rows are in their softmax the other half's products run,
 //     eight warps    softmax (fp32): s from tensor memory, p as fp16 back over it, o rescaled only when a row's weights may have passed

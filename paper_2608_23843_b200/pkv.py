@@ -670,8 +670,9 @@ class Q4Cache:
 
     def attention(self, page_table, lengths, q, out=None, offsets=None, max_q_len=None, max_len=0):
         """Attention of the newest positions over the cache; out (default: a new tensor of q's shape) is returned.  With
-        offsets, max_q_len bounds the rows of a sequence (default: all rows); it and max_len, the longest length expected,
-        choose the kernel and how the work is spread, so tight ones are faster."""
+        offsets, max_q_len bounds the rows of a sequence (default, and at most: all rows); it and max_len, the longest length
+        expected, choose the kernel and how the work is spread, so tight ones are faster.  Rows that belong to no sequence are
+        left as they were (undefined in a new tensor); without rows nothing is done."""
         if out is None:
             out = torch.empty_like(q, memory_format=torch.contiguous_format)
         elif out.shape != q.shape:
