@@ -125,11 +125,12 @@ __device__ __forceinline__ float q4_max_rows(float x) {
     return fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 16));
 }
 
-// The softmax's references of a query row (a column), all whole numbers, so that moving one is exact.  The weights are 2^(score -
-// F) * value scale, and what brings the largest near 2^kQ4Place in a group of channels is
-//     R = the group's largest score + log2(value scale), less kQ4Place.
-// F is the largest R of the groups.  A group whose R is not far below shares it; the others get a reference A = R of their own and
-// their weights a gain of 2^(F - A).  Only tokens that the row sees enter, each with its own scores and scales.
+// The softmax's references of a query row (a column).  The weights are 2^(score - F) * value scale, and what brings the largest near
+// 2^kQ4Place in a group of channels is
+//     R = the group's largest score + log2(value scale), less kQ4Place,
+// a whole number away from the largest score, so that this one's weight is a power of two times the scale and is not rounded.
+// F is the largest R of the groups.  A group whose R is not far below shares it; the others get a reference A near R of their own,
+// and their weights a gain of 2^(F - A), F - A whole.  Only tokens that the row sees enter, each with its own scores and scales.
 // The lanes of a column share the work: a lane has group (g / 2) % NG of column 2c + g % 2.
 // The largest of a column's eight lanes for each group, to the lane that has it:
 template <int NG>
@@ -162,14 +163,16 @@ __device__ __forceinline__ Q4Refs q4_follow(float best, float score, float F, fl
     const uint32_t passed = __ballot_sync(0xffffffffu, best > A + kQ4Most || score > F + kQ4Floor + 10.f);
     Q4Refs r{R, A, F, 1.f, 1.f};
     const bool follow = (passed >> (lane & 7)) & 0x01010101u;  // some group of the column
-    if (follow) r.R = fmaxf(r.R, ceilf(best) - kQ4Place);
-    const float top = fmaxf(q4_max_groups(r.R), ceilf(score) - kQ4Floor);
+    if (follow) r.R = fmaxf(r.R, score + (ceilf(best - score) - kQ4Place));      // (the other operand where nothing is seen: NaN)
+    const float top = fmaxf(q4_max_groups(r.R), score - kQ4Floor);
+    int apart = __float2int_rn(F - A);
     if (follow) {
         r.F = fmaxf(F, top);
-        r.A = r.R > kNegInf && r.F - r.R > kQ4Share ? fmaxf(r.R, r.F - 126.f) : r.F;
+        apart = r.R > kNegInf && r.F - r.R > kQ4Share ? min(__float2int_rn(r.F - r.R), 126) : 0;
+        r.A = r.F - (float)apart;
         r.corr = ex2(A - r.A);
     }
-    r.gain = q4_pow2(min(max(__float2int_rn(r.F - r.A), 0), 126));
+    r.gain = q4_pow2(min(max(apart, 0), 126));
     return r;
 }
 // The scores up to which nothing of the lane's columns can have been passed, given the largest value scale of each group.

@@ -713,7 +713,7 @@ __global__ void __launch_bounds__(kBThreads, 1) q4_block_kernel(const __grid_con
                         top = fmaxf(top, fmaf(fmaxf(m0, m1), fk[k], ev[k]));
                     }
                     if (__any_sync(0xffffffffu, top > F + kQ4Most)) {
-                        const float Fn = top > F + kQ4Most ? ceilf(top) - kQ4Place : F, corr = ex2(F - Fn);
+                        const float Fn = top > F + kQ4Most ? top - kQ4Place : F, corr = ex2(F - Fn);
                         F = Fn;
                         l *= corr;
                         if (i > i0) {                          // (every earlier product of this half is complete: s was committed behind it)

@@ -12,7 +12,7 @@ namespace {
 
 constexpr int kQ4Unit = 64;            // tokens per unit: four tiles
 constexpr int kQ4UnitTiles = kQ4Unit / kQ4Tile;
-// Weights in fp16: a reference places the largest at 2^(kQ4Place - 1) .. 2^kQ4Place and follows when one may have passed 2^kQ4Most (fp16
+// Weights in fp16: a reference places the largest near 2^kQ4Place and follows when one may have passed 2^kQ4Most (fp16
 // holds 2^16 less an eighth).  fp16's smallest step is 2^-24, so weights down to 2^-(13 + kQ4Place) of the largest are rounded by 2^-11
 // of themselves and smaller ones by 2^-(24 + kQ4Place) of the largest.  Placed higher, the reference moves more often (kQ4Place 6 / 8 / 10: one
 // sequence of 128K 41.5 / 42 / 43 us, 8 x 4 positions 110 / 114 / 118, 2048 positions 1254 / 1281 / 1296); at 6 what 2^17 tokens lose together is 2^-13 of the
