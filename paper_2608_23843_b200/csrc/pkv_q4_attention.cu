@@ -522,7 +522,7 @@ __global__ void __launch_bounds__(Q4Shape<D, NG, NT>::kThreads, q4_ctas_per_sm(N
         }
         vis_all = __reduce_min_sync(0xffffffffu, vis_all);
         consumers_sync();                                      // (the queries are there; those before were done with at the segment's end)
-        const uint32_t q_at = smem_u32(&queries[0][0][lane]), gain_at = smem_u32(&gains[warp][0][0][c]);
+        const uint32_t q_at = smem_u32(&queries[0][0][lane]);
 
         // ---- the segment's units ----
         const bool any = at < seg_hi;
@@ -766,8 +766,7 @@ __global__ void __launch_bounds__(Q4Shape<D, NG, NT>::kThreads, q4_ctas_per_sm(N
                             const float *p = sc[tl][nt];
                             float w0 = p[0] * f0, w1 = p[1] * f0, w2 = p[2] * f1, w3 = p[3] * f1;
                             if (kCareful) {                    // a hidden token's weight is zero whatever its scale holds
-                                uint32_t gain;
-                                asm volatile("ld.shared.u32 %0, [%1];" : "=r"(gain) : "r"(gain_at + (nt * NG + k) * 16));
+                                const uint32_t gain = *const_cast<const volatile uint32_t *>(&gains[warp][nt][k][c]);      // (not kept in registers)
                                 w0 *= bf16lo_f(gain); w1 *= bf16hi_f(gain); w2 *= bf16lo_f(gain); w3 *= bf16hi_f(gain);
                                 const int t = t0 + tl * kQ4Tile + g;
                                 const bool ok = (here >> tl) & 1;

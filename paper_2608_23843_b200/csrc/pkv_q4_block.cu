@@ -728,6 +728,7 @@ __global__ void __launch_bounds__(kBThreads, 1) q4_block_kernel(const __grid_con
                             }
                         }
                     }
+                    l = fmaf(apart, ex2(apart_m - F), l);
                     uint32_t pk[kQ4Unit / 2];
 #pragma unroll
                     for (int k = 0; k < kQ4UnitTiles; ++k) {
@@ -747,7 +748,6 @@ __global__ void __launch_bounds__(kBThreads, 1) q4_block_kernel(const __grid_con
                         f2_unpack(f2_add(sum[0], sum[1]), s0, s1);
                         l = fmaf(s0 + s1, inf.ev_inv[k], l);
                     }
-                    l = fmaf(apart, ex2(apart_m - F), l);
                     tmem_st32(t_s, pk);
                     tmem_st_wait();
                     tc_fence_before();

@@ -187,3 +187,14 @@ def test_sizes_drawn_at_random(n, G, d, g, P, seed):
     for s, q in enumerate(qs):
         check(out[s], *h.expected(q, s))
     assert h.cache.stats() == {"device_timeouts": 0, "bad_pages": 0, "bad_lengths": 0}
+
+
+@pytest.mark.parametrize("dtype, g, power", [(BF16, 32, 12), (BF16, 64, 26), (FP16, 32, 12)])
+def test_the_tolerance_judges_every_group_by_its_own_values(dtype, g, power):
+    """Results of zero, or off by a tenth, would not pass in the small groups either."""
+    T, n, G = 200, 2, 4
+    k, v, q = randn(1, T, 1, 128).to(dtype), randn(2, T, 1, 128) * 2.0 ** (-power // 2), randn(3, n, G, 128).to(dtype)
+    v[..., :g] *= 2.0 ** power
+    ref, tol = attention(q, k, v.to(dtype), g, T - n, 1 / math.sqrt(128), dtype)
+    for group in (tol / ref.abs()).split(g, -1):
+        assert group.median() < 0.06 and (group < 1).float().mean() > 0.95
