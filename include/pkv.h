@@ -598,8 +598,8 @@ pkv_status pkv_q4_read_kv(pkv_q4_cache *c, int32_t n_seqs, const int32_t *page_t
  * 2^-11 of itself or 2^-26 of the largest such product of its query and channel group, whichever is more; with more rows by
  * 2^-11 of itself or, together with the row's largest scale, by 2^-25 of the largest such product of its query.  Only rows that a query
  * sees count for it, and sizes may differ from token to token and from channel group to channel group: query channels down to 2^-24 of a
- * query's largest (bf16: 2^-27) are exact; with more than 32 rows, so are channel groups down to 2^-18 (values: 2^-25) of their row's largest,
- * smaller ones are rounded by 2^-27 (2^-33) of that.
+ * query's largest (bf16: 2^-27) are exact; with more than 32 rows, so are channel groups down to 2^-19 (values: 2^-20) of their row's largest,
+ * smaller ones are rounded by 2^-27 (2^-28) of that.
  * That holds for magnitudes of q, k and v from 2^-60 to 2^60 (every fp16 value lies inside) and for values of a sequence that differ by
  * less than 2^100; of larger ones products may become infinite or NaN, smaller ones may count as zero.  A query or key that is not
  * finite makes the results that depend on it NaN or meaningless, and no others; a value that is not finite makes its channel

@@ -9,7 +9,7 @@
 //                    (128-byte swizzle, panels of 64 channels).  A code (3 bits and a sign) times a bf16 scale (8 bits) has
 //                    11 bits, so fp16 holds it exactly where the scale is in its range: a power of two per tile, or per token in tiles of
 //                    uneven sizes, is handed on to the rows, and what is left lies at the upper end of the range, so that channel groups
-//                    down to 2^-18 (values: 2^-25) of their row's largest are exact too,
+//                    down to 2^-19 (values: 2^-20) of their row's largest are exact too,
 //     one warp       issues the products, one lane: s = Q K^T with Q and, later, p as row operands in tensor memory,
 //                    o += p V; while one half's rows are in their softmax the other half's products run,
 //     eight warps    softmax (fp32): s from tensor memory, p as fp16 back over it, o rescaled only when a row's weights may have passed
@@ -151,22 +151,26 @@ __device__ __forceinline__ void block_advance(const Q4AttentionArgs &a, BlockCur
     }
 }
 
-// A tile's scales lose one power of two, kBAbove above that of the first token's largest, which comes to 2^kBTop .. 2^(kBTop + 1): seven
-// times that fits fp16, and a scale 2^-29 of it times a code is still exact.  Where another token's largest is more than kBAbove
-// above or kBKeys (kBValues) below, the tile is uneven: each token has a power of two of its own.  (The tile's largest instead of the
-// first token's, by redux: 2048 positions 38 us slower.)
-constexpr uint32_t kBAbove = 2, kBKeys = 8, kBValues = 2;
+// A tile's scales lose one power of two, that of the largest, which comes to 2^kBTop .. 2^(kBTop + 1): seven times that fits fp16, and
+// a scale 2^-29 of it times a code is still exact.  Where a token's largest is further below than kBKeys (kBValues), the tile is uneven:
+// each token has a power of two of its own.
+constexpr uint32_t kBKeys = 10, kBValues = 9;
 constexpr int kBTop = 12;
+// Where values spread more than 2^kBSpread, a reference goes by each token's own.  Placed there, weights stay inside fp16: a token's may be
+// 2^kBValues above what it adds.  (Measured, 2048 positions: 1256 us; with every other token's values 64 times larger 1494, with every
+// other token's keys 1024 times smaller, all tiles uneven, 2145.)
+constexpr uint32_t kBSpread = 4;
+static_assert(kQ4Place + kBValues < kQ4Most, "see above");
 // (values that are zero count as the least there are: their tokens' weights must not set the reference that all share)
 constexpr int kBLeast = -80;                        // least exponent: below those of all values of the documented range, far above fp32's least
 
 // What the widening warps tell the rows about a unit.
 struct __align__(16) UnitInfo {
     float tk[kQ4Unit];                              // powers of two taken out of each token's keys, in uneven tiles
-    float tv[kQ4Unit];                              // ... of its values: exponents
+    float tv[kQ4Unit];                              // exponents of each token's values, in uneven tiles and where they spread
     float ek[kQ4UnitTiles];                         // ... of the other tiles' keys (uneven: 1)
     float ev[kQ4UnitTiles], ev_inv[kQ4UnitTiles];   // ... and values: exponents, and 2^-exponent (uneven: 0, 0)
-    uint8_t odd[kQ4UnitTiles];                      // 1: uneven keys, 2: uneven values, 4: values that are not finite
+    uint8_t odd[kQ4UnitTiles];                      // 1: uneven keys, 2: uneven values, 4: values that are not finite, 8: values that spread
     uint16_t v_nan[kQ4UnitTiles][4];                // per channel group: tokens whose values are not finite there (zeros here)
     uint32_t tiles, tokens;                         // which tiles are there; tokens of the sequence in the unit
 };
@@ -442,11 +446,13 @@ __global__ void __launch_bounds__(kBThreads, 1) q4_block_kernel(const __grid_con
                 }
             }
             // one for the tile's keys and one for its values, or for each token
-            const uint32_t own = z >> 7, side = lane & 16, k_first = __shfl_sync(0xffffffffu, own, 0), v_first = __shfl_sync(0xffffffffu, own, 16);
-            const uint32_t uneven = __ballot_sync(0xffffffffu, (lane & 15) < valid && (side ? own + kBValues - v_first > kBValues + kBAbove || v_first == 0u : z != 0u && own + kBKeys - k_first > kBKeys + kBAbove));
+            const uint32_t own = z >> 7, side = lane & 16, k_most = __reduce_max_sync(0xffffffffu, side ? 0u : own), v_most = __reduce_max_sync(0xffffffffu, side ? own : 0u);
+            const bool there = (lane & 15) < valid;
+            const uint32_t uneven = __ballot_sync(0xffffffffu, there && (side ? own + kBValues < v_most || v_most == 0u : z != 0u && own + kBKeys < k_most));
+            const bool spread = __any_sync(0xffffffffu, there && side && own + kBSpread < v_most);
             const bool each = uneven >> side & 0xffffu;
-            const int top = 127 + kBTop, e = each ? min(max((int)own - top, kBLeast), 100) : 0;
-            const int ek = min(max((int)(k_first + kBAbove) - top, kBLeast), 100), ev = min(max((int)(v_first + kBAbove) - top, kBLeast), 100);
+            const int top = 127 + kBTop, e = min(max((int)own - top, kBLeast), 100);
+            const int ek = min(max((int)k_most - top, kBLeast), 100), ev = min(max((int)v_most - top, kBLeast), 100);
             float fk[2], fv[2];                                // of tokens t_lane, t_lane + 8
             fk[0] = fk[1] = pow2(-ek);
             fv[0] = fv[1] = pow2(-ev);
@@ -458,7 +464,7 @@ __global__ void __launch_bounds__(kBThreads, 1) q4_block_kernel(const __grid_con
                     if (uneven >> 16) fv[half] = pow2(-y);
                 }
             if (wu > 0 && !mbar_wait_warp(smem_u32(&wide_empty[ws]), (wu - 1) & 1, abort_flag)) { ok = false; break; }
-            if (each) (side ? info[ws].tv : info[ws].tk)[dw * kQ4Tile + (lane & 15)] = side ? (float)e : pow2(e);
+            if (side ? spread || each : each) (side ? info[ws].tv : info[ws].tk)[dw * kQ4Tile + (lane & 15)] = side ? (float)e : pow2(e);
             if (lane == 0) {
                 uint32_t any = 0;
 #pragma unroll
@@ -469,7 +475,7 @@ __global__ void __launch_bounds__(kBThreads, 1) q4_block_kernel(const __grid_con
                 info[ws].ek[dw] = uneven & 0xffffu ? 1.f : pow2(ek);
                 info[ws].ev[dw] = uneven >> 16 ? 0.f : (float)ev;
                 info[ws].ev_inv[dw] = uneven >> 16 ? 0.f : pow2(-ev);
-                info[ws].odd[dw] = (uint8_t)((uneven & 0xffffu ? 1 : 0) | (uneven >> 16 ? 2 : 0) | (any ? 4 : 0));
+                info[ws].odd[dw] = (uint8_t)((uneven & 0xffffu ? 1 : 0) | (uneven >> 16 ? 2 : 0) | (any ? 4 : 0) | (spread ? 8 : 0));
                 if (dw == 0) { info[ws].tiles = bits; info[ws].tokens = tokens; }
             }
             const uint32_t d0 = d_at[0] + ws * S::kWide, d1 = d_at[1] + ws * S::kWide;
@@ -640,7 +646,7 @@ __global__ void __launch_bounds__(kBThreads, 1) q4_block_kernel(const __grid_con
                     const UnitInfo &inf = info[ws];
                     const int t0 = (c.unit + i) * kQ4Unit, lim = min(vis - t0, (int)inf.tokens);
                     const uint32_t tiles = inf.tiles, odd = *reinterpret_cast<const uint32_t *>(inf.odd);
-                    const bool special = __any_sync(0xffffffffu, lim < kQ4Unit || odd != 0u) || tiles != (1u << kQ4UnitTiles) - 1u;
+                    const bool special = __any_sync(0xffffffffu, lim < kQ4Unit || (odd & 0x07070707u) != 0u) || tiles != (1u << kQ4UnitTiles) - 1u;
                     float fk[kQ4UnitTiles], ev[kQ4UnitTiles];
 #pragma unroll
                     for (int k = 0; k < kQ4UnitTiles; ++k) {
@@ -654,9 +660,8 @@ __global__ void __launch_bounds__(kBThreads, 1) q4_block_kernel(const __grid_con
                     tmem_ld<kQ4Unit>(t_s, reinterpret_cast<uint32_t *>(sv));
                     float apart = 0.f, apart_m = kNegInf;      // sum of the weights of tiles with uneven values, relative to 2^apart_m
                     if (special) {
-                        if (odd) {
-                            // each token's powers of two, in tensor memory, four at a time: little code, out of the way of
-                            // the registers
+                        if (odd & 0x07070707u) {
+                            // each token's powers of two, in tensor memory, a tile at a time: out of the way of the registers
 #pragma unroll 1
                             for (int k = 0; k < kQ4UnitTiles; ++k) {
                                 const uint32_t un = odd >> (8 * k);
@@ -668,28 +673,34 @@ __global__ void __launch_bounds__(kBThreads, 1) q4_block_kernel(const __grid_con
                                 }
                                 if (!(un & 3u)) continue;
                                 const float fx = fmaxf(f * inf.ek[k], 1.2e-38f);
-#pragma unroll 1
-                                for (int b = k * kQ4Tile; b < (k + 1) * kQ4Tile; b += 4) {
-                                    uint32_t r[4];
-                                    tmem_ld4(t_s + b, r);
-                                    tmem_ld_wait();
+                                float x[kQ4Tile];
+                                tmem_ld16(t_s + k * kQ4Tile, reinterpret_cast<uint32_t *>(x));
+                                tmem_ld_wait();
+                                if (un & 1u) {
 #pragma unroll
-                                    for (int i = 0; i < 4; ++i) {
-                                        float x = __uint_as_float(r[i]);
-                                        if (un & 1u) x *= inf.tk[b + i];
-                                        if (un & 2u) {
-                                            x *= fx;
-                                            if (b + i < see) {
-                                                const float m = fmaxf(apart_m, x);
-                                                apart = apart * ex2(apart_m - m) + ex2(x - m);
-                                                apart_m = m;
-                                            }
-                                            x += inf.tv[b + i];
-                                        }
-                                        r[i] = __float_as_uint(x);
+                                    for (int b = 0; b < kQ4Tile; b += 4) {
+                                        const float4 t = *reinterpret_cast<const float4 *>(inf.tk + k * kQ4Tile + b);
+                                        x[b] *= t.x; x[b + 1] *= t.y; x[b + 2] *= t.z; x[b + 3] *= t.w;
                                     }
-                                    tmem_st4(t_s + b, r);
                                 }
+                                if (un & 2u) {
+                                    float m = apart_m, sum = 0.f;
+#pragma unroll
+                                    for (int b = 0; b < kQ4Tile; ++b) {
+                                        x[b] *= fx;
+                                        if (k * kQ4Tile + b < see) m = fmaxf(m, x[b]);
+                                    }
+#pragma unroll
+                                    for (int b = 0; b < kQ4Tile; ++b) sum += k * kQ4Tile + b < see ? ex2(x[b] - m) : 0.f;
+                                    apart = fmaf(apart, ex2(apart_m - m), sum);
+                                    apart_m = m;
+#pragma unroll
+                                    for (int b = 0; b < kQ4Tile; b += 4) {
+                                        const float4 t = *reinterpret_cast<const float4 *>(inf.tv + k * kQ4Tile + b);
+                                        x[b] += t.x; x[b + 1] += t.y; x[b + 2] += t.z; x[b + 3] += t.w;
+                                    }
+                                }
+                                tmem_st16(t_s + k * kQ4Tile, reinterpret_cast<const uint32_t *>(x));
                             }
                             tmem_st_wait();
                             tmem_ld<kQ4Unit>(t_s, reinterpret_cast<uint32_t *>(sv));
@@ -713,7 +724,28 @@ __global__ void __launch_bounds__(kBThreads, 1) q4_block_kernel(const __grid_con
                         top = fmaxf(top, fmaf(fmaxf(m0, m1), fk[k], ev[k]));
                     }
                     if (__any_sync(0xffffffffu, top > F + kQ4Most)) {
-                        const float Fn = top > F + kQ4Most ? top - kQ4Place : F, corr = ex2(F - Fn);
+                        float own = top;
+                        if (odd & 0x08080808u) {               // the largest x, each token with its own Ev
+                            own = -INFINITY;
+#pragma unroll 1
+                            for (int k = 0; k < kQ4UnitTiles; ++k) {
+                                const uint32_t un = odd >> (8 * k);
+                                const int see = (tiles >> k & 1 ? lim : 0) - k * kQ4Tile;
+                                const float fx = un & 2u ? 1.f : fmaxf(f * inf.ek[k], 1.2e-38f);
+                                float x[kQ4Tile];
+                                tmem_ld16(t_s + k * kQ4Tile, reinterpret_cast<uint32_t *>(x));
+                                tmem_ld_wait();
+#pragma unroll
+                                for (int b = 0; b < kQ4Tile; b += 4) {
+                                    const float4 t = (un & 10u) == 8u ? *reinterpret_cast<const float4 *>(inf.tv + k * kQ4Tile + b) : make_float4(inf.ev[k], inf.ev[k], inf.ev[k], inf.ev[k]);
+                                    if (b < see) own = fmaxf(own, fmaf(x[b], fx, t.x));
+                                    if (b + 1 < see) own = fmaxf(own, fmaf(x[b + 1], fx, t.y));
+                                    if (b + 2 < see) own = fmaxf(own, fmaf(x[b + 2], fx, t.z));
+                                    if (b + 3 < see) own = fmaxf(own, fmaf(x[b + 3], fx, t.w));
+                                }
+                            }
+                        }
+                        const float Fn = top > F + kQ4Most ? fmaxf(own - kQ4Place, top - kQ4Most) : F, corr = ex2(F - Fn);
                         F = Fn;
                         l *= corr;
                         if (i > i0) {                          // (every earlier product of this half is complete: s was committed behind it)

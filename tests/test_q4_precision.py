@@ -176,7 +176,7 @@ def test_sizes_drawn_at_random(n, G, d, g, P, seed):
         some = (torch.rand(T, 1, 1, 1, generator=gen) < 0.3).float()
         kt, vt = (torch.randn(T, H, d // g, g, generator=gen) for _ in "kv")
         kt = kt * groups * torch.where(some > 0, power(-16, 1, T, 1, 1, 1), torch.ones(1))
-        vt = vt * power(-12, 12, T, H, d // g, 1) * torch.where(some > 0, power(-20, 20, T, 1, 1, 1), torch.ones(1))
+        vt = vt * power(-10, 10, T, H, d // g, 1) * torch.where(some > 0, power(-20, 20, T, 1, 1, 1), torch.ones(1))
         zero = torch.rand(T, 1, 1, 1, generator=gen) < 0.05
         k.append(kt.masked_fill(zero, 0.0).flatten(2).to(BF16))
         v.append(vt.masked_fill(zero.roll(1, 0) & (torch.arange(T) > 0).view(T, 1, 1, 1), 0.0).flatten(2).to(BF16))
