@@ -18,8 +18,8 @@ namespace {
 // Both copy kernels are bound by HBM: 4 d bytes of 16-bit rows and d + 4 d/g bytes of cache per token and KV head.  A CTA
 // takes a few rows of the call: it looks up where they lie once, a thread each, while the first 16-byte loads are in flight
 // (K and V of a row and head together), so that nothing but the loads, the arithmetic and the stores is paid per
-// head.  Measured, 8 heads, d = 128, g = 32, bf16: append of 65536 rows 65 us (5.3 TB/s), read of 131072 rows 117 us
-// (5.9 TB/s); both have issue slots 65 % and the integer pipe 58 % busy, next to a copy's 6.45 TB/s.
+// head.  Measured, 8 heads, d = 128, g = 32, bf16: append of 65536 rows 65 us (5.3 TB/s), read of 131072 rows 120 us
+// (5.7 TB/s); both have issue slots 65 % and the integer pipe 58 % busy, next to a copy's 6.45 TB/s.
 constexpr int kCopyThreads = 256, kCopyUnroll = 4, kCopyRows = 128;
 
 struct RowPlace { long long off; int t, ok; };      // byte offset of the head-0 tile in the pool; token within its tile

@@ -16,8 +16,8 @@
 //     while the groups of a row share a reference.  (One reference for all rows and groups of a warp, with the largest at 1, was 5 % faster
 //     at eight rows and 8 % at sixteen, and rounded small weights, and groups of smaller values, to few bits or to zero.)
 //   Queries are brought to fp16 with a power of two per row, which is exact for bf16 and fp16 alike.
-// Measured, 8 KV heads, d = 128, g = 32: 8 sequences of 32K (302 MB) 71 us with 4 or 8 rows per KV head (4.3 TB/s; issue slots
-// 58 % busy, tensor pipe 26 %), 110 us with 16; one of 128K 41.5 us; the kernel's rate on further tokens is 5.5 to 5.8 TB/s,
+// Measured, 8 KV heads, d = 128, g = 32: 8 sequences of 32K (302 MB) 71 to 74 us with 4 or 8 rows per KV head (4.1 TB/s; issue slots
+// 58 % busy, tensor pipe 26 %), 112 us with 16; one of 128K 41.5 us; the kernel's rate on further tokens is 5.5 to 5.8 TB/s,
 // and some 15 us of a call that joins states are launches, the first copies, the last units and the join.
 // One warp of a CTA looks up pages and issues the bulk copies; the others take the units of 64 tokens in turn and keep (m, l, o)
 // in registers; at the end of a (sequence, KV head, row tile) segment the warps' states are joined through shared memory.  The CTAs of

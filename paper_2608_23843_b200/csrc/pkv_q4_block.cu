@@ -14,12 +14,12 @@
 //                    o += p V; while one half's rows are in their softmax the other half's products run,
 //     eight warps    softmax (fp32): s from tensor memory, p as fp16 back over it, o rescaled only when a row's weights may have passed
 //                    fp16's range (see kQ4Place).
-// Measured: 2048 positions against 32K (32 / 8 heads, d = 128, g = 32; 1.07 TFLOP, one call) 1254 us, 850 TFLOP/s; 5 x 37
+// Measured: 2048 positions against 32K (32 / 8 heads, d = 128, g = 32; 1.07 TFLOP, one call) 1256 to 1293 us, 840 TFLOP/s; 5 x 37
 // positions of sequences up to 4001 (28 / 4 heads, d = 64) 28 us, of which the launch, the partition, the first units, the last
 // states and the join are most.
 // What bounds it: products and exponentials each take 1024 cycles per unit of 256 rows, but a half's chain - s, softmax, o,
 // the hand-overs between them - is some 1800 cycles long even with both for free, and the widening competes with the softmax
-// for issue slots (tensor pipe 42 %, exponentials 42 %, issue slots 56 % busy).  Tried on the same call and not kept: Q of one half in shared memory
+// for issue slots (tensor pipe 39 %, exponentials 40 %, issue slots 55 % busy).  Tried on the same call and not kept: Q of one half in shared memory
 // so that s of the next unit can be computed behind the softmax (the products then wait for shared memory), s in two
 // buffers of 32 tokens for the same end (1509 us: twice the hand-overs, 40 products to issue per unit instead of 24; 1364 with an
 // issuing warp per half, which by itself costs more than it gives, 1501), five or six
