@@ -613,6 +613,93 @@ pkv_status pkv_q4_attention(pkv_q4_cache *c, int32_t n_seqs, const int32_t *page
                             void *out, int64_t out_row_stride, int64_t out_head_stride, float *state,
                             void *workspace, int64_t workspace_bytes, void *stream);
 
+/*
+ * ---- Attention over a part of the positions: a sliding window with sinks, trees of drafted tokens ------------------
+ * pkv_q4_attention() for queries that see less than all positions up to their own.
+ *
+ *   window, sinks   with window = W > 0 a query at position p sees the positions t <= p that lie in its window (t > p - W, its own
+ *                   included: W positions) and the first `sinks` positions of the sequence.  Nothing else is looked up: table entries of pages
+ *                   that hold no position any query of the call sees may be stale or -1, so such pages can have gone back to the
+ *                   pool (pkv_q4_plan() sends them there).  window = 0: no window (sinks must be 0).
+ *   tree            [device] uint64 [n_rows, tree_words], or NULL: causal.  The new rows of a sequence (n of them, behind a context of C = T - n
+ *                   tokens) are then drafted tokens: row j sees new row i if bit i % 64 of tree[row j][i / 64] is set (bits of
+ *                   rows that the sequence does not have are ignored), and the context.  With a window it sees of the context the last W - b positions and
+ *                   the sinks, b being the number of its bits (of rows the sequence has): with masks of pkv_q4_tree_masks() that
+ *                   is a window that ends at the row's own place in its branch.  64 * tree_words has to be max_q_len at least.
+ * Everything else - rows, strides, states, workspace, accuracy, what contents that make no sense lead to - is as for pkv_q4_attention();
+ * a query that sees nothing gets zeros.  A call with window = 0 and tree = NULL is pkv_q4_attention().
+ */
+typedef struct pkv_q4_select {
+    int32_t window, sinks;      /* 0 or more */
+    const uint64_t *tree;       /* 8-byte aligned */
+    int32_t tree_words;
+} pkv_q4_select;
+
+pkv_status pkv_q4_attention_select_workspace(const pkv_q4_cache *c, int32_t n_seqs, int32_t max_q_len, int32_t max_len,
+                                             const pkv_q4_select *select, int64_t *bytes);
+pkv_status pkv_q4_attention_select(pkv_q4_cache *c, int32_t n_seqs, const int32_t *page_table, int32_t max_pages,
+                                   const int32_t *lengths, int64_t n_rows, const int32_t *offsets, int32_t max_q_len,
+                                   int32_t max_len, const pkv_q4_select *select, const void *q, int64_t q_row_stride,
+                                   int64_t q_head_stride, void *out, int64_t out_row_stride, int64_t out_head_stride, float *state,
+                                   void *workspace, int64_t workspace_bytes, void *stream);
+
+/*
+ * Masks of drafted tokens from the tree's edges, once per step for all layers.  parents [device] int32 [n_rows]: the row of the same
+ * sequence (0 .. j - 1 for row j) that row j continues, -1 for the last token of the context; any other value counts as -1 and in
+ * pkv_q4_stats.bad_lengths.  Written:
+ *   tree    [device] uint64 [n_rows, tree_words]: bits of the row itself and its ancestors.  With window = W > 0 only of those
+ *           within the window of the row's place (the W - 1 nearest ancestors), and of those whose place C + depth lies below `sinks`
+ *   depths  [device] int32 [n_rows], or NULL: the number of ancestors.  C + depth is the position of a drafted token (for rotary embeddings)
+ * lengths may be NULL where window or sinks is 0.  Rows that belong to no sequence are left as they were.  max_q_len as in the attention call (rows of a
+ * sequence beyond it are left as they were, and counted).
+ */
+pkv_status pkv_q4_tree_masks(pkv_q4_cache *c, int32_t n_seqs, const int32_t *lengths, int64_t n_rows, const int32_t *offsets,
+                             int32_t max_q_len, const int32_t *parents, int32_t window, int32_t sinks, uint64_t *tree,
+                             int32_t tree_words, int32_t *depths, void *stream);
+
+/*
+ * Keeps the accepted rows of each sequence's n new rows: row paths[s][i] becomes new row i, for i < counts[s] (held inside [0, min(n, max_path)]),
+ * all at once, codes and scales as they are; lengths_out[s] = T - n + counts[s] (0 at least).
+ *   paths   [device] int32 [n_seqs, max_path], i <= paths[s][i] < n (rows of a path ascend, so that holds for every path of a tree whose
+ *           parents come before their children); an entry outside that is skipped (new row i stays as it was) and counted in bad_lengths
+ *   counts  [device] int32 [n_seqs]
+ *   lengths_out  [device] int32 [n_seqs], not overlapping lengths
+ * All layers can be kept in one call, each layer's tables as sequences of their own.  Pages shared between sequences must not be written here.
+ */
+pkv_status pkv_q4_keep_rows(pkv_q4_cache *c, int32_t n_seqs, const int32_t *page_table, int32_t max_pages, const int32_t *lengths,
+                            int64_t n_rows, const int32_t *offsets, const int32_t *paths, int32_t max_path, const int32_t *counts,
+                            int32_t *lengths_out, void *stream);
+
+/*
+ * Plans a step on the device: new lengths, pages, offsets, positions and slots from the rows that each request adds.
+ *   lengths  [device] int32 [n_seqs]: T, before the step;   rows [device] int32 [n_seqs]: new rows, or -1: the request is done
+ *   spans    [device] int32 [n_seqs, 2]: (first, end).  A request holds the pages of its table entries first .. end - 1 and, with a
+ *            window, those of entries 0 .. ceil(sinks / P) - 1 (below end).  An empty request is (0, 0).
+ *   ring     [device] int32 [n_pages] (of the configuration): free page numbers, in the places head % n_pages .. (tail - 1) % n_pages
+ *   counters [device] int64 [4]: head, tail (0 <= head <= tail), and two that are only written
+ * A request with rows >= 0 gets pages for positions up to T + rows: entries end .. ceil((T + rows) / P) - 1, from the ring's head
+ * on, requests in order.  A request that is done gives all its pages back and becomes empty.  With window = W > 0 a request gives back the
+ * pages (behind those of the sinks) whose positions all lie below T + 1 - W, which no query at position T or later sees; use the
+ * same window and sinks in every step.  Pages that come back go behind the ring's tail, requests in order, and are given out by later steps only (a captured
+ * step that failed for want of pages can be repeated after others are done).  Entries of pages that went back keep their numbers.
+ * Pages shared between requests need the caller's own count: they go back with each.
+ * Written:
+ *   lengths_out [n_seqs], spans_out [n_seqs, 2], counters_out [4]  (each may be its input: in place)
+ *   offsets   [device] int32 [n_seqs + 1]: prefix sums of the new rows, as the other calls take them
+ *   positions [device] int32 [n_rows], or NULL: the position of every new row;   slots [device] int64 [n_rows], or NULL: page * P + row in the page (-1: no
+ *             such page).  n_rows bounds the step's rows; places behind the last row are left as they were
+ *   page_table, ring: the entries above
+ * All or nothing: where the ring has too few pages (counters_out[2]: how many are missing) or requests make no sense (counters_out[3]: how
+ * many; rows below -1, lengths or spans outside the table, T + rows above max_pages * P; the sum of the rows above n_rows and a ring whose
+ * counters cannot be count as one more each) nothing changes: lengths, spans, head and tail stay, offsets are 0.  Otherwise counters_out[2] and [3] are 0.
+ * workspace [device] pkv_q4_plan_workspace() bytes, 16-byte aligned; NULL where that is 0.
+ */
+pkv_status pkv_q4_plan_workspace(const pkv_q4_cache *c, int32_t n_seqs, int64_t n_rows, int64_t *bytes);
+pkv_status pkv_q4_plan(pkv_q4_cache *c, int32_t n_seqs, int32_t *page_table, int32_t max_pages, const int32_t *lengths,
+                       const int32_t *rows, const int32_t *spans, int32_t *ring, const int64_t *counters, int32_t window,
+                       int32_t sinks, int32_t *lengths_out, int32_t *spans_out, int64_t *counters_out, int32_t *offsets,
+                       int64_t n_rows, int32_t *positions, int64_t *slots, void *workspace, int64_t workspace_bytes, void *stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -3,6 +3,7 @@
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 
+#include <algorithm>
 #include <cmath>
 #include <cstdarg>
 #include <cstdio>
@@ -380,7 +381,7 @@ pkv_status q4_validate(const pkv_q4_config *cfg, Q4Geometry *g) {
 
 // What append, read and attention have in common: the sequences, and the rows that belong to them.
 pkv_status q4_rows(pkv_q4_cache *c, const char *what, int32_t n_seqs, const int32_t *table, int32_t max_pages,
-                   const int32_t *lengths, int64_t n_rows, const int32_t *offsets, Q4Rows *r) {
+                   const int32_t *lengths, int64_t n_rows, const int32_t *offsets, Q4Rows *r, bool with_table = true, bool with_lengths = true) {
     if (n_seqs < 1 || n_seqs > 65535) return q4_fail(c, PKV_ERR_INVALID_ARG, "%s: n_seqs %d out of range", what, n_seqs);
     if (max_pages < 1 || max_pages > ((1 << 30) >> c->geo.page_shift))
         return q4_fail(c, PKV_ERR_INVALID_ARG, "%s: max_pages %d out of range", what, max_pages);
@@ -388,7 +389,8 @@ pkv_status q4_rows(pkv_q4_cache *c, const char *what, int32_t n_seqs, const int3
         return q4_fail(c, PKV_ERR_INVALID_ARG, "%s: n_rows %lld out of range", what, (long long)n_rows);
     if (!offsets && n_rows % n_seqs != 0)
         return q4_fail(c, PKV_ERR_INVALID_ARG, "%s: %lld rows do not divide among %d sequences (give offsets)", what, (long long)n_rows, n_seqs);
-    if (!c->dry && (!table || !lengths)) return q4_fail(c, PKV_ERR_INVALID_ARG, "%s: page_table or lengths is NULL", what);
+    if (!c->dry && ((with_table && !table) || (with_lengths && !lengths)))
+        return q4_fail(c, PKV_ERR_INVALID_ARG, "%s: %s is NULL", what, with_table ? "page_table or lengths" : "lengths");
     if (((uintptr_t)table | (uintptr_t)lengths | (uintptr_t)offsets) & 3)
         return q4_fail(c, PKV_ERR_INVALID_ARG, "%s: page_table, lengths and offsets must be 4-byte aligned", what);
     *r = Q4Rows{table, lengths, offsets, n_seqs, max_pages, offsets ? 0 : (int)(n_rows / n_seqs), n_rows};
@@ -433,6 +435,67 @@ pkv_status q4_copy(pkv_q4_cache *c, bool write, int32_t n_seqs, const int32_t *t
     a.k_row = k_row; a.k_head = k_head; a.v_row = v_row; a.v_head = v_head;
     a.status = c->status;
     const cudaError_t e = write ? launch_q4_append(a, (cudaStream_t)stream) : launch_q4_read(a, (cudaStream_t)stream);
+    if (e != cudaSuccess) return q4_fail(c, PKV_ERR_CUDA, "%s: %s", what, cudaGetErrorString(e));
+    return PKV_OK;
+}
+
+// ---- attention: what every form checks -----------------------------------------------------------------------------------
+// What is wrong with a choice of positions, or NULL.
+const char *q4_select_error(const pkv_q4_select &s, int max_q_len) {
+    if (s.window < 0 || s.sinks < 0) return "window and sinks must not be negative";
+    if (s.sinks > 0 && s.window == 0) return "sinks need a window";
+    if ((uintptr_t)s.tree & 7) return "the tree's masks must be 8-byte aligned";
+    if (s.tree && (s.tree_words < 1 || s.tree_words < (max_q_len + 63LL) / 64)) return "tree_words must be max_q_len / 64, rounded up, at least";
+    return nullptr;
+}
+bool q4_selects(const pkv_q4_select &s) { return s.window > 0 || s.tree; }
+// (positions stay below 2^30: a wider window is none, and sums of a few stay in 32 bits)
+Q4Select q4_selection(const pkv_q4_select &s) { return Q4Select{std::min(s.window, 1 << 30), std::min(s.sinks, 1 << 30), s.tree != nullptr}; }
+
+pkv_status q4_attend(pkv_q4_cache *c, const char *what, int32_t n_seqs, const int32_t *page_table, int32_t max_pages, const int32_t *lengths,
+                     int64_t n_rows, const int32_t *offsets, int32_t max_q_len, int32_t max_len, const pkv_q4_select *select, const void *q,
+                     int64_t q_row_stride, int64_t q_head_stride, void *out, int64_t out_row_stride, int64_t out_head_stride, float *state,
+                     void *workspace, int64_t workspace_bytes, void *stream) {
+    if (!c) return PKV_ERR_INVALID_ARG;
+    Q4AttentionArgs a{};
+    if (pkv_status st = q4_rows(c, what, n_seqs, page_table, max_pages, lengths, n_rows, offsets, &a.rows)) return st;
+    const Q4Geometry &g = c->geo;
+    const int capacity = max_pages << g.page_shift;
+    if (!offsets) max_q_len = a.rows.per_seq;
+    if (n_rows > 0 && (max_q_len < 0 || max_q_len > n_rows)) return q4_fail(c, PKV_ERR_INVALID_ARG, "%s: max_q_len %d out of range", what, max_q_len);
+    if (max_len < 0) return q4_fail(c, PKV_ERR_INVALID_ARG, "%s: max_len %d out of range", what, max_len);
+    if (max_len == 0 || max_len > capacity) max_len = capacity;
+    if (!c->dry && n_rows > 0 && (!q || (!out == !state)))
+        return q4_fail(c, PKV_ERR_INVALID_ARG, "%s: q is NULL, or not exactly one of out and state is given", what);
+    if (!q4_strides(q, q_row_stride, q_head_stride, g.head_dim, g.n_q_heads, n_rows) ||
+        (out && !q4_strides(out, out_row_stride, out_head_stride, g.head_dim, g.n_q_heads, n_rows)))
+        return q4_fail(c, PKV_ERR_INVALID_ARG, "%s: q and out need 16-byte aligned rows: strides that are multiples of 8 elements, no row or "
+                                               "head on top of another", what);
+    if (select)
+        if (const char *error = q4_select_error(*select, n_rows > 0 ? max_q_len : 0)) return q4_fail(c, PKV_ERR_INVALID_ARG, "%s: %s", what, error);
+    const bool part = select && q4_selects(*select);
+    if ((uintptr_t)state & 7) return q4_fail(c, PKV_ERR_INVALID_ARG, "%s: state must be 8-byte aligned", what);
+    if (n_rows == 0 || max_q_len == 0) return PKV_OK;
+    const long long need = part ? q4_select_workspace(g, n_seqs, max_q_len, max_len, q4_selection(*select)) : q4_attention_workspace(g, n_seqs, max_q_len, max_len);
+    if (!c->dry && need > 0 && (!workspace || workspace_bytes < need || ((uintptr_t)workspace & 15)))
+        return q4_fail(c, PKV_ERR_INVALID_ARG, "%s: the workspace needs %lld bytes, 16-byte aligned", what, need);
+    if (c->dry) return PKV_OK;
+    if (pkv_status st = q4_device(c, what)) return st;
+    a.geo = g;
+    a.pool = c->pool;
+    a.q = q; a.out = out; a.state = state;
+    a.q_row = q_row_stride; a.q_head = q_head_stride; a.out_row = out_row_stride; a.out_head = out_head_stride;
+    a.max_q_len = max_q_len;
+    a.max_len = max_len;
+    a.workspace = static_cast<unsigned char *>(workspace);
+    a.status = c->status;
+    if (part) {
+        a.window = q4_selection(*select).window;
+        a.sinks = q4_selection(*select).sinks;
+        a.tree = reinterpret_cast<const unsigned long long *>(select->tree);
+        a.tree_words = select->tree_words;
+    }
+    const cudaError_t e = part ? launch_q4_select(a, (cudaStream_t)stream) : launch_q4_attention(a, (cudaStream_t)stream);
     if (e != cudaSuccess) return q4_fail(c, PKV_ERR_CUDA, "%s: %s", what, cudaGetErrorString(e));
     return PKV_OK;
 }
@@ -511,38 +574,139 @@ pkv_status pkv_q4_attention(pkv_q4_cache *c, int32_t n_seqs, const int32_t *page
                             int64_t n_rows, const int32_t *offsets, int32_t max_q_len, int32_t max_len, const void *q,
                             int64_t q_row_stride, int64_t q_head_stride, void *out, int64_t out_row_stride, int64_t out_head_stride,
                             float *state, void *workspace, int64_t workspace_bytes, void *stream) {
+    return q4_attend(c, "pkv_q4_attention", n_seqs, page_table, max_pages, lengths, n_rows, offsets, max_q_len, max_len, nullptr, q, q_row_stride,
+                     q_head_stride, out, out_row_stride, out_head_stride, state, workspace, workspace_bytes, stream);
+}
+
+pkv_status pkv_q4_attention_select_workspace(const pkv_q4_cache *c, int32_t n_seqs, int32_t max_q_len, int32_t max_len,
+                                             const pkv_q4_select *select, int64_t *bytes) {
+    if (!c || !bytes || !select || n_seqs < 1 || n_seqs > 65535 || max_q_len < 1 || max_len < 1) return PKV_ERR_INVALID_ARG;
+    if (q4_select_error(*select, max_q_len)) return PKV_ERR_INVALID_ARG;
+    *bytes = q4_selects(*select) ? q4_select_workspace(c->geo, n_seqs, max_q_len, max_len, q4_selection(*select))
+                                 : q4_attention_workspace(c->geo, n_seqs, max_q_len, max_len);
+    return PKV_OK;
+}
+
+pkv_status pkv_q4_attention_select(pkv_q4_cache *c, int32_t n_seqs, const int32_t *page_table, int32_t max_pages, const int32_t *lengths,
+                                   int64_t n_rows, const int32_t *offsets, int32_t max_q_len, int32_t max_len, const pkv_q4_select *select,
+                                   const void *q, int64_t q_row_stride, int64_t q_head_stride, void *out, int64_t out_row_stride,
+                                   int64_t out_head_stride, float *state, void *workspace, int64_t workspace_bytes, void *stream) {
     if (!c) return PKV_ERR_INVALID_ARG;
-    const char *what = "pkv_q4_attention";
-    Q4AttentionArgs a{};
-    if (pkv_status st = q4_rows(c, what, n_seqs, page_table, max_pages, lengths, n_rows, offsets, &a.rows)) return st;
-    const Q4Geometry &g = c->geo;
-    const int capacity = max_pages << g.page_shift;
+    const char *what = "pkv_q4_attention_select";
+    if (!select) return q4_fail(c, PKV_ERR_INVALID_ARG, "%s: select is NULL", what);
+    return q4_attend(c, what, n_seqs, page_table, max_pages, lengths, n_rows, offsets, max_q_len, max_len, select, q, q_row_stride, q_head_stride,
+                     out, out_row_stride, out_head_stride, state, workspace, workspace_bytes, stream);
+}
+
+pkv_status pkv_q4_tree_masks(pkv_q4_cache *c, int32_t n_seqs, const int32_t *lengths, int64_t n_rows, const int32_t *offsets,
+                             int32_t max_q_len, const int32_t *parents, int32_t window, int32_t sinks, uint64_t *tree,
+                             int32_t tree_words, int32_t *depths, void *stream) {
+    if (!c) return PKV_ERR_INVALID_ARG;
+    const char *what = "pkv_q4_tree_masks";
+    Q4TreeArgs a{};
+    const bool far = window > 0 && sinks > 0;      // lengths are needed
+    if (pkv_status st = q4_rows(c, what, n_seqs, nullptr, 1, lengths, n_rows, offsets, &a.rows, false, far)) return st;
     if (!offsets) max_q_len = a.rows.per_seq;
     if (n_rows > 0 && (max_q_len < 0 || max_q_len > n_rows)) return q4_fail(c, PKV_ERR_INVALID_ARG, "%s: max_q_len %d out of range", what, max_q_len);
-    if (max_len < 0) return q4_fail(c, PKV_ERR_INVALID_ARG, "%s: max_len %d out of range", what, max_len);
-    if (max_len == 0 || max_len > capacity) max_len = capacity;
-    if (!c->dry && n_rows > 0 && (!q || (!out == !state)))
-        return q4_fail(c, PKV_ERR_INVALID_ARG, "%s: q is NULL, or not exactly one of out and state is given", what);
-    if (!q4_strides(q, q_row_stride, q_head_stride, g.head_dim, g.n_q_heads, n_rows) ||
-        (out && !q4_strides(out, out_row_stride, out_head_stride, g.head_dim, g.n_q_heads, n_rows)))
-        return q4_fail(c, PKV_ERR_INVALID_ARG, "%s: q and out need 16-byte aligned rows: strides that are multiples of 8 elements, no row or "
-                                               "head on top of another", what);
-    if ((uintptr_t)state & 7) return q4_fail(c, PKV_ERR_INVALID_ARG, "%s: state must be 8-byte aligned", what);
-    if (n_rows == 0 || max_q_len == 0) return PKV_OK;
-    const long long need = q4_attention_workspace(g, n_seqs, max_q_len, max_len);
+    const pkv_q4_select sel{window, sinks, tree, tree_words};
+    if (const char *error = q4_select_error(sel, max_q_len)) return q4_fail(c, PKV_ERR_INVALID_ARG, "%s: %s", what, error);
+    if (tree_words < 1 || tree_words < (max_q_len + 63LL) / 64) return q4_fail(c, PKV_ERR_INVALID_ARG, "%s: tree_words %d out of range", what, tree_words);
+    if (((uintptr_t)parents | (uintptr_t)depths) & 3) return q4_fail(c, PKV_ERR_INVALID_ARG, "%s: parents and depths must be 4-byte aligned", what);
+    if (!c->dry && n_rows > 0 && (!parents || !tree)) return q4_fail(c, PKV_ERR_INVALID_ARG, "%s: parents or tree is NULL", what);
+    if (c->dry || n_rows == 0 || max_q_len == 0) return PKV_OK;
+    if (pkv_status st = q4_device(c, what)) return st;
+    if (!far) a.rows.lengths = nullptr;
+    a.parents = parents;
+    a.tree = reinterpret_cast<unsigned long long *>(tree);
+    a.depths = depths;
+    a.status = c->status;
+    a.max_q_len = max_q_len;
+    a.words = tree_words;
+    a.window = q4_selection(sel).window;
+    a.sinks = q4_selection(sel).sinks;
+    const cudaError_t e = launch_q4_tree_masks(a, (cudaStream_t)stream);
+    if (e != cudaSuccess) return q4_fail(c, PKV_ERR_CUDA, "%s: %s", what, cudaGetErrorString(e));
+    return PKV_OK;
+}
+
+pkv_status pkv_q4_keep_rows(pkv_q4_cache *c, int32_t n_seqs, const int32_t *page_table, int32_t max_pages, const int32_t *lengths,
+                            int64_t n_rows, const int32_t *offsets, const int32_t *paths, int32_t max_path, const int32_t *counts,
+                            int32_t *lengths_out, void *stream) {
+    if (!c) return PKV_ERR_INVALID_ARG;
+    const char *what = "pkv_q4_keep_rows";
+    Q4KeepArgs a{};
+    if (pkv_status st = q4_rows(c, what, n_seqs, page_table, max_pages, lengths, n_rows, offsets, &a.rows)) return st;
+    if (max_path < 0) return q4_fail(c, PKV_ERR_INVALID_ARG, "%s: max_path %d out of range", what, max_path);
+    if (((uintptr_t)paths | (uintptr_t)counts | (uintptr_t)lengths_out) & 3)
+        return q4_fail(c, PKV_ERR_INVALID_ARG, "%s: paths, counts and lengths_out must be 4-byte aligned", what);
+    if (!c->dry && ((!paths && max_path > 0) || !counts || !lengths_out)) return q4_fail(c, PKV_ERR_INVALID_ARG, "%s: paths, counts or lengths_out is NULL", what);
+    if (lengths && lengths_out < lengths + n_seqs && lengths < lengths_out + n_seqs)
+        return q4_fail(c, PKV_ERR_INVALID_ARG, "%s: lengths_out overlaps lengths", what);
+    if (c->dry) return PKV_OK;
+    if (pkv_status st = q4_device(c, what)) return st;
+    a.geo = c->geo;
+    a.pool = c->pool;
+    a.paths = paths;
+    a.counts = counts;
+    a.lengths_out = lengths_out;
+    a.status = c->status;
+    a.max_path = max_path;
+    const cudaError_t e = launch_q4_keep(a, (cudaStream_t)stream);
+    if (e != cudaSuccess) return q4_fail(c, PKV_ERR_CUDA, "%s: %s", what, cudaGetErrorString(e));
+    return PKV_OK;
+}
+
+pkv_status pkv_q4_plan_workspace(const pkv_q4_cache *c, int32_t n_seqs, int64_t n_rows, int64_t *bytes) {
+    if (!c || !bytes || n_seqs < 1 || n_seqs > 65535 || n_rows < 0 || n_rows > 0x3fffffff) return PKV_ERR_INVALID_ARG;
+    *bytes = q4_plan_workspace(n_seqs, n_rows);
+    return PKV_OK;
+}
+
+pkv_status pkv_q4_plan(pkv_q4_cache *c, int32_t n_seqs, int32_t *page_table, int32_t max_pages, const int32_t *lengths, const int32_t *rows,
+                       const int32_t *spans, int32_t *ring, const int64_t *counters, int32_t window, int32_t sinks, int32_t *lengths_out,
+                       int32_t *spans_out, int64_t *counters_out, int32_t *offsets, int64_t n_rows, int32_t *positions, int64_t *slots,
+                       void *workspace, int64_t workspace_bytes, void *stream) {
+    if (!c) return PKV_ERR_INVALID_ARG;
+    const char *what = "pkv_q4_plan";
+    const Q4Geometry &g = c->geo;
+    if (n_seqs < 1 || n_seqs > 65535) return q4_fail(c, PKV_ERR_INVALID_ARG, "%s: n_seqs %d out of range", what, n_seqs);
+    if (max_pages < 1 || max_pages > ((1 << 30) >> g.page_shift)) return q4_fail(c, PKV_ERR_INVALID_ARG, "%s: max_pages %d out of range", what, max_pages);
+    if (n_rows < 0 || n_rows > 0x3fffffff) return q4_fail(c, PKV_ERR_INVALID_ARG, "%s: n_rows %lld out of range", what, (long long)n_rows);
+    const pkv_q4_select sel{window, sinks, nullptr, 0};
+    if (const char *error = q4_select_error(sel, 0)) return q4_fail(c, PKV_ERR_INVALID_ARG, "%s: %s", what, error);
+    if (((uintptr_t)page_table | (uintptr_t)lengths | (uintptr_t)rows | (uintptr_t)spans | (uintptr_t)ring | (uintptr_t)lengths_out |
+         (uintptr_t)spans_out | (uintptr_t)offsets | (uintptr_t)positions) & 3 ||
+        ((uintptr_t)counters | (uintptr_t)counters_out | (uintptr_t)slots) & 7)
+        return q4_fail(c, PKV_ERR_INVALID_ARG, "%s: int32 arrays must be 4-byte and int64 arrays 8-byte aligned", what);
+    if (!c->dry && (!page_table || !lengths || !rows || !spans || !ring || !counters || !lengths_out || !spans_out || !counters_out || !offsets))
+        return q4_fail(c, PKV_ERR_INVALID_ARG, "%s: only positions and slots may be NULL", what);
+    const long long need = q4_plan_workspace(n_seqs, n_rows);
     if (!c->dry && need > 0 && (!workspace || workspace_bytes < need || ((uintptr_t)workspace & 15)))
         return q4_fail(c, PKV_ERR_INVALID_ARG, "%s: the workspace needs %lld bytes, 16-byte aligned", what, need);
     if (c->dry) return PKV_OK;
     if (pkv_status st = q4_device(c, what)) return st;
-    a.geo = g;
-    a.pool = c->pool;
-    a.q = q; a.out = out; a.state = state;
-    a.q_row = q_row_stride; a.q_head = q_head_stride; a.out_row = out_row_stride; a.out_head = out_head_stride;
-    a.max_q_len = max_q_len;
-    a.max_len = max_len;
+    Q4PlanArgs a{};
+    a.n_seqs = n_seqs;
+    a.max_pages = max_pages;
+    a.page_shift = g.page_shift;
+    a.window = q4_selection(sel).window;
+    a.sink_pages = window > 0 ? (int)(((long long)q4_selection(sel).sinks + g.page - 1) >> g.page_shift) : 0;
+    a.n_pages = g.n_pages;
+    a.n_rows = n_rows;
+    a.table = page_table;
+    a.ring = ring;
+    a.lengths = lengths;
+    a.rows = rows;
+    a.spans = spans;
+    a.counters = reinterpret_cast<const long long *>(counters);
+    a.lengths_out = lengths_out;
+    a.spans_out = spans_out;
+    a.counters_out = reinterpret_cast<long long *>(counters_out);
+    a.offsets = offsets;
+    a.positions = positions;
+    a.slots = reinterpret_cast<long long *>(slots);
     a.workspace = static_cast<unsigned char *>(workspace);
-    a.status = c->status;
-    const cudaError_t e = launch_q4_attention(a, (cudaStream_t)stream);
+    const cudaError_t e = launch_q4_plan(a, (cudaStream_t)stream);
     if (e != cudaSuccess) return q4_fail(c, PKV_ERR_CUDA, "%s: %s", what, cudaGetErrorString(e));
     return PKV_OK;
 }

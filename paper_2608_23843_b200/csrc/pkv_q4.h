@@ -71,6 +71,43 @@ struct Q4AttentionArgs {
     int join;                          // ... the call's second kernel follows
     unsigned char *workspace;
     int *status;
+    int window, sinks;                 // a query sees `window` positions and the first `sinks`; 0: all up to its own
+    const unsigned long long *tree;    // NULL, or which new rows a row sees: [n_rows][tree_words] bits
+    int tree_words;
+};
+
+// Which positions a call's queries see, as the host knows it.
+struct Q4Select {
+    int window, sinks, tree;           // tree: 0 or 1
+};
+
+struct Q4TreeArgs {
+    Q4Rows rows;                       // (no table; lengths may be NULL)
+    const int *parents;
+    unsigned long long *tree;
+    int *depths, *status;
+    int max_q_len, words, window, sinks, chained;
+};
+
+struct Q4KeepArgs {
+    Q4Geometry geo;
+    Q4Rows rows;
+    unsigned char *pool;
+    const int *paths, *counts;
+    int *lengths_out, *status;
+    int max_path, chained;
+};
+
+struct Q4PlanArgs {
+    int n_seqs, max_pages, page_shift, window, sink_pages;
+    long long n_pages, n_rows;
+    int *table, *ring;
+    const int *lengths, *rows, *spans;
+    const long long *counters;
+    int *lengths_out, *spans_out, *offsets, *positions;
+    long long *counters_out, *slots;
+    unsigned char *workspace;
+    int chained;
 };
 
 // Calls of this cache are launched so that one may be set up while the kernel before it on the stream finishes
@@ -84,6 +121,12 @@ inline bool q4_chained() { return !unordered_decodes; }
 cudaError_t launch_q4_append(const Q4CopyArgs &a, cudaStream_t st);
 cudaError_t launch_q4_read(const Q4CopyArgs &a, cudaStream_t st);
 cudaError_t launch_q4_attention(Q4AttentionArgs a, cudaStream_t st);
+cudaError_t launch_q4_select(Q4AttentionArgs a, cudaStream_t st);      // attention over a part of the positions
+long long q4_select_workspace(const Q4Geometry &g, int n_seqs, int max_q_len, int max_len, const Q4Select &sel);
+cudaError_t launch_q4_tree_masks(Q4TreeArgs a, cudaStream_t st);
+cudaError_t launch_q4_keep(Q4KeepArgs a, cudaStream_t st);
+cudaError_t launch_q4_plan(Q4PlanArgs a, cudaStream_t st);
+long long q4_plan_workspace(int n_seqs, long long n_rows);
 cudaError_t q4_attention_setup();      // raises dynamic shared-memory limits, once per cache
 // the row-block kernel (pkv_q4_block.cu); n: CTAs, from q4_block_grid
 constexpr int kQ4BlockRows = 256;

@@ -8,6 +8,7 @@ There is no CPU fallback: if the library has not been built, loading fails.
 """
 import ctypes
 import os
+from typing import NamedTuple
 
 import torch
 
@@ -34,6 +35,8 @@ EXPORTS = [
     "pkv_get_rotation_schedule", "pkv_read_basis", "pkv_get_row_block_ranges",
     "pkv_q4_query_sizes", "pkv_q4_init_cache", "pkv_q4_destroy_cache", "pkv_q4_last_error", "pkv_q4_get_stats",
     "pkv_q4_append_kv", "pkv_q4_read_kv", "pkv_q4_attention_workspace", "pkv_q4_attention",
+    "pkv_q4_attention_select_workspace", "pkv_q4_attention_select", "pkv_q4_tree_masks", "pkv_q4_keep_rows",
+    "pkv_q4_plan_workspace", "pkv_q4_plan",
 ]
 
 
@@ -79,6 +82,10 @@ class PkvQ4Sizes(ctypes.Structure):
 
 class PkvQ4Stats(ctypes.Structure):
     _fields_ = [(n, ctypes.c_int64) for n in ("device_timeouts", "bad_pages", "bad_lengths")]
+
+
+class PkvQ4Select(ctypes.Structure):
+    _fields_ = [("window", ctypes.c_int32), ("sinks", ctypes.c_int32), ("tree", ctypes.c_void_p), ("tree_words", ctypes.c_int32)]
 
 
 class PkvError(RuntimeError):
@@ -136,6 +143,13 @@ def lib():
         L.pkv_q4_read_kv.argtypes = L.pkv_q4_append_kv.argtypes
         L.pkv_q4_attention_workspace.argtypes = [vp, i32, i32, i32, ctypes.POINTER(i64)]
         L.pkv_q4_attention.argtypes = [vp, i32, vp, i32, vp, i64, vp, i32, i32, vp, i64, i64, vp, i64, i64, vp, vp, i64, vp]
+        sel = ctypes.POINTER(PkvQ4Select)
+        L.pkv_q4_attention_select_workspace.argtypes = [vp, i32, i32, i32, sel, ctypes.POINTER(i64)]
+        L.pkv_q4_attention_select.argtypes = [vp, i32, vp, i32, vp, i64, vp, i32, i32, sel, vp, i64, i64, vp, i64, i64, vp, vp, i64, vp]
+        L.pkv_q4_tree_masks.argtypes = [vp, i32, vp, i64, vp, i32, vp, i32, i32, vp, i32, vp, vp]
+        L.pkv_q4_keep_rows.argtypes = [vp, i32, vp, i32, vp, i64, vp, vp, i32, vp, vp, vp]
+        L.pkv_q4_plan_workspace.argtypes = [vp, i32, i64, ctypes.POINTER(i64)]
+        L.pkv_q4_plan.argtypes = [vp, i32, vp, i32, vp, vp, vp, vp, vp, i32, i32, vp, vp, vp, vp, i64, vp, vp, vp, i64, vp]
         for name in EXPORTS:
             if name not in ("pkv_last_error", "pkv_q4_last_error"):
                 getattr(L, name).restype = ctypes.c_int32
@@ -421,6 +435,50 @@ def pkv_q4_attention(handle, n_seqs, page_table, max_pages, lengths, n_rows, off
                                              _ptr(workspace), workspace_bytes, _stream(stream)))
 
 
+def pkv_q4_attention_select_workspace(handle, n_seqs, max_q_len, max_len, window=0, sinks=0, tree=None, tree_words=0) -> int:
+    """tree: the masks, or anything that is not None (its contents do not matter for the size)."""
+    n = ctypes.c_int64(0)
+    sel = PkvQ4Select(window, sinks, None if tree is None else 8, tree_words)
+    st = lib().pkv_q4_attention_select_workspace(handle, n_seqs, max_q_len, max_len, ctypes.byref(sel), ctypes.byref(n))
+    if st != PKV_OK:
+        raise PkvError(st, "pkv_q4_attention_select_workspace(%r, %r, %r, window %r, sinks %r)" % (n_seqs, max_q_len, max_len, window, sinks))
+    return n.value
+
+
+def pkv_q4_attention_select(handle, n_seqs, page_table, max_pages, lengths, n_rows, offsets, max_q_len, max_len, window, sinks, tree,
+                            tree_words, q, q_strides, out, out_strides, state, workspace, workspace_bytes, stream=None):
+    """q, out, state as pkv_q4_attention(); tree: int64 [n_rows, tree_words] or None."""
+    sel = PkvQ4Select(window, sinks, _ptr(tree), tree_words)
+    _q4_check(handle, lib().pkv_q4_attention_select(handle, n_seqs, _ptr(page_table), max_pages, _ptr(lengths), n_rows, _ptr(offsets), max_q_len,
+                                                    max_len, ctypes.byref(sel), _ptr(q), *q_strides, _ptr(out), *out_strides, _ptr(state),
+                                                    _ptr(workspace), workspace_bytes, _stream(stream)))
+
+
+def pkv_q4_tree_masks(handle, n_seqs, lengths, n_rows, offsets, max_q_len, parents, window, sinks, tree, tree_words, depths, stream=None):
+    _q4_check(handle, lib().pkv_q4_tree_masks(handle, n_seqs, _ptr(lengths), n_rows, _ptr(offsets), max_q_len, _ptr(parents), window, sinks,
+                                              _ptr(tree), tree_words, _ptr(depths), _stream(stream)))
+
+
+def pkv_q4_keep_rows(handle, n_seqs, page_table, max_pages, lengths, n_rows, offsets, paths, max_path, counts, lengths_out, stream=None):
+    _q4_check(handle, lib().pkv_q4_keep_rows(handle, n_seqs, _ptr(page_table), max_pages, _ptr(lengths), n_rows, _ptr(offsets), _ptr(paths),
+                                             max_path, _ptr(counts), _ptr(lengths_out), _stream(stream)))
+
+
+def pkv_q4_plan_workspace(handle, n_seqs, n_rows) -> int:
+    n = ctypes.c_int64(0)
+    st = lib().pkv_q4_plan_workspace(handle, n_seqs, n_rows, ctypes.byref(n))
+    if st != PKV_OK:
+        raise PkvError(st, "pkv_q4_plan_workspace(%r, %r)" % (n_seqs, n_rows))
+    return n.value
+
+
+def pkv_q4_plan(handle, n_seqs, page_table, max_pages, lengths, rows, spans, ring, counters, window, sinks, lengths_out, spans_out,
+                counters_out, offsets, n_rows, positions, slots, workspace, workspace_bytes, stream=None):
+    _q4_check(handle, lib().pkv_q4_plan(handle, n_seqs, _ptr(page_table), max_pages, _ptr(lengths), _ptr(rows), _ptr(spans), _ptr(ring),
+                                        _ptr(counters), window, sinks, _ptr(lengths_out), _ptr(spans_out), _ptr(counters_out), _ptr(offsets),
+                                        n_rows, _ptr(positions), _ptr(slots), _ptr(workspace), workspace_bytes, _stream(stream)))
+
+
 # ---- convenience wrapper ----------------------------------------------------------
 def make_config(n_layers, n_kv_heads, n_q_heads, rank, sink_tokens, recent_tokens, max_seqs, max_pages_per_seq,
                 n_dense_slots, n_factor_slots, head_dim=128, page_size=64, rank_v=None, softmax_scale=0.0,
@@ -550,7 +608,7 @@ class Cache:
             pass
 
 
-_INT32 = torch.int32
+_INT32, _INT64 = torch.int32, torch.int64
 _Q4_DTYPES = {torch.bfloat16: PKV_DTYPE_BF16, torch.float16: PKV_DTYPE_FP16}
 
 
@@ -559,6 +617,17 @@ def make_q4_config(n_kv_heads, n_q_heads, n_pages, head_dim=128, page_size=64, g
     if dtype not in _Q4_DTYPES:
         raise PkvError(PKV_ERR_UNSUPPORTED, "dtype must be torch.bfloat16 or torch.float16, not %r" % (dtype,))
     return PkvQ4Config(n_kv_heads, n_q_heads, head_dim, page_size, group_size, _Q4_DTYPES[dtype], n_pages, softmax_scale, n_ctas)
+
+
+class Q4Plan(NamedTuple):
+    """What Q4Cache.plan() writes: int32 lengths [n_seqs], offsets [n_seqs + 1], positions [n_rows], spans [n_seqs, 2], int64 slots
+    [n_rows], counters [4] (head, tail, pages missing, requests refused)."""
+    lengths: torch.Tensor
+    offsets: torch.Tensor
+    positions: torch.Tensor
+    slots: torch.Tensor
+    spans: torch.Tensor
+    counters: torch.Tensor
 
 
 class Q4Cache:
@@ -668,35 +737,46 @@ class Q4Cache:
         self._call(fn, n_seqs, page_table.data_ptr(), max_pages, lengths.data_ptr(), n, offsets.data_ptr() if ragged else None,
                    k.data_ptr(), k_row, k_head, v.data_ptr(), v_row, v_head, self._stream())
 
-    def attention(self, page_table, lengths, q, out=None, offsets=None, max_q_len=None, max_len=0):
+    def attention(self, page_table, lengths, q, out=None, offsets=None, max_q_len=None, max_len=0, window=0, sinks=0, tree=None):
         """Attention of the newest positions over the cache; out (default: a new tensor of q's shape) is returned.  With
         offsets, max_q_len bounds the rows of a sequence (default, and at most: all rows); it and max_len, the longest length
         expected, choose the kernel and how the work is spread, so tight ones are faster.  Rows that belong to no sequence are
-        left as they were (undefined in a new tensor); without rows nothing is done."""
+        left as they were (undefined in a new tensor); without rows nothing is done.
+
+        window > 0: a query sees its own position, the window - 1 before it and the first `sinks` ones; pages that hold none of these may
+        have gone back to the pool.  tree (int64, q's rows by words, see tree_masks()): the rows are drafted tokens, which see the context (or its
+        part in the window) and the rows whose bits are set."""
         if out is None:
             out = torch.empty_like(q, memory_format=torch.contiguous_format)
         elif out.shape != q.shape:
             self._fail("out must have the shape of q")
-        self._attention(page_table, lengths, q, out, None, offsets, max_q_len, max_len)
+        self._attention(page_table, lengths, q, out, None, offsets, max_q_len, max_len, window, sinks, tree)
         return out
 
-    def attention_partial(self, page_table, lengths, q, state=None, offsets=None, max_q_len=None, max_len=0):
+    def attention_partial(self, page_table, lengths, q, state=None, offsets=None, max_q_len=None, max_len=0, window=0, sinks=0, tree=None):
         """The same as softmax states [..., d + 2] fp32 (o, m, l) for pkv_merge_attention_states()."""
         shape = (*q.shape[:-1], q.shape[-1] + 2)
         if state is None:
             state = torch.empty(shape, dtype=torch.float32, device=q.device)
         elif state.shape != shape or state.dtype != torch.float32 or state.device != self.device or not state.is_contiguous():
             self._fail("state must be a contiguous fp32 tensor of shape %r on %s" % (shape, self.device))
-        self._attention(page_table, lengths, q, None, state, offsets, max_q_len, max_len)
+        self._attention(page_table, lengths, q, None, state, offsets, max_q_len, max_len, window, sinks, tree)
         return state
 
-    def _attention(self, page_table, lengths, q, out, state, offsets, max_q_len, max_len):
+    def _attention(self, page_table, lengths, q, out, state, offsets, max_q_len, max_len, window, sinks, tree):
         n_seqs, max_pages = self._seqs(page_table, lengths, offsets)
         ragged = offsets is not None
         n, q_row, q_head = self._rows("q", q, self._hq, n_seqs, ragged)
         o_row, o_head = q_row, q_head
         if out is not None:
             _, o_row, o_head = self._rows("out", out, self._hq, n_seqs, ragged)
+        words = 0
+        if tree is not None:
+            if not (tree.dim() == q.dim() - 1 and tree.shape[:-1] == q.shape[:-2] and tree.dtype is _INT64 and tree.get_device() == self._device_index and
+                    tree.is_contiguous()):
+                self._fail("tree must be a contiguous int64 tensor %r on %s" % ([*q.shape[:-2], "words"], self.device))
+            words = tree.shape[-1]
+        part = words > 0 or window or sinks or tree is not None
         if n == 0:
             return
         if not ragged:
@@ -708,17 +788,116 @@ class Q4Cache:
         most = max_pages * self.cfg.page_size
         if not 0 < max_len < most:
             max_len = most
-        size = self._workspaces.get((n_seqs, max_q_len, max_len))
+        key = (n_seqs, max_q_len, max_len, window, sinks, words) if part else (n_seqs, max_q_len, max_len)
+        size = self._workspaces.get(key)
         if size is None:
             if len(self._workspaces) >= 256:
                 self._workspaces.clear()
-            size = self._workspaces[n_seqs, max_q_len, max_len] = pkv_q4_attention_workspace(self.handle, n_seqs, max_q_len, max_len)
+            if part:
+                size = pkv_q4_attention_select_workspace(self.handle, n_seqs, max_q_len, max_len, window, sinks, tree, words)
+            else:
+                size = pkv_q4_attention_workspace(self.handle, n_seqs, max_q_len, max_len)
+            self._workspaces[key] = size
         # (from the caching allocator at each call: ordered with this stream, and private to a graph that is being captured)
         work = torch.empty(size, dtype=torch.uint8, device=self.device) if size and not self.dry_run else None
-        self._call(lib().pkv_q4_attention, n_seqs, page_table.data_ptr(), max_pages, lengths.data_ptr(), n,
-                   offsets.data_ptr() if ragged else None, max_q_len, max_len, q.data_ptr(), q_row, q_head,
-                   None if out is None else out.data_ptr(), o_row, o_head, None if state is None else state.data_ptr(),
+        rest = (q.data_ptr(), q_row, q_head, None if out is None else out.data_ptr(), o_row, o_head, None if state is None else state.data_ptr(),
+                None if work is None else work.data_ptr(), size, self._stream())
+        shape = (n_seqs, page_table.data_ptr(), max_pages, lengths.data_ptr(), n, offsets.data_ptr() if ragged else None, max_q_len, max_len)
+        if part:
+            sel = PkvQ4Select(window, sinks, None if tree is None else tree.data_ptr(), words)
+            self._call(lib().pkv_q4_attention_select, *shape, ctypes.byref(sel), *rest)
+        else:
+            self._call(lib().pkv_q4_attention, *shape, *rest)
+
+    def _ints(self, name, t, shape, dtype=_INT32):
+        if not (t.shape == shape and t.dtype is dtype and t.get_device() == self._device_index and t.is_contiguous()):
+            self._fail("%s must be a contiguous %s tensor %r on %s" % (name, str(dtype)[6:], list(shape), self.device))
+        return t.data_ptr()
+
+    def _offsets(self, offsets, n_seqs):
+        return None if offsets is None else self._ints("offsets", offsets, (n_seqs + 1,))
+
+    def tree_masks(self, parents, lengths=None, offsets=None, max_q_len=None, window=0, sinks=0):
+        """Masks and depths of drafted tokens.  parents: int32 [n_seqs, n], or [rows] with offsets: the row of the same sequence, an
+        earlier one, that a row continues, -1 for the last token of the context.  -> (int64 parents.shape + (words,), for attention(tree=...),
+        int32 depths of parents' shape: a row's position is the context's length + its depth).  With a window and sinks, those of the attention call and the
+        sequences' lengths (the rows included).  With offsets, max_q_len bounds the rows of a sequence (default: all rows)."""
+        ragged = offsets is not None
+        if parents.dim() != (1 if ragged else 2):
+            self._fail("parents must be [rows] with offsets and [n_seqs, n] without")
+        n_seqs = offsets.numel() - 1 if ragged else parents.shape[0]
+        n = parents.numel()
+        if not ragged:
+            max_q_len = parents.shape[1]
+        elif max_q_len is None:
+            max_q_len = n
+        words = max(1, -(-max_q_len // 64))
+        if lengths is None and window and sinks:
+            self._fail("a window with sinks needs the sequences' lengths")
+        self._ints("parents", parents, parents.shape)
+        length_ptr = None if lengths is None else self._ints("lengths", lengths, (n_seqs,))
+        off = self._offsets(offsets, n_seqs)
+        masks = torch.empty((*parents.shape, words), dtype=_INT64, device=self.device)
+        depths = torch.empty(parents.shape, dtype=_INT32, device=self.device)
+        self._call(lib().pkv_q4_tree_masks, n_seqs, length_ptr, n, off, max_q_len, parents.data_ptr(), window, sinks, masks.data_ptr(), words,
+                   depths.data_ptr(), self._stream())
+        return masks, depths
+
+    def keep_rows(self, page_table, lengths, paths, counts, new_rows, offsets=None, out=None):
+        """Keeps the accepted ones of the newest rows: row paths[s, i] (int32 [n_seqs, m]) of sequence s becomes its new row i, for
+        i < counts[s] (int32 [n_seqs]); rows of a path ascend.  new_rows: how many new rows each sequence has, or with offsets how many
+        the call has.  -> the lengths (out, not overlapping `lengths`, or a new tensor)."""
+        n_seqs, max_pages = self._seqs(page_table, lengths, offsets)
+        if paths.dim() != 2:
+            self._fail("paths must be int32 [n_seqs, m]")
+        self._ints("paths", paths, (n_seqs, paths.shape[1]))
+        self._ints("counts", counts, (n_seqs,))
+        if out is None:
+            out = torch.empty_like(lengths)
+        self._ints("out", out, (n_seqs,))
+        n = new_rows if offsets is not None else new_rows * n_seqs
+        self._call(lib().pkv_q4_keep_rows, n_seqs, page_table.data_ptr(), max_pages, lengths.data_ptr(), n, None if offsets is None else offsets.data_ptr(),
+                   paths.data_ptr(), paths.shape[1], counts.data_ptr(), out.data_ptr(), self._stream())
+        return out
+
+    def new_ring(self, pages=None):
+        """Free pages (default: all of the pool) as plan() takes them: (ring int32 [n_pages], counters int64 [4])."""
+        n = self.cfg.n_pages
+        pages = torch.arange(n, dtype=_INT32) if pages is None else torch.as_tensor(pages, dtype=_INT32).flatten().cpu()
+        if pages.numel() > n or (pages.numel() and not (0 <= int(pages.min()) and int(pages.max()) < n)) or pages.unique().numel() != pages.numel():
+            self._fail("pages must be different page numbers of the pool")
+        ring = torch.full((n,), -1, dtype=_INT32)
+        ring[:pages.numel()] = pages
+        return ring.to(self.device), torch.tensor([0, pages.numel(), 0, 0], dtype=_INT64, device=self.device)
+
+    def plan(self, page_table, lengths, rows, spans, ring, counters, n_rows, window=0, sinks=0, out=None):
+        """Plans a step on the device (see pkv_q4_plan in include/pkv.h): rows int32 [n_seqs] new rows for each request, -1 where it is
+        done; spans int32 [n_seqs, 2] the table entries it holds; ring, counters: free pages, see new_ring(); n_rows: a bound of the new rows
+        in all.  Writes new entries into page_table and returned pages into ring.  -> Q4Plan of new tensors, or `out`, whose
+        lengths, spans and counters may be the ones given (in place).  Where pages are missing or requests make no sense nothing is done: counters[2:]."""
+        n_seqs, max_pages = self._seqs(page_table, lengths, None)
+        dev = self.device
+        if out is None:
+            ints = torch.empty(n_seqs * 4 + 1 + n_rows, dtype=_INT32, device=dev)      # (one allocation of each type)
+            longs = torch.empty(4 + n_rows, dtype=_INT64, device=dev)
+            out = Q4Plan(ints[:n_seqs], ints[n_seqs:2 * n_seqs + 1], ints[4 * n_seqs + 1:], longs[4:], ints[2 * n_seqs + 1:4 * n_seqs + 1].view(n_seqs, 2),
+                         longs[:4])
+        args = [self._ints("rows", rows, (n_seqs,)), self._ints("spans", spans, (n_seqs, 2)), self._ints("ring", ring, (self.cfg.n_pages,)),
+                self._ints("counters", counters, (4,), _INT64)]
+        outs = [self._ints("out.lengths", out.lengths, (n_seqs,)), self._ints("out.spans", out.spans, (n_seqs, 2)),
+                self._ints("out.counters", out.counters, (4,), _INT64), self._ints("out.offsets", out.offsets, (n_seqs + 1,))]
+        pos = None if out.positions is None else self._ints("out.positions", out.positions, (n_rows,))
+        slots = None if out.slots is None else self._ints("out.slots", out.slots, (n_rows,), _INT64)
+        key = (n_seqs, n_rows)
+        size = self._workspaces.get(key)
+        if size is None:
+            if len(self._workspaces) >= 256:
+                self._workspaces.clear()
+            size = self._workspaces[key] = pkv_q4_plan_workspace(self.handle, n_seqs, n_rows)
+        work = torch.empty(size, dtype=torch.uint8, device=dev) if size and not self.dry_run else None
+        self._call(lib().pkv_q4_plan, n_seqs, page_table.data_ptr(), max_pages, lengths.data_ptr(), *args, window, sinks, *outs, n_rows, pos, slots,
                    None if work is None else work.data_ptr(), size, self._stream())
+        return out
 
     def stats(self):
         if not self.dry_run:
