@@ -448,7 +448,6 @@ const char *q4_select_error(const pkv_q4_select &s, int max_q_len) {
     if (s.tree && (s.tree_words < 1 || s.tree_words < (max_q_len + 63LL) / 64)) return "tree_words must be max_q_len / 64, rounded up, at least";
     return nullptr;
 }
-bool q4_selects(const pkv_q4_select &s) { return s.window > 0 || s.tree; }
 // (positions stay below 2^30: a wider window is none, and sums of a few stay in 32 bits)
 Q4Select q4_selection(const pkv_q4_select &s) { return Q4Select{std::min(s.window, 1 << 30), std::min(s.sinks, 1 << 30), s.tree != nullptr}; }
 
@@ -473,10 +472,10 @@ pkv_status q4_attend(pkv_q4_cache *c, const char *what, int32_t n_seqs, const in
                                                "head on top of another", what);
     if (select)
         if (const char *error = q4_select_error(*select, n_rows > 0 ? max_q_len : 0)) return q4_fail(c, PKV_ERR_INVALID_ARG, "%s: %s", what, error);
-    const bool part = select && q4_selects(*select);
+    const Q4Select sel = select ? q4_selection(*select) : Q4Select{};
     if ((uintptr_t)state & 7) return q4_fail(c, PKV_ERR_INVALID_ARG, "%s: state must be 8-byte aligned", what);
     if (n_rows == 0 || max_q_len == 0) return PKV_OK;
-    const long long need = part ? q4_select_workspace(g, n_seqs, max_q_len, max_len, q4_selection(*select)) : q4_attention_workspace(g, n_seqs, max_q_len, max_len);
+    const long long need = q4_attention_workspace(g, n_seqs, max_q_len, max_len, sel);
     if (!c->dry && need > 0 && (!workspace || workspace_bytes < need || ((uintptr_t)workspace & 15)))
         return q4_fail(c, PKV_ERR_INVALID_ARG, "%s: the workspace needs %lld bytes, 16-byte aligned", what, need);
     if (c->dry) return PKV_OK;
@@ -489,13 +488,13 @@ pkv_status q4_attend(pkv_q4_cache *c, const char *what, int32_t n_seqs, const in
     a.max_len = max_len;
     a.workspace = static_cast<unsigned char *>(workspace);
     a.status = c->status;
-    if (part) {
-        a.window = q4_selection(*select).window;
-        a.sinks = q4_selection(*select).sinks;
+    a.window = sel.window;
+    a.sinks = sel.sinks;
+    if (select) {
         a.tree = reinterpret_cast<const unsigned long long *>(select->tree);
         a.tree_words = select->tree_words;
     }
-    const cudaError_t e = part ? launch_q4_select(a, (cudaStream_t)stream) : launch_q4_attention(a, (cudaStream_t)stream);
+    const cudaError_t e = launch_q4_attention(a, (cudaStream_t)stream);
     if (e != cudaSuccess) return q4_fail(c, PKV_ERR_CUDA, "%s: %s", what, cudaGetErrorString(e));
     return PKV_OK;
 }
@@ -566,7 +565,7 @@ pkv_status pkv_q4_read_kv(pkv_q4_cache *c, int32_t n_seqs, const int32_t *page_t
 
 pkv_status pkv_q4_attention_workspace(const pkv_q4_cache *c, int32_t n_seqs, int32_t max_q_len, int32_t max_len, int64_t *bytes) {
     if (!c || !bytes || n_seqs < 1 || n_seqs > 65535 || max_q_len < 1 || max_len < 1) return PKV_ERR_INVALID_ARG;
-    *bytes = q4_attention_workspace(c->geo, n_seqs, max_q_len, max_len);
+    *bytes = q4_attention_workspace(c->geo, n_seqs, max_q_len, max_len, Q4Select{});
     return PKV_OK;
 }
 
@@ -582,8 +581,7 @@ pkv_status pkv_q4_attention_select_workspace(const pkv_q4_cache *c, int32_t n_se
                                              const pkv_q4_select *select, int64_t *bytes) {
     if (!c || !bytes || !select || n_seqs < 1 || n_seqs > 65535 || max_q_len < 1 || max_len < 1) return PKV_ERR_INVALID_ARG;
     if (q4_select_error(*select, max_q_len)) return PKV_ERR_INVALID_ARG;
-    *bytes = q4_selects(*select) ? q4_select_workspace(c->geo, n_seqs, max_q_len, max_len, q4_selection(*select))
-                                 : q4_attention_workspace(c->geo, n_seqs, max_q_len, max_len);
+    *bytes = q4_attention_workspace(c->geo, n_seqs, max_q_len, max_len, q4_selection(*select));
     return PKV_OK;
 }
 

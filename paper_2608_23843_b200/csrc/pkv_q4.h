@@ -121,8 +121,6 @@ inline bool q4_chained() { return !unordered_decodes; }
 cudaError_t launch_q4_append(const Q4CopyArgs &a, cudaStream_t st);
 cudaError_t launch_q4_read(const Q4CopyArgs &a, cudaStream_t st);
 cudaError_t launch_q4_attention(Q4AttentionArgs a, cudaStream_t st);
-cudaError_t launch_q4_select(Q4AttentionArgs a, cudaStream_t st);      // attention over a part of the positions
-long long q4_select_workspace(const Q4Geometry &g, int n_seqs, int max_q_len, int max_len, const Q4Select &sel);
 cudaError_t launch_q4_tree_masks(Q4TreeArgs a, cudaStream_t st);
 cudaError_t launch_q4_keep(Q4KeepArgs a, cudaStream_t st);
 cudaError_t launch_q4_plan(Q4PlanArgs a, cudaStream_t st);
@@ -131,10 +129,10 @@ cudaError_t q4_attention_setup();      // raises dynamic shared-memory limits, o
 // the row-block kernel (pkv_q4_block.cu); n: CTAs, from q4_block_grid
 constexpr int kQ4BlockRows = 256;
 cudaError_t q4_block_setup();
-int q4_block_grid(const Q4Geometry &g, int n_seqs, int max_q_len, int max_len);
-long long q4_block_workspace(const Q4Geometry &g, int n_seqs, int max_q_len, int max_len);
+int q4_block_grid(const Q4Geometry &g, int n_seqs, int max_q_len, int max_len, const Q4Select &sel);
+long long q4_block_workspace(const Q4Geometry &g, int n_seqs, int max_q_len, int max_len, const Q4Select &sel);
 cudaError_t launch_q4_block(const Q4AttentionArgs &a, int n, cudaStream_t st);
-long long q4_attention_workspace(const Q4Geometry &g, int n_seqs, int max_q_len, int max_len);
+long long q4_attention_workspace(const Q4Geometry &g, int n_seqs, int max_q_len, int max_len, const Q4Select &sel);
 
 // byte offsets inside a tile
 __host__ __device__ constexpr int q4_v_base(int d) { return kQ4Tile * d / 2; }

@@ -190,15 +190,30 @@ __device__ __forceinline__ void q4_pass(float *pass, float F, float A, const uin
 struct Q4Cursor {
     int seq, tile, head, unit;         // seq == n_seqs: past the end
     int T, tiles, units;               // of the sequence
+    int su, gap, lo;                   // kSel: see Q4Span (every row tile visits what the sequence's rows see)
 };
+template <bool kSel>
+__device__ __forceinline__ int q4_unit_at(const Q4Cursor &c, int unit) { return unit + (kSel && unit >= c.su ? c.gap : 0); }
 
+// units of 64 tokens that a sequence's rows visit
+template <bool kSel>
+__device__ __forceinline__ int q4_seq_units(const Q4AttentionArgs &a, int T, int all) {
+    return kSel ? q4_span(a, T, q4_lowest(a, T - all, 0)).units : max(1, (T + kQ4Unit - 1) / kQ4Unit);
+}
+template <bool kSel>
 __device__ __forceinline__ void q4_load_seq(const Q4AttentionArgs &a, int rows_per_tile, Q4Cursor &c) {
     int first, all;
     const int n = q4_new_rows(a, c.seq, first, all, nullptr);
     c.T = q4_length(a.rows, a.geo, c.seq, nullptr);
     c.tiles = (n * a.geo.group + rows_per_tile - 1) / rows_per_tile;
-    c.units = max(1, (c.T + kQ4Unit - 1) / kQ4Unit);
+    if (kSel) {
+        const Q4Span r = q4_span(a, c.T, q4_lowest(a, c.T - all, 0));
+        c.units = r.units; c.su = r.su; c.gap = r.gap; c.lo = r.lo;
+    } else {
+        c.units = max(1, (c.T + kQ4Unit - 1) / kQ4Unit);
+    }
 }
+template <bool kSel>
 __device__ __forceinline__ void q4_advance(const Q4AttentionArgs &a, int rows_per_tile, Q4Cursor &c, int by) {
     c.unit += by;
     while (c.unit >= c.units) {
@@ -209,14 +224,15 @@ __device__ __forceinline__ void q4_advance(const Q4AttentionArgs &a, int rows_pe
                 c.tile = 0;
                 do {
                     if (++c.seq >= a.rows.n_seqs) return;
-                    q4_load_seq(a, rows_per_tile, c);
+                    q4_load_seq<kSel>(a, rows_per_tile, c);
                 } while (c.tiles == 0);
             }
         }
     }
 }
 
-template <int D, int NG, bool H16, int NT>
+// kSel: the queries see a part of the positions
+template <int D, int NG, bool H16, int NT, bool kSel>
 __global__ void __launch_bounds__(Q4Shape<D, NG, NT>::kThreads, q4_ctas_per_sm(NT)) q4_decode_kernel(const __grid_constant__ Q4AttentionArgs a) {
     using S = Q4Shape<D, NG, NT>;
     constexpr int NW = D / 32, WPG = NW / NG, R = 8 * NT;      // 32-channel words per row, words per scale, query rows
@@ -228,7 +244,9 @@ __global__ void __launch_bounds__(Q4Shape<D, NG, NT>::kThreads, q4_ctas_per_sm(N
     __shared__ float2 ml[kCons][8];
     __shared__ float refs[kCons][NT][32];                      // R of the lane's group and column, see q4_own_max
     __shared__ uint32_t gains[kCons][NT][NG][4];               // bf16, two columns to a word
-    __shared__ int vis[8 * NT];                                // tokens a column's query sees
+    __shared__ int vis[kSel ? 1 : 8 * NT];                     // tokens a column's query sees
+    __shared__ Q4Seen part[kSel ? 8 * NT : 1];                 // kSel: which ones
+    __shared__ uint16_t seen[kSel ? kCons : 1][8 * NT][kQ4UnitTiles];      // ... in a warp's unit, a bit each
     __shared__ uint4 queries[NT][NW][32];                      // of the segment, as the lanes of a warp take them
     __shared__ long long sums[kQ4Warps], found_at;
     __shared__ int found_seq, offs[kCons], gave_up;
@@ -248,7 +266,7 @@ __global__ void __launch_bounds__(Q4Shape<D, NG, NT>::kThreads, q4_ctas_per_sm(N
         if (s >= n_seqs) return 0;
         int first, all;
         const int n = q4_new_rows(a, s, first, all, st), T = q4_length(a.rows, geo, s, st);
-        return (long long)((n * geo.group + R - 1) / R) * H * (a.whole ? 1 : max(1, (T + kQ4Unit - 1) / kQ4Unit) + kSegCost);
+        return (long long)((n * geo.group + R - 1) / R) * H * (a.whole ? 1 : q4_seq_units<kSel>(a, T, all) + kSegCost);
     };
     long long total = 0;
     if (n_seqs == 1) {
@@ -312,7 +330,7 @@ __global__ void __launch_bounds__(Q4Shape<D, NG, NT>::kThreads, q4_ctas_per_sm(N
         seg.seq = found_seq;
         at0 = found_at;
     }
-    q4_load_seq(a, R, seg);
+    q4_load_seq<kSel>(a, R, seg);
     int left_cta;                                              // units of the CTA
     long long seg_pos = 0;                                     // where the current segment begins, on the scale of the weights
     if (a.whole) {
@@ -322,7 +340,7 @@ __global__ void __launch_bounds__(Q4Shape<D, NG, NT>::kThreads, q4_ctas_per_sm(N
         Q4Cursor w = seg;
         left_cta = w.units;
         for (int k = 1; k < (int)(end - begin); ++k) {
-            q4_advance(a, R, w, w.units);
+            q4_advance<kSel>(a, R, w, w.units);
             left_cta += w.units;
         }
     } else {
@@ -334,7 +352,7 @@ __global__ void __launch_bounds__(Q4Shape<D, NG, NT>::kThreads, q4_ctas_per_sm(N
         seg_pos = begin - off;
         if (seg.unit == seg.units) {                           // the share begins behind a segment's units
             seg_pos += len;
-            q4_advance(a, R, seg, 0);
+            q4_advance<kSel>(a, R, seg, 0);
         }
         left_cta = 0;
         Q4Cursor w = seg;
@@ -344,7 +362,7 @@ __global__ void __launch_bounds__(Q4Shape<D, NG, NT>::kThreads, q4_ctas_per_sm(N
             left_cta += here;
             if (here < w.units - w.unit) break;
             pos += w.units + kSegCost;
-            q4_advance(a, R, w, w.units - w.unit);
+            q4_advance<kSel>(a, R, w, w.units - w.unit);
         }
         if (left_cta == 0) {
             if (tid == 0 && joined) parts[blockIdx.x].seq = -1;
@@ -357,27 +375,29 @@ __global__ void __launch_bounds__(Q4Shape<D, NG, NT>::kThreads, q4_ctas_per_sm(N
         // ---- copies: 32 units are looked up at a time, a lane each, and issued in turn ----
         const int per_page = min(kQ4Unit, geo.page), n_parts = kQ4Unit / per_page, per_tiles = per_page / kQ4Tile;      // copies per unit: 1, 2 or 4
         Q4Cursor nx = seg;
-        if (lane < left_cta) q4_advance(a, R, nx, lane);
+        if (lane < left_cta) q4_advance<kSel>(a, R, nx, lane);
         bool ok = true;
         int st = 0, use = 0, u = 0;                            // stage, times it has been used before; units issued
         for (int at = lane; u < left_cta && ok; at += 32) {
             uint32_t bits = 0;
             int pg[4] = {-1, -1, -1, -1};
-            const int t0 = nx.unit * kQ4Unit, head = nx.head;
+            const int t0 = q4_unit_at<kSel>(nx, nx.unit) * kQ4Unit, head = nx.head;
             if (at < left_cta) {
                 const int tiles = (max(0, min(kQ4Unit, nx.T - t0)) + kQ4Tile - 1) / kQ4Tile;
+                bits = kSel ? q4_needed(a, t0, nx.lo, tiles, n_parts, per_page, per_tiles) : (1u << tiles) - 1u;
+                const uint32_t wanted = bits;
+                auto want = [&](int i) { return kSel ? (wanted >> (i * per_tiles) & 1u) != 0u : i * per_tiles < tiles; };      // (a part from its first tile on)
 #pragma unroll
                 for (int i = 0; i < 4; ++i)
-                    if (i * per_tiles < tiles)
+                    if (want(i))
                         pg[i] = __ldg(a.rows.table + (long long)nx.seq * a.rows.max_pages + ((t0 + i * per_page) >> geo.page_shift));
-                bits = (1u << tiles) - 1u;
 #pragma unroll
                 for (int i = 0; i < 4; ++i)
-                    if (i * per_tiles < tiles && (unsigned)pg[i] >= (unsigned)geo.n_pages) {
+                    if (want(i) && (unsigned)pg[i] >= (unsigned)geo.n_pages) {
                         atomicAdd(a.status + 1, 1);
                         bits &= ~(((1u << per_tiles) - 1u) << (i * per_tiles));
                     }
-                if (at + 32 < left_cta) q4_advance(a, R, nx, 32);
+                if (at + 32 < left_cta) q4_advance<kSel>(a, R, nx, 32);
             }
             for (int i = 0; i < 32 && u < left_cta; ++i, ++u) {
                 const uint32_t bar = smem_u32(&full[st]);
@@ -424,7 +444,14 @@ __global__ void __launch_bounds__(Q4Shape<D, NG, NT>::kThreads, q4_ctas_per_sm(N
         uint32_t gained = 0;                                   // bit nt: some group of a column has a reference of its own
 #pragma unroll
         for (int i = 0; i < (NG + 1) / 2; ++i) big_run[i] = 0;
-        int vis_all = seg.T;                                   // tokens every row of the tile sees
+        int vis_all = seg.T, lo_all = 0;                       // tokens every row of the tile sees (kSel: from lo_all on)
+        if (kSel) {
+            const int col = lane % (8 * NT), j = (seg.tile * R + col) / G;
+            const Q4Seen v = j < n ? q4_seen(a, seg.T, all, first, j) : Q4Seen{0, seg.T};
+            if (warp == 0 && lane < 8 * NT) part[col] = v;
+            vis_all = min(vis_all, v.end);
+            lo_all = (int)__reduce_max_sync(0xffffffffu, (unsigned)v.lo);
+        }
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
             const int row = seg.tile * R + nt * 8 + g, j = row / G, h = row - j * G;
@@ -505,9 +532,11 @@ __global__ void __launch_bounds__(Q4Shape<D, NG, NT>::kThreads, q4_ctas_per_sm(N
             for (int b = 0; b < 2; ++b) {
                 const int col = 2 * c + b, r2 = seg.tile * R + nt * 8 + col, j2 = r2 / G;
                 fb[b] = fmaxf(__shfl_sync(0xffffffffu, fr, 4 * col), 1.2e-38f);      // (never 0: a hidden score is -inf)
-                const int v = j2 < n ? seg.T - all + j2 + 1 : seg.T;
-                if (warp == 0 && g == 0) vis[nt * 8 + col] = v;
-                vis_all = min(vis_all, v);
+                if (!kSel) {
+                    const int v = j2 < n ? seg.T - all + j2 + 1 : seg.T;
+                    if (warp == 0 && g == 0) vis[nt * 8 + col] = v;
+                    vis_all = min(vis_all, v);
+                }
                 F[nt][b] = pass[nt][b] = kNegInf;
             }
             refs[warp][nt][lane] = kNegInf;
@@ -528,11 +557,23 @@ __global__ void __launch_bounds__(Q4Shape<D, NG, NT>::kThreads, q4_ctas_per_sm(N
         const bool any = at < seg_hi;
         int st_last = 0;
         while (at < seg_hi) {
-            const int t_unit = (seg.unit + at - seg_lo) * kQ4Unit;
+            const int t_unit = q4_unit_at<kSel>(seg, seg.unit + at - seg_lo) * kQ4Unit;
             uint32_t tiles = 0;
             if ((mbar_wait_warp(smem_u32(&full[st]), phase, abort_flag))) tiles = tiles_here[st];
             else if (lane == 0 && !*abort_flag) { *abort_flag = 1; atomicAdd(a.status, 1); }      // (the unit counts as not there)
-            const bool whole = tiles == (1u << kQ4UnitTiles) - 1u && t_unit + kQ4Unit <= vis_all;
+            const bool whole = tiles == (1u << kQ4UnitTiles) - 1u && t_unit + kQ4Unit <= vis_all && (!kSel || t_unit >= lo_all || t_unit + kQ4Unit <= a.sinks);
+            if (kSel && !whole) {                              // what each row sees of the unit, a lane each
+                if (lane < 8 * NT) {
+                    const int row = seg.tile * R + lane, j = row / G;
+                    unsigned long long m = q4_below(seg.T - t_unit);
+                    if (j < n) m = q4_unit_mask(a, part[lane], t_unit, seg.T, all, first + j);
+                    m &= q4_tile_mask(tiles);
+                    *reinterpret_cast<uint2 *>(&seen[warp][lane][0]) = make_uint2((uint32_t)m, (uint32_t)(m >> 32));
+                }
+                __syncwarp();
+            }
+            // (not kept in registers)
+            auto sees = [&](int col, int tile) -> uint32_t { return kSel ? (whole ? 0xffffu : *const_cast<const volatile uint16_t *>(&seen[warp][col][tile])) : 0u; };
             const unsigned char *sp = smem + st * S::kStage;
             // bounds of the value scales so far (lane: tokens 2 lane, 2 lane + 1)
             {
@@ -637,8 +678,12 @@ __global__ void __launch_bounds__(Q4Shape<D, NG, NT>::kThreads, q4_ctas_per_sm(N
                         for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
                             for (int i = 0; i < 4; ++i) {
-                                const int t = t0 + tl * kQ4Tile + g + (i >> 1) * 8;
-                                if (!(t < vis[nt * 8 + 2 * c + (i & 1)] && ((here >> tl) & 1))) sc[tl][nt][i] = -INFINITY;
+                                if (kSel) {
+                                    if (!(sees(nt * 8 + 2 * c + (i & 1), step * TS + tl) >> (g + (i >> 1) * 8) & 1u)) sc[tl][nt][i] = -INFINITY;
+                                } else {
+                                    const int t = t0 + tl * kQ4Tile + g + (i >> 1) * 8;
+                                    if (!(t < vis[nt * 8 + 2 * c + (i & 1)] && ((here >> tl) & 1))) sc[tl][nt][i] = -INFINITY;
+                                }
                             }
                 }
                 // ---- softmax ----
@@ -768,12 +813,20 @@ __global__ void __launch_bounds__(Q4Shape<D, NG, NT>::kThreads, q4_ctas_per_sm(N
                             if (kCareful) {                    // a hidden token's weight is zero whatever its scale holds
                                 const uint32_t gain = *const_cast<const volatile uint32_t *>(&gains[warp][nt][k][c]);      // (not kept in registers)
                                 w0 *= bf16lo_f(gain); w1 *= bf16hi_f(gain); w2 *= bf16lo_f(gain); w3 *= bf16hi_f(gain);
-                                const int t = t0 + tl * kQ4Tile + g;
-                                const bool ok = (here >> tl) & 1;
-                                if (!(ok && t < vis[nt * 8 + 2 * c + 0])) w0 = 0.f;
-                                if (!(ok && t < vis[nt * 8 + 2 * c + 1])) w1 = 0.f;
-                                if (!(ok && t + 8 < vis[nt * 8 + 2 * c + 0])) w2 = 0.f;
-                                if (!(ok && t + 8 < vis[nt * 8 + 2 * c + 1])) w3 = 0.f;
+                                if (kSel) {
+                                    const uint32_t m0 = sees(nt * 8 + 2 * c, step * TS + tl) >> g, m1 = sees(nt * 8 + 2 * c + 1, step * TS + tl) >> g;
+                                    if (!(m0 & 1u)) w0 = 0.f;
+                                    if (!(m1 & 1u)) w1 = 0.f;
+                                    if (!(m0 & 256u)) w2 = 0.f;
+                                    if (!(m1 & 256u)) w3 = 0.f;
+                                } else {
+                                    const int t = t0 + tl * kQ4Tile + g;
+                                    const bool ok = (here >> tl) & 1;
+                                    if (!(ok && t < vis[nt * 8 + 2 * c + 0])) w0 = 0.f;
+                                    if (!(ok && t < vis[nt * 8 + 2 * c + 1])) w1 = 0.f;
+                                    if (!(ok && t + 8 < vis[nt * 8 + 2 * c + 0])) w2 = 0.f;
+                                    if (!(ok && t + 8 < vis[nt * 8 + 2 * c + 1])) w3 = 0.f;
+                                }
                             }
                             b0[nt] = movmatrix(pack_f16(w0, w1));
                             b1[nt] = movmatrix(pack_f16(w2, w3));
@@ -902,7 +955,7 @@ __global__ void __launch_bounds__(Q4Shape<D, NG, NT>::kThreads, q4_ctas_per_sm(N
         seg_lo = seg_hi;
         if (seg_lo < left_cta) {
             seg_pos += seg.units + kSegCost;
-            q4_advance(a, R, seg, seg.units - seg.unit);
+            q4_advance<kSel>(a, R, seg, seg.units - seg.unit);
         }
     }
 }
@@ -1053,23 +1106,34 @@ int q4_grid(const Q4Geometry &g, int n_seqs, int max_q_len, int max_len) {
 cudaError_t q4_attention_setup() {
     cudaError_t e = q4_block_setup();
     if (e != cudaSuccess) return e;
-#define PKV_Q4_SETUP1(D, NG, H16, NT) \
-    if ((e = cudaFuncSetAttribute(q4_decode_kernel<D, NG, H16, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, Q4Shape<D, NG, NT>::kSmem)) != cudaSuccess) return e;
+#define PKV_Q4_SETUP2(D, NG, H16, NT, SEL) \
+    if ((e = cudaFuncSetAttribute(q4_decode_kernel<D, NG, H16, NT, SEL>, cudaFuncAttributeMaxDynamicSharedMemorySize, Q4Shape<D, NG, NT>::kSmem)) != cudaSuccess) return e;
+#define PKV_Q4_SETUP1(D, NG, H16, NT) PKV_Q4_SETUP2(D, NG, H16, NT, false) PKV_Q4_SETUP2(D, NG, H16, NT, true)
 #define PKV_Q4_SETUP(D, NG) PKV_Q4_SETUP1(D, NG, false, 1) PKV_Q4_SETUP1(D, NG, false, 2) PKV_Q4_SETUP1(D, NG, true, 1) PKV_Q4_SETUP1(D, NG, true, 2)
     PKV_Q4_SHAPES(PKV_Q4_SETUP)
     return cudaSuccess;
 }
 
-long long q4_attention_workspace(const Q4Geometry &g, int n_seqs, int max_q_len, int max_len) {
-    if (q4_by_blocks(g, n_seqs, max_q_len, max_len)) return q4_block_workspace(g, n_seqs, max_q_len, max_len);
+// Tokens that a call's rows visit of a sequence at most, as far as the host can tell: what steers the launch where the queries see a part.
+int q4_visited(int max_q_len, int max_len, const Q4Select &sel) {
+    const long long most = (long long)sel.window + max_q_len + sel.sinks + 2 * kQ4Unit - 2;      // (units are cut at both ends)
+    return sel.window > 0 && most < max_len ? (int)most : max_len;
+}
+
+long long q4_attention_workspace(const Q4Geometry &g, int n_seqs, int max_q_len, int max_len, const Q4Select &sel) {
+    max_len = q4_visited(max_q_len, max_len, sel);
+    if (q4_by_blocks(g, n_seqs, max_q_len, max_len)) return q4_block_workspace(g, n_seqs, max_q_len, max_len, sel);
     const int n = q4_grid(g, n_seqs, max_q_len, max_len);
     return n <= 1 || q4_whole(max_len) ? 0 : q4_parts_bytes(n) + 2LL * n * q4_state_floats(q4_rows_per_tile(g, max_q_len), g.head_dim) * 4;
 }
 
 cudaError_t launch_q4_attention(Q4AttentionArgs a, cudaStream_t st) {
     const Q4Geometry &g = a.geo;
+    const Q4Select sel{a.window, a.sinks, a.tree != nullptr};
+    const bool part = a.window > 0 || a.tree;
+    a.max_len = q4_visited(a.max_q_len, a.max_len, sel);
     const bool blocks = q4_by_blocks(g, a.rows.n_seqs, a.max_q_len, a.max_len);
-    const int n = blocks ? q4_block_grid(g, a.rows.n_seqs, a.max_q_len, a.max_len) : q4_grid(g, a.rows.n_seqs, a.max_q_len, a.max_len);
+    const int n = blocks ? q4_block_grid(g, a.rows.n_seqs, a.max_q_len, a.max_len, sel) : q4_grid(g, a.rows.n_seqs, a.max_q_len, a.max_len);
     const int R = blocks ? kQ4BlockRows : q4_rows_per_tile(g, a.max_q_len);
     a.whole = !blocks && q4_whole(a.max_len);
     a.chained = q4_chained();
@@ -1087,7 +1151,7 @@ cudaError_t launch_q4_attention(Q4AttentionArgs a, cudaStream_t st) {
         cfg.gridDim = dim3(n);                                              \
         cfg.blockDim = dim3(Q4Shape<D, NG, NT>::kThreads);                  \
         cfg.dynamicSmemBytes = Q4Shape<D, NG, NT>::kSmem;                   \
-        e = cudaLaunchKernelEx(&cfg, q4_decode_kernel<D, NG, H, NT>, a);    \
+        e = part ? cudaLaunchKernelEx(&cfg, q4_decode_kernel<D, NG, H, NT, true>, a) : cudaLaunchKernelEx(&cfg, q4_decode_kernel<D, NG, H, NT, false>, a); \
     }
 #define PKV_Q4_LAUNCH(D, NG)                                                                     \
     if (g.head_dim == D && g.groups == NG) {                                                     \

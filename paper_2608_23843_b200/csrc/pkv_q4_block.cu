@@ -30,6 +30,8 @@
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 
+#include <algorithm>
+
 #include "pkv_q4_device.cuh"
 #include "pkv_umma.cuh"
 
@@ -82,35 +84,54 @@ __device__ __forceinline__ BlockSeq block_seq(const Q4AttentionArgs &a, int s, i
     q.blocks = (int)(((long long)q.n * q.G + kBRows - 1) / kBRows);
     return q;
 }
-__device__ __forceinline__ int block_units(const BlockSeq &q, int r) {
+__device__ __forceinline__ int block_see(const BlockSeq &q, int r) {
     const int last = min(q.n - 1, ((r + 1) * kBRows - 1) / q.G);
-    const int see = q.all > q.T ? q.T : q.T - q.all + last + 1;          // (more rows than tokens: not worth a rule of its own)
-    return max(1, (see + kQ4Unit - 1) / kQ4Unit);
+    return q.all > q.T ? q.T : q.T - q.all + last + 1;                   // (more rows than tokens: not worth a rule of its own)
+}
+// kSel: what the block's rows see, from the window of its first row on (all rows of a tree visit the same)
+__device__ __forceinline__ Q4Span block_span(const Q4AttentionArgs &a, const BlockSeq &q, int r) {
+    return q4_span(a, a.tree ? q.T : block_see(q, r), q.all > q.T ? 0 : q4_lowest(a, q.T - q.all, (int)((long long)r * kBRows / q.G)));
+}
+template <bool kSel>
+__device__ __forceinline__ int block_units(const Q4AttentionArgs &a, const BlockSeq &q, int r) {
+    return kSel ? block_span(a, q, r).units : max(1, (block_see(q, r) + kQ4Unit - 1) / kQ4Unit);
 }
 // What a block costs a CTA beside its units - queries, results, the first unit's latency - in units.
 constexpr int kBSegCost = 5;
 // Units and fixed costs of all blocks of a sequence, for one head.  (The last block may end before its 256 rows do; the others
 // have a closed form: block i's last row is 256 i + 255, its units floor((T - all + 1 + floor((256 i + 255) / G) + 63) / 64).)
-__device__ long long block_weight(const BlockSeq &q) {
+// kSel: less the units before a block's window and behind the sinks, g(i) = max(0, floor((T - all + 1 - W + floor(256 i / G)) / 64) - su), whose
+// terms are above zero from some block on.
+template <bool kSel>
+__device__ long long block_weight(const Q4AttentionArgs &a, const BlockSeq &q) {
     if (q.blocks == 0) return 0;
     const long long fixed = (long long)q.blocks * kBSegCost;
-    if (q.all > q.T) return fixed + (long long)q.blocks * block_units(q, 0);
-    long long sum = fixed + block_units(q, q.blocks - 1);
+    if (q.all > q.T || (kSel && a.tree)) return fixed + (long long)q.blocks * block_units<kSel>(a, q, 0);
+    long long sum = fixed + block_units<kSel>(a, q, q.blocks - 1);
     if (q.blocks <= 8) {                            // (few: adding them up beats the recursion's divisions)
-        for (int i = 0; i < q.blocks - 1; ++i) sum += block_units(q, i);
+        for (int i = 0; i < q.blocks - 1; ++i) sum += block_units<kSel>(a, q, i);
         return sum;
     }
     const long long A = (long long)q.T - q.all + 1 + kQ4Unit - 1;
-    return sum + floor_sum(q.blocks - 1, (long long)kQ4Unit * q.G, kBRows, kBRows - 1 + A * q.G);
+    sum += floor_sum(q.blocks - 1, (long long)kQ4Unit * q.G, kBRows, kBRows - 1 + A * q.G);
+    if (kSel && a.window) {
+        const long long W = (long long)q.T - q.all + 1 - a.window, su = ((long long)a.sinks + kQ4Unit - 1) / kQ4Unit;
+        const long long need = kQ4Unit * (su + 1) - W;                   // floor(256 i / G) from here on
+        const long long i0 = need <= 0 ? 0 : (need * q.G + kBRows - 1) / kBRows;
+        const long long n = q.blocks - 1 - i0;
+        if (n > 0) sum -= floor_sum(n, (long long)kQ4Unit * q.G, kBRows, W * q.G + kBRows * i0) - n * su;
+    }
+    return sum;
 }
 // The block that holds position `at` of a sequence's weights (blocks in turn, all heads of one before the next), and the
 // position where it begins; a whole warp, 32 blocks at a time.
-__device__ int block_locate(const BlockSeq &q, int H, long long at, long long &begins) {
+template <bool kSel>
+__device__ int block_locate(const Q4AttentionArgs &a, const BlockSeq &q, int H, long long at, long long &begins) {
     const int lane = threadIdx.x & 31;
     long long base = 0;
     for (int r0 = 0;; r0 += 32) {
         const int r = r0 + lane;
-        const int v = r < q.blocks ? block_units(q, r) + kBSegCost : 0;
+        const int v = r < q.blocks ? block_units<kSel>(a, q, r) + kBSegCost : 0;
         int x = v;                                  // (at most 32 * 2^25)
 #pragma unroll
         for (int d = 1; d < 32; d <<= 1) {
@@ -133,7 +154,20 @@ __device__ int block_locate(const BlockSeq &q, int H, long long at, long long &b
 struct BlockCursor {
     int seq, block, head, unit, units;
     BlockSeq q;
+    int su, gap, lo;                                // kSel: see Q4Span
 };
+template <bool kSel>
+__device__ __forceinline__ void block_enter(const Q4AttentionArgs &a, BlockCursor &c) {
+    if (kSel) {
+        const Q4Span r = block_span(a, c.q, c.block);
+        c.units = r.units; c.su = r.su; c.gap = r.gap; c.lo = r.lo;
+    } else {
+        c.units = block_units<false>(a, c.q, c.block);
+    }
+}
+template <bool kSel>
+__device__ __forceinline__ int block_unit_at(const BlockCursor &c, int unit) { return unit + (kSel && unit >= c.su ? c.gap : 0); }
+template <bool kSel>
 __device__ __forceinline__ void block_advance(const Q4AttentionArgs &a, BlockCursor &c, int by) {
     c.unit += by;
     while (c.unit >= c.units) {
@@ -147,7 +181,7 @@ __device__ __forceinline__ void block_advance(const Q4AttentionArgs &a, BlockCur
                 c.q = block_seq(a, c.seq, nullptr);
             } while (c.q.blocks == 0);
         }
-        c.units = block_units(c.q, c.block);
+        block_enter<kSel>(a, c);
     }
 }
 
@@ -204,7 +238,8 @@ __device__ __forceinline__ uint64_t f2_fma3(uint64_t a, uint64_t b, uint64_t c) 
 }
 __device__ __forceinline__ float pow2(int e) { return __uint_as_float((uint32_t)(e + 127) << 23); }      // -126 <= e <= 127
 
-template <int D, int NG, bool H16>
+// kSel: the queries see a part of the positions
+template <int D, int NG, bool H16, bool kSel>
 __global__ void __launch_bounds__(kBThreads, 1) q4_block_kernel(const __grid_constant__ Q4AttentionArgs a) {
     using S = BlockShape<D, NG>;
     constexpr int NW = D / 32, WPG = NW / NG, kWS = S::kWideStages, kCS = S::kCodeStages;
@@ -243,7 +278,7 @@ __global__ void __launch_bounds__(kBThreads, 1) q4_block_kernel(const __grid_con
     int *status = blockIdx.x == 0 ? a.status : nullptr;
     auto weight = [&](int s, int *st) -> long long {
         if (s >= n_seqs) return 0;
-        return block_weight(block_seq(a, s, st)) * H;
+        return block_weight<kSel>(a, block_seq(a, s, st)) * H;
     };
     long long total = 0;
     if (n_seqs == 1) {
@@ -302,8 +337,8 @@ __global__ void __launch_bounds__(kBThreads, 1) q4_block_kernel(const __grid_con
     long long seg_pos;                                         // where the current block begins, on the scale of the weights
     {
         long long b0;
-        seg.block = block_locate(seg.q, H, at0, b0);
-        seg.units = block_units(seg.q, seg.block);
+        seg.block = block_locate<kSel>(a, seg.q, H, at0, b0);
+        block_enter<kSel>(a, seg);
         const int len = seg.units + kBSegCost;
         seg.head = (int)((at0 - b0) / len);
         const int off = (int)(at0 - b0 - (long long)seg.head * len);
@@ -311,7 +346,7 @@ __global__ void __launch_bounds__(kBThreads, 1) q4_block_kernel(const __grid_con
         seg_pos = begin - off;
         if (seg.unit == seg.units) {                           // the share begins behind a block's units
             seg_pos += len;
-            block_advance(a, seg, 0);
+            block_advance<kSel>(a, seg, 0);
         }
     }
     int left = 0;                                              // units of the CTA
@@ -323,7 +358,7 @@ __global__ void __launch_bounds__(kBThreads, 1) q4_block_kernel(const __grid_con
             left += here;
             if (here < w.units - w.unit) break;
             pos += w.units + kBSegCost;
-            block_advance(a, w, w.units - w.unit);
+            block_advance<kSel>(a, w, w.units - w.unit);
         }
     }
     if (left == 0) {
@@ -344,27 +379,29 @@ __global__ void __launch_bounds__(kBThreads, 1) q4_block_kernel(const __grid_con
         // ---------------- copies: 32 units are looked up at a time, a lane each, and issued in turn ----------------
         const int per_page = min(kQ4Unit, geo.page), n_parts = kQ4Unit / per_page, per_tiles = per_page / kQ4Tile;
         BlockCursor nx = seg;
-        if (lane < left) block_advance(a, nx, lane);
+        if (lane < left) block_advance<kSel>(a, nx, lane);
         bool ok = true;
         int st = 0, use = 0, u = 0;
         for (int at = lane; u < left && ok; at += 32) {
             uint32_t bits = 0;
             int pg[4] = {-1, -1, -1, -1};
-            const int t0 = nx.unit * kQ4Unit, head = nx.head, tokens = at < left ? max(0, min(kQ4Unit, nx.q.T - t0)) : 0;
+            const int t0 = block_unit_at<kSel>(nx, nx.unit) * kQ4Unit, head = nx.head, tokens = at < left ? max(0, min(kQ4Unit, nx.q.T - t0)) : 0;
             if (at < left) {
                 const int tiles = (tokens + kQ4Tile - 1) / kQ4Tile;
+                bits = kSel ? q4_needed(a, t0, nx.lo, tiles, n_parts, per_page, per_tiles) : (1u << tiles) - 1u;
+                const uint32_t wanted = bits;
+                auto want = [&](int i) { return kSel ? (wanted >> (i * per_tiles) & 1u) != 0u : i * per_tiles < tiles; };      // (a part from its first tile on)
 #pragma unroll
                 for (int i = 0; i < 4; ++i)
-                    if (i * per_tiles < tiles)
+                    if (want(i))
                         pg[i] = __ldg(a.rows.table + (long long)nx.seq * a.rows.max_pages + ((t0 + i * per_page) >> geo.page_shift));
-                bits = (1u << tiles) - 1u;
 #pragma unroll
                 for (int i = 0; i < 4; ++i)
-                    if (i * per_tiles < tiles && (unsigned)pg[i] >= (unsigned)geo.n_pages) {
+                    if (want(i) && (unsigned)pg[i] >= (unsigned)geo.n_pages) {
                         atomicAdd(a.status + 1, 1);
                         bits &= ~(((1u << per_tiles) - 1u) << (i * per_tiles));
                     }
-                if (at + 32 < left) block_advance(a, nx, 32);
+                if (at + 32 < left) block_advance<kSel>(a, nx, 32);
             }
             for (int i = 0; i < 32 && u < left; ++i, ++u) {
                 const uint32_t bar = smem_u32(&code_full[st]);
@@ -571,7 +608,7 @@ __global__ void __launch_bounds__(kBThreads, 1) q4_block_kernel(const __grid_con
                     }
                 }
                 u += n_units;
-                if (u < left && ok) block_advance(a, c, n_units);
+                if (u < left && ok) block_advance<kSel>(a, c, n_units);
             }
             if (!ok && !*abort_flag) { *abort_flag = 1; atomicAdd(a.status, 1); }
             // nothing of this CTA's may still be running on the tensor cores when tensor memory is given back
@@ -639,14 +676,28 @@ __global__ void __launch_bounds__(kBThreads, 1) q4_block_kernel(const __grid_con
                     mbar_arrive(smem_u32(&q_ready[x]));
                 }
                 const int vis = row_ok ? c.q.T - c.q.all + j + 1 : c.q.T;
+                Q4Seen part{0, c.q.T};                         // kSel: what the row sees; what all of the warp's see
+                int vis_all = 0, lo_all = 0;
+                if (kSel) {
+                    if (row_ok) part = q4_seen(a, c.q.T, c.q.all, c.q.first, j);
+                    vis_all = __reduce_min_sync(0xffffffffu, part.end);
+                    lo_all = __reduce_max_sync(0xffffffffu, part.lo);
+                }
                 for (int i = i0; i < n_units; i += step) {
                     const int ws = (u + i) % kWS;
                     // what the unit is like, while its scores are being computed
                     if (!mbar_wait_warp(smem_u32(&wide_full[ws]), ((u + i) / kWS) & 1, abort_flag)) { ok = false; break; }
                     const UnitInfo &inf = info[ws];
-                    const int t0 = (c.unit + i) * kQ4Unit, lim = min(vis - t0, (int)inf.tokens);
+                    const int t0 = block_unit_at<kSel>(c, c.unit + i) * kQ4Unit, lim = kSel ? 0 : min(vis - t0, (int)inf.tokens);
                     const uint32_t tiles = inf.tiles, odd = *reinterpret_cast<const uint32_t *>(inf.odd);
-                    const bool special = __any_sync(0xffffffffu, lim < kQ4Unit || (odd & 0x07070707u) != 0u) || tiles != (1u << kQ4UnitTiles) - 1u;
+                    const bool part_of = kSel && !(t0 + kQ4Unit <= vis_all && (t0 >= lo_all || t0 + kQ4Unit <= a.sinks));      // (the same for the warp)
+                    const bool special = (kSel ? part_of || (odd & 0x07070707u) != 0u : __any_sync(0xffffffffu, lim < kQ4Unit || (odd & 0x07070707u) != 0u)) ||
+                                         tiles != (1u << kQ4UnitTiles) - 1u;
+                    unsigned long long mask = ~0ull;           // kSel: tokens of the unit that the row sees
+                    if (kSel && special) {
+                        if (part_of && row_ok) mask = q4_unit_mask(a, part, t0, c.q.T, c.q.all, c.q.first + j);
+                        mask &= q4_tile_mask(tiles) & q4_below((int)inf.tokens);
+                    }
                     float fk[kQ4UnitTiles], ev[kQ4UnitTiles];
 #pragma unroll
                     for (int k = 0; k < kQ4UnitTiles; ++k) {
@@ -666,8 +717,10 @@ __global__ void __launch_bounds__(kBThreads, 1) q4_block_kernel(const __grid_con
                             for (int k = 0; k < kQ4UnitTiles; ++k) {
                                 const uint32_t un = odd >> (8 * k);
                                 const int see = tiles >> k & 1 ? lim : 0;
+                                const uint32_t m16 = (uint32_t)(mask >> (k * kQ4Tile)) & 0xffffu;
+                                auto sees = [&](int b) { return kSel ? (m16 >> b & 1u) != 0u : k * kQ4Tile + b < see; };
                                 if (un & 4u) {
-                                    const uint32_t seen = (1u << min(max(see - k * kQ4Tile, 0), kQ4Tile)) - 1u;
+                                    const uint32_t seen = kSel ? m16 : (1u << min(max(see - k * kQ4Tile, 0), kQ4Tile)) - 1u;
 #pragma unroll 1
                                     for (int b = 0; b < NG; ++b) bad |= (inf.v_nan[k][b] & seen) ? 1u << b : 0u;
                                 }
@@ -688,10 +741,10 @@ __global__ void __launch_bounds__(kBThreads, 1) q4_block_kernel(const __grid_con
 #pragma unroll
                                     for (int b = 0; b < kQ4Tile; ++b) {
                                         x[b] *= fx;
-                                        if (k * kQ4Tile + b < see) m = fmaxf(m, x[b]);
+                                        if (sees(b)) m = fmaxf(m, x[b]);
                                     }
 #pragma unroll
-                                    for (int b = 0; b < kQ4Tile; ++b) sum += k * kQ4Tile + b < see ? ex2(x[b] - m) : 0.f;
+                                    for (int b = 0; b < kQ4Tile; ++b) sum += sees(b) ? ex2(x[b] - m) : 0.f;
                                     apart = fmaf(apart, ex2(apart_m - m), sum);
                                     apart_m = m;
 #pragma unroll
@@ -710,7 +763,7 @@ __global__ void __launch_bounds__(kBThreads, 1) q4_block_kernel(const __grid_con
                         }
 #pragma unroll
                         for (int k = 0; k < kQ4Unit; ++k)
-                            if (!(k < lim && (tiles >> (k / kQ4Tile) & 1))) sv[k] = -INFINITY;
+                            if (!(kSel ? (mask >> k & 1ull) != 0ull : k < lim && (tiles >> (k / kQ4Tile) & 1))) sv[k] = -INFINITY;
                     }
                     // x = s * f 2^Ek + Ev, against a reference of the row's own
                     float top = -INFINITY;
@@ -731,6 +784,8 @@ __global__ void __launch_bounds__(kBThreads, 1) q4_block_kernel(const __grid_con
                             for (int k = 0; k < kQ4UnitTiles; ++k) {
                                 const uint32_t un = odd >> (8 * k);
                                 const int see = (tiles >> k & 1 ? lim : 0) - k * kQ4Tile;
+                                const uint32_t m16 = (uint32_t)(mask >> (k * kQ4Tile));
+                                auto sees = [&](int b) { return kSel ? (m16 >> b & 1u) != 0u : b < see; };
                                 const float fx = un & 2u ? 1.f : fmaxf(f * inf.ek[k], 1.2e-38f);
                                 float x[kQ4Tile];
                                 tmem_ld16(t_s + k * kQ4Tile, reinterpret_cast<uint32_t *>(x));
@@ -738,10 +793,10 @@ __global__ void __launch_bounds__(kBThreads, 1) q4_block_kernel(const __grid_con
 #pragma unroll
                                 for (int b = 0; b < kQ4Tile; b += 4) {
                                     const float4 t = (un & 10u) == 8u ? *reinterpret_cast<const float4 *>(inf.tv + k * kQ4Tile + b) : make_float4(inf.ev[k], inf.ev[k], inf.ev[k], inf.ev[k]);
-                                    if (b < see) own = fmaxf(own, fmaf(x[b], fx, t.x));
-                                    if (b + 1 < see) own = fmaxf(own, fmaf(x[b + 1], fx, t.y));
-                                    if (b + 2 < see) own = fmaxf(own, fmaf(x[b + 2], fx, t.z));
-                                    if (b + 3 < see) own = fmaxf(own, fmaf(x[b + 3], fx, t.w));
+                                    if (sees(b)) own = fmaxf(own, fmaf(x[b], fx, t.x));
+                                    if (sees(b + 1)) own = fmaxf(own, fmaf(x[b + 1], fx, t.y));
+                                    if (sees(b + 2)) own = fmaxf(own, fmaf(x[b + 2], fx, t.z));
+                                    if (sees(b + 3)) own = fmaxf(own, fmaf(x[b + 3], fx, t.w));
                                 }
                             }
                         }
@@ -896,7 +951,7 @@ __global__ void __launch_bounds__(kBThreads, 1) q4_block_kernel(const __grid_con
                 parts[blockIdx.x] = p;
             }
             seg_pos += c.units + kBSegCost;
-            if (u < left) block_advance(a, c, n_units);
+            if (u < left) block_advance<kSel>(a, c, n_units);
         }
         if (!ok && lane == 0 && !*abort_flag) { *abort_flag = 1; atomicAdd(a.status, 1); }
         if (!ok && tid == 0 && gridDim.x > 1) parts[blockIdx.x].seq = -1;
@@ -913,22 +968,25 @@ __global__ void __launch_bounds__(kBThreads, 1) q4_block_kernel(const __grid_con
 
 cudaError_t q4_block_setup() {
     cudaError_t e;
-#define PKV_Q4_SETUP1(D, NG, H16) \
-    if ((e = cudaFuncSetAttribute(q4_block_kernel<D, NG, H16>, cudaFuncAttributeMaxDynamicSharedMemorySize, BlockShape<D, NG>::kSmem)) != cudaSuccess) return e;
+#define PKV_Q4_SETUP2(D, NG, H16, SEL) \
+    if ((e = cudaFuncSetAttribute(q4_block_kernel<D, NG, H16, SEL>, cudaFuncAttributeMaxDynamicSharedMemorySize, BlockShape<D, NG>::kSmem)) != cudaSuccess) return e;
+#define PKV_Q4_SETUP1(D, NG, H16) PKV_Q4_SETUP2(D, NG, H16, false) PKV_Q4_SETUP2(D, NG, H16, true)
 #define PKV_Q4_SETUP(D, NG) PKV_Q4_SETUP1(D, NG, false) PKV_Q4_SETUP1(D, NG, true)
     PKV_Q4_SHAPES(PKV_Q4_SETUP)
     return cudaSuccess;
 }
 
 // CTAs: one per SM, four units each at least, as far as the host can tell.
-int q4_block_grid(const Q4Geometry &g, int n_seqs, int max_q_len, int max_len) {
-    const double blocks = (double)(((long long)max_q_len * g.group + kBRows - 1) / kBRows), units = (max_len + kQ4Unit - 1) / kQ4Unit;
+int q4_block_grid(const Q4Geometry &g, int n_seqs, int max_q_len, int max_len, const Q4Select &sel) {
+    const double blocks = (double)(((long long)max_q_len * g.group + kBRows - 1) / kBRows);
+    double units = (max_len + kQ4Unit - 1) / kQ4Unit;
+    if (sel.window > 0 && !sel.tree) units = std::min(units, ((double)sel.window + sel.sinks + kBRows / g.group) / kQ4Unit + 2);      // (a block's window)
     const double all = (double)n_seqs * g.n_kv_heads * blocks * (units + kBSegCost) / (4 + kBSegCost);
     return all >= g.n_sms ? g.n_sms : all < 1 ? 1 : (int)all;
 }
 
-long long q4_block_workspace(const Q4Geometry &g, int n_seqs, int max_q_len, int max_len) {
-    const int n = q4_block_grid(g, n_seqs, max_q_len, max_len);
+long long q4_block_workspace(const Q4Geometry &g, int n_seqs, int max_q_len, int max_len, const Q4Select &sel) {
+    const int n = q4_block_grid(g, n_seqs, max_q_len, max_len, sel);
     return n <= 1 ? 0 : q4_parts_bytes(n) + 2LL * n * q4_state_floats(kBRows, g.head_dim) * 4;
 }
 
@@ -946,7 +1004,8 @@ cudaError_t launch_q4_block(const Q4AttentionArgs &a, int n, cudaStream_t st) {
 #define PKV_Q4_LAUNCH1(D, NG, H16)                                                                       \
     if (g.head_dim == D && g.groups == NG && (g.fp16 != 0) == H16) {                                     \
         cfg.dynamicSmemBytes = BlockShape<D, NG>::kSmem;                                                 \
-        return cudaLaunchKernelEx(&cfg, q4_block_kernel<D, NG, H16>, a);                                 \
+        return a.window > 0 || a.tree ? cudaLaunchKernelEx(&cfg, q4_block_kernel<D, NG, H16, true>, a)   \
+                                      : cudaLaunchKernelEx(&cfg, q4_block_kernel<D, NG, H16, false>, a); \
     }
 #define PKV_Q4_LAUNCH(D, NG) PKV_Q4_LAUNCH1(D, NG, false) PKV_Q4_LAUNCH1(D, NG, true)
     PKV_Q4_SHAPES(PKV_Q4_LAUNCH)

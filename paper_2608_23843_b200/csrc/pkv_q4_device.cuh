@@ -34,6 +34,65 @@ __device__ __forceinline__ int q4_new_rows(const Q4AttentionArgs &a, int s, int 
     return max(0, min(all, a.max_q_len));
 }
 
+// ---- Queries that see a part of the positions (Q4AttentionArgs: window, sinks, tree) -----------------------------------
+// A run of units (64 tokens) that holds what any of some query rows sees: the first `su` of a sequence, then those behind a gap.
+struct Q4Span { int units, su, gap, lo; };             // lo: the lowest position behind the sinks that one of the rows sees
+// see: the positions below it are visited; low: the rows' lowest position in the window (0 or less: no gap)
+__device__ __forceinline__ Q4Span q4_span(const Q4AttentionArgs &a, int see, int low) {
+    const int all = (see + kQ4Unit - 1) / kQ4Unit;
+    Q4Span r;
+    r.lo = max(0, low);
+    r.su = min((int)(((unsigned)a.sinks + kQ4Unit - 1) / kQ4Unit), all);
+    r.gap = max(0, r.lo / kQ4Unit - r.su);
+    r.units = max(1, all - r.gap);
+    return r;
+}
+// The lowest position in the window of new row j of a sequence with a context of C tokens, for a row of a tree when no new row counts.
+__device__ __forceinline__ int q4_lowest(const Q4AttentionArgs &a, int C, int j) {
+    return a.window ? C + (a.tree ? 0 : j + 1) - a.window : 0;
+}
+// Tiles of the unit at t0 that have to be there (of the first `tiles`): those of parts - a page's, or the whole unit - that hold a position
+// below the sinks or from lo on.  Pages of other parts may be anyone's.
+__device__ __forceinline__ uint32_t q4_needed(const Q4AttentionArgs &a, int t0, int lo, int tiles, int n_parts, int per_page, int per_tiles) {
+    uint32_t bits = 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+        if (i < n_parts && (t0 + i * per_page < a.sinks || t0 + (i + 1) * per_page > lo)) bits |= ((1u << per_tiles) - 1u) << (i * per_tiles);
+    return bits & ((1u << tiles) - 1u);
+}
+// What a query row sees: positions from lo (or below the sinks) up to `end`, and new rows by the bits of its mask.
+struct Q4Seen { int lo, end; };
+__device__ __forceinline__ Q4Seen q4_seen(const Q4AttentionArgs &a, int T, int all, int first, int j) {
+    const int C = T - all;
+    if (!a.tree) return Q4Seen{a.window ? max(0, C + j + 1 - a.window) : 0, C + j + 1};
+    int own = 0;
+    if (a.window) {                                    // new rows that it sees, of those the sequence has
+        const unsigned long long *w = a.tree + (long long)(first + j) * a.tree_words;
+        for (int i = 0; i < min(a.tree_words, (all + 63) >> 6); ++i) own += __popcll(__ldg(w + i) & (all - 64 * i >= 64 ? ~0ull : (1ull << (all - 64 * i)) - 1ull));
+    }
+    return Q4Seen{a.window ? max(0, C + own - a.window) : 0, C};
+}
+__device__ __forceinline__ unsigned long long q4_below(int x) { return x <= 0 ? 0ull : x >= 64 ? ~0ull : (1ull << x) - 1ull; }
+// ... as bits of the unit at t0
+__device__ __forceinline__ unsigned long long q4_unit_mask(const Q4AttentionArgs &a, const Q4Seen &v, int t0, int T, int all, long long row) {
+    unsigned long long m = q4_below(v.end - t0) & (~q4_below(v.lo - t0) | q4_below(a.sinks - t0));
+    const int at = t0 - (T - all);                     // the unit's first token as a new row
+    if (a.tree && at > -64) {
+        const unsigned long long *w = a.tree + row * a.tree_words;
+        const int i = at >> 6, sh = at & 63;
+        unsigned long long x = 0;
+        if (i >= 0 && i < a.tree_words) x = __ldg(w + i) >> sh;
+        if (sh && i + 1 < a.tree_words) x |= __ldg(w + i + 1) << (64 - sh);      // (i + 1 >= 0)
+        m |= x & q4_below(T - t0);
+    }
+    return m;
+}
+// the tiles that are there, 16 bits each
+__device__ __forceinline__ unsigned long long q4_tile_mask(uint32_t tiles) {
+    const uint32_t lo = (tiles & 1u ? 0xffffu : 0u) | (tiles & 2u ? 0xffff0000u : 0u), hi = (tiles & 4u ? 0xffffu : 0u) | (tiles & 8u ? 0xffff0000u : 0u);
+    return (unsigned long long)hi << 32 | lo;
+}
+
 __device__ __forceinline__ float ex2(float x) {
     float y;
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
