@@ -67,6 +67,7 @@ struct Q4AttentionArgs {
     int max_q_len;                     // no sequence has more rows than this
     int max_len;                       // hint: lengths are expected up to this
     int whole;                         // set by the launcher: no segment is cut
+    int cluster;                       // ... CTAs that share a segment (1, 2, 4 or 8)
     int chained;                       // ... the kernel that follows the call's last may be set up early (see q4_chained)
     int join;                          // ... the call's second kernel follows
     unsigned char *workspace;
@@ -130,7 +131,6 @@ cudaError_t q4_attention_setup();      // raises dynamic shared-memory limits, o
 constexpr int kQ4BlockRows = 256;
 cudaError_t q4_block_setup();
 int q4_block_grid(const Q4Geometry &g, int n_seqs, int max_q_len, int max_len, const Q4Select &sel);
-long long q4_block_workspace(const Q4Geometry &g, int n_seqs, int max_q_len, int max_len, const Q4Select &sel);
 cudaError_t launch_q4_block(const Q4AttentionArgs &a, int n, cudaStream_t st);
 long long q4_attention_workspace(const Q4Geometry &g, int n_seqs, int max_q_len, int max_len, const Q4Select &sel);
 

@@ -26,6 +26,10 @@
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 
+#include <algorithm>
+#include <cmath>
+#include <cstdio>
+#include <cstdlib>
 #include <type_traits>
 
 #include "pkv_q4_device.cuh"
@@ -42,12 +46,13 @@ __host__ __device__ constexpr int q4_seg_cost(int nt) { return nt == 1 ? 6 : 12;
 // registers allow - of one column of query rows, in 128 registers a thread, two CTAs of eight per SM (one CTA of sixteen, which
 // idles while it joins its warps' states: 87 us instead of 69 for 8 x 32K when this was measured); of two columns, in 168 registers, one CTA of
 // twelve (two of six, with one consumer fewer and twice the segments: 115 us instead of 103).
-__host__ __device__ constexpr int q4_warps(int nt) { return nt == 1 ? 8 : 12; }
-__host__ __device__ constexpr int q4_ctas_per_sm(int nt) { return nt == 1 ? 2 : 1; }
+// Where queries see a part of the positions a segment is often short: four CTAs of four warps (`small`), and clusters of them to a segment.
+__host__ __device__ constexpr int q4_warps(int nt, bool small = false) { return small ? 4 : nt == 1 ? 8 : 12; }
+__host__ __device__ constexpr int q4_ctas_per_sm(int nt, bool small = false) { return small ? 4 : nt == 1 ? 2 : 1; }
 
-template <int D, int NG, int NT>
+template <int D, int NG, int NT, bool kSmall = false>
 struct Q4Shape {
-    static constexpr int kWarps = q4_warps(NT), kCons = kWarps - 1, kThreads = 32 * kWarps, kPerSM = q4_ctas_per_sm(NT);
+    static constexpr int kWarps = q4_warps(NT, kSmall), kCons = kWarps - 1, kThreads = 32 * kWarps, kPerSM = q4_ctas_per_sm(NT, kSmall);
     // tiles per softmax step: with one column a whole unit, which leaves the scheduler most to choose from (8 x 32K: one tile 72 us,
     // two 69, four 66.7); with two columns more than one would spill (16 rows, two tiles: 105 us instead of 103)
     static constexpr int kStep = NT == 1 ? 4 : 1;
@@ -57,7 +62,8 @@ struct Q4Shape {
     static constexpr int kFlush = 8 * kRowFloats * 4;                               // a warp's o (eight rows at a time) at a segment's end: over the stage it has just read
     static constexpr int kStage = ((kUnitBytes > kFlush ? kUnitBytes : kFlush) + 127) / 128 * 128;
     // the other arrays in shared memory: per warp the states' (m, l), references and gains, per stage two barriers and a word; 1 KB is the system's
-    static constexpr int kOther = 1024 + kCons * (64 + NT * (128 + 16 * NG)) + 32 / kPerSM * 20 + 256;
+    // (kSmall: and the cluster's share of the segment's state)
+    static constexpr int kOther = 1024 + kCons * (64 + NT * (128 + 16 * NG)) + 32 / kPerSM * 20 + 256 + (kSmall ? kFlush + kCons * 64 + 192 : 0);
     static constexpr int kFit = (227 * 1024 / kPerSM - kOther - kQueries) / kStage, kStages = kFit < 32 / kPerSM ? kFit : 32 / kPerSM;
     static constexpr int kSmem = kStages * kStage;
     static_assert(kStages > kCons && kPerSM * (kSmem + kQueries + kOther) <= 227 * 1024, "a stage per warp and some in flight");
@@ -231,10 +237,31 @@ __device__ __forceinline__ void q4_advance(const Q4AttentionArgs &a, int rows_pe
     }
 }
 
-// kSel: the queries see a part of the positions
-template <int D, int NG, bool H16, int NT, bool kSel>
-__global__ void __launch_bounds__(Q4Shape<D, NG, NT>::kThreads, q4_ctas_per_sm(NT)) q4_decode_kernel(const __grid_constant__ Q4AttentionArgs a) {
-    using S = Q4Shape<D, NG, NT>;
+__device__ __forceinline__ void cluster_sync() {
+    asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+__device__ __forceinline__ uint32_t cluster_at(uint32_t at, int rank) {      // the same place in another CTA's shared memory
+    uint32_t r;
+    asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(at), "r"(rank));
+    return r;
+}
+__device__ __forceinline__ float4 cluster_ld4(uint32_t at) {
+    float4 v;
+    asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(at) : "memory");
+    return v;
+}
+__device__ __forceinline__ float2 cluster_ld2(uint32_t at) {
+    float2 v;
+    asm volatile("ld.shared::cluster.v2.f32 {%0, %1}, [%2];" : "=f"(v.x), "=f"(v.y) : "r"(at) : "memory");
+    return v;
+}
+
+// kSel: the queries see a part of the positions.  kSmall: whole segments only, each by one CTA or by a cluster whose CTAs take an equal run
+// of its units each and join their states through shared memory, some of the rows each.
+template <int D, int NG, bool H16, int NT, bool kSel, bool kSmall = false>
+__global__ void __launch_bounds__(Q4Shape<D, NG, NT, kSmall>::kThreads, q4_ctas_per_sm(NT, kSmall)) q4_decode_kernel(const __grid_constant__ Q4AttentionArgs a) {
+    static_assert(!kSmall || (kSel && NT == 1), "see above");
+    using S = Q4Shape<D, NG, NT, kSmall>;
     constexpr int NW = D / 32, WPG = NW / NG, R = 8 * NT;      // 32-channel words per row, words per scale, query rows
     constexpr int TS = S::kStep, kSt = S::kStages, kQ4Warps = S::kWarps, kCons = S::kCons, kQ4Threads = S::kThreads, kSegCost = q4_seg_cost(NT);
     const Q4Geometry &geo = a.geo;
@@ -246,7 +273,9 @@ __global__ void __launch_bounds__(Q4Shape<D, NG, NT>::kThreads, q4_ctas_per_sm(N
     __shared__ uint32_t gains[kCons][NT][NG][4];               // bf16, two columns to a word
     __shared__ int vis[kSel ? 1 : 8 * NT];                     // tokens a column's query sees
     __shared__ Q4Seen part[kSel ? 8 * NT : 1];                 // kSel: which ones
-    __shared__ uint16_t seen[kSel ? kCons : 1][8 * NT][kQ4UnitTiles];      // ... in a warp's unit, a bit each
+    __shared__ __align__(8) uint16_t seen[kSel ? kCons : 1][8 * NT][kQ4UnitTiles];      // ... in a warp's unit, a bit each
+    __shared__ __align__(16) float share_o[kSmall ? 8 * S::kRowFloats : 1];      // kSmall: the state of this CTA's part of a segment
+    __shared__ float2 share_ml[kSmall ? 8 : 1];
     __shared__ uint4 queries[NT][NW][32];                      // of the segment, as the lanes of a warp take them
     __shared__ long long sums[kQ4Warps], found_at;
     __shared__ int found_seq, offs[kCons], gave_up;
@@ -259,6 +288,11 @@ __global__ void __launch_bounds__(Q4Shape<D, NG, NT>::kThreads, q4_ctas_per_sm(N
     asm volatile("griddepcontrol.wait;" ::: "memory");
     if (a.chained || a.join) asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
 
+    // kSmall: clusters take the place of CTAs in what follows
+    const int cluster = kSmall ? a.cluster : 1, rank = kSmall ? (int)blockIdx.x % cluster : 0;
+    const int block = kSmall ? (int)blockIdx.x / cluster : (int)blockIdx.x, grid = kSmall ? (int)gridDim.x / cluster : (int)gridDim.x;
+    const bool a_whole = kSmall || a.whole;
+
     // ---- this CTA's share of the batch's units (a.whole: of its segments) ----
     const int H = geo.n_kv_heads, n_seqs = a.rows.n_seqs;
     int *status = blockIdx.x == 0 ? a.status : nullptr;
@@ -266,7 +300,7 @@ __global__ void __launch_bounds__(Q4Shape<D, NG, NT>::kThreads, q4_ctas_per_sm(N
         if (s >= n_seqs) return 0;
         int first, all;
         const int n = q4_new_rows(a, s, first, all, st), T = q4_length(a.rows, geo, s, st);
-        return (long long)((n * geo.group + R - 1) / R) * H * (a.whole ? 1 : q4_seq_units<kSel>(a, T, all) + kSegCost);
+        return (long long)((n * geo.group + R - 1) / R) * H * (a_whole ? 1 : q4_seq_units<kSel>(a, T, all) + kSegCost);
     };
     long long total = 0;
     if (n_seqs == 1) {
@@ -282,18 +316,18 @@ __global__ void __launch_bounds__(Q4Shape<D, NG, NT>::kThreads, q4_ctas_per_sm(N
         for (int w = 0; w < kQ4Warps; ++w) total += sums[w];
     }
     // (no more CTAs than there are units for a warp of each; the launch could only estimate that)
-    const int n_ctas = (int)min((long long)gridDim.x, max(1LL, a.whole ? total : total / (kCons + kSegCost)));
+    const int n_ctas = (int)min((long long)grid, max(1LL, a_whole ? total : total / (kCons + kSegCost)));
     // (b * total / n without a 64-bit division where the total has 31 bits)
     auto share = [&](long long b) -> long long {
         if (total >> 31) return total * b / n_ctas;
         const unsigned q = (unsigned)total / (unsigned)n_ctas, r = (unsigned)total % (unsigned)n_ctas;
         return (long long)q * b + r * (unsigned)b / (unsigned)n_ctas;
     };
-    const long long begin = share(blockIdx.x), end = share(blockIdx.x + 1LL);
+    const long long begin = share(block), end = share(block + 1LL);
     Q4Part *parts = reinterpret_cast<Q4Part *>(a.workspace);
     float *states = reinterpret_cast<float *>(a.workspace + q4_parts_bytes(gridDim.x));
-    const bool joined = !a.whole && gridDim.x > 1;             // segments may span CTAs
-    if (blockIdx.x >= n_ctas || begin >= end) {
+    const bool joined = !a_whole && gridDim.x > 1;             // segments may span CTAs
+    if (block >= n_ctas || begin >= end) {
         if (tid == 0 && joined) parts[blockIdx.x].seq = -1;
         return;
     }
@@ -333,7 +367,7 @@ __global__ void __launch_bounds__(Q4Shape<D, NG, NT>::kThreads, q4_ctas_per_sm(N
     q4_load_seq<kSel>(a, R, seg);
     int left_cta;                                              // units of the CTA
     long long seg_pos = 0;                                     // where the current segment begins, on the scale of the weights
-    if (a.whole) {
+    if (a_whole) {
         seg.unit = 0;
         seg.head = (int)(at0 % H);
         seg.tile = (int)(at0 / H);
@@ -342,6 +376,10 @@ __global__ void __launch_bounds__(Q4Shape<D, NG, NT>::kThreads, q4_ctas_per_sm(N
         for (int k = 1; k < (int)(end - begin); ++k) {
             q4_advance<kSel>(a, R, w, w.units);
             left_cta += w.units;
+        }
+        if (kSmall && cluster > 1) {                           // (its one segment: the launch gives every segment a cluster)
+            seg.unit = (int)((long long)seg.units * rank / cluster);
+            left_cta = (int)((long long)seg.units * (rank + 1) / cluster) - seg.unit;
         }
     } else {
         const int len = seg.units + kSegCost;
@@ -424,6 +462,11 @@ __global__ void __launch_bounds__(Q4Shape<D, NG, NT>::kThreads, q4_ctas_per_sm(N
         if (!ok && lane == 0 && !*abort_flag) { *abort_flag = 1; atomicAdd(a.status, 1); }
         // copies in flight must land before the CTA retires: wait (bounded) for the stages armed last
         for (int back = 1; back <= min(u, kSt); ++back) (void)mbar_wait(smem_u32(&full[(u - back) % kSt]), ((u - back) / kSt) & 1);
+        if (kSmall && cluster > 1) {
+            __syncwarp();
+            cluster_sync();
+            cluster_sync();
+        }
         return;
     }
 
@@ -433,7 +476,7 @@ __global__ void __launch_bounds__(Q4Shape<D, NG, NT>::kThreads, q4_ctas_per_sm(N
     int seg_lo = 0;                                            // the segment's first unit, within the CTA's units
     int st = warp, phase = 0;                                  // its stage and the parity of that use
     const float scale = geo.scale_log2e;
-    while (seg_lo < left_cta) {
+    do {                                                       // (there is one, if without units: a cluster's CTA)
         const int seg_hi = min(left_cta, seg_lo + seg.units - seg.unit);
         // ---- the segment's queries ----
         int first, all;
@@ -561,15 +604,20 @@ __global__ void __launch_bounds__(Q4Shape<D, NG, NT>::kThreads, q4_ctas_per_sm(N
             uint32_t tiles = 0;
             if ((mbar_wait_warp(smem_u32(&full[st]), phase, abort_flag))) tiles = tiles_here[st];
             else if (lane == 0 && !*abort_flag) { *abort_flag = 1; atomicAdd(a.status, 1); }      // (the unit counts as not there)
+            uint32_t need = (1u << kQ4UnitTiles) - 1u;         // kSel: tiles that some row sees a token of
             const bool whole = tiles == (1u << kQ4UnitTiles) - 1u && t_unit + kQ4Unit <= vis_all && (!kSel || t_unit >= lo_all || t_unit + kQ4Unit <= a.sinks);
             if (kSel && !whole) {                              // what each row sees of the unit, a lane each
+                uint32_t lo = 0, hi = 0;                       // (rows that are not there see nothing)
                 if (lane < 8 * NT) {
-                    const int row = seg.tile * R + lane, j = row / G;
-                    unsigned long long m = q4_below(seg.T - t_unit);
-                    if (j < n) m = q4_unit_mask(a, part[lane], t_unit, seg.T, all, first + j);
-                    m &= q4_tile_mask(tiles);
-                    *reinterpret_cast<uint2 *>(&seen[warp][lane][0]) = make_uint2((uint32_t)m, (uint32_t)(m >> 32));
+                    const int j = (seg.tile * R + lane) / G;
+                    const unsigned long long m = j < n ? q4_unit_mask(a, part[lane], t_unit, seg.T, all, first + j) & q4_tile_mask(tiles) : 0ull;
+                    lo = (uint32_t)m;
+                    hi = (uint32_t)(m >> 32);
+                    *reinterpret_cast<uint2 *>(&seen[warp][lane][0]) = make_uint2(lo, hi);
                 }
+                lo = __reduce_or_sync(0xffffffffu, lo);
+                hi = __reduce_or_sync(0xffffffffu, hi);
+                need = (lo & 0xffffu ? 1u : 0u) | (lo >> 16 ? 2u : 0u) | (hi & 0xffffu ? 4u : 0u) | (hi >> 16 ? 8u : 0u);
                 __syncwarp();
             }
             // (not kept in registers)
@@ -625,6 +673,13 @@ __global__ void __launch_bounds__(Q4Shape<D, NG, NT>::kThreads, q4_ctas_per_sm(N
 #pragma unroll
                 for (int tl = 0; tl < TS; ++tl) {
                     const unsigned char *tp = tp0 + tl * S::kTile;
+                    if (kCareful && kSel && !(need >> (step * TS + tl) & 1u)) {
+#pragma unroll
+                        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                            for (int i = 0; i < 4; ++i) sc[tl][nt][i] = -INFINITY;
+                        continue;
+                    }
                     uint32_t k0[NW], k1[NW], s0[(NG + 1) / 2], s1[(NG + 1) / 2];
                     if (NW == 4) {
                         const uint4 x = *reinterpret_cast<const uint4 *>(tp + q4_k_chunk(D, g, c)), y = *reinterpret_cast<const uint4 *>(tp + q4_k_chunk(D, g + 8, c));
@@ -788,6 +843,7 @@ __global__ void __launch_bounds__(Q4Shape<D, NG, NT>::kThreads, q4_ctas_per_sm(N
 #pragma unroll
                 for (int tl = 0; tl < TS; ++tl) {
                     const unsigned char *tp = tp0 + tl * S::kTile, *vp = tp + q4_v_base(D);
+                    if (kCareful && kSel && !(need >> (step * TS + tl) & 1u)) continue;
                     uint32_t s0[(NG + 1) / 2], s1[(NG + 1) / 2];
                     q4_scales<NG>(tp + q4_vs_base(D, NG), g, s0, s1);
                     // words of tokens 2c, 2c + 1, 2c + 8, 2c + 9: chunk g
@@ -902,6 +958,24 @@ __global__ void __launch_bounds__(Q4Shape<D, NG, NT>::kThreads, q4_ctas_per_sm(N
             }
             consumers_sync();
             float *part = states + (2LL * blockIdx.x + slot) * q4_state_floats(R, D);
+            // row r's state (M, L, acc at channels ch ..) to where it goes
+            auto write = [&](int r, int ch, float M, float L, const float4 &acc) {
+                const int row = seg.tile * R + r, j = row / G;
+                if (j >= n) return;
+                const int h = seg.head * G + row - j * G;
+                if (a.state) {
+                    float *dst = a.state + ((long long)(first + j) * geo.n_q_heads + h) * (D + 2);
+                    *reinterpret_cast<float2 *>(dst + ch) = make_float2(acc.x, acc.y);
+                    *reinterpret_cast<float2 *>(dst + ch + 2) = make_float2(acc.z, acc.w);
+                    if (ch == 0) *reinterpret_cast<float2 *>(dst + D) = make_float2(M, L);
+                } else {
+                    const float inv = L != 0.f ? 1.f / L : 0.f;
+                    const uint2 v = H16 ? make_uint2(pack_f16(acc.x * inv, acc.y * inv), pack_f16(acc.z * inv, acc.w * inv))
+                                        : make_uint2(pack_bf16(acc.x * inv, acc.y * inv), pack_bf16(acc.z * inv, acc.w * inv));
+                    *reinterpret_cast<uint2 *>(reinterpret_cast<unsigned short *>(a.out) + (long long)(first + j) * a.out_row +
+                                               (long long)h * a.out_head + ch) = v;
+                }
+            };
             for (int i = tid; i < 8 * (D / 4); i += 32 * kCons) {
                 const int r8 = i / (D / 4), r = nt * 8 + r8, ch = i % (D / 4) * 4;
                 float M = kNegInf;
@@ -918,26 +992,42 @@ __global__ void __launch_bounds__(Q4Shape<D, NG, NT>::kThreads, q4_ctas_per_sm(N
                     L += f * ml[w][r8].y;
                     acc.x += f * x.x; acc.y += f * x.y; acc.z += f * x.z; acc.w += f * x.w;
                 }
+                if (kSmall && cluster > 1) {
+                    *reinterpret_cast<float4 *>(share_o + r * S::kRowFloats + ch) = acc;
+                    if (ch == 0) share_ml[r] = make_float2(M, L);
+                    continue;
+                }
                 if (!complete) {
                     *reinterpret_cast<float4 *>(part + r * D + ch) = acc;
                     if (ch == 0) { part[R * D + r] = M; part[R * D + R + r] = L; }
                     continue;
                 }
-                const int row = seg.tile * R + r, j = row / G;
-                if (j >= n) continue;
-                const int h = seg.head * G + row - j * G;
-                if (a.state) {
-                    float *dst = a.state + ((long long)(first + j) * geo.n_q_heads + h) * (D + 2);
-                    *reinterpret_cast<float2 *>(dst + ch) = make_float2(acc.x, acc.y);
-                    *reinterpret_cast<float2 *>(dst + ch + 2) = make_float2(acc.z, acc.w);
-                    if (ch == 0) *reinterpret_cast<float2 *>(dst + D) = make_float2(M, L);
-                } else {
-                    const float inv = L != 0.f ? 1.f / L : 0.f;
-                    const uint2 v = H16 ? make_uint2(pack_f16(acc.x * inv, acc.y * inv), pack_f16(acc.z * inv, acc.w * inv))
-                                        : make_uint2(pack_bf16(acc.x * inv, acc.y * inv), pack_bf16(acc.z * inv, acc.w * inv));
-                    *reinterpret_cast<uint2 *>(reinterpret_cast<unsigned short *>(a.out) + (long long)(first + j) * a.out_row +
-                                               (long long)h * a.out_head + ch) = v;
+                write(r, ch, M, L, acc);
+            }
+            if (kSmall && cluster > 1) {                       // rows rank, rank + cluster, ... of all parts, in order
+                cluster_sync();
+                for (int i = tid; i < 8 / cluster * (D / 4); i += 32 * kCons) {
+                    const int r = i / (D / 4) * cluster + rank, ch = i % (D / 4) * 4;
+                    float2 s[8];
+                    float M = kNegInf, L = 0.f;
+                    float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+                    for (int k = 0; k < 8; ++k) {
+                        if (k >= cluster) break;
+                        s[k] = cluster_ld2(cluster_at(smem_u32(&share_ml[r]), k));
+                        M = fmaxf(M, s[k].x);
+                    }
+#pragma unroll
+                    for (int k = 0; k < 8; ++k) {
+                        if (k >= cluster) break;
+                        const float f = ex2(s[k].x - M);
+                        const float4 x = cluster_ld4(cluster_at(smem_u32(share_o + r * S::kRowFloats + ch), k));
+                        L += f * s[k].y;
+                        acc.x += f * x.x; acc.y += f * x.y; acc.z += f * x.z; acc.w += f * x.w;
+                    }
+                    write(r, ch, M, L, acc);
                 }
+                cluster_sync();                                // (no CTA leaves while its state is read)
             }
             if (nt == NT - 1) asm volatile("fence.proxy.async.shared::cta;" ::: "memory");      // the stages go back to the copies
             consumers_sync();
@@ -957,7 +1047,7 @@ __global__ void __launch_bounds__(Q4Shape<D, NG, NT>::kThreads, q4_ctas_per_sm(N
             seg_pos += seg.units + kSegCost;
             q4_advance<kSel>(a, R, seg, seg.units - seg.unit);
         }
-    }
+    } while (seg_lo < left_cta);
 }
 
 // Joins the states of the segments (tiles of R rows) that span CTAs, in token order: blocks (b, y) take the rows of the
@@ -1092,10 +1182,10 @@ bool q4_by_blocks(const Q4Geometry &g, int n_seqs, int max_q_len, int max_len) {
 }
 
 // CTAs of a launch: enough units for every warp of each, as far as the host can tell.
-int q4_grid(const Q4Geometry &g, int n_seqs, int max_q_len, int max_len) {
+int q4_grid(const Q4Geometry &g, int n_seqs, int max_q_len, int max_len, bool whole) {
     const int nt = q4_rows_per_tile(g, max_q_len) / 8, most = max(1, g.n_ctas * q4_ctas_per_sm(nt) / 2);
     const double segs = q4_segments(g, n_seqs, max_q_len), units = (max_len + kQ4Unit - 1) / kQ4Unit;
-    const double all = q4_whole(max_len) ? segs : segs * units / (q4_warps(nt) - 1);
+    const double all = whole ? segs : segs * units / (q4_warps(nt) - 1);
     return all >= most ? most : all < 1 ? 1 : (int)all;
 }
 
@@ -1109,7 +1199,9 @@ cudaError_t q4_attention_setup() {
 #define PKV_Q4_SETUP2(D, NG, H16, NT, SEL) \
     if ((e = cudaFuncSetAttribute(q4_decode_kernel<D, NG, H16, NT, SEL>, cudaFuncAttributeMaxDynamicSharedMemorySize, Q4Shape<D, NG, NT>::kSmem)) != cudaSuccess) return e;
 #define PKV_Q4_SETUP1(D, NG, H16, NT) PKV_Q4_SETUP2(D, NG, H16, NT, false) PKV_Q4_SETUP2(D, NG, H16, NT, true)
-#define PKV_Q4_SETUP(D, NG) PKV_Q4_SETUP1(D, NG, false, 1) PKV_Q4_SETUP1(D, NG, false, 2) PKV_Q4_SETUP1(D, NG, true, 1) PKV_Q4_SETUP1(D, NG, true, 2)
+#define PKV_Q4_SETUP3(D, NG, H16) \
+    if ((e = cudaFuncSetAttribute(q4_decode_kernel<D, NG, H16, 1, true, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, Q4Shape<D, NG, 1, true>::kSmem)) != cudaSuccess) return e;
+#define PKV_Q4_SETUP(D, NG) PKV_Q4_SETUP3(D, NG, false) PKV_Q4_SETUP3(D, NG, true) PKV_Q4_SETUP1(D, NG, false, 1) PKV_Q4_SETUP1(D, NG, false, 2) PKV_Q4_SETUP1(D, NG, true, 1) PKV_Q4_SETUP1(D, NG, true, 2)
     PKV_Q4_SHAPES(PKV_Q4_SETUP)
     return cudaSuccess;
 }
@@ -1120,57 +1212,113 @@ int q4_visited(int max_q_len, int max_len, const Q4Select &sel) {
     return sel.window > 0 && most < max_len ? (int)most : max_len;
 }
 
+// How a call is launched: which kernel, on how many CTAs, with how many rows to a tile.
+struct Q4Route { int blocks, small, whole, cluster, n, R; };
+
+Q4Route q4_route(const Q4Geometry &g, int n_seqs, int max_q_len, int max_len, const Q4Select &sel) {
+    Q4Route r{};
+    r.cluster = 1;
+    const bool part = sel.window > 0 || sel.tree;
+    if (part) max_len = q4_visited(max_q_len, max_len, sel);
+    const double units = (max_len + kQ4Unit - 1) / kQ4Unit, rows = (double)max_q_len * g.group, heads = (double)n_seqs * g.n_kv_heads;
+    r.blocks = q4_by_blocks(g, n_seqs, max_q_len, max_len);
+    if (part) {
+        // Estimates in us, fitted to 45 shapes (1 to 128 sequences, 1 to 64 new rows, windows of 256 to 16384 and whole contexts up to 64K, d = 128; the
+        // choice was within 5 % of the best of the three in all but two):
+        // small CTAs: rounds of a unit's chain, 1.6 us alone and 4.1 with all warps busy (one request, window of 4096: 15.2 against 17.7 us on the
+        // column kernel's even shares; 64 requests, 1024: 34 against 62; 8 requests, 16384: 49 against 47)
+        const double segs = heads * std::ceil(rows / 8), slots = 2. * g.n_ctas;
+        int c = 1;
+        while (c < 8 && segs * 2 * c <= slots && 3 * c < units) c *= 2;
+        const double waves = std::ceil(segs * c / slots), busy = std::min(1., segs * c / slots);
+        const double small = 9.2 + (c > 1) + waves * std::ceil(units / (3 * c)) * (1.6 + 2.5 * busy) + 5 * (waves - 1);
+        // even shares: units, what a segment costs beside them, two launches (8 rows / 16 rows to a tile)
+        const double tiles = heads * std::ceil(rows / 16), blocks = heads * std::ceil(rows / kQ4BlockRows), share = 296. / g.n_ctas;
+        const double split = rows <= 8 ? std::max(17 + segs * units * 1.3e-3 * share, 10 + segs * (units + 31) * 2.05e-3 * share)
+                                       : std::max(24.5, 17.6 + tiles * (units + 15) * 2.95e-3 * share);
+        // row blocks (8 requests, 64 rows x 4 heads against 32K: 355 us; 8 rows x 4 heads against 16K: 158 us against 116)
+        const double per = (g.head_dim == 128 ? 1. : 0.7) * (rows <= 128 ? 1.24 : 1.49);
+        const double by_blocks = (rows <= 128 ? 20 : g.head_dim == 128 ? 33 : 25) + blocks * (units + 4) * per / g.n_sms;
+        r.small = small <= split && small <= by_blocks;
+        r.blocks = !r.small && by_blocks < split;
+#ifdef PKV_ROUTE_TEST
+        if (const char *e = getenv("PKV_ROUTE")) { r.small = e[0] == 's'; r.blocks = e[0] == 'b'; if (r.small && e[1]) while (c > e[1] - '0') c /= 2; }
+        if (getenv("PKV_ROUTE_SHOW")) fprintf(stderr, "small %.1f (c %d) split %.1f blocks %.1f\n", small, c, split, by_blocks);
+#endif
+        if (r.small) {
+            r.whole = 1;
+            r.cluster = c;
+            r.R = 8;
+            r.n = c * (int)std::min(segs, std::floor(slots / c));
+            return r;
+        }
+    }
+    r.R = r.blocks ? kQ4BlockRows : q4_rows_per_tile(g, max_q_len);
+    r.whole = !part && !r.blocks && q4_whole(max_len);
+    r.n = r.blocks ? q4_block_grid(g, n_seqs, max_q_len, max_len, sel) : q4_grid(g, n_seqs, max_q_len, max_len, r.whole);
+    return r;
+}
+
 long long q4_attention_workspace(const Q4Geometry &g, int n_seqs, int max_q_len, int max_len, const Q4Select &sel) {
-    max_len = q4_visited(max_q_len, max_len, sel);
-    if (q4_by_blocks(g, n_seqs, max_q_len, max_len)) return q4_block_workspace(g, n_seqs, max_q_len, max_len, sel);
-    const int n = q4_grid(g, n_seqs, max_q_len, max_len);
-    return n <= 1 || q4_whole(max_len) ? 0 : q4_parts_bytes(n) + 2LL * n * q4_state_floats(q4_rows_per_tile(g, max_q_len), g.head_dim) * 4;
+    const Q4Route r = q4_route(g, n_seqs, max_q_len, max_len, sel);
+    return r.n <= 1 || r.whole ? 0 : q4_parts_bytes(r.n) + 2LL * r.n * q4_state_floats(r.R, g.head_dim) * 4;
 }
 
 cudaError_t launch_q4_attention(Q4AttentionArgs a, cudaStream_t st) {
     const Q4Geometry &g = a.geo;
-    const Q4Select sel{a.window, a.sinks, a.tree != nullptr};
     const bool part = a.window > 0 || a.tree;
-    a.max_len = q4_visited(a.max_q_len, a.max_len, sel);
-    const bool blocks = q4_by_blocks(g, a.rows.n_seqs, a.max_q_len, a.max_len);
-    const int n = blocks ? q4_block_grid(g, a.rows.n_seqs, a.max_q_len, a.max_len, sel) : q4_grid(g, a.rows.n_seqs, a.max_q_len, a.max_len);
-    const int R = blocks ? kQ4BlockRows : q4_rows_per_tile(g, a.max_q_len);
-    a.whole = !blocks && q4_whole(a.max_len);
+    const Q4Route r = q4_route(g, a.rows.n_seqs, a.max_q_len, a.max_len, Q4Select{a.window, a.sinks, a.tree != nullptr});
+    const int n = r.n, R = r.R;
+    a.whole = r.whole;
+    a.cluster = r.cluster;
     a.chained = q4_chained();
     a.join = n > 1 && !a.whole;
-    cudaLaunchAttribute at[1];
+    cudaLaunchAttribute at[2];
     at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     at[0].val.programmaticStreamSerializationAllowed = 1;
+    at[1].id = cudaLaunchAttributeClusterDimension;
+    at[1].val.clusterDim.x = r.cluster;
+    at[1].val.clusterDim.y = at[1].val.clusterDim.z = 1;
     cudaLaunchConfig_t cfg = {};
     cfg.stream = st;
     cfg.attrs = at;
     cfg.numAttrs = a.chained;
     cudaError_t e = cudaErrorInvalidValue;
 #define PKV_Q4_LAUNCH1(D, NG, H, NT)                                        \
-    if ((g.fp16 != 0) == H && R == 8 * NT) {                                \
+    if ((g.fp16 != 0) == H && R == 8 * NT && !r.small) {                    \
         cfg.gridDim = dim3(n);                                              \
         cfg.blockDim = dim3(Q4Shape<D, NG, NT>::kThreads);                  \
         cfg.dynamicSmemBytes = Q4Shape<D, NG, NT>::kSmem;                   \
         e = part ? cudaLaunchKernelEx(&cfg, q4_decode_kernel<D, NG, H, NT, true>, a) : cudaLaunchKernelEx(&cfg, q4_decode_kernel<D, NG, H, NT, false>, a); \
     }
+#define PKV_Q4_LAUNCH2(D, NG, H)                                            \
+    if ((g.fp16 != 0) == H && r.small) {                                    \
+        cfg.gridDim = dim3(n);                                              \
+        cfg.blockDim = dim3(Q4Shape<D, NG, 1, true>::kThreads);             \
+        cfg.dynamicSmemBytes = Q4Shape<D, NG, 1, true>::kSmem;              \
+        cfg.attrs = a.chained ? at : at + 1;                                \
+        cfg.numAttrs = a.chained + 1;                                       \
+        e = cudaLaunchKernelEx(&cfg, q4_decode_kernel<D, NG, H, 1, true, true>, a); \
+    }
 #define PKV_Q4_LAUNCH(D, NG)                                                                     \
     if (g.head_dim == D && g.groups == NG) {                                                     \
+        PKV_Q4_LAUNCH2(D, NG, false) PKV_Q4_LAUNCH2(D, NG, true)                                 \
         PKV_Q4_LAUNCH1(D, NG, false, 1) PKV_Q4_LAUNCH1(D, NG, false, 2)                          \
         PKV_Q4_LAUNCH1(D, NG, true, 1) PKV_Q4_LAUNCH1(D, NG, true, 2)                            \
     }
-    if (blocks) {
+    if (r.blocks) {
         e = launch_q4_block(a, n, st);
     } else {
         PKV_Q4_SHAPES(PKV_Q4_LAUNCH)
     }
     if (e != cudaSuccess || !a.join) return e;
     cfg.numAttrs = 1;
-    cfg.gridDim = dim3(n, blocks ? R / (4 * kQ4JoinWarps) : R);
+    cfg.gridDim = dim3(n, r.blocks ? R / (4 * kQ4JoinWarps) : R);
     cfg.blockDim = dim3(32 * kQ4JoinWarps);
     cfg.dynamicSmemBytes = 0;
 #define PKV_Q4_JOIN(D, H)                                                                                         \
     if (g.head_dim == D && (g.fp16 != 0) == H)                                                                    \
-        return blocks ? cudaLaunchKernelEx(&cfg, q4_join_kernel<D, H, 4>, a, R) : cudaLaunchKernelEx(&cfg, q4_join_kernel<D, H, 1>, a, R);
+        return r.blocks ? cudaLaunchKernelEx(&cfg, q4_join_kernel<D, H, 4>, a, R) : cudaLaunchKernelEx(&cfg, q4_join_kernel<D, H, 1>, a, R);
     PKV_Q4_JOIN(128, false) PKV_Q4_JOIN(128, true) PKV_Q4_JOIN(64, false) PKV_Q4_JOIN(64, true)
     return cudaErrorInvalidValue;
 }

@@ -985,11 +985,6 @@ int q4_block_grid(const Q4Geometry &g, int n_seqs, int max_q_len, int max_len, c
     return all >= g.n_sms ? g.n_sms : all < 1 ? 1 : (int)all;
 }
 
-long long q4_block_workspace(const Q4Geometry &g, int n_seqs, int max_q_len, int max_len, const Q4Select &sel) {
-    const int n = q4_block_grid(g, n_seqs, max_q_len, max_len, sel);
-    return n <= 1 ? 0 : q4_parts_bytes(n) + 2LL * n * q4_state_floats(kBRows, g.head_dim) * 4;
-}
-
 cudaError_t launch_q4_block(const Q4AttentionArgs &a, int n, cudaStream_t st) {
     const Q4Geometry &g = a.geo;
     cudaLaunchAttribute at[1];

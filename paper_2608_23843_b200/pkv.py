@@ -812,35 +812,36 @@ class Q4Cache:
     def _ints(self, name, t, shape, dtype=_INT32):
         if not (t.shape == shape and t.dtype is dtype and t.get_device() == self._device_index and t.is_contiguous()):
             self._fail("%s must be a contiguous %s tensor %r on %s" % (name, str(dtype)[6:], list(shape), self.device))
-        return t.data_ptr()
-
-    def _offsets(self, offsets, n_seqs):
-        return None if offsets is None else self._ints("offsets", offsets, (n_seqs + 1,))
 
     def tree_masks(self, parents, lengths=None, offsets=None, max_q_len=None, window=0, sinks=0):
         """Masks and depths of drafted tokens.  parents: int32 [n_seqs, n], or [rows] with offsets: the row of the same sequence, an
         earlier one, that a row continues, -1 for the last token of the context.  -> (int64 parents.shape + (words,), for attention(tree=...),
         int32 depths of parents' shape: a row's position is the context's length + its depth).  With a window and sinks, those of the attention call and the
         sequences' lengths (the rows included).  With offsets, max_q_len bounds the rows of a sequence (default: all rows)."""
-        ragged = offsets is not None
-        if parents.dim() != (1 if ragged else 2):
-            self._fail("parents must be [rows] with offsets and [n_seqs, n] without")
-        n_seqs = offsets.numel() - 1 if ragged else parents.shape[0]
-        n = parents.numel()
-        if not ragged:
-            max_q_len = parents.shape[1]
-        elif max_q_len is None:
-            max_q_len = n
-        words = max(1, -(-max_q_len // 64))
-        if lengths is None and window and sinks:
+        shape, n, dev = parents.shape, parents.numel(), self._device_index
+        if offsets is None:
+            if len(shape) != 2:
+                self._fail("parents must be [rows] with offsets and [n_seqs, n] without")
+            n_seqs, max_q_len = shape
+        else:
+            if len(shape) != 1:
+                self._fail("parents must be [rows] with offsets and [n_seqs, n] without")
+            n_seqs = offsets.numel() - 1
+            if max_q_len is None:
+                max_q_len = n
+            self._ints("offsets", offsets, (n_seqs + 1,))
+        if not (parents.dtype is _INT32 and parents.get_device() == dev and parents.is_contiguous()):
+            self._ints("parents", parents, shape)
+        if lengths is not None:
+            if not (lengths.dtype is _INT32 and lengths.shape == (n_seqs,) and lengths.get_device() == dev and lengths.is_contiguous()):
+                self._ints("lengths", lengths, (n_seqs,))
+        elif window and sinks:
             self._fail("a window with sinks needs the sequences' lengths")
-        self._ints("parents", parents, parents.shape)
-        length_ptr = None if lengths is None else self._ints("lengths", lengths, (n_seqs,))
-        off = self._offsets(offsets, n_seqs)
-        masks = torch.empty((*parents.shape, words), dtype=_INT64, device=self.device)
-        depths = torch.empty(parents.shape, dtype=_INT32, device=self.device)
-        self._call(lib().pkv_q4_tree_masks, n_seqs, length_ptr, n, off, max_q_len, parents.data_ptr(), window, sinks, masks.data_ptr(), words,
-                   depths.data_ptr(), self._stream())
+        words = max_q_len + 63 >> 6 if max_q_len > 0 else 1
+        depths = torch.empty_like(parents)
+        masks = torch.empty((*shape, words), dtype=_INT64, device=self.device)
+        self._call(lib().pkv_q4_tree_masks, n_seqs, None if lengths is None else lengths.data_ptr(), n, None if offsets is None else offsets.data_ptr(),
+                   max_q_len, parents.data_ptr(), window, sinks, masks.data_ptr(), words, depths.data_ptr(), self._stream())
         return masks, depths
 
     def keep_rows(self, page_table, lengths, paths, counts, new_rows, offsets=None, out=None):
@@ -848,16 +849,18 @@ class Q4Cache:
         i < counts[s] (int32 [n_seqs]); rows of a path ascend.  new_rows: how many new rows each sequence has, or with offsets how many
         the call has.  -> the lengths (out, not overlapping `lengths`, or a new tensor)."""
         n_seqs, max_pages = self._seqs(page_table, lengths, offsets)
-        if paths.dim() != 2:
-            self._fail("paths must be int32 [n_seqs, m]")
-        self._ints("paths", paths, (n_seqs, paths.shape[1]))
-        self._ints("counts", counts, (n_seqs,))
+        dev, most = self._device_index, paths.shape
+        if not (len(most) == 2 and most[0] == n_seqs and paths.dtype is counts.dtype is _INT32 and counts.shape == (n_seqs,) and
+                paths.get_device() == counts.get_device() == dev and paths.is_contiguous() and counts.is_contiguous()):
+            self._ints("paths", paths, (n_seqs, most[-1] if len(most) == 2 else "m"))
+            self._ints("counts", counts, (n_seqs,))
         if out is None:
             out = torch.empty_like(lengths)
-        self._ints("out", out, (n_seqs,))
+        else:
+            self._ints("out", out, (n_seqs,))
         n = new_rows if offsets is not None else new_rows * n_seqs
         self._call(lib().pkv_q4_keep_rows, n_seqs, page_table.data_ptr(), max_pages, lengths.data_ptr(), n, None if offsets is None else offsets.data_ptr(),
-                   paths.data_ptr(), paths.shape[1], counts.data_ptr(), out.data_ptr(), self._stream())
+                   paths.data_ptr(), most[1], counts.data_ptr(), out.data_ptr(), self._stream())
         return out
 
     def new_ring(self, pages=None):
@@ -876,27 +879,40 @@ class Q4Cache:
         in all.  Writes new entries into page_table and returned pages into ring.  -> Q4Plan of new tensors, or `out`, whose
         lengths, spans and counters may be the ones given (in place).  Where pages are missing or requests make no sense nothing is done: counters[2:]."""
         n_seqs, max_pages = self._seqs(page_table, lengths, None)
-        dev = self.device
+        dev, one = self._device_index, (n_seqs,)
+        if not (rows.dtype is spans.dtype is ring.dtype is _INT32 and counters.dtype is _INT64 and rows.shape == one and spans.shape == (n_seqs, 2) and
+                ring.shape == (self.cfg.n_pages,) and counters.shape == (4,) and
+                rows.get_device() == spans.get_device() == ring.get_device() == counters.get_device() == dev and
+                rows.is_contiguous() and spans.is_contiguous() and ring.is_contiguous() and counters.is_contiguous()):
+            self._ints("rows", rows, one)
+            self._ints("spans", spans, (n_seqs, 2))
+            self._ints("ring", ring, (self.cfg.n_pages,))
+            self._ints("counters", counters, (4,), _INT64)
         if out is None:
-            ints = torch.empty(n_seqs * 4 + 1 + n_rows, dtype=_INT32, device=dev)      # (one allocation of each type)
-            longs = torch.empty(4 + n_rows, dtype=_INT64, device=dev)
-            out = Q4Plan(ints[:n_seqs], ints[n_seqs:2 * n_seqs + 1], ints[4 * n_seqs + 1:], longs[4:], ints[2 * n_seqs + 1:4 * n_seqs + 1].view(n_seqs, 2),
-                         longs[:4])
-        args = [self._ints("rows", rows, (n_seqs,)), self._ints("spans", spans, (n_seqs, 2)), self._ints("ring", ring, (self.cfg.n_pages,)),
-                self._ints("counters", counters, (4,), _INT64)]
-        outs = [self._ints("out.lengths", out.lengths, (n_seqs,)), self._ints("out.spans", out.spans, (n_seqs, 2)),
-                self._ints("out.counters", out.counters, (4,), _INT64), self._ints("out.offsets", out.offsets, (n_seqs + 1,))]
-        pos = None if out.positions is None else self._ints("out.positions", out.positions, (n_rows,))
-        slots = None if out.slots is None else self._ints("out.slots", out.slots, (n_rows,), _INT64)
+            # (each from the allocator: slices of one tensor take longer)
+            out = Q4Plan(torch.empty_like(lengths), lengths.new_empty(n_seqs + 1), lengths.new_empty(n_rows), counters.new_empty(n_rows), torch.empty_like(spans),
+                         torch.empty_like(counters))
+        else:
+            self._ints("out.lengths", out.lengths, one)
+            self._ints("out.spans", out.spans, (n_seqs, 2))
+            self._ints("out.counters", out.counters, (4,), _INT64)
+            self._ints("out.offsets", out.offsets, (n_seqs + 1,))
+            if out.positions is not None:
+                self._ints("out.positions", out.positions, (n_rows,))
+            if out.slots is not None:
+                self._ints("out.slots", out.slots, (n_rows,), _INT64)
         key = (n_seqs, n_rows)
         size = self._workspaces.get(key)
         if size is None:
             if len(self._workspaces) >= 256:
                 self._workspaces.clear()
             size = self._workspaces[key] = pkv_q4_plan_workspace(self.handle, n_seqs, n_rows)
-        work = torch.empty(size, dtype=torch.uint8, device=dev) if size and not self.dry_run else None
-        self._call(lib().pkv_q4_plan, n_seqs, page_table.data_ptr(), max_pages, lengths.data_ptr(), *args, window, sinks, *outs, n_rows, pos, slots,
-                   None if work is None else work.data_ptr(), size, self._stream())
+        work = torch.empty(size, dtype=torch.uint8, device=self.device) if size and not self.dry_run else None
+        pos, slots = out.positions, out.slots
+        self._call(lib().pkv_q4_plan, n_seqs, page_table.data_ptr(), max_pages, lengths.data_ptr(), rows.data_ptr(), spans.data_ptr(), ring.data_ptr(),
+                   counters.data_ptr(), window, sinks, out.lengths.data_ptr(), out.spans.data_ptr(), out.counters.data_ptr(), out.offsets.data_ptr(), n_rows,
+                   None if pos is None else pos.data_ptr(), None if slots is None else slots.data_ptr(), None if work is None else work.data_ptr(), size,
+                   self._stream())
         return out
 
     def stats(self):
