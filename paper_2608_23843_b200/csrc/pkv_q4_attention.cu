@@ -63,7 +63,7 @@ struct Q4Shape {
     static constexpr int kStage = ((kUnitBytes > kFlush ? kUnitBytes : kFlush) + 127) / 128 * 128;
     // the other arrays in shared memory: per warp the states' (m, l), references and gains, per stage two barriers and a word; 1 KB is the system's
     // (kSmall: and the cluster's share of the segment's state)
-    static constexpr int kOther = 1024 + kCons * (64 + NT * (128 + 16 * NG)) + 32 / kPerSM * 20 + 256 + (kSmall ? kFlush + kCons * 64 + 192 : 0);
+    static constexpr int kOther = 1024 + kCons * (64 + NT * (128 + 16 * NG)) + 32 / kPerSM * 20 + 256 + (kSmall ? 8 * D * 4 + 512 + kCons * 64 + 128 : 0);
     static constexpr int kFit = (227 * 1024 / kPerSM - kOther - kQueries) / kStage, kStages = kFit < 32 / kPerSM ? kFit : 32 / kPerSM;
     static constexpr int kSmem = kStages * kStage;
     static_assert(kStages > kCons && kPerSM * (kSmem + kQueries + kOther) <= 227 * 1024, "a stage per warp and some in flight");
@@ -237,27 +237,23 @@ __device__ __forceinline__ void q4_advance(const Q4AttentionArgs &a, int rows_pe
     }
 }
 
-__device__ __forceinline__ void cluster_sync() {
-    asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
-}
+__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
+__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
 __device__ __forceinline__ uint32_t cluster_at(uint32_t at, int rank) {      // the same place in another CTA's shared memory
     uint32_t r;
     asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(at), "r"(rank));
     return r;
 }
-__device__ __forceinline__ float4 cluster_ld4(uint32_t at) {
-    float4 v;
-    asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(at) : "memory");
-    return v;
+__device__ __forceinline__ void cluster_st4(uint32_t at, const float4 &v) {
+    asm volatile("st.shared::cluster.v4.f32 [%0], {%1, %2, %3, %4};" ::"r"(at), "f"(v.x), "f"(v.y), "f"(v.z), "f"(v.w) : "memory");
 }
-__device__ __forceinline__ float2 cluster_ld2(uint32_t at) {
-    float2 v;
-    asm volatile("ld.shared::cluster.v2.f32 {%0, %1}, [%2];" : "=f"(v.x), "=f"(v.y) : "r"(at) : "memory");
-    return v;
+__device__ __forceinline__ void cluster_st2(uint32_t at, float x, float y) {
+    asm volatile("st.shared::cluster.v2.f32 [%0], {%1, %2};" ::"r"(at), "f"(x), "f"(y) : "memory");
 }
 
 // kSel: the queries see a part of the positions.  kSmall: whole segments only, each by one CTA or by a cluster whose CTAs take an equal run
-// of its units each and join their states through shared memory, some of the rows each.
+// of its units each.  They join their states through shared memory: each CTA sees to some of the channels, the others push theirs there (read by
+// those that need them instead, behind one barrier and ahead of another: 10.9 us for 7 drafted tokens against 1500).
 template <int D, int NG, bool H16, int NT, bool kSel, bool kSmall = false>
 __global__ void __launch_bounds__(Q4Shape<D, NG, NT, kSmall>::kThreads, q4_ctas_per_sm(NT, kSmall)) q4_decode_kernel(const __grid_constant__ Q4AttentionArgs a) {
     static_assert(!kSmall || (kSel && NT == 1), "see above");
@@ -274,8 +270,8 @@ __global__ void __launch_bounds__(Q4Shape<D, NG, NT, kSmall>::kThreads, q4_ctas_
     __shared__ int vis[kSel ? 1 : 8 * NT];                     // tokens a column's query sees
     __shared__ Q4Seen part[kSel ? 8 * NT : 1];                 // kSel: which ones
     __shared__ __align__(8) uint16_t seen[kSel ? kCons : 1][8 * NT][kQ4UnitTiles];      // ... in a warp's unit, a bit each
-    __shared__ __align__(16) float share_o[kSmall ? 8 * S::kRowFloats : 1];      // kSmall: the state of this CTA's part of a segment
-    __shared__ float2 share_ml[kSmall ? 8 : 1];
+    __shared__ __align__(16) float share_o[kSmall ? 8 * D : 1];      // kSmall: [CTA of the cluster][row][this CTA's channels], and (m, l)
+    __shared__ float2 share_ml[kSmall ? 8 : 1][8];
     __shared__ uint4 queries[NT][NW][32];                      // of the segment, as the lanes of a warp take them
     __shared__ long long sums[kQ4Warps], found_at;
     __shared__ int found_seq, offs[kCons], gave_up;
@@ -302,9 +298,24 @@ __global__ void __launch_bounds__(Q4Shape<D, NG, NT, kSmall>::kThreads, q4_ctas_
         const int n = q4_new_rows(a, s, first, all, st), T = q4_length(a.rows, geo, s, st);
         return (long long)((n * geo.group + R - 1) / R) * H * (a_whole ? 1 : q4_seq_units<kSel>(a, T, all) + kSegCost);
     };
-    long long total = 0;
+    const bool once = kSel && n_seqs <= kQ4Threads;            // a sequence to a thread: one scan for the sum and the place
+    long long total = 0, upto = 0, own_weight = 0;
     if (n_seqs == 1) {
         total = weight(0, tid == 0 ? status : nullptr);
+    } else if (once) {
+        own_weight = upto = weight(tid, status);
+#pragma unroll
+        for (int d = 1; d < 32; d <<= 1) {
+            const long long y = __shfl_up_sync(0xffffffffu, upto, d);
+            if (lane >= d) upto += y;
+        }
+        if (lane == 31) sums[warp] = upto;
+        __syncthreads();
+#pragma unroll
+        for (int w = 0; w < kQ4Warps; ++w) {
+            if (w < warp) upto += sums[w];
+            total += sums[w];
+        }
     } else {
         long long mine = 0;
         for (int s = tid; s < n_seqs; s += kQ4Threads) mine += weight(s, status);
@@ -336,6 +347,11 @@ __global__ void __launch_bounds__(Q4Shape<D, NG, NT, kSmall>::kThreads, q4_ctas_
     if (n_seqs == 1) {
         seg.seq = 0;
         __syncthreads();                                       // (the barriers are initialised)
+    } else if (once) {
+        if (begin >= upto - own_weight && begin < upto) { found_seq = tid; found_at = begin - (upto - own_weight); }
+        __syncthreads();
+        seg.seq = found_seq;
+        at0 = found_at;
     } else {                                                   // the sequence that holds `begin`
         long long base = 0;
         for (int s0 = 0; s0 < n_seqs; s0 += kQ4Threads) {
@@ -380,6 +396,7 @@ __global__ void __launch_bounds__(Q4Shape<D, NG, NT, kSmall>::kThreads, q4_ctas_
         if (kSmall && cluster > 1) {                           // (its one segment: the launch gives every segment a cluster)
             seg.unit = (int)((long long)seg.units * rank / cluster);
             left_cta = (int)((long long)seg.units * (rank + 1) / cluster) - seg.unit;
+            cluster_arrive();                                  // (waited for before anything is written to another CTA's shared memory: it has begun)
         }
     } else {
         const int len = seg.units + kSegCost;
@@ -464,8 +481,9 @@ __global__ void __launch_bounds__(Q4Shape<D, NG, NT, kSmall>::kThreads, q4_ctas_
         for (int back = 1; back <= min(u, kSt); ++back) (void)mbar_wait(smem_u32(&full[(u - back) % kSt]), ((u - back) / kSt) & 1);
         if (kSmall && cluster > 1) {
             __syncwarp();
-            cluster_sync();
-            cluster_sync();
+            cluster_wait();
+            cluster_arrive();
+            cluster_wait();
         }
         return;
     }
@@ -976,7 +994,9 @@ __global__ void __launch_bounds__(Q4Shape<D, NG, NT, kSmall>::kThreads, q4_ctas_
                                                (long long)h * a.out_head + ch) = v;
                 }
             };
-            for (int i = tid; i < 8 * (D / 4); i += 32 * kCons) {
+            if (kSmall && cluster > 1) cluster_wait();
+            const int rows_here = kSmall ? min(8, n * G - seg.tile * R) : 8;
+            for (int i = tid; i < rows_here * (D / 4); i += 32 * kCons) {
                 const int r8 = i / (D / 4), r = nt * 8 + r8, ch = i % (D / 4) * 4;
                 float M = kNegInf;
 #pragma unroll
@@ -993,8 +1013,9 @@ __global__ void __launch_bounds__(Q4Shape<D, NG, NT, kSmall>::kThreads, q4_ctas_
                     acc.x += f * x.x; acc.y += f * x.y; acc.z += f * x.z; acc.w += f * x.w;
                 }
                 if (kSmall && cluster > 1) {
-                    *reinterpret_cast<float4 *>(share_o + r * S::kRowFloats + ch) = acc;
-                    if (ch == 0) share_ml[r] = make_float2(M, L);
+                    const int own = D / cluster, to = ch / own, in = ch - to * own;
+                    cluster_st4(cluster_at(smem_u32(share_o + (rank * 8 + r) * own + in), to), acc);
+                    if (in == 0) cluster_st2(cluster_at(smem_u32(&share_ml[rank][r]), to), M, L);
                     continue;
                 }
                 if (!complete) {
@@ -1004,30 +1025,23 @@ __global__ void __launch_bounds__(Q4Shape<D, NG, NT, kSmall>::kThreads, q4_ctas_
                 }
                 write(r, ch, M, L, acc);
             }
-            if (kSmall && cluster > 1) {                       // rows rank, rank + cluster, ... of all parts, in order
-                cluster_sync();
-                for (int i = tid; i < 8 / cluster * (D / 4); i += 32 * kCons) {
-                    const int r = i / (D / 4) * cluster + rank, ch = i % (D / 4) * 4;
-                    float2 s[8];
+            if (kSmall && cluster > 1) {                       // this CTA's channels of all parts, in order
+                cluster_arrive();
+                cluster_wait();
+                const int own = D / cluster;
+                for (int i = tid; i < rows_here * (own / 4); i += 32 * kCons) {
+                    const int r = i / (own / 4), in = i % (own / 4) * 4;
                     float M = kNegInf, L = 0.f;
                     float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll
-                    for (int k = 0; k < 8; ++k) {
-                        if (k >= cluster) break;
-                        s[k] = cluster_ld2(cluster_at(smem_u32(&share_ml[r]), k));
-                        M = fmaxf(M, s[k].x);
-                    }
-#pragma unroll
-                    for (int k = 0; k < 8; ++k) {
-                        if (k >= cluster) break;
-                        const float f = ex2(s[k].x - M);
-                        const float4 x = cluster_ld4(cluster_at(smem_u32(share_o + r * S::kRowFloats + ch), k));
-                        L += f * s[k].y;
+                    for (int k = 0; k < cluster; ++k) M = fmaxf(M, share_ml[k][r].x);
+                    for (int k = 0; k < cluster; ++k) {
+                        const float f = ex2(share_ml[k][r].x - M);
+                        const float4 x = *reinterpret_cast<const float4 *>(share_o + (k * 8 + r) * own + in);
+                        L += f * share_ml[k][r].y;
                         acc.x += f * x.x; acc.y += f * x.y; acc.z += f * x.z; acc.w += f * x.w;
                     }
-                    write(r, ch, M, L, acc);
+                    write(r, rank * own + in, M, L, acc);
                 }
-                cluster_sync();                                // (no CTA leaves while its state is read)
             }
             if (nt == NT - 1) asm volatile("fence.proxy.async.shared::cta;" ::: "memory");      // the stages go back to the copies
             consumers_sync();
@@ -1225,18 +1239,18 @@ Q4Route q4_route(const Q4Geometry &g, int n_seqs, int max_q_len, int max_len, co
     if (part) {
         // Estimates in us, fitted to 45 shapes (1 to 128 sequences, 1 to 64 new rows, windows of 256 to 16384 and whole contexts up to 64K, d = 128; the
         // choice was within 5 % of the best of the three in all but two):
-        // small CTAs: rounds of a unit's chain, 1.6 us alone and 4.1 with all warps busy (one request, window of 4096: 15.2 against 17.7 us on the
-        // column kernel's even shares; 64 requests, 1024: 34 against 62; 8 requests, 16384: 49 against 47)
+        // small CTAs: rounds of a unit's chain, 1.5 us alone and 3.7 with all warps busy (one request, window of 4096: 13.5 against 17.0 us on the
+        // column kernel's even shares; 64 requests, 1024: 31 against 62; 32 requests, 8192: 86.0 against 84.6; one, 16384: 25.6 against 19.2)
         const double segs = heads * std::ceil(rows / 8), slots = 2. * g.n_ctas;
         int c = 1;
         while (c < 8 && segs * 2 * c <= slots && 3 * c < units) c *= 2;
         const double waves = std::ceil(segs * c / slots), busy = std::min(1., segs * c / slots);
-        const double small = 9.2 + (c > 1) + waves * std::ceil(units / (3 * c)) * (1.6 + 2.5 * busy) + 5 * (waves - 1);
+        const double small = 8 + waves * std::ceil(units / (3 * c)) * (1.5 + 2.2 * busy) + 4 * (waves - 1);
         // even shares: units, what a segment costs beside them, two launches (8 rows / 16 rows to a tile)
         const double tiles = heads * std::ceil(rows / 16), blocks = heads * std::ceil(rows / kQ4BlockRows), share = 296. / g.n_ctas;
         const double split = rows <= 8 ? std::max(17 + segs * units * 1.3e-3 * share, 10 + segs * (units + 31) * 2.05e-3 * share)
                                        : std::max(24.5, 17.6 + tiles * (units + 15) * 2.95e-3 * share);
-        // row blocks (8 requests, 64 rows x 4 heads against 32K: 355 us; 8 rows x 4 heads against 16K: 158 us against 116)
+        // row blocks (8 requests, 64 rows x 4 heads against 32K: 355 us and 1540 by even shares; 8 rows x 4 heads against 16K: 161 us and 116)
         const double per = (g.head_dim == 128 ? 1. : 0.7) * (rows <= 128 ? 1.24 : 1.49);
         const double by_blocks = (rows <= 128 ? 20 : g.head_dim == 128 ? 33 : 25) + blocks * (units + 4) * per / g.n_sms;
         r.small = small <= split && small <= by_blocks;

@@ -280,9 +280,24 @@ __global__ void __launch_bounds__(kBThreads, 1) q4_block_kernel(const __grid_con
         if (s >= n_seqs) return 0;
         return block_weight<kSel>(a, block_seq(a, s, st)) * H;
     };
-    long long total = 0;
+    const bool once = kSel && n_seqs <= kBThreads;             // a sequence to a thread: one scan for the sum and the place
+    long long total = 0, upto = 0, own_weight = 0;
     if (n_seqs == 1) {
         total = weight(0, tid == 0 ? status : nullptr);
+    } else if (once) {
+        own_weight = upto = weight(tid, status);
+#pragma unroll
+        for (int d = 1; d < 32; d <<= 1) {
+            const long long y = __shfl_up_sync(0xffffffffu, upto, d);
+            if (lane >= d) upto += y;
+        }
+        if (lane == 31) sums[warp] = upto;
+        __syncthreads();
+#pragma unroll
+        for (int w = 0; w < kBThreads / 32; ++w) {
+            if (w < warp) upto += sums[w];
+            total += sums[w];
+        }
     } else {
         long long mine = 0;
         for (int s = tid; s < n_seqs; s += kBThreads) mine += weight(s, status);
@@ -305,6 +320,11 @@ __global__ void __launch_bounds__(kBThreads, 1) q4_block_kernel(const __grid_con
     long long at0 = begin;                                     // `begin` within its sequence
     if (n_seqs == 1) {
         seg.seq = 0;
+    } else if (once) {
+        if (begin >= upto - own_weight && begin < upto) { found_seq = tid; found_at = begin - (upto - own_weight); }
+        __syncthreads();
+        seg.seq = found_seq;
+        at0 = found_at;
     } else {
         long long base = 0;
         for (int s0 = 0; s0 < n_seqs; s0 += kBThreads) {

@@ -10,16 +10,19 @@ namespace {
 
 // A launch that may be set up while the kernel before it finishes; each kernel here waits before it touches memory.
 template <typename Args>
-cudaError_t launch_chained(void (*kernel)(Args), const Args &a, dim3 grid, int threads, cudaStream_t st) {
-    cudaLaunchAttribute at[1];
-    at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    at[0].val.programmaticStreamSerializationAllowed = 1;
+cudaError_t launch_chained(void (*kernel)(Args), const Args &a, dim3 grid, int threads, cudaStream_t st, int cluster = 1) {
+    cudaLaunchAttribute at[2];
+    at[0].id = cudaLaunchAttributeClusterDimension;
+    at[0].val.clusterDim.x = cluster;
+    at[0].val.clusterDim.y = at[0].val.clusterDim.z = 1;
+    at[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    at[1].val.programmaticStreamSerializationAllowed = 1;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = grid;
     cfg.blockDim = dim3(threads);
     cfg.stream = st;
-    cfg.attrs = at;
-    cfg.numAttrs = a.chained;
+    cfg.attrs = cluster > 1 ? at : at + 1;
+    cfg.numAttrs = (cluster > 1) + a.chained;
     return cudaLaunchKernelEx(&cfg, kernel, a);
 }
 
@@ -145,13 +148,15 @@ __global__ void __launch_bounds__(kKeepThreads) q4_keep_kernel(const __grid_cons
 }
 
 // ---- planning a step ------------------------------------------------------------------------------------------------------
-// One CTA goes over the requests: prefix sums of new rows, pages taken and pages given back, from which every row, taken
-// page and returned page follows by itself - a thread each, which finds its request by bisection in the sums.  Few of them are
-// left to the same CTA; more go to a second kernel over the SMs.  Entries that are read (below `end`) and written (from it on), and
+// Prefix sums over the requests - new rows, pages taken, pages given back - from which every row, taken page and returned page follows
+// by itself: a thread each, which finds its request by bisection in the sums.  Up to kPlanHeld requests the sums fit shared memory,
+// and a CTA, or a cluster of eight that all work them out, fills everything in (64 requests: 4.5 us, all latency: launch, counters and lengths, the scan,
+// pages, results; 700 requests with chunks of prompts, one kernel for the sums and one for the rest: 10.6 us and a launch more).  More requests
+// leave the sums in the workspace to a second kernel over the SMs.  Entries that are read (below `end`) and written (from it on), and
 // places of the ring that are read (from the head) and written (from the tail), are different ones, so the order does not matter.
-constexpr int kPlanThreads = 1024, kPlanFillThreads = 256;
-constexpr int kPlanHeld = 1024;                  // requests whose sums fit shared memory
-constexpr long long kPlanFew = 8192;             // rows that one CTA sees to
+constexpr int kPlanThreads = 1024, kPlanFillThreads = 256, kPlanCluster = 8;
+constexpr int kPlanHeld = 1024;                  // a thread each
+constexpr long long kPlanAlone = 2048, kPlanFew = 65536;      // rows that one CTA, a cluster see to
 
 struct PlanRequest { int T, end, a, b; };        // length and end before the step; entries [0, a) and from b on go back
 struct PlanHead { long long head, tail; int rows, taken, back, ok; };
@@ -213,9 +218,10 @@ __device__ __forceinline__ void plan_fill(const Q4PlanArgs &p, const PlanSums &z
         const long long at = head + k;
         return p.ring[at >= n ? at - n : at];
     };
-    if (p.positions || p.slots)
-        for (int i = me; i < h.rows; i += many) {
-            const int s = plan_find(z.rows, p.n_seqs, i);
+    const int rows = p.positions || p.slots ? h.rows : 0;
+    for (long long i0 = me; i0 < (long long)rows + h.taken + h.back; i0 += many) {
+        if (i0 < rows) {
+            const int i = (int)i0, s = plan_find(z.rows, p.n_seqs, i);
             const PlanRequest r = z.req[s];
             const int pos = r.T + i - z.rows[s], e = pos >> p.page_shift;
             if (p.positions) p.positions[i] = pos;
@@ -223,16 +229,15 @@ __device__ __forceinline__ void plan_fill(const Q4PlanArgs &p, const PlanSums &z
                 const int page = e < r.end ? p.table[(long long)s * p.max_pages + e] : free_page(z.taken[s] + e - r.end);
                 p.slots[i] = page < 0 || page >= n ? -1LL : ((long long)page << p.page_shift) + (pos & ((1 << p.page_shift) - 1));
             }
+        } else if (i0 < (long long)rows + h.taken) {
+            const int k = (int)(i0 - rows), s = plan_find(z.taken, p.n_seqs, k);
+            p.table[(long long)s * p.max_pages + z.req[s].end + k - z.taken[s]] = free_page(k);
+        } else {
+            const int k = (int)(i0 - rows - h.taken), s = plan_find(z.back, p.n_seqs, k), x = k - z.back[s];
+            const PlanRequest r = z.req[s];
+            const long long at = tail + k;
+            p.ring[at >= n ? at - n : at] = p.table[(long long)s * p.max_pages + (x < r.a ? x : r.b + x - r.a)];
         }
-    for (int k = me; k < h.taken; k += many) {
-        const int s = plan_find(z.taken, p.n_seqs, k);
-        p.table[(long long)s * p.max_pages + z.req[s].end + k - z.taken[s]] = free_page(k);
-    }
-    for (int k = me; k < h.back; k += many) {
-        const int s = plan_find(z.back, p.n_seqs, k), x = k - z.back[s];
-        const PlanRequest r = z.req[s];
-        const long long at = tail + k;
-        p.ring[at >= n ? at - n : at] = p.table[(long long)s * p.max_pages + (x < r.a ? x : r.b + x - r.a)];
     }
 }
 
@@ -248,7 +253,8 @@ __host__ __device__ inline PlanSums plan_sums(unsigned char *w, int n_seqs) {
 constexpr int kPlanBytes = 64 + kPlanHeld * (int)sizeof(PlanRequest) + 3 * (kPlanHeld + 1) * 4;
 static_assert(sizeof(PlanHead) <= 64 && kPlanBytes <= 48 * 1024, "fits shared memory");
 
-// kAll: the sums stay in shared memory and the same CTA fills in everything
+// kAll: the sums stay in shared memory and the same CTA, or its cluster, fills in everything.  Outputs may be inputs: the cluster's first CTA
+// writes them once all CTAs have read.
 template <bool kAll>
 __global__ void __launch_bounds__(kPlanThreads) q4_plan_kernel(const __grid_constant__ Q4PlanArgs p) {
     __shared__ __align__(16) unsigned char here[kAll ? kPlanBytes : 16];
@@ -257,6 +263,7 @@ __global__ void __launch_bounds__(kPlanThreads) q4_plan_kernel(const __grid_cons
     asm volatile("griddepcontrol.wait;" ::: "memory");
     if (p.chained || !kAll) asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     const PlanSums z = plan_sums(kAll ? here : p.workspace, p.n_seqs);
+    const bool shared = kAll && gridDim.x > 1, writes = !kAll || blockIdx.x == 0;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const long long head = p.counters[0], tail = p.counters[1];
     // this thread's requests: neighbours
@@ -308,10 +315,14 @@ __global__ void __launch_bounds__(kPlanThreads) q4_plan_kernel(const __grid_cons
     const int refused = bad + (total[0] > p.n_rows) + !ring_ok;
     const long long missing = ring_ok ? max(0LL, total[1] - (tail - head)) : 0;
     const bool ok = refused == 0 && missing == 0;
+    if (shared) {
+        asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+        asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+    }
     for (int s = s0; s < s1; ++s) {
         if (per > 1) q = plan_need(p, s);        // (its inputs are this thread's own: it has not written them yet)
         const int rows = (int)before[0];
-        p.offsets[s] = ok ? rows : 0;
+        if (writes) p.offsets[s] = ok ? rows : 0;
         if (ok) {
             z.rows[s] = rows;
             z.taken[s] = (int)before[1];
@@ -321,27 +332,30 @@ __global__ void __launch_bounds__(kPlanThreads) q4_plan_kernel(const __grid_cons
             before[1] += q.taken;
             before[2] += q.back;
         }
+        if (!writes) continue;
         p.lengths_out[s] = !ok ? q.T : q.n < 0 ? 0 : q.T + q.n;
         p.spans_out[2 * s] = !ok ? q.first : q.first_out;
         p.spans_out[2 * s + 1] = !ok ? q.end : q.end_out;
     }
     const PlanHead h{head, tail, ok ? (int)total[0] : 0, ok ? (int)total[1] : 0, ok ? (int)total[2] : 0, ok};
     if (tid == 0) {
-        p.offsets[p.n_seqs] = h.rows;
+        if (writes) p.offsets[p.n_seqs] = h.rows;
         if (ok) {
             z.rows[p.n_seqs] = h.rows;
             z.taken[p.n_seqs] = h.taken;
             z.back[p.n_seqs] = h.back;
         }
         if (!kAll) *z.head = h;
-        p.counters_out[0] = head + h.taken;
-        p.counters_out[1] = tail + h.back;
-        p.counters_out[2] = missing;
-        p.counters_out[3] = refused;
+        if (writes) {
+            p.counters_out[0] = head + h.taken;
+            p.counters_out[1] = tail + h.back;
+            p.counters_out[2] = missing;
+            p.counters_out[3] = refused;
+        }
     }
     if (!kAll) return;
     __syncthreads();
-    plan_fill(p, z, h, tid, kPlanThreads);
+    plan_fill(p, z, h, (int)blockIdx.x * kPlanThreads + tid, (int)gridDim.x * kPlanThreads);
 }
 
 __global__ void __launch_bounds__(kPlanFillThreads) q4_plan_fill_kernel(const __grid_constant__ Q4PlanArgs p) {
@@ -351,7 +365,7 @@ __global__ void __launch_bounds__(kPlanFillThreads) q4_plan_fill_kernel(const __
     plan_fill(p, z, *z.head, (int)(blockIdx.x * kPlanFillThreads + threadIdx.x), (int)(gridDim.x * kPlanFillThreads));
 }
 
-bool plan_by_one(int n_seqs, long long n_rows) { return n_seqs <= kPlanHeld && n_rows <= kPlanFew; }
+bool plan_at_once(int n_seqs, long long n_rows) { return n_seqs <= kPlanHeld && n_rows <= kPlanFew; }
 
 }  // namespace
 
@@ -372,18 +386,19 @@ cudaError_t launch_q4_keep(Q4KeepArgs a, cudaStream_t st) {
 }
 
 long long q4_plan_workspace(int n_seqs, long long n_rows) {
-    return plan_by_one(n_seqs, n_rows) ? 0 : 64 + (long long)n_seqs * (int)sizeof(PlanRequest) + 3LL * (n_seqs + 1) * 4;
+    return plan_at_once(n_seqs, n_rows) ? 0 : 64 + (long long)n_seqs * (int)sizeof(PlanRequest) + 3LL * (n_seqs + 1) * 4;
 }
 
 cudaError_t launch_q4_plan(Q4PlanArgs a, cudaStream_t st) {
     a.chained = q4_chained();
-    if (plan_by_one(a.n_seqs, a.n_rows)) return launch_chained(q4_plan_kernel<true>, a, dim3(1), kPlanThreads, st);
-    const int chained = a.chained;
+    if (plan_at_once(a.n_seqs, a.n_rows)) {
+        const int n = a.n_rows <= kPlanAlone ? 1 : kPlanCluster;
+        return launch_chained(q4_plan_kernel<true>, a, dim3(n), kPlanThreads, st, n);
+    }
     cudaError_t e = launch_chained(q4_plan_kernel<false>, a, dim3(1), kPlanThreads, st);
     if (e != cudaSuccess) return e;
     const long long jobs = a.n_rows + a.n_seqs;
     const int grid = (int)(jobs / kPlanFillThreads + 1 < 592 ? jobs / kPlanFillThreads + 1 : 592);
-    a.chained = chained;
     return launch_chained(q4_plan_fill_kernel, a, dim3(grid), kPlanFillThreads, st);
 }
 

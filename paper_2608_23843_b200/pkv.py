@@ -776,7 +776,7 @@ class Q4Cache:
                     tree.is_contiguous()):
                 self._fail("tree must be a contiguous int64 tensor %r on %s" % ([*q.shape[:-2], "words"], self.device))
             words = tree.shape[-1]
-        part = words > 0 or window or sinks or tree is not None
+        part = window or sinks or tree is not None
         if n == 0:
             return
         if not ragged:
@@ -800,14 +800,17 @@ class Q4Cache:
             self._workspaces[key] = size
         # (from the caching allocator at each call: ordered with this stream, and private to a graph that is being captured)
         work = torch.empty(size, dtype=torch.uint8, device=self.device) if size and not self.dry_run else None
-        rest = (q.data_ptr(), q_row, q_head, None if out is None else out.data_ptr(), o_row, o_head, None if state is None else state.data_ptr(),
-                None if work is None else work.data_ptr(), size, self._stream())
-        shape = (n_seqs, page_table.data_ptr(), max_pages, lengths.data_ptr(), n, offsets.data_ptr() if ragged else None, max_q_len, max_len)
         if part:
             sel = PkvQ4Select(window, sinks, None if tree is None else tree.data_ptr(), words)
-            self._call(lib().pkv_q4_attention_select, *shape, ctypes.byref(sel), *rest)
-        else:
-            self._call(lib().pkv_q4_attention, *shape, *rest)
+            self._call(lib().pkv_q4_attention_select, n_seqs, page_table.data_ptr(), max_pages, lengths.data_ptr(), n,
+                       offsets.data_ptr() if ragged else None, max_q_len, max_len, ctypes.byref(sel), q.data_ptr(), q_row, q_head,
+                       None if out is None else out.data_ptr(), o_row, o_head, None if state is None else state.data_ptr(),
+                       None if work is None else work.data_ptr(), size, self._stream())
+            return
+        self._call(lib().pkv_q4_attention, n_seqs, page_table.data_ptr(), max_pages, lengths.data_ptr(), n,
+                   offsets.data_ptr() if ragged else None, max_q_len, max_len, q.data_ptr(), q_row, q_head,
+                   None if out is None else out.data_ptr(), o_row, o_head, None if state is None else state.data_ptr(),
+                   None if work is None else work.data_ptr(), size, self._stream())
 
     def _ints(self, name, t, shape, dtype=_INT32):
         if not (t.shape == shape and t.dtype is dtype and t.get_device() == self._device_index and t.is_contiguous()):
@@ -839,7 +842,7 @@ class Q4Cache:
             self._fail("a window with sinks needs the sequences' lengths")
         words = max_q_len + 63 >> 6 if max_q_len > 0 else 1
         depths = torch.empty_like(parents)
-        masks = torch.empty((*shape, words), dtype=_INT64, device=self.device)
+        masks = torch.empty(*shape, words, dtype=_INT64, device=self.device)
         self._call(lib().pkv_q4_tree_masks, n_seqs, None if lengths is None else lengths.data_ptr(), n, None if offsets is None else offsets.data_ptr(),
                    max_q_len, parents.data_ptr(), window, sinks, masks.data_ptr(), words, depths.data_ptr(), self._stream())
         return masks, depths
