@@ -1112,7 +1112,8 @@ __global__ void __launch_bounds__(32 * kQ4JoinWarps) q4_join_kernel(const __grid
                 s1[i] = s[R * D + R + r];
 #pragma unroll
                 for (int c = 0; c < NV; ++c) {
-                    const float *src = s + r * D + (c * LR + l) * V;
+                    // (row after row; of a row block, four channels of all rows, then the next four: how the row threads store it side by side)
+                    const float *src = kRows == 1 ? s + r * D + (c * LR + l) * V : s + ((c * LR + l) * V / 4 * R + r) * 4 + (c * LR + l) * V % 4;
                     if (V == 4) { const float4 v = *reinterpret_cast<const float4 *>(src); x[i][4 * c] = v.x; x[i][4 * c + 1] = v.y; x[i][4 * c + V - 2] = v.z; x[i][4 * c + V - 1] = v.w; }
                     else { const float2 v = *reinterpret_cast<const float2 *>(src); x[i][2 * c] = v.x; x[i][2 * c + 1] = v.y; }
                 }

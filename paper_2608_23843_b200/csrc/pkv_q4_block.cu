@@ -309,7 +309,13 @@ __global__ void __launch_bounds__(kBThreads, 1) q4_block_kernel(const __grid_con
         for (int w = 0; w < kBThreads / 32; ++w) total += sums[w];
     }
     const int n_ctas = (int)min((long long)gridDim.x, max(1LL, total / (4 + kBSegCost)));
-    const long long begin = total * blockIdx.x / n_ctas, end = total * (blockIdx.x + 1) / n_ctas;
+    // (b * total / n without a 64-bit division where the total has 31 bits)
+    auto share = [&](long long b) -> long long {
+        if (!kSel || total >> 31) return total * b / n_ctas;
+        const unsigned q = (unsigned)total / (unsigned)n_ctas, r = (unsigned)total % (unsigned)n_ctas;
+        return (long long)q * b + r * (unsigned)b / (unsigned)n_ctas;
+    };
+    const long long begin = share(blockIdx.x), end = share(blockIdx.x + 1LL);
     Q4Part *parts = reinterpret_cast<Q4Part *>(a.workspace);
     float *states = reinterpret_cast<float *>(a.workspace + q4_parts_bytes(gridDim.x));
     if (blockIdx.x >= n_ctas || begin >= end) {
@@ -907,7 +913,7 @@ __global__ void __launch_bounds__(kBThreads, 1) q4_block_kernel(const __grid_con
                 f0 *= inv;
                 f1 *= inv;
                 float *dst = nullptr;
-                if (!complete) dst = states + (2LL * blockIdx.x + slot) * q4_state_floats(kBRows, D) + (long long)r_block * D;
+                if (!complete) dst = states + (2LL * blockIdx.x + slot) * q4_state_floats(kBRows, D) + r_block * 4;      // (four channels of all rows, then the next four)
                 else if (a.state && row_ok) dst = a.state + ((long long)(c.q.first + j) * geo.n_q_heads + h) * (D + 2);
                 unsigned short *out = reinterpret_cast<unsigned short *>(a.out) + (long long)(c.q.first + j) * a.out_row + (long long)h * a.out_head;
 #pragma unroll 1
@@ -929,10 +935,10 @@ __global__ void __launch_bounds__(kBThreads, 1) q4_block_kernel(const __grid_con
                     if (bad >> (b / WPG) & 1)                  // (a group is 32 channels or more)
 #pragma unroll
                         for (int k = 0; k < 32; ++k) r[k] = 0x7fc00000u;
-                    if (!complete) {                           // (16-byte aligned, unlike a row of the caller's states)
+                    if (!complete) {                           // (16-byte aligned, unlike a row of the caller's states; neighbours side by side)
 #pragma unroll
                         for (int k = 0; k < 8; ++k)
-                            *reinterpret_cast<uint4 *>(dst + 32 * b + 4 * k) =
+                            *reinterpret_cast<uint4 *>(dst + (8 * b + k) * (4 * kBRows)) =
                                 make_uint4(r[(4 * k & ~7) + kVOrder[4 * k & 7]], r[(4 * k & ~7) + kVOrder[(4 * k + 1) & 7]],
                                            r[(4 * k & ~7) + kVOrder[(4 * k + 2) & 7]], r[(4 * k & ~7) + kVOrder[(4 * k + 3) & 7]]);
                     } else if (dst) {
