@@ -644,6 +644,15 @@ pkv_status pkv_q4_attention_select(pkv_q4_cache *c, int32_t n_seqs, const int32_
                                    void *workspace, int64_t workspace_bytes, void *stream);
 
 /*
+ * How a call would be launched, for inspection and tests.  Host only: no GPU work.  select may be NULL: pkv_q4_attention().
+ *   *kernel   0: tiles of 8 or 16 query rows on all SMs, the batch's tokens shared evenly;  1: blocks of 256 query rows (tcgen05);
+ *             2: four small CTAs per SM, a segment (sequence, KV head, 8 query rows) to each or to a cluster of *cluster of them
+ *   *n_ctas   CTAs launched.  max_q_len, max_len: 1 or more each, as for the workspace
+ */
+pkv_status pkv_q4_attention_route(const pkv_q4_cache *c, int32_t n_seqs, int32_t max_q_len, int32_t max_len, const pkv_q4_select *select,
+                                  int32_t *kernel, int32_t *n_ctas, int32_t *cluster);
+
+/*
  * Masks of drafted tokens from the tree's edges, once per step for all layers.  parents [device] int32 [n_rows]: the row of the same
  * sequence (0 .. j - 1 for row j) that row j continues, -1 for the last token of the context; any other value counts as -1 and in
  * pkv_q4_stats.bad_lengths.  Written:

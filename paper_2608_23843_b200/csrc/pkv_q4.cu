@@ -585,6 +585,14 @@ pkv_status pkv_q4_attention_select_workspace(const pkv_q4_cache *c, int32_t n_se
     return PKV_OK;
 }
 
+pkv_status pkv_q4_attention_route(const pkv_q4_cache *c, int32_t n_seqs, int32_t max_q_len, int32_t max_len, const pkv_q4_select *select,
+                                  int32_t *kernel, int32_t *n_ctas, int32_t *cluster) {
+    if (!c || !kernel || !n_ctas || !cluster || n_seqs < 1 || n_seqs > 65535 || max_q_len < 1 || max_len < 1) return PKV_ERR_INVALID_ARG;
+    if (select && q4_select_error(*select, max_q_len)) return PKV_ERR_INVALID_ARG;
+    q4_attention_route(c->geo, n_seqs, max_q_len, max_len, select ? q4_selection(*select) : Q4Select{}, kernel, n_ctas, cluster);
+    return PKV_OK;
+}
+
 pkv_status pkv_q4_attention_select(pkv_q4_cache *c, int32_t n_seqs, const int32_t *page_table, int32_t max_pages, const int32_t *lengths,
                                    int64_t n_rows, const int32_t *offsets, int32_t max_q_len, int32_t max_len, const pkv_q4_select *select,
                                    const void *q, int64_t q_row_stride, int64_t q_head_stride, void *out, int64_t out_row_stride,

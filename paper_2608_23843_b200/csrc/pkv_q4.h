@@ -133,6 +133,7 @@ cudaError_t q4_block_setup();
 int q4_block_grid(const Q4Geometry &g, int n_seqs, int max_q_len, int max_len, const Q4Select &sel);
 cudaError_t launch_q4_block(const Q4AttentionArgs &a, int n, cudaStream_t st);
 long long q4_attention_workspace(const Q4Geometry &g, int n_seqs, int max_q_len, int max_len, const Q4Select &sel);
+void q4_attention_route(const Q4Geometry &g, int n_seqs, int max_q_len, int max_len, const Q4Select &sel, int *kernel, int *n_ctas, int *cluster);
 
 // byte offsets inside a tile
 __host__ __device__ constexpr int q4_v_base(int d) { return kQ4Tile * d / 2; }

@@ -28,8 +28,6 @@
 
 #include <algorithm>
 #include <cmath>
-#include <cstdio>
-#include <cstdlib>
 #include <type_traits>
 
 #include "pkv_q4_device.cuh"
@@ -1256,10 +1254,6 @@ Q4Route q4_route(const Q4Geometry &g, int n_seqs, int max_q_len, int max_len, co
         const double by_blocks = (rows <= 128 ? 20 : g.head_dim == 128 ? 33 : 25) + blocks * (units + 4) * per / g.n_sms;
         r.small = small <= split && small <= by_blocks;
         r.blocks = !r.small && by_blocks < split;
-#ifdef PKV_ROUTE_TEST
-        if (const char *e = getenv("PKV_ROUTE")) { r.small = e[0] == 's'; r.blocks = e[0] == 'b'; if (r.small && e[1]) while (c > e[1] - '0') c /= 2; }
-        if (getenv("PKV_ROUTE_SHOW")) fprintf(stderr, "small %.1f (c %d) split %.1f blocks %.1f\n", small, c, split, by_blocks);
-#endif
         if (r.small) {
             r.whole = 1;
             r.cluster = c;
@@ -1277,6 +1271,13 @@ Q4Route q4_route(const Q4Geometry &g, int n_seqs, int max_q_len, int max_len, co
 long long q4_attention_workspace(const Q4Geometry &g, int n_seqs, int max_q_len, int max_len, const Q4Select &sel) {
     const Q4Route r = q4_route(g, n_seqs, max_q_len, max_len, sel);
     return r.n <= 1 || r.whole ? 0 : q4_parts_bytes(r.n) + 2LL * r.n * q4_state_floats(r.R, g.head_dim) * 4;
+}
+
+void q4_attention_route(const Q4Geometry &g, int n_seqs, int max_q_len, int max_len, const Q4Select &sel, int *kernel, int *n_ctas, int *cluster) {
+    const Q4Route r = q4_route(g, n_seqs, max_q_len, max_len, sel);
+    *kernel = r.small ? 2 : r.blocks ? 1 : 0;
+    *n_ctas = r.n;
+    *cluster = r.cluster;
 }
 
 cudaError_t launch_q4_attention(Q4AttentionArgs a, cudaStream_t st) {

@@ -36,7 +36,7 @@ EXPORTS = [
     "pkv_q4_query_sizes", "pkv_q4_init_cache", "pkv_q4_destroy_cache", "pkv_q4_last_error", "pkv_q4_get_stats",
     "pkv_q4_append_kv", "pkv_q4_read_kv", "pkv_q4_attention_workspace", "pkv_q4_attention",
     "pkv_q4_attention_select_workspace", "pkv_q4_attention_select", "pkv_q4_tree_masks", "pkv_q4_keep_rows",
-    "pkv_q4_plan_workspace", "pkv_q4_plan",
+    "pkv_q4_plan_workspace", "pkv_q4_plan", "pkv_q4_attention_route",
 ]
 
 
@@ -146,6 +146,7 @@ def lib():
         sel = ctypes.POINTER(PkvQ4Select)
         L.pkv_q4_attention_select_workspace.argtypes = [vp, i32, i32, i32, sel, ctypes.POINTER(i64)]
         L.pkv_q4_attention_select.argtypes = [vp, i32, vp, i32, vp, i64, vp, i32, i32, sel, vp, i64, i64, vp, i64, i64, vp, vp, i64, vp]
+        L.pkv_q4_attention_route.argtypes = [vp, i32, i32, i32, sel, ip, ip, ip]
         L.pkv_q4_tree_masks.argtypes = [vp, i32, vp, i64, vp, i32, vp, i32, i32, vp, i32, vp, vp]
         L.pkv_q4_keep_rows.argtypes = [vp, i32, vp, i32, vp, i64, vp, vp, i32, vp, vp, vp]
         L.pkv_q4_plan_workspace.argtypes = [vp, i32, i64, ctypes.POINTER(i64)]
@@ -452,6 +453,16 @@ def pkv_q4_attention_select(handle, n_seqs, page_table, max_pages, lengths, n_ro
     _q4_check(handle, lib().pkv_q4_attention_select(handle, n_seqs, _ptr(page_table), max_pages, _ptr(lengths), n_rows, _ptr(offsets), max_q_len,
                                                     max_len, ctypes.byref(sel), _ptr(q), *q_strides, _ptr(out), *out_strides, _ptr(state),
                                                     _ptr(workspace), workspace_bytes, _stream(stream)))
+
+
+def pkv_q4_attention_route(handle, n_seqs, max_q_len, max_len, window=0, sinks=0, tree=None, tree_words=0):
+    """-> (kernel, n_ctas, cluster), see include/pkv.h; tree as for pkv_q4_attention_select_workspace()."""
+    out = [ctypes.c_int32(0) for _ in range(3)]
+    sel = PkvQ4Select(window, sinks, None if tree is None else 8, tree_words)
+    st = lib().pkv_q4_attention_route(handle, n_seqs, max_q_len, max_len, ctypes.byref(sel), *(ctypes.byref(x) for x in out))
+    if st != PKV_OK:
+        raise PkvError(st, "pkv_q4_attention_route(%r, %r, %r, window %r, sinks %r)" % (n_seqs, max_q_len, max_len, window, sinks))
+    return tuple(x.value for x in out)
 
 
 def pkv_q4_tree_masks(handle, n_seqs, lengths, n_rows, offsets, max_q_len, parents, window, sinks, tree, tree_words, depths, stream=None):
@@ -777,6 +788,8 @@ class Q4Cache:
                 self._fail("tree must be a contiguous int64 tensor %r on %s" % ([*q.shape[:-2], "words"], self.device))
             words = tree.shape[-1]
         part = window or sinks or tree is not None
+        if part:
+            self._positions(window, sinks)
         if n == 0:
             return
         if not ragged:
@@ -812,6 +825,10 @@ class Q4Cache:
                    None if out is None else out.data_ptr(), o_row, o_head, None if state is None else state.data_ptr(),
                    None if work is None else work.data_ptr(), size, self._stream())
 
+    def _positions(self, window, sinks):
+        if not (0 <= window < 1 << 31 and 0 <= sinks < 1 << 31):      # (beyond 32 bits they would arrive as other numbers)
+            self._fail("window and sinks must be from 0 to 2^31 - 1")
+
     def _ints(self, name, t, shape, dtype=_INT32):
         if not (t.shape == shape and t.dtype is dtype and t.get_device() == self._device_index and t.is_contiguous()):
             self._fail("%s must be a contiguous %s tensor %r on %s" % (name, str(dtype)[6:], list(shape), self.device))
@@ -821,6 +838,7 @@ class Q4Cache:
         earlier one, that a row continues, -1 for the last token of the context.  -> (int64 parents.shape + (words,), for attention(tree=...),
         int32 depths of parents' shape: a row's position is the context's length + its depth).  With a window and sinks, those of the attention call and the
         sequences' lengths (the rows included).  With offsets, max_q_len bounds the rows of a sequence (default: all rows)."""
+        self._positions(window, sinks)
         shape, n, dev = parents.shape, parents.numel(), self._device_index
         if offsets is None:
             if len(shape) != 2:
@@ -882,6 +900,7 @@ class Q4Cache:
         in all.  Writes new entries into page_table and returned pages into ring.  -> Q4Plan of new tensors, or `out`, whose
         lengths, spans and counters may be the ones given (in place).  Where pages are missing or requests make no sense nothing is done: counters[2:]."""
         n_seqs, max_pages = self._seqs(page_table, lengths, None)
+        self._positions(window, sinks)
         dev, one = self._device_index, (n_seqs,)
         if not (rows.dtype is spans.dtype is ring.dtype is _INT32 and counters.dtype is _INT64 and rows.shape == one and spans.shape == (n_seqs, 2) and
                 ring.shape == (self.cfg.n_pages,) and counters.shape == (4,) and

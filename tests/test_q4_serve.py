@@ -56,6 +56,10 @@ def _ring():
     lambda c, t, n, q: c.attention(t, n, q, window=-1),
     lambda c, t, n, q: c.attention(t, n, q, sinks=4),                          # sinks without a window
     lambda c, t, n, q: c.attention(t, n, q, window=4, sinks=-1),
+    lambda c, t, n, q: c.attention(t, n, q, window=2 ** 31),
+    lambda c, t, n, q: c.attention(t, n, q, window=2 ** 32 + 4),                # would arrive as 4
+    lambda c, t, n, q: c.tree_masks(torch.zeros(3, 2, **INTS), n, window=2 ** 32 + 4),
+    lambda c, t, n, q: c.plan(t, n, n, _spans(), *_ring(), 4, window=4, sinks=2 ** 32),
     lambda c, t, n, q: c.attention(t, n, q, tree=torch.zeros(3, 2, 1, **INTS)),
     lambda c, t, n, q: c.attention(t, n, q, tree=torch.zeros(3, 2, **LONGS)),
     lambda c, t, n, q: c.attention(t, n, q, tree=torch.zeros(3, 3, 1, **LONGS)),
@@ -125,6 +129,47 @@ def test_refusals_of_the_c_entry_points():
         assert plan(**k) == bad, k
     assert L.pkv_q4_plan_workspace(h, 3, 6, None) == bad and L.pkv_q4_plan_workspace(h, 0, 6, ctypes.byref(size)) == bad
     assert pkv.pkv_q4_plan_workspace(h, 3, 6) == 0 and pkv.pkv_q4_plan_workspace(h, 3, 1 << 20) > 0 and pkv.pkv_q4_plan_workspace(h, 5000, 6) > 0
+
+
+# What serves which call: kernel (0: even shares, 1: row blocks, 2: small CTAs), CTAs of a cluster.  (n_ctas leaves the row blocks alone: few of the
+# others make them the choice for short sequences too.)
+ROUTES = [
+    ("small, one CTA to a segment", dict(H=2, G=4, n_ctas=20), 20, 1, 300, dict(window=200, sinks=5), 2, 1),
+    ("small, segments in turn", dict(H=2, G=4), 320, 1, 300, dict(window=200, sinks=5), 2, 1),
+    ("small, clusters of 2", dict(H=2, G=4, n_ctas=20), 8, 1, 700, dict(window=300, sinks=5), 2, 2),
+    ("small, clusters of 4", dict(H=2, G=4, n_ctas=50), 8, 2, 1000, dict(window=700, sinks=5), 2, 4),
+    ("small, clusters of 8", dict(H=2, G=4), 3, 5, 1500, dict(window=1400), 2, 8),
+    ("small, a tree", dict(H=1, G=7), 2, 7, 1500, dict(tree=True), 2, 8),
+    ("small, a tree and a window", dict(H=2, G=3), 2, 12, 2000, dict(tree=True, window=900, sinks=70), 2, 8),
+    ("even shares, 8 rows", dict(H=1, G=4), 1, 1, 20000, dict(window=18000, sinks=100), 0, 1),
+    ("even shares, 8 rows, a tree", dict(H=2, G=2), 1, 4, 30000, dict(tree=True), 0, 1),
+    ("even shares, 16 rows", dict(H=2, G=4), 4, 4, 20000, dict(tree=True, window=19000, sinks=3), 0, 1),
+    ("even shares, two tiles", dict(H=2, G=4), 4, 6, 20000, dict(window=19500), 0, 1),
+    ("row blocks, halves in turn", dict(H=2, G=4, n_ctas=10), 4, 30, 2000, dict(tree=True), 1, 1),
+    ("row blocks, halves in turn, a window", dict(H=3, G=3, n_ctas=10), 5, 40, 2500, dict(window=1100, sinks=20), 1, 1),
+    ("row blocks, both halves", dict(H=2, G=4, n_ctas=10), 5, 50, 1500, dict(tree=True, window=700, sinks=9), 1, 1),
+    ("row blocks, several", dict(H=2, G=8, n_ctas=10), 5, 100, 1200, dict(window=333, sinks=65), 1, 1),
+    ("row blocks, more than eight", dict(H=1, G=16, n_ctas=10), 2, 150, 700, dict(window=64, sinks=1), 1, 1),
+    ("row blocks, a tree over several", dict(H=1, G=8, n_ctas=10), 6, 90, 900, dict(tree=True), 1, 1),
+]
+
+
+def _route(cache, S, n, most, kw):
+    return pkv.pkv_q4_attention_route(cache.handle, S, n, most, kw.get("window", 0), kw.get("sinks", 0), kw.get("tree"), -(-n // 64))
+
+
+@pytest.mark.parametrize("name, shape, S, n, T, kw, kernel, cluster", ROUTES, ids=[r[0] for r in ROUTES])
+def test_which_kernel_serves_a_call(name, shape, S, n, T, kw, kernel, cluster):
+    H, G = shape["H"], shape["G"]
+    cache = pkv.Q4Cache(config(n_kv_heads=H, n_q_heads=H * G, n_ctas=shape.get("n_ctas", 0)), dry_run=True)
+    got = _route(cache, S, n, -(-T // 64) * 64, kw)
+    assert (got[0], got[2]) == (kernel, cluster), got
+    if name == "small, segments in turn":
+        assert got[1] < S * H
+    assert pkv.pkv_q4_attention_route(cache.handle, 1, 1, 64)[0] == 0
+    for bad in ((0, 1, 64), (1, 0, 64), (1, 1, 0)):
+        with pytest.raises(pkv.PkvError):
+            pkv.pkv_q4_attention_route(cache.handle, *bad)
 
 
 def test_the_references_agree_with_one_another():
@@ -294,6 +339,55 @@ def test_windows_over_values_of_very_different_sizes(n, G, dtype):
     out = f.cache.attention(f.table, f.lengths, torch.stack(qs).cuda(), window=W, sinks=S)
     for s, q in enumerate(qs):
         check(out[s], *seen_by(f, q, s, window_seen(f.lens[s], n, W, S))[::2])
+
+
+FORMATS = [dict(dtype=BF16, d=128, g=32, P=64), dict(dtype=FP16, d=64, g=64, P=16), dict(dtype=FP16, d=128, g=128, P=32), dict(dtype=BF16, d=64, g=32, P=64),
+           dict(dtype=BF16, d=128, g=64, P=128)]
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("form", range(len(FORMATS)))
+@pytest.mark.parametrize("name, shape, S, n, T, kw, kernel, cluster", ROUTES, ids=[r[0] for r in ROUTES])
+def test_every_kernel(name, shape, S, n, T, kw, kernel, cluster, form):
+    """Ragged lengths and rows on each kernel, what is not seen being anything: pages gone back, keys and values infinite and NaN.
+    (d = 64 and other formats may be served by another kernel than the one named, as the rule sees fit.)"""
+    rng = random.Random(S * n + form)
+    lens = [T] + [rng.choice([n, n + 1, rng.randint(n, T), rng.randint(n, T)]) for _ in range(S - 1)]
+    ns = [n] + [rng.choice([0, 1, n, rng.randint(0, n)]) for _ in range(S - 1)]
+    f = Filled(lens, seed=form, room=T, **shape, **FORMATS[form])
+    W, sinks, tree = kw.get("window", 0), kw.get("sinks", 0), kw.get("tree", False)
+    if form == 0:
+        assert _route(f.cache, S, n, f.table.shape[1] * FORMATS[form]["P"], kw)[::2] == (kernel, cluster)
+    table = without_hidden_pages(f, FORMATS[form]["P"], ns, W, sinks) if W else f.table
+    if W:
+        k, v = [x.clone() for x in f.k], [x.clone() for x in f.v]
+        for s, (T_s, n_s) in enumerate(zip(lens, ns)):
+            low = max(0, T_s - n_s + 1 - W)
+            k[s][sinks:low:3] *= 2.0 ** 5
+            k[s][sinks + 1:low:7] = math.nan
+            v[s][sinks:low:5] = math.inf
+        f.cache.append_kv(f.table, f.lengths, torch.cat(k).cuda(), torch.cat(v).cuda(), f.off)
+    qs = f.queries(ns)
+    off = offsets_of(ns, start=1).cuda()
+    pad = torch.zeros(1, f.H * f.G, f.d, dtype=f.dtype)
+    q = torch.cat([pad, *qs, pad]).cuda()
+    parents = [random_parents(rng, x, 6) for x in ns]
+    masks = f.cache.tree_masks(torch.tensor([0] + sum(parents, []) + [0], **INTS).cuda(), f.lengths, off, n, W, sinks)[0] if tree else None
+    out = torch.full_like(q, 5.0)
+    f.cache.attention(table, f.lengths, q, out=out, offsets=off, max_q_len=n, window=W, sinks=sinks, tree=masks)
+    state = f.cache.attention_partial(table, f.lengths, q, offsets=off, max_q_len=n, window=W, sinks=sinks, tree=masks)
+    assert (out[0] == 5).all() and (out[-1] == 5).all()
+    out, state, at = out.cpu(), state.to("cpu", torch.float64), 1
+    for s, (n_s, T_s) in enumerate(zip(ns, lens)):
+        if n_s:
+            see = tree_seen(T_s, tree_bits(parents[s], T_s - n_s, W, sinks)[0], W, sinks) if tree else window_seen(T_s, n_s, W, sinks)
+            ref, lse, tol = seen_by(f, qs[s], s, see)
+            check(out[at:at + n_s], ref, tol)
+            st = state[at:at + n_s]
+            check(st[..., :f.d] / st[..., f.d + 1:], ref, tol)
+            assert (st[..., f.d] + torch.log2(st[..., f.d + 1]) - lse).abs().max() < 2.0 ** -12      # (as for the causal states)
+        at += n_s
+    f.clean()
 
 
 @pytest.mark.gpu
@@ -973,3 +1067,13 @@ def test_random_selections(seed):
                 check(out[at:at + n], *seen_by(f, qs[s], s, see)[::2])
             at += n
         f.clean()
+
+
+@pytest.mark.gpu
+def test_in_a_process_without_caches_that_overlap():
+    """Kernels are launched differently there (other test files make a page cache whose decodes do not wait): this file's tests by themselves."""
+    import subprocess
+    import sys
+    r = subprocess.run([sys.executable, "-m", "pytest", "-q", "-x", "-m", "gpu", "-k", "not in_a_process", "-p", "no:cacheprovider", __file__],
+                       capture_output=True, text=True, timeout=900)
+    assert r.returncode == 0, r.stdout[-3000:]
