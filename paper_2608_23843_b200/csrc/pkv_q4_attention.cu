@@ -1249,8 +1249,8 @@ Q4Route q4_route(const Q4Geometry &g, int n_seqs, int max_q_len, int max_len, co
         const double tiles = heads * std::ceil(rows / 16), blocks = heads * std::ceil(rows / kQ4BlockRows), share = 296. / g.n_ctas;
         const double split = rows <= 8 ? std::max(17 + segs * units * 1.3e-3 * share, 10 + segs * (units + 31) * 2.05e-3 * share)
                                        : std::max(24.5, 17.6 + tiles * (units + 15) * 2.95e-3 * share);
-        // row blocks (8 requests, 64 rows x 4 heads against 32K: 355 us and 1540 by even shares; 8 rows x 4 heads against 16K: 161 us and 116)
-        const double per = (g.head_dim == 128 ? 1. : 0.7) * (rows <= 128 ? 1.24 : 1.49);
+        // row blocks (8 requests, 64 rows x 4 heads against 32K: 355 us and 1540 by even shares; 16 rows x 4 heads against 16K: 140 us and about 230)
+        const double per = (g.head_dim == 128 ? 1. : 0.7) * (rows <= 128 ? 1.06 : 1.49);
         const double by_blocks = (rows <= 128 ? 20 : g.head_dim == 128 ? 33 : 25) + blocks * (units + 4) * per / g.n_sms;
         r.small = small <= split && small <= by_blocks;
         r.blocks = !r.small && by_blocks < split;

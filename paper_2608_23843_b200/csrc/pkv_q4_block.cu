@@ -31,6 +31,7 @@
 #include <cuda_fp16.h>
 
 #include <algorithm>
+#include <type_traits>
 
 #include "pkv_q4_device.cuh"
 #include "pkv_umma.cuh"
@@ -40,7 +41,16 @@ namespace pkv {
 namespace {
 
 constexpr int kBRows = kQ4BlockRows, kBHalf = 128;
-constexpr int kBThreads = 448, kBRowWarps = 8, kBWidenWarps = kQ4UnitTiles, kBIssueWarp = 12, kBCopyWarp = 13;
+constexpr int kBRowWarps = 8;
+// kPairs: where a call's blocks have 128 rows at most, and queries see a part of the positions, keys and values of a tile are widened by a warp
+// each: both halves then have the same rows and every other unit, and the widening is what takes longest (8 x 16 drafted tokens against 16000: 162 ->
+// 140 us; with rows of their own for both halves the row threads need the issue slots: 8 x 64 against 32K 356 -> 370).  The 18 warps take
+// registers by their needs, in whole groups of four warps (two idle ones make up the last): they start with 96 a thread.
+__host__ __device__ constexpr int block_widen_warps(bool pairs) { return pairs ? 2 * kQ4UnitTiles : kQ4UnitTiles; }
+__host__ __device__ constexpr int block_threads(bool pairs) { return 32 * (kBRowWarps + block_widen_warps(pairs) + (pairs ? 4 : 2)); }
+constexpr int kBRegs = 96, kBRowRegs = 144, kBWidenRegs = 64, kBOtherRegs = 64;
+static_assert(block_threads(true) * kBRegs <= 65536 && 256 * kBRowRegs + 256 * kBWidenRegs + 128 * kBOtherRegs <= block_threads(true) * kBRegs,
+              "more would be waited for in vain");
 constexpr uint32_t kBTmemCols = 512;
 
 template <int D, int NG>
@@ -204,6 +214,7 @@ struct __align__(16) UnitInfo {
     float tv[kQ4Unit];                              // exponents of each token's values, in uneven tiles and where they spread
     float ek[kQ4UnitTiles];                         // ... of the other tiles' keys (uneven: 1)
     float ev[kQ4UnitTiles], ev_inv[kQ4UnitTiles];   // ... and values: exponents, and 2^-exponent (uneven: 0, 0)
+    uint8_t odd_keys[kQ4UnitTiles];                 // kPairs: the first of these, by the warp that has the keys
     uint8_t odd[kQ4UnitTiles];                      // 1: uneven keys, 2: uneven values, 4: values that are not finite, 8: values that spread
     uint16_t v_nan[kQ4UnitTiles][4];                // per channel group: tokens whose values are not finite there (zeros here)
     uint32_t tiles, tokens;                         // which tiles are there; tokens of the sequence in the unit
@@ -239,10 +250,11 @@ __device__ __forceinline__ uint64_t f2_fma3(uint64_t a, uint64_t b, uint64_t c) 
 __device__ __forceinline__ float pow2(int e) { return __uint_as_float((uint32_t)(e + 127) << 23); }      // -126 <= e <= 127
 
 // kSel: the queries see a part of the positions
-template <int D, int NG, bool H16, bool kSel>
-__global__ void __launch_bounds__(kBThreads, 1) q4_block_kernel(const __grid_constant__ Q4AttentionArgs a) {
+template <int D, int NG, bool H16, bool kSel, bool kPairs>
+__global__ void __launch_bounds__(block_threads(kPairs), 1) q4_block_kernel(const __grid_constant__ Q4AttentionArgs a) {
     using S = BlockShape<D, NG>;
     constexpr int NW = D / 32, WPG = NW / NG, kWS = S::kWideStages, kCS = S::kCodeStages;
+    constexpr int kBThreads = block_threads(kPairs), kWiden = block_widen_warps(kPairs), kBIssueWarp = kBRowWarps + kWiden, kBCopyWarp = kBIssueWarp + 1;
     const Q4Geometry &geo = a.geo;
     extern __shared__ unsigned char smem_raw[];
     unsigned char *wide = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u), *codes = wide + kWS * S::kWide;
@@ -258,8 +270,8 @@ __global__ void __launch_bounds__(kBThreads, 1) q4_block_kernel(const __grid_con
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     volatile int *abort_flag = &gave_up;
     if (tid == 0) {
-        for (int s = 0; s < kCS; ++s) { mbar_init(smem_u32(&code_full[s]), 1); mbar_init(smem_u32(&code_empty[s]), kQ4UnitTiles); }
-        for (int s = 0; s < kWS; ++s) { mbar_init(smem_u32(&wide_full[s]), kQ4UnitTiles); mbar_init(smem_u32(&wide_empty[s]), 1); }
+        for (int s = 0; s < kCS; ++s) { mbar_init(smem_u32(&code_full[s]), 1); mbar_init(smem_u32(&code_empty[s]), kWiden); }
+        for (int s = 0; s < kWS; ++s) { mbar_init(smem_u32(&wide_full[s]), kWiden); mbar_init(smem_u32(&wide_empty[s]), 1); }
         for (int x = 0; x < 2; ++x) {
             mbar_init(smem_u32(&s_full[x]), 1); mbar_init(smem_u32(&p_ready[x]), kBHalf);
             mbar_init(smem_u32(&q_ready[x]), kBHalf); mbar_init(smem_u32(&o_done[x]), 1);
@@ -401,6 +413,7 @@ __global__ void __launch_bounds__(kBThreads, 1) q4_block_kernel(const __grid_con
     const uint32_t tm = tmem_slot;
     const long long limit = kWaitClocks;
 
+    if (kPairs && warp >= kBIssueWarp) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kBOtherRegs));
     if (warp == kBCopyWarp) {
         // ---------------- copies: 32 units are looked up at a time, a lane each, and issued in turn ----------------
         const int per_page = min(kQ4Unit, geo.page), n_parts = kQ4Unit / per_page, per_tiles = per_page / kQ4Tile;
@@ -455,7 +468,120 @@ __global__ void __launch_bounds__(kBThreads, 1) q4_block_kernel(const __grid_con
         if (!ok && lane == 0 && !*abort_flag) { *abort_flag = 1; atomicAdd(a.status, 1); }
         // copies in flight must land before the CTA retires: wait (bounded) for the stages armed last
         for (int back = 1; back <= min(u, kCS); ++back) (void)mbar_wait(smem_u32(&code_full[(u - back) % kCS]), ((u - back) / kCS) & 1, limit);
-    } else if (warp >= kBRowWarps && warp < kBRowWarps + kBWidenWarps) {
+    } else if (kPairs && warp >= kBRowWarps && warp < kBRowWarps + kWiden) {
+        // ---------------- codes times scales as fp16, a side of a tile per warp (as below, where a warp sees to both) ----------------
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kBWidenRegs));
+        const int c = lane & 3, i8 = lane >> 2, t_lane = (i8 >> 1) ^ (i8 & 1 ? 5 : 0), dw = (warp - kBRowWarps) % kQ4UnitTiles;
+        constexpr uint32_t kNext = q4_k_chunk(D, 8, 0);
+        const uint32_t d_row = smem_u32(wide) + (dw * kQ4Tile + t_lane) * 128, d_at[2] = {d_row + ((c ^ (t_lane & 7)) << 4), d_row + (((4 + c) ^ (t_lane & 7)) << 4)};
+        auto widen = [&](auto side) {
+            constexpr bool kV = decltype(side)::value;
+            constexpr uint32_t kScales = kV ? q4_vs_base(D, NG) : q4_ks_base(D), kFar = kV ? kBValues : kBKeys;
+            const uint32_t a_at = kV ? q4_v_base(D) + q4_v_chunk(D, t_lane, 2 * c) : q4_k_chunk(D, t_lane, c), b_at = q4_v_base(D) + q4_v_chunk(D, t_lane, 2 * c + 1);
+            bool ok = true;
+            int cs = 0, cu = 0;
+            for (int u = 0; u < left; ++u) {
+                const int ws = u % kWS, wu = u / kWS;
+                if (!mbar_wait_warp(smem_u32(&code_full[cs]), cu & 1, abort_flag)) { ok = false; break; }
+                const uint32_t bits = code_tiles[cs], tokens = code_tokens[cs];
+                const int valid = (bits >> dw) & 1 ? min(max((int)tokens - dw * kQ4Tile, 0), kQ4Tile) : 0;
+                const uint32_t tp = smem_u32(codes) + cs * S::kCodes + dw * S::kTile;
+                uint32_t z2[(NG + 1) / 2], sc[2][(NG + 1) / 2], x0[2][kV ? (NW + 1) / 2 : NW], x1[2][(NW + 1) / 2];
+                lds_scales<NG>(z2, tp + kScales + (lane & 15) * 2 * NG);
+#pragma unroll
+                for (int half = 0; half < 2; ++half) {
+                    lds_scales<NG>(sc[half], tp + kScales + (t_lane + 8 * half) * 2 * NG);
+                    if (!kV) {
+                        if (NW == 4) lds128(x0[half], tp + a_at + half * kNext);
+                        else lds64(x0[half], tp + a_at + half * kNext);
+                    } else if (NW == 4) {
+                        lds64(x0[half], tp + a_at + half * kNext);
+                        lds64(x1[half], tp + b_at + half * kNext);
+                    } else {
+                        lds32(x0[half], tp + a_at + half * kNext);
+                        lds32(x1[half], tp + b_at + half * kNext);
+                    }
+                }
+                // (lanes l and l + 16 have the same token)
+                uint32_t z = z2[0], nans[NG] = {};
+                if (NG == 4) z = __vmaxu2(z, z2[(NG - 1) / 2]);
+                z = max(z & 0xffffu, z >> 16);
+                const bool there = (lane & 15) < valid;
+                if (!there) z = 0u;
+                bool plain = valid == kQ4Tile;
+                if (__any_sync(0xffffffffu, z > 0x7f80u)) {
+                    const bool some = z != 0u;
+                    plain = false;
+                    z = 0u;
+#pragma unroll
+                    for (int k = 0; k < NG; ++k) {
+                        const uint32_t x = some ? (z2[k / 2] >> (16 * (k & 1))) & 0xffffu : 0u;
+                        nans[k] = __ballot_sync(0xffffffffu, x > 0x7f80u) & 0xffffu;
+                        if (x <= 0x7f80u) z = max(z, x);
+                    }
+                }
+                const uint32_t own = z >> 7, most = __reduce_max_sync(0xffffffffu, own);
+                const bool uneven = __any_sync(0xffffffffu, there && (kV ? own + kFar < most || most == 0u : z != 0u && own + kFar < most));
+                const bool spread = kV && __any_sync(0xffffffffu, there && own + kBSpread < most);
+                const int top = 127 + kBTop, e = min(max((int)own - top, kBLeast), 100), e1 = min(max((int)most - top, kBLeast), 100);
+                float f[2];
+                f[0] = f[1] = pow2(-e1);
+                if (uneven)
+#pragma unroll
+                    for (int half = 0; half < 2; ++half) f[half] = pow2(-__shfl_sync(0xffffffffu, e, t_lane + 8 * half));
+                if (wu > 0 && !mbar_wait_warp(smem_u32(&wide_empty[ws]), (wu - 1) & 1, abort_flag)) { ok = false; break; }
+                UnitInfo &inf = info[ws];
+                if (lane < 16 && (uneven || spread)) (kV ? inf.tv : inf.tk)[dw * kQ4Tile + lane] = kV ? (float)e : pow2(e);
+                if (lane == 0) {
+                    if (kV) {
+                        uint32_t any = 0;
+#pragma unroll
+                        for (int k = 0; k < NG; ++k) {
+                            any |= nans[k];
+                            inf.v_nan[dw][k] = (uint16_t)nans[k];
+                        }
+                        inf.ev[dw] = uneven ? 0.f : (float)e1;
+                        inf.ev_inv[dw] = uneven ? 0.f : pow2(-e1);
+                        inf.odd[dw] = (uint8_t)((uneven ? 2 : 0) | (any ? 4 : 0) | (spread ? 8 : 0));
+                    } else {
+                        inf.ek[dw] = uneven ? 1.f : pow2(e1);
+                        inf.odd_keys[dw] = uneven ? 1 : 0;
+                        if (dw == 0) { inf.tiles = bits; inf.tokens = tokens; }
+                    }
+                }
+                const uint32_t d0 = d_at[0] + ws * S::kWide + (kV ? S::kSide : 0), d1 = d_at[1] + ws * S::kWide + (kV ? S::kSide : 0);
+#pragma unroll
+                for (int half = 0; half < 2; ++half) {
+                    uint32_t s2[NG];
+#pragma unroll
+                    for (int k = 0; k < NG; ++k) {
+                        float y = (k & 1 ? bf16hi_f(sc[half][k / 2]) : bf16lo_f(sc[half][k / 2])) * f[half];
+                        if (!plain) {
+                            if (t_lane + 8 * half >= valid) y = 0.f;
+                            if (kV && y != y) y = 0.f;
+                        }
+                        s2[k] = pack_f16(y, y);
+                    }
+#pragma unroll
+                    for (int w = 0; w < NW; ++w) {
+                        const uint32_t x = kV ? __byte_perm(x0[half][w / 2], x1[half][w / 2], w & 1 ? 0x7632u : 0x5410u) : x0[half][kV ? 0 : w], x8 = x >> 8, m = s2[w / WPG];
+                        sts128((w & 1 ? d1 : d0) + (w >> 1) * (kQ4Unit * 128) + half * 1024, h2_mul(codes_lo(x), m), h2_mul(codes_hi(x), m),
+                               h2_mul(codes_lo(x8), m), h2_mul(codes_hi(x8), m));
+                    }
+                }
+                fence_async_smem();
+                __syncwarp();
+                if (lane == 0) {
+                    mbar_arrive(smem_u32(&wide_full[ws]));
+                    mbar_arrive(smem_u32(&code_empty[cs]));
+                }
+                if (++cs == kCS) { cs = 0; ++cu; }
+            }
+            if (!ok && lane == 0 && !*abort_flag) { *abort_flag = 1; atomicAdd(a.status, 1); }
+        };
+        if (warp < kBRowWarps + kQ4UnitTiles) widen(std::false_type());
+        else widen(std::true_type());
+    } else if (!kPairs && warp >= kBRowWarps && warp < kBRowWarps + kWiden) {
         // ---------------- codes times scales as fp16: a tile of 16 tokens per warp, keys or values ----------------
         const int c = lane & 3, i8 = lane >> 2;
         const int t_lane = (i8 >> 1) ^ (i8 & 1 ? 5 : 0);       // tokens t and t ^ 5 side by side: different halves of a line of codes, different banks of a line of fp16
@@ -643,6 +769,7 @@ __global__ void __launch_bounds__(kBThreads, 1) q4_block_kernel(const __grid_con
         }
     } else if (warp < kBRowWarps) {
         // ---------------- rows: one query row per thread ----------------
+        if (kPairs) asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kBRowRegs));
         const int x = warp >> 2, r_half = (warp & 3) * 32 + lane;
         const uint32_t t_lane = tm + ((uint32_t)((warp & 3) * 32) << 16);
         const uint32_t t_o = t_lane + S::kColO + x * D, t_s = t_lane + S::kColS + x * kQ4Unit;
@@ -715,7 +842,7 @@ __global__ void __launch_bounds__(kBThreads, 1) q4_block_kernel(const __grid_con
                     if (!mbar_wait_warp(smem_u32(&wide_full[ws]), ((u + i) / kWS) & 1, abort_flag)) { ok = false; break; }
                     const UnitInfo &inf = info[ws];
                     const int t0 = block_unit_at<kSel>(c, c.unit + i) * kQ4Unit, lim = kSel ? 0 : min(vis - t0, (int)inf.tokens);
-                    const uint32_t tiles = inf.tiles, odd = *reinterpret_cast<const uint32_t *>(inf.odd);
+                    const uint32_t tiles = inf.tiles, odd = *reinterpret_cast<const uint32_t *>(inf.odd) | (kPairs ? *reinterpret_cast<const uint32_t *>(inf.odd_keys) : 0u);
                     const bool part_of = kSel && !(t0 + kQ4Unit <= vis_all && (t0 >= lo_all || t0 + kQ4Unit <= a.sinks));      // (the same for the warp)
                     const bool special = (kSel ? part_of || (odd & 0x07070707u) != 0u : __any_sync(0xffffffffu, lim < kQ4Unit || (odd & 0x07070707u) != 0u)) ||
                                          tiles != (1u << kQ4UnitTiles) - 1u;
@@ -994,9 +1121,9 @@ __global__ void __launch_bounds__(kBThreads, 1) q4_block_kernel(const __grid_con
 
 cudaError_t q4_block_setup() {
     cudaError_t e;
-#define PKV_Q4_SETUP2(D, NG, H16, SEL) \
-    if ((e = cudaFuncSetAttribute(q4_block_kernel<D, NG, H16, SEL>, cudaFuncAttributeMaxDynamicSharedMemorySize, BlockShape<D, NG>::kSmem)) != cudaSuccess) return e;
-#define PKV_Q4_SETUP1(D, NG, H16) PKV_Q4_SETUP2(D, NG, H16, false) PKV_Q4_SETUP2(D, NG, H16, true)
+#define PKV_Q4_SETUP2(D, NG, H16, SEL, PAIRS) \
+    if ((e = cudaFuncSetAttribute(q4_block_kernel<D, NG, H16, SEL, PAIRS>, cudaFuncAttributeMaxDynamicSharedMemorySize, BlockShape<D, NG>::kSmem)) != cudaSuccess) return e;
+#define PKV_Q4_SETUP1(D, NG, H16) PKV_Q4_SETUP2(D, NG, H16, false, false) PKV_Q4_SETUP2(D, NG, H16, true, false) PKV_Q4_SETUP2(D, NG, H16, true, true)
 #define PKV_Q4_SETUP(D, NG) PKV_Q4_SETUP1(D, NG, false) PKV_Q4_SETUP1(D, NG, true)
     PKV_Q4_SHAPES(PKV_Q4_SETUP)
     return cudaSuccess;
@@ -1021,12 +1148,14 @@ cudaError_t launch_q4_block(const Q4AttentionArgs &a, int n, cudaStream_t st) {
     cfg.attrs = at;
     cfg.numAttrs = a.chained;
     cfg.gridDim = dim3(n);
-    cfg.blockDim = dim3(kBThreads);
+    const bool part = a.window > 0 || a.tree, pairs = part && (long long)a.max_q_len * g.group <= kBHalf;
+    cfg.blockDim = dim3(block_threads(pairs));
 #define PKV_Q4_LAUNCH1(D, NG, H16)                                                                       \
     if (g.head_dim == D && g.groups == NG && (g.fp16 != 0) == H16) {                                     \
         cfg.dynamicSmemBytes = BlockShape<D, NG>::kSmem;                                                 \
-        return a.window > 0 || a.tree ? cudaLaunchKernelEx(&cfg, q4_block_kernel<D, NG, H16, true>, a)   \
-                                      : cudaLaunchKernelEx(&cfg, q4_block_kernel<D, NG, H16, false>, a); \
+        return pairs  ? cudaLaunchKernelEx(&cfg, q4_block_kernel<D, NG, H16, true, true>, a)             \
+               : part ? cudaLaunchKernelEx(&cfg, q4_block_kernel<D, NG, H16, true, false>, a)            \
+                      : cudaLaunchKernelEx(&cfg, q4_block_kernel<D, NG, H16, false, false>, a);          \
     }
 #define PKV_Q4_LAUNCH(D, NG) PKV_Q4_LAUNCH1(D, NG, false) PKV_Q4_LAUNCH1(D, NG, true)
     PKV_Q4_SHAPES(PKV_Q4_LAUNCH)
