@@ -879,6 +879,62 @@ def test_steps_that_make_no_sense_change_nothing(S, bad):
     same_plan(ref, dev, out, result, capacity)
 
 
+@pytest.mark.gpu
+def test_windows_trees_and_kept_rows_in_pages_beyond_four_gigabytes():
+    H, P, n, T = 8, 64, 5, 180
+    cache = pkv.Q4Cache(config(n_kv_heads=H, n_q_heads=H, n_pages=70000, page_size=P))
+    assert 60000 * cache.sizes.page_bytes > 1 << 32
+    gen = torch.Generator().manual_seed(1)
+    k, v, q = (rows_of(gen, T, H, 128, BF16) for _ in "kvq")
+    table, lengths = torch.tensor([[69999, 65000, 60000]], **INTS).cuda(), torch.tensor([T], **INTS).cuda()
+    cache.append_kv(table, lengths, k[None].cuda(), v[None].cuda())
+    K, V, q = quantised(k, 32), quantised(v, 32), q[-n:]
+    parents = [-1, 0, 0, 1, -1]
+    masks, _ = cache.tree_masks(torch.tensor([parents], **INTS).cuda(), lengths, window=100, sinks=3)
+    out = cache.attention(table, lengths, q[None].cuda(), tree=masks, window=100, sinks=3)
+    ref, _, tol = attention_seen(q, K, V, tree_seen(T, tree_bits(parents, T - n, 100, 3)[0], 100, 3), 1 / math.sqrt(128), BF16)
+    check(out[0], ref, tol)
+    kept = cache.keep_rows(table, lengths, torch.tensor([[0, 1, 3]], **INTS).cuda(), torch.tensor([3], **INTS).cuda(), n)
+    ko, vo = (torch.empty(1, T - 2, H, 128, dtype=BF16, device="cuda") for _ in "kv")
+    cache.read_kv(table, kept, ko, vo)
+    rows = list(range(T - n)) + [T - n + i for i in (0, 1, 3)]
+    assert kept.tolist() == [T - 2] and torch.equal(ko[0].cpu(), K[rows].to(BF16)) and torch.equal(vo[0].cpu(), V[rows].to(BF16))
+
+
+@pytest.mark.gpu
+def test_windows_plans_and_kept_rows_of_as_many_sequences_as_a_call_takes():
+    """65535 requests of one token, every ninth empty: each sees its own token, the value as it was quantised."""
+    S, H, d, P = 65535, 2, 64, 16
+    cache = pkv.Q4Cache(config(n_kv_heads=H, n_q_heads=2 * H, head_dim=d, page_size=P, n_pages=S))
+    rows = torch.ones(S, dtype=torch.int32)
+    rows[::9] = 0
+    n = int(rows.sum())
+    ring, counters = cache.new_ring(torch.randperm(S, generator=torch.Generator().manual_seed(1)))
+    table = torch.full((S, 2), -1, **INTS).cuda()
+    p = cache.plan(table, torch.zeros(S, **INTS).cuda(), rows.cuda(), torch.zeros(S, 2, **INTS).cuda(), ring, counters, n, window=40, sinks=3)
+    assert p.counters.tolist() == [n, S, 0, 0] and torch.equal(p.lengths.cpu(), rows) and torch.equal(p.offsets[1:].cpu(), rows.cumsum(0).int())
+    there = rows.bool()
+    assert torch.equal(p.slots.cpu(), table.cpu()[there, 0].long() * P) and (p.positions == 0).all()
+    assert torch.equal(table.cpu()[there, 0], ring.cpu()[:n])
+    k, v = (torch.randn(n, H, d, generator=torch.Generator().manual_seed(i)).to(BF16) for i in (2, 3))
+    cache.append_kv(table, p.lengths, k.cuda(), v.cuda(), p.offsets)
+    q = torch.randn(n, 2 * H, d, generator=torch.Generator().manual_seed(4)).to(BF16).cuda()
+    # (one token: the result is code * scale, off by half a bf16 step where it lies between two numbers, and by 2^-20 from exp2; see the
+    # causal call's test of the same)
+    exact = quantised(v, 32).repeat_interleave(2, 1)
+    near = lambda out: ((out.cpu().double() - exact).abs() <= exact.abs() * (2.0 ** -8 + 2.0 ** -20)).all()      # noqa: E731
+    assert near(cache.attention(table, p.lengths, q, offsets=p.offsets, max_q_len=1, window=40, sinks=3))
+    masks, depths = cache.tree_masks(torch.full((n,), -1, **INTS).cuda(), p.lengths, p.offsets, 1)
+    assert (masks == 1).all() and (depths == 0).all()
+    assert near(cache.attention(table, p.lengths, q, offsets=p.offsets, max_q_len=1, tree=masks))
+    counts = (torch.arange(S) % 2).int()
+    kept = cache.keep_rows(table, p.lengths, torch.zeros(S, 1, **INTS).cuda(), torch.minimum(counts, rows).cuda(), n, p.offsets)
+    assert torch.equal(kept.cpu(), torch.minimum(counts, rows))
+    done = cache.plan(table, p.lengths, torch.full((S,), -1, **INTS).cuda(), p.spans, ring, p.counters, 0)
+    assert done.counters.tolist() == [n, S + n, 0, 0] and torch.equal(ring[:n].cpu(), table.cpu()[there, 0])
+    assert cache.stats() == {"device_timeouts": 0, "bad_pages": 0, "bad_lengths": 0}
+
+
 # ---- GPU: a run of them together --------------------------------------------------------------------------------------
 class Served:
     """Requests served with planned steps, drafted trees and kept rows; what they hold, in 64 bits."""
@@ -1071,9 +1127,10 @@ def test_random_selections(seed):
 
 @pytest.mark.gpu
 def test_in_a_process_without_caches_that_overlap():
-    """Kernels are launched differently there (other test files make a page cache whose decodes do not wait): this file's tests by themselves."""
+    """Kernels are launched differently there (other test files make a page cache whose decodes do not wait): the tests of calls that follow one
+    another, by themselves."""
     import subprocess
     import sys
-    r = subprocess.run([sys.executable, "-m", "pytest", "-q", "-x", "-m", "gpu", "-k", "not in_a_process", "-p", "no:cacheprovider", __file__],
+    r = subprocess.run([sys.executable, "-m", "pytest", "-q", "-x", "-m", "gpu", "-k", "every_kernel or serving or captured or same_bits or random or planned or kept", "-p", "no:cacheprovider", __file__],
                        capture_output=True, text=True, timeout=900)
     assert r.returncode == 0, r.stdout[-3000:]
