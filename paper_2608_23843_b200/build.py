@@ -1,8 +1,10 @@
-"""Builds libpkv.so (the C-ABI CUDA library) in-tree with nvcc for sm_100a."""
+"""Builds libpkv.so (the C-ABI CUDA library) in-tree with nvcc for sm_100a, and _pkvcall.so, through which the Python binding makes
+the calls of a decode step (a C source against it, gcc)."""
 import glob
 import os
 import subprocess
 import sys
+import sysconfig
 import tempfile
 from concurrent.futures import ThreadPoolExecutor
 
@@ -10,11 +12,24 @@ _HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(_HERE)
 CSRC = os.path.join(_HERE, "csrc")
 LIB = os.path.join(_HERE, "libpkv.so")
+CALL, CALL_SOURCE = os.path.join(_HERE, "_pkvcall.so"), os.path.join(CSRC, "pkv_call.c")
 NVCC = os.environ.get("NVCC", "/usr/local/cuda/bin/nvcc")
 
 
 def sources():
     return sorted(glob.glob(os.path.join(CSRC, "*.cu")))
+
+
+def build_call(force=False):
+    """Compile the binding's calls; returns its path."""
+    deps = [CALL_SOURCE, os.path.join(ROOT, "include", "pkv.h")]
+    if not force and os.path.exists(CALL) and all(os.path.getmtime(f) <= os.path.getmtime(CALL) for f in deps):
+        return CALL
+    tmp = CALL + ".tmp.%d" % os.getpid()
+    subprocess.run([os.environ.get("CC", "gcc"), "-O2", "-std=c11", "-Wall", "-shared", "-fPIC", "-I", sysconfig.get_path("include"), "-I", os.path.join(ROOT, "include"),
+                    CALL_SOURCE, "-o", tmp, "-L", _HERE, "-l:libpkv.so", "-Wl,-rpath,$ORIGIN"], check=True)
+    os.replace(tmp, CALL)
+    return CALL
 
 
 def _stale():
@@ -26,8 +41,9 @@ def _stale():
 
 
 def build(force=False, verbose=False):
-    """Compile every .cu under csrc/ into one shared library; returns its path."""
+    """Compile every .cu under csrc/ into one shared library, and the binding's calls; returns the library's path."""
     if not force and not _stale():
+        build_call()
         return LIB
     # one nvcc per source, side by side: the kernels' many shapes take minutes one after the other
     flags = ["-gencode", "arch=compute_100a,code=sm_100a", "-O3", "-lineinfo", "-std=c++17", "-Xcompiler", "-fPIC",
@@ -45,6 +61,7 @@ def build(force=False, verbose=False):
             list(pool.map(compile_one, zip(sources(), objects)))
         subprocess.run([NVCC, *flags, "-shared", *objects, "-o", tmp], check=True)
     os.replace(tmp, LIB)
+    build_call(force=True)
     return LIB
 
 

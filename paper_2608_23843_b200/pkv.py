@@ -1,4 +1,4 @@
-"""ctypes binding of libpkv.so (see include/pkv.h): argument marshalling only.
+"""Binding of libpkv.so (see include/pkv.h) by ctypes, and by a small C module for the calls of a decode step: argument marshalling only.
 
 Module-level functions carry the C names (`pkv_init_cache`, `pkv_append_kv`,
 `pkv_compress_eligible_pages`, `pkv_decode_attention`, ...).  `Cache` is a
@@ -156,6 +156,19 @@ def lib():
                 getattr(L, name).restype = ctypes.c_int32
         _lib = L
     return _lib
+
+
+_calls_module = None
+
+
+def _calls():
+    """The calls of a decode step without ctypes (3 us less each): numbers in, a status out.  Raises if they have not been built."""
+    global _calls_module
+    if _calls_module is None:
+        lib()                                            # (says what to do where nothing has been built)
+        from . import _pkvcall
+        _calls_module = _pkvcall
+    return _calls_module
 
 
 _INT_ARRAYS = {}
@@ -682,11 +695,15 @@ class Q4Cache:
 
     def _call(self, fn, *args):
         """A C call with the cache's device current (the library refuses another one)."""
-        st = fn(self.handle, *args)
+        handle = None if self.handle is None else self.handle.value
+        try:
+            st = fn(handle, *args)
+        except (TypeError, OverflowError) as e:          # an argument that is no whole number, or too large for the C call
+            self._fail(str(e))
         if st != PKV_OK:
             if not self.dry_run and torch.cuda.current_device() != self._device_index:
                 with torch.cuda.device(self._device_index):
-                    st = fn(self.handle, *args)
+                    st = fn(handle, *args)
             _q4_check(self.handle, st)
 
     # A decode step makes a few of these calls per layer and each is some microseconds of host time: the checks below are
@@ -731,11 +748,11 @@ class Q4Cache:
 
     def append_kv(self, page_table, lengths, k, v, offsets=None):
         """Quantises the new rows k, v into the cache."""
-        self._copy(lib().pkv_q4_append_kv, page_table, lengths, k, v, offsets)
+        self._copy(_calls().append_kv, page_table, lengths, k, v, offsets)
 
     def read_kv(self, page_table, lengths, k, v, offsets=None):
         """Reads the last positions of each sequence back into k, v."""
-        self._copy(lib().pkv_q4_read_kv, page_table, lengths, k, v, offsets)
+        self._copy(_calls().read_kv, page_table, lengths, k, v, offsets)
         return k, v
 
     def _copy(self, fn, page_table, lengths, k, v, offsets):
@@ -814,13 +831,12 @@ class Q4Cache:
         # (from the caching allocator at each call: ordered with this stream, and private to a graph that is being captured)
         work = torch.empty(size, dtype=torch.uint8, device=self.device) if size and not self.dry_run else None
         if part:
-            sel = PkvQ4Select(window, sinks, None if tree is None else tree.data_ptr(), words)
-            self._call(lib().pkv_q4_attention_select, n_seqs, page_table.data_ptr(), max_pages, lengths.data_ptr(), n,
-                       offsets.data_ptr() if ragged else None, max_q_len, max_len, ctypes.byref(sel), q.data_ptr(), q_row, q_head,
+            self._call(_calls().attention_select, n_seqs, page_table.data_ptr(), max_pages, lengths.data_ptr(), n,
+                       offsets.data_ptr() if ragged else None, max_q_len, max_len, q.data_ptr(), q_row, q_head,
                        None if out is None else out.data_ptr(), o_row, o_head, None if state is None else state.data_ptr(),
-                       None if work is None else work.data_ptr(), size, self._stream())
+                       None if work is None else work.data_ptr(), size, self._stream(), window, sinks, None if tree is None else tree.data_ptr(), words)
             return
-        self._call(lib().pkv_q4_attention, n_seqs, page_table.data_ptr(), max_pages, lengths.data_ptr(), n,
+        self._call(_calls().attention, n_seqs, page_table.data_ptr(), max_pages, lengths.data_ptr(), n,
                    offsets.data_ptr() if ragged else None, max_q_len, max_len, q.data_ptr(), q_row, q_head,
                    None if out is None else out.data_ptr(), o_row, o_head, None if state is None else state.data_ptr(),
                    None if work is None else work.data_ptr(), size, self._stream())
@@ -861,7 +877,7 @@ class Q4Cache:
         words = max_q_len + 63 >> 6 if max_q_len > 0 else 1
         depths = torch.empty_like(parents)
         masks = torch.empty(*shape, words, dtype=_INT64, device=self.device)
-        self._call(lib().pkv_q4_tree_masks, n_seqs, None if lengths is None else lengths.data_ptr(), n, None if offsets is None else offsets.data_ptr(),
+        self._call(_calls().tree_masks, n_seqs, None if lengths is None else lengths.data_ptr(), n, None if offsets is None else offsets.data_ptr(),
                    max_q_len, parents.data_ptr(), window, sinks, masks.data_ptr(), words, depths.data_ptr(), self._stream())
         return masks, depths
 
@@ -880,7 +896,7 @@ class Q4Cache:
         else:
             self._ints("out", out, (n_seqs,))
         n = new_rows if offsets is not None else new_rows * n_seqs
-        self._call(lib().pkv_q4_keep_rows, n_seqs, page_table.data_ptr(), max_pages, lengths.data_ptr(), n, None if offsets is None else offsets.data_ptr(),
+        self._call(_calls().keep_rows, n_seqs, page_table.data_ptr(), max_pages, lengths.data_ptr(), n, None if offsets is None else offsets.data_ptr(),
                    paths.data_ptr(), most[1], counts.data_ptr(), out.data_ptr(), self._stream())
         return out
 
@@ -931,7 +947,7 @@ class Q4Cache:
             size = self._workspaces[key] = pkv_q4_plan_workspace(self.handle, n_seqs, n_rows)
         work = torch.empty(size, dtype=torch.uint8, device=self.device) if size and not self.dry_run else None
         pos, slots = out.positions, out.slots
-        self._call(lib().pkv_q4_plan, n_seqs, page_table.data_ptr(), max_pages, lengths.data_ptr(), rows.data_ptr(), spans.data_ptr(), ring.data_ptr(),
+        self._call(_calls().plan, n_seqs, page_table.data_ptr(), max_pages, lengths.data_ptr(), rows.data_ptr(), spans.data_ptr(), ring.data_ptr(),
                    counters.data_ptr(), window, sinks, out.lengths.data_ptr(), out.spans.data_ptr(), out.counters.data_ptr(), out.offsets.data_ptr(), n_rows,
                    None if pos is None else pos.data_ptr(), None if slots is None else slots.data_ptr(), None if work is None else work.data_ptr(), size,
                    self._stream())

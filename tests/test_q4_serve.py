@@ -89,6 +89,8 @@ def _ring():
     lambda c, t, n, q: c.plan(t, n, n, _spans(), *_ring(), 4, sinks=1),
     lambda c, t, n, q: c.plan(t, n, n, _spans(), *_ring(), 4, out=c.plan(t, n, n, _spans(), *_ring(), 5)),
     lambda c, t, n, q: c.plan(t.long(), n, n, _spans(), *_ring(), 4),
+    lambda c, t, n, q: c.keep_rows(t, n, torch.zeros(3, 2, **INTS), n, 2 ** 62),               # more than 64 bits in all
+    lambda c, t, n, q: c.keep_rows(t, n, torch.zeros(3, 2, **INTS), n, 2.0),
     lambda c, t, n, q: c.new_ring([0, 1, 1]),
     lambda c, t, n, q: c.new_ring([16]),
     lambda c, t, n, q: c.new_ring(torch.arange(17)),
@@ -170,6 +172,28 @@ def test_which_kernel_serves_a_call(name, shape, S, n, T, kw, kernel, cluster):
     for bad in ((0, 1, 64), (1, 0, 64), (1, 1, 0)):
         with pytest.raises(pkv.PkvError):
             pkv.pkv_q4_attention_route(cache.handle, *bad)
+
+
+def test_calls_without_ctypes_check_their_numbers():
+    from paper_2608_23843_b200 import _pkvcall
+    c, t, n, q = _dry()
+    h = c.handle.value
+    good = dict(append_kv=(h, 3, 0, 4, 0, 6, 0, 0, 256, 128, 0, 256, 128, 0), attention=(h, 3, 0, 4, 0, 6, 0, 2, 0, 0, 1024, 128, 0, 1024, 128, 0, 0, 0, 0),
+                attention_select=(h, 3, 0, 4, 0, 6, 0, 2, 0, 0, 1024, 128, 0, 1024, 128, 0, 0, 0, 0, 9, 4, None, 0),
+                tree_masks=(h, 3, None, 6, None, 2, 0, 0, 0, 0, 1, 0, 0), keep_rows=(h, 3, 0, 4, 0, 6, 0, 0, 2, 0, 0, 0),
+                plan=(h, 3, 0, 4, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 6, 0, 0, 0, 0, 0))
+    good["read_kv"] = good["append_kv"]
+    for name, args in good.items():
+        fn = getattr(_pkvcall, name)
+        assert fn(*args) == pkv.PKV_OK, name
+        assert fn(None, *args[1:]) == pkv.PKV_ERR_INVALID_ARG
+        with pytest.raises(TypeError):
+            fn(*args[:-1])
+        with pytest.raises(TypeError):
+            fn(h, 3.0, *args[2:])
+        for wrong in (1 << 31, -(1 << 31) - 1, 1 << 64):                             # n_seqs
+            with pytest.raises(OverflowError):
+                fn(h, wrong, *args[2:])
 
 
 def test_the_references_agree_with_one_another():
