@@ -19,6 +19,10 @@
 // Measured, 8 KV heads, d = 128, g = 32: 8 sequences of 32K (302 MB) 71 to 74 us with 4 or 8 rows per KV head (4.1 TB/s; issue slots
 // 58 % busy, tensor pipe 26 %), 112 us with 16; one of 128K 41.5 us; the kernel's rate on further tokens is 5.5 to 5.8 TB/s,
 // and some 15 us of a call that joins states are launches, the first copies, the last units and the join.
+// Where queries see a part of the positions (kSel: a window with sinks, a drafted tree) units that nobody sees are not visited, units seen in part get
+// 64 bits a row, and short segments go to small CTAs, clusters of them where there are few (kSmall).  8 sequences of 32K with a window of 4096: 17.5 us (37.9
+// MB; three rounds of a unit's chain, 3.5 us each with twelve warps per SM, and 7 us of launch, share, first copies and join), 64 ragged ones
+// with 1024: 27.6 us (71 MB, seven rounds, 41 % of the issue slots), 7 drafted tokens against 1500: 9.9 us.
 // One warp of a CTA looks up pages and issues the bulk copies; the others take the units of 64 tokens in turn and keep (m, l, o)
 // in registers; at the end of a (sequence, KV head, row tile) segment the warps' states are joined through shared memory.  The CTAs of
 // a launch share the whole batch's units evenly, whatever the lengths; a segment that spans CTAs leaves its states in the

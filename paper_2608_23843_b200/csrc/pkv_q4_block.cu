@@ -25,6 +25,8 @@
 // issuing warp per half, which by itself costs more than it gives, 1501), five or six
 // widening warps, a quarter of the exponentials by polynomial, the halves' exponentials in turn, weights with the old
 // reference before the maximum is known.
+// Where queries see a part of the positions (kSel) a block visits the units from its first row's window on and those of the sinks: 2048 positions with a
+// window of 4096 211 us (140 GFLOP, 66 units a block), 8 drafted trees of 64 against 32K 354 us (274 GFLOP).
 // CTAs share the batch's units evenly, one CTA per SM; blocks that span CTAs leave states that a second kernel joins.  Units
 // after a block's last visible position are not visited.
 #include <cuda_bf16.h>

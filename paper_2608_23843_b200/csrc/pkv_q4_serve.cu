@@ -29,7 +29,8 @@ cudaError_t launch_chained(void (*kernel)(Args), const Args &a, dim3 grid, int t
 // ---- masks of drafted trees ---------------------------------------------------------------------------------------------
 // A thread per row walks up its branch: once for the depth, which says where the window ends, once for the bits.  Ancestors
 // have smaller numbers, so a word is finished when the walk leaves it.  A CTA's rows belong to one sequence; its parents up to
-// kTreeHeld lie in shared memory, since the walk is a chain of loads.  (A few KB in and out: latency and the launch.)
+// kTreeHeld lie in shared memory, since the walk is a chain of loads.  (A few KB in and out: latency and the launch; 7 rows 1.6 us, 16 x 25 with
+// a window 3.1 us in a row of them.)
 constexpr int kTreeThreads = 128, kTreeHeld = 2048;
 
 __global__ void __launch_bounds__(kTreeThreads) q4_tree_kernel(const __grid_constant__ Q4TreeArgs a) {
@@ -79,7 +80,8 @@ __global__ void __launch_bounds__(kTreeThreads) q4_tree_kernel(const __grid_cons
 // ---- accepted rows --------------------------------------------------------------------------------------------------------
 // A CTA moves the rows of one sequence and KV head, eight lanes a row: K codes and V's chunks (which lie differently in every
 // row of a tile), then the scales.  Row i comes from row path[i] >= i, so 128 rows at a time are read, then written: what a
-// later 128 reads was not written before.  (Bound by latency: a trip for the path, one for the pages, one for the rows.)
+// later 128 reads was not written before.  (Bound by latency: a trip for the path, one for the pages, one for the rows; 8 x 64 drafted rows, about half
+// of them kept, with their append and reading back 8.2 us, of which this is a third.)
 constexpr int kKeepThreads = 256, kKeepUnroll = 4, kKeepSlots = kKeepThreads / 8;
 
 template <int D, int NG>
@@ -150,8 +152,8 @@ __global__ void __launch_bounds__(kKeepThreads) q4_keep_kernel(const __grid_cons
 // ---- planning a step ------------------------------------------------------------------------------------------------------
 // Prefix sums over the requests - new rows, pages taken, pages given back - from which every row, taken page and returned page follows
 // by itself: a thread each, which finds its request by bisection in the sums.  Up to kPlanHeld requests the sums fit shared memory,
-// and a CTA, or a cluster of eight that all work them out, fills everything in (64 requests: 4.5 us, all latency: launch, counters and lengths, the scan,
-// pages, results; 700 requests with chunks of prompts, one kernel for the sums and one for the rest: 10.6 us and a launch more).  More requests
+// and a CTA, or a cluster of eight that all work them out, fills everything in (64 requests: 4.6 us, all latency: launch, counters and lengths, the scan,
+// pages, results; 700 requests with chunks of prompts 7.5 us, and one kernel for the sums and one for the rest 10.6 and a launch more).  More requests
 // leave the sums in the workspace to a second kernel over the SMs.  Entries that are read (below `end`) and written (from it on), and
 // places of the ring that are read (from the head) and written (from the tail), are different ones, so the order does not matter.
 constexpr int kPlanThreads = 1024, kPlanFillThreads = 256, kPlanCluster = 8;
