@@ -624,7 +624,7 @@ pkv_status pkv_q4_attention(pkv_q4_cache *c, int32_t n_seqs, const int32_t *page
  *   tree            [device] uint64 [n_rows, tree_words], or NULL: causal.  The new rows of a sequence (n of them, behind a context of C = T - n
  *                   tokens) are then drafted tokens: row j sees new row i if bit i % 64 of tree[row j][i / 64] is set (bits of
  *                   rows that the sequence does not have are ignored), and the context.  With a window it sees of the context the last W - b positions and
- *                   the sinks, b being the number of its bits (of rows the sequence has): with masks of pkv_q4_tree_masks() that
+ *                   the sinks, b being the number of its bits (of rows the sequence has; 1 at least, the row's own place): with masks of pkv_q4_tree_masks() that
  *                   is a window that ends at the row's own place in its branch.  64 * tree_words has to be max_q_len at least.
  * Everything else - rows, strides, states, workspace, accuracy, what contents that make no sense lead to - is as for pkv_q4_attention();
  * a query that sees nothing gets zeros.  A call with window = 0 and tree = NULL is pkv_q4_attention().
@@ -667,7 +667,7 @@ pkv_status pkv_q4_tree_masks(pkv_q4_cache *c, int32_t n_seqs, const int32_t *len
                              int32_t tree_words, int32_t *depths, void *stream);
 
 /*
- * Keeps the accepted rows of each sequence's n new rows: row paths[s][i] becomes new row i, for i < counts[s] (held inside [0, min(n, max_path)]),
+ * Keeps the accepted rows of each sequence's n new rows: row paths[s][i] becomes new row i, for i < counts[s] (held inside [0, min(n, max_path)], and counted in bad_lengths),
  * all at once, codes and scales as they are; lengths_out[s] = T - n + counts[s] (0 at least).
  *   paths   [device] int32 [n_seqs, max_path], i <= paths[s][i] < n (rows of a path ascend, so that holds for every path of a tree whose
  *           parents come before their children); an entry outside that is skipped (new row i stays as it was) and counted in bad_lengths

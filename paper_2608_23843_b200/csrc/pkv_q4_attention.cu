@@ -1241,7 +1241,7 @@ Q4Route q4_route(const Q4Geometry &g, int n_seqs, int max_q_len, int max_len, co
     r.blocks = q4_by_blocks(g, n_seqs, max_q_len, max_len);
     if (part) {
         // Estimates in us, fitted to 45 shapes (1 to 128 sequences, 1 to 64 new rows, windows of 256 to 16384 and whole contexts up to 64K, d = 128; the
-        // choice was within 5 % of the best of the three in all but two):
+        // choice is within 2 % of the best of the three in all but one, 6 %):
         // small CTAs: rounds of a unit's chain, 1.5 us alone and 3.7 with all warps busy (one request, window of 4096: 13.5 against 17.0 us on the
         // column kernel's even shares; 64 requests, 1024: 31 against 62; 32 requests, 8192: 86.0 against 84.6; one, 16384: 25.6 against 19.2)
         const double segs = heads * std::ceil(rows / 8), slots = 2. * g.n_ctas;

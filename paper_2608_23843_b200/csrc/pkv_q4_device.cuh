@@ -47,9 +47,10 @@ __device__ __forceinline__ Q4Span q4_span(const Q4AttentionArgs &a, int see, int
     r.units = max(1, all - r.gap);
     return r;
 }
-// The lowest position in the window of new row j of a sequence with a context of C tokens, for a row of a tree when no new row counts.
+// The lowest position in the window of new row j of a sequence with a context of C tokens, or of any row of a tree (whose own position counts at
+// least).  Pages below it may have gone back.
 __device__ __forceinline__ int q4_lowest(const Q4AttentionArgs &a, int C, int j) {
-    return a.window ? C + (a.tree ? 0 : j + 1) - a.window : 0;
+    return a.window ? C + (a.tree ? 0 : j) + 1 - a.window : 0;
 }
 // Tiles of the unit at t0 that have to be there (of the first `tiles`): those of parts - a page's, or the whole unit - that hold a position
 // below the sinks or from lo on.  Pages of other parts may be anyone's.
@@ -70,7 +71,7 @@ __device__ __forceinline__ Q4Seen q4_seen(const Q4AttentionArgs &a, int T, int a
         const unsigned long long *w = a.tree + (long long)(first + j) * a.tree_words;
         for (int i = 0; i < min(a.tree_words, (all + 63) >> 6); ++i) own += __popcll(__ldg(w + i) & (all - 64 * i >= 64 ? ~0ull : (1ull << (all - 64 * i)) - 1ull));
     }
-    return Q4Seen{a.window ? max(0, C + own - a.window) : 0, C};
+    return Q4Seen{a.window ? max(0, C + max(own, 1) - a.window) : 0, C};
 }
 __device__ __forceinline__ unsigned long long q4_below(int x) { return x <= 0 ? 0ull : x >= 64 ? ~0ull : (1ull << x) - 1ull; }
 // ... as bits of the unit at t0

@@ -38,7 +38,7 @@ def tree_seen(T, bits, window=0, sinks=0):
     C, t = T - n, torch.arange(T)
     see = torch.zeros(n, T, dtype=torch.bool)
     for j in range(n):
-        low = max(0, C + int(bits[j].sum()) - window) if window else 0
+        low = max(0, C + max(1, int(bits[j].sum())) - window) if window else 0
         see[j] = (t >= low) | (t < sinks)
         see[j, max(C, 0):] = bits[j, max(0, -C):]
     return see

@@ -519,6 +519,29 @@ def test_any_masks(n, G):
     f.clean()
 
 
+@pytest.mark.gpu
+@pytest.mark.parametrize("P", [16, 64])
+@pytest.mark.parametrize("n, G, n_ctas, kernel", [(3, 4, 0, 2), (20, 4, 1, 1), (40, 4, 1, 1), (4, 2, 0, 0)])
+def test_the_page_that_ends_before_a_window_may_be_gone(n, G, n_ctas, kernel, P):
+    """The last position of a page is the first that no row sees: the page has gone back."""
+    long = 30000 if kernel == 0 else 0
+    C = 20 * P + 5 + long // P * P
+    W = C - (4 * P - 1)                                    # C + 1 - W: the first position of page 4
+    f = Filled([C + n], G=G, H=2, P=P, seed=60, n_ctas=n_ctas)
+    assert _route(f.cache, 1, n, f.table.shape[1] * P, dict(window=W, sinks=3, tree=True))[0] == kernel
+    parents = random_parents(random.Random(n), n)
+    q = f.queries([n])[0]
+    for tree in (True, False):
+        masks = f.cache.tree_masks(torch.tensor([parents], **INTS).cuda(), f.lengths, window=W, sinks=3)[0] if tree else None
+        table = f.table.clone()
+        table[0, 1:4] = -1
+        out = f.cache.attention(table, f.lengths, q[None].cuda(), tree=masks, window=W, sinks=3)
+        see = tree_seen(C + n, tree_bits(parents, C, W, 3)[0], W, 3) if tree else window_seen(C + n, n, W, 3)
+        assert see[:, 4 * P].any() and not see[:, P:4 * P].any()
+        check(out[0], *seen_by(f, q, 0, see)[::2])
+    f.clean()
+
+
 @pytest.mark.usefixtures("room")
 @pytest.mark.gpu
 @pytest.mark.parametrize("shape", SHAPES[:4], ids=str)
