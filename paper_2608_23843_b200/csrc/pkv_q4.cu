@@ -531,7 +531,8 @@ pkv_status pkv_q4_init_cache(const pkv_q4_config *cfg, void *pool, void *meta, p
     if (!dry) {
         cudaError_t e = cudaGetDevice(&c->device);
         if (e == cudaSuccess) e = cudaDeviceGetAttribute(&g.n_sms, cudaDevAttrMultiProcessorCount, c->device);
-        if (e == cudaSuccess) e = q4_attention_setup();
+        if (e == cudaSuccess) e = q4_attention_setup(g);
+        if (e == cudaSuccess) e = q4_serve_setup(g);
         if (e == cudaSuccess) e = cudaMemset(meta, 0, 256);
         if (e != cudaSuccess) { delete c; return PKV_ERR_CUDA; }
     }

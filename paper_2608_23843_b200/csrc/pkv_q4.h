@@ -126,10 +126,11 @@ cudaError_t launch_q4_tree_masks(Q4TreeArgs a, cudaStream_t st);
 cudaError_t launch_q4_keep(Q4KeepArgs a, cudaStream_t st);
 cudaError_t launch_q4_plan(Q4PlanArgs a, cudaStream_t st);
 long long q4_plan_workspace(int n_seqs, long long n_rows);
-cudaError_t q4_attention_setup();      // raises dynamic shared-memory limits, once per cache
+cudaError_t q4_attention_setup(const Q4Geometry &g);      // raises dynamic shared-memory limits of a cache's kernels, once per cache
+cudaError_t q4_serve_setup(const Q4Geometry &g);
 // the row-block kernel (pkv_q4_block.cu); n: CTAs, from q4_block_grid
 constexpr int kQ4BlockRows = 256;
-cudaError_t q4_block_setup();
+cudaError_t q4_block_setup(const Q4Geometry &g);
 int q4_block_grid(const Q4Geometry &g, int n_seqs, int max_q_len, int max_len, const Q4Select &sel);
 cudaError_t launch_q4_block(const Q4AttentionArgs &a, int n, cudaStream_t st);
 long long q4_attention_workspace(const Q4Geometry &g, int n_seqs, int max_q_len, int max_len, const Q4Select &sel);

@@ -1210,14 +1210,20 @@ int q4_grid(const Q4Geometry &g, int n_seqs, int max_q_len, int max_len, bool wh
 
 }  // namespace
 
-cudaError_t q4_attention_setup() {
-    cudaError_t e = q4_block_setup();
+cudaError_t q4_attention_setup(const Q4Geometry &g) {
+    cudaError_t e = q4_block_setup(g);
     if (e != cudaSuccess) return e;
+    cudaFuncAttributes known;              // (asking for them loads a kernel: not on its first call, which may be captured)
+#define PKV_Q4_LOAD(D, H16) \
+    if (g.head_dim == D && (g.fp16 != 0) == H16 && ((e = cudaFuncGetAttributes(&known, q4_join_kernel<D, H16, 1>)) != cudaSuccess || \
+                                                    (e = cudaFuncGetAttributes(&known, q4_join_kernel<D, H16, 4>)) != cudaSuccess)) return e;
+    PKV_Q4_LOAD(128, false) PKV_Q4_LOAD(128, true) PKV_Q4_LOAD(64, false) PKV_Q4_LOAD(64, true)
+#define PKV_Q4_OWN(D, NG, H16) g.head_dim == D && g.groups == NG && (g.fp16 != 0) == H16
 #define PKV_Q4_SETUP2(D, NG, H16, NT, SEL) \
-    if ((e = cudaFuncSetAttribute(q4_decode_kernel<D, NG, H16, NT, SEL>, cudaFuncAttributeMaxDynamicSharedMemorySize, Q4Shape<D, NG, NT>::kSmem)) != cudaSuccess) return e;
+    if (PKV_Q4_OWN(D, NG, H16) && (e = cudaFuncSetAttribute(q4_decode_kernel<D, NG, H16, NT, SEL>, cudaFuncAttributeMaxDynamicSharedMemorySize, Q4Shape<D, NG, NT>::kSmem)) != cudaSuccess) return e;
 #define PKV_Q4_SETUP1(D, NG, H16, NT) PKV_Q4_SETUP2(D, NG, H16, NT, false) PKV_Q4_SETUP2(D, NG, H16, NT, true)
 #define PKV_Q4_SETUP3(D, NG, H16) \
-    if ((e = cudaFuncSetAttribute(q4_decode_kernel<D, NG, H16, 1, true, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, Q4Shape<D, NG, 1, true>::kSmem)) != cudaSuccess) return e;
+    if (PKV_Q4_OWN(D, NG, H16) && (e = cudaFuncSetAttribute(q4_decode_kernel<D, NG, H16, 1, true, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, Q4Shape<D, NG, 1, true>::kSmem)) != cudaSuccess) return e;
 #define PKV_Q4_SETUP(D, NG) PKV_Q4_SETUP3(D, NG, false) PKV_Q4_SETUP3(D, NG, true) PKV_Q4_SETUP1(D, NG, false, 1) PKV_Q4_SETUP1(D, NG, false, 2) PKV_Q4_SETUP1(D, NG, true, 1) PKV_Q4_SETUP1(D, NG, true, 2)
     PKV_Q4_SHAPES(PKV_Q4_SETUP)
     return cudaSuccess;

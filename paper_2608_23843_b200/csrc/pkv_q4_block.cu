@@ -1121,10 +1121,10 @@ __global__ void __launch_bounds__(block_threads(kPairs), 1) q4_block_kernel(cons
 
 }  // namespace
 
-cudaError_t q4_block_setup() {
+cudaError_t q4_block_setup(const Q4Geometry &g) {
     cudaError_t e;
 #define PKV_Q4_SETUP2(D, NG, H16, SEL, PAIRS) \
-    if ((e = cudaFuncSetAttribute(q4_block_kernel<D, NG, H16, SEL, PAIRS>, cudaFuncAttributeMaxDynamicSharedMemorySize, BlockShape<D, NG>::kSmem)) != cudaSuccess) return e;
+    if (g.head_dim == D && g.groups == NG && (g.fp16 != 0) == H16 && (e = cudaFuncSetAttribute(q4_block_kernel<D, NG, H16, SEL, PAIRS>, cudaFuncAttributeMaxDynamicSharedMemorySize, BlockShape<D, NG>::kSmem)) != cudaSuccess) return e;
 #define PKV_Q4_SETUP1(D, NG, H16) PKV_Q4_SETUP2(D, NG, H16, false, false) PKV_Q4_SETUP2(D, NG, H16, true, false) PKV_Q4_SETUP2(D, NG, H16, true, true)
 #define PKV_Q4_SETUP(D, NG) PKV_Q4_SETUP1(D, NG, false) PKV_Q4_SETUP1(D, NG, true)
     PKV_Q4_SHAPES(PKV_Q4_SETUP)

@@ -371,6 +371,20 @@ bool plan_at_once(int n_seqs, long long n_rows) { return n_seqs <= kPlanHeld && 
 
 }  // namespace
 
+// Loads the kernels of a cache's format: a first call may be captured.
+cudaError_t q4_serve_setup(const Q4Geometry &g) {
+    cudaFuncAttributes known;
+    cudaError_t e;
+    if ((e = cudaFuncGetAttributes(&known, q4_tree_kernel)) != cudaSuccess || (e = cudaFuncGetAttributes(&known, q4_plan_kernel<true>)) != cudaSuccess ||
+        (e = cudaFuncGetAttributes(&known, q4_plan_kernel<false>)) != cudaSuccess || (e = cudaFuncGetAttributes(&known, q4_plan_fill_kernel)) != cudaSuccess)
+        return e;
+#define PKV_Q4_LOAD(D, NG) \
+    if (g.head_dim == D && g.groups == NG) return cudaFuncGetAttributes(&known, q4_keep_kernel<D, NG>);
+    PKV_Q4_LOAD(128, 4) PKV_Q4_LOAD(128, 2) PKV_Q4_LOAD(128, 1) PKV_Q4_LOAD(64, 2) PKV_Q4_LOAD(64, 1)
+#undef PKV_Q4_LOAD
+    return cudaErrorInvalidValue;
+}
+
 cudaError_t launch_q4_tree_masks(Q4TreeArgs a, cudaStream_t st) {
     a.chained = q4_chained();
     return launch_chained(q4_tree_kernel, a, dim3(a.rows.n_seqs, (a.max_q_len + kTreeThreads - 1) / kTreeThreads), kTreeThreads, st);

@@ -1172,6 +1172,49 @@ def test_random_selections(seed):
         f.clean()
 
 
+def captured_first():
+    """Every call of a step is captured before it has ever run; the replay does what the calls do."""
+    S, n, H, G, P = 2, 3, 2, 4, 16
+    cache = pkv.Q4Cache(config(n_kv_heads=H, n_q_heads=H * G, page_size=P, n_pages=40))
+    table, lengths = torch.full((S, 12), -1, **INTS).cuda(), torch.zeros(S, **INTS).cuda()
+    ring, counters = cache.new_ring()
+    rows, spans = torch.full((S,), n, **INTS).cuda(), torch.zeros(S, 2, **INTS).cuda()
+    parents, paths, counts = torch.full((S, n), -1, **INTS).cuda(), torch.zeros(S, 1, **INTS).cuda(), torch.ones(S, **INTS).cuda()
+    gen = torch.Generator().manual_seed(3)
+    k, v, q = (rows_of(gen, S * n, h, 128, BF16, False).view(S, n, h, 128).cuda() for h in (H, H, H * G))
+
+    def step():
+        p = cache.plan(table, lengths, rows, spans, ring, counters, S * n, window=20, sinks=2)
+        cache.append_kv(table, p.lengths, k, v)
+        masks, _ = cache.tree_masks(parents, p.lengths, window=20, sinks=2)
+        return (cache.attention(table, p.lengths, q, tree=masks, window=20, sinks=2), cache.attention(table, p.lengths, q, window=2),
+                cache.keep_rows(table, p.lengths, paths, counts, n))
+
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        outs = step()
+    g.replay()
+    torch.cuda.synchronize()
+    assert outs[2].tolist() == [1, 1]
+    for s in range(S):
+        K, V = quantised(k[s].cpu(), 32), quantised(v[s].cpu(), 32)
+        for out, see in ((outs[0], torch.eye(n, dtype=torch.bool)), (outs[1], window_seen(n, n, 2, 0))):
+            ref, _, tol = attention_seen(q[s].cpu(), K, V, see, 1 / math.sqrt(128), BF16)
+            check(out[s], ref, tol)
+    assert cache.stats() == {"device_timeouts": 0, "bad_pages": 0, "bad_lengths": 0}
+
+
+@pytest.mark.gpu
+def test_in_a_process_whose_first_calls_are_captured():
+    import os
+    import subprocess
+    import sys
+    here = os.path.dirname(os.path.abspath(__file__))
+    r = subprocess.run([sys.executable, "-c", "import test_q4_serve as t; t.captured_first()"], capture_output=True, text=True, timeout=600, cwd=here,
+                       env={**os.environ, "PYTHONPATH": os.pathsep.join([os.path.dirname(here), here])})
+    assert r.returncode == 0, (r.stdout + r.stderr)[-3000:]
+
+
 @pytest.mark.gpu
 def test_in_a_process_without_caches_that_overlap():
     """Kernels are launched differently there (other test files make a page cache whose decodes do not wait): the tests of calls that follow one
