@@ -150,3 +150,41 @@ class Plan:
             if rows[s] < 0:
                 self.lengths[s], self.spans[s] = 0, (0, 0)
         return 0, 0, offsets, positions, slots
+
+
+def attention_precise(q, k, v, group, see, scale, out_type):
+    """q4_precision_reference.attention() - every channel judged by its own group's values, the same roundings counted - for queries that
+    see what `see` says ([n, T] bool, something each).  k, v: as they were written, finite where a query sees them."""
+    from q4_precision_reference import group_scales
+    from q4_reference import quantised
+    info = torch.finfo(out_type)
+    n, hq, d = q.shape
+    T, hk, _ = k.shape
+    some = see.any(0)
+    k, v = (torch.where(some[:, None, None], x, torch.zeros((), dtype=x.dtype)) for x in (k, v))
+    K, V, S = quantised(k, group), quantised(v, group), group_scales(v, group)
+    q = q.to(torch.float64)
+    to2 = scale * math.log2(math.e)
+    out, tol = torch.empty(n, hq, d, dtype=torch.float64), torch.empty(n, hq, d, dtype=torch.float64)
+    assert see.any(-1).all()
+    seen = see.to(torch.float64)
+    count = seen.sum(-1, keepdim=True)
+    runs = torch.nn.functional.pad(see, (0, -T % 16)).view(n, -1, 16).any(-1).sum(-1, keepdim=True).to(torch.float64)
+    for h in range(hq):
+        kk, vv, ss = (x[:, h // (hq // hk)] for x in (K, V, S))
+        s = ((q[:, h] @ kk.T) * to2).masked_fill(~see, -math.inf)
+        w = torch.exp2(s - s.amax(-1, keepdim=True))
+        l = w.sum(-1, keepdim=True)
+        out[:, h] = w @ vv / l
+        A = w @ vv.abs() / l
+        star = ss.amax(-1)
+        per_group = torch.stack([(w * ss[:, i]).amax(-1) for i in range(ss.shape[1])], -1) / l
+        own = (7 * 2.0 ** -26 * count * per_group).repeat_interleave(group, -1)
+        ratio = vv.abs() / star.clamp(min=1e-300)[:, None]
+        alike = 2.0 ** -25 * ((w * star).amax(-1, keepdim=True) / l) * (seen @ ratio)
+        sums = (119 * 2.0 ** -20 * runs * (w @ ss) / l).repeat_interleave(group, -1)
+        size = (((q[:, h].abs() @ kk.abs().T) * to2) * seen).amax(-1, keepdim=True)
+        ds = (2.0 ** -20 * d / 16 + 2.0 ** -23 * d / group) * size + 2.0 ** -22 * (size + 64)
+        tol[:, h] = (info.eps / 2 * out[:, h].abs().clamp(min=info.smallest_normal) + (2.0 ** -11 + 2.0 ** -19 + 2 * ds) * A +
+                     torch.maximum(own, alike) + sums)
+    return out, tol
