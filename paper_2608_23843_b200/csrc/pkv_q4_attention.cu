@@ -239,6 +239,7 @@ __device__ __forceinline__ void q4_advance(const Q4AttentionArgs &a, int rows_pe
     }
 }
 
+// (.aligned: the warp has to be converged, so a __syncwarp() comes before them wherever its lanes may have gone different ways)
 __device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
 __device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
 __device__ __forceinline__ uint32_t cluster_at(uint32_t at, int rank) {      // the same place in another CTA's shared memory
@@ -491,7 +492,8 @@ __global__ void __launch_bounds__(Q4Shape<D, NG, NT, kSmall>::kThreads, q4_ctas_
     }
 
     const int v_at[4] = {q4_v_chunk(D, 2 * c, g), q4_v_chunk(D, 2 * c + 1, g), q4_v_chunk(D, 2 * c + 8, g), q4_v_chunk(D, 2 * c + 9, g)};
-    auto consumers_sync = [] { asm volatile("bar.sync 1, %0;" ::"n"(32 * kCons) : "memory"); };
+    // (bar.sync asks for converged warps, and the loops before it may end with some lanes of a warp in their last round)
+    auto consumers_sync = [] { __syncwarp(); asm volatile("bar.sync 1, %0;" ::"n"(32 * kCons) : "memory"); };
     int at = warp;                                             // this warp's next unit, within the CTA's units
     int seg_lo = 0;                                            // the segment's first unit, within the CTA's units
     int st = warp, phase = 0;                                  // its stage and the parity of that use
@@ -1028,6 +1030,7 @@ __global__ void __launch_bounds__(Q4Shape<D, NG, NT, kSmall>::kThreads, q4_ctas_
                 write(r, ch, M, L, acc);
             }
             if (kSmall && cluster > 1) {                       // this CTA's channels of all parts, in order
+                __syncwarp();                                  // (rows_here * D / 4 states need not fill the last round's warps)
                 cluster_arrive();
                 cluster_wait();
                 const int own = D / cluster;
