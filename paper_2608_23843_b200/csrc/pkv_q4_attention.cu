@@ -331,9 +331,9 @@ __global__ void __launch_bounds__(Q4Shape<D, NG, NT, kSmall>::kThreads, q4_ctas_
     }
     // (no more CTAs than there are units for a warp of each; the launch could only estimate that)
     const int n_ctas = (int)min((long long)grid, max(1LL, a_whole ? total : total / (kCons + kSegCost)));
-    // (b * total / n without a 64-bit division where the total has 31 bits)
+    // (b * total / n without a 64-bit division where the total has 31 bits and r * b below, less than n squared, 32: kSmall has up to 2 * 65535 CTAs)
     auto share = [&](long long b) -> long long {
-        if (total >> 31) return total * b / n_ctas;
+        if (total >> 31 || n_ctas > 65536) return total * b / n_ctas;
         const unsigned q = (unsigned)total / (unsigned)n_ctas, r = (unsigned)total % (unsigned)n_ctas;
         return (long long)q * b + r * (unsigned)b / (unsigned)n_ctas;
     };

@@ -4,8 +4,8 @@ import pytest
 import torch
 
 from paper_2608_23843_b200 import pkv
-from q4_select_reference import window_seen
-from test_q4_cache import BF16, FP16, Filled, check
+from q4_select_reference import attention_seen, window_seen
+from test_q4_cache import BF16, FP16, INTS, Filled, check
 from test_q4_serve import seen_by
 
 
@@ -26,4 +26,28 @@ def test_clusters_join_any_number_of_rows(dtype, d, g, G, S, T, W, n_ctas, clust
         ref, _, tol = seen_by(f, qs[s], s, window_seen(f.lens[s], 1, W, 3))
         check(out[s], ref, tol)
         check(state[s][..., :d] / state[s][..., d + 1:], ref, tol)
+    f.clean()
+
+
+# ---- more CTAs than 16 bits count ----------------------------------------------------------------------------------------
+@pytest.mark.gpu
+@pytest.mark.parametrize("S, H, n_ctas", [(50000, 3, 40000), (65535, 3, 65535), (65535, 2, 65535)])
+def test_windows_on_more_ctas_than_16_bits_count(S, H, n_ctas):
+    """Segments that do not divide among the CTAs, on grids beyond 65536: each is worked on once, none is left out.  All sequences
+    read the same page, and every 320 the same positions with the same queries."""
+    f = Filled([64], H=H, G=1, n_ctas=n_ctas)
+    kernel, grid, cluster = pkv.pkv_q4_attention_route(f.cache.handle, S, 1, 64, 40, 2)
+    assert kernel == 2 and cluster == 1 and grid == min(2 * n_ctas, S * H) and grid > 65536
+    qs = f.queries([1] * 5)
+    lens = [1 + s % 64 for s in range(320)]
+    repeat = lambda x: x.repeat(-(-S // 320), *[1] * (x.dim() - 1))[:S].contiguous().cuda()      # noqa: E731
+    q = repeat(torch.stack([qs[s % 5] for s in range(320)]))
+    out = torch.full_like(q, 5.0)
+    f.cache.attention(f.table[:1].expand(S, -1).contiguous(), repeat(torch.tensor(lens, **INTS)), q, out=out, window=40, sinks=2)
+    out = out.cpu()
+    for s in range(320):
+        T = lens[s]
+        ref, _, tol = attention_seen(qs[s % 5], f.K[0][:T], f.V[0][:T], window_seen(T, 1, 40, 2), 128 ** -0.5, BF16)
+        check(out[s], ref, tol)
+    assert torch.equal(out, out[:320].repeat(-(-S // 320), 1, 1, 1)[:S])
     f.clean()
