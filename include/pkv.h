@@ -672,7 +672,7 @@ pkv_status pkv_q4_tree_masks(pkv_q4_cache *c, int32_t n_seqs, const int32_t *len
  *   paths   [device] int32 [n_seqs, max_path], i <= paths[s][i] < n (rows of a path ascend, so that holds for every path of a tree whose
  *           parents come before their children); an entry outside that is skipped (new row i stays as it was) and counted in bad_lengths
  *   counts  [device] int32 [n_seqs]
- *   lengths_out  [device] int32 [n_seqs], not overlapping lengths
+ *   lengths_out  [device] int32 [n_seqs], not overlapping lengths, counts, paths, offsets or page_table (each is read again for every KV head)
  * All layers can be kept in one call, each layer's tables as sequences of their own.  Pages shared between sequences must not be written here.
  */
 pkv_status pkv_q4_keep_rows(pkv_q4_cache *c, int32_t n_seqs, const int32_t *page_table, int32_t max_pages, const int32_t *lengths,

@@ -439,6 +439,18 @@ pkv_status q4_copy(pkv_q4_cache *c, bool write, int32_t n_seqs, const int32_t *t
     return PKV_OK;
 }
 
+// An array of a call; the first ones of a list are written.  Kernels read and write in no particular order, so what is written must not lie on
+// anything else.
+struct Q4Array { const char *name; const void *at; long long bytes; };
+pkv_status q4_apart(pkv_q4_cache *c, const char *what, const Q4Array *x, int n_written, int n) {
+    for (int i = 0; i < n_written; ++i)
+        for (int k = i + 1; k < n; ++k) {
+            const uintptr_t a = (uintptr_t)x[i].at, b = (uintptr_t)x[k].at;
+            if (a && b && a < b + x[k].bytes && b < a + x[i].bytes) return q4_fail(c, PKV_ERR_INVALID_ARG, "%s: %s overlaps %s", what, x[i].name, x[k].name);
+        }
+    return PKV_OK;
+}
+
 // ---- attention: what every form checks -----------------------------------------------------------------------------------
 // What is wrong with a choice of positions, or NULL.
 const char *q4_select_error(const pkv_q4_select &s, int max_q_len) {
@@ -647,8 +659,10 @@ pkv_status pkv_q4_keep_rows(pkv_q4_cache *c, int32_t n_seqs, const int32_t *page
     if (((uintptr_t)paths | (uintptr_t)counts | (uintptr_t)lengths_out) & 3)
         return q4_fail(c, PKV_ERR_INVALID_ARG, "%s: paths, counts and lengths_out must be 4-byte aligned", what);
     if (!c->dry && ((!paths && max_path > 0) || !counts || !lengths_out)) return q4_fail(c, PKV_ERR_INVALID_ARG, "%s: paths, counts or lengths_out is NULL", what);
-    if (lengths && lengths_out < lengths + n_seqs && lengths < lengths_out + n_seqs)
-        return q4_fail(c, PKV_ERR_INVALID_ARG, "%s: lengths_out overlaps lengths", what);
+    const Q4Array arrays[] = {{"lengths_out", lengths_out, 4LL * n_seqs}, {"lengths", lengths, 4LL * n_seqs}, {"counts", counts, 4LL * n_seqs},
+                              {"paths", paths, 4LL * n_seqs * max_path}, {"offsets", offsets, 4LL * (n_seqs + 1)},
+                              {"page_table", page_table, 4LL * n_seqs * max_pages}};
+    if (pkv_status st = q4_apart(c, what, arrays, 1, 6)) return st;
     if (c->dry) return PKV_OK;
     if (pkv_status st = q4_device(c, what)) return st;
     a.geo = c->geo;

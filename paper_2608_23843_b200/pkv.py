@@ -884,7 +884,7 @@ class Q4Cache:
     def keep_rows(self, page_table, lengths, paths, counts, new_rows, offsets=None, out=None):
         """Keeps the accepted ones of the newest rows: row paths[s, i] (int32 [n_seqs, m]) of sequence s becomes its new row i, for
         i < counts[s] (int32 [n_seqs]); rows of a path ascend.  new_rows: how many new rows each sequence has, or with offsets how many
-        the call has.  -> the lengths (out, not overlapping `lengths`, or a new tensor)."""
+        the call has.  -> the lengths (out, a tensor that overlaps none of the others, or a new one)."""
         n_seqs, max_pages = self._seqs(page_table, lengths, offsets)
         dev, most = self._device_index, paths.shape
         if not (len(most) == 2 and most[0] == n_seqs and paths.dtype is counts.dtype is _INT32 and counts.shape == (n_seqs,) and

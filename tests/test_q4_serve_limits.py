@@ -6,7 +6,34 @@ import torch
 from paper_2608_23843_b200 import pkv
 from q4_select_reference import attention_seen, window_seen
 from test_q4_cache import BF16, FP16, INTS, Filled, check
-from test_q4_serve import seen_by
+from test_q4_serve import _dry, offsets_of, seen_by
+
+
+LONGS = dict(dtype=torch.int64)
+
+
+def refused(call):
+    with pytest.raises(pkv.PkvError) as e:
+        call()
+    assert e.value.status == pkv.PKV_ERR_INVALID_ARG and str(e.value)
+    return str(e.value)
+
+
+# ---- arrays on top of one another ----------------------------------------------------------------------------------------
+def test_kept_lengths_must_not_lie_on_what_is_read():
+    """The CTAs of all KV heads read counts, paths, offsets and tables; one of them writes the lengths."""
+    c, t, n, _ = _dry()
+    counts, paths, off = torch.ones_like(n), torch.zeros(3, 2, **INTS), offsets_of([2, 2, 2])
+    for name, out in (("counts", counts), ("paths", paths.flatten()[:3]), ("paths", paths.flatten()[3:]), ("page_table", t[1, 1:]), ("lengths", n)):
+        assert name in refused(lambda: c.keep_rows(t, n, paths, counts, 2, out=out))
+    for at in (0, 1):
+        assert "offsets" in refused(lambda: c.keep_rows(t, n, paths, counts, 6, offsets=off, out=off[at:at + 3]))
+    around = torch.zeros(9, **INTS)                        # side by side is fine
+    assert c.keep_rows(t, around[3:6], paths, around[6:], 2, out=around[:3]).data_ptr() == around.data_ptr()
+    keep = lambda **k: pkv.lib().pkv_q4_keep_rows(*{**dict(h=c.handle, S=3, t=0, mp=4, n=0, rows=6, off=0, path=0, m=2, cnt=0, out=256, st=0), **k}.values())  # noqa: E731
+    assert keep(cnt=244) == keep(cnt=268) == keep(path=232) == keep(off=240) == keep(t=208) == pkv.PKV_OK
+    for k in (dict(cnt=248), dict(cnt=264), dict(path=236), dict(path=264), dict(off=244), dict(off=264), dict(t=212), dict(t=264), dict(n=256), dict(n=248)):
+        assert keep(**k) == pkv.PKV_ERR_INVALID_ARG, k
 
 
 # ---- clusters whose joins leave a warp in part ---------------------------------------------------------------------------
