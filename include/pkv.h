@@ -693,7 +693,7 @@ pkv_status pkv_q4_keep_rows(pkv_q4_cache *c, int32_t n_seqs, const int32_t *page
  * step that failed for want of pages can be repeated after others are done).  Entries of pages that went back keep their numbers.
  * Pages shared between requests need the caller's own count: they go back with each.
  * Written:
- *   lengths_out [n_seqs], spans_out [n_seqs, 2], counters_out [4]  (each may be its input: in place)
+ *   lengths_out [n_seqs], spans_out [n_seqs, 2], counters_out [4]  (each may be its input: in place; nothing else that is written may overlap another array)
  *   offsets   [device] int32 [n_seqs + 1]: prefix sums of the new rows, as the other calls take them
  *   positions [device] int32 [n_rows], or NULL: the position of every new row;   slots [device] int64 [n_rows], or NULL: page * P + row in the page (-1: no
  *             such page).  n_rows bounds the step's rows; places behind the last row are left as they were

@@ -702,6 +702,14 @@ pkv_status pkv_q4_plan(pkv_q4_cache *c, int32_t n_seqs, int32_t *page_table, int
     if (!c->dry && (!page_table || !lengths || !rows || !spans || !ring || !counters || !lengths_out || !spans_out || !counters_out || !offsets))
         return q4_fail(c, PKV_ERR_INVALID_ARG, "%s: only positions and slots may be NULL", what);
     const long long need = q4_plan_workspace(n_seqs, n_rows);
+    // (in place is the same array, not a part of it: a thread reads its own request before it writes it)
+    const Q4Array arrays[] = {{"page_table", page_table, 4LL * n_seqs * max_pages}, {"ring", ring, 4LL * g.n_pages},
+                              {"lengths_out", lengths_out, 4LL * n_seqs}, {"spans_out", spans_out, 8LL * n_seqs}, {"counters_out", counters_out, 32},
+                              {"offsets", offsets, 4LL * (n_seqs + 1)}, {"positions", positions, 4LL * n_rows}, {"slots", slots, 8LL * n_rows},
+                              {"workspace", need > 0 ? workspace : nullptr, need}, {"rows", rows, 4LL * n_seqs},
+                              {"lengths", lengths == lengths_out ? nullptr : lengths, 4LL * n_seqs}, {"spans", spans == spans_out ? nullptr : spans, 8LL * n_seqs},
+                              {"counters", counters == counters_out ? nullptr : counters, 32}};
+    if (pkv_status st = q4_apart(c, what, arrays, 9, 13)) return st;
     if (!c->dry && need > 0 && (!workspace || workspace_bytes < need || ((uintptr_t)workspace & 15)))
         return q4_fail(c, PKV_ERR_INVALID_ARG, "%s: the workspace needs %lld bytes, 16-byte aligned", what, need);
     if (c->dry) return PKV_OK;

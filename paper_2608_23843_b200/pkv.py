@@ -914,7 +914,7 @@ class Q4Cache:
         """Plans a step on the device (see pkv_q4_plan in include/pkv.h): rows int32 [n_seqs] new rows for each request, -1 where it is
         done; spans int32 [n_seqs, 2] the table entries it holds; ring, counters: free pages, see new_ring(); n_rows: a bound of the new rows
         in all.  Writes new entries into page_table and returned pages into ring.  -> Q4Plan of new tensors, or `out`, whose
-        lengths, spans and counters may be the ones given (in place).  Where pages are missing or requests make no sense nothing is done: counters[2:]."""
+        lengths, spans and counters may be the ones given (in place; no other tensors may overlap).  Where pages are missing or requests make no sense nothing is done: counters[2:]."""
         n_seqs, max_pages = self._seqs(page_table, lengths, None)
         self._positions(window, sinks)
         dev, one = self._device_index, (n_seqs,)

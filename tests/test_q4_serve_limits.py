@@ -36,6 +36,29 @@ def test_kept_lengths_must_not_lie_on_what_is_read():
         assert keep(**k) == pkv.PKV_ERR_INVALID_ARG, k
 
 
+def test_what_a_plan_writes_must_not_lie_on_other_arrays():
+    """Only lengths, spans and counters may be written in place, as whole arrays."""
+    c, t, n, _ = _dry()
+    spans, (ring, counters) = torch.zeros(3, 2, **INTS), c.new_ring()
+    rows = torch.ones_like(n)
+    plan = lambda out, n_rows=4: c.plan(t, n, rows, spans, ring, counters, n_rows, out=out)      # noqa: E731
+    out = plan(None)
+    plan(out._replace(lengths=n, spans=spans, counters=counters))
+    both = torch.zeros(6, **INTS)
+    longs = torch.zeros(8, **LONGS)
+    for bad in (dict(lengths=rows), dict(lengths=spans.flatten()[1:4]), dict(spans=t.flatten()[:6].view(3, 2)),
+                dict(offsets=t[1]), dict(offsets=ring[:4]), dict(offsets=ring[12:]), dict(positions=ring[3:7]), dict(positions=t[2]),
+                dict(lengths=both[:3], spans=both.view(3, 2)), dict(positions=out.offsets), dict(slots=counters), dict(counters=longs[1:5], slots=longs[4:])):
+        refused(lambda: plan(out._replace(**bad)))
+    lengths = torch.zeros(4, **INTS)                       # neither in place nor apart
+    refused(lambda: c.plan(t, lengths[:3], rows, spans, ring, counters, 4, out=out._replace(lengths=lengths[1:])))
+    plan = lambda **k: pkv.lib().pkv_q4_plan(*{**dict(h=c.handle, S=3, t=0, mp=4, n=0, r=0, sp=0, ring=0, cnt=0, W=0, sinks=0, no=0, so=0, co=0, off=0, rows=6, pos=0,      # noqa: E731
+                                                      slot=0, work=0, wb=0, st=0), **k}.values())
+    assert plan(n=256, no=256, sp=512, so=512, cnt=768, co=768) == pkv.PKV_OK
+    assert plan(S=2000, work=4096, wb=1 << 20) == pkv.PKV_OK
+    assert plan(S=2000, work=4096, wb=1 << 20, slot=4096 + 64) == pkv.PKV_ERR_INVALID_ARG
+
+
 # ---- clusters whose joins leave a warp in part ---------------------------------------------------------------------------
 # A segment's states are rows * d / 4 pieces for 96 threads, and rows * d / 4 / cluster for each CTA of a cluster: these end inside a warp.
 @pytest.mark.gpu
