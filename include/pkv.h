@@ -659,6 +659,7 @@ pkv_status pkv_q4_attention_route(const pkv_q4_cache *c, int32_t n_seqs, int32_t
  *   tree    [device] uint64 [n_rows, tree_words]: bits of the row itself and its ancestors.  With window = W > 0 only of those
  *           within the window of the row's place (the W - 1 nearest ancestors), and of those whose place C + depth lies below `sinks`
  *   depths  [device] int32 [n_rows], or NULL: the number of ancestors.  C + depth is the position of a drafted token (for rotary embeddings)
+ * Neither may overlap the other, parents, lengths or offsets.
  * lengths may be NULL where window or sinks is 0.  Rows that belong to no sequence are left as they were.  max_q_len as in the attention call (rows of a
  * sequence beyond it are left as they were, and counted).
  */

@@ -490,6 +490,12 @@ pkv_status q4_attend(pkv_q4_cache *c, const char *what, int32_t n_seqs, const in
     const long long need = q4_attention_workspace(g, n_seqs, max_q_len, max_len, sel);
     if (!c->dry && need > 0 && (!workspace || workspace_bytes < need || ((uintptr_t)workspace & 15)))
         return q4_fail(c, PKV_ERR_INVALID_ARG, "%s: the workspace needs %lld bytes, 16-byte aligned", what, need);
+    if (select && select->tree) {                      // (read by all KV heads, while the first of them write)
+        const long long heads = (long long)n_rows * g.n_q_heads;
+        const Q4Array arrays[] = {{"tree", select->tree, 8LL * n_rows * select->tree_words}, {"state", state, heads * (g.head_dim + 2) * 4}, {"workspace", need > 0 ? workspace : nullptr, need},
+                                  {"out", out, 2 * ((n_rows - 1) * out_row_stride + (g.n_q_heads - 1) * out_head_stride + g.head_dim)}};
+        if (pkv_status st = q4_apart(c, what, arrays, 1, 4)) return st;
+    }
     if (c->dry) return PKV_OK;
     if (pkv_status st = q4_device(c, what)) return st;
     a.geo = g;
@@ -632,6 +638,9 @@ pkv_status pkv_q4_tree_masks(pkv_q4_cache *c, int32_t n_seqs, const int32_t *len
     if (tree_words < 1 || tree_words < (max_q_len + 63LL) / 64) return q4_fail(c, PKV_ERR_INVALID_ARG, "%s: tree_words %d out of range", what, tree_words);
     if (((uintptr_t)parents | (uintptr_t)depths) & 3) return q4_fail(c, PKV_ERR_INVALID_ARG, "%s: parents and depths must be 4-byte aligned", what);
     if (!c->dry && n_rows > 0 && (!parents || !tree)) return q4_fail(c, PKV_ERR_INVALID_ARG, "%s: parents or tree is NULL", what);
+    const Q4Array arrays[] = {{"tree", tree, 8LL * n_rows * tree_words}, {"depths", depths, 4LL * n_rows}, {"parents", parents, 4LL * n_rows},
+                              {"lengths", far ? lengths : nullptr, 4LL * n_seqs}, {"offsets", offsets, 4LL * (n_seqs + 1)}};
+    if (pkv_status st = q4_apart(c, what, arrays, 2, 5)) return st;
     if (c->dry || n_rows == 0 || max_q_len == 0) return PKV_OK;
     if (pkv_status st = q4_device(c, what)) return st;
     if (!far) a.rows.lengths = nullptr;

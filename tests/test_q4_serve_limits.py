@@ -1,5 +1,7 @@
 """Serving from the 4-bit cache at its limits: rows that leave a warp in part, arrays that lie on top of one another, more CTAs than 16 bits count,
 numbers that are none, bindings that were not built."""
+import ctypes
+
 import pytest
 import torch
 
@@ -7,7 +9,6 @@ from paper_2608_23843_b200 import pkv
 from q4_select_reference import attention_seen, window_seen
 from test_q4_cache import BF16, FP16, INTS, Filled, check
 from test_q4_serve import _dry, offsets_of, seen_by
-
 
 LONGS = dict(dtype=torch.int64)
 
@@ -57,6 +58,34 @@ def test_what_a_plan_writes_must_not_lie_on_other_arrays():
     assert plan(n=256, no=256, sp=512, so=512, cnt=768, co=768) == pkv.PKV_OK
     assert plan(S=2000, work=4096, wb=1 << 20) == pkv.PKV_OK
     assert plan(S=2000, work=4096, wb=1 << 20, slot=4096 + 64) == pkv.PKV_ERR_INVALID_ARG
+
+
+def test_masks_must_not_lie_on_what_is_read_or_written_with_them():
+    """CTAs read the parents of rows that others write masks and depths of; an attention call's heads read the masks one after another."""
+    c, t, n, q = _dry()
+    L, bad = pkv.lib(), pkv.PKV_ERR_INVALID_ARG
+    masks = lambda **k: L.pkv_q4_tree_masks(*{**dict(h=c.handle, S=3, n=0, rows=6, off=0, most=2, par=0, W=4, sinks=2, tree=0, words=2, dep=0, st=0), **k}.values())  # noqa: E731
+    assert masks(tree=1024, dep=1120, par=1000) == masks(dep=256, par=280) == masks(tree=1024, n=1012, off=1120) == pkv.PKV_OK
+    assert masks(tree=1024, n=1024, W=0, sinks=0) == pkv.PKV_OK                         # (not looked at)
+    for k in (dict(tree=1024, dep=1116), dict(tree=1024, par=1004), dict(dep=256, par=256), dict(dep=256, par=276), dict(tree=1024, n=1016), dict(dep=256, off=244), dict(dep=256, n=276)):
+        assert masks(**k) == bad, k
+    words = torch.zeros(3, 2, 1, **LONGS)
+    c.attention(t, n, q, tree=words)
+    state = torch.zeros(3 * 2 * 8 * 130 + 12)
+    tail = state[-12:].view(torch.int64).view(3, 2, 1)
+    assert c.attention_partial(t, n, q, state=state[:-12].view(3, 2, 8, 130), tree=tail).shape == (3, 2, 8, 130)
+    assert "state" in refused(lambda: c.attention_partial(t, n, q, state=state[:-12].view(3, 2, 8, 130), tree=state[-14:-2].view(torch.int64).view(3, 2, 1)))
+    out = torch.zeros(6 * 1024 + 32, dtype=q.dtype)
+    assert out.data_ptr() % 16 == 0
+    there = out[:6144].view(3, 2, 8, 128)
+    assert c.attention(t, n, q, out=there, tree=out[6144:6168].view(torch.int64).view(3, 2, 1)) is there
+    assert "out" in refused(lambda: c.attention(t, n, q, out=there, tree=out[6140:6164].view(torch.int64).view(3, 2, 1)))
+    room = ctypes.c_int64()                                # a call that joins states needs a workspace
+    sel = pkv.PkvQ4Select(0, 0, 1 << 30, 1)
+    assert L.pkv_q4_attention_select_workspace(c.handle, 1, 64, 60000, ctypes.byref(sel), ctypes.byref(room)) == pkv.PKV_OK and room.value > 0
+    call = lambda work: L.pkv_q4_attention_select(c.handle, 1, 0, 1000, 0, 64, 0, 64, 60000, ctypes.byref(sel), 0, 1024, 128, 0, 1024, 128, 0, work, room.value, 0)      # noqa: E731
+    assert call((1 << 30) + 64 * 8) == call(0) == pkv.PKV_OK
+    assert call((1 << 30) + 63 * 8) == call((1 << 30) - room.value + 8) == bad
 
 
 # ---- clusters whose joins leave a warp in part ---------------------------------------------------------------------------
