@@ -5,18 +5,18 @@
 
 #include "pkv.h"
 
-/* n numbers; those whose bit is set in `ints` have to fit 32 bits */
-static int numbers(PyObject *const *args, Py_ssize_t n_args, long long *v, int n, unsigned ints) {
+/* One number for each letter of `kinds`: p a pointer (None is NULL), i of 32 bits, l of 64 */
+static int numbers(PyObject *const *args, Py_ssize_t n_args, long long *v, const char *kinds, int n) {
     if (n_args != n) {
         PyErr_Format(PyExc_TypeError, "%d arguments expected, not %zd", n, n_args);
         return 0;
     }
     for (int i = 0; i < n; ++i) {
         v[i] = 0;
-        if (args[i] == Py_None) continue;
+        if (args[i] == Py_None && kinds[i] == 'p') continue;
         v[i] = PyLong_AsLongLong(args[i]);
         if (v[i] == -1 && PyErr_Occurred()) return 0;
-        if ((ints >> i & 1u) && (v[i] > INT32_MAX || v[i] < INT32_MIN)) {
+        if (kinds[i] == 'i' && (v[i] > INT32_MAX || v[i] < INT32_MIN)) {
             PyErr_Format(PyExc_OverflowError, "argument %d does not fit 32 bits", i);
             return 0;
         }
@@ -27,26 +27,25 @@ static int numbers(PyObject *const *args, Py_ssize_t n_args, long long *v, int n
 #define AT(type, i) ((type *)(intptr_t)v[i])
 #define I32(i) ((int32_t)v[i])
 #define CACHE AT(pkv_q4_cache, 0)
-#define BITS2(a, b) (1u << (a) | 1u << (b))
-#define FUNCTION(name, n, ints, call)                                                          \
+#define FUNCTION(name, kinds, call)                                                            \
     static PyObject *name(PyObject *self, PyObject *const *args, Py_ssize_t n_args) {          \
-        long long v[n];                                                                        \
+        long long v[sizeof kinds - 1];                                                         \
         pkv_status st;                                                                         \
         (void)self;                                                                            \
-        if (!numbers(args, n_args, v, n, ints)) return NULL;                                   \
+        if (!numbers(args, n_args, v, kinds, (int)sizeof kinds - 1)) return NULL;              \
         Py_BEGIN_ALLOW_THREADS st = call;                                                      \
         Py_END_ALLOW_THREADS return PyLong_FromLong(st);                                       \
     }
 
 /* handle, n_seqs, page_table, max_pages, lengths, n_rows, offsets, k, row, head, v, row, head, stream */
-FUNCTION(append_kv, 14, BITS2(1, 3),
+FUNCTION(append_kv, "pipiplppllpllp",
          pkv_q4_append_kv(CACHE, I32(1), AT(const int32_t, 2), I32(3), AT(const int32_t, 4), v[5], AT(const int32_t, 6), AT(const void, 7), v[8], v[9],
                           AT(const void, 10), v[11], v[12], AT(void, 13)))
-FUNCTION(read_kv, 14, BITS2(1, 3),
+FUNCTION(read_kv, "pipiplppllpllp",
          pkv_q4_read_kv(CACHE, I32(1), AT(const int32_t, 2), I32(3), AT(const int32_t, 4), v[5], AT(const int32_t, 6), AT(void, 7), v[8], v[9],
                         AT(void, 10), v[11], v[12], AT(void, 13)))
 /* handle, n_seqs, page_table, max_pages, lengths, n_rows, offsets, max_q_len, max_len, q, row, head, out, row, head, state, workspace, bytes, stream */
-FUNCTION(attention, 19, BITS2(1, 3) | BITS2(7, 8),
+FUNCTION(attention, "pipiplpiipllpllpplp",
          pkv_q4_attention(CACHE, I32(1), AT(const int32_t, 2), I32(3), AT(const int32_t, 4), v[5], AT(const int32_t, 6), I32(7), I32(8),
                           AT(const void, 9), v[10], v[11], AT(void, 12), v[13], v[14], AT(float, 15), AT(void, 16), v[17], AT(void, 18)))
 /* ... as above, then window, sinks, tree, tree_words */
@@ -55,18 +54,18 @@ static pkv_status select_call(const long long *v) {
     return pkv_q4_attention_select(CACHE, I32(1), AT(const int32_t, 2), I32(3), AT(const int32_t, 4), v[5], AT(const int32_t, 6), I32(7), I32(8), &sel,
                                    AT(const void, 9), v[10], v[11], AT(void, 12), v[13], v[14], AT(float, 15), AT(void, 16), v[17], AT(void, 18));
 }
-FUNCTION(attention_select, 23, BITS2(1, 3) | BITS2(7, 8) | BITS2(19, 20) | 1u << 22, select_call(v))
+FUNCTION(attention_select, "pipiplpiipllpllpplpiipi", select_call(v))
 /* handle, n_seqs, lengths, n_rows, offsets, max_q_len, parents, window, sinks, tree, tree_words, depths, stream */
-FUNCTION(tree_masks, 13, BITS2(1, 5) | BITS2(7, 8) | 1u << 10,
+FUNCTION(tree_masks, "piplpipiipipp",
          pkv_q4_tree_masks(CACHE, I32(1), AT(const int32_t, 2), v[3], AT(const int32_t, 4), I32(5), AT(const int32_t, 6), I32(7), I32(8),
                            AT(uint64_t, 9), I32(10), AT(int32_t, 11), AT(void, 12)))
 /* handle, n_seqs, page_table, max_pages, lengths, n_rows, offsets, paths, max_path, counts, lengths_out, stream */
-FUNCTION(keep_rows, 12, BITS2(1, 3) | 1u << 8,
+FUNCTION(keep_rows, "pipiplppippp",
          pkv_q4_keep_rows(CACHE, I32(1), AT(const int32_t, 2), I32(3), AT(const int32_t, 4), v[5], AT(const int32_t, 6), AT(const int32_t, 7), I32(8),
                           AT(const int32_t, 9), AT(int32_t, 10), AT(void, 11)))
 /* handle, n_seqs, page_table, max_pages, lengths, rows, spans, ring, counters, window, sinks, lengths_out, spans_out, counters_out, offsets, n_rows,
  * positions, slots, workspace, bytes, stream */
-FUNCTION(plan, 21, BITS2(1, 3) | BITS2(9, 10),
+FUNCTION(plan, "pipipppppiipppplppplp",
          pkv_q4_plan(CACHE, I32(1), AT(int32_t, 2), I32(3), AT(const int32_t, 4), AT(const int32_t, 5), AT(const int32_t, 6), AT(int32_t, 7),
                      AT(const int64_t, 8), I32(9), I32(10), AT(int32_t, 11), AT(int32_t, 12), AT(int64_t, 13), AT(int32_t, 14), v[15], AT(int32_t, 16),
                      AT(int64_t, 17), AT(void, 18), v[19], AT(void, 20)))

@@ -88,6 +88,31 @@ def test_masks_must_not_lie_on_what_is_read_or_written_with_them():
     assert call((1 << 30) + 63 * 8) == call((1 << 30) - room.value + 8) == bad
 
 
+# ---- numbers that are none -----------------------------------------------------------------------------------------------
+def test_none_is_no_number():
+    """None may stand for a pointer; as a number it would arrive as 0, and rows would be kept of none."""
+    c, t, n, _ = _dry()
+    off = offsets_of([2, 2, 2])
+    refused(lambda: c.keep_rows(t, n, torch.zeros(3, 2, **INTS), n, None, offsets=off))
+    h = c.handle.value
+    kinds = dict(append_kv="pipiplppllpllp", attention="pipiplpiipllpllpplp", attention_select="pipiplpiipllpllpplpiipi", tree_masks="piplpipiipipp",
+                 keep_rows="pipiplppippp", plan="pipipppppiipppplppplp")
+    good = dict(append_kv=(h, 3, 0, 4, 0, 6, 0, 0, 256, 128, 0, 256, 128, 0), attention=(h, 3, 0, 4, 0, 6, 0, 2, 0, 0, 1024, 128, 0, 1024, 128, 0, 0, 0, 0),
+                attention_select=(h, 3, 0, 4, 0, 6, 0, 2, 0, 0, 1024, 128, 0, 1024, 128, 0, 0, 0, 0, 9, 4, 0, 0),
+                tree_masks=(h, 3, 0, 6, 0, 2, 0, 0, 0, 0, 1, 0, 0), keep_rows=(h, 3, 0, 4, 0, 6, 0, 0, 2, 0, 0, 0), plan=(h, 3, 0, 4) + (0,) * 11 + (6,) + (0,) * 5)
+    kinds["read_kv"], good["read_kv"] = kinds["append_kv"], good["append_kv"]
+    for name, args in good.items():
+        fn = getattr(pkv._calls(), name)
+        assert len(args) == len(kinds[name]) and fn(*args) == pkv.PKV_OK, name
+        for i, kind in enumerate(kinds[name]):
+            with_none = args[:i] + (None,) + args[i + 1:]
+            if kind == "p":
+                assert fn(*with_none) == (pkv.PKV_OK if i else pkv.PKV_ERR_INVALID_ARG), (name, i)
+            else:
+                with pytest.raises(TypeError):
+                    fn(*with_none)
+
+
 # ---- clusters whose joins leave a warp in part ---------------------------------------------------------------------------
 # A segment's states are rows * d / 4 pieces for 96 threads, and rows * d / 4 / cluster for each CTA of a cluster: these end inside a warp.
 @pytest.mark.gpu
