@@ -801,8 +801,8 @@ class Q4Cache:
         words = 0
         if tree is not None:
             if not (tree.dim() == q.dim() - 1 and tree.shape[:-1] == q.shape[:-2] and tree.dtype is _INT64 and tree.get_device() == self._device_index and
-                    tree.is_contiguous()):
-                self._fail("tree must be a contiguous int64 tensor %r on %s" % ([*q.shape[:-2], "words"], self.device))
+                    tree.is_contiguous() and tree.shape[-1] > 0):
+                self._fail("tree must be a contiguous int64 tensor %r on %s, of a word at least" % ([*q.shape[:-2], "words"], self.device))
             words = tree.shape[-1]
         part = window or sinks or tree is not None
         if part:

@@ -113,6 +113,19 @@ def test_none_is_no_number():
                     fn(*with_none)
 
 
+# ---- refusals that must not depend on what was called before -------------------------------------------------------------
+@pytest.mark.parametrize("before", [False, True])
+@pytest.mark.parametrize("kw", [dict(), dict(window=5), dict(window=5, sinks=2)])
+def test_masks_without_words_are_refused_whatever_was_called_before(before, kw):
+    """(their data pointer is NULL, which would make the call a causal one)"""
+    c, t, n, q = _dry()
+    if before:
+        c.attention(t, n, q, **kw)
+    for call in (c.attention, c.attention_partial):
+        assert "tree" in refused(lambda: call(t, n, q, tree=torch.zeros(3, 2, 0, **LONGS), **kw))
+        assert "tree" in refused(lambda: call(t, n, q[:, :0], tree=torch.zeros(3, 0, 0, **LONGS), **kw))
+
+
 # ---- clusters whose joins leave a warp in part ---------------------------------------------------------------------------
 # A segment's states are rows * d / 4 pieces for 96 threads, and rows * d / 4 / cluster for each CTA of a cluster: these end inside a warp.
 @pytest.mark.gpu
