@@ -903,11 +903,13 @@ class Q4Cache:
     def new_ring(self, pages=None):
         """Free pages (default: all of the pool) as plan() takes them: (ring int32 [n_pages], counters int64 [4])."""
         n = self.cfg.n_pages
-        pages = torch.arange(n, dtype=_INT32) if pages is None else torch.as_tensor(pages, dtype=_INT32).flatten().cpu()
-        if pages.numel() > n or (pages.numel() and not (0 <= int(pages.min()) and int(pages.max()) < n)) or pages.unique().numel() != pages.numel():
+        pages = torch.arange(n) if pages is None else torch.as_tensor(pages).flatten().cpu()
+        whole = pages.numel() == 0 or not (pages.is_floating_point() or pages.is_complex() or pages.dtype is torch.bool)
+        pages = pages.to(_INT64)                         # (in 32 bits 2^32 + 4 would be 4)
+        if not whole or pages.numel() > n or (pages.numel() and not (0 <= int(pages.min()) and int(pages.max()) < n)) or pages.unique().numel() != pages.numel():
             self._fail("pages must be different page numbers of the pool")
         ring = torch.full((n,), -1, dtype=_INT32)
-        ring[:pages.numel()] = pages
+        ring[:pages.numel()] = pages.to(_INT32)
         return ring.to(self.device), torch.tensor([0, pages.numel(), 0, 0], dtype=_INT64, device=self.device)
 
     def plan(self, page_table, lengths, rows, spans, ring, counters, n_rows, window=0, sinks=0, out=None):

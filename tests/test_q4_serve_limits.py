@@ -113,6 +113,17 @@ def test_none_is_no_number():
                     fn(*with_none)
 
 
+def test_pages_of_a_ring_are_whole_numbers_below_the_pools():
+    c = _dry()[0]
+    for pages in ([0.5, 1.7], [1.0, 2.0], [True, False], torch.tensor([2 ** 32 + 4]), [2 ** 32 + 4], torch.tensor([-2 ** 32 + 4]), [-1], [16], [3, 3]):
+        assert "page numbers" in refused(lambda: c.new_ring(pages))
+    for pages in ([7, 3], torch.tensor([7, 3]), torch.tensor([[7], [3]], dtype=torch.int16), torch.tensor([7, 3], dtype=torch.uint8), torch.tensor([7, 3], dtype=torch.uint32)):
+        ring, counters = c.new_ring(pages)
+        assert ring.tolist() == [7, 3] + [-1] * 14 and counters.tolist() == [0, 2, 0, 0] and ring.dtype == torch.int32
+    for pages in ([], torch.empty(0)):
+        assert c.new_ring(pages)[1].tolist() == [0, 0, 0, 0]
+
+
 # ---- refusals that must not depend on what was called before -------------------------------------------------------------
 @pytest.mark.parametrize("before", [False, True])
 @pytest.mark.parametrize("kw", [dict(), dict(window=5), dict(window=5, sinks=2)])
