@@ -8,6 +8,7 @@ There is no CPU fallback: if the library has not been built, loading fails.
 """
 import ctypes
 import os
+from operator import index
 from typing import NamedTuple
 
 import torch
@@ -842,8 +843,19 @@ class Q4Cache:
                    None if work is None else work.data_ptr(), size, self._stream())
 
     def _positions(self, window, sinks):
-        if not (0 <= window < 1 << 31 and 0 <= sinks < 1 << 31):      # (beyond 32 bits they would arrive as other numbers)
-            self._fail("window and sinks must be from 0 to 2^31 - 1")
+        self._whole("window", window, (1 << 31) - 1)      # (beyond 32 bits they would arrive as other numbers)
+        self._whole("sinks", sinks, (1 << 31) - 1)
+
+    def _whole(self, name, x, most):
+        """A size, from 0 to `most`: looked at before anything is allocated by it."""
+        if type(x) is int and 0 <= x <= most:
+            return
+        try:
+            ok = 0 <= index(x) <= most
+        except TypeError:
+            ok = False
+        if not ok:
+            self._fail("%s must be a whole number from 0 to %d, not %r" % (name, most, x))
 
     def _ints(self, name, t, shape, dtype=_INT32):
         if not (t.shape == shape and t.dtype is dtype and t.get_device() == self._device_index and t.is_contiguous()):
@@ -866,6 +878,7 @@ class Q4Cache:
             n_seqs = offsets.numel() - 1
             if max_q_len is None:
                 max_q_len = n
+            self._whole("max_q_len", max_q_len, n)
             self._ints("offsets", offsets, (n_seqs + 1,))
         if not (parents.dtype is _INT32 and parents.get_device() == dev and parents.is_contiguous()):
             self._ints("parents", parents, shape)
@@ -919,6 +932,7 @@ class Q4Cache:
         lengths, spans and counters may be the ones given (in place; no other tensors may overlap).  Where pages are missing or requests make no sense nothing is done: counters[2:]."""
         n_seqs, max_pages = self._seqs(page_table, lengths, None)
         self._positions(window, sinks)
+        self._whole("n_rows", n_rows, 0x3fffffff)
         dev, one = self._device_index, (n_seqs,)
         if not (rows.dtype is spans.dtype is ring.dtype is _INT32 and counters.dtype is _INT64 and rows.shape == one and spans.shape == (n_seqs, 2) and
                 ring.shape == (self.cfg.n_pages,) and counters.shape == (4,) and

@@ -124,6 +124,25 @@ def test_pages_of_a_ring_are_whole_numbers_below_the_pools():
         assert c.new_ring(pages)[1].tolist() == [0, 0, 0, 0]
 
 
+def test_sizes_are_refused_before_anything_is_allocated_by_them():
+    """... and as other arguments are, not by the allocator or by a comparison."""
+    c, t, n, q = _dry()
+    off, parents, spans = offsets_of([2, 2, 2]), torch.full((6,), -1, **INTS), torch.zeros(3, 2, **INTS)
+    for most in (7, 2 ** 50, -1, 2.0, "2"):
+        assert "max_q_len" in refused(lambda: c.tree_masks(parents, n, off, max_q_len=most))
+    for n_rows in (-1, 2 ** 30, 2 ** 50, 2.0, None):
+        assert "n_rows" in refused(lambda: c.plan(t, n, n, spans, *c.new_ring(), n_rows))
+    for _ in range(2):
+        for bad in (dict(window=4.0), dict(window="4"), dict(window=4, sinks=2.5), dict(window=4, sinks=None), dict(window=None, sinks=3)):
+            for call in (lambda: c.attention(t, n, q, **bad), lambda: c.tree_masks(parents, n, off, **bad), lambda: c.plan(t, n, n, spans, *c.new_ring(), 4, **bad)):
+                assert "whole number" in refused(call)
+        c.attention(t, n, q, window=4, sinks=2)
+    import numpy
+    assert c.tree_masks(parents, n, off, max_q_len=numpy.int64(2), window=numpy.int32(4))[0].shape == (6, 1)
+    assert c.attention(t, n, q, window=numpy.int64(4), sinks=numpy.int16(1)).shape == q.shape
+    assert c.plan(t, n, n, spans, *c.new_ring(), numpy.int64(5)).slots.shape == (5,)
+
+
 # ---- refusals that must not depend on what was called before -------------------------------------------------------------
 @pytest.mark.parametrize("before", [False, True])
 @pytest.mark.parametrize("kw", [dict(), dict(window=5), dict(window=5, sinks=2)])
