@@ -1,18 +1,20 @@
-"""Builds libpkv.so (the C-ABI CUDA library) in-tree with nvcc for sm_100a, and _pkvcall.so, through which the Python binding makes
-the calls of a decode step (a C source against it, gcc)."""
+"""Builds libpkv.so (the C-ABI CUDA library) in-tree with nvcc for sm_100a, and _pkvcall, a module of the interpreter that builds it through
+which the Python binding makes the calls of a decode step (a C source against the library, gcc and Python's headers)."""
 import glob
 import os
 import subprocess
 import sys
 import sysconfig
 import tempfile
+import warnings
 from concurrent.futures import ThreadPoolExecutor
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(_HERE)
 CSRC = os.path.join(_HERE, "csrc")
 LIB = os.path.join(_HERE, "libpkv.so")
-CALL, CALL_SOURCE = os.path.join(_HERE, "_pkvcall.so"), os.path.join(CSRC, "pkv_call.c")
+# (the name has the interpreter's ABI in it: another one neither takes it for its own nor finds it fresh)
+CALL, CALL_SOURCE = os.path.join(_HERE, "_pkvcall" + (sysconfig.get_config_var("EXT_SUFFIX") or ".so")), os.path.join(CSRC, "pkv_call.c")
 NVCC = os.environ.get("NVCC", "/usr/local/cuda/bin/nvcc")
 
 
@@ -21,13 +23,23 @@ def sources():
 
 
 def build_call(force=False):
-    """Compile the binding's calls; returns its path."""
+    """Compile the binding's calls; returns the module's path.  Where that fails (no C compiler, no Python headers) it warns and returns None: the library is
+    complete without, and the binding makes its calls through ctypes."""
     deps = [CALL_SOURCE, os.path.join(ROOT, "include", "pkv.h")]
     if not force and os.path.exists(CALL) and all(os.path.getmtime(f) <= os.path.getmtime(CALL) for f in deps):
         return CALL
     tmp = CALL + ".tmp.%d" % os.getpid()
-    subprocess.run([os.environ.get("CC", "gcc"), "-O2", "-std=c11", "-Wall", "-shared", "-fPIC", "-I", sysconfig.get_path("include"), "-I", os.path.join(ROOT, "include"),
-                    CALL_SOURCE, "-o", tmp, "-L", _HERE, "-l:libpkv.so", "-Wl,-rpath,$ORIGIN"], check=True)
+    old = os.path.join(_HERE, "_pkvcall.so")             # (a name that any interpreter would import)
+    if old != CALL and os.path.exists(old):
+        os.remove(old)
+    try:
+        subprocess.run([os.environ.get("CC", "gcc"), "-O2", "-std=c11", "-Wall", "-shared", "-fPIC", "-I", sysconfig.get_path("include"), "-I", os.path.join(ROOT, "include"),
+                        CALL_SOURCE, "-o", tmp, "-L", _HERE, "-l:libpkv.so", "-Wl,-rpath,$ORIGIN"], check=True)
+    except (OSError, subprocess.CalledProcessError) as e:
+        if os.path.exists(CALL):                         # (of another source: not to be called)
+            os.remove(CALL)
+        warnings.warn("%s was not built (%s): calls of a decode step go through ctypes, 3 us more each" % (os.path.basename(CALL), e))
+        return None
     os.replace(tmp, CALL)
     return CALL
 

@@ -1,4 +1,5 @@
-"""Binding of libpkv.so (see include/pkv.h) by ctypes, and by a small C module for the calls of a decode step: argument marshalling only.
+"""Binding of libpkv.so (see include/pkv.h) by ctypes, and for the calls of a decode step by a small C module where it has been built: argument
+marshalling only.
 
 Module-level functions carry the C names (`pkv_init_cache`, `pkv_append_kv`,
 `pkv_compress_eligible_pages`, `pkv_decode_attention`, ...).  `Cache` is a
@@ -159,16 +160,50 @@ def lib():
     return _lib
 
 
+# The calls of a decode step and their arguments, a letter each: p a pointer (None is NULL), i a number of 32 bits, l one of 64.
+_CALLS = {"append_kv": "pipiplppllpllp", "read_kv": "pipiplppllpllp", "attention": "pipiplpiipllpllpplp", "attention_select": "pipiplpiipllpllpplpiipi",
+          "tree_masks": "piplpipiipipp", "keep_rows": "pipiplppippp", "plan": "pipipppppiipppplppplp"}
 _calls_module = None
 
 
+class _CtypesCalls:
+    """The calls of _pkvcall through ctypes, with the same checks, where that module has not been built for this interpreter."""
+
+    def __init__(self):
+        for name, kinds in _CALLS.items():
+            setattr(self, name, self._checked(kinds, self._select if name == "attention_select" else getattr(lib(), "pkv_q4_" + name)))
+
+    @staticmethod
+    def _checked(kinds, fn):
+        def call(*args):
+            if len(args) != len(kinds):
+                raise TypeError("%d arguments expected, not %d" % (len(kinds), len(args)))
+            for i, (x, kind) in enumerate(zip(args, kinds)):
+                if x is None and kind == "p":
+                    continue
+                bits = 31 if kind == "i" else 63
+                if not -1 << bits <= index(x) < 1 << bits:
+                    raise OverflowError("argument %d does not fit %d bits" % (i, bits + 1))
+            return fn(*args)
+        return call
+
+    @staticmethod
+    def _select(*args):
+        sel = PkvQ4Select(*args[19:])
+        return lib().pkv_q4_attention_select(*args[:9], ctypes.byref(sel), *args[9:19])
+
+
 def _calls():
-    """The calls of a decode step without ctypes (3 us less each): numbers in, a status out.  Raises if they have not been built."""
+    """The calls of a decode step: numbers in, a status out.  By a C module (ctypes takes 3 us more each) if it has been built for this interpreter, and
+    links this library."""
     global _calls_module
     if _calls_module is None:
+        from . import build
         lib()                                            # (says what to do where nothing has been built)
-        from . import _pkvcall
-        _calls_module = _pkvcall
+        built = os.path.exists(build.CALL) and os.path.samefile(LIB_PATH, build.LIB)
+        if built:
+            from . import _pkvcall
+        _calls_module = _pkvcall if built else _CtypesCalls()
     return _calls_module
 
 

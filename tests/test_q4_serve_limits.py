@@ -143,6 +143,86 @@ def test_sizes_are_refused_before_anything_is_allocated_by_them():
     assert c.plan(t, n, n, spans, *c.new_ring(), numpy.int64(5)).slots.shape == (5,)
 
 
+# ---- bindings that were not built ----------------------------------------------------------------------------------------
+def test_the_binding_is_named_for_its_interpreter(tmp_path, monkeypatch):
+    """... so that another one does not load it; without a C compiler or Python's headers the library is built all the same."""
+    import os
+    import sysconfig
+    from paper_2608_23843_b200 import build
+    assert build.CALL.endswith("_pkvcall" + sysconfig.get_config_var("EXT_SUFFIX")) and os.path.basename(build.CALL) != "_pkvcall.so"
+    call = str(tmp_path / os.path.basename(build.CALL))
+    monkeypatch.setattr(build, "CALL", call)
+    assert build.build_call() == call and os.path.exists(call)
+    for name, value in (("CC", "false"), ("CC", str(tmp_path / "no compiler"))):
+        monkeypatch.setenv(name, value)
+        with pytest.warns(UserWarning, match="ctypes"):
+            assert build.build_call(force=True) is None
+        assert not os.path.exists(call) and os.listdir(tmp_path) == []
+    monkeypatch.setattr(pkv, "_calls_module", None)
+    assert isinstance(pkv._calls(), pkv._CtypesCalls)
+    c, t, n, q = _dry()
+    assert c.attention(t, n, q, window=5, sinks=1).shape == q.shape and c.keep_rows(t, n, torch.zeros(3, 2, **INTS), n, 2).shape == (3,)
+    refused(lambda: c.keep_rows(t, n, torch.zeros(3, 2, **INTS), n, 2, out=n))
+    refused(lambda: c.keep_rows(t, n, torch.zeros(3, 2, **INTS), n, 2.0))
+
+
+def test_the_binding_is_passed_over_for_another_library(tmp_path, monkeypatch):
+    """(it would bring the one that it was linked with beside it)"""
+    import os
+    from paper_2608_23843_b200 import build
+    other = tmp_path / "libpkv.so"
+    os.symlink(build.LIB, other)
+    monkeypatch.setattr(pkv, "_calls_module", None)
+    monkeypatch.setattr(pkv, "LIB_PATH", str(other))
+    assert not isinstance(pkv._calls(), pkv._CtypesCalls)                  # the same file
+    other.unlink()
+    other.write_bytes(b"")
+    monkeypatch.setattr(pkv, "_calls_module", None)
+    assert isinstance(pkv._calls(), pkv._CtypesCalls)
+
+
+def test_calls_through_ctypes_check_their_numbers():
+    c, t, n, q = _dry()
+    h = c.handle.value
+    good = dict(append_kv=(h, 3, 0, 4, 0, 6, 0, 0, 256, 128, 0, 256, 128, 0), attention=(h, 3, 0, 4, 0, 6, 0, 2, 0, 0, 1024, 128, 0, 1024, 128, 0, 0, 0, 0),
+                attention_select=(h, 3, 0, 4, 0, 6, 0, 2, 0, 0, 1024, 128, 0, 1024, 128, 0, 0, 0, 0, 9, 4, None, 0),
+                tree_masks=(h, 3, None, 6, None, 2, 0, 0, 0, 0, 1, 0, 0), keep_rows=(h, 3, 0, 4, 0, 6, 0, 0, 2, 0, 0, 0), plan=(h, 3, 0, 4) + (0,) * 11 + (6,) + (0,) * 5)
+    good["read_kv"] = good["append_kv"]
+    assert sorted(good) == sorted(pkv._CALLS)
+    for name, args in good.items():
+        fn = getattr(pkv._CtypesCalls(), name)
+        assert fn(*args) == pkv.PKV_OK and fn(None, *args[1:]) == pkv.PKV_ERR_INVALID_ARG, name
+        for bad in (args[:-1], (h, 3.0, *args[2:]), (h, None, *args[2:])):
+            with pytest.raises(TypeError):
+                fn(*bad)
+        for wrong in (1 << 31, -(1 << 31) - 1, 1 << 64):
+            with pytest.raises(OverflowError):
+                fn(h, wrong, *args[2:])
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("n", [1, 5])
+def test_calls_through_ctypes_do_the_same(n, monkeypatch):
+    results = []
+    for through in (pkv._calls(), pkv._CtypesCalls()):
+        monkeypatch.setattr(pkv, "_calls_module", through)
+        f = Filled([300, 90, 700], seed=3)
+        ns = [n] * 3
+        q = torch.stack(f.queries(ns)).cuda()
+        parents = torch.tensor([[j - 1 - j % 2 for j in range(n)]] * 3, **INTS).cuda()
+        masks, depths = f.cache.tree_masks(parents, f.lengths, window=200, sinks=5)
+        got = [masks, depths, f.cache.attention(f.table, f.lengths, q), f.cache.attention(f.table, f.lengths, q, window=100, sinks=4),
+               f.cache.attention_partial(f.table, f.lengths, q, window=200, sinks=5, tree=masks)]
+        kept = f.cache.keep_rows(f.table, f.lengths, torch.tensor([[n - 1]] * 3, **INTS).cuda(), torch.ones(3, **INTS).cuda(), n)
+        got += [kept, *f.cache.read_kv(f.table, kept, *(torch.empty(3, 9, f.H, f.d, dtype=f.dtype, device="cuda") for _ in "kv"))]
+        spans = torch.stack([torch.zeros_like(kept), (kept + 63) // 64], 1).to(torch.int32)
+        ring, counters = f.cache.new_ring([0, 1, 2, 3])
+        got += [*f.cache.plan(f.table, kept, torch.ones_like(kept), spans, ring, counters, 3), f.table, ring]
+        results.append(got)
+        f.clean()
+    assert all(torch.equal(a, b) for a, b in zip(*results))
+
+
 # ---- refusals that must not depend on what was called before -------------------------------------------------------------
 @pytest.mark.parametrize("before", [False, True])
 @pytest.mark.parametrize("kw", [dict(), dict(window=5), dict(window=5, sinks=2)])
