@@ -7,7 +7,7 @@ import torch
 
 from paper_2608_23843_b200 import pkv
 from q4_select_reference import attention_seen, window_seen
-from test_q4_cache import BF16, FP16, INTS, Filled, check
+from test_q4_cache import BF16, FP16, INTS, Filled, check, config
 from test_q4_serve import _dry, offsets_of, seen_by
 
 LONGS = dict(dtype=torch.int64)
@@ -86,6 +86,23 @@ def test_masks_must_not_lie_on_what_is_read_or_written_with_them():
     call = lambda work: L.pkv_q4_attention_select(c.handle, 1, 0, 1000, 0, 64, 0, 64, 60000, ctypes.byref(sel), 0, 1024, 128, 0, 1024, 128, 0, work, room.value, 0)      # noqa: E731
     assert call((1 << 30) + 64 * 8) == call(0) == pkv.PKV_OK
     assert call((1 << 30) + 63 * 8) == call((1 << 30) - room.value + 8) == bad
+
+
+# ---- how many CTAs a call may take -----------------------------------------------------------------------------------------
+@pytest.mark.parametrize("n_ctas", [1, 2, 3, 7, 20, 148, 296, 1000, 65535])
+def test_a_call_takes_no_more_ctas_than_configured(n_ctas):
+    """Half as many of twice the size for sixteen rows, twice as many of half the size for short segments; a CTA per SM for row blocks."""
+    cache = pkv.Q4Cache(config(n_kv_heads=4, n_q_heads=16, n_ctas=n_ctas), dry_run=True)
+    kernels = set()
+    for S in (1, 3, 64, 700):
+        for n in (1, 2, 3, 4, 9, 70):
+            for T in (64, 1000, 30000):
+                for kw in (dict(), dict(window=40), dict(window=900, sinks=100), dict(tree=True, tree_words=2), dict(window=20000)):
+                    kernel, n_cta, cluster = pkv.pkv_q4_attention_route(cache.handle, S, n, T, **kw)
+                    most = {0: n_ctas if n * 4 <= 8 else max(1, n_ctas // 2), 1: 148, 2: 2 * n_ctas}[kernel]
+                    assert 1 <= n_cta <= most and n_cta % cluster == 0, (S, n, T, kw)
+                    kernels.add(kernel)
+    assert kernels >= {0, 1, 2} or n_ctas < 20
 
 
 # ---- numbers that are none -----------------------------------------------------------------------------------------------
