@@ -1249,8 +1249,9 @@ Q4Route q4_route(const Q4Geometry &g, int n_seqs, int max_q_len, int max_len, co
     const double units = (max_len + kQ4Unit - 1) / kQ4Unit, rows = (double)max_q_len * g.group, heads = (double)n_seqs * g.n_kv_heads;
     r.blocks = q4_by_blocks(g, n_seqs, max_q_len, max_len);
     if (part) {
-        // Estimates in us, fitted to 45 shapes (1 to 128 sequences, 1 to 64 new rows, windows of 256 to 16384 and whole contexts up to 64K, d = 128; the
-        // choice is within 2 % of the best of the three in all but one, 6 %):
+        // Estimates in us, fitted to 44 shapes (1 to 128 sequences, 1 to 64 new rows, windows of 256 to 16384 and whole contexts up to 64K, d = 128; the
+        // choice is within 3 % of the best of the three in all but one, 13 %.  At d = 64 the small CTAs' rounds and the even shares take some 60 to 70 % of this, which only the
+        // row blocks' term allows for: 32 of 39 shapes within 1 %, one 8, six 13 to 34 % too early away from the small CTAs):
         // small CTAs: rounds of a unit's chain, 1.5 us alone and 3.7 with all warps busy (one request, window of 4096: 13.5 against 17.0 us on the
         // column kernel's even shares; 64 requests, 1024: 31 against 62; 32 requests, 8192: 86.0 against 84.6; one, 16384: 25.6 against 19.2)
         const double segs = heads * std::ceil(rows / 8), slots = 2. * g.n_ctas;

@@ -47,7 +47,8 @@ constexpr int kBRowWarps = 8;
 // kPairs: where a call's blocks have 128 rows at most, and queries see a part of the positions, keys and values of a tile are widened by a warp
 // each: both halves then have the same rows and every other unit, and the widening is what takes longest (8 x 16 drafted tokens against 16000: 162 ->
 // 140 us; with rows of their own for both halves the row threads need the issue slots: 8 x 64 against 32K 356 -> 370).  The 18 warps take
-// registers by their needs, in whole groups of four warps (two idle ones make up the last): they start with 96 a thread.
+// registers in the shares below, in whole groups of four warps (two idle ones make up the last): they start with 96 a thread.  The shares do not
+// hold everything: 500 to 580 bytes of a thread's values are spilled and 690 to 740 loaded again, against 200 to 230 and 360 to 370 without kPairs (128 registers a thread).
 __host__ __device__ constexpr int block_widen_warps(bool pairs) { return pairs ? 2 * kQ4UnitTiles : kQ4UnitTiles; }
 __host__ __device__ constexpr int block_threads(bool pairs) { return 32 * (kBRowWarps + block_widen_warps(pairs) + (pairs ? 4 : 2)); }
 constexpr int kBRegs = 96, kBRowRegs = 144, kBWidenRegs = 64, kBOtherRegs = 64;

@@ -152,9 +152,11 @@ __global__ void __launch_bounds__(kKeepThreads) q4_keep_kernel(const __grid_cons
 // ---- planning a step ------------------------------------------------------------------------------------------------------
 // Prefix sums over the requests - new rows, pages taken, pages given back - from which every row, taken page and returned page follows
 // by itself: a thread each, which finds its request by bisection in the sums.  Up to kPlanHeld requests the sums fit shared memory,
-// and a CTA, or a cluster of eight that all work them out, fills everything in (64 requests: 4.6 us, all latency: launch, counters and lengths, the scan,
+// and up to kPlanFew rows (of the caller's bound) a CTA, or a cluster of eight that all work them out, fills everything in (64 requests: 4.6 us, all latency: launch, counters and lengths, the scan,
 // pages, results; 700 requests with chunks of prompts 7.5 us, and one kernel for the sums and one for the rest 10.6 and a launch more).  More requests
-// leave the sums in the workspace to a second kernel over the SMs.  Entries that are read (below `end`) and written (from it on), and
+// or rows leave the sums in the workspace to a second kernel over the SMs.  The launch goes by requests and rows, which is what most steps are
+// made of; pages that go back are the threads' work too, but the host does not know their number, so a step in which many long requests are done takes longer
+// (64 of 32K on pages of 16, 131072 pages: 85.6 us by one CTA, 14.5 where the bound of the rows brings the cluster; 777 of 11000, 534576 pages: 445).  Entries that are read (below `end`) and written (from it on), and
 // places of the ring that are read (from the head) and written (from the tail), are different ones, so the order does not matter.
 constexpr int kPlanThreads = 1024, kPlanFillThreads = 256, kPlanCluster = 8;
 constexpr int kPlanHeld = 1024;                  // a thread each
