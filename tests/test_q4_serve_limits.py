@@ -240,6 +240,47 @@ def test_calls_through_ctypes_do_the_same(n, monkeypatch):
     assert all(torch.equal(a, b) for a, b in zip(*results))
 
 
+@pytest.mark.gpu
+def test_the_functions_of_the_binding_do_what_the_cache_does():
+    f = Filled([300, 90, 700], seed=4)
+    c, n, S, W, sinks = f.cache, 5, 3, 100, 4
+    h, (_, max_pages) = c.handle, f.table.shape
+    q = torch.stack(f.queries([n] * S)).cuda()
+    parents = torch.tensor([[-1, 0, 0, 1, 3]] * S, **INTS).cuda()
+    masks, depths = c.tree_masks(parents, f.lengths, window=W, sinks=sinks)
+    masks2, depths2 = torch.empty_like(masks), torch.empty_like(depths)
+    pkv.pkv_q4_tree_masks(h, S, f.lengths, S * n, None, n, parents, W, sinks, masks2, 1, depths2)
+    assert torch.equal(masks, masks2) and torch.equal(depths, depths2)
+    size = pkv.pkv_q4_attention_select_workspace(h, S, n, max_pages * 64, W, sinks, masks, 1)
+    work = torch.empty(max(size, 16), dtype=torch.uint8, device="cuda")
+    strides, out = (q.stride(1), q.stride(2)), torch.empty_like(q)
+    pkv.pkv_q4_attention_select(h, S, f.table, max_pages, f.lengths, S * n, None, n, max_pages * 64, W, sinks, masks, 1, q, strides, out, strides, None, work, size)
+    assert torch.equal(out, c.attention(f.table, f.lengths, q, window=W, sinks=sinks, tree=masks))
+    paths, counts = torch.tensor([[0, 1, 3]] * S, **INTS).cuda(), torch.tensor([3, 1, 0], **INTS).cuda()
+    pool, kept = c.pool.clone(), torch.empty_like(f.lengths)
+    pkv.pkv_q4_keep_rows(h, S, f.table, max_pages, f.lengths, S * n, None, paths, 3, counts, kept)
+    moved = c.pool.clone()
+    c.pool.copy_(pool)
+    kept2 = c.keep_rows(f.table, f.lengths, paths, counts, n)
+    assert torch.equal(kept, kept2) and torch.equal(moved, c.pool) and kept.tolist() == [298, 86, 695]
+    for last in (30, 5):                                   # 695 + 30 rows are more than the table takes: nothing is done
+        results = []
+        for by_hand in (True, False):
+            table, (ring, counters) = f.table.clone(), c.new_ring([1, 0, 2, 3])
+            spans = torch.stack([torch.zeros_like(kept), (kept + 63) // 64], 1).to(torch.int32)
+            rows = torch.tensor([1, -1, last], **INTS).cuda()
+            p = pkv.Q4Plan(*(torch.full_like(x, 7) for x in (kept, torch.empty(S + 1, **INTS).cuda(), torch.empty(31, **INTS).cuda(), torch.empty(31, **LONGS).cuda(), spans, counters)))
+            if by_hand:
+                assert pkv.pkv_q4_plan_workspace(h, S, 31) == 0
+                pkv.pkv_q4_plan(h, S, table, max_pages, kept, rows, spans, ring, counters, W, sinks, p.lengths, p.spans, p.counters, p.offsets, 31, p.positions, p.slots, None, 0)
+            else:
+                assert c.plan(table, kept, rows, spans, ring, counters, 31, window=W, sinks=sinks, out=p) is p
+            results.append([*p, table, ring])
+        assert all(torch.equal(a, b) for a, b in zip(*results))
+        assert p.counters[3] == (last == 30) and p.lengths.tolist() == ([299, 0, 700] if last == 5 else kept.tolist())
+    f.clean()
+
+
 # ---- refusals that must not depend on what was called before -------------------------------------------------------------
 @pytest.mark.parametrize("before", [False, True])
 @pytest.mark.parametrize("kw", [dict(), dict(window=5), dict(window=5, sinks=2)])
