@@ -446,7 +446,7 @@ pkv_status q4_apart(pkv_q4_cache *c, const char *what, const Q4Array *x, int n_w
     for (int i = 0; i < n_written; ++i)
         for (int k = i + 1; k < n; ++k) {
             const uintptr_t a = (uintptr_t)x[i].at, b = (uintptr_t)x[k].at;
-            if (a && b && a < b + x[k].bytes && b < a + x[i].bytes) return q4_fail(c, PKV_ERR_INVALID_ARG, "%s: %s overlaps %s", what, x[i].name, x[k].name);
+            if (a && b && x[i].bytes > 0 && x[k].bytes > 0 && a < b + x[k].bytes && b < a + x[i].bytes) return q4_fail(c, PKV_ERR_INVALID_ARG, "%s: %s overlaps %s", what, x[i].name, x[k].name);
         }
     return PKV_OK;
 }
@@ -491,9 +491,10 @@ pkv_status q4_attend(pkv_q4_cache *c, const char *what, int32_t n_seqs, const in
     if (!c->dry && need > 0 && (!workspace || workspace_bytes < need || ((uintptr_t)workspace & 15)))
         return q4_fail(c, PKV_ERR_INVALID_ARG, "%s: the workspace needs %lld bytes, 16-byte aligned", what, need);
     if (select && select->tree) {                      // (read by all KV heads, while the first of them write)
-        const long long heads = (long long)n_rows * g.n_q_heads;
+        // (strided results may have anything between their rows)
+        const long long heads = (long long)n_rows * g.n_q_heads, span = (n_rows - 1) * out_row_stride + (g.n_q_heads - 1) * out_head_stride + g.head_dim;
         const Q4Array arrays[] = {{"tree", select->tree, 8LL * n_rows * select->tree_words}, {"state", state, heads * (g.head_dim + 2) * 4}, {"workspace", need > 0 ? workspace : nullptr, need},
-                                  {"out", out, 2 * ((n_rows - 1) * out_row_stride + (g.n_q_heads - 1) * out_head_stride + g.head_dim)}};
+                                  {"out", out, span == heads * g.head_dim ? 2 * span : 0}};
         if (pkv_status st = q4_apart(c, what, arrays, 1, 4)) return st;
     }
     if (c->dry) return PKV_OK;

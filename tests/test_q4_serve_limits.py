@@ -294,6 +294,20 @@ def test_masks_without_words_are_refused_whatever_was_called_before(before, kw):
         assert "tree" in refused(lambda: call(t, n, q[:, :0], tree=torch.zeros(3, 0, 0, **LONGS), **kw))
 
 
+def test_empty_arrays_and_gaps_overlap_nothing():
+    c, t, n, q = _dry()
+    L, h = pkv.lib(), c.handle
+    assert L.pkv_q4_keep_rows(h, 3, 0, 4, 0, 6, 0, 260, 0, 0, 256, 0) == pkv.PKV_OK                            # no paths
+    assert L.pkv_q4_tree_masks(h, 3, 0, 0, 260, 0, 264, 0, 0, 256, 1, 264, 0) == pkv.PKV_OK                    # no rows
+    plan = [h, 3, 256, 4, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 260, 264, 0, 0, 0]
+    assert L.pkv_q4_plan(*plan) == pkv.PKV_OK
+    plan[15] = 1
+    assert L.pkv_q4_plan(*plan) == pkv.PKV_ERR_INVALID_ARG
+    row = torch.zeros(1, 1, 8, 136, dtype=BF16)             # masks beside a head's channels
+    masks = row.flatten()[128:132].view(torch.int64).view(1, 1, 1)
+    assert c.attention(t[:1], n[:1], q[:1, :1], out=row[..., :128], tree=masks).shape == (1, 1, 8, 128)
+
+
 # ---- clusters whose joins leave a warp in part ---------------------------------------------------------------------------
 # A segment's states are rows * d / 4 pieces for 96 threads, and rows * d / 4 / cluster for each CTA of a cluster: these end inside a warp.
 @pytest.mark.gpu
