@@ -200,7 +200,7 @@ def _calls():
     if _calls_module is None:
         from . import build
         lib()                                            # (says what to do where nothing has been built)
-        built = os.path.exists(build.CALL) and os.path.samefile(LIB_PATH, build.LIB)
+        built = os.path.exists(build.CALL) and os.path.exists(build.LIB) and os.path.samefile(LIB_PATH, build.LIB)
         if built:
             from . import _pkvcall
         _calls_module = _pkvcall if built else _CtypesCalls()

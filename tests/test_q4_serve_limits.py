@@ -196,6 +196,9 @@ def test_the_binding_is_passed_over_for_another_library(tmp_path, monkeypatch):
     other.write_bytes(b"")
     monkeypatch.setattr(pkv, "_calls_module", None)
     assert isinstance(pkv._calls(), pkv._CtypesCalls)
+    monkeypatch.setattr(build, "LIB", str(tmp_path / "none"))              # no library in the tree
+    monkeypatch.setattr(pkv, "_calls_module", None)
+    assert isinstance(pkv._calls(), pkv._CtypesCalls)
 
 
 def test_calls_through_ctypes_check_their_numbers():
